@@ -427,6 +427,61 @@ int surelock_attention_split(const void *q, const void *k_cache, const void *v_c
                              int max_rows, int B, int N, int H, int head_dim, int splits, void *o, void *workspace,
                              int diag_skip, int32_t *dev_status, void *stream);
 
+/* ---- paged K/V cache, in bf16 or quantised to 8 bits ------------------------------------------------------------
+ * The same cache (Algorithm 1 line 11) for callers that keep many sequences of different lengths: a pool of pages of
+ * page_size tokens, and per sequence a table of the pages its tokens lie on (token i of sequence b: place i % page_size
+ * of page page_table[b][i / page_size]).  A page may be in the tables of several sequences that only read it.
+ *   k, v              dev [n_pages][n_kv_heads][page_size][head_dim] of `dtype`: SL_BF16, SL_E4M3 or SL_INT8 codes
+ *   k_scale, v_scale  dev fp32 [n_pages][n_kv_heads][page_size], one scale per (token, head): value = code * scale.
+ *                     Not negative.  NULL with SL_BF16
+ *   page_table        dev int32 [n_seq][max_pages]; entries behind a sequence's last token are not read
+ * page_size 16, 32, 64, 128 or 256, head_dim 64 or 128 (SL_EUNSUPPORTED otherwise, also for pointers that are not 16-byte
+ * aligned).  A page number outside 0 ... n_pages - 1 that a call meets stores device status 4 in its dev_status. */
+enum { SL_E4M3 = 2, SL_INT8 = 3 };     /* element types of a paged cache, beside SL_BF16 */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  const int32_t *page_table;
+  int32_t n_pages, page_size, max_pages, n_kv_heads, head_dim, dtype;
+} surelock_paged_kv;
+
+/* Cache scatter into pages (the counterpart of surelock_kv_scatter), quantising on the way: packed row r of k and v goes to
+ * flat position active_idx[r] = b*N + i (b < B) for r < *n_active.  Per (row, head): scale = fp32(max |x| / 448) for
+ * SL_E4M3, / 127 for SL_INT8, code = x / scale rounded once to nearest even; an all-zero head gets scale 0, one with an
+ * infinity or NaN gets scale NaN.  k, v: dev, row r at r * row_stride elements, heads packed [n_kv_heads][head_dim], of
+ * `dtype` SL_BF16 or SL_FP32; row_stride * sizeof(elem) a multiple of 16, so they may be parts of wider rows.  The positions
+ * are distinct, and two of them do not share a page place through equal table entries (the values left there would be a
+ * mixture).  A position outside the tables, or on a bad page, is skipped (device status 4).  Nothing else is touched.
+ * dev_status may be NULL.  Asynchronous on `stream`; may be captured into a graph. */
+int surelock_kv_scatter_paged(const surelock_paged_kv *cache, const void *k, const void *v, int64_t row_stride,
+                              const int32_t *active_idx, const int32_t *n_active, int max_rows, int B, int N, int dtype,
+                              int32_t *dev_status, void *stream);
+
+/* The way back: packed rows r < *n_active of k and v (layout as above, row_stride too, `dtype` SL_BF16 or SL_FP32) receive
+ * code * scale of positions active_idx[r]; any order, repeats allowed.  A bad position gives a row of zeros and device
+ * status 4.  For instance to fill a contiguous cache (surelock_kv_cache) or to move sequences between pools. */
+int surelock_kv_gather_paged(const surelock_paged_kv *cache, const int32_t *active_idx, const int32_t *n_active, int max_rows,
+                             int B, int N, void *k, void *v, int64_t row_stride, int dtype, int32_t *dev_status, void *stream);
+
+/* Attention of the packed queries against a paged cache (Algorithm 1 line 12; with one row per sequence, the attention of a
+ * new token): for packed row r of sequence b, row_offsets[b] <= r < row_offsets[b + 1], and every head h of H,
+ *   o[r][h] = softmax_j(q[r][h] . K_j[h'] / sqrt(d_h)) V_j[h'],  0 <= j < seq_lens[b],  h' = h / (H / n_kv_heads)
+ * over the sequence's cached tokens; no mask besides the length.  seq_lens[b] = 0 gives rows of zeros.
+ *   q, o         dev bf16, row r at r * q_stride / o_stride elements (multiples of 8), heads packed [H][head_dim]
+ *   row_offsets  dev int32 [B + 1], seq_lens dev int32 [B] (0 ... max_pages * page_size); a value out of range is clamped to
+ *                it and stores device status 4; rows behind row_offsets[B] are left as they are
+ *   workspace    dev, surelock_attention_paged_workspace_bytes(head_dim) bytes, any contents, 16-byte aligned; holds partial
+ *                results during the call only, so calls (and captured graphs) that may run at the same time need one each
+ * H a multiple of n_kv_heads, B <= 1024.  The keys are split over the whole GPU whatever the sequences' lengths are, and the
+ * parts are joined in a fixed order: results do not change from run to run.  Made for few rows per sequence (1 ... 128 /
+ * (H / n_kv_heads)); more rows are correct but re-read the cache per 16 or 32 (row, head) pairs.  A bad page reads as
+ * zeros (K = V = 0).  Scores, maxima, sums and outputs are accumulated in fp32; the weights enter the last product with 11
+ * (SL_BF16 cache: 8) bits.  dev_status may be NULL; 3 = a bounded wait ran out.  Asynchronous on `stream`. */
+size_t surelock_attention_paged_workspace_bytes(int head_dim);
+int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int64_t q_stride, const int32_t *row_offsets,
+                             const int32_t *seq_lens, int max_rows, int B, int H, void *o, int64_t o_stride, void *workspace,
+                             int32_t *dev_status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

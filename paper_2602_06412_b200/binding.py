@@ -15,7 +15,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsurelock.so")
-SL_BF16, SL_FP32 = 0, 1
+SL_BF16, SL_FP32, SL_E4M3, SL_INT8 = 0, 1, 2, 3
 _lib = None
 
 
@@ -49,6 +49,11 @@ class _ProbeOut(C.Structure):
     _fields_ = [("step", C.c_int32), ("probed", C.c_int32)] + \
                [(n, C.c_void_p) for n in ("probed_idx", "n_probed", "drift", "conf", "theta", "n_unlocked", "t_star",
                                           "cool_until")]
+
+
+class _PagedKV(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim", "dtype")]
 
 
 def lib() -> C.CDLL:
@@ -98,6 +103,10 @@ def lib() -> C.CDLL:
         "surelock_gemm": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]),
         "surelock_gemm_workspace_bytes": (sz, []),
         "surelock_gemm_fused": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
+        "surelock_kv_scatter_paged": (i32, [C.POINTER(_PagedKV), vp, vp, C.c_int64, vp, vp, i32, i32, i32, i32, vp, vp]),
+        "surelock_kv_gather_paged": (i32, [C.POINTER(_PagedKV), vp, vp, i32, i32, i32, vp, vp, C.c_int64, i32, vp, vp]),
+        "surelock_attention_paged_workspace_bytes": (sz, [i32]),
+        "surelock_attention_paged": (i32, [C.POINTER(_PagedKV), vp, C.c_int64, vp, vp, i32, i32, i32, vp, C.c_int64, vp, vp, vp]),
         "surelock_attention": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i32, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -429,3 +438,82 @@ def surelock_attention(q, k_cache, v_cache, active_idx, row_offsets, n_active, B
     _check(lib().surelock_attention(_p(q), _p(k_cache), _p(v_cache), _p(active_idx), _p(row_offsets), _p(n_active),
                                     q.shape[0], B, N, H, dh, _p(o), _dt(q), impl, _p(dev_status), _stream()),
            "surelock_attention")
+
+
+# ---- paged K/V cache ---------------------------------------------------------------------------------------
+_PAGED_DT = {torch.bfloat16: SL_BF16, torch.float8_e4m3fn: SL_E4M3, torch.int8: SL_INT8}
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise SurelockError(what)
+
+
+def _rows(t: torch.Tensor, heads: int, dh: int, what: str) -> int:
+    """Row stride, in elements, of a tensor [rows][heads][dh] whose rows are packed (they may lie apart)."""
+    _want(t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dh, f"{what}: a CUDA tensor [rows][{heads}][{dh}] is wanted")
+    st = t.stride()
+    _want(st[2] == 1 and (st[1] == dh or heads == 1), f"{what}: the heads of a row must be packed")
+    return st[0] if t.shape[0] > 1 else max(st[0], heads * dh)
+
+
+def _ints(t: torch.Tensor, least: int, what: str):
+    _want(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= least,
+          f"{what}: a contiguous int32 CUDA tensor of at least {least} entries is wanted")
+    return t.data_ptr()
+
+
+class PagedKV:
+    """A paged K/V cache: pools k, v [n_pages][n_kv_heads][page_size][head_dim] (bfloat16, float8_e4m3fn or int8), page_table
+    int32 [n_seq][max_pages], and for the 8-bit types fp32 scales [n_pages][n_kv_heads][page_size].  Keeps the tensors alive."""
+
+    def __init__(self, k, v, page_table, k_scale=None, v_scale=None):
+        _want(k.dtype in _PAGED_DT, f"unsupported cache dtype {k.dtype}")
+        _want(k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype, "k and v pools must be alike, [n_pages][n_kv_heads][page_size][head_dim]")
+        _want(page_table.dtype == torch.int32 and page_table.dim() == 2, "page_table: int32 [n_seq][max_pages]")
+        quantised = k.dtype != torch.bfloat16
+        for s in (k_scale, v_scale):
+            _want((s is not None) == quantised, "scales go with the 8-bit types")
+            _want(s is None or (s.dtype == torch.float32 and s.shape == k.shape[:3]), "scales: fp32 [n_pages][n_kv_heads][page_size]")
+        tensors = [t for t in (k, v, page_table, k_scale, v_scale) if t is not None]
+        _want(all(t.is_cuda and t.device == k.device and t.is_contiguous() for t in tensors), "pools, scales and table: contiguous, on one CUDA device")
+        self._keep = tensors
+        self.n_seq, self.n_kv_heads, self.head_dim = page_table.shape[0], k.shape[1], k.shape[3]
+        self.raw = _PagedKV(k.data_ptr(), v.data_ptr(), _p(k_scale), _p(v_scale), page_table.data_ptr(), k.shape[0], k.shape[2],
+                            page_table.shape[1], k.shape[1], k.shape[3], _PAGED_DT[k.dtype])
+        self.ref = C.byref(self.raw)
+
+
+def surelock_kv_scatter_paged(cache: PagedKV, k, v, active_idx, n_active, N: int, dev_status=None):
+    """Rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32; rows may lie apart) into the pages, quantised on the way."""
+    stride = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
+    _want(_rows(v, cache.n_kv_heads, cache.head_dim, "v") == stride and v.shape == k.shape and v.dtype == k.dtype, "k and v must be laid out alike")
+    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), stride, _ints(active_idx, k.shape[0], "active_idx"),
+                                           _p(n_active), k.shape[0], cache.n_seq, N, _dt(k), _p(dev_status), _stream()),
+           "surelock_kv_scatter_paged")
+
+
+def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v, dev_status=None):
+    """Positions active_idx back into the rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32)."""
+    stride = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
+    _want(_rows(v, cache.n_kv_heads, cache.head_dim, "v") == stride and v.shape == k.shape and v.dtype == k.dtype, "k and v must be laid out alike")
+    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0], "active_idx"), _p(n_active), k.shape[0], cache.n_seq,
+                                          N, k.data_ptr(), v.data_ptr(), stride, _dt(k), _p(dev_status), _stream()),
+           "surelock_kv_gather_paged")
+
+
+def surelock_attention_paged_workspace_bytes(head_dim: int) -> int:
+    return lib().surelock_attention_paged_workspace_bytes(head_dim)
+
+
+def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, workspace, dev_status=None):
+    """q, o: bf16 [M][H][head_dim] (rows may lie apart); row_offsets int32 [B+1], seq_lens int32 [B]; workspace: uint8 tensor of
+    surelock_attention_paged_workspace_bytes(head_dim) bytes, one per call that may run at the same time."""
+    _want(q.dim() == 3 and o.shape == q.shape and q.dtype == torch.bfloat16 and o.dtype == torch.bfloat16, "q, o: bf16 [M][H][head_dim], alike")
+    H, B = q.shape[1], seq_lens.numel()
+    _want(B <= cache.n_seq, "more sequences than the page table has")
+    _want(workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= surelock_attention_paged_workspace_bytes(cache.head_dim),
+          "workspace too small")
+    _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, cache.head_dim, "q"), _ints(row_offsets, B + 1, "row_offsets"),
+                                          _ints(seq_lens, B, "seq_lens"), q.shape[0], B, H, o.data_ptr(), _rows(o, H, cache.head_dim, "o"),
+                                          workspace.data_ptr(), _p(dev_status), _stream()), "surelock_attention_paged")

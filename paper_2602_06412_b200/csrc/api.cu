@@ -7,6 +7,7 @@
 #include <new>
 #include <vector>
 
+#include "paged_kv.cuh"
 #include "tc_common.cuh"
 
 using namespace sl;
@@ -1072,6 +1073,49 @@ int surelock_attention(const void* q, const void* k_cache, const void* v_cache, 
   }
   return launch_attention_simt(q, k_cache, v_cache, active_idx, n_active, max_rows, N, H, head_dim, o, dtype,
                                (cudaStream_t)stream);
+}
+
+static int paged_rows_check(const surelock_paged_kv* cache, const void* k, const void* v, int64_t row_stride,
+                            const int32_t* active_idx, const int32_t* n_active, int max_rows, int B, int N, int dtype) {
+  if (!k || !v || !active_idx || !n_active || max_rows < 0 || B <= 0 || N <= 0) return SL_EINVAL;
+  if (dtype != SL_BF16 && dtype != SL_FP32) return SL_EINVAL;
+  const int rc = check_paged_kv(cache);
+  if (rc != SL_OK) return rc;
+  if (row_stride < (int64_t)cache->n_kv_heads * cache->head_dim) return SL_EINVAL;
+  if (((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15) || row_stride % (dtype == SL_BF16 ? 8 : 4))
+    return SL_EUNSUPPORTED;
+  return SL_OK;
+}
+
+int surelock_kv_scatter_paged(const surelock_paged_kv* cache, const void* k, const void* v, int64_t row_stride,
+                              const int32_t* active_idx, const int32_t* n_active, int max_rows, int B, int N, int dtype,
+                              int32_t* dev_status, void* stream) {
+  const int rc = paged_rows_check(cache, k, v, row_stride, active_idx, n_active, max_rows, B, N, dtype);
+  if (rc != SL_OK) return rc;
+  return launch_kv_scatter_paged(*cache, k, v, row_stride, active_idx, n_active, max_rows, B, N, dtype, dev_status,
+                                 (cudaStream_t)stream);
+}
+
+int surelock_kv_gather_paged(const surelock_paged_kv* cache, const int32_t* active_idx, const int32_t* n_active, int max_rows,
+                             int B, int N, void* k, void* v, int64_t row_stride, int dtype, int32_t* dev_status, void* stream) {
+  const int rc = paged_rows_check(cache, k, v, row_stride, active_idx, n_active, max_rows, B, N, dtype);
+  if (rc != SL_OK) return rc;
+  return launch_kv_gather_paged(*cache, active_idx, n_active, max_rows, B, N, k, v, row_stride, dtype, dev_status,
+                                (cudaStream_t)stream);
+}
+
+size_t surelock_attention_paged_workspace_bytes(int head_dim) { return attention_paged_workspace_bytes(head_dim); }
+
+int surelock_attention_paged(const surelock_paged_kv* cache, const void* q, int64_t q_stride, const int32_t* row_offsets,
+                             const int32_t* seq_lens, int max_rows, int B, int H, void* o, int64_t o_stride, void* workspace,
+                             int32_t* dev_status, void* stream) {
+  if (!q || !row_offsets || !seq_lens || !o || !workspace || max_rows < 0 || B <= 0 || H <= 0) return SL_EINVAL;
+  const int rc = check_paged_kv(cache);
+  if (rc != SL_OK) return rc;
+  if (H % cache->n_kv_heads || q_stride < (int64_t)H * cache->head_dim || o_stride < (int64_t)H * cache->head_dim) return SL_EINVAL;
+  if (max_rows == 0) return SL_OK;
+  return launch_attention_paged(*cache, q, q_stride, row_offsets, seq_lens, max_rows, B, H, o, o_stride, workspace, dev_status,
+                                (cudaStream_t)stream);
 }
 
 }  // extern "C"

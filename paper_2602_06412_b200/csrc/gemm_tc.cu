@@ -901,12 +901,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 }
 
 // ----------------------------------------------------------------------------------------------- host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
+TensorMapEncodeFn tensor_map_encode_fn() {
+  static TensorMapEncodeFn fn = nullptr;
   static bool tried = false;
   if (!tried) {
     tried = true;
@@ -914,7 +910,7 @@ static EncodeTiledFn encode_fn() {
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
         qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
+      fn = reinterpret_cast<TensorMapEncodeFn>(p);
   }
   return fn;
 }
@@ -943,7 +939,7 @@ int get_tensor_map_2d(const void* ptr, long long rows, long long cols, int box_r
     *out = it->second;
     return SL_OK;
   }
-  EncodeTiledFn fn = encode_fn();
+  TensorMapEncodeFn fn = tensor_map_encode_fn();
   if (!fn) return SL_ECUDA;
   CUtensorMap m;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};

@@ -248,6 +248,12 @@ struct SplitWs {
 };
 constexpr size_t SPLIT_TILE_BYTES = 128 * 256 * sizeof(float);
 
+// the driver's cuTensorMapEncodeTiled, nullptr when it cannot be had
+typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+TensorMapEncodeFn tensor_map_encode_fn();
+
 // 2-D bf16 row-major [rows][cols] tensor map, box = box_rows x 64 elements, 128-byte swizzle, zero fill out of
 // bounds.  Maps are cached per (pointer, shape).  Returns SL_OK / SL_ECUDA.
 int get_tensor_map_2d(const void* ptr, long long rows, long long cols, int box_rows, CUtensorMap* out);
