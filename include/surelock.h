@@ -402,6 +402,26 @@ int surelock_gemm_fused(const void *A, const void *W, const void *W2, void *C, c
                         int n_out, int K, int dtype, int epilogue, int impl, void *workspace, int32_t *dev_status,
                         void *stream);
 
+/* Weights held in four bits, for surelock_gemm_quantized:  W[n][k] = (code[n][k] - zero[n][k / group]) * scale[n][k / group].
+ *   codes   dev uint8 [n_out][K / 2]: byte j of a row holds k = 2j in its low and k = 2j + 1 in its high four bits
+ *   scales  dev [n_out][K / group] of scale_dtype (SL_BF16 or SL_FP32)
+ *   zeros   dev uint8 [n_out][K / group], values 0 ... 127, or NULL: then the zero point is 8 everywhere
+ *   group   32, 64 or 128, a divisor of K */
+typedef struct {
+  const void *codes, *scales, *zeros;
+  int32_t group, scale_dtype;
+} surelock_w4;
+
+/* surelock_gemm_fused with 4-bit weights, for few rows: C[r][n] = sum_k A[r][k] W[n][k] for r < *n_active, A dev bf16 [M][K],
+ * epilogue 0: C bf16 [M][n_out]; 1: C is the fp32 residual stream, C[r][n] += sum; 2: C bf16 = silu(A W^T) * (A W2^T), W2 of
+ * the same group, scale type and kind of zero point as W (W2 is ignored otherwise).  The codes enter the products exactly,
+ * group sums are fp32 and are multiplied by their scale in fp32.  Any n_out; K a multiple of the group.  A pass over the
+ * weights serves 64 rows; more rows take further passes.  Rows >= *n_active of C are not touched.  Deterministic; needs no
+ * workspace.  SL_EINVAL on NULL pointers, a group that does not divide K, an unknown epilogue, a missing or different W2;
+ * SL_EUNSUPPORTED for another group or for codes or A that are not 16-byte aligned.  Asynchronous on `stream`. */
+int surelock_gemm_quantized(const void *A, const surelock_w4 *W, const surelock_w4 *W2, void *C, const int32_t *n_active,
+                            int max_rows, int n_out, int K, int epilogue, void *stream);
+
 /* M x N bidirectional attention of the packed queries against the whole cache (Algorithm 1 line 12; Sec. 2.1: the
  * packed active queries attend to all N cached keys and values of their sequence): for packed row r at flat position
  * active_idx[r] = b*N+i and every head h, o[r][h] = softmax_j(q[r][h] . K[b*N+j][h] / sqrt(d_h)) V[b*N+j][h],

@@ -51,6 +51,10 @@ class _ProbeOut(C.Structure):
                                           "cool_until")]
 
 
+class _W4(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales", "zeros")] + [("group", C.c_int32), ("scale_dtype", C.c_int32)]
+
+
 class _PagedKV(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim", "dtype")]
@@ -103,6 +107,7 @@ def lib() -> C.CDLL:
         "surelock_gemm": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]),
         "surelock_gemm_workspace_bytes": (sz, []),
         "surelock_gemm_fused": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
+        "surelock_gemm_quantized": (i32, [vp, C.POINTER(_W4), C.POINTER(_W4), vp, vp, i32, i32, i32, i32, vp]),
         "surelock_kv_scatter_paged": (i32, [C.POINTER(_PagedKV), vp, vp, C.c_int64, vp, vp, i32, i32, i32, i32, vp, vp]),
         "surelock_kv_gather_paged": (i32, [C.POINTER(_PagedKV), vp, vp, i32, i32, i32, vp, vp, C.c_int64, i32, vp, vp]),
         "surelock_attention_paged_workspace_bytes": (sz, [i32]),
@@ -438,6 +443,30 @@ def surelock_attention(q, k_cache, v_cache, active_idx, row_offsets, n_active, B
     _check(lib().surelock_attention(_p(q), _p(k_cache), _p(v_cache), _p(active_idx), _p(row_offsets), _p(n_active),
                                     q.shape[0], B, N, H, dh, _p(o), _dt(q), impl, _p(dev_status), _stream()),
            "surelock_attention")
+
+
+# ---- 4-bit weights ------------------------------------------------------------------------------------------
+def _w4(W, K: int):
+    """The C struct of (codes uint8 [n_out][K/2], scales bf16 or fp32 [n_out][K/group], zeros uint8 [n_out][K/group] or None)."""
+    codes, scales, zeros = W
+    n, ng = scales.shape
+    if codes.dtype != torch.uint8 or tuple(codes.shape) != (n, K // 2) or not ng or K % ng or \
+            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != scales.shape)):
+        raise SurelockError("4-bit weights: codes uint8 [n_out][K/2], scales [n_out][K/group], zeros uint8 like scales or None")
+    return _W4(_p(codes), _p(scales), _p(zeros), K // ng, _dt(scales))
+
+
+def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None):
+    """4-bit weights W = (codes, scales, zeros or None); epilogue 0: Cout (bf16) = A W^T; 1: Cout (fp32) += A W^T;
+    2: Cout (bf16) = silu(A W^T) * (A W2^T)."""
+    M, K = A.shape
+    n = W[0].shape[0]
+    if A.dtype != torch.bfloat16 or Cout.dtype != (torch.float32 if epilogue == 1 else torch.bfloat16) or tuple(Cout.shape) != (M, n):
+        raise SurelockError("surelock_gemm_quantized: A bf16 [M][K], Cout [M][n_out] (fp32 with epilogue 1, else bf16)")
+    if W2 is not None and W2[0].shape[0] != n:
+        raise SurelockError("surelock_gemm_quantized: W and W2 must have the same features")
+    _check(lib().surelock_gemm_quantized(_p(A), C.byref(_w4(W, K)), C.byref(_w4(W2, K)) if W2 is not None else None, _p(Cout),
+                                         _p(n_active), M, n, K, epilogue, _stream()), "surelock_gemm_quantized")
 
 
 # ---- paged K/V cache ---------------------------------------------------------------------------------------

@@ -1029,6 +1029,29 @@ int surelock_gemm_fused(const void* A, const void* W, const void* W2, void* C, c
   return launch_gemm_simt(A, W, W2, C, n_active, max_rows, n_out, K, dtype, epilogue, (cudaStream_t)stream);
 }
 
+static int w4_check(const surelock_w4* W, int K) {
+  if (!W || !W->codes || !W->scales || W->group <= 0 || K % W->group) return SL_EINVAL;
+  if (W->scale_dtype != SL_BF16 && W->scale_dtype != SL_FP32) return SL_EINVAL;
+  if (W->group != 32 && W->group != 64 && W->group != 128) return SL_EUNSUPPORTED;
+  return (reinterpret_cast<uintptr_t>(W->codes) & 15) ? SL_EUNSUPPORTED : SL_OK;
+}
+
+int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active,
+                            int max_rows, int n_out, int K, int epilogue, void* stream) {
+  if (!A || !C || !n_active || max_rows < 0 || n_out <= 0 || K <= 0) return SL_EINVAL;
+  if (epilogue != EPI_STORE && epilogue != EPI_RESIDUAL && epilogue != EPI_SWIGLU) return SL_EINVAL;
+  int rc = w4_check(W, K);
+  if (rc == SL_OK && epilogue == EPI_SWIGLU) {
+    rc = w4_check(W2, K);
+    if (rc == SL_OK && (W2->group != W->group || W2->scale_dtype != W->scale_dtype || !W2->zeros != !W->zeros)) rc = SL_EINVAL;
+  }
+  if (rc != SL_OK) return rc;
+  if (reinterpret_cast<uintptr_t>(A) & 15) return SL_EUNSUPPORTED;
+  if (max_rows == 0) return SL_OK;
+  return launch_gemm_quantized(A, W, epilogue == EPI_SWIGLU ? W2 : nullptr, C, n_active, max_rows, n_out, K, epilogue,
+                               (cudaStream_t)stream);
+}
+
 int surelock_update_mask(const float* conf, const int32_t* argmax, const int32_t* active_idx, const int32_t* row_offsets,
                          int B, int N, int lo, int hi, int k, int32_t mask_token, int32_t* tokens, uint8_t* mask_state,
                          int32_t* n_revealed, void* stream) {

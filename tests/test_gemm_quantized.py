@@ -1,0 +1,184 @@
+"""Products with 4-bit weights against plain statements in 64 bits.
+
+Two kinds of case.  With small whole numbers in A and powers of two as scales every product, group sum and total is exact in
+fp32 in any order, so the fp32 epilogue is compared bit for bit: that pins every index.  With random values the bound is
+that of the summation: a lane's chain is K / 16 matrix instructions and K / group scaled adds, then at most 64 partial sums
+are joined; each step is off by at most 2^-22 of sum |a| |w| (an fp32 addition that may truncate: 2^-23, twice over for the
+sum inside the instruction); a bf16 result is off by half a step more, 2^-8 of its value.  silu(x) y: the derivative of
+silu is at most 1.1 and |silu(x)| <= |x|, and its exponential is off by 2^-20 of it at most."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_06412_b200 import binding as SL
+from paper_2602_06412_b200 import build as build_mod
+
+DEV = "cuda"
+gpu = pytest.mark.gpu
+
+
+def _weights(n, K, group, zeros, scale_t, seed, exact=False):
+    g = torch.Generator().manual_seed(seed)
+    codes = torch.randint(0, 256, (n, K // 2), generator=g, dtype=torch.uint8)
+    if exact:
+        scales = torch.exp2(torch.randint(-2, 3, (n, K // group), generator=g).float()).to(scale_t)
+    else:
+        scales = (torch.randn(n, K // group, generator=g) * 0.02).to(scale_t)          # either sign
+    z = torch.randint(0, 16, (n, K // group), generator=g, dtype=torch.uint8) if zeros else None
+    u = torch.stack([codes & 15, codes >> 4], 2).reshape(n, K).double().numpy()
+    w = (u.reshape(n, -1, group) - (z.double().numpy()[..., None] if zeros else 8)) * scales.double().numpy()[..., None]
+    return tuple(t.to(DEV) if t is not None else None for t in (codes, scales, z)), w.reshape(n, K)
+
+
+def _run(A, W, C, M, epilogue, W2=None):
+    SL.surelock_gemm_quantized(A, W, C, torch.tensor([M], dtype=torch.int32, device=DEV), epilogue=epilogue, W2=W2)
+
+
+# ---- refusals, without a GPU ------------------------------------------------------------------------------------------
+def test_refusals_on_the_host():
+    build_mod.build()
+    L = SL.lib()
+    W = lambda **o: ctypes.byref(SL._W4(**{**dict(codes=0x1000, scales=0x2000, zeros=None, group=64, scale_dtype=SL.SL_BF16), **o}))
+    good = [0x100, W(), None, 0x200, 0x300, 4, 10, 128, 0, None]
+    cases = [(0, None, -1), (1, None, -1), (3, None, -1), (4, None, -1), (5, -1, -1), (6, 0, -1), (7, 0, -1), (7, 96, -1), (8, 3, -1), (8, -1, -1),
+             (1, W(codes=None), -1), (1, W(scales=None), -1), (1, W(group=0), -1), (1, W(scale_dtype=SL.SL_INT8), -1), (1, W(group=16), -5),
+             (1, W(codes=0x1008), -5), (0, 0x108, -5), (8, 2, -1), (5, 0, 0)]
+    for at, value, rc in cases:
+        bad = list(good)
+        bad[at] = value
+        assert L.surelock_gemm_quantized(*bad) == rc, (at, value)
+    swiglu = [0x100, W(), W(), 0x200, 0x300, 4, 10, 128, 2, None]
+    for w2 in (W(group=32), W(scale_dtype=SL.SL_FP32), W(zeros=0x3000), W(codes=None)):
+        swiglu[2] = w2
+        assert L.surelock_gemm_quantized(*swiglu) == -1
+
+
+def test_binding_refuses_wrong_shapes():
+    A, C = torch.zeros(2, 128, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.bfloat16)
+    codes, scales = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, 2)
+    n = torch.zeros(1, dtype=torch.int32)
+    for a, w, c, e in [(A.float(), (codes, scales, None), C, 0), (A, (codes, scales, None), C, 1), (A, (codes[:, :32].contiguous(), scales, None), C, 0),
+                       (A, (codes, scales[:, :1].expand(5, 3), None), C, 0), (A, (codes, scales, scales), C, 0), (A, (codes, scales, None), C[:1], 0)]:
+        with pytest.raises(SL.SurelockError):
+            SL.surelock_gemm_quantized(a, w, c, n, epilogue=e)
+
+
+# ---- exact cases ------------------------------------------------------------------------------------------------------
+SHAPES = [  # M, n_out, K, group
+    (1, 1, 32, 32), (1, 17, 128, 128), (3, 100, 96, 32), (8, 129, 192, 64), (9, 64, 640, 128), (23, 200, 1056, 32), (16, 40, 1344, 64),
+    (33, 130, 256, 64), (64, 65, 384, 128), (65, 33, 512, 128), (128, 300, 1280, 64), (130, 48, 4096, 128), (1, 1000, 4096, 128), (5, 37, 12288, 64),
+    (40, 72, 13824, 128), (64, 31, 12320, 32), (7, 4096, 4096, 128), (100, 777, 2048, 32),
+]
+
+
+@gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("scale_t", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,n,K,group", SHAPES)
+def test_whole_numbers_are_exact(M, n, K, group, zeros, scale_t):
+    W, w = _weights(n, K, group, zeros, scale_t, seed=M + n, exact=True)
+    g = torch.Generator().manual_seed(K)
+    a = torch.randint(-4, 5, (M + 3, K), generator=g)
+    a[M:] = 1 << 10                                                   # rows behind the count take no part
+    A = a.to(torch.bfloat16).to(DEV)
+    C = torch.randint(-8, 9, (M + 3, n), generator=g).float()
+    want = C.double().numpy()
+    want[:M] += a[:M].double().numpy() @ w.T
+    D = C.to(DEV)
+    _run(A, W, D, M, 1)
+    assert np.array_equal(D.cpu().double().numpy(), want)
+    D = torch.full((M + 3, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    _run(A, W, D, M, 0)
+    want0 = torch.from_numpy(want[:M] - C[:M].double().numpy()).float().to(torch.bfloat16)
+    assert torch.equal(D[:M].cpu(), want0) and torch.all(D[M:] == 7.0)
+
+
+# ---- random cases -----------------------------------------------------------------------------------------------------
+def _tol(A, w, K, group):
+    return (K / 16 + K / group + 64) * 2.0 ** -22 * (np.abs(A) @ np.abs(w).T)
+
+
+@gpu
+@pytest.mark.parametrize("M,n,K,group,zeros,scale_t,epilogue", [
+    (1, 4096, 4096, 128, False, torch.bfloat16, 0), (23, 1000, 4096, 128, True, torch.bfloat16, 2), (128, 515, 2048, 64, True, torch.float32, 1),
+    (8, 300, 1024, 32, False, torch.float32, 2), (64, 129, 768, 64, False, torch.bfloat16, 2), (12, 77, 96, 32, True, torch.bfloat16, 2),
+    (90, 200, 640, 128, True, torch.float32, 2), (31, 2049, 5120, 128, False, torch.float32, 0), (2, 50, 12288, 64, True, torch.float32, 1)])
+def test_random_values(M, n, K, group, zeros, scale_t, epilogue):
+    W, w = _weights(n, K, group, zeros, scale_t, seed=1)
+    g = torch.Generator().manual_seed(2)
+    A = (torch.randn(M, K, generator=g) * torch.exp(torch.randn(M, 1, generator=g))).to(torch.bfloat16)
+    a = A.double().numpy()
+    x, tx = a @ w.T, _tol(a, w, K, group)
+    W2 = None
+    if epilogue == 2:
+        W2, w2 = _weights(n, K, group, zeros, scale_t, seed=3)
+        y, ty = a @ w2.T, _tol(a, w2, K, group)
+        s = x / (1 + np.exp(-x))
+        want, tol = s * y, 1.1 * tx * (np.abs(y) + ty) + np.abs(s) * (ty + 2.0 ** -20 * np.abs(y))
+    else:
+        want, tol = x, tx
+    if epilogue == 1:
+        C = torch.randn(M, n, generator=g)
+        want = want + C.double().numpy()
+        tol = tol + 2.0 ** -24 * np.abs(want)
+        D = C.to(DEV)
+    else:
+        tol = tol + 2.0 ** -8 * np.abs(want)
+        D = torch.empty(M, n, dtype=torch.bfloat16, device=DEV)
+    keep = D.clone()
+    _run(A.to(DEV), W, D, M, epilogue, W2)
+    d = np.abs(D.cpu().double().numpy() - want)
+    assert np.all(d <= tol), float((d / tol).max())
+    again = keep
+    _run(A.to(DEV), W, again, M, epilogue, W2)
+    assert torch.equal(again, D)                                      # the same bits again
+
+
+@gpu
+def test_rows_do_not_meet():
+    """A row of infinities or NaN leaves the others as they are; large finite values stay finite."""
+    W, w = _weights(64, 256, 64, True, torch.bfloat16, seed=5)
+    A = torch.randn(12, 256, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    D = torch.empty(12, 64, dtype=torch.bfloat16, device=DEV)
+    _run(A.to(DEV), W, D, 12, 0)
+    B = A.clone()
+    B[3] = float("inf")
+    B[10, 7] = float("nan")
+    B[5] = A[5] * 2.0 ** 100
+    E = torch.empty_like(D)
+    _run(B.to(DEV), W, E, 12, 0)
+    rest = [r for r in range(12) if r not in (3, 5, 10)]
+    assert torch.equal(D[rest], E[rest]) and torch.all(torch.isnan(E[10]))
+    assert torch.equal(E[5].float(), D[5].float() * 2.0 ** 100)
+
+
+@gpu
+def test_graph_streams_and_changing_counts():
+    M, n, K = 20, 600, 1024
+    W, w = _weights(n, K, 128, False, torch.bfloat16, seed=7)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).to(DEV)
+    want = torch.zeros(M, n, dtype=torch.bfloat16, device=DEV)
+    _run(A, W, want, M, 0)
+    count = torch.tensor([M], dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        SL.surelock_gemm_quantized(A, W, out, count)
+    for m in (20, 0, 1, 13):
+        out.zero_()
+        count.fill_(m)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:m], want[:m]) and torch.all(out[m:] == 0)
+    streams, outs = [torch.cuda.Stream() for _ in range(3)], [torch.zeros_like(want) for _ in range(3)]
+    count.fill_(M)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, o in zip(streams, outs):
+            with torch.cuda.stream(s):
+                SL.surelock_gemm_quantized(A, W, o, count)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
