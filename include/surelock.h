@@ -471,7 +471,7 @@ typedef struct {
  * infinity or NaN gets scale NaN.  k, v: dev, row r at r * row_stride elements, heads packed [n_kv_heads][head_dim], of
  * `dtype` SL_BF16 or SL_FP32; row_stride * sizeof(elem) a multiple of 16, so they may be parts of wider rows.  The positions
  * are distinct, and two of them do not share a page place through equal table entries (the values left there would be a
- * mixture).  A position outside the tables, or on a bad page, is skipped (device status 4).  Nothing else is touched.
+ * mixture).  max_rows * n_kv_heads < 2^31.  A position outside the tables, or on a bad page, is skipped (device status 4).  Nothing else is touched.
  * dev_status may be NULL.  Asynchronous on `stream`; may be captured into a graph. */
 int surelock_kv_scatter_paged(const surelock_paged_kv *cache, const void *k, const void *v, int64_t row_stride,
                               const int32_t *active_idx, const int32_t *n_active, int max_rows, int B, int N, int dtype,

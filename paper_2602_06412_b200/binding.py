@@ -134,7 +134,7 @@ def _p(t: Optional[torch.Tensor]):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())   # the current stream without a wrapper object
 
 
 def _dt(t: torch.Tensor) -> int:
@@ -478,17 +478,17 @@ def _want(ok: bool, what: str):
         raise SurelockError(what)
 
 
-def _rows(t: torch.Tensor, heads: int, dh: int, what: str) -> int:
-    """Row stride, in elements, of a tensor [rows][heads][dh] whose rows are packed (they may lie apart)."""
-    _want(t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dh, f"{what}: a CUDA tensor [rows][{heads}][{dh}] is wanted")
-    st = t.stride()
-    _want(st[2] == 1 and (st[1] == dh or heads == 1), f"{what}: the heads of a row must be packed")
-    return st[0] if t.shape[0] > 1 else max(st[0], heads * dh)
+def _rows(t: torch.Tensor, heads: int, dh: int) -> int:
+    """Row stride, in elements, of a CUDA tensor [rows][heads][dh] whose rows are packed (they may lie apart)."""
+    shape, st = t.shape, t.stride()
+    if not (t.is_cuda and len(shape) == 3 and shape[1] == heads and shape[2] == dh and st[2] == 1 and (st[1] == dh or heads == 1)):
+        raise SurelockError(f"a CUDA tensor [rows][{heads}][{dh}] with packed rows is wanted, got {tuple(shape)}, strides {st}, on {t.device}")
+    return st[0] if shape[0] > 1 else max(st[0], heads * dh)
 
 
-def _ints(t: torch.Tensor, least: int, what: str):
-    _want(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= least,
-          f"{what}: a contiguous int32 CUDA tensor of at least {least} entries is wanted")
+def _ints(t: torch.Tensor, least: int) -> int:
+    if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= least):
+        raise SurelockError(f"a contiguous int32 CUDA tensor of at least {least} entries is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -511,22 +511,23 @@ class PagedKV:
         self.raw = _PagedKV(k.data_ptr(), v.data_ptr(), _p(k_scale), _p(v_scale), page_table.data_ptr(), k.shape[0], k.shape[2],
                             page_table.shape[1], k.shape[1], k.shape[3], _PAGED_DT[k.dtype])
         self.ref = C.byref(self.raw)
+        self._ws_bytes = 0
 
 
 def surelock_kv_scatter_paged(cache: PagedKV, k, v, active_idx, n_active, N: int, dev_status=None):
     """Rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32; rows may lie apart) into the pages, quantised on the way."""
-    stride = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
-    _want(_rows(v, cache.n_kv_heads, cache.head_dim, "v") == stride and v.shape == k.shape and v.dtype == k.dtype, "k and v must be laid out alike")
-    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), stride, _ints(active_idx, k.shape[0], "active_idx"),
+    stride = _rows(k, cache.n_kv_heads, cache.head_dim)
+    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == stride, "k and v must be laid out alike")
+    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), stride, _ints(active_idx, k.shape[0]),
                                            _p(n_active), k.shape[0], cache.n_seq, N, _dt(k), _p(dev_status), _stream()),
            "surelock_kv_scatter_paged")
 
 
 def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v, dev_status=None):
     """Positions active_idx back into the rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32)."""
-    stride = _rows(k, cache.n_kv_heads, cache.head_dim, "k")
-    _want(_rows(v, cache.n_kv_heads, cache.head_dim, "v") == stride and v.shape == k.shape and v.dtype == k.dtype, "k and v must be laid out alike")
-    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0], "active_idx"), _p(n_active), k.shape[0], cache.n_seq,
+    stride = _rows(k, cache.n_kv_heads, cache.head_dim)
+    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == stride, "k and v must be laid out alike")
+    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0]), _p(n_active), k.shape[0], cache.n_seq,
                                           N, k.data_ptr(), v.data_ptr(), stride, _dt(k), _p(dev_status), _stream()),
            "surelock_kv_gather_paged")
 
@@ -539,10 +540,11 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
     """q, o: bf16 [M][H][head_dim] (rows may lie apart); row_offsets int32 [B+1], seq_lens int32 [B]; workspace: uint8 tensor of
     surelock_attention_paged_workspace_bytes(head_dim) bytes, one per call that may run at the same time."""
     _want(q.dim() == 3 and o.shape == q.shape and q.dtype == torch.bfloat16 and o.dtype == torch.bfloat16, "q, o: bf16 [M][H][head_dim], alike")
-    H, B = q.shape[1], seq_lens.numel()
+    H, B, dh = q.shape[1], seq_lens.numel(), cache.head_dim
     _want(B <= cache.n_seq, "more sequences than the page table has")
-    _want(workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= surelock_attention_paged_workspace_bytes(cache.head_dim),
-          "workspace too small")
-    _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, cache.head_dim, "q"), _ints(row_offsets, B + 1, "row_offsets"),
-                                          _ints(seq_lens, B, "seq_lens"), q.shape[0], B, H, o.data_ptr(), _rows(o, H, cache.head_dim, "o"),
-                                          workspace.data_ptr(), _p(dev_status), _stream()), "surelock_attention_paged")
+    if not cache._ws_bytes:
+        cache._ws_bytes = surelock_attention_paged_workspace_bytes(dh)
+    _want(workspace.is_cuda and workspace.is_contiguous() and workspace.nbytes >= cache._ws_bytes, "workspace too small, or not on the GPU")
+    _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh), _ints(row_offsets, B + 1), _ints(seq_lens, B), q.shape[0],
+                                          B, H, o.data_ptr(), _rows(o, H, dh), workspace.data_ptr(), _p(dev_status), _stream()),
+           "surelock_attention_paged")

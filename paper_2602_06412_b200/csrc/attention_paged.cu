@@ -15,10 +15,13 @@
 // with programmatic dependent launch, adds them in unit order: no atomics, no counters, nothing kept between calls.
 //   warp 4     producer: TMA boxes of a page (and of its scales) into a ring of stages, 128-byte (64-byte for rows of 64
 //              bytes) swizzle; a page number outside the pool is replaced by one past its end, which TMA fills with zeros
-//   warps 0-3  16 keys of the unit each, with their own running maximum and sum: S = Q K^T by mma.sync m16n8k16 (the tile
-//              has 16 rows, an eighth of a tcgen05 tile; the codes become fp16, exactly, in registers on the way), exp2, O += P V.
+//   warps 0-3  S = Q K^T for 16 keys of the unit each (mma.sync m16n8k16: a tile of 16 rows is an eighth of a tcgen05 tile; the
+//              codes become fp16, exactly, in registers on the way), exp2, the weights into shared memory as the A fragments
+//              they already are; then O += P V for a quarter of the columns each, over all 64 keys.  O so takes d_h / 8
+//              registers per 16 rows, which lets four CTAs live on an SM: the chain of dependent steps of a unit, not the
+//              bandwidth, would bound fewer (one O per warp, two CTAs per SM: 4.2 - 5.2 TB/s).
 // The contraction index is permuted (the same way for Q and K) so that a lane reads its share of a key as 16-byte loads, and
-// the columns of O so that it reads 16 bytes of a value row; two keys' bytes are interleaved by byte permutes.
+// the columns of O so that it reads neighbouring bytes of a value row; two keys' bytes are interleaved by byte permutes.
 // Numerics: q becomes fp16 times a power of two per row (its largest magnitude in [1, 2)), the weight w_j = p_j sv_j becomes
 // fp16 under a power of two per row that follows the row's largest weight so far; both keep 11 bits, and weights below
 // 2^-33 of the largest vanish.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
@@ -71,9 +74,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
   return r;
 }
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 r;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t r;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
   return r;
 }
 __device__ __forceinline__ void ldsm_x4_t(uint32_t a, uint32_t* r) {
@@ -83,6 +86,17 @@ __device__ __forceinline__ void ldsm_x4_t(uint32_t a, uint32_t* r) {
 // bounded wait of a whole warp, with the same answer in every lane
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+// whether the flag is set in any of the 128 consumer threads; also a barrier of them
+__device__ __forceinline__ bool consumers_any(bool x) {
+  int r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, 3, 128, q;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(r) : "r"((int)x) : "memory");
+  return r != 0;
 }
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
@@ -117,6 +131,9 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 }
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
+// rows of a query tile: MT tiles of 16 as the 16-row operand of the products, or (MT = 0) 8 as their columns
+template <int MT> __host__ __device__ constexpr int ap_rows() { return MT == 0 ? 8 : 16 * MT; }
+
 // one sequence's share of the units
 struct Seq {
   int r0, rows, len, tiles, nb;   // first packed row, rows, keys, query tiles, units per (key head, tile)
@@ -127,7 +144,7 @@ template <int MT> __device__ __forceinline__ Seq seq_of(const PagedAttnArgs& a, 
   s.rows = min(a.row_offsets[b + 1], a.max_rows) - s.r0;
   const int len = a.seq_lens[b];
   s.len = min(max(len, 0), a.max_tokens);
-  s.tiles = s.rows > 0 ? (int)(((long long)s.rows * a.G + 16 * MT - 1) / (16 * MT)) : 0;
+  s.tiles = s.rows > 0 ? (int)(((long long)s.rows * a.G + ap_rows<MT>() - 1) / ap_rows<MT>()) : 0;
   s.nb = max(1, (s.len + AP_KEYS - 1) / AP_KEYS);   // a sequence without keys has one unit, which writes its zeros
   return s;
 }
@@ -140,46 +157,114 @@ template <int DH, int KIND> struct Tile {
   static constexpr int KV = SLABS * SLAB;
   static constexpr bool SCALED = KIND != SL_BF16;
   static constexpr int STAGE = 2 * KV + (SCALED ? 1024 : 0);    // K, V, K scales, V scales (512 bytes each)
-  static constexpr int STAGES = STAGE > 20000 ? 2 : STAGE > 17000 ? 3 : STAGE > 10000 ? 4 : 6;   // two CTAs per SM
   static constexpr int STEPS = DH / 16;
-  static constexpr int PITCH = DH + 4 * (DH / 32);              // floats per row of the join buffer
-  static constexpr int JOIN = 4 * 16 * PITCH * 4;
 };
-template <int DH, int KIND, int MT> constexpr int ap_smem() {
+// CTAs per SM that the registers are bounded for, and stages of the ring: what then fits the shared memory
+template <int MT> __host__ __device__ constexpr int ap_occupancy() { return MT <= 1 ? 4 : MT == 2 ? 3 : 2; }
+template <int DH, int KIND, int MT> struct Plan {
   using T = Tile<DH, KIND>;
-  return 1024 + T::STAGES * T::STAGE + T::JOIN + MT * T::STEPS * 512 + 16 * MT * 4 + 2 * 4 * 16 * MT * 4 + 256;   // and 8 bytes per sequence
+  static constexpr int TILES = MT ? MT : 1;
+  static constexpr int FIXED = 1024 + TILES * T::STEPS * 512 + TILES * 4 * 512 + 16 * TILES * 4 * 9 + 256;   // Q, P, row factors, statistics
+  static constexpr int ROOM = 228 * 1024 / ap_occupancy<MT>() - 1024 - 256 - FIXED;                // 256: prefix sums of up to 31 sequences
+  static constexpr int FIT = ROOM / T::STAGE;
+  static constexpr int STAGES = FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
+  static constexpr int SMEM = FIXED + STAGES * T::STAGE;                                           // and 8 bytes per sequence
+};
+
+// a row's bf16 words (this lane's W of them, LANES lanes to the row) become fp16 times a power of two that brings the row's
+// largest magnitude into [1, 2); returns the inverse power.  In two factors each, as 2^-126 ... 2^127 need not be normal
+// numbers both ways; a row with an infinity or NaN stays as it is.
+template <int W, int LANES> __device__ __forceinline__ float rows_to_f16(uint32_t* w) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  int ex = (int)(top >> 7) - 127;
+  ex = top == 0 || ex > 127 ? 0 : max(ex, -126);
+  const float d0 = pow2i(-ex / 2), d1 = pow2i(-ex - (-ex / 2));
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = pack_f16(__uint_as_float(w[i] << 16) * d0 * d1, __uint_as_float(w[i] & 0xffff0000u) * d0 * d1);
+  return pow2i(ex / 2) * pow2i(ex - ex / 2);
+}
+// Values behind the last key may be anything, NaN included: they become zeros (their weight is zero too).  Rows are cleared
+// whole, so the swizzle does not matter; the fence orders this before the next copy into the stage.
+template <typename T> __device__ __forceinline__ void clear_rows(uint32_t vb, int key0, int left, int lane) {
+  const int row = lane >> 1, half = lane & 1;
+  if (row >= left) {
+#pragma unroll
+    for (int i = 0; i < T::ROW / 32; ++i) {
+      const int byte = half * (T::ROW / 2) + 16 * i;
+      st_shared_f4(vb + (byte / T::SLAB_ROW) * T::SLAB + (key0 + row) * T::SLAB_ROW + byte % T::SLAB_ROW, 0, 0, 0, 0);
+    }
+  }
+  fence_async_smem();
+}
+// A row's maximum becomes max(m, top): returns the factor of O.  The weights shrink with it, and E, their exponent, follows,
+// so that O keeps its size instead.
+template <bool SCALED> __device__ __forceinline__ float follow_max(float& m, float& l, int& E, float top) {
+  const float x = fmaxf(top, m), d = m - x;
+  const bool fresh = m == -INFINITY;             // nothing summed yet
+  m = x;
+  float f = fresh ? 0.f : fast_exp2(d);
+  l *= f;
+  if (SCALED) {
+    const int En = fresh ? AP_E_LEAST : max(E + (int)fmaxf(floorf(d), -400.f), AP_E_LEAST);
+    f = fresh ? 0.f : fast_exp2(d + (float)(E - En));
+    E = En;
+  }
+  return f;
+}
+// E becomes the exponent of the largest weight if that is more: returns the factor of O
+__device__ __forceinline__ float follow_weight(int& E, float top) {
+  const int En = max(E, (int)(__float_as_uint(top) >> 23) - 127);
+  const float f = E - En < -126 ? 0.f : pow2i(E - En);
+  E = En;
+  return f;
+}
+// four keys of step k (2 t, 2 t + 1, and 8 on) of this warp's quarter of the columns: four consecutive ones (DH = 128), or
+// a word with this lane's two in it
+template <int DH> __device__ __forceinline__ void load_values(uint32_t vb, int k, int warp, int g, int t, uint32_t* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t key = 16 * k + (i >> 1) * 8 + 2 * t + (i & 1);
+    if (DH == 128) v[i] = lds32(vb + key * 128 + (((2 * warp + (g >> 2)) ^ (key & 7)) << 4) + (g & 3) * 4);
+    else v[i] = lds32(vb + key * 64 + ((warp ^ ((key >> 1) & 3)) << 4) + (g >> 1) * 4);
+  }
 }
 
 }  // namespace
 
 template <int DH, int KIND, int MT>
-__global__ void __launch_bounds__(AP_THREADS, 2)
+__global__ void __launch_bounds__(AP_THREADS, ap_occupancy<MT>())
 attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                        const __grid_constant__ CUtensorMap tmKs, const __grid_constant__ CUtensorMap tmVs, const PagedAttnArgs a) {
   using T = Tile<DH, KIND>;
   constexpr bool BF = KIND == SL_BF16;
   constexpr int QK = BF ? SL_E4M3 : KIND;   // a type for the conversions that a bf16 cache does not reach
-  constexpr int ROWS = 16 * MT;
-  constexpr int NT = DH / 8;                // column tiles of O
+  constexpr int ROWS = ap_rows<MT>();
+  constexpr int TILES = Plan<DH, KIND, MT>::TILES;
+  constexpr int STAGES = Plan<DH, KIND, MT>::STAGES;
+  constexpr int NT = DH / 32;               // column tiles of O per warp
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* sStage = smem;
-  float* sJoin = reinterpret_cast<float*>(sStage + T::STAGES * T::STAGE);
-  uint4* sQ = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(sJoin) + T::JOIN);       // [MT][STEPS][32]
-  float* sRow = reinterpret_cast<float*>(sQ + MT * T::STEPS * 32);                          // [ROWS] factor of S
+  uint4* sQ = reinterpret_cast<uint4*>(sStage + STAGES * T::STAGE);                         // [TILES][STEPS][32]
+  uint4* sP = sQ + TILES * T::STEPS * 32;                                                   // [TILES][4][32]
+  float* sRow = reinterpret_cast<float*>(sP + TILES * 4 * 32);                                 // [ROWS] factor of S
   float* sM = sRow + ROWS;                                                                  // [4][ROWS]
   float* sL = sM + 4 * ROWS;                                                                // [4][ROWS]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sL + 4 * ROWS);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(bars + 2 * T::STAGES);
-  long long* sCum = reinterpret_cast<long long*>(bars + 2 * T::STAGES + 1);                 // [B + 1]
+  volatile int* s_abort = reinterpret_cast<volatile int*>(bars + 2 * STAGES);
+  long long* sCum = reinterpret_cast<long long*>(bars + 2 * STAGES + 1);                    // [B + 1]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int s) { return bar0 + 8u * s; };
-  auto empty = [&](int s) { return bar0 + 8u * (T::STAGES + s); };
+  auto empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < T::STAGES; ++i) {
+    for (int i = 0; i < STAGES; ++i) {
       mbar_init(full(i), 1);
       mbar_init(empty(i), 4);
     }
@@ -248,8 +333,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
       };
       int next = page_of(blk0);
       for (int j = blk0; j < blk0 + nblk; ++j, ++cnt) {
-        const int st = (int)(cnt % T::STAGES);
-        const uint32_t ph = (cnt / T::STAGES) & 1;
+        const int st = (int)(cnt % STAGES);
+        const uint32_t ph = (cnt / STAGES) & 1;
         const int t = j * AP_KEYS + lane * box;
         const bool have = lane < pieces && t < s.len;
         int page = next;
@@ -283,8 +368,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
     if (!ok) {
       // gave up: the copies in flight still write to this CTA's shared memory, wait for them (bounded)
       const unsigned long long t0 = clock64();
-      for (unsigned i = cnt > (unsigned)T::STAGES ? cnt - T::STAGES : 0; i < cnt; ++i)
-        while (!mbar_try(full((int)(i % T::STAGES)), (i / T::STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      for (unsigned i = cnt > (unsigned)STAGES ? cnt - STAGES : 0; i < cnt; ++i)
+        while (!mbar_try(full((int)(i % STAGES)), (i / STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
       if (lane == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
     }
     return;
@@ -303,422 +388,641 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
     const int nblk = (int)min((long long)(s.nb - blk0), u1 - u);
     const int valid = (int)min((long long)ROWS, (long long)s.rows * a.G - (long long)tile * ROWS);
 
-    // query tile -> shared memory in the order of the A fragments; 8 threads per row, DH / 8 elements each
-    {
-      constexpr int PER = DH / 8, RUN = (DH == 128 && !BF) ? 32 : 16;
-      for (int mt = 0; mt < MT; ++mt) {
-        const int row = threadIdx.x >> 3, part = threadIdx.x & 7, e = tile * ROWS + mt * 16 + row;
-        uint4 w[PER / 8];
+    if constexpr (MT == 0) {
+      // ---- at most 8 rows: S^T = K Q^T and O^T = V^T P^T, the rows are the 8 columns of the products ----
+      // Q -> B fragments; 16 threads per row, DH / 16 elements each
+      {
+        constexpr int PER = DH / 16, RUN = (DH == 128 && !BF) ? 32 : 16;
+        const int row = threadIdx.x >> 4, part = threadIdx.x & 15, e = tile * ROWS + row;
+        uint32_t w[PER / 2];
 #pragma unroll
-        for (int i = 0; i < PER / 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
-        if (mt * 16 + row < valid) {
-          const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(s.r0 + e / a.G) * a.q_stride +
+        for (int i = 0; i < PER / 2; ++i) w[i] = 0;
+        if (row < valid) {
+          const uint2* src = reinterpret_cast<const uint2*>(a.q + (long long)(s.r0 + e / a.G) * a.q_stride +
                                                             (long long)(kvh * a.G + e % a.G) * DH + part * PER);
 #pragma unroll
-          for (int i = 0; i < PER / 8; ++i) w[i] = src[i];
+          for (int i = 0; i < PER / 4; ++i) {
+            const uint2 x = src[i];
+            w[2 * i] = x.x;
+            w[2 * i + 1] = x.y;
+          }
         }
-        uint32_t* pw = reinterpret_cast<uint32_t*>(w);
-        float factor = a.scale_log2;
-        if (!BF) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < PER / 2; ++i) top = max(top, max(pw[i] & 0x7fffu, (pw[i] >> 16) & 0x7fffu));
-#pragma unroll
-          for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          int ex = (int)(top >> 7) - 127;                               // exponent of the row's largest magnitude
-          ex = top == 0 || ex > 127 ? 0 : max(ex, -126);
-          // times 2^-ex in two steps, since 2^-ex and 2^ex need not both be normal numbers
-          const float d0 = pow2i(-ex / 2), d1 = pow2i(-ex - (-ex / 2));
-#pragma unroll
-          for (int i = 0; i < PER / 2; ++i)
-            pw[i] = pack_f16(__uint_as_float(pw[i] << 16) * d0 * d1, __uint_as_float(pw[i] & 0xffff0000u) * d0 * d1);
-          factor = factor * pow2i(ex / 2) * pow2i(ex - ex / 2);
-        }
-        if (part == 0) sRow[mt * 16 + row] = factor;
-        uint32_t* dst = reinterpret_cast<uint32_t*>(sQ + mt * T::STEPS * 32);
+        const float factor = BF ? a.scale_log2 : a.scale_log2 * rows_to_f16<PER / 2, 16>(w);
+        if (part == 0) sRow[row] = factor;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(sQ);       // [step][lane][2]
 #pragma unroll
         for (int i = 0; i < PER / 2; ++i) {
           const int d = part * PER + 2 * i, block = d / (4 * RUN), in = d % (4 * RUN), tt = in / RUN, rem = in % RUN;
-          const int step = block * (RUN / 4) + rem / 4, pair = (rem & 3) >> 1;
-          dst[((step * 32 + (row & 7) * 4 + tt) << 2) + (row >> 3) + 2 * pair] = pw[i];
+          dst[((block * (RUN / 4) + rem / 4) * 32 + row * 4 + tt) * 2 + ((rem & 3) >> 1)] = w[i];
         }
       }
-    }
-    bar_consumers();
-    float fr[MT][2];
+      bar_consumers();
+      constexpr int VT = DH / 64;                              // tiles of 16 columns per warp
+      uint2 qb[T::STEPS];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      fr[mt][0] = sRow[mt * 16 + g];
-      fr[mt][1] = sRow[mt * 16 + g + 8];
-    }
-    uint4 qa[MT == 1 ? T::STEPS : 1];
-    if (MT == 1) {
+      for (int i = 0; i < T::STEPS; ++i) qb[i] = reinterpret_cast<const uint2*>(sQ)[i * 32 + lane];
+      const float fr[2] = {sRow[2 * t], sRow[2 * t + 1]};      // of this lane's two rows, and so are m, l, E
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, acc[VT][4];
+      int E[2] = {AP_E_LEAST, AP_E_LEAST};
 #pragma unroll
-      for (int i = 0; i < T::STEPS; ++i) qa[MT == 1 ? i : 0] = sQ[i * 32 + lane];
-    }
+      for (int j = 0; j < VT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+      __half* sPh = reinterpret_cast<__half*>(sP);
+      const int pput = (warp >> 1) * 256 + (8 * t + (g >> 1)) * 8 + (warp & 1) * 4 + (g & 1);   // [2][lane of the reader][step & 1][key / 8][key & 1]
 
-    float acc[MT][NT][4];
-    float m[MT][2], l[MT][2];
+      for (int j = blk0; j < blk0 + nblk; ++j, ++cnt) {
+        const int st = (int)(cnt % STAGES);
+        if (ok) ok = warp_wait(full(st), (cnt / STAGES) & 1, s_abort);
+        const int here = min(s.len - j * AP_KEYS, AP_KEYS);    // keys of the unit
+        const int left = here - (int)jkey;                     // of this warp: 16 or more, fewer, none
+        const uint32_t kb = smem_u32(sStage + st * T::STAGE), vb = kb + T::KV;
+        if (left > 0 && left < 16) clear_rows<T>(vb, (int)jkey, left, lane);
+        float sc[2][4] = {};                                   // two chains; key g + 8 (i >> 1), row 2 t + (i & 1)
+        float ks[2] = {0.f, 0.f}, vs[2] = {0.f, 0.f};
+        if (left > 0) {
+          if (T::SCALED) {
+            const float* scp = reinterpret_cast<const float*>(sStage + st * T::STAGE + 2 * T::KV) + (a.page_size == 16 ? 32 : 16) * warp + g;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m[mt][0] = m[mt][1] = -INFINITY;
-      l[mt][0] = l[mt][1] = 0.f;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[mt][j][0] = acc[mt][j][1] = acc[mt][j][2] = acc[mt][j][3] = 0.f;
-    }
-    int E[MT][2];                                // exponent of the largest weight so far, in units of the present maximum
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) E[mt][0] = E[mt][1] = AP_E_LEAST;
-
-    for (int j = blk0; j < blk0 + nblk && ok; ++j, ++cnt) {
-      const int st = (int)(cnt % T::STAGES);
-      if (!(ok = warp_wait(full(st), (cnt / T::STAGES) & 1, s_abort))) break;
-      const int left = s.len - j * AP_KEYS - (int)jkey;      // keys from this warp's first one on
-      if (left > 0) {
-        uint8_t* stage = sStage + st * T::STAGE;
-        const uint32_t sk_base = smem_u32(stage), sv_base = sk_base + T::KV;
-        const bool tail = left < 16;
-        if (tail) {
-          // values behind the last key may be anything, NaN included: they become zeros (their weight is zero too)
-          const int row = lane >> 1, half = lane & 1;
-          if (row >= left) {
-#pragma unroll
-            for (int i = 0; i < T::ROW / 32; ++i) {
-              const int byte = half * (T::ROW / 2) + 16 * i;   // a whole row is cleared, so the swizzle does not matter
-              st_shared_f4(sv_base + (byte / T::SLAB_ROW) * T::SLAB + (jkey + row) * T::SLAB_ROW + byte % T::SLAB_ROW, 0, 0, 0, 0);
+            for (int n = 0; n < 2; ++n) {
+              const bool in = 8 * n + g < left;
+              ks[n] = in ? scp[8 * n] : 0.f;
+              vs[n] = in ? scp[128 + 8 * n] : 0.f;
             }
           }
-          fence_async_smem();   // before the stage is handed back to the copies
-          __syncwarp();
+#pragma unroll
+          for (int sl = 0; sl < T::SLABS; ++sl) {
+            constexpr int CH = T::SLAB_ROW / 64;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+              uint32_t w[2][4];
+#pragma unroll
+              for (int n = 0; n < 2; ++n) {
+                const uint32_t key = jkey + n * 8 + g, chunk = t * CH + c;
+                const uint32_t sw = T::SLAB_ROW == 128 ? (chunk ^ (key & 7)) : (chunk ^ ((key >> 1) & 3));
+                const uint4 w4 = lds128(kb + sl * T::SLAB + key * T::SLAB_ROW + (sw << 4));
+                w[n][0] = w4.x; w[n][1] = w4.y; w[n][2] = w4.z; w[n][3] = w4.w;
+              }
+#pragma unroll
+              for (int i = 0; i < (BF ? 2 : 4); ++i) {
+                const int step = BF ? sl * 4 + c * 2 + i : c * 4 + i;
+                uint4 k4;
+                if (BF) k4 = make_uint4(w[0][BF ? 2 * i : 0], w[1][BF ? 2 * i : 0], w[0][BF ? 2 * i + 1 : 0], w[1][BF ? 2 * i + 1 : 0]);
+                else {
+                  codes_to_f16<QK>(w[0][i], k4.x, k4.z);
+                  codes_to_f16<QK>(w[1][i], k4.y, k4.w);
+                }
+                mma16<BF>(sc[i & 1], k4, qb[step].x, qb[step].y);
+              }
+            }
+          }
         }
-        float ks[4], vs[4];
-        if (T::SCALED) {
-          const float* sc = reinterpret_cast<const float*>(stage + 2 * T::KV) + (a.page_size == 16 ? 32 : 16) * warp + 2 * t;
-          ks[0] = sc[0]; ks[1] = sc[1]; ks[2] = sc[8]; ks[3] = sc[9];
-          vs[0] = sc[128]; vs[1] = sc[129]; vs[2] = sc[136]; vs[3] = sc[137];
+        float x[4];
+        bool grow = !ok;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = (sc[0][i] + sc[1][i]) * fr[i & 1];
+          if (T::SCALED) x[i] *= ks[i >> 1];
+          x[i] = 8 * (i >> 1) + g < left ? x[i] : -INFINITY;
+          grow |= x[i] > m[i & 1] + AP_TAU;
         }
-        // S = Q K^T: two tiles of 8 keys
+        auto row_tops = [&](float x0, float x1, float* top) {  // over all keys of the unit
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
+            x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
+          }
+          if (g == 0) {
+            sM[warp * ROWS + 2 * t] = x0;
+            sM[warp * ROWS + 2 * t + 1] = x1;
+          }
+          bar_consumers();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float* p = sM + 2 * t + i;
+            top[i] = fmaxf(fmaxf(p[0], p[ROWS]), fmaxf(p[2 * ROWS], p[3 * ROWS]));
+          }
+        };
+        auto rescale = [&](int i, float f) {
+#pragma unroll
+          for (int c = 0; c < VT; ++c) {
+            acc[c][i] *= f;
+            acc[c][i + 2] *= f;
+          }
+        };
+        if (consumers_any(grow)) {
+          if (!epilogue_warps_agree(ok)) {                     // a wait ran out: all four warps leave together
+            ok = false;
+            break;
+          }
+          float top[2];
+          row_tops(fmaxf(x[0], x[2]), fmaxf(x[1], x[3]), top);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) rescale(i, follow_max<T::SCALED>(m[i], l[i], E[i], top[i]));
+        }
+        bool over = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float mm = m[i & 1] == -INFINITY ? 0.f : m[i & 1];
+          x[i] = fast_exp2(x[i] - mm);
+          l[i & 1] += x[i];
+          if (T::SCALED) {
+            x[i] *= vs[i >> 1];
+            over |= fabsf(x[i] * pow2i(AP_W_EXP - E[i & 1])) >= AP_W_MOST;
+          }
+        }
+        auto put_weights = [&]() {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = pput + (i & 1) * 32 + (i >> 1) * 2;
+            if (BF) reinterpret_cast<bf16*>(sPh)[at] = __float2bfloat16_rn(x[i]);
+            else sPh[at] = __float2half_rn(x[i] * pow2i(AP_W_EXP - E[i & 1]));
+          }
+        };
+        put_weights();
+        if (consumers_any(T::SCALED && over)) {
+          float top[2];
+          row_tops(fmaxf(fabsf(x[0]), fabsf(x[2])), fmaxf(fabsf(x[1]), fabsf(x[3])), top);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) rescale(i, follow_weight(E[i], top[i]));
+          put_weights();
+          bar_consumers();
+        }
+        const uint4 p0 = sP[lane], p1 = sP[32 + lane];
+        const uint32_t pb[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (16 * k >= here) break;
+          if (BF) {
+#pragma unroll
+            for (int c = 0; c < VT; ++c) {
+              uint4 v;
+              const uint32_t key = 16 * k + (lane >> 4) * 8 + (lane & 7), chunk = 2 * (warp * VT + c) + ((lane >> 3) & 1);
+              ldsm_x4_t(vb + (chunk >> 3) * T::SLAB + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), reinterpret_cast<uint32_t*>(&v));
+              mma16<BF>(acc[c], v, pb[2 * k], pb[2 * k + 1]);
+            }
+          } else {
+            uint32_t v[4];
+            load_values<DH>(vb, k, warp, g, t, v);
+#pragma unroll
+            for (int c = 0; c < VT; ++c) {
+              const uint32_t sel = (DH == 128 ? c == 1 : (g & 1) == 1) ? 0x7362 : 0x5140;
+              uint4 v4;
+              codes_to_f16<QK>(__byte_perm(v[0], v[1], sel), v4.x, v4.y);
+              codes_to_f16<QK>(__byte_perm(v[2], v[3], sel), v4.z, v4.w);
+              mma16<BF>(acc[c], v4, pb[2 * k], pb[2 * k + 1]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(st));
+      }
+
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+        if (g == 0) sL[warp * ROWS + 2 * t + i] = l[i];
+      }
+      if (!epilogue_warps_agree(ok)) {
+        if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
+        return;
+      }
+      const bool starts = blk0 == 0, whole = starts && nblk == s.nb;
+      const long long slot = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * ROWS;
+      if (starts && !whole && threadIdx.x == 0) {
+        const long long last = (u + s.nb - 1) / per;           // CTA of the item's last unit
+        a.desc[blockIdx.x] = make_int4(s.r0, tile * ROWS, (valid << 16) | kvh, (int)last);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = 2 * t + i;
+        if (row >= valid) continue;
+        const float* p = sL + row;
+        const float sum = (p[0] + p[ROWS]) + (p[2 * ROWS] + p[3 * ROWS]);
+        const int e = tile * ROWS + row;
+        const float f = (T::SCALED ? pow2i(E[i] - AP_W_EXP) : 1.f) * (whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f);
+        bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + warp * (DH / 4);
+        float* part = a.part + (slot + row) * DH + warp * (DH / 4);
+        if (!whole && warp == 0 && g == 0) a.ml[slot + row] = make_float2(m[i], sum);
+        if (BF) {
+#pragma unroll
+          for (int c = 0; c < VT; ++c)
+#pragma unroll
+            for (int b8 = 0; b8 < 2; ++b8) {
+              const float y = acc[c][2 * b8 + i] * f;
+              if (whole) o[16 * c + 8 * b8 + g] = __float2bfloat16_rn(y);
+              else part[16 * c + 8 * b8 + g] = y;
+            }
+        } else {
+#pragma unroll
+          for (int c = 0; c < VT; ++c) {                       // consecutive columns 2 VT g ...
+            const float y0 = acc[c][i] * f, y1 = acc[c][i + 2] * f;
+            if (whole) *reinterpret_cast<uint32_t*>(o + 2 * VT * g + 2 * c) = pack_bf16(y0, y1);
+            else *reinterpret_cast<float2*>(part + 2 * VT * g + 2 * c) = make_float2(y0, y1);
+          }
+        }
+      }
+    } else {
+      // query tile -> shared memory in the order of the A fragments; 8 threads per row, DH / 8 elements each
+      {
+        constexpr int PER = DH / 8, RUN = (DH == 128 && !BF) ? 32 : 16;
+        const int row = threadIdx.x >> 3, part = threadIdx.x & 7;
+        uint4 wq[MT][PER / 8];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const int e = tile * ROWS + mt * 16 + row;
+#pragma unroll
+          for (int i = 0; i < PER / 8; ++i) wq[mt][i] = make_uint4(0, 0, 0, 0);
+          if (mt * 16 + row < valid) {
+            const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(s.r0 + e / a.G) * a.q_stride +
+                                                              (long long)(kvh * a.G + e % a.G) * DH + part * PER);
+#pragma unroll
+            for (int i = 0; i < PER / 8; ++i) wq[mt][i] = src[i];
+          }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t* pw = reinterpret_cast<uint32_t*>(wq[mt]);
+          const float factor = BF ? a.scale_log2 : a.scale_log2 * rows_to_f16<PER / 2, 8>(pw);
+          if (part == 0) sRow[mt * 16 + row] = factor;
+          uint32_t* dst = reinterpret_cast<uint32_t*>(sQ + mt * T::STEPS * 32);
+#pragma unroll
+          for (int i = 0; i < PER / 2; ++i) {
+            const int d = part * PER + 2 * i, block = d / (4 * RUN), in = d % (4 * RUN), tt = in / RUN, rem = in % RUN;
+            const int step = block * (RUN / 4) + rem / 4, pair = (rem & 3) >> 1;
+            dst[((step * 32 + (row & 7) * 4 + tt) << 2) + (row >> 3) + 2 * pair] = pw[i];
+          }
+        }
+      }
+      bar_consumers();
+      float fr[MT][2], m[MT][2], l[MT][2], acc[MT][NT][4];
+      int E[MT][2];                                // exponent of the largest weight so far, in units of the present maximum
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          fr[mt][h] = sRow[mt * 16 + g + 8 * h];
+          m[mt][h] = -INFINITY;                    // the same in all four warps, and so is E; l is of this warp's keys
+          l[mt][h] = 0.f;
+          E[mt][h] = AP_E_LEAST;
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[mt][j][0] = acc[mt][j][1] = acc[mt][j][2] = acc[mt][j][3] = 0.f;
+      }
+
+      for (int j = blk0; j < blk0 + nblk; ++j, ++cnt) {
+        const int st = (int)(cnt % STAGES);
+        if (ok) ok = warp_wait(full(st), (cnt / STAGES) & 1, s_abort);
+        const int here = min(s.len - j * AP_KEYS, AP_KEYS);    // keys of the unit
+        const int left = here - (int)jkey;                     // of this warp: 16 or more, fewer, none
+        const uint32_t kb = smem_u32(sStage + st * T::STAGE), vb = kb + T::KV;
+        const float* scp = reinterpret_cast<const float*>(sStage + st * T::STAGE + 2 * T::KV) + (a.page_size == 16 ? 32 : 16) * warp + 2 * t;
+        if (left > 0 && left < 16) clear_rows<T>(vb, (int)jkey, left, lane);
+        float ks[2][2], vs[2][2];
         float sc[MT][2][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int i = 0; i < 8; ++i) sc[mt][i >> 2][i & 3] = 0.f;
+        if (left > 0) {
+          if (T::SCALED) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          const uint32_t key = jkey + nt * 8 + g;
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const bool in = 8 * n + 2 * t + c < left;
+                ks[n][c] = in ? scp[8 * n + c] : 0.f;
+                vs[n][c] = in ? scp[128 + 8 * n + c] : 0.f;
+              }
+          }
+          // S = Q K^T: two tiles of 8 keys
 #pragma unroll
           for (int sl = 0; sl < T::SLABS; ++sl) {
-            constexpr int CH = T::SLAB_ROW / 64;            // 16-byte chunks of the row that belong to a lane: 1 or 2
+            constexpr int CH = T::SLAB_ROW / 64;              // 16-byte chunks of the row that belong to a lane: 1 or 2
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-              const uint32_t chunk = t * CH + c;
-              const uint32_t sw = T::SLAB_ROW == 128 ? (chunk ^ (key & 7)) : (chunk ^ ((key >> 1) & 3));
-              const uint4 w4 = lds128(sk_base + sl * T::SLAB + key * T::SLAB_ROW + (sw << 4));
-              const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+              uint32_t w[2][4];
+#pragma unroll
+              for (int n = 0; n < 2; ++n) {
+                const uint32_t key = jkey + n * 8 + g, chunk = t * CH + c;
+                const uint32_t sw = T::SLAB_ROW == 128 ? (chunk ^ (key & 7)) : (chunk ^ ((key >> 1) & 3));
+                const uint4 w4 = lds128(kb + sl * T::SLAB + key * T::SLAB_ROW + (sw << 4));
+                w[n][0] = w4.x; w[n][1] = w4.y; w[n][2] = w4.z; w[n][3] = w4.w;
+              }
 #pragma unroll
               for (int i = 0; i < (BF ? 2 : 4); ++i) {
                 const int step = BF ? sl * 4 + c * 2 + i : c * 4 + i;
-                uint32_t b0, b1;
-                if (BF) {
-                  b0 = w[BF ? 2 * i : 0];
-                  b1 = w[BF ? 2 * i + 1 : 0];
-                } else {
-                  codes_to_f16<QK>(w[i], b0, b1);
-                }
+                uint4 q4[MT];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                  const uint4 q4 = MT == 1 ? qa[MT == 1 ? step : 0] : sQ[(mt * T::STEPS + step) * 32 + lane];
-                  mma16<BF>(sc[mt][nt], q4, b0, b1);
+                for (int mt = 0; mt < MT; ++mt) q4[mt] = sQ[(mt * T::STEPS + step) * 32 + lane];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                  uint32_t b0, b1;
+                  if (BF) {
+                    b0 = w[n][BF ? 2 * i : 0];
+                    b1 = w[n][BF ? 2 * i + 1 : 0];
+                  } else {
+                    codes_to_f16<QK>(w[n][i], b0, b1);
+                  }
+#pragma unroll
+                  for (int mt = 0; mt < MT; ++mt) mma16<BF>(sc[mt][n], q4[mt], b0, b1);
                 }
               }
             }
           }
         }
         // scores in log2 units; keys behind the last one take no part
-        bool grow = false;
+        bool grow = !ok;
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const bool out = tail && nt * 8 + 2 * t + c >= left;
-            if (T::SCALED && out) vs[2 * nt + c] = 0.f;
+            const bool in = 8 * n + 2 * t + c < left;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                float x = sc[mt][nt][2 * h + c] * fr[mt][h];
-                if (T::SCALED) x *= ks[2 * nt + c];
-                if (out) x = -INFINITY;
-                sc[mt][nt][2 * h + c] = x;
-                if (x > m[mt][h] + AP_TAU) grow = true;
+                float x = sc[mt][n][2 * h + c] * fr[mt][h];
+                if (T::SCALED && left > 0) x *= ks[n][c];
+                x = in ? x : -INFINITY;
+                sc[mt][n][2 * h + c] = x;
+                grow |= x > m[mt][h] + AP_TAU;
               }
           }
-        if (__any_sync(0xffffffffu, grow)) {
+        auto rescale = [&](int mt, int h, float f) {
+#pragma unroll
+          for (int i = 0; i < NT; ++i) {
+            acc[mt][i][2 * h] *= f;
+            acc[mt][i][2 * h + 1] *= f;
+          }
+        };
+        // largest score (or weight's magnitude) of every row over the four warps' keys
+        auto row_tops = [&](bool mag, float (*top)[2]) {
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float x = fmaxf(fmaxf(sc[mt][0][2 * h], sc[mt][0][2 * h + 1]), fmaxf(sc[mt][1][2 * h], sc[mt][1][2 * h + 1]));
+              float x = mag ? 0.f : -INFINITY;
+#pragma unroll
+              for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) x = fmaxf(x, mag ? fabsf(sc[mt][n][2 * h + c]) : sc[mt][n][2 * h + c]);
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-              x = fmaxf(x, m[mt][h]);
-              const float d = m[mt][h] - x;                  // <= 0; nothing summed yet: -inf (or, 0 x 0, NaN)
-              const bool fresh = m[mt][h] == -INFINITY;
-              m[mt][h] = x;
-              l[mt][h] *= fresh ? 0.f : fast_exp2(d);
-              float f = fresh ? 0.f : fast_exp2(d);
-              if (T::SCALED) {                               // weights shrink by 2^d, and E with them
-                const int En = fresh ? AP_E_LEAST : max(E[mt][h] + (int)fmaxf(floorf(d), -400.f), AP_E_LEAST);
-                f = fresh ? 0.f : fast_exp2(d + (float)(E[mt][h] - En));
-                E[mt][h] = En;
-              }
-#pragma unroll
-              for (int i = 0; i < NT; ++i) {
-                acc[mt][i][2 * h] *= f;
-                acc[mt][i][2 * h + 1] *= f;
-              }
+              if (t == 0) sM[warp * ROWS + mt * 16 + g + 8 * h] = x;
             }
+          bar_consumers();
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float* p = sM + mt * 16 + g + 8 * h;
+              top[mt][h] = fmaxf(fmaxf(p[0], p[ROWS]), fmaxf(p[2 * ROWS], p[3 * ROWS]));
+            }
+        };
+        if (consumers_any(grow)) {
+          if (!epilogue_warps_agree(ok)) {                     // a wait ran out: all four warps leave together
+            ok = false;
+            break;
+          }
+          float top[MT][2];
+          row_tops(false, top);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              rescale(mt, h, follow_max<T::SCALED>(m[mt][h], l[mt][h], E[mt][h], top[mt][h]));
         }
-        // P: exp2, times the value scales, to 16 bits; it is the A operand of O += P V as it stands
-        uint4 pa[MT];
+        // P: exp2, times the value scales
         bool over = false;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float mm = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
             const float up = T::SCALED ? pow2i(AP_W_EXP - E[mt][h]) : 1.f;
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
-                float& x = sc[mt][nt][2 * h + c];
+                float& x = sc[mt][n][2 * h + c];
                 x = fast_exp2(x - mm);
                 l[mt][h] += x;
-                if (T::SCALED) {
-                  x *= vs[2 * nt + c];
+                if (T::SCALED && left > 0) {
+                  x *= vs[n][c];
                   over |= fabsf(x * up) >= AP_W_MOST;
                 }
               }
           }
-        }
-        if (T::SCALED && __any_sync(0xffffffffu, over)) {
+        // to 16 bits; a warp's weights are the A operand of its 16 keys' step as they stand
+        auto put_weights = [&]() {
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t pr[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float up = T::SCALED ? pow2i(AP_W_EXP - E[mt][h]) : 1.f;
+#pragma unroll
+              for (int n = 0; n < 2; ++n)
+                pr[2 * n + h] = BF ? pack_bf16(sc[mt][n][2 * h], sc[mt][n][2 * h + 1]) : pack_f16(sc[mt][n][2 * h] * up, sc[mt][n][2 * h + 1] * up);
+            }
+            sP[(mt * 4 + warp) * 32 + lane] = make_uint4(pr[0], pr[1], pr[2], pr[3]);
+          }
+        };
+        put_weights();
+        if (consumers_any(T::SCALED && over)) {
+          float top[MT][2];
+          row_tops(true, top);
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float x = fmaxf(fmaxf(fabsf(sc[mt][0][2 * h]), fabsf(sc[mt][0][2 * h + 1])), fmaxf(fabsf(sc[mt][1][2 * h]), fabsf(sc[mt][1][2 * h + 1])));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-              const int En = max(E[mt][h], (int)(__float_as_uint(x) >> 23) - 127);
-              const float f = E[mt][h] - En < -126 ? 0.f : pow2i(E[mt][h] - En);
-              E[mt][h] = En;
-#pragma unroll
-              for (int i = 0; i < NT; ++i) {
-                acc[mt][i][2 * h] *= f;
-                acc[mt][i][2 * h + 1] *= f;
-              }
-            }
+            for (int h = 0; h < 2; ++h)
+              rescale(mt, h, follow_weight(E[mt][h], top[mt][h]));
+          put_weights();
+          bar_consumers();
         }
+        // O += P V: this warp's columns, 16 keys at a time
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          uint32_t* pr = reinterpret_cast<uint32_t*>(&pa[mt]);
+        for (int k = 0; k < 4; ++k) {
+          if (16 * k >= here) break;
+          uint4 pa[MT];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float up = T::SCALED ? pow2i(AP_W_EXP - E[mt][h]) : 1.f;
+          for (int mt = 0; mt < MT; ++mt) pa[mt] = sP[(mt * 4 + k) * 32 + lane];
+          if (BF) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-              pr[2 * nt + h] = BF ? pack_bf16(sc[mt][nt][2 * h], sc[mt][nt][2 * h + 1])
-                                  : pack_f16(sc[mt][nt][2 * h] * up, sc[mt][nt][2 * h + 1] * up);
-          }
-        }
-        // O += P V
-        if (BF) {
-#pragma unroll
-          for (int c = 0; c < DH / 8; c += 2) {
-            uint32_t v[4];
-            const uint32_t key = jkey + (lane & 15), chunk = c + (lane >> 4);
-            ldsm_x4_t(sv_base + (chunk >> 3) * T::SLAB + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), v);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma16<BF>(acc[mt][c], pa[mt], v[0], v[1]);
-              mma16<BF>(acc[mt][c + 1], pa[mt], v[2], v[3]);
-            }
-          }
-        } else {
-          uint32_t v[4][NT / 4];                              // four keys, NT consecutive columns
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t key = jkey + (i >> 1) * 8 + 2 * t + (i & 1);
-            if (DH == 128) {
-              const uint4 x = lds128(sv_base + key * 128 + ((g ^ (key & 7)) << 4));
-              v[i][0] = x.x; v[i][1] = x.y; v[i][NT / 4 - 2] = x.z; v[i][NT / 4 - 1] = x.w;
-            } else {
-              const uint2 x = lds64(sv_base + key * 64 + (((g >> 1) ^ ((key >> 1) & 3)) << 4) + (g & 1) * 8);
-              v[i][0] = x.x; v[i][1] = x.y;
-            }
-          }
-#pragma unroll
-          for (int w = 0; w < NT / 4; ++w)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              const uint32_t sel = hh ? 0x7362 : 0x5140;
-              uint32_t lo0, hi0, lo1, hi1;
-              codes_to_f16<QK>(__byte_perm(v[0][w], v[1][w], sel), lo0, hi0);
-              codes_to_f16<QK>(__byte_perm(v[2][w], v[3][w], sel), lo1, hi1);
+            for (int c = 0; c < NT; c += 2) {
+              uint32_t v[4];
+              const uint32_t key = 16 * k + (lane & 15), chunk = warp * NT + c + (lane >> 4);
+              ldsm_x4_t(vb + (chunk >> 3) * T::SLAB + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), v);
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) {
-                mma16<BF>(acc[mt][4 * w + 2 * hh], pa[mt], lo0, lo1);
-                mma16<BF>(acc[mt][4 * w + 2 * hh + 1], pa[mt], hi0, hi1);
+                mma16<BF>(acc[mt][c], pa[mt], v[0], v[1]);
+                mma16<BF>(acc[mt][c + 1], pa[mt], v[2], v[3]);
               }
             }
-        }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty(st));
-    }
-
-    // the four warps' results become one
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x = l[mt][h];
-        x += __shfl_xor_sync(0xffffffffu, x, 1);
-        x += __shfl_xor_sync(0xffffffffu, x, 2);
-        if (t == 0) {
-          sM[warp * ROWS + mt * 16 + g + 8 * h] = m[mt][h];
-          sL[warp * ROWS + mt * 16 + g + 8 * h] = x;
-        }
-      }
-    if (!epilogue_warps_agree(ok)) {
-      if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
-      return;
-    }
-    const bool starts = blk0 == 0, ends = blk0 + nblk == s.nb;
-    const long long slot = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * ROWS;
-    if (starts && !ends && threadIdx.x == 0) {
-      const long long last = (u - blk0 + s.nb - 1) / per;    // CTA of the item's last unit
-      a.desc[blockIdx.x] = make_int4(s.r0, tile * ROWS, (valid << 16) | kvh, (int)last);
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      if (mt) bar_consumers();
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = g + 8 * h;
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, sM[w * ROWS + mt * 16 + row]);
-        const float back = T::SCALED ? pow2i(E[mt][h] - AP_W_EXP) : 1.f;
-        const float f = m[mt][h] == -INFINITY ? 0.f : fast_exp2(m[mt][h] - top) * back;
-        float* dst = sJoin + (warp * 16 + row) * T::PITCH;
-        if (BF) {
-#pragma unroll
-          for (int i = 0; i < NT; ++i) {
-            const int col = 8 * i + 2 * t;
-            *reinterpret_cast<float2*>(dst + col + 4 * (col >> 5)) = make_float2(acc[mt][i][2 * h] * f, acc[mt][i][2 * h + 1] * f);
-          }
-        } else {
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < NT; i += 4) {
-              const int col = (2 * t + c) * NT + i;
-              *reinterpret_cast<float4*>(dst + col + 4 * (col >> 5)) =
-                  make_float4(acc[mt][i][2 * h + c] * f, acc[mt][i + 1][2 * h + c] * f, acc[mt][i + 2][2 * h + c] * f, acc[mt][i + 3][2 * h + c] * f);
-            }
-        }
-      }
-      bar_consumers();
-      const int row = threadIdx.x >> 3, part = threadIdx.x & 7, lr = mt * 16 + row;
-      if (lr < valid) {
-        float top = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, sM[w * ROWS + lr]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float mw = sM[w * ROWS + lr];
-          if (mw != -INFINITY) sum += sL[w * ROWS + lr] * fast_exp2(mw - top);
-          else sum += sL[w * ROWS + lr];                     // 0, or NaN from a score that is not a number
-        }
-        const int e = tile * ROWS + lr;
-        const bool whole = starts && ends;
-        const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
-        if (!whole && part == 0) a.ml[slot + lr] = make_float2(top, sum);
-        bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH;
-        float* pt = a.part + (slot + lr) * DH;
-#pragma unroll
-        for (int i = 0; i < DH / 8; i += 4) {
-          const int col = i * 8 + part * 4;                  // the 8 threads of a row take consecutive 16 bytes
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float4 y = *reinterpret_cast<const float4*>(sJoin + (w * 16 + row) * T::PITCH + col + 4 * (col >> 5));
-            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-          }
-          if (whole) {
-            *reinterpret_cast<uint2*>(o + col) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
           } else {
-            *reinterpret_cast<float4*>(pt + col) = x;
+            uint32_t v[4];
+            load_values<DH>(vb, k, warp, g, t, v);
+#pragma unroll
+            for (int hh = 0; hh < NT / 2; ++hh) {
+              // columns 0,1 or 2,3 of the four; with 64 columns in all a lane has two of them
+              const uint32_t sel = (DH == 128 ? hh == 1 : (g & 1) == 1) ? 0x7362 : 0x5140;
+              uint32_t lo0, hi0, lo1, hi1;
+              codes_to_f16<QK>(__byte_perm(v[0], v[1], sel), lo0, hi0);
+              codes_to_f16<QK>(__byte_perm(v[2], v[3], sel), lo1, hi1);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                mma16<BF>(acc[mt][2 * hh], pa[mt], lo0, lo1);
+                mma16<BF>(acc[mt][2 * hh + 1], pa[mt], hi0, hi1);
+              }
+            }
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(st));
       }
+
+      // sums of the four warps' keys
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x = l[mt][h];
+          x += __shfl_xor_sync(0xffffffffu, x, 1);
+          x += __shfl_xor_sync(0xffffffffu, x, 2);
+          if (t == 0) sL[warp * ROWS + mt * 16 + g + 8 * h] = x;
+        }
+      if (!epilogue_warps_agree(ok)) {
+        if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
+        return;
+      }
+      const bool starts = blk0 == 0, whole = starts && nblk == s.nb;
+      const long long slot = ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * ROWS;
+      if (starts && !whole && threadIdx.x == 0) {
+        const long long last = (u + s.nb - 1) / per;           // CTA of the item's last unit
+        a.desc[blockIdx.x] = make_int4(s.r0, tile * ROWS, (valid << 16) | kvh, (int)last);
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = mt * 16 + g + 8 * h;
+          if (row >= valid) continue;
+          const float* p = sL + row;
+          const float sum = (p[0] + p[ROWS]) + (p[2 * ROWS] + p[3 * ROWS]);
+          const int e = tile * ROWS + row;
+          const float f = (T::SCALED ? pow2i(E[mt][h] - AP_W_EXP) : 1.f) * (whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f);
+          bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + warp * (DH / 4);
+          float* part = a.part + (slot + row) * DH + warp * (DH / 4);
+          if (!whole && warp == 0 && t == 0) a.ml[slot + row] = make_float2(m[mt][h], sum);
+          if (BF) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+              const float x = acc[mt][i][2 * h] * f, y = acc[mt][i][2 * h + 1] * f;
+              if (whole) *reinterpret_cast<uint32_t*>(o + 8 * i + 2 * t) = pack_bf16(x, y);
+              else *reinterpret_cast<float2*>(part + 8 * i + 2 * t) = make_float2(x, y);
+            }
+          } else {
+            float x[2 * NT];                                   // consecutive columns 2 NT t ...
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+              x[i] = acc[mt][i][2 * h] * f;
+              x[NT + i] = acc[mt][i][2 * h + 1] * f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * NT; i += 4) {
+              if (whole) *reinterpret_cast<uint2*>(o + 2 * NT * t + i) = make_uint2(pack_bf16(x[i], x[i + 1]), pack_bf16(x[i + 2], x[i + 3]));
+              else *reinterpret_cast<float4*>(part + 2 * NT * t + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            }
+          }
+        }
     }
     u += nblk;
   }
 }
 
 // The pieces of an item that run borders cut: o = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m), in unit order.  CTA
-// (c, y) takes rows y, y + 4, ... of the item that starts in run c; its 8 warps take every eighth piece each.
+// (c, y) has the item that starts in run c.  Of its 8 warps SPLIT take every SPLIT-th piece of a row each: 1 when there are
+// few pieces (a warp per row, 32 rows at once over the grid's 4 y), 8 when there are many.
+template <int DH, int ROWS, int SPLIT> __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const int4& d, float (*sO)[DH], float* sSum) {
+  constexpr int PER = DH / 32, LOADS = 4;
+  const int valid = d.z >> 16, kvh = d.z & 0xffff, n = d.w - (int)blockIdx.x + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SPLIT;
+  auto slot = [&](int i, int row) { return (long long)((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row; };
+  for (int r0 = blockIdx.y * (8 / SPLIT); r0 < valid; r0 += 4 * (8 / SPLIT)) {
+    const int row = r0 + warp / SPLIT;
+    float sum = 0.f, x[PER] = {};
+    if (row < valid) {
+      float top = -INFINITY;
+      for (int i = lane; i < n; i += 32) top = fmaxf(top, a.ml[slot(i, row)].x);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int i0 = sub; i0 < n; i0 += SPLIT * LOADS) {
+        float2 ml[LOADS];
+        float p[LOADS][PER];
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+          const int i = i0 + u * SPLIT;
+          ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+          for (int c = 0; c < PER; ++c) p[u][c] = 0.f;
+          if (i < n) {
+            ml[u] = a.ml[slot(i, row)];
+            const float* src = a.part + slot(i, row) * DH + lane * PER;
+#pragma unroll
+            for (int c = 0; c < PER; c += 2) {
+              const float2 y = *reinterpret_cast<const float2*>(src + c);
+              p[u][c] = y.x;
+              p[u][c + 1] = y.y;
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+          const float w = ml[u].x == -INFINITY ? 0.f : fast_exp2(ml[u].x - top);
+          sum += w * ml[u].y;
+#pragma unroll
+          for (int c = 0; c < PER; ++c) x[c] += w * p[u][c];
+        }
+      }
+    }
+    if (SPLIT > 1) {
+#pragma unroll
+      for (int c = 0; c < PER; ++c) sO[warp][lane * PER + c] = x[c];
+      if (lane == 0) sSum[warp] = sum;
+      __syncthreads();
+      if (sub == 0) {
+#pragma unroll
+        for (int w = 1; w < SPLIT; ++w) {
+          sum += sSum[warp + w];
+#pragma unroll
+          for (int c = 0; c < PER; ++c) x[c] += sO[warp + w][lane * PER + c];
+        }
+      }
+    }
+    if (row < valid && sub == 0) {
+      const int e = d.y + row;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      bf16* o = a.o + (long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + lane * PER;
+#pragma unroll
+      for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(x[c] * inv, x[c + 1] * inv);
+    }
+    if (SPLIT > 1) __syncthreads();
+  }
+}
 template <int DH, int ROWS>
 __global__ void __launch_bounds__(256) attention_paged_join_kernel(const PagedAttnArgs a) {
-  constexpr int PER = DH / 32;
   __shared__ float sO[8][DH];
   __shared__ float sSum[8];
   griddep_wait();
   griddep_launch();
   const int4 d = a.desc[blockIdx.x];
-  const int valid = d.z >> 16, kvh = d.z & 0xffff, n = d.w - (int)blockIdx.x + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int row = blockIdx.y; row < valid; row += gridDim.y) {
-    auto slot = [&](int i) { return (long long)((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row; };
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, a.ml[slot(i)].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float sum = 0.f, x[PER] = {};
-#pragma unroll 4
-    for (int i = warp; i < n; i += 8) {
-      const float2 ml = a.ml[slot(i)];
-      const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
-      sum += w * ml.y;
-      const float* p = a.part + slot(i) * DH + lane * PER;
-#pragma unroll
-      for (int c = 0; c < PER; ++c) x[c] += w * p[c];
-    }
-#pragma unroll
-    for (int c = 0; c < PER; ++c) sO[warp][lane * PER + c] = x[c];
-    if (lane == 0) sSum[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x < DH) {
-      float y = 0.f, l = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        y += sO[i][threadIdx.x];
-        l += sSum[i];
-      }
-      const int e = d.y + row;
-      a.o[(long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + threadIdx.x] =
-          __float2bfloat16_rn(l == 0.f ? 0.f : y / l);
-    }
-    __syncthreads();
-  }
+  if (d.w - (int)blockIdx.x < 16) join_rows<DH, ROWS, 1>(a, d, sO, sSum);
+  else join_rows<DH, ROWS, 8>(a, d, sO, sSum);
 }
 
 namespace {
 
-constexpr int AP_MAX_ROWS = 32, AP_MAX_OCC = 2;
+constexpr int AP_SLOT_ROWS = 128;   // most of (CTAs per SM) x (rows of a tile): 4 x 16, 3 x 32, 2 x 64
 
 // pool [n_pages][Hkv][page_size][head_dim] (or its scales, without the last dimension) in boxes of at most 64 places
 int page_map(CUtensorMap* out, const surelock_paged_kv& c, void* base, bool scales) {
@@ -750,24 +1054,25 @@ int page_map(CUtensorMap* out, const surelock_paged_kv& c, void* base, bool scal
 
 template <int DH, int KIND, int MT>
 int launch_ap(const CUtensorMap* maps, PagedAttnArgs a, long long max_units, void* workspace, cudaStream_t st) {
-  const int smem = ap_smem<DH, KIND, MT>() + (a.B + 1) * 8;
+  using PL = Plan<DH, KIND, MT>;
+  const int smem = PL::SMEM + (a.B + 1) * 8;
   static std::once_flag once;
   static cudaError_t attr;
   std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(attention_paged_kernel<DH, KIND, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                ap_smem<DH, KIND, MT>() + (AP_MAX_B + 1) * 8);
+    attr = cudaFuncSetAttribute(attention_paged_kernel<DH, KIND, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM + (AP_MAX_B + 1) * 8);
   });
   SL_CUDA_TRY(attr);
-  const int occ = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;
+  const int fit = 228 * 1024 / (smem + 1024);   // all CTAs of the grid are resident at once, so equal runs end together
+  const int occ = fit < ap_occupancy<MT>() ? fit : ap_occupancy<MT>();
   const int cap = sm_count() * occ, grid = (int)(max_units < cap ? max_units : cap);
-  const size_t rows = (size_t)sm_count() * AP_MAX_OCC * 2 * AP_MAX_ROWS;
+  const size_t rows = (size_t)sm_count() * AP_SLOT_ROWS * 2;
   a.part = reinterpret_cast<float*>(workspace);
   a.ml = reinterpret_cast<float2*>(a.part + rows * DH);
   a.desc = reinterpret_cast<int4*>(a.ml + rows);
   SL_CUDA_TRY(launch_pdl(attention_paged_kernel<DH, KIND, MT>, dim3(grid), dim3(AP_THREADS), (size_t)smem, st, maps[0], maps[1], maps[2],
                          maps[3], a));
   if (grid > 1 && a.max_tokens > AP_KEYS)   // otherwise no item has two units
-    SL_CUDA_TRY(launch_pdl(attention_paged_join_kernel<DH, 16 * MT>, dim3(grid - 1, 4), dim3(256), 0, st, a));
+    SL_CUDA_TRY(launch_pdl(attention_paged_join_kernel<DH, ap_rows<MT>()>, dim3(grid - 1, 4), dim3(256), 0, st, a));
   return SL_OK;
 }
 
@@ -775,8 +1080,7 @@ int launch_ap(const CUtensorMap* maps, PagedAttnArgs a, long long max_units, voi
 
 size_t attention_paged_workspace_bytes(int head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
-  const size_t ctas = (size_t)sm_count() * AP_MAX_OCC;
-  return ctas * 2 * AP_MAX_ROWS * (head_dim * sizeof(float) + sizeof(float2)) + ctas * sizeof(int4);
+  return (size_t)sm_count() * (AP_SLOT_ROWS * 2 * (head_dim * sizeof(float) + sizeof(float2)) + 4 * sizeof(int4));
 }
 
 int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long q_stride, const int32_t* row_offsets,
@@ -810,12 +1114,16 @@ int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long 
   a.max_tokens = c.max_pages * c.page_size;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c.head_dim);
   a.status = status;
-  // 16 or 32 rows to a tile: two row tiles share the conversions of the codes, but pad more rows
-  const bool wide = (long long)max_rows * a.G > 16ll * B;
-  const int tile_rows = wide ? 32 : 16;
+  // rows of a tile: as many as a sequence has on average share the conversions of the codes; more would be padding
+  const long long rows = ((long long)max_rows * a.G + B - 1) / B;
+  const int mt = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4, tile_rows = mt ? 16 * mt : 8;
   const long long tiles = ((long long)max_rows * a.G + tile_rows - 1) / tile_rows + B;
   const long long max_units = tiles * a.Hkv * ((a.max_tokens + AP_KEYS - 1) / AP_KEYS);
-#define SL_AP(DH, KIND) (wide ? launch_ap<DH, KIND, 2>(maps, a, max_units, workspace, st) : launch_ap<DH, KIND, 1>(maps, a, max_units, workspace, st))
+#define SL_AP(DH, KIND)                                                                                        \
+  (mt == 0   ? launch_ap<DH, KIND, 0>(maps, a, max_units, workspace, st)                                       \
+   : mt == 1 ? launch_ap<DH, KIND, 1>(maps, a, max_units, workspace, st)                                       \
+   : mt == 2 ? launch_ap<DH, KIND, 2>(maps, a, max_units, workspace, st)                                       \
+             : launch_ap<DH, KIND, 4>(maps, a, max_units, workspace, st))
   if (c.head_dim == 128) return c.dtype == SL_BF16 ? SL_AP(128, SL_BF16) : c.dtype == SL_E4M3 ? SL_AP(128, SL_E4M3) : SL_AP(128, SL_INT8);
   return c.dtype == SL_BF16 ? SL_AP(64, SL_BF16) : c.dtype == SL_E4M3 ? SL_AP(64, SL_E4M3) : SL_AP(64, SL_INT8);
 #undef SL_AP

@@ -6,11 +6,11 @@
 // once to 32 bits and, for a bf16 output, once more.  s = 0 (all zero) gives codes 0; a row with an infinity or a NaN gets
 // s = NaN, so that everything read back of it is NaN.
 //
-// Exact rounding without a division per element: y = x * (1 / s) is within 2^-22 of the quotient (two roundings), so when
-// y (1 + 2^-21) and y (1 - 2^-21) round to the same code, that is the code of the exact quotient too.  Otherwise (about one
-// value in 10^5) the quotient is formed truncated with its lowest bit set when it is inexact ("round to odd"), whose
+// Exact rounding without a division per element: x times an approximate 1 / s (2^-23) is within 2^-22 of the quotient, so
+// when the products by (1 + 2^-21) / s and (1 - 2^-21) / s round to the same code, that is the code of the exact quotient
+// too.  Otherwise (about one value in 10^5) the quotient is formed truncated with its lowest bit set when it is inexact ("round to odd"), whose
 // rounding to a code's few bits is that of the exact value.  Rows below 2^-64 are first multiplied by 2^64 (exactly), so
-// that 1 / s stays finite and the remainder in the odd rounding stays representable.
+// that 1 / s is a normal number and the remainder in the odd rounding stays representable.
 //
 // Memory-bound: DH / 8 lanes take one (row, head) of K and of V, 8 elements a lane in 16-byte loads, all loads issued before
 // the first use; the 8-byte stores of a half-warp (DH = 128) fill one 128-byte line, as one head's places in a page are
@@ -35,40 +35,86 @@ int check_paged_kv(const surelock_paged_kv* c) {
 namespace {
 
 constexpr int PK_THREADS = 256;
+constexpr int PK_GATHER = 2;
 
 struct PagedArgs {
   void *k, *v;
   float *ks, *vs;
   const int32_t *table, *idx, *n_active;
   int n_pages, page_shift, max_pages, Hkv, B, N, max_rows;
+  uint32_t div_h, div_n;        // ceil(2^32 / Hkv), ceil(2^32 / N): see fast_div
   long long row_stride;
   int32_t* status;
 };
 
+// x / d by the reciprocal m = ceil(2^32 / d) (0 for d = 1): the product is the quotient or one more
+__device__ __forceinline__ unsigned fast_div(unsigned x, unsigned d, unsigned m) {
+  if (m == 0) return x;
+  const unsigned q = __umulhi(x, m);
+  return q * d > x ? q - 1 : q;
+}
 // slot index ((page * Hkv + h) * page_size + place) of flat position f, or -1
 __device__ __forceinline__ long long paged_slot(const PagedArgs& a, int f, int h) {
   if (f < 0) return -1;
-  const int b = f / a.N, i = f - b * a.N;
+  const int b = (int)fast_div((unsigned)f, (unsigned)a.N, a.div_n), i = f - b * a.N;
   if (b >= a.B || (i >> a.page_shift) >= a.max_pages) return -1;
   const int page = __ldg(a.table + (long long)b * a.max_pages + (i >> a.page_shift));
   if ((unsigned)page >= (unsigned)a.n_pages) return -1;
   return ((((long long)page * a.Hkv + h)) << a.page_shift) + (i & ((1 << a.page_shift) - 1));
 }
 
-// 8 consecutive elements, widened
-__device__ __forceinline__ void load8(const bf16* p, float* x) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// 8 consecutive elements as they are stored
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> { uint4 u; };
+template <> struct Raw8<float> { uint4 u, w; };
+__device__ __forceinline__ void load8(const bf16* p, Raw8<bf16>& r) { r.u = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void load8(const float* p, Raw8<float>& r) {
+  r.u = *reinterpret_cast<const uint4*>(p);
+  r.w = *reinterpret_cast<const uint4*>(p + 4);
+}
+__device__ __forceinline__ void widen8(const Raw8<bf16>& r, float* x) {
+  const uint32_t w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(w[i] << 16);
     x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float* x) {
+  const uint32_t w[8] = {r.u.x, r.u.y, r.u.z, r.u.w, r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+}
+// bits of the largest magnitudes of K's and of V's elements over the lanes of a (row, head) (magnitudes order like their
+// bits, NaN above all); bf16 pairs are compared two at a time, and K's and V's travel together
+template <int LANES> __device__ __forceinline__ void tops(const Raw8<bf16>& k, const Raw8<bf16>& v, uint32_t& tk, uint32_t& tv) {
+  constexpr uint32_t A = 0x7fff7fffu;
+  const uint32_t a = __vmaxu2(__vmaxu2(k.u.x & A, k.u.y & A), __vmaxu2(k.u.z & A, k.u.w & A));
+  const uint32_t b = __vmaxu2(__vmaxu2(v.u.x & A, v.u.y & A), __vmaxu2(v.u.z & A, v.u.w & A));
+  uint32_t both = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+  tk = both << 16;
+  tv = both & 0xffff0000u;
+}
+template <int LANES> __device__ __forceinline__ void tops(const Raw8<float>& k, const Raw8<float>& v, uint32_t& tk, uint32_t& tv) {
+  constexpr uint32_t A = 0x7fffffffu;
+  tk = max(max(max(k.u.x & A, k.u.y & A), max(k.u.z & A, k.u.w & A)), max(max(k.w.x & A, k.w.y & A), max(k.w.z & A, k.w.w & A)));
+  tv = max(max(max(v.u.x & A, v.u.y & A), max(v.u.z & A, v.u.w & A)), max(max(v.w.x & A, v.w.y & A), max(v.w.z & A, v.w.w & A)));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    tk = max(tk, __shfl_xor_sync(0xffffffffu, tk, o));
+    tv = max(tv, __shfl_xor_sync(0xffffffffu, tv, o));
+  }
+}
+// x[0..3] * f, two products to an instruction
+__device__ __forceinline__ void mul4(const float* x, float f, float* y) {
+#pragma unroll
+  for (int i = 0; i < 4; i += 2)
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\t"
+        "mul.rn.f32x2 c, a, b;\n\tmov.b64 {%0, %1}, c;\n\t}"
+        : "=f"(y[i]), "=f"(y[i + 1]) : "f"(x[i]), "f"(x[i + 1]), "f"(f));
 }
 __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -83,7 +129,8 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-// four values -> four codes, lowest byte first; values beyond the largest code become it
+// four values -> four codes, lowest byte first.  e4m3: values beyond the largest code become it.  int8: |value| < 127.5; adding
+// 1.5 x 2^23 rounds to a whole number, to nearest even, and leaves it in the low byte.
 template <int KIND> __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   if (KIND == SL_E4M3) {
     uint16_t lo, hi;
@@ -91,8 +138,10 @@ template <int KIND> __device__ __forceinline__ uint32_t codes4(float a, float b,
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
     return (uint32_t)lo | ((uint32_t)hi << 16);
   } else {
-    auto one = [](float v) { return (uint32_t)(__float2int_rn(fminf(fmaxf(v, -127.f), 127.f)) & 0xff); };
-    return one(a) | (one(b) << 8) | (one(c) << 16) | (one(d) << 24);
+    constexpr float R = 12582912.f;
+    const uint32_t lo = __byte_perm(__float_as_uint(a + R), __float_as_uint(b + R), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(c + R), __float_as_uint(d + R), 0x0040);
+    return __byte_perm(lo, hi, 0x5410);
   }
 }
 // x / s truncated, lowest bit set when inexact: rounds to a shorter format as the exact quotient does
@@ -100,34 +149,36 @@ __device__ __noinline__ float quotient_to_odd(float x, float s) {
   const float q = __fdiv_rz(x, s);
   return __fmaf_rn(-q, s, x) != 0.f ? __uint_as_float(__float_as_uint(q) | 1u) : q;
 }
-
-// quantise the 8 elements of this lane; all LANES lanes of the (row, head) take part.  Returns the scale.
-template <int KIND, int LANES> __device__ __forceinline__ float quantise8(float* x, uint2& out) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);   // orders like the magnitude, NaN above all
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+// quantise the 8 elements of this lane; top = bits of the largest magnitude of the whole (row, head).  Returns the scale.
+template <int KIND> __device__ __forceinline__ float quantise8(float* x, uint32_t top, uint2& out) {
+  constexpr float Q = KvKind<KIND>::QMAX, RQ = 1.f / Q;
   out = make_uint2(0u, 0u);
   if (top >= 0x7f800000u) return __uint_as_float(0x7fffffffu);
   const float amax = __uint_as_float(top);
-  const float scale = __fdiv_rn(amax, KvKind<KIND>::QMAX);
-  if (scale == 0.f) return 0.f;
-  float s = scale;
-  if (amax < 5.421010862427522e-20f) {   // 2^-64
-    s *= 18446744073709551616.f;
+  float scale, s;
+  if (top >= 0x1f800000u) {   // 2^-64
+    // amax / Q, correctly rounded: one residual step from amax * RN(1 / Q) (Markstein's theorem; nothing underflows here)
+    const float q = amax * RQ;
+    scale = s = __fmaf_rn(__fmaf_rn(-q, Q, amax), RQ, q);
+  } else {
+    scale = __fdiv_rn(amax, Q);
+    if (scale == 0.f) return 0.f;
+    s = scale * 18446744073709551616.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= 18446744073709551616.f;
+    for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(x[i] * 18446744073709551616.f, -Q * s), Q * s);   // a subnormal scale may be far from amax / Q
   }
-  const float inv = __fdiv_rn(1.f, s);
-  constexpr float UP = 1.f + 4.76837158e-7f, DOWN = 1.f - 4.76837158e-7f;   // 1 +- 2^-21
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  const float up = inv * (1.f + 4.76837158e-7f), down = inv * (1.f - 4.76837158e-7f);   // 1 +- 2^-21
   uint32_t c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float* p = x + 4 * h;
-    const float y[4] = {p[0] * inv, p[1] * inv, p[2] * inv, p[3] * inv};
-    c[h] = codes4<KIND>(y[0] * UP, y[1] * UP, y[2] * UP, y[3] * UP);
-    if (c[h] != codes4<KIND>(y[0] * DOWN, y[1] * DOWN, y[2] * DOWN, y[3] * DOWN))
+    const float* p = x + 4 * h;
+    float y[4], z[4];
+    mul4(p, up, y);
+    mul4(p, down, z);
+    c[h] = codes4<KIND>(y[0], y[1], y[2], y[3]);
+    if (c[h] != codes4<KIND>(z[0], z[1], z[2], z[3]))
       c[h] = codes4<KIND>(quotient_to_odd(p[0], s), quotient_to_odd(p[1], s), quotient_to_odd(p[2], s), quotient_to_odd(p[3], s));
   }
   out = make_uint2(c[0], c[1]);
@@ -138,34 +189,37 @@ template <int KIND, int DH, typename T>
 __global__ void __launch_bounds__(PK_THREADS)
 kv_scatter_paged_kernel(PagedArgs a, const T* __restrict__ k, const T* __restrict__ v) {
   constexpr int LANES = DH / 8;
+  constexpr int QK = KIND == SL_BF16 ? SL_E4M3 : KIND;
   griddep_wait();
   griddep_launch();
   const int M = min(*a.n_active, a.max_rows);
   const int lane = threadIdx.x % LANES;
-  const long long items = (long long)M * a.Hkv, step = (long long)gridDim.x * (PK_THREADS / LANES);
+  const unsigned items = (unsigned)max(M, 0) * a.Hkv, step = gridDim.x * (PK_THREADS / LANES);
   // the lanes of a warp stay together (they shuffle): the loop bound is taken for the warp's first item
-  for (long long it = (long long)blockIdx.x * (PK_THREADS / LANES) + threadIdx.x / LANES;; it += step) {
-    const long long first = it - (threadIdx.x % 32) / LANES;
-    if (first >= items) return;
+  for (unsigned it = blockIdx.x * (PK_THREADS / LANES) + threadIdx.x / LANES;; it += step) {
+    if (it - (threadIdx.x % 32) / LANES >= items) return;
     const bool live = it < items;
-    const long long w = live ? it : items - 1;
-    const int r = (int)(w / a.Hkv), h = (int)(w - (long long)r * a.Hkv);
-    const long long src = (long long)r * a.row_stride + (long long)h * DH + lane * 8;
-    float xk[8], xv[8];
-    load8(k + src, xk);
-    load8(v + src, xv);
+    const unsigned w = live ? it : items - 1, r = fast_div(w, a.Hkv, a.div_h), h = w - r * a.Hkv;
+    const long long src = r * a.row_stride + (long long)h * DH + lane * 8;
+    Raw8<T> rk, rv;
+    load8(k + src, rk);
+    load8(v + src, rv);
     const long long slot = paged_slot(a, __ldg(a.idx + r), h);
     if (live && slot < 0 && lane == 0 && h == 0) set_status(a.status, SL_DEV_BAD_INDEX);
     const bool put = live && slot >= 0;
+    float xk[8], xv[8];
+    widen8(rk, xk);
+    widen8(rv, xv);
     if (KIND == SL_BF16) {
       if (put) {
         store8((bf16*)a.k + slot * DH + lane * 8, xk);
         store8((bf16*)a.v + slot * DH + lane * 8, xv);
       }
     } else {
+      uint32_t tk, tv;
+      tops<LANES>(rk, rv, tk, tv);
       uint2 ck, cv;
-      const float sk = quantise8<KIND == SL_BF16 ? SL_E4M3 : KIND, LANES>(xk, ck);
-      const float sv = quantise8<KIND == SL_BF16 ? SL_E4M3 : KIND, LANES>(xv, cv);
+      const float sk = quantise8<QK>(xk, tk, ck), sv = quantise8<QK>(xv, tv, cv);
       if (put) {
         *reinterpret_cast<uint2*>((uint8_t*)a.k + slot * DH + lane * 8) = ck;
         *reinterpret_cast<uint2*>((uint8_t*)a.v + slot * DH + lane * 8) = cv;
@@ -195,31 +249,68 @@ template <int KIND> __device__ __forceinline__ void dequantise8(uint2 c, float s
 
 template <int KIND, int DH, typename T>
 __global__ void __launch_bounds__(PK_THREADS) kv_gather_paged_kernel(PagedArgs a, T* __restrict__ k, T* __restrict__ v) {
-  constexpr int LANES = DH / 8;
+  constexpr int LANES = DH / 8, U = PK_GATHER;   // items of a lane group under way at a time: the chain position -> page -> codes is long
+  constexpr int QK = KIND == SL_BF16 ? SL_E4M3 : KIND;
   griddep_wait();
   griddep_launch();
   const int M = min(*a.n_active, a.max_rows);
   const int lane = threadIdx.x % LANES;
-  const long long items = (long long)M * a.Hkv, step = (long long)gridDim.x * (PK_THREADS / LANES);
-  for (long long it = (long long)blockIdx.x * (PK_THREADS / LANES) + threadIdx.x / LANES; it < items; it += step) {
-    const int r = (int)(it / a.Hkv), h = (int)(it - (long long)r * a.Hkv);
-    const long long slot = paged_slot(a, __ldg(a.idx + r), h);
-    float xk[8] = {}, xv[8] = {};
-    if (slot < 0) {
-      if (lane == 0 && h == 0) set_status(a.status, SL_DEV_BAD_INDEX);
-    } else if (KIND == SL_BF16) {
-      load8((const bf16*)a.k + slot * DH + lane * 8, xk);
-      load8((const bf16*)a.v + slot * DH + lane * 8, xv);
-    } else {
-      const uint2 ck = *reinterpret_cast<const uint2*>((const uint8_t*)a.k + slot * DH + lane * 8);
-      const uint2 cv = *reinterpret_cast<const uint2*>((const uint8_t*)a.v + slot * DH + lane * 8);
-      const float sk = a.ks[slot], sv = a.vs[slot];
-      dequantise8<KIND == SL_BF16 ? SL_E4M3 : KIND>(ck, sk, xk);
-      dequantise8<KIND == SL_BF16 ? SL_E4M3 : KIND>(cv, sv, xv);
+  const unsigned items = (unsigned)max(M, 0) * a.Hkv, step = gridDim.x * (PK_THREADS / LANES);
+  for (unsigned it = blockIdx.x * (PK_THREADS / LANES) + threadIdx.x / LANES; it < items; it += U * step) {
+    long long slot[U], dst[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      slot[u] = -2;
+      if (items - it > u * step) {
+        const unsigned w = it + u * step, r = fast_div(w, a.Hkv, a.div_h), h = w - r * a.Hkv;
+        slot[u] = paged_slot(a, __ldg(a.idx + r), h);
+        dst[u] = r * a.row_stride + (long long)h * DH + lane * 8;
+        if (slot[u] < 0 && lane == 0 && h == 0) set_status(a.status, SL_DEV_BAD_INDEX);
+      }
     }
-    const long long dst = (long long)r * a.row_stride + (long long)h * DH + lane * 8;
-    store8(k + dst, xk);
-    store8(v + dst, xv);
+    if (KIND == SL_BF16) {
+      Raw8<bf16> rk[U], rv[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        rk[u].u = rv[u].u = make_uint4(0u, 0u, 0u, 0u);
+        if (slot[u] >= 0) {
+          load8((const bf16*)a.k + slot[u] * DH + lane * 8, rk[u]);
+          load8((const bf16*)a.v + slot[u] * DH + lane * 8, rv[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (slot[u] != -2) {
+          float x[8];
+          widen8(rk[u], x);
+          store8(k + dst[u], x);
+          widen8(rv[u], x);
+          store8(v + dst[u], x);
+        }
+    } else {
+      uint2 ck[U], cv[U];
+      float sk[U], sv[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        ck[u] = cv[u] = make_uint2(0u, 0u);
+        sk[u] = sv[u] = 0.f;
+        if (slot[u] >= 0) {
+          ck[u] = *reinterpret_cast<const uint2*>((const uint8_t*)a.k + slot[u] * DH + lane * 8);
+          cv[u] = *reinterpret_cast<const uint2*>((const uint8_t*)a.v + slot[u] * DH + lane * 8);
+          sk[u] = a.ks[slot[u]];
+          sv[u] = a.vs[slot[u]];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (slot[u] != -2) {
+          float x[8];
+          dequantise8<QK>(ck[u], sk[u], x);
+          store8(k + dst[u], x);
+          dequantise8<QK>(cv[u], sv[u], x);
+          store8(v + dst[u], x);
+        }
+    }
   }
 }
 
@@ -231,20 +322,25 @@ PagedArgs paged_args(const surelock_paged_kv& c, const int32_t* idx, const int32
   a.n_pages = c.n_pages; a.max_pages = c.max_pages; a.Hkv = c.n_kv_heads;
   a.page_shift = 0;
   while ((1 << a.page_shift) < c.page_size) ++a.page_shift;
+  a.div_h = c.n_kv_heads == 1 ? 0u : (uint32_t)(0x100000000ull / c.n_kv_heads + (0x100000000ull % c.n_kv_heads != 0));
+  a.div_n = N == 1 ? 0u : (uint32_t)(0x100000000ull / N + (0x100000000ull % N != 0));
   a.B = B; a.N = N; a.max_rows = max_rows; a.row_stride = row_stride; a.status = status;
   return a;
 }
 
-int paged_grid(const surelock_paged_kv& c, int max_rows) {
-  const long long groups = PK_THREADS / (c.head_dim / 8);
-  const long long want = ((long long)max_rows * c.n_kv_heads + groups - 1) / groups;
-  const long long cap = (long long)sm_count() * 16;
-  return (int)(want < 1 ? 1 : want > cap ? cap : want);
+// a grid that deals every lane group `per` items at once; the kernels still loop should it be cut
+int paged_grid(const surelock_paged_kv& c, int max_rows, int per) {
+  const long long items = (long long)max_rows * c.n_kv_heads, groups = (long long)PK_THREADS / (c.head_dim / 8) * per;
+  if (items > 0x7fffffffll) return -1;   // the kernels count (row, head) pairs in 32 bits
+  const long long want = (items + groups - 1) / groups;
+  return (int)(want < 1 ? 1 : want > (1 << 20) ? 1 << 20 : want);
 }
 
 template <int KIND, int DH>
 int scatter_kind(const surelock_paged_kv& c, const PagedArgs& a, const void* k, const void* v, int dtype, cudaStream_t st) {
-  const dim3 g(paged_grid(c, a.max_rows));
+  const int grid = paged_grid(c, a.max_rows, 1);
+  if (grid < 0) return SL_EUNSUPPORTED;
+  const dim3 g(grid);
   if (dtype == SL_BF16)
     SL_CUDA_TRY(launch_pdl(kv_scatter_paged_kernel<KIND, DH, bf16>, g, dim3(PK_THREADS), 0, st, a, (const bf16*)k, (const bf16*)v));
   else
@@ -254,7 +350,9 @@ int scatter_kind(const surelock_paged_kv& c, const PagedArgs& a, const void* k, 
 
 template <int KIND, int DH>
 int gather_kind(const surelock_paged_kv& c, const PagedArgs& a, void* k, void* v, int dtype, cudaStream_t st) {
-  const dim3 g(paged_grid(c, a.max_rows));
+  const int grid = paged_grid(c, a.max_rows, PK_GATHER);
+  if (grid < 0) return SL_EUNSUPPORTED;
+  const dim3 g(grid);
   if (dtype == SL_BF16)
     SL_CUDA_TRY(launch_pdl(kv_gather_paged_kernel<KIND, DH, bf16>, g, dim3(PK_THREADS), 0, st, a, (bf16*)k, (bf16*)v));
   else
