@@ -107,7 +107,8 @@ def lib() -> C.CDLL:
         "surelock_gemm": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]),
         "surelock_gemm_workspace_bytes": (sz, []),
         "surelock_gemm_fused": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]),
-        "surelock_gemm_quantized": (i32, [vp, C.POINTER(_W4), C.POINTER(_W4), vp, vp, i32, i32, i32, i32, vp]),
+        "surelock_gemm_quantized": (i32, [vp, C.POINTER(_W4), C.POINTER(_W4), vp, vp, i32, i32, i32, i32, vp, vp, vp]),
+        "surelock_gemm_quantized_workspace_bytes": (sz, [i32, i32]),
         "surelock_kv_scatter_paged": (i32, [C.POINTER(_PagedKV), vp, vp, C.c_int64, vp, vp, i32, i32, i32, i32, vp, vp]),
         "surelock_kv_gather_paged": (i32, [C.POINTER(_PagedKV), vp, vp, i32, i32, i32, vp, vp, C.c_int64, i32, vp, vp]),
         "surelock_attention_paged_workspace_bytes": (sz, [i32]),
@@ -456,17 +457,27 @@ def _w4(W, K: int):
     return _W4(_p(codes), _p(scales), _p(zeros), K // ng, _dt(scales))
 
 
-def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None):
+def surelock_gemm_quantized_workspace_bytes(max_rows: int, K: int) -> int:
+    return lib().surelock_gemm_quantized_workspace_bytes(max_rows, K)
+
+
+def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, workspace=None, dev_status=None):
     """4-bit weights W = (codes, scales, zeros or None); epilogue 0: Cout (bf16) = A W^T; 1: Cout (fp32) += A W^T;
-    2: Cout (bf16) = silu(A W^T) * (A W2^T)."""
+    2: Cout (bf16) = silu(A W^T) * (A W2^T).  workspace: uint8 CUDA tensor of surelock_gemm_quantized_workspace_bytes(M, K)
+    bytes that no call running at the same time uses; None takes one from torch's allocator for this call."""
     M, K = A.shape
     n = W[0].shape[0]
     if A.dtype != torch.bfloat16 or Cout.dtype != (torch.float32 if epilogue == 1 else torch.bfloat16) or tuple(Cout.shape) != (M, n):
         raise SurelockError("surelock_gemm_quantized: A bf16 [M][K], Cout [M][n_out] (fp32 with epilogue 1, else bf16)")
     if W2 is not None and W2[0].shape[0] != n:
         raise SurelockError("surelock_gemm_quantized: W and W2 must have the same features")
+    need = surelock_gemm_quantized_workspace_bytes(M, K)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=A.device)
+    if workspace.nbytes < need:
+        raise SurelockError("surelock_gemm_quantized: workspace too small")
     _check(lib().surelock_gemm_quantized(_p(A), C.byref(_w4(W, K)), C.byref(_w4(W2, K)) if W2 is not None else None, _p(Cout),
-                                         _p(n_active), M, n, K, epilogue, _stream()), "surelock_gemm_quantized")
+                                         _p(n_active), M, n, K, epilogue, _p(workspace), _p(dev_status), _stream()), "surelock_gemm_quantized")
 
 
 # ---- paged K/V cache ---------------------------------------------------------------------------------------

@@ -1037,8 +1037,8 @@ static int w4_check(const surelock_w4* W, int K) {
 }
 
 int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active,
-                            int max_rows, int n_out, int K, int epilogue, void* stream) {
-  if (!A || !C || !n_active || max_rows < 0 || n_out <= 0 || K <= 0) return SL_EINVAL;
+                            int max_rows, int n_out, int K, int epilogue, void* workspace, int32_t* dev_status, void* stream) {
+  if (!A || !C || !n_active || !workspace || max_rows < 0 || n_out <= 0 || K <= 0) return SL_EINVAL;
   if (epilogue != EPI_STORE && epilogue != EPI_RESIDUAL && epilogue != EPI_SWIGLU) return SL_EINVAL;
   int rc = w4_check(W, K);
   if (rc == SL_OK && epilogue == EPI_SWIGLU) {
@@ -1046,10 +1046,14 @@ int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_
     if (rc == SL_OK && (W2->group != W->group || W2->scale_dtype != W->scale_dtype || !W2->zeros != !W->zeros)) rc = SL_EINVAL;
   }
   if (rc != SL_OK) return rc;
-  if (reinterpret_cast<uintptr_t>(A) & 15) return SL_EUNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(A) & 15) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return SL_EUNSUPPORTED;
   if (max_rows == 0) return SL_OK;
-  return launch_gemm_quantized(A, W, epilogue == EPI_SWIGLU ? W2 : nullptr, C, n_active, max_rows, n_out, K, epilogue,
-                               (cudaStream_t)stream);
+  return launch_gemm_quantized(A, W, epilogue == EPI_SWIGLU ? W2 : nullptr, C, n_active, max_rows, n_out, K, epilogue, workspace,
+                               dev_status, (cudaStream_t)stream);
+}
+
+size_t surelock_gemm_quantized_workspace_bytes(int max_rows, int K) {
+  return max_rows < 0 || K <= 0 ? 0 : gemm_quantized_workspace_bytes(max_rows, K);
 }
 
 int surelock_update_mask(const float* conf, const int32_t* argmax, const int32_t* active_idx, const int32_t* row_offsets,

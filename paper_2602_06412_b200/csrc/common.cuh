@@ -174,7 +174,8 @@ size_t gemm_chain_workspace_bytes(int np_max);
 
 // products with 4-bit weights (gemm_quantized.cu); W2 only for EPI_SWIGLU
 int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active, int max_rows,
-                          int n_out, int K, int epilogue, cudaStream_t st);
+                          int n_out, int K, int epilogue, void* workspace, int32_t* status, cudaStream_t st);
+size_t gemm_quantized_workspace_bytes(int max_rows, int K);
 
 // optional un-locking (unlock.cu)
 int launch_invert_mask(const uint8_t* lock, uint8_t* inv, int total, cudaStream_t st);

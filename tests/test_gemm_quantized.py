@@ -41,15 +41,15 @@ def test_refusals_on_the_host():
     build_mod.build()
     L = SL.lib()
     W = lambda **o: ctypes.byref(SL._W4(**{**dict(codes=0x1000, scales=0x2000, zeros=None, group=64, scale_dtype=SL.SL_BF16), **o}))
-    good = [0x100, W(), None, 0x200, 0x300, 4, 10, 128, 0, None]
+    good = [0x100, W(), None, 0x200, 0x300, 4, 10, 128, 0, 0x1000, None, None]
     cases = [(0, None, -1), (1, None, -1), (3, None, -1), (4, None, -1), (5, -1, -1), (6, 0, -1), (7, 0, -1), (7, 96, -1), (8, 3, -1), (8, -1, -1),
              (1, W(codes=None), -1), (1, W(scales=None), -1), (1, W(group=0), -1), (1, W(scale_dtype=SL.SL_INT8), -1), (1, W(group=16), -5),
-             (1, W(codes=0x1008), -5), (0, 0x108, -5), (8, 2, -1), (5, 0, 0)]
+             (1, W(codes=0x1008), -5), (0, 0x108, -5), (8, 2, -1), (9, None, -1), (9, 0x1080, -5), (5, 0, 0)]
     for at, value, rc in cases:
         bad = list(good)
         bad[at] = value
         assert L.surelock_gemm_quantized(*bad) == rc, (at, value)
-    swiglu = [0x100, W(), W(), 0x200, 0x300, 4, 10, 128, 2, None]
+    swiglu = [0x100, W(), W(), 0x200, 0x300, 4, 10, 128, 2, 0x1000, None, None]
     for w2 in (W(group=32), W(scale_dtype=SL.SL_FP32), W(zeros=0x3000), W(codes=None)):
         swiglu[2] = w2
         assert L.surelock_gemm_quantized(*swiglu) == -1
