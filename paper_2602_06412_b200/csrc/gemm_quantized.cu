@@ -7,25 +7,29 @@
 // their scales, are streamed once; the instructions that make operands of the codes come next, 46 codes per clock and SM at
 // the memory's rate.
 //
-// A 4-bit code in a byte IS a number of the e4m3 format: the byte u = 0 ... 15 means u 2^-9 (subnormal up to 7, then exponent
-// field 1).  So the codes enter an 8-bit tcgen05.mma after three instructions per eight of them (even and odd ones masked
-// into two words), and the activations take the other side of the bargain: a small kernel in front splits every row, group
-// by group of k, into two e4m3 terms, a = 2^e (t1 + t2), e from the group's largest magnitude in the row.  A bf16 number's 8
-// bits are 4 + 4, so the split is exact down to 2^-9 of that magnitude, and off by at most 2^-17 of it below.  Per group
-//   sum_k (u - z) a = 2^(e + 9) (D - z q),   D = sum_k (u 2^-9) (t1 + t2),   q = 2^-9 sum_k (t1 + t2),
-// D from the products (both terms into one accumulator), q and 2^e from the splitting kernel; the bracket is formed in fp32
-// and multiplied by its group's scale in fp32, so a weight is never rounded.
-// The weights are the 128-row operand, read from TENSOR MEMORY: one thread per feature takes its codes from a TMA stage and
-// stores twice as many bytes there.  The rows' terms, NP = 16 ... 128 rows, are the N operand, by TMA.
-//   warps 0-7  feature 32 (w % 4) + lane; w / 4 = half of the k of a step for unpacking, half of the rows for adding up
-//   warp 8     one thread issues the TMA copies: codes (128 features x 128 bytes per matrix), terms, q and 2^e of a stage's 256 k
-//   warp 9     one thread issues the MMAs of a step, 8 per 128 k
-// The eight warps unpack step i into one of two operand tiles while the MMAs of step i - 1 run, hand it over and add up step
-// i - 1; with two sets of accumulators (where tensor memory has room) it is handed over before that.  The first codes are
-// requested before the splitting kernel has finished: it does not write them.
-// Many features: a CTA goes on from tile to tile, results are stored from the registers.  Few: K is split over the CTAs of a
-// cluster, whose sums meet through distributed shared memory in a fixed order: deterministic.  With SwiGLU a step is two
-// tiles, gate and up, that share the rows' terms.  All waits are bounded.
+// A 4-bit code alone in 16 bits IS an fp16 number: u 2^-24 (subnormal) in the lowest bits, u 2^-20 four bits up.  So eight
+// codes become operands of 16-bit matrix instructions with four masks and one shift, (0,4) (1,5) of the word and (2,6) (3,7)
+// of the word shifted by 8 (11 instructions to make bf16 numbers of them); the factor 16 between the pairs is taken out of the
+// activations, which a small kernel in front rewrites once: per row and group of k as fp16 numbers a' = a 2^-e, the largest
+// magnitude 2^14 ... 2^15, every other pair over 16.  fp16 has 11 bits to bf16's 8, so this is exact down to 2^-25 of the
+// largest magnitude and off by at most 2^-36 of it below.  Per group
+//   sum_k (u - z) a = 2^(e + 24) (D - z q),   D = sum_k (u 2^-24) a',   q = 2^-24 sum_k a',
+// D from the products, q and 2^e from the rewriting kernel; the bracket is formed in fp32 and multiplied by its group's scale
+// in fp32, so a weight is never rounded.
+//
+// mma.sync m16n8k16 with 16 features as the rows and 8 packed rows as the columns: 970 multiply-adds per clock and SM
+// measured, enough for some 20 rows at the memory's rate.  Warps work alone, each on 32 features, and many of them hide each
+// other's steps.  (tcgen05 with the codes as the tensor-memory operand was built with bf16 and with e4m3 operands: unpack ->
+// tensor memory -> product -> back per group is a chain of ~1000 clocks per 256 k that 16 warps per SM did not hide: 84 - 116
+// us for 8 rows of the 4096 x 126464 head.  mma.sync with e4m3 operands converts them to fp16 on the way: 77 us.)
+//   warps 0-3  32 features each (with SwiGLU 16 of the gate and the same 16 of the up matrix), all k of the CTA's range
+//   warp 4     one thread issues the copies: a stage is 256 k, 128 bytes of codes of 128 features by TMA (128-byte swizzle)
+//              and the rewritten rows, already in the order of the MMA fragments, as one bulk copy
+// The contraction index is permuted within 32 ... 128 k (a lane owns 16, 8 or 4 code bytes of a feature, for groups of 128,
+// 64, 32), and the features within 8 (by bit reversal), so that the code loads touch all banks.
+// The first codes are requested before the rewriting kernel has finished: it does not write them.  K is split over the CTAs
+// of a cluster when the features alone do not fill the GPU; the sums meet through distributed shared memory in a fixed
+// order: deterministic.  All waits are bounded.
 #include <cuda_fp16.h>
 
 #include <mutex>
@@ -36,39 +40,24 @@ namespace sl {
 
 namespace {
 
-constexpr int GQ_THREADS = 320;
-constexpr int GQ_BK = 256;             // k per stage: 128 bytes of a feature's codes (64-byte rows stream at two thirds of the rate)
+constexpr int GQ_THREADS = 160;
+constexpr int GQ_BK = 256;             // k per stage
 constexpr int GQ_CODES = 128 * GQ_BK / 2;
+constexpr int GQ_TERMS = 8 * GQ_BK * 2;   // bytes of 8 rewritten rows in a stage
 
 struct GqArgs {
-  const uint8_t* zeros[2];
+  const uint8_t *zeros[2], *terms;
   const void* scales[2];
   void* C;
   const int32_t* n_active;
   int max_rows, n_out, K, ng;
-  int vec;                             // a 16-byte load of scales (and the zero points with it) is aligned
+  int pairs;                           // scales and zero points of two neighbouring groups lie on aligned addresses
   int32_t* status;
 };
 
-__device__ __forceinline__ void gq_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum)
-      : "memory");
-}
-__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
+__device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
   float4 v;
@@ -80,126 +69,78 @@ __device__ __forceinline__ uint4 gq_lds128(uint32_t a) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
   return r;
 }
-__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ float gq_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
-// Scales and zero points of one feature, group after group: 16 bytes of scales (8 bf16 or 4 fp32) with their zero points at a
-// time, the next ones requested one such chunk ahead.
+// Scales and zero points of one feature, shared out over the four lanes that work on it: a chunk of 8 groups (bf16 scales,
+// two groups per lane) or 4 (fp32, one per lane); the next chunk is requested when one begins.  Zero points are kept like
+// the scales, negated.
 template <bool FP32> struct GroupReader {
   static constexpr int CHUNK = FP32 ? 4 : 8;
-  const uint8_t *s0, *z0;      // of feature 0; z0 may be null
-  const uint8_t *s, *z;        // of the present feature
-  uint32_t c[4], n[4];         // present and next chunk of scales
-  uint32_t cz[2], nz[2];       // ... and of zero points
-  int grp, end, ng;            // next group, end of this CTA's range, groups of the feature
-  bool vec;
+  const uint8_t *s, *z;        // of the feature; z may be null
+  uint32_t c, cz, n, nz;       // present and next chunk
 
-  __device__ __forceinline__ void fetch(int g0) {   // chunk of groups from g0 (a multiple of the chunk) -> n, nz
-    if (g0 >= end) return;
-    if (vec) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(s + (size_t)g0 * (FP32 ? 4 : 2)));
-      n[0] = x.x; n[1] = x.y; n[2] = x.z; n[3] = x.w;
-      if (z) {
-        nz[0] = __ldg(reinterpret_cast<const uint32_t*>(z + g0));
-        if (!FP32) nz[1] = __ldg(reinterpret_cast<const uint32_t*>(z + g0 + 4));
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < CHUNK; ++i)                   // features whose scales do not start on 16-byte boundaries
-      if (g0 + i < ng) {
-        if (FP32) n[i & 3] = __ldg(reinterpret_cast<const uint32_t*>(s) + g0 + i);
-        else n[i >> 1] = __byte_perm(n[i >> 1], __ldg(reinterpret_cast<const uint16_t*>(s) + g0 + i), i & 1 ? 0x5410 : 0x3254);
-        if (z) {
-          const uint32_t x = (uint32_t)__ldg(z + g0 + i) << (8 * (i & 3));
-          nz[i >> 2] = (nz[i >> 2] & ~(0xffu << (8 * (i & 3)))) | x;
-        }
-      }
-  }
-  __device__ __forceinline__ void rotate() {          // drop the first group of the chunk
+  __device__ __forceinline__ void fetch(int g0, int t, int ng, bool pairs) {   // chunk of groups from g0 -> n, nz
     if (FP32) {
-      c[0] = c[1]; c[1] = c[2]; c[2] = c[3];
+      const int g = g0 + t;
+      n = g < ng ? __ldg(reinterpret_cast<const uint32_t*>(s) + g) : 0u;
+      nz = __float_as_uint(z && g < ng ? -(float)__ldg(z + g) : -8.f);
     } else {
-      c[0] = __funnelshift_r(c[0], c[1], 16); c[1] = __funnelshift_r(c[1], c[2], 16); c[2] = __funnelshift_r(c[2], c[3], 16); c[3] >>= 16;
+      const int g = g0 + 2 * t;
+      uint32_t a = 8, b = 8;
+      n = 0;
+      if (pairs) {
+        if (g < ng) {
+          n = __ldg(reinterpret_cast<const uint32_t*>(s + 2 * (size_t)g));
+          if (z) {
+            const uint32_t y = __ldg(reinterpret_cast<const uint16_t*>(z + g));
+            a = y & 0xffu;
+            b = y >> 8;
+          }
+        }
+      } else {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(s);
+        if (g < ng) n = __ldg(p + g);
+        if (g + 1 < ng) n |= (uint32_t)__ldg(p + g + 1) << 16;
+        if (z && g < ng) a = __ldg(z + g);
+        if (z && g + 1 < ng) b = __ldg(z + g + 1);
+      }
+      nz = pack_bf16(-(float)a, -(float)b);
     }
-    cz[0] = __funnelshift_r(cz[0], cz[1], 8);
-    cz[1] >>= 8;
   }
-  __device__ __forceinline__ void turn() {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = n[i];
-    cz[0] = nz[0];
-    cz[1] = nz[1];
-  }
-  __device__ __forceinline__ void begin(long long feature, int g, int e) {   // requests the first chunk
-    s = s0 + feature * ng * (FP32 ? 4 : 2);
-    z = z0 ? z0 + feature * ng : nullptr;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) n[i] = 0;
-    nz[0] = nz[1] = 0x08080808u;
-    grp = g;
-    end = e;
-    fetch(g & ~(CHUNK - 1));
-  }
-  __device__ __forceinline__ void prime() {                                  // before the first next()
-    const int at = grp & ~(CHUNK - 1);
-    turn();
-    fetch(at + CHUNK);
-    for (int i = at; i < grp; ++i) rotate();
-  }
-  // scale times 2^9 and minus the zero point of the next group (behind the feature's last one anything finite: its D and q are 0)
-  __device__ __forceinline__ void next(float& scale, float& minus_z) {
-    scale = __uint_as_float(FP32 ? c[0] : c[0] << 16) * 512.f;
-    minus_z = -(float)(cz[0] & 0xffu);
-    ++grp;
-    if ((grp & (CHUNK - 1)) == 0) {
-      turn();
-      fetch(grp + CHUNK);
-    } else {
-      rotate();
-    }
+  // group g: scale and minus the zero point (behind the feature's last group anything finite: its D and q are 0)
+  template <int ODD> __device__ __forceinline__ void get(int g, int lane, float& scale, float& minus_z) const {
+    const int src = (lane & 28) | (FP32 ? g & 3 : (g >> 1) & 3);
+    const uint32_t x = __shfl_sync(0xffffffffu, c, src), y = __shfl_sync(0xffffffffu, cz, src);
+    scale = __uint_as_float(FP32 ? x : ODD ? x & 0xffff0000u : x << 16);
+    minus_z = __uint_as_float(FP32 ? y : ODD ? y & 0xffff0000u : y << 16);
   }
 };
 
-template <int G, int NP, bool DUAL> struct GqPlan {
-  static constexpr int T = DUAL ? 2 : 1;
+template <int G, int NT> struct GqPlan {
   static constexpr int GPT = GQ_BK / G;                       // groups per stage
-  static constexpr int KS = NP <= 32 && GPT * NP <= 64 ? GQ_BK : GQ_BK / 2;   // k per step: as the accumulators' columns allow
-  static constexpr int H = GQ_BK / KS;                        // steps per stage and matrix
-  static constexpr int GPS = KS / G;                          // groups per step
-  static constexpr int SLAB = NP * 128;                       // bytes of one term of NP rows of 128 k
-  static constexpr int TERMS = 4 * SLAB;                      // t1 and t2 of the first 128 k, then of the second
-  static constexpr int SUMS = GPT * NP * 8;                   // q and 2^e of a stage
-  static constexpr int LOADED = T * GQ_CODES + TERMS + SUMS;
-  static constexpr int STAGE = T * GQ_CODES + TERMS + (SUMS + 1023) / 1024 * 1024;
-  static constexpr uint32_t A_COLS = KS / 4, D_COL = 2 * A_COLS, D_COLS = GPS * NP;   // two operand tiles, then accumulators
-  static constexpr bool TWICE = D_COL + 2 * D_COLS <= 512;    // two sets of accumulators
-  static constexpr uint32_t USED = D_COL + (TWICE ? 2 : 1) * D_COLS, COLS = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
-  static constexpr int OCC = NP * T <= 32 && COLS <= 256 ? 2 : 1;
-  static constexpr int ROOM = (OCC == 2 ? 112 : 220) * 1024 - 2048;
-  static constexpr int STAGES = ROOM / STAGE > 6 ? 6 : ROOM / STAGE;
-  static constexpr int PITCH = T * 128;                       // floats per packed row of the partial sums
-  static constexpr int SMEM = 1024 + STAGES * STAGE + 512;
-  static_assert(USED <= 512, "tensor memory");
-  static_assert(STAGES >= 2 && NP * PITCH * 4 <= STAGES * STAGE, "partial sums take the place of the stages");
+  static constexpr int CHUNK = GQ_TERMS + GPT * 64;           // 8 rewritten rows, then their (q, 2^(e + 12)): [group][row]
+  static constexpr int STAGE = GQ_CODES + (NT * CHUNK + 1023) / 1024 * 1024;
+  static constexpr int OCC = NT <= 2 ? 4 : NT <= 4 ? 3 : 2;
+  static constexpr int ROOM = 228 * 1024 / OCC - 1024 - 1024 - 256;
+  static constexpr int STAGES = ROOM / STAGE > 4 ? 4 : ROOM / STAGE;
+  static constexpr int PITCH = 132;                           // floats per packed row of the partial sums
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 256;
+  static_assert(STAGES >= 2 && NT * 8 * PITCH * 4 <= STAGES * STAGE, "partial sums take the place of the stages");
 };
 
-// ---- the rows' terms -------------------------------------------------------------------------------------------------
-// 8 k per thread; per (row, group): e from the largest magnitude, a' = a 2^-e in [-256, 256], t1 = e4m3(a'), t2 = e4m3(a' -
-// t1); the bytes of 8 k in the order 0 2 4 6 1 3 5 7 in which the codes come out of their words.  A group with an infinity
-// or a NaN is NaN throughout.  terms: [2][max_rows][Kp], Kp = K rounded up to 256, zeros behind K; sums: [Kp / g][ld] of (q, 2^e).
+// ---- the rewritten rows ----------------------------------------------------------------------------------------------
+// 8 k per thread; per (row, group) e from the largest magnitude.  A group with an infinity or a NaN is NaN throughout.  Out:
+// per (256 k, 8 rows) one chunk of GqPlan::CHUNK bytes, [word of a code fragment][lane] of 16 bytes: a' of the 8 k whose
+// codes that word holds, in the order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16); then (2^-24 sum a', 2^(e + 12)); zeros behind K.
 constexpr int GS_THREADS = 256;
 
 template <int G>
 __global__ void __launch_bounds__(GS_THREADS)
-gq_split_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, int Kp, int ld,
-                     uint8_t* __restrict__ terms, float2* __restrict__ sums) {
+gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, uint8_t* __restrict__ terms) {
   griddep_wait();
   griddep_launch();
   const int r = blockIdx.y, i = blockIdx.x * GS_THREADS + threadIdx.x;
@@ -212,148 +153,108 @@ gq_split_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_a
   for (int o = 1; o < G / 8; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
   top = max(top & 0xffffu, top >> 16);
   const bool bad = top >= 0x7f80u;
-  int e = (int)(top >> 7) - 127 - 7;                 // the largest magnitude becomes 128 ... 256
+  int e = (int)(top >> 7) - 127 - 14;                // the largest magnitude becomes 2^14 ... 2^15
   if (top == 0 || bad) e = 0;
-  e = max(e, -133);                                  // subnormal numbers
+  e = max(e, -140);                                  // subnormal numbers
   const float d0 = gq_pow2(-e / 2), d1 = gq_pow2(-e - (-e / 2));
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   float x[8], sum = 0.f;
-  uint32_t t1[2] = {}, t2[2] = {};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     x[2 * j] = __uint_as_float(w[j] << 16) * d0 * d1;
     x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) * d0 * d1;
   }
-  auto widen = [](uint16_t two) {
-    uint32_t f;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(two));
-    return __half22float2(*reinterpret_cast<const __half2*>(&f));
-  };
+  uint32_t out[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)                        // even k, odd k
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int a = 4 * j + h, b = a + 2;
-      uint16_t c, d;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x[b]), "f"(x[a]));
-      const float2 high = widen(c);
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(x[b] - high.y), "f"(x[a] - high.x));
-      const float2 low = widen(d);
-      t1[h] |= (uint32_t)c << (16 * j);
-      t2[h] |= (uint32_t)d << (16 * j);
-      sum += (high.x + low.x) + (high.y + low.y);
-    }
-  if (bad) {
-    t1[0] = t1[1] = 0x7f7f7f7fu;
-    sum = __uint_as_float(0x7fffffffu);
+  for (int j = 0; j < 4; ++j) {
+    const float f = j & 1 ? 0.0625f : 1.f;
+    const __half2 h = __floats2half2_rn(x[j] * f, x[j + 4] * f);
+    const float2 back = __half22float2(h);           // what the products see
+    sum += (back.x + back.y) * (j & 1 ? 16.f : 1.f);
+    out[j] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
   }
+  if (bad) sum = __uint_as_float(0x7fffffffu);
 #pragma unroll
   for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (i < Kp / 8) {
-    const long long at = (long long)r * Kp + 8 * i;
-    *reinterpret_cast<uint2*>(terms + at) = make_uint2(t1[0], t1[1]);
-    *reinterpret_cast<uint2*>(terms + (long long)max_rows * Kp + at) = make_uint2(t2[0], t2[1]);
-    if (i % (G / 8) == 0) sums[(long long)(i / (G / 8)) * ld + r] = make_float2(sum * 0.001953125f, ldexpf(1.f, e));
+  const int block = i / 32, k8 = i % 32, in = k8 % 16;
+  if (block < (K + GQ_BK - 1) / GQ_BK) {
+    const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
+    const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
+    uint8_t* chunk = terms + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
+    *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) =
+        make_uint4(out[0], out[1], out[2], out[3]);
+    if (k8 % (G / 8) == 0)
+      *reinterpret_cast<float2*>(chunk + GQ_TERMS + k8 / (G / 8) * 64 + (r % 8) * 8) = make_float2(sum * 5.9604644775390625e-8f, ldexpf(1.f, e + 12));
   }
 }
 
 }  // namespace
 
-template <int G, int NP, bool DUAL, bool FP32>
-__global__ void __launch_bounds__(GQ_THREADS, GqPlan<G, NP, DUAL>::OCC)
-gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2,
-                      const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmQ, const GqArgs a,
-                      const int epilogue) {
-  using P = GqPlan<G, NP, DUAL>;
-  constexpr int T = P::T, H = P::H, GPS = P::GPS, HC = NP / 2;   // HC: rows that a thread adds up
-  constexpr int SPS = T * H;                                  // steps per stage: for every part of its k, gate then up
+template <int G, int NT, bool DUAL, bool FP32>
+__global__ void __launch_bounds__(GQ_THREADS, GqPlan<G, NT>::OCC)
+gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2, const GqArgs a, const int epilogue) {
+  using P = GqPlan<G, NT>;
+  constexpr int TO = DUAL ? 64 : 128;                         // output features of the CTA
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  float* sRed = reinterpret_cast<float*>(smem);               // [NP][PITCH] after the last step
+  float* sRed = reinterpret_cast<float*>(smem);               // [8 NT][PITCH] after the last stage
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + P::STAGES * P::STAGE);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (P::STAGES + s); };
-  auto a_full = [&](int i) { return bar0 + 8u * (2 * P::STAGES + (i & 1)); };       // of step i: operand tile written
-  auto done = [&](int i) { return bar0 + 8u * (2 * P::STAGES + 2 + (i & 1)); };     // of step i: MMAs finished
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 2 * P::STAGES + 4);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(bars + 2 * P::STAGES);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < P::STAGES; ++i) {
       mbar_init(full(i), 1);
-      mbar_init(empty(i), 8 + 8 + 1);                         // readers of the codes, of q (a step later), and the MMAs
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(a_full(i), 8);
-      mbar_init(done(i), 1);
+      mbar_init(empty(i), 4);
     }
     *s_abort = 0;
     fence_mbar_init();
   }
-  if (warp == 9) tc_alloc(smem_u32(s_tmem), P::COLS);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *s_tmem;
 
   uint32_t S, rank = 0;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(S));
   if (S > 1) rank = cluster_ctarank();
-  const int r0 = blockIdx.y * NP, tiles = (a.n_out + 127) / 128;
-  const int tile0 = blockIdx.x / S, tile_step = gridDim.x / S;   // a cluster of more than one CTA has one tile
-  // *n_active, the weights and C were written before the splitting kernel began; its terms come after griddep_wait()
+  const int n0 = (int)(blockIdx.x / S) * TO, r0 = blockIdx.y * 8 * NT;
+  // *n_active, the weights and C were written before the rewriting kernel began; its rows come after griddep_wait()
   const int M = min(*a.n_active, a.max_rows) - r0;            // rows of this tile; none: the whole cluster leaves
   const int nblk = (a.K + GQ_BK - 1) / GQ_BK;
   const int b0 = (int)((long long)nblk * rank / S), b1 = (int)((long long)nblk * (rank + 1) / S);
-  const int my_tiles = M > 0 && tile0 < tiles ? (tiles - tile0 + tile_step - 1) / tile_step : 0;
-  const int nstage = b1 - b0, per_tile = nstage * SPS, steps = my_tiles * per_tile;
+  const int n = M > 0 ? b1 - b0 : 0;
 
-  float acc[T][HC];
-  auto clear = [&]() {
+  float acc[2][NT][4];
 #pragma unroll
-    for (int i = 0; i < T; ++i)
+  for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int c = 0; c < HC; ++c) acc[i][c] = 0.f;
-  };
-  clear();
+    for (int j = 0; j < NT; ++j) acc[mt][j][0] = acc[mt][j][1] = acc[mt][j][2] = acc[mt][j][3] = 0.f;
 
-  if (warp == 8) {
+  if (warp == 4) {
     if (lane == 0) {
       const uint64_t once = gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();   // a code is read once per row tile
-      const int n = my_tiles * nstage, ahead = min(n, P::STAGES);
-      int ct = tile0, cb = b0;                                // tile and block of the next codes
+      const int row_tiles = (a.max_rows + 7) / 8, mine = min(NT, row_tiles - r0 / 8), ahead = min(n, P::STAGES);
       auto codes = [&](int i) {
         const int st = i % P::STAGES;
         const uint32_t at = smem_u32(smem + st * P::STAGE);
-        mbar_expect_tx(full(st), P::LOADED);
-        tma_load_2d_hint(at, &tmW, cb * (GQ_BK / 2), ct * 128, full(st), once);
-        if (DUAL) tma_load_2d_hint(at + GQ_CODES, &tmW2, cb * (GQ_BK / 2), ct * 128, full(st), once);
-        if (++cb == b1) {
-          cb = b0;
-          ct += tile_step;
-        }
+        mbar_expect_tx(full(st), GQ_CODES + mine * P::CHUNK);
+        tma_load_2d_hint(at, &tmW, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
+        if (DUAL) tma_load_2d_hint(at + GQ_CODES / 2, &tmW2, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
       };
       for (int i = 0; i < ahead; ++i) codes(i);
       griddep_wait();
       griddep_launch();
       bool ok = true;
-      int i = 0, b = b0;
+      int i = 0;
       for (; i < n; ++i) {
         const int st = i % P::STAGES;
         if (i >= ahead) {
           if (!(ok = mbar_wait(empty(st), ((i / P::STAGES) & 1) ^ 1, s_abort))) break;
           codes(i);
         }
-        const uint32_t at = smem_u32(smem + st * P::STAGE) + T * GQ_CODES;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          tma_load_2d(at + (2 * k) * P::SLAB, &tmT, b * GQ_BK + k * 128, r0, full(st));
-          tma_load_2d(at + (2 * k + 1) * P::SLAB, &tmT, b * GQ_BK + k * 128, a.max_rows + r0, full(st));
-        }
-        tma_load_2d(at + P::TERMS, &tmQ, 2 * r0, b * P::GPT, full(st));
-        if (++b == b1) b = b0;
+        bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.terms + ((long long)(b0 + i) * row_tiles + r0 / 8) * P::CHUNK,
+                  (uint32_t)(mine * P::CHUNK), full(st));
       }
       if (!ok) {
         // gave up: wait (bounded) for the copies in flight, which write to this CTA's shared memory
@@ -363,184 +264,148 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         set_status(a.status, SL_DEV_GEMM_TIMEOUT);
       }
     }
-  } else if (warp == 9) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // e4m3 x e4m3 -> fp32, M = 128, N = NP
-      for (int i = 0; i < steps; ++i) {
-        const int sg = i / SPS, st = sg % P::STAGES, part = i % SPS / T;
-        if (!mbar_wait(full(st), (sg / P::STAGES) & 1, s_abort) || !mbar_wait(a_full(i), (i >> 1) & 1, s_abort)) {
-          set_status(a.status, SL_DEV_GEMM_TIMEOUT);
-          const unsigned long long t0 = clock64();            // the last step issued still uses the tensor memory
-          while (i > 0 && !mbar_try(done(i - 1), ((i - 1) >> 1) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-          break;
-        }
-        tc_fence_after();
-        const uint32_t rows = smem_u32(smem + st * P::STAGE + T * GQ_CODES) + part * 2 * P::SLAB;
-        const uint32_t d = tmem + P::D_COL + (P::TWICE ? (i & 1) * P::D_COLS : 0), op = tmem + (i & 1) * P::A_COLS;
-#pragma unroll
-        for (int k = 0; k < P::KS / 32; ++k)                  // 32 k: 8 columns of the operand, 32 bytes of the terms' rows
-#pragma unroll
-          for (int term = 0; term < 2; ++term)
-            gq_mma_ta(d + (k / (G / 32)) * NP, op + k * 8, smem_desc_k_sw128(rows + (2 * (k >> 2) + term) * P::SLAB + (k & 3) * 32), idesc,
-                      k % (G / 32) != 0 || term != 0);
-        if (i % SPS == SPS - 1) tc_commit(empty(st));
-        tc_commit(done(i));
-      }
-    }
   } else {
-    const int lane_feature = (warp & 3) * 32 + lane, half = warp >> 2;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's lanes of the tensor memory
-    constexpr int CH = P::KS / 64;                            // 16-byte chunks of a feature's codes that a thread unpacks in a step
-    GroupReader<FP32> rd[T];
+    const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
+    // feature rows of this lane in a stage: tile mt, rows rev and 8 + rev of it
+    GroupReader<FP32> rd[2][2];
+    uint32_t row[2][2];
 #pragma unroll
-    for (int i = 0; i < T; ++i) {
-      rd[i].vec = a.vec != 0;
-      rd[i].s0 = (const uint8_t*)a.scales[i];
-      rd[i].z0 = a.zeros[i];
-      rd[i].ng = a.ng;
-    }
-    bool ok = true, fresh = false;
-    // the codes of step i -> operand tile i & 1; `at` = its place among the stage's steps
-    auto unpack = [&](int i, const int at) {
-      const int sg = i / SPS, st = sg % P::STAGES, tile = at % T, part = at / T;
-      if (at == 0) ok = __all_sync(0xffffffffu, mbar_wait(full(st), (sg / P::STAGES) & 1, s_abort));
-      if (!ok) return;
-      const uint32_t row = smem_u32(smem + st * P::STAGE + tile * GQ_CODES) + lane_feature * 128;
-      const uint32_t dst = tmem + lanes + (i & 1) * P::A_COLS + half * (P::A_COLS / 2);
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int c = 0; c < CH; c += 2) {
-        const uint32_t chunk = part * (8 / H) + half * CH + c;   // of the 128-byte row, swizzled
-        const uint4 v0 = gq_lds128(row + ((chunk ^ (lane & 7)) << 4)), v1 = gq_lds128(row + (((chunk + 1) ^ (lane & 7)) << 4));
-        const uint32_t w[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-        uint32_t x[16];
+      for (int h = 0; h < 2; ++h) {
+        const int f = (DUAL ? warp * 16 : warp * 32 + mt * 16) + h * 8 + rev;
+        const long long at = (long long)min(n0 + f, a.n_out - 1) * a.ng;   // features behind the last one: any scales, codes are 0
+        row[mt][h] = (uint32_t)((DUAL ? mt * 64 : 0) + f) * 128;
+        rd[mt][h].s = (const uint8_t*)a.scales[DUAL ? mt : 0] + at * (FP32 ? 4 : 2);
+        rd[mt][h].z = a.zeros[DUAL ? mt : 0] ? a.zeros[DUAL ? mt : 0] + at : nullptr;
+      }
+    constexpr int CH = GroupReader<FP32>::CHUNK;
+    int grp = b0 * P::GPT;
+    auto fetch = [&](int g0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[2 * j] = w[j] & 0x0f0f0f0fu;
-          x[2 * j + 1] = (w[j] >> 4) & 0x0f0f0f0fu;
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) rd[mt][h].fetch(g0, t, a.ng, a.pairs != 0);
+    };
+    auto turn = [&](int g0) {                                 // the chunk that was requested becomes the present one
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          rd[mt][h].c = rd[mt][h].n;
+          rd[mt][h].cz = rd[mt][h].nz;
         }
-        tc_st16(dst + c * 8, x);
-      }
-      if (at == SPS - 1) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty(st));
-      }
+      fetch(g0 + CH);
     };
-    // add up step i (accumulators of its groups)
-    auto add = [&](int i, const int at) {
-      const int st = i / SPS % P::STAGES, tile = at % T, part = at / T;
-      if (fresh) {                                            // a new tile's first scales have arrived by now
+    if (n > 0) fetch(grp & ~(CH - 1));
+    bool ok = true;
+    for (int i = 0; i < n; ++i) {
+      const int st = i % P::STAGES;
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(st), (i / P::STAGES) & 1, s_abort)))) break;
+      const uint32_t base = smem_u32(smem + st * P::STAGE), tb = base + GQ_CODES + lane * 16;
+      const uint32_t sw = (uint32_t)rev << 4;                 // swizzle: rows rev and 8 + rev of a tile have the same low bits
 #pragma unroll
-        for (int m = 0; m < T; ++m) rd[m].prime();
-        fresh = false;
-      }
-      ok = __all_sync(0xffffffffu, mbar_wait(done(i), (i >> 1) & 1, s_abort));
-      if (!ok) return;
-      tc_fence_after();
-      const float4* sq = reinterpret_cast<const float4*>(smem + st * P::STAGE + T * GQ_CODES + P::TERMS) + part * GPS * (NP / 2) + half * (HC / 2);
-      const uint32_t d0 = tmem + lanes + P::D_COL + (P::TWICE ? (i & 1) * P::D_COLS : 0) + half * HC;
-      constexpr int LD = HC < 16 ? 8 : 16, LOADS = GPS * HC / LD;   // accumulators are requested one load ahead
-      uint32_t d[2][LD];
-      auto request = [&](int k) {
-        const uint32_t col = d0 + (k * LD / HC) * NP + k * LD % HC;
-        if (LD == 8) tc_ld8(col, d[k & 1]);
-        else tc_ld16(col, d[k & 1]);
-      };
-      request(0);
-      float sc = 0.f, mz = 0.f;
+      for (int hf = 0; hf < 2; ++hf) {
+        uint32_t cw[2][2][4];
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        const int g = k * LD / HC, c = k * LD % HC;
-        if (c == 0) rd[tile].next(sc, mz);
-        float4 qf[LD / 2];
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int e = 0; e < LD / 2; ++e) qf[e] = sq[g * (NP / 2) + c / 2 + e];
-        tc_wait_ld();
-        if (k + 1 < LOADS) request(k + 1);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t* c = cw[mt][h];
+            const uint32_t at = base + row[mt][h];
+            if (G == 128) {
+              const uint4 x = gq_lds128(at + (((hf * 4 + t) << 4) ^ sw));
+              c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
+            } else if (G == 64) {
 #pragma unroll
-        for (int e = 0; e < LD; ++e) {
-          const float q = e & 1 ? qf[e / 2].z : qf[e / 2].x, f = e & 1 ? qf[e / 2].w : qf[e / 2].y;
-          acc[tile][c + e] = fmaf(sc * f, fmaf(mz, q, __uint_as_float(d[k & 1][e])), acc[tile][c + e]);
-        }
-      }
-      if (at == SPS - 1) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty(st));
-      }
-    };
-    auto release = [&](int i) {                               // operand tile written; the accumulators of step i are free
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(a_full(i));
-    };
-    // one CTA to a tile: results straight from the registers, a warp's lanes are neighbouring features
-    auto store = [&](int tile) {
-      const int n = tile * 128 + lane_feature;
-      if (n < a.n_out) {
+              for (int q = 0; q < 2; ++q)
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[2 * q]), "=r"(c[2 * q + 1])
+                             : "r"(at + (((hf * 4 + 2 * q + (t >> 1)) << 4) ^ sw) + (t & 1) * 8) : "memory");
+            } else {
 #pragma unroll
-        for (int c = 0; c < HC; ++c) {
-          const int r = half * HC + c;
-          if (r >= M) break;
-          const long long out = (long long)(r0 + r) * a.n_out + n;
-          const float x = acc[0][c];
-          if (DUAL) reinterpret_cast<bf16*>(a.C)[out] = __float2bfloat16_rn(x / (1.f + __expf(-x)) * acc[T - 1][c]);
-          else if (epilogue == EPI_RESIDUAL) reinterpret_cast<float*>(a.C)[out] += x;
-          else reinterpret_cast<bf16*>(a.C)[out] = __float2bfloat16_rn(x);
-        }
-      }
-      clear();
-    };
-    const int stages = my_tiles * nstage;
-    for (int sg = 0, in_tile = 0, tile = tile0; sg < stages && ok; ++sg) {
-#pragma unroll
-      for (int at = 0; at < SPS; ++at) {
-        const int i = sg * SPS + at;
-        unpack(i, at);
-        if (!ok) break;
-        if (P::TWICE) release(i);
-        if (i > 0) add(i - 1, (at + SPS - 1) % SPS);
-        if (!ok) break;
-        if (at == 0 && in_tile == 0) {                        // the tile before this one is complete
-          if (sg > 0) {
-            if (S == 1) store(tile);
-            tile += tile_step;
+              for (int q = 0; q < 4; ++q)
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(c[q]) : "r"(at + (((hf * 4 + q) << 4) ^ sw) + t * 4) : "memory");
+            }
           }
-          const long long feature = min(tile * 128 + lane_feature, a.n_out - 1);
+        float ga[2][NT][4];
+        constexpr int WPG = G / 32;                           // words per group
 #pragma unroll
-          for (int m = 0; m < T; ++m) rd[m].begin(feature, b0 * P::GPT, min(b1 * P::GPT, a.ng));
-          fresh = true;
+        for (int w = 0; w < 4; ++w) {
+          if (w % WPG == 0) {
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int j = 0; j < NT; ++j) ga[mt][j][0] = ga[mt][j][1] = ga[mt][j][2] = ga[mt][j][3] = 0.f;
+          }
+          uint32_t x[2][2][4];                                // [tile][codes 0 4 1 5 | 2 6 3 7]
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t lo = cw[mt][h][w], hi = lo >> 8;
+              x[mt][0][h] = lo & 0x000f000fu;
+              x[mt][0][2 + h] = lo & 0x00f000f0u;
+              x[mt][1][h] = hi & 0x000f000fu;
+              x[mt][1][2 + h] = hi & 0x00f000f0u;
+            }
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const uint4 b = gq_lds128(tb + j * P::CHUNK + (hf * 4 + w) * 512);
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) mma_f16(ga[mt][j], x[mt][0], b.x, b.y);
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) mma_f16(ga[mt][j], x[mt][1], b.z, b.w);
+          }
+          if (w % WPG == WPG - 1) {
+            constexpr int HG = 4 / WPG;                       // groups per 128 k
+            const int gi = hf * HG + w / WPG;
+            if (((grp & (CH - 1)) == 0) || (i == 0 && gi == 0)) turn(grp & ~(CH - 1));
+            float sc[2][2], mz[2][2];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                if (gi & 1) rd[mt][h].template get<1>(grp, lane, sc[mt][h], mz[mt][h]);
+                else rd[mt][h].template get<0>(grp, lane, sc[mt][h], mz[mt][h]);
+              }
+            ++grp;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              const uint4 y = gq_lds128(base + GQ_CODES + j * P::CHUNK + GQ_TERMS + gi * 64 + t * 16);   // q, 2^(e + 12) of rows 2 t, 2 t + 1
+              const float q[2] = {__uint_as_float(y.x), __uint_as_float(y.z)}, f[2] = {__uint_as_float(y.y), __uint_as_float(y.w)};
+#pragma unroll
+              for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  acc[mt][j][e] = fmaf(sc[mt][e >> 1] * f[e & 1], fmaf(mz[mt][e >> 1], q[e & 1], ga[mt][j][e]), acc[mt][j][e]);
+            }
+          }
         }
-        if (!P::TWICE) release(i);
       }
-      if (++in_tile == nstage) in_tile = 0;
-      if (sg == stages - 1 && ok) {
-        add(steps - 1, SPS - 1);
-        if (ok && S == 1) store(tile);
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(st));
     }
     if (!ok && lane == 0) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
   }
 
   // ---- sums of the cluster, epilogue ----
   __syncthreads();
-  if (warp == 9) {
-    __syncwarp();
-    tc_fence_after();
-    tc_dealloc(tmem, P::COLS);
-  }
-  if (S == 1) return;
   const bool good = *s_abort == 0;
-  if (warp < 8) {
-    const int lane_feature = (warp & 3) * 32 + lane, half = warp >> 2;
+  if (warp < 4) {
+    const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
 #pragma unroll
-    for (int i = 0; i < T; ++i)
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int c = 0; c < HC; ++c) sRed[(half * HC + c) * P::PITCH + i * 128 + lane_feature] = acc[i][c];
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + (DUAL ? mt * 64 + warp * 16 : warp * 32 + mt * 16) + (e >> 1) * 8 + rev] = acc[mt][j][e] * 4096.f;
   }
-  cluster_sync_all();
-  if (my_tiles > 0 && good) {
+  if (S > 1) cluster_sync_all(); else __syncthreads();
+  if (M > 0 && good) {
     const uint32_t sred = smem_u32(sRed);
     auto total = [&](int at) {                                // four neighbouring features, the CTAs in order
+      if (S == 1) return *reinterpret_cast<const float4*>(sRed + at);
       float4 p[8], x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (uint32_t s = 0; s < 8; ++s)
@@ -552,104 +417,68 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         }
       return x;
     };
-    const int c0 = (int)(32 * rank / S), cols = (int)(32 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
-    for (int i = threadIdx.x; i < min(M, NP) * cols; i += GQ_THREADS) {
-      const int r = i / cols, col = 4 * (c0 + i % cols), n = tile0 * 128 + col;
-      if (n >= a.n_out) continue;
-      const long long out = (long long)(r0 + r) * a.n_out + n;
-      const float4 t = total(r * P::PITCH + col);
-      float x[4] = {t.x, t.y, t.z, t.w};
+    const int c0 = (int)(TO / 4 * rank / S), cols = (int)(TO / 4 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
+    for (int i = threadIdx.x; i < min(M, 8 * NT) * cols; i += GQ_THREADS) {
+      const int r = i / cols, col = 4 * (c0 + i % cols), nn = n0 + col;
+      if (nn >= a.n_out) continue;
+      const long long out = (long long)(r0 + r) * a.n_out + nn;
+      const float4 y = total(r * P::PITCH + col);
+      float x[4] = {y.x, y.y, y.z, y.w};
       if (DUAL) {
-        const float4 u = total(r * P::PITCH + 128 + col);
+        const float4 u = total(r * P::PITCH + 64 + col);
         const float up[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = x[e] / (1.f + __expf(-x[e])) * up[e];
       }
       if (epilogue == EPI_RESIDUAL && !DUAL) {
         float* c = reinterpret_cast<float*>(a.C) + out;
-        if ((a.n_out & 3) == 0) {
-          float4 y = *reinterpret_cast<const float4*>(c);
-          y.x += x[0]; y.y += x[1]; y.z += x[2]; y.w += x[3];
-          *reinterpret_cast<float4*>(c) = y;
-        } else {
-          for (int e = 0; e < 4; ++e)
-            if (n + e < a.n_out) c[e] += x[e];
-        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (nn + e < a.n_out) c[e] += x[e];
       } else {
         bf16* c = reinterpret_cast<bf16*>(a.C) + out;
         if ((a.n_out & 3) == 0) {
           *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
         } else {
+#pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (n + e < a.n_out) c[e] = __float2bfloat16_rn(x[e]);
+            if (nn + e < a.n_out) c[e] = __float2bfloat16_rn(x[e]);
         }
       }
     }
   }
-  cluster_sync_all();                                         // the others may still be reading this CTA's partial sums
+  if (S > 1) cluster_sync_all();                              // the others may still be reading this CTA's partial sums
 }
 
 namespace {
 
-// 2-D row-major tensor map, zeros out of bounds
-int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, long long rows, long long cols, int box_rows, int box_cols,
-           CUtensorMapSwizzle swizzle) {
+// codes [n_out][K / 2], boxes of `rows` features x 128 bytes, zeros out of bounds
+int gq_map(CUtensorMap* out, const void* p, long long n_out, long long row_bytes, int rows) {
   TensorMapEncodeFn fn = tensor_map_encode_fn();
   if (!fn) return SL_ECUDA;
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * elem};
-  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
-  const CUresult r = fn(out, type, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                        CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)n_out}, strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t box[2] = {GQ_BK / 2, (cuuint32_t)rows}, one[2] = {1, 1};
+  const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SL_OK : SL_ECUDA;
 }
 
-// the workspace: terms, then (q, 2^e) with room for the smallest groups
-struct GqWs {
-  long long kp, ld;
-  size_t q_at, bytes;
-};
-GqWs gq_ws(int max_rows, int K) {
-  GqWs w;
-  w.kp = ((long long)K + GQ_BK - 1) / GQ_BK * GQ_BK;
-  w.ld = ((long long)max_rows + 1) / 2 * 2;          // rows of 16 bytes
-  w.q_at = ((size_t)2 * max_rows * w.kp + 255) / 256 * 256;
-  w.bytes = w.q_at + (size_t)w.kp / 32 * w.ld * 8;
-  return w;
-}
-
-template <int G, int NP, bool DUAL, bool FP32>
-int launch_gq(const CUtensorMap* w, void* ws, const GqWs& lay, const GqArgs& a, int epilogue, cudaStream_t st) {
-  using P = GqPlan<G, NP, DUAL>;
-  CUtensorMap terms, q;
-  int rc = gq_map(&terms, ws, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, 2ll * a.max_rows, lay.kp, NP, 128, CU_TENSOR_MAP_SWIZZLE_128B);
-  if (rc == SL_OK)
-    rc = gq_map(&q, (char*)ws + lay.q_at, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, lay.kp / G, 2 * lay.ld, P::GPT, 2 * NP, CU_TENSOR_MAP_SWIZZLE_NONE);
-  if (rc != SL_OK) return rc;
-  const int tiles = (a.n_out + 127) / 128, nblk = (a.K + GQ_BK - 1) / GQ_BK, row_tiles = (a.max_rows + NP - 1) / NP;
-  // With S = 1 the CTAs go on to further tiles, all of them resident.  Otherwise K is split over S CTAs: the S with the least
-  // estimated time, rounds of CTAs times (stages of one + 3 stages' time to start and to join).
+template <int G, int NT, bool DUAL, bool FP32>
+int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
+  using P = GqPlan<G, NT>;
+  constexpr int TO = DUAL ? 64 : 128;
+  const int tiles = (a.n_out + TO - 1) / TO, nblk = (a.K + GQ_BK - 1) / GQ_BK, row_tiles = (a.max_rows + 8 * NT - 1) / (8 * NT);
+  // K is split over S CTAs of a cluster while the CTAs still fit the GPU at once
   const long long slots = (long long)sm_count() * P::OCC, work = (long long)tiles * row_tiles;
   int S = 1;
-  long long best = (work + slots - 1) / slots * nblk * P::T + 2;
-  for (int s = 2; s <= 8 && s <= nblk; ++s) {
-    const long long t = (work * s + slots - 1) / slots * ((nblk + s - 1) / s * P::T + 3);
-    if (t < best) {
-      best = t;
-      S = s;
-    }
-  }
-  int grid = tiles * S;
-  if (S == 1) {
-    const int most = (int)(slots / row_tiles > 0 ? slots / row_tiles : 1), rounds = (tiles + most - 1) / most;
-    grid = (tiles + rounds - 1) / rounds;
-  }
-  auto kernel = gemm_quantized_kernel<G, NP, DUAL, FP32>;
+  while (S < 8 && S < nblk && work * (S + 1) <= slots) ++S;
+  auto kernel = gemm_quantized_kernel<G, NT, DUAL, FP32>;
   static std::once_flag once;
   static cudaError_t attr;
   std::call_once(once, [&] { attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P::SMEM); });
   SL_CUDA_TRY(attr);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, row_tiles);
+  cfg.gridDim = dim3(tiles * S, row_tiles);
   cfg.blockDim = dim3(GQ_THREADS);
   cfg.dynamicSmemBytes = P::SMEM;
   cfg.stream = st;
@@ -666,60 +495,60 @@ int launch_gq(const CUtensorMap* w, void* ws, const GqWs& lay, const GqArgs& a, 
   }
   cfg.attrs = at;
   cfg.numAttrs = n;
-  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, w[0], w[1], terms, q, a, epilogue));
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, w[0], w[1], a, epilogue));
   return SL_OK;
 }
 
-// rows to a pass: what the accumulators of a step's groups leave of the tensor memory, and the sums of two matrices of the registers
-template <int G, bool DUAL, bool FP32>
-int by_rows(const CUtensorMap* w, void* ws, const GqWs& lay, const GqArgs& a, int epilogue, cudaStream_t st) {
-  if (a.max_rows <= 16) return launch_gq<G, 16, DUAL, FP32>(w, ws, lay, a, epilogue, st);
-  if (a.max_rows <= 32) return launch_gq<G, 32, DUAL, FP32>(w, ws, lay, a, epilogue, st);
-  if (G == 32 || DUAL || a.max_rows <= 64) return launch_gq<G, 64, DUAL, FP32>(w, ws, lay, a, epilogue, st);
-  return launch_gq<G, G == 32 || DUAL ? 64 : 128, DUAL, FP32>(w, ws, lay, a, epilogue, st);
+// rows to a pass: 8 to 64, as many as there are
+template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
+  if (a.max_rows <= 8) return launch_gq<G, 1, DUAL, FP32>(w, a, epilogue, st);
+  if (a.max_rows <= 16) return launch_gq<G, 2, DUAL, FP32>(w, a, epilogue, st);
+  if (a.max_rows <= 24) return launch_gq<G, 3, DUAL, FP32>(w, a, epilogue, st);
+  if (a.max_rows <= 32) return launch_gq<G, 4, DUAL, FP32>(w, a, epilogue, st);
+  return launch_gq<G, 8, DUAL, FP32>(w, a, epilogue, st);
 }
-template <int G>
-int by_kind(const CUtensorMap* w, const void* A, void* ws, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
-  const GqWs lay = gq_ws(a.max_rows, a.K);
-  if (a.max_rows > 65535) return SL_EUNSUPPORTED;
-  SL_CUDA_TRY(launch_pdl(gq_split_rows_kernel<G>, dim3((unsigned)((lay.kp / 8 + GS_THREADS - 1) / GS_THREADS), a.max_rows), dim3(GS_THREADS),
-                         0, st, (const bf16*)A, a.n_active, a.max_rows, a.K, (int)lay.kp, (int)lay.ld, (uint8_t*)ws,
-                         (float2*)((char*)ws + lay.q_at)));
-  if (epilogue == EPI_SWIGLU)
-    return fp32 ? by_rows<G, true, true>(w, ws, lay, a, epilogue, st) : by_rows<G, true, false>(w, ws, lay, a, epilogue, st);
-  return fp32 ? by_rows<G, false, true>(w, ws, lay, a, epilogue, st) : by_rows<G, false, false>(w, ws, lay, a, epilogue, st);
+template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
+  const unsigned per_row = (unsigned)(((a.K + GQ_BK - 1) / GQ_BK * (GQ_BK / 8) + GS_THREADS - 1) / GS_THREADS);
+  SL_CUDA_TRY(launch_pdl(gq_rewrite_rows_kernel<G>, dim3(per_row, a.max_rows), dim3(GS_THREADS), 0, st, (const bf16*)A, a.n_active, a.max_rows,
+                         a.K, (uint8_t*)a.terms));
+  if (epilogue == EPI_SWIGLU) return fp32 ? by_rows<G, true, true>(w, a, epilogue, st) : by_rows<G, true, false>(w, a, epilogue, st);
+  return fp32 ? by_rows<G, false, true>(w, a, epilogue, st) : by_rows<G, false, false>(w, a, epilogue, st);
 }
 
 }  // namespace
 
-size_t gemm_quantized_workspace_bytes(int max_rows, int K) { return gq_ws(max_rows, K).bytes; }
+// room for the rewritten rows with the smallest groups
+size_t gemm_quantized_workspace_bytes(int max_rows, int K) {
+  return (size_t)((K + GQ_BK - 1) / GQ_BK) * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
+}
 
 int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active, int max_rows,
                           int n_out, int K, int epilogue, void* workspace, int32_t* status, cudaStream_t st) {
+  if (max_rows > 65535) return SL_EUNSUPPORTED;
   GqArgs a{};
   CUtensorMap maps[2];
-  const int ng = K / W->group;
-  const bool fp32 = W->scale_dtype == SL_FP32;
-  a.vec = ng % (fp32 ? 4 : 8) == 0;
+  a.ng = K / W->group;
+  a.pairs = a.ng % 2 == 0;
   for (int i = 0; i < 2; ++i) {
     const surelock_w4* w = i && W2 ? W2 : W;
     a.zeros[i] = (const uint8_t*)w->zeros;
     a.scales[i] = w->scales;
-    if ((reinterpret_cast<uintptr_t>(w->scales) & 15) || (reinterpret_cast<uintptr_t>(w->zeros) & 3)) a.vec = 0;
-    const int rc = gq_map(&maps[i], w->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, n_out, K / 2, 128, GQ_BK / 2, CU_TENSOR_MAP_SWIZZLE_128B);
+    if ((reinterpret_cast<uintptr_t>(w->scales) & 3) || (reinterpret_cast<uintptr_t>(w->zeros) & 1)) a.pairs = 0;
+    const int rc = gq_map(&maps[i], w->codes, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128);
     if (rc != SL_OK) return rc;
   }
+  a.terms = (const uint8_t*)workspace;
   a.C = C;
   a.n_active = n_active;
   a.max_rows = max_rows;
   a.n_out = n_out;
   a.K = K;
-  a.ng = ng;
   a.status = status;
+  const bool fp32 = W->scale_dtype == SL_FP32;
   switch (W->group) {
-    case 32: return by_kind<32>(maps, A, workspace, a, epilogue, fp32, st);
-    case 64: return by_kind<64>(maps, A, workspace, a, epilogue, fp32, st);
-    default: return by_kind<128>(maps, A, workspace, a, epilogue, fp32, st);
+    case 32: return by_kind<32>(maps, A, a, epilogue, fp32, st);
+    case 64: return by_kind<64>(maps, A, a, epilogue, fp32, st);
+    default: return by_kind<128>(maps, A, a, epilogue, fp32, st);
   }
 }
 
