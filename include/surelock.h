@@ -415,8 +415,7 @@ typedef struct {
 /* surelock_gemm_fused with 4-bit weights, for few rows: C[r][n] = sum_k A[r][k] W[n][k] for r < *n_active, A dev bf16 [M][K],
  * epilogue 0: C bf16 [M][n_out]; 1: C is the fp32 residual stream, C[r][n] += sum; 2: C bf16 = silu(A W^T) * (A W2^T), W2 of
  * the same group, scale type and kind of zero point as W (W2 is ignored otherwise).  The codes enter the products exactly,
- * the rows as fp16 numbers (per group of k exact down to 2^-25 of the row's largest magnitude there, off by at most 2^-36
- * of it below); group sums are fp32 and are multiplied by their scale in fp32.  A row with an infinity or a NaN gives NaN,
+ * the rows as fp16 numbers (exact down to 2^-25 of the row's largest magnitude, off by at most 2^-35 of it below); group sums are fp32 and are multiplied by their scale in fp32.  A row with an infinity or a NaN gives NaN,
  * and no other row is
  * affected.  Any n_out; K a multiple of the group.  A pass over the weights serves up to 64 rows; more take further passes,
  * at most 65535 rows in all.  Rows >= *n_active of C are not touched.

@@ -450,11 +450,11 @@ def surelock_attention(q, k_cache, v_cache, active_idx, row_offsets, n_active, B
 def _w4(W, K: int):
     """The C struct of (codes uint8 [n_out][K/2], scales bf16 or fp32 [n_out][K/group], zeros uint8 [n_out][K/group] or None)."""
     codes, scales, zeros = W
-    n, ng = scales.shape
-    if codes.dtype != torch.uint8 or tuple(codes.shape) != (n, K // 2) or not ng or K % ng or \
-            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != scales.shape)):
+    n, ng = shape = scales.shape
+    if codes.dtype != torch.uint8 or codes.shape != (n, K // 2) or not ng or K % ng or \
+            (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != shape)):
         raise SurelockError("4-bit weights: codes uint8 [n_out][K/2], scales [n_out][K/group], zeros uint8 like scales or None")
-    return _W4(_p(codes), _p(scales), _p(zeros), K // ng, _dt(scales))
+    return _W4(_p(codes), _p(scales), _p(zeros), K // ng, _dt(scales)), n
 
 
 def surelock_gemm_quantized_workspace_bytes(max_rows: int, K: int) -> int:
@@ -466,18 +466,21 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
     2: Cout (bf16) = silu(A W^T) * (A W2^T).  workspace: uint8 CUDA tensor of surelock_gemm_quantized_workspace_bytes(M, K)
     bytes that no call running at the same time uses; None takes one from torch's allocator for this call."""
     M, K = A.shape
-    n = W[0].shape[0]
-    if A.dtype != torch.bfloat16 or Cout.dtype != (torch.float32 if epilogue == 1 else torch.bfloat16) or tuple(Cout.shape) != (M, n):
+    w, n = _w4(W, K)
+    w2 = None
+    if W2 is not None:
+        w2, n2 = _w4(W2, K)
+        if n2 != n:
+            raise SurelockError("surelock_gemm_quantized: W and W2 must have the same features")
+    if A.dtype != torch.bfloat16 or Cout.dtype != (torch.float32 if epilogue == 1 else torch.bfloat16) or Cout.shape != (M, n):
         raise SurelockError("surelock_gemm_quantized: A bf16 [M][K], Cout [M][n_out] (fp32 with epilogue 1, else bf16)")
-    if W2 is not None and W2[0].shape[0] != n:
-        raise SurelockError("surelock_gemm_quantized: W and W2 must have the same features")
     need = surelock_gemm_quantized_workspace_bytes(M, K)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=A.device)
-    if workspace.nbytes < need:
+        workspace = torch.empty(need or 1, dtype=torch.uint8, device=A.device)
+    elif workspace.nbytes < need:
         raise SurelockError("surelock_gemm_quantized: workspace too small")
-    _check(lib().surelock_gemm_quantized(_p(A), C.byref(_w4(W, K)), C.byref(_w4(W2, K)) if W2 is not None else None, _p(Cout),
-                                         _p(n_active), M, n, K, epilogue, _p(workspace), _p(dev_status), _stream()), "surelock_gemm_quantized")
+    _check(lib().surelock_gemm_quantized(_p(A), C.byref(w), C.byref(w2) if w2 is not None else None, _p(Cout), _p(n_active), M, n, K,
+                                         epilogue, _p(workspace), _p(dev_status), _stream()), "surelock_gemm_quantized")
 
 
 # ---- paged K/V cache ---------------------------------------------------------------------------------------

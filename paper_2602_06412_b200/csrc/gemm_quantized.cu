@@ -10,20 +10,20 @@
 // A 4-bit code alone in 16 bits IS an fp16 number: u 2^-24 (subnormal) in the lowest bits, u 2^-20 four bits up.  So eight
 // codes become operands of 16-bit matrix instructions with four masks and one shift, (0,4) (1,5) of the word and (2,6) (3,7)
 // of the word shifted by 8 (11 instructions to make bf16 numbers of them); the factor 16 between the pairs is taken out of the
-// activations, which a small kernel in front rewrites once: per row and group of k as fp16 numbers a' = a 2^-e, the largest
-// magnitude 2^14 ... 2^15, every other pair over 16.  fp16 has 11 bits to bf16's 8, so this is exact down to 2^-25 of the
-// largest magnitude and off by at most 2^-36 of it below.  Per group
+// activations, which a small kernel in front rewrites once: a row as fp16 numbers a' = a 2^-e, the largest magnitude 2^14 ...
+// 2^15, every other pair over 16.  fp16 has 11 bits to bf16's 8, so this is exact down to 2^-25 of the row's largest
+// magnitude and off by at most 2^-35 of it below.  Per group
 //   sum_k (u - z) a = 2^(e + 24) (D - z q),   D = sum_k (u 2^-24) a',   q = 2^-24 sum_k a',
-// D from the products, q and 2^e from the rewriting kernel; the bracket is formed in fp32 and multiplied by its group's scale
+// D from the products, q and e from the rewriting kernel; the bracket is formed in fp32 and multiplied by its group's scale
 // in fp32, so a weight is never rounded.
 //
 // mma.sync m16n8k16 with 16 features as the rows and 8 packed rows as the columns: 970 multiply-adds per clock and SM
-// measured, enough for some 20 rows at the memory's rate.  Warps work alone, each on 32 features, and many of them hide each
+// measured, enough for some 20 rows at the memory's rate.  Warps work alone, each on its features, and many of them hide each
 // other's steps.  (tcgen05 with the codes as the tensor-memory operand was built with bf16 and with e4m3 operands: unpack ->
 // tensor memory -> product -> back per group is a chain of ~1000 clocks per 256 k that 16 warps per SM did not hide: 84 - 116
 // us for 8 rows of the 4096 x 126464 head.  mma.sync with e4m3 operands converts them to fp16 on the way: 77 us.)
-//   warps 0-3  32 features each (with SwiGLU 16 of the gate and the same 16 of the up matrix), all k of the CTA's range
-//   warp 4     one thread issues the copies: a stage is 256 k, 128 bytes of codes of 128 features by TMA (128-byte swizzle)
+//   warps 0-7  16 features each (with SwiGLU half of the warps have the gate, half the up matrix), all k of the CTA's range
+//   warp 8     one thread issues the copies: a stage is 256 k, 128 bytes of codes of 128 features by TMA (128-byte swizzle)
 //              and the rewritten rows, already in the order of the MMA fragments, as one bulk copy
 // The contraction index is permuted within 32 ... 128 k (a lane owns 16, 8 or 4 code bytes of a feature, for groups of 128,
 // 64, 32), and the features within 8 (by bit reversal), so that the code loads touch all banks.
@@ -40,16 +40,17 @@ namespace sl {
 
 namespace {
 
-constexpr int GQ_THREADS = 160;
 constexpr int GQ_BK = 256;             // k per stage
 constexpr int GQ_CODES = 128 * GQ_BK / 2;
-constexpr int GQ_TERMS = 8 * GQ_BK * 2;   // bytes of 8 rewritten rows in a stage
+constexpr int GQ_WARPS = 8, GQ_THREADS = 32 * GQ_WARPS + 32;
+constexpr int GQ_ROWS = 8 * GQ_BK * 2;   // bytes of 8 rewritten rows in a stage
 
 struct GqArgs {
-  const uint8_t *zeros[2], *terms;
+  const uint8_t *zeros[2], *rows;
   const void* scales[2];
   void* C;
   const int32_t* n_active;
+  const int32_t* row_exp;              // e + 24 of every row
   int max_rows, n_out, K, ng;
   int pairs;                           // scales and zero points of two neighbouring groups lie on aligned addresses
   int32_t* status;
@@ -122,9 +123,9 @@ template <bool FP32> struct GroupReader {
 
 template <int G, int NT> struct GqPlan {
   static constexpr int GPT = GQ_BK / G;                       // groups per stage
-  static constexpr int CHUNK = GQ_TERMS + GPT * 64;           // 8 rewritten rows, then their (q, 2^(e + 12)): [group][row]
+  static constexpr int CHUNK = GQ_ROWS + GPT * 32;           // 8 rewritten rows, then their q: [group][row]
   static constexpr int STAGE = GQ_CODES + (NT * CHUNK + 1023) / 1024 * 1024;
-  static constexpr int OCC = NT <= 2 ? 4 : NT <= 4 ? 3 : 2;
+  static constexpr int OCC = NT <= 4 ? 3 : 2;
   static constexpr int ROOM = 228 * 1024 / OCC - 1024 - 1024 - 256;
   static constexpr int STAGES = ROOM / STAGE > 4 ? 4 : ROOM / STAGE;
   static constexpr int PITCH = 132;                           // floats per packed row of the partial sums
@@ -133,58 +134,75 @@ template <int G, int NT> struct GqPlan {
 };
 
 // ---- the rewritten rows ----------------------------------------------------------------------------------------------
-// 8 k per thread; per (row, group) e from the largest magnitude.  A group with an infinity or a NaN is NaN throughout.  Out:
-// per (256 k, 8 rows) one chunk of GqPlan::CHUNK bytes, [word of a code fragment][lane] of 16 bytes: a' of the 8 k whose
-// codes that word holds, in the order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16); then (2^-24 sum a', 2^(e + 12)); zeros behind K.
-constexpr int GS_THREADS = 256;
+// One CTA per row, 8 k per thread at a time.  A row with an infinity or a NaN is NaN throughout.  Out: per (256 k, 8 rows) one
+// chunk of GqPlan::CHUNK bytes, [word of a code fragment][lane] of 16 bytes: a' of the 8 k whose codes that word holds, in the
+// order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16), zeros behind K; then q of the groups, [group][row].  And e + 24 per row.
+constexpr int GS_THREADS = 512;
 
 template <int G>
 __global__ void __launch_bounds__(GS_THREADS)
-gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, uint8_t* __restrict__ terms) {
+gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, uint8_t* __restrict__ rows,
+                       int32_t* __restrict__ row_exp) {
+  __shared__ uint32_t sTop[GS_THREADS / 32];
   griddep_wait();
   griddep_launch();
-  const int r = blockIdx.y, i = blockIdx.x * GS_THREADS + threadIdx.x;
+  const int r = blockIdx.x;
   if (r >= min(*n_active, max_rows)) return;
-  uint4 v = make_uint4(0, 0, 0, 0);
-  if (i < K / 8) v = __ldg(reinterpret_cast<const uint4*>(A + (long long)r * K) + i);
+  const uint4* row = reinterpret_cast<const uint4*>(A + (long long)r * K);
   constexpr uint32_t MAG = 0x7fff7fffu;
-  uint32_t top = __vmaxu2(__vmaxu2(v.x & MAG, v.y & MAG), __vmaxu2(v.z & MAG, v.w & MAG));
+  uint4 first = make_uint4(0, 0, 0, 0);
+  uint32_t top = 0;
+  for (int i = threadIdx.x; i < K / 8; i += GS_THREADS) {
+    const uint4 v = __ldg(row + i);
+    if (i == threadIdx.x) first = v;
+    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & MAG, v.y & MAG), __vmaxu2(v.z & MAG, v.w & MAG)));
+  }
 #pragma unroll
-  for (int o = 1; o < G / 8; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+  for (int o = 16; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((threadIdx.x & 31) == 0) sTop[threadIdx.x >> 5] = top;
+  __syncthreads();
+  top = sTop[threadIdx.x & (GS_THREADS / 32 - 1)];
+#pragma unroll
+  for (int o = GS_THREADS / 64; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
   top = max(top & 0xffffu, top >> 16);
   const bool bad = top >= 0x7f80u;
   int e = (int)(top >> 7) - 127 - 14;                // the largest magnitude becomes 2^14 ... 2^15
   if (top == 0 || bad) e = 0;
   e = max(e, -140);                                  // subnormal numbers
+  if (threadIdx.x == 0) row_exp[r] = e + 24;
   const float d0 = gq_pow2(-e / 2), d1 = gq_pow2(-e - (-e / 2));
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float x[8], sum = 0.f;
+  const int blocks = (K + GQ_BK - 1) / GQ_BK, end = (blocks * 32 + GS_THREADS - 1) / GS_THREADS * GS_THREADS;   // whole warps: they shuffle
+  for (int i = threadIdx.x; i < end; i += GS_THREADS) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (i < K / 8) v = i == threadIdx.x ? first : __ldg(row + i);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float x[8], sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x[2 * j] = __uint_as_float(w[j] << 16) * d0 * d1;
-    x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) * d0 * d1;
-  }
-  uint32_t out[4];
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(w[j] << 16) * d0 * d1;
+      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) * d0 * d1;
+    }
+    uint32_t out[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float f = j & 1 ? 0.0625f : 1.f;
-    const __half2 h = __floats2half2_rn(x[j] * f, x[j + 4] * f);
-    const float2 back = __half22float2(h);           // what the products see
-    sum += (back.x + back.y) * (j & 1 ? 16.f : 1.f);
-    out[j] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
-  }
-  if (bad) sum = __uint_as_float(0x7fffffffu);
+    for (int j = 0; j < 4; ++j) {
+      const float f = j & 1 ? 0.0625f : 1.f;
+      const __half2 h = __floats2half2_rn(x[j] * f, x[j + 4] * f);
+      const float2 back = __half22float2(h);         // what the products see
+      sum += (back.x + back.y) * (j & 1 ? 16.f : 1.f);
+      out[j] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
+    }
+    if (bad) sum = __uint_as_float(0x7fffffffu);
 #pragma unroll
-  for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const int block = i / 32, k8 = i % 32, in = k8 % 16;
-  if (block < (K + GQ_BK - 1) / GQ_BK) {
-    const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
-    const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
-    uint8_t* chunk = terms + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
-    *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) =
-        make_uint4(out[0], out[1], out[2], out[3]);
-    if (k8 % (G / 8) == 0)
-      *reinterpret_cast<float2*>(chunk + GQ_TERMS + k8 / (G / 8) * 64 + (r % 8) * 8) = make_float2(sum * 5.9604644775390625e-8f, ldexpf(1.f, e + 12));
+    for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const int block = i / 32, k8 = i % 32, in = k8 % 16;
+    if (block < blocks) {
+      const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
+      const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
+      uint8_t* chunk = rows + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
+      *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
+      if (k8 % (G / 8) == 0)
+        *reinterpret_cast<float*>(chunk + GQ_ROWS + k8 / (G / 8) * 32 + (r % 8) * 4) = sum * 5.9604644775390625e-8f;
+    }
   }
 }
 
@@ -208,7 +226,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   if (threadIdx.x == 0) {
     for (int i = 0; i < P::STAGES; ++i) {
       mbar_init(full(i), 1);
-      mbar_init(empty(i), 4);
+      mbar_init(empty(i), GQ_WARPS);
     }
     *s_abort = 0;
     fence_mbar_init();
@@ -225,13 +243,11 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   const int b0 = (int)((long long)nblk * rank / S), b1 = (int)((long long)nblk * (rank + 1) / S);
   const int n = M > 0 ? b1 - b0 : 0;
 
-  float acc[2][NT][4];
+  float acc[NT][4];
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[mt][j][0] = acc[mt][j][1] = acc[mt][j][2] = acc[mt][j][3] = 0.f;
+    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 
-  if (warp == 4) {
+  if (warp == GQ_WARPS) {
     if (lane == 0) {
       const uint64_t once = gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();   // a code is read once per row tile
       const int row_tiles = (a.max_rows + 7) / 8, mine = min(NT, row_tiles - r0 / 8), ahead = min(n, P::STAGES);
@@ -253,7 +269,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
           if (!(ok = mbar_wait(empty(st), ((i / P::STAGES) & 1) ^ 1, s_abort))) break;
           codes(i);
         }
-        bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.terms + ((long long)(b0 + i) * row_tiles + r0 / 8) * P::CHUNK,
+        bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.rows + ((long long)(b0 + i) * row_tiles + r0 / 8) * P::CHUNK,
                   (uint32_t)(mine * P::CHUNK), full(st));
       }
       if (!ok) {
@@ -266,34 +282,29 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     }
   } else {
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
-    // feature rows of this lane in a stage: tile mt, rows rev and 8 + rev of it
-    GroupReader<FP32> rd[2][2];
-    uint32_t row[2][2];
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    // feature rows of this lane in a stage: rows rev and 8 + rev of the warp's 16; with SwiGLU the first 64 of a
+    // stage are the gate's, the others the up matrix's
+    GroupReader<FP32> rd[2];
+    const int mat = DUAL ? warp / (GQ_WARPS / 2) : 0;
+    const uint32_t row0 = (uint32_t)(warp * 16 + rev) * 128;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int f = (DUAL ? warp * 16 : warp * 32 + mt * 16) + h * 8 + rev;
+        const int f = (DUAL ? warp % (GQ_WARPS / 2) : warp) * 16 + h * 8 + rev;
         const long long at = (long long)min(n0 + f, a.n_out - 1) * a.ng;   // features behind the last one: any scales, codes are 0
-        row[mt][h] = (uint32_t)((DUAL ? mt * 64 : 0) + f) * 128;
-        rd[mt][h].s = (const uint8_t*)a.scales[DUAL ? mt : 0] + at * (FP32 ? 4 : 2);
-        rd[mt][h].z = a.zeros[DUAL ? mt : 0] ? a.zeros[DUAL ? mt : 0] + at : nullptr;
+        rd[h].s = (const uint8_t*)a.scales[mat] + at * (FP32 ? 4 : 2);
+        rd[h].z = a.zeros[mat] ? a.zeros[mat] + at : nullptr;
       }
     constexpr int CH = GroupReader<FP32>::CHUNK;
     int grp = b0 * P::GPT;
     auto fetch = [&](int g0) {
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) rd[mt][h].fetch(g0, t, a.ng, a.pairs != 0);
+        for (int h = 0; h < 2; ++h) rd[h].fetch(g0, t, a.ng, a.pairs != 0);
     };
     auto turn = [&](int g0) {                                 // the chunk that was requested becomes the present one
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
         for (int h = 0; h < 2; ++h) {
-          rd[mt][h].c = rd[mt][h].n;
-          rd[mt][h].cz = rd[mt][h].nz;
+          rd[h].c = rd[h].n;
+          rd[h].cz = rd[h].nz;
         }
       fetch(g0 + CH);
     };
@@ -306,13 +317,11 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       const uint32_t sw = (uint32_t)rev << 4;                 // swizzle: rows rev and 8 + rev of a tile have the same low bits
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        uint32_t cw[2][2][4];
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        uint32_t cw[2][4];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            uint32_t* c = cw[mt][h];
-            const uint32_t at = base + row[mt][h];
+            uint32_t* c = cw[h];
+            const uint32_t at = base + row0 + h * 8 * 128;
             if (G == 128) {
               const uint4 x = gq_lds128(at + (((hf * 4 + t) << 4) ^ sw));
               c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
@@ -327,57 +336,48 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(c[q]) : "r"(at + (((hf * 4 + q) << 4) ^ sw) + t * 4) : "memory");
             }
           }
-        float ga[2][NT][4];
+        float ga[NT][4];
         constexpr int WPG = G / 32;                           // words per group
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           if (w % WPG == 0) {
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-              for (int j = 0; j < NT; ++j) ga[mt][j][0] = ga[mt][j][1] = ga[mt][j][2] = ga[mt][j][3] = 0.f;
+              for (int j = 0; j < NT; ++j) ga[j][0] = ga[j][1] = ga[j][2] = ga[j][3] = 0.f;
           }
-          uint32_t x[2][2][4];                                // [tile][codes 0 4 1 5 | 2 6 3 7]
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+          uint32_t x[2][4];                              // codes 0 4 1 5 | 2 6 3 7
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint32_t lo = cw[mt][h][w], hi = lo >> 8;
-              x[mt][0][h] = lo & 0x000f000fu;
-              x[mt][0][2 + h] = lo & 0x00f000f0u;
-              x[mt][1][h] = hi & 0x000f000fu;
-              x[mt][1][2 + h] = hi & 0x00f000f0u;
+              const uint32_t lo = cw[h][w], hi = lo >> 8;
+              x[0][h] = lo & 0x000f000fu;
+              x[0][2 + h] = lo & 0x00f000f0u;
+              x[1][h] = hi & 0x000f000fu;
+              x[1][2 + h] = hi & 0x00f000f0u;
             }
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             const uint4 b = gq_lds128(tb + j * P::CHUNK + (hf * 4 + w) * 512);
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) mma_f16(ga[mt][j], x[mt][0], b.x, b.y);
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) mma_f16(ga[mt][j], x[mt][1], b.z, b.w);
+            mma_f16(ga[j], x[0], b.x, b.y);
+            mma_f16(ga[j], x[1], b.z, b.w);
           }
           if (w % WPG == WPG - 1) {
             constexpr int HG = 4 / WPG;                       // groups per 128 k
             const int gi = hf * HG + w / WPG;
             if (((grp & (CH - 1)) == 0) || (i == 0 && gi == 0)) turn(grp & ~(CH - 1));
-            float sc[2][2], mz[2][2];
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            float sc[2], mz[2];
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                if (gi & 1) rd[mt][h].template get<1>(grp, lane, sc[mt][h], mz[mt][h]);
-                else rd[mt][h].template get<0>(grp, lane, sc[mt][h], mz[mt][h]);
+                if (gi & 1) rd[h].template get<1>(grp, lane, sc[h], mz[h]);
+                else rd[h].template get<0>(grp, lane, sc[h], mz[h]);
               }
             ++grp;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-              const uint4 y = gq_lds128(base + GQ_CODES + j * P::CHUNK + GQ_TERMS + gi * 64 + t * 16);   // q, 2^(e + 12) of rows 2 t, 2 t + 1
-              const float q[2] = {__uint_as_float(y.x), __uint_as_float(y.z)}, f[2] = {__uint_as_float(y.y), __uint_as_float(y.w)};
-#pragma unroll
-              for (int mt = 0; mt < 2; ++mt)
+              float q[2];                                     // of rows 2 t, 2 t + 1
+              asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(q[0]), "=f"(q[1])
+                           : "r"(base + GQ_CODES + j * P::CHUNK + GQ_ROWS + gi * 32 + t * 8) : "memory");
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  acc[mt][j][e] = fmaf(sc[mt][e >> 1] * f[e & 1], fmaf(mz[mt][e >> 1], q[e & 1], ga[mt][j][e]), acc[mt][j][e]);
+                  acc[j][e] = fmaf(sc[e >> 1], fmaf(mz[e >> 1], q[e & 1], ga[j][e]), acc[j][e]);
             }
           }
         }
@@ -391,15 +391,13 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   // ---- sums of the cluster, epilogue ----
   __syncthreads();
   const bool good = *s_abort == 0;
-  if (warp < 4) {
+  if (warp < GQ_WARPS) {
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + (DUAL ? mt * 64 + warp * 16 : warp * 32 + mt * 16) + (e >> 1) * 8 + rev] = acc[mt][j][e] * 4096.f;
+          sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + warp * 16 + (e >> 1) * 8 + rev] = acc[j][e];
   }
   if (S > 1) cluster_sync_all(); else __syncthreads();
   if (M > 0 && good) {
@@ -422,13 +420,15 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       const int r = i / cols, col = 4 * (c0 + i % cols), nn = n0 + col;
       if (nn >= a.n_out) continue;
       const long long out = (long long)(r0 + r) * a.n_out + nn;
+      const int ex = __ldcg(a.row_exp + r0 + r);              // the row's power of two, in two normal factors
+      const float p0 = gq_pow2(ex / 2), p1 = gq_pow2(ex - ex / 2);
       const float4 y = total(r * P::PITCH + col);
-      float x[4] = {y.x, y.y, y.z, y.w};
+      float x[4] = {y.x * p0 * p1, y.y * p0 * p1, y.z * p0 * p1, y.w * p0 * p1};
       if (DUAL) {
         const float4 u = total(r * P::PITCH + 64 + col);
         const float up[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = x[e] / (1.f + __expf(-x[e])) * up[e];
+        for (int e = 0; e < 4; ++e) x[e] = x[e] / (1.f + __expf(-x[e])) * (up[e] * p0 * p1);
       }
       if (epilogue == EPI_RESIDUAL && !DUAL) {
         float* c = reinterpret_cast<float*>(a.C) + out;
@@ -508,19 +508,19 @@ template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const G
   return launch_gq<G, 8, DUAL, FP32>(w, a, epilogue, st);
 }
 template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
-  const unsigned per_row = (unsigned)(((a.K + GQ_BK - 1) / GQ_BK * (GQ_BK / 8) + GS_THREADS - 1) / GS_THREADS);
-  SL_CUDA_TRY(launch_pdl(gq_rewrite_rows_kernel<G>, dim3(per_row, a.max_rows), dim3(GS_THREADS), 0, st, (const bf16*)A, a.n_active, a.max_rows,
-                         a.K, (uint8_t*)a.terms));
+  SL_CUDA_TRY(launch_pdl(gq_rewrite_rows_kernel<G>, dim3(a.max_rows), dim3(GS_THREADS), 0, st, (const bf16*)A, a.n_active, a.max_rows, a.K,
+                         (uint8_t*)a.rows, (int32_t*)a.row_exp));
   if (epilogue == EPI_SWIGLU) return fp32 ? by_rows<G, true, true>(w, a, epilogue, st) : by_rows<G, true, false>(w, a, epilogue, st);
   return fp32 ? by_rows<G, false, true>(w, a, epilogue, st) : by_rows<G, false, false>(w, a, epilogue, st);
 }
 
 }  // namespace
 
-// room for the rewritten rows with the smallest groups
-size_t gemm_quantized_workspace_bytes(int max_rows, int K) {
+// the rewritten rows, with room for the smallest groups, and their exponents
+static size_t gq_rows_bytes(int max_rows, int K) {
   return (size_t)((K + GQ_BK - 1) / GQ_BK) * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
 }
+size_t gemm_quantized_workspace_bytes(int max_rows, int K) { return gq_rows_bytes(max_rows, K) + (size_t)max_rows * sizeof(int32_t); }
 
 int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active, int max_rows,
                           int n_out, int K, int epilogue, void* workspace, int32_t* status, cudaStream_t st) {
@@ -537,7 +537,8 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
     const int rc = gq_map(&maps[i], w->codes, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128);
     if (rc != SL_OK) return rc;
   }
-  a.terms = (const uint8_t*)workspace;
+  a.rows = (const uint8_t*)workspace;
+  a.row_exp = reinterpret_cast<const int32_t*>((const uint8_t*)workspace + gq_rows_bytes(max_rows, K));
   a.C = C;
   a.n_active = n_active;
   a.max_rows = max_rows;
