@@ -8,9 +8,9 @@
 //
 // Exact rounding without a division per element: x times an approximate 1 / s (2^-23) is within 2^-22 of the quotient, so
 // when the products by (1 + 2^-21) / s and (1 - 2^-21) / s round to the same code, that is the code of the exact quotient
-// too.  Otherwise (about one value in 10^5) the quotient is formed truncated with its lowest bit set when it is inexact ("round to odd"), whose
-// rounding to a code's few bits is that of the exact value.  Rows below 2^-64 are first multiplied by 2^64 (exactly), so
-// that 1 / s is a normal number and the remainder in the odd rounding stays representable.
+// too.  Otherwise the sign of x - b s, b the border between the two codes, settles it: one fma, so the sign is exact.  (With
+// bf16 inputs this is not rare: where the largest magnitude has a factor 7, one value in 16 lies on a border.)  Rows below
+// 2^-64 are first multiplied by 2^64 (exactly), so that 1 / s is a normal number and x - b s does not underflow.
 //
 // Memory-bound: DH / 8 lanes take one (row, head) of K and of V, 8 elements a lane in 16-byte loads, all loads issued before
 // the first use; the 8-byte stores of a half-warp (DH = 128) fill one 128-byte line, as one head's places in a page are
@@ -86,14 +86,18 @@ __device__ __forceinline__ void widen8(const Raw8<float>& r, float* x) {
   for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
 }
 // bits of the largest magnitudes of K's and of V's elements over the lanes of a (row, head) (magnitudes order like their
-// bits, NaN above all); bf16 pairs are compared two at a time, and K's and V's travel together
+// bits, NaN above all); bf16 pairs are compared two at a time, and K's and V's go through the shuffles together
 template <int LANES> __device__ __forceinline__ void tops(const Raw8<bf16>& k, const Raw8<bf16>& v, uint32_t& tk, uint32_t& tv) {
+  auto top = [](uint32_t x, uint32_t y) {            // of magnitudes, two at a time; a NaN stays one
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&x), *reinterpret_cast<__nv_bfloat162*>(&y));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  };
   constexpr uint32_t A = 0x7fff7fffu;
-  const uint32_t a = __vmaxu2(__vmaxu2(k.u.x & A, k.u.y & A), __vmaxu2(k.u.z & A, k.u.w & A));
-  const uint32_t b = __vmaxu2(__vmaxu2(v.u.x & A, v.u.y & A), __vmaxu2(v.u.z & A, v.u.w & A));
-  uint32_t both = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+  const uint32_t a = top(top(k.u.x & A, k.u.y & A), top(k.u.z & A, k.u.w & A));
+  const uint32_t b = top(top(v.u.x & A, v.u.y & A), top(v.u.z & A, v.u.w & A));
+  uint32_t both = top(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+  for (int o = LANES / 2; o > 0; o >>= 1) both = top(both, __shfl_xor_sync(0xffffffffu, both, o));
   tk = both << 16;
   tv = both & 0xffff0000u;
 }
@@ -144,11 +148,33 @@ template <int KIND> __device__ __forceinline__ uint32_t codes4(float a, float b,
     return __byte_perm(lo, hi, 0x5410);
   }
 }
-// x / s truncated, lowest bit set when inexact: rounds to a shorter format as the exact quotient does
-__device__ __noinline__ float quotient_to_odd(float x, float s) {
-  const float q = __fdiv_rz(x, s);
-  return __fmaf_rn(-q, s, x) != 0.f ? __uint_as_float(__float_as_uint(q) | 1u) : q;
+// the numbers that four codes stand for
+template <int KIND> __device__ __forceinline__ void values4(uint32_t c, float* v) {
+  if (KIND == SL_E4M3) {
+    const uint32_t lo = e4m3x2_to_f16x2((uint16_t)(c & 0xffffu)), hi = e4m3x2_to_f16x2((uint16_t)(c >> 16));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(c >> (8 * i));
+  }
 }
+// the codes of the exact quotients x / s, which lie between those of `low` and `high` (neighbours or the same): on which side
+// of the border b between the two is told by the sign of x - b s, which one fma gives exactly; on the border the conversion
+// takes the even one
+template <int KIND> __device__ __forceinline__ uint32_t settle4(const float* x, float s, uint32_t low, uint32_t high) {
+  float a[4], b[4];
+  values4<KIND>(low, a);
+  values4<KIND>(high, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    b[i] = 0.5f * (a[i] + b[i]);
+    const float r = fmaf(-b[i], s, x[i]), step = fabsf(b[i]) * 9.5367431640625e-7f;   // 2^-20
+    b[i] += r > 0.f ? step : r < 0.f ? -step : 0.f;
+  }
+  return codes4<KIND>(b[0], b[1], b[2], b[3]);
+}
+
 // quantise the 8 elements of this lane; top = bits of the largest magnitude of the whole (row, head).  Returns the scale.
 template <int KIND> __device__ __forceinline__ float quantise8(float* x, uint32_t top, uint2& out) {
   constexpr float Q = KvKind<KIND>::QMAX, RQ = 1.f / Q;
@@ -178,8 +204,8 @@ template <int KIND> __device__ __forceinline__ float quantise8(float* x, uint32_
     mul4(p, up, y);
     mul4(p, down, z);
     c[h] = codes4<KIND>(y[0], y[1], y[2], y[3]);
-    if (c[h] != codes4<KIND>(z[0], z[1], z[2], z[3]))
-      c[h] = codes4<KIND>(quotient_to_odd(p[0], s), quotient_to_odd(p[1], s), quotient_to_odd(p[2], s), quotient_to_odd(p[3], s));
+    const uint32_t other = codes4<KIND>(z[0], z[1], z[2], z[3]);
+    if (c[h] != other) c[h] = settle4<KIND>(p, s, other, c[h]);
   }
   out = make_uint2(c[0], c[1]);
   return scale;
