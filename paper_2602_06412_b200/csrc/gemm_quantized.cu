@@ -30,51 +30,23 @@
 // The first codes are requested before the rewriting kernel has finished: it does not write them.  K is split over the CTAs
 // of a cluster when the features alone do not fill the GPU; the sums meet through distributed shared memory in a fixed
 // order: deterministic.  All waits are bounded.
-#include <cuda_fp16.h>
-
-#include <mutex>
-
-#include "tc_common.cuh"
+#include "gemm_quantized.cuh"
 
 namespace sl {
 
 namespace {
 
-constexpr int GQ_BK = 256;             // k per stage
-constexpr int GQ_CODES = 128 * GQ_BK / 2;
 constexpr int GQ_WARPS = 8, GQ_THREADS = 32 * GQ_WARPS + 32;
 constexpr int GQ_ROWS = 8 * GQ_BK * 2;   // bytes of 8 rewritten rows in a stage
-
-struct GqArgs {
-  const uint8_t *zeros[2], *rows;
-  const void* scales[2];
-  void* C;
-  const int32_t* n_active;
-  const int32_t* row_exp;              // e + 24 of every row
-  int max_rows, n_out, K, ng;
-  int pairs;                           // scales and zero points of two neighbouring groups lie on aligned addresses
-  int32_t* status;
-};
 
 __device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint4 gq_lds128(uint32_t a) {
-  uint4 r;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
-  return r;
-}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ float gq_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 // Scales and zero points of one feature, shared out over the four lanes that work on it: a chunk of 8 groups (bf16 scales,
 // two groups per lane) or 4 (fp32, one per lane); the next chunk is requested when one begins.  Zero points are kept like
@@ -136,13 +108,14 @@ template <int G, int NT> struct GqPlan {
 // ---- the rewritten rows ----------------------------------------------------------------------------------------------
 // One CTA per row, 8 k per thread at a time.  A row with an infinity or a NaN is NaN throughout.  Out: per (256 k, 8 rows) one
 // chunk of GqPlan::CHUNK bytes, [word of a code fragment][lane] of 16 bytes: a' of the 8 k whose codes that word holds, in the
-// order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16), zeros behind K; then q of the groups, [group][row].  And e + 24 per row.
+// order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16), zeros behind K; then q of the groups, [group][row].  Or, not in FRAGMENTS, the
+// same 16 bytes row by row, and q apart, [group][ld].  And e + 24 per row.
 constexpr int GS_THREADS = 512;
 
-template <int G>
+template <int G, bool FRAGMENTS>
 __global__ void __launch_bounds__(GS_THREADS)
 gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, uint8_t* __restrict__ rows,
-                       int32_t* __restrict__ row_exp) {
+                       float* __restrict__ sums, int ld, int32_t* __restrict__ row_exp) {
   __shared__ uint32_t sTop[GS_THREADS / 32];
   griddep_wait();
   griddep_launch();
@@ -196,12 +169,18 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
     for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const int block = i / 32, k8 = i % 32, in = k8 % 16;
     if (block < blocks) {
-      const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
-      const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
-      uint8_t* chunk = rows + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
-      *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
-      if (k8 % (G / 8) == 0)
-        *reinterpret_cast<float*>(chunk + GQ_ROWS + k8 / (G / 8) * 32 + (r % 8) * 4) = sum * 5.9604644775390625e-8f;
+      const uint4 y = make_uint4(out[0], out[1], out[2], out[3]);
+      const float q = sum * 5.9604644775390625e-8f;
+      if (FRAGMENTS) {
+        const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
+        const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
+        uint8_t* chunk = rows + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
+        *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) = y;
+        if (k8 % (G / 8) == 0) *reinterpret_cast<float*>(chunk + GQ_ROWS + k8 / (G / 8) * 32 + (r % 8) * 4) = q;
+      } else {
+        *reinterpret_cast<uint4*>(rows + ((long long)r * blocks * 32 + i) * 16) = y;
+        if (i % (G / 8) == 0) sums[(long long)(i / (G / 8)) * ld + r] = q;
+      }
     }
   }
 }
@@ -401,67 +380,18 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   }
   if (S > 1) cluster_sync_all(); else __syncthreads();
   if (M > 0 && good) {
-    const uint32_t sred = smem_u32(sRed);
-    auto total = [&](int at) {                                // four neighbouring features, the CTAs in order
-      if (S == 1) return *reinterpret_cast<const float4*>(sRed + at);
-      float4 p[8], x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (uint32_t s = 0; s < 8; ++s)
-        if (s < S) p[s] = ld_cluster_f4(mapa_u32(sred + 4 * at, s));
-#pragma unroll
-      for (uint32_t s = 0; s < 8; ++s)
-        if (s < S) {
-          x.x += p[s].x; x.y += p[s].y; x.z += p[s].z; x.w += p[s].w;
-        }
-      return x;
-    };
     const int c0 = (int)(TO / 4 * rank / S), cols = (int)(TO / 4 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
     for (int i = threadIdx.x; i < min(M, 8 * NT) * cols; i += GQ_THREADS) {
-      const int r = i / cols, col = 4 * (c0 + i % cols), nn = n0 + col;
-      if (nn >= a.n_out) continue;
-      const long long out = (long long)(r0 + r) * a.n_out + nn;
-      const int ex = __ldcg(a.row_exp + r0 + r);              // the row's power of two, in two normal factors
-      const float p0 = gq_pow2(ex / 2), p1 = gq_pow2(ex - ex / 2);
-      const float4 y = total(r * P::PITCH + col);
-      float x[4] = {y.x * p0 * p1, y.y * p0 * p1, y.z * p0 * p1, y.w * p0 * p1};
-      if (DUAL) {
-        const float4 u = total(r * P::PITCH + 64 + col);
-        const float up[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = x[e] / (1.f + __expf(-x[e])) * (up[e] * p0 * p1);
-      }
-      if (epilogue == EPI_RESIDUAL && !DUAL) {
-        float* c = reinterpret_cast<float*>(a.C) + out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (nn + e < a.n_out) c[e] += x[e];
-      } else {
-        bf16* c = reinterpret_cast<bf16*>(a.C) + out;
-        if ((a.n_out & 3) == 0) {
-          *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (nn + e < a.n_out) c[e] = __float2bfloat16_rn(x[e]);
-        }
-      }
+      const int r = i / cols, col = 4 * (c0 + i % cols);
+      if (n0 + col >= a.n_out) continue;
+      const float4 y = gq_total(sRed, S, r * P::PITCH + col);
+      gq_store<DUAL>(a, epilogue, r0 + r, n0 + col, y, DUAL ? gq_total(sRed, S, r * P::PITCH + 64 + col) : y);
     }
   }
   if (S > 1) cluster_sync_all();                              // the others may still be reading this CTA's partial sums
 }
 
 namespace {
-
-// codes [n_out][K / 2], boxes of `rows` features x 128 bytes, zeros out of bounds
-int gq_map(CUtensorMap* out, const void* p, long long n_out, long long row_bytes, int rows) {
-  TensorMapEncodeFn fn = tensor_map_encode_fn();
-  if (!fn) return SL_ECUDA;
-  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)n_out}, strides[1] = {(cuuint64_t)row_bytes};
-  const cuuint32_t box[2] = {GQ_BK / 2, (cuuint32_t)rows}, one[2] = {1, 1};
-  const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? SL_OK : SL_ECUDA;
-}
 
 template <int G, int NT, bool DUAL, bool FP32>
 int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
@@ -477,48 +407,45 @@ int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
   static cudaError_t attr;
   std::call_once(once, [&] { attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P::SMEM); });
   SL_CUDA_TRY(attr);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tiles * S, row_tiles);
-  cfg.blockDim = dim3(GQ_THREADS);
-  cfg.dynamicSmemBytes = P::SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  int n = 0;
-  at[n].id = cudaLaunchAttributeClusterDimension;
-  at[n].val.clusterDim.x = S;
-  at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
-  ++n;
-  if (pdl_enabled()) {
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
-  cfg.attrs = at;
-  cfg.numAttrs = n;
-  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, w[0], w[1], a, epilogue));
+  SL_CUDA_TRY(gq_launch(kernel, dim3(tiles * S, row_tiles), GQ_THREADS, P::SMEM, S, st, w[0], w[1], a, epilogue));
   return SL_OK;
 }
 
-// rows to a pass: 8 to 64, as many as there are
+constexpr int GQ_FEW = 32;             // most rows of the kernel for few rows
+
 template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
   if (a.max_rows <= 8) return launch_gq<G, 1, DUAL, FP32>(w, a, epilogue, st);
   if (a.max_rows <= 16) return launch_gq<G, 2, DUAL, FP32>(w, a, epilogue, st);
   if (a.max_rows <= 24) return launch_gq<G, 3, DUAL, FP32>(w, a, epilogue, st);
-  if (a.max_rows <= 32) return launch_gq<G, 4, DUAL, FP32>(w, a, epilogue, st);
-  return launch_gq<G, 8, DUAL, FP32>(w, a, epilogue, st);
+  return launch_gq<G, 4, DUAL, FP32>(w, a, epilogue, st);
 }
-template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
-  SL_CUDA_TRY(launch_pdl(gq_rewrite_rows_kernel<G>, dim3(a.max_rows), dim3(GS_THREADS), 0, st, (const bf16*)A, a.n_active, a.max_rows, a.K,
-                         (uint8_t*)a.rows, (int32_t*)a.row_exp));
+template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, float* q, int ld, int epilogue, bool fp32, cudaStream_t st) {
+  const bool few = a.max_rows <= GQ_FEW;
+  SL_CUDA_TRY(launch_pdl(few ? gq_rewrite_rows_kernel<G, true> : gq_rewrite_rows_kernel<G, false>, dim3(a.max_rows), dim3(GS_THREADS), 0, st,
+                         (const bf16*)A, a.n_active, a.max_rows, a.K, (uint8_t*)a.rows, q, ld, (int32_t*)a.row_exp));
+  if (!few) return launch_gemm_quantized_tc(w, a, q, ld, G, fp32, epilogue, st);
   if (epilogue == EPI_SWIGLU) return fp32 ? by_rows<G, true, true>(w, a, epilogue, st) : by_rows<G, true, false>(w, a, epilogue, st);
   return fp32 ? by_rows<G, false, true>(w, a, epilogue, st) : by_rows<G, false, false>(w, a, epilogue, st);
 }
 
 }  // namespace
 
-// the rewritten rows, with room for the smallest groups, and their exponents
+int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, long long rows, long long cols, int box_rows, int box_cols) {
+  TensorMapEncodeFn fn = tensor_map_encode_fn();
+  if (!fn) return SL_ECUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * elem};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
+  const CUresult r = fn(out, type, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        box_cols * elem == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? SL_OK : SL_ECUDA;
+}
+
+// the workspace: the rewritten rows in either layout with room for the smallest groups, then their exponents
 static size_t gq_rows_bytes(int max_rows, int K) {
-  return (size_t)((K + GQ_BK - 1) / GQ_BK) * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
+  const size_t blocks = (K + GQ_BK - 1) / GQ_BK;
+  if (max_rows <= GQ_FEW) return blocks * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
+  return blocks * GQ_BK * 2 * max_rows + blocks * (GQ_BK / 32) * ((max_rows + 3) / 4 * 4) * 4;
 }
 size_t gemm_quantized_workspace_bytes(int max_rows, int K) { return gq_rows_bytes(max_rows, K) + (size_t)max_rows * sizeof(int32_t); }
 
@@ -528,13 +455,14 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   GqArgs a{};
   CUtensorMap maps[2];
   a.ng = K / W->group;
-  a.pairs = a.ng % 2 == 0;
+  const bool fp32 = W->scale_dtype == SL_FP32, few = max_rows <= GQ_FEW;
+  a.pairs = a.ng % (few || fp32 ? 2 : 4) == 0;
   for (int i = 0; i < 2; ++i) {
     const surelock_w4* w = i && W2 ? W2 : W;
     a.zeros[i] = (const uint8_t*)w->zeros;
     a.scales[i] = w->scales;
-    if ((reinterpret_cast<uintptr_t>(w->scales) & 3) || (reinterpret_cast<uintptr_t>(w->zeros) & 1)) a.pairs = 0;
-    const int rc = gq_map(&maps[i], w->codes, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128);
+    if ((reinterpret_cast<uintptr_t>(w->scales) & 7) || (reinterpret_cast<uintptr_t>(w->zeros) & 3)) a.pairs = 0;
+    const int rc = gq_map(&maps[i], w->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128, GQ_BK / 2);
     if (rc != SL_OK) return rc;
   }
   a.rows = (const uint8_t*)workspace;
@@ -545,11 +473,12 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   a.n_out = n_out;
   a.K = K;
   a.status = status;
-  const bool fp32 = W->scale_dtype == SL_FP32;
+  const int ld = (max_rows + 3) / 4 * 4;             // rows of 16 bytes
+  float* q = reinterpret_cast<float*>((uint8_t*)workspace + (size_t)((K + GQ_BK - 1) / GQ_BK) * GQ_BK * 2 * max_rows);   // of the row-by-row layout
   switch (W->group) {
-    case 32: return by_kind<32>(maps, A, a, epilogue, fp32, st);
-    case 64: return by_kind<64>(maps, A, a, epilogue, fp32, st);
-    default: return by_kind<128>(maps, A, a, epilogue, fp32, st);
+    case 32: return by_kind<32>(maps, A, a, q, ld, epilogue, fp32, st);
+    case 64: return by_kind<64>(maps, A, a, q, ld, epilogue, fp32, st);
+    default: return by_kind<128>(maps, A, a, q, ld, epilogue, fp32, st);
   }
 }
 
