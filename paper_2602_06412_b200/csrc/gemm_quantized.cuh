@@ -78,7 +78,7 @@ template <bool DUAL> __device__ __forceinline__ void gq_store(const GqArgs& a, i
   }
 }
 
-// 2-D row-major tensor map, 128-byte swizzle for boxes of 128-byte rows, zeros out of bounds
+// 2-D row-major tensor map, zeros out of bounds; operands (not fp32) in boxes of 128-byte rows under the 128-byte swizzle
 int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, long long rows, long long cols, int box_rows, int box_cols);
 // launch with a cluster of S CTAs along x and programmatic dependent launch
 template <typename... KArgs, typename... Args>
