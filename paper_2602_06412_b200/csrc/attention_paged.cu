@@ -79,6 +79,17 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
   return r;
 }
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 r;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
+  return r;
+}
+// 8 x 8 matrix of 16-bit elements, two of a row per lane
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
 __device__ __forceinline__ void ldsm_x4_t(uint32_t a, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
@@ -164,7 +175,8 @@ template <int MT> __host__ __device__ constexpr int ap_occupancy() { return MT <
 template <int DH, int KIND, int MT> struct Plan {
   using T = Tile<DH, KIND>;
   static constexpr int TILES = MT ? MT : 1;
-  static constexpr int FIXED = 1024 + TILES * T::STEPS * 512 + TILES * 4 * 512 + 16 * TILES * 4 * 9 + 256;   // Q, P, row factors, statistics
+  static constexpr int EXCHANGE = MT ? MT * 4 * 512 : 4 * 8 * (DH + 4) * 4;   // weights, or the warps' results
+  static constexpr int FIXED = 1024 + TILES * T::STEPS * 512 + EXCHANGE + 16 * TILES * 4 * 9 + 256;   // Q, exchange, row factors, statistics
   static constexpr int ROOM = 228 * 1024 / ap_occupancy<MT>() - 1024 - 256 - FIXED;                // 256: prefix sums of up to 31 sequences
   static constexpr int FIT = ROOM / T::STAGE;
   static constexpr int STAGES = FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
@@ -252,7 +264,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   uint8_t* sStage = smem;
   uint4* sQ = reinterpret_cast<uint4*>(sStage + STAGES * T::STAGE);                         // [TILES][STEPS][32]
   uint4* sP = sQ + TILES * T::STEPS * 32;                                                   // [TILES][4][32]
-  float* sRow = reinterpret_cast<float*>(sP + TILES * 4 * 32);                                 // [ROWS] factor of S
+  float* sJoin = reinterpret_cast<float*>(sP);                                              // [4][8][DH + 4]: MT = 0
+  float* sRow = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(sP) + Plan<DH, KIND, MT>::EXCHANGE);   // [ROWS] factor of S
   float* sM = sRow + ROWS;                                                                  // [4][ROWS]
   float* sL = sM + 4 * ROWS;                                                                // [4][ROWS]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sL + 4 * ROWS);
@@ -417,7 +430,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         }
       }
       bar_consumers();
-      constexpr int VT = DH / 64;                              // tiles of 16 columns per warp
+      constexpr int VT = DH / 16;                              // tiles of 16 columns
       uint2 qb[T::STEPS];
 #pragma unroll
       for (int i = 0; i < T::STEPS; ++i) qb[i] = reinterpret_cast<const uint2*>(sQ)[i * 32 + lane];
@@ -426,16 +439,15 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
       int E[2] = {AP_E_LEAST, AP_E_LEAST};
 #pragma unroll
       for (int j = 0; j < VT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-      __half* sPh = reinterpret_cast<__half*>(sP);
-      const int pput = (warp >> 1) * 256 + (8 * t + (g >> 1)) * 8 + (warp & 1) * 4 + (g & 1);   // [2][lane of the reader][step & 1][key / 8][key & 1]
-
       for (int j = blk0; j < blk0 + nblk; ++j, ++cnt) {
         const int st = (int)(cnt % STAGES);
-        if (ok) ok = warp_wait(full(st), (cnt / STAGES) & 1, s_abort);
-        const int here = min(s.len - j * AP_KEYS, AP_KEYS);    // keys of the unit
-        const int left = here - (int)jkey;                     // of this warp: 16 or more, fewer, none
+        if (!(ok = warp_wait(full(st), (cnt / STAGES) & 1, s_abort))) break;
+        const int left = s.len - j * AP_KEYS - (int)jkey;      // keys from this warp's first one on
         const uint32_t kb = smem_u32(sStage + st * T::STAGE), vb = kb + T::KV;
-        if (left > 0 && left < 16) clear_rows<T>(vb, (int)jkey, left, lane);
+        if (left > 0 && left < 16) {
+          clear_rows<T>(vb, (int)jkey, left, lane);
+          __syncwarp();
+        }
         float sc[2][4] = {};                                   // two chains; key g + 8 (i >> 1), row 2 t + (i & 1)
         float ks[2] = {0.f, 0.f}, vs[2] = {0.f, 0.f};
         if (left > 0) {
@@ -475,100 +487,86 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
             }
           }
         }
-        float x[4];
-        bool grow = !ok;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = (sc[0][i] + sc[1][i]) * fr[i & 1];
-          if (T::SCALED) x[i] *= ks[i >> 1];
-          x[i] = 8 * (i >> 1) + g < left ? x[i] : -INFINITY;
-          grow |= x[i] > m[i & 1] + AP_TAU;
-        }
-        auto row_tops = [&](float x0, float x1, float* top) {  // over all keys of the unit
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
-            x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
-          }
-          if (g == 0) {
-            sM[warp * ROWS + 2 * t] = x0;
-            sM[warp * ROWS + 2 * t + 1] = x1;
-          }
-          bar_consumers();
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float* p = sM + 2 * t + i;
-            top[i] = fmaxf(fmaxf(p[0], p[ROWS]), fmaxf(p[2 * ROWS], p[3 * ROWS]));
-          }
-        };
-        auto rescale = [&](int i, float f) {
-#pragma unroll
-          for (int c = 0; c < VT; ++c) {
-            acc[c][i] *= f;
-            acc[c][i + 2] *= f;
-          }
-        };
-        if (consumers_any(grow)) {
-          if (!epilogue_warps_agree(ok)) {                     // a wait ran out: all four warps leave together
-            ok = false;
-            break;
-          }
-          float top[2];
-          row_tops(fmaxf(x[0], x[2]), fmaxf(x[1], x[3]), top);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) rescale(i, follow_max<T::SCALED>(m[i], l[i], E[i], top[i]));
-        }
-        bool over = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float mm = m[i & 1] == -INFINITY ? 0.f : m[i & 1];
-          x[i] = fast_exp2(x[i] - mm);
-          l[i & 1] += x[i];
-          if (T::SCALED) {
-            x[i] *= vs[i >> 1];
-            over |= fabsf(x[i] * pow2i(AP_W_EXP - E[i & 1])) >= AP_W_MOST;
-          }
-        }
-        auto put_weights = [&]() {
+        if (left > 0) {
+          float x[4];
+          bool grow = false;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int at = pput + (i & 1) * 32 + (i >> 1) * 2;
-            if (BF) reinterpret_cast<bf16*>(sPh)[at] = __float2bfloat16_rn(x[i]);
-            else sPh[at] = __float2half_rn(x[i] * pow2i(AP_W_EXP - E[i & 1]));
+            x[i] = (sc[0][i] + sc[1][i]) * fr[i & 1];
+            if (T::SCALED) x[i] *= ks[i >> 1];
+            x[i] = 8 * (i >> 1) + g < left ? x[i] : -INFINITY;
+            grow |= x[i] > m[i & 1] + AP_TAU;
           }
-        };
-        put_weights();
-        if (consumers_any(T::SCALED && over)) {
-          float top[2];
-          row_tops(fmaxf(fabsf(x[0]), fabsf(x[2])), fmaxf(fabsf(x[1]), fabsf(x[3])), top);
+          auto over_keys = [&](float a0, float a1) {           // the larger of the two, over this warp's 16 keys
+            float y = fmaxf(a0, a1);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) rescale(i, follow_weight(E[i], top[i]));
-          put_weights();
-          bar_consumers();
-        }
-        const uint4 p0 = sP[lane], p1 = sP[32 + lane];
-        const uint32_t pb[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+            for (int o = 4; o < 32; o <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, o));
+            return y;
+          };
+          auto rescale = [&](int i, float f) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (16 * k >= here) break;
+            for (int c = 0; c < VT; ++c) {
+              acc[c][i] *= f;
+              acc[c][i + 2] *= f;
+            }
+          };
+          if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float top = over_keys(x[i], x[i + 2]);
+              rescale(i, follow_max<T::SCALED>(m[i], l[i], E[i], top));
+            }
+          }
+          bool over = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float mm = m[i & 1] == -INFINITY ? 0.f : m[i & 1];
+            x[i] = fast_exp2(x[i] - mm);
+            l[i & 1] += x[i];
+            if (T::SCALED) {
+              x[i] *= vs[i >> 1];
+              over |= fabsf(x[i] * pow2i(AP_W_EXP - E[i & 1])) >= AP_W_MOST;
+            }
+          }
+          if (T::SCALED && __any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float top = over_keys(fabsf(x[i]), fabsf(x[i + 2]));
+              rescale(i, follow_weight(E[i], top));
+            }
+          }
+          // the weights to 16 bits, [key][row] -> [row][key]: the B operand of O^T += V^T P^T
+          const float u0 = T::SCALED ? pow2i(AP_W_EXP - E[0]) : 1.f, u1 = T::SCALED ? pow2i(AP_W_EXP - E[1]) : 1.f;
+          const uint32_t p0 = transposed(BF ? pack_bf16(x[0], x[1]) : pack_f16(x[0] * u0, x[1] * u1));
+          const uint32_t p1 = transposed(BF ? pack_bf16(x[2], x[3]) : pack_f16(x[2] * u0, x[3] * u1));
           if (BF) {
 #pragma unroll
             for (int c = 0; c < VT; ++c) {
               uint4 v;
-              const uint32_t key = 16 * k + (lane >> 4) * 8 + (lane & 7), chunk = 2 * (warp * VT + c) + ((lane >> 3) & 1);
+              const uint32_t key = jkey + (lane >> 4) * 8 + (lane & 7), chunk = 2 * c + ((lane >> 3) & 1);
               ldsm_x4_t(vb + (chunk >> 3) * T::SLAB + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), reinterpret_cast<uint32_t*>(&v));
-              mma16<BF>(acc[c], v, pb[2 * k], pb[2 * k + 1]);
+              mma16<BF>(acc[c], v, p0, p1);
             }
           } else {
-            uint32_t v[4];
-            load_values<DH>(vb, k, warp, g, t, v);
+            uint32_t v[4][VT / 2];                             // four keys, DH / 8 consecutive columns
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t key = jkey + (i >> 1) * 8 + 2 * t + (i & 1);
+              if (DH == 128) {
+                const uint4 y = lds128(vb + key * 128 + ((g ^ (key & 7)) << 4));
+                v[i][0] = y.x; v[i][1] = y.y; v[i][VT / 2 - 2] = y.z; v[i][VT / 2 - 1] = y.w;
+              } else {
+                const uint2 y = lds64(vb + key * 64 + (((g >> 1) ^ ((key >> 1) & 3)) << 4) + (g & 1) * 8);
+                v[i][0] = y.x; v[i][1] = y.y;
+              }
+            }
 #pragma unroll
             for (int c = 0; c < VT; ++c) {
-              const uint32_t sel = (DH == 128 ? c == 1 : (g & 1) == 1) ? 0x7362 : 0x5140;
+              const uint32_t sel = c & 1 ? 0x7362 : 0x5140;    // columns 2, 3 or 0, 1 of a word
               uint4 v4;
-              codes_to_f16<QK>(__byte_perm(v[0], v[1], sel), v4.x, v4.y);
-              codes_to_f16<QK>(__byte_perm(v[2], v[3], sel), v4.z, v4.w);
-              mma16<BF>(acc[c], v4, pb[2 * k], pb[2 * k + 1]);
+              codes_to_f16<QK>(__byte_perm(v[0][c / 2], v[1][c / 2], sel), v4.x, v4.y);
+              codes_to_f16<QK>(__byte_perm(v[2][c / 2], v[3][c / 2], sel), v4.z, v4.w);
+              mma16<BF>(acc[c], v4, p0, p1);
             }
           }
         }
@@ -576,11 +574,15 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         if (lane == 0) mbar_arrive(empty(st));
       }
 
+      // the four warps' results become one
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
-        if (g == 0) sL[warp * ROWS + 2 * t + i] = l[i];
+        if (g == 0) {
+          sM[warp * ROWS + 2 * t + i] = m[i];
+          sL[warp * ROWS + 2 * t + i] = l[i];
+        }
       }
       if (!epilogue_warps_agree(ok)) {
         if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
@@ -592,32 +594,53 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         const long long last = (u + s.nb - 1) / per;           // CTA of the item's last unit
         a.desc[blockIdx.x] = make_int4(s.r0, tile * ROWS, (valid << 16) | kvh, (int)last);
       }
+      constexpr int PITCH = DH + 4;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int row = 2 * t + i;
-        if (row >= valid) continue;
-        const float* p = sL + row;
-        const float sum = (p[0] + p[ROWS]) + (p[2 * ROWS] + p[3 * ROWS]);
-        const int e = tile * ROWS + row;
-        const float f = (T::SCALED ? pow2i(E[i] - AP_W_EXP) : 1.f) * (whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f);
-        bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + warp * (DH / 4);
-        float* part = a.part + (slot + row) * DH + warp * (DH / 4);
-        if (!whole && warp == 0 && g == 0) a.ml[slot + row] = make_float2(m[i], sum);
+        const float* p = sM + 2 * t + i;
+        const float top = fmaxf(fmaxf(p[0], p[ROWS]), fmaxf(p[2 * ROWS], p[3 * ROWS]));
+        const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top) * (T::SCALED ? pow2i(E[i] - AP_W_EXP) : 1.f);
+        float* dst = sJoin + (warp * 8 + 2 * t + i) * PITCH;
         if (BF) {
 #pragma unroll
-          for (int c = 0; c < VT; ++c)
-#pragma unroll
-            for (int b8 = 0; b8 < 2; ++b8) {
-              const float y = acc[c][2 * b8 + i] * f;
-              if (whole) o[16 * c + 8 * b8 + g] = __float2bfloat16_rn(y);
-              else part[16 * c + 8 * b8 + g] = y;
-            }
+          for (int c = 0; c < VT; ++c) {
+            dst[16 * c + g] = acc[c][i] * f;
+            dst[16 * c + 8 + g] = acc[c][2 + i] * f;
+          }
         } else {
 #pragma unroll
-          for (int c = 0; c < VT; ++c) {                       // consecutive columns 2 VT g ...
-            const float y0 = acc[c][i] * f, y1 = acc[c][i + 2] * f;
-            if (whole) *reinterpret_cast<uint32_t*>(o + 2 * VT * g + 2 * c) = pack_bf16(y0, y1);
-            else *reinterpret_cast<float2*>(part + 2 * VT * g + 2 * c) = make_float2(y0, y1);
+          for (int c = 0; c < VT; c += 2)                      // columns DH / 8 g + 2 c ...
+            *reinterpret_cast<float4*>(dst + 2 * VT * g + 2 * c) = make_float4(acc[c][i] * f, acc[c][2 + i] * f, acc[c + 1][i] * f, acc[c + 1][2 + i] * f);
+        }
+      }
+      bar_consumers();
+      {
+        const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
+        if (row < valid) {
+          float top = -INFINITY, sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) top = fmaxf(top, sM[w * ROWS + row]);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float mw = sM[w * ROWS + row];
+            sum += sL[w * ROWS + row] * (mw == -INFINITY ? 1.f : fast_exp2(mw - top));   // without keys 0, or NaN from a score that is none
+          }
+          const int e = tile * ROWS + row;
+          const float inv = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+          if (!whole && part == 0) a.ml[slot + row] = make_float2(top, sum);
+          bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH;
+          float* pt = a.part + (slot + row) * DH;
+#pragma unroll
+          for (int i = 0; i < DH / 64; ++i) {
+            const int col = i * 64 + part * 4;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float4 y = *reinterpret_cast<const float4*>(sJoin + (w * 8 + row) * PITCH + col);
+              x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+            }
+            if (whole) *reinterpret_cast<uint2*>(o + col) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+            else *reinterpret_cast<float4*>(pt + col) = x;
           }
         }
       }
