@@ -171,7 +171,7 @@ template <int DH, int KIND> struct Tile {
   static constexpr int STEPS = DH / 16;
 };
 // CTAs per SM that the registers are bounded for, and stages of the ring: what then fits the shared memory
-template <int MT> __host__ __device__ constexpr int ap_occupancy() { return MT <= 1 ? 4 : MT == 2 ? 3 : 2; }
+template <int MT> __host__ __device__ constexpr int ap_occupancy() { return MT <= 1 ? 4 : 3; }
 template <int DH, int KIND, int MT> struct Plan {
   using T = Tile<DH, KIND>;
   static constexpr int TILES = MT ? MT : 1;
@@ -964,72 +964,97 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
 }
 
 // The pieces of an item that run borders cut: o = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m), in unit order.  CTA
-// (c, y) has the item that starts in run c.  Of its 8 warps SPLIT take every SPLIT-th piece of a row each: 1 when there are
-// few pieces (a warp per row, 32 rows at once over the grid's 4 y), 8 when there are many.
-template <int DH, int ROWS, int SPLIT> __device__ __forceinline__ void join_rows(const PagedAttnArgs& a, const int4& d, float (*sO)[DH], float* sSum) {
+// (c, y) has the item that starts in run c.
+//
+// Few pieces (at most 16): a warp per row, 32 rows at once over the grid's 4 y; lane i has the statistics of piece i, and the
+// pieces' values are requested together with them.
+template <int DH, int ROWS> __device__ __forceinline__ void join_few(const PagedAttnArgs& a, const int4& d, int n) {
+  constexpr int PER = DH / 32, LOADS = 8;
+  const int valid = d.z >> 16, kvh = d.z & 0xffff, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int row = blockIdx.y * 8 + warp; row < valid; row += 32) {
+    auto slot = [&](int i) { return (long long)((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row; };
+    const float2 ml = lane < n ? a.ml[slot(lane)] : make_float2(-INFINITY, 0.f);
+    float w = 0.f, sum = 0.f, x[PER] = {};
+    for (int i0 = 0; i0 < n; i0 += LOADS) {
+      float2 p[LOADS][PER / 2];
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u)
+#pragma unroll
+        for (int c = 0; c < PER / 2; ++c)
+          p[u][c] = i0 + u < n ? reinterpret_cast<const float2*>(a.part + slot(i0 + u) * DH + lane * PER)[c] : make_float2(0.f, 0.f);
+      if (i0 == 0) {
+        float top = ml.x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
+        sum = ml.x == -INFINITY ? ml.y : w * ml.y;           // a piece without a maximum has the sum 0, or NaN
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      }
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) {
+        const float wi = __shfl_sync(0xffffffffu, w, i0 + u);
+#pragma unroll
+        for (int c = 0; c < PER / 2; ++c) {
+          x[2 * c] += wi * p[u][c].x;
+          x[2 * c + 1] += wi * p[u][c].y;
+        }
+      }
+    }
+    const int e = d.y + row;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    bf16* o = a.o + (long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + lane * PER;
+#pragma unroll
+    for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(x[c] * inv, x[c + 1] * inv);
+  }
+}
+// Many: the CTA's 8 warps take every eighth piece of a row each.
+template <int DH, int ROWS> __device__ __forceinline__ void join_many(const PagedAttnArgs& a, const int4& d, int n, float (*sO)[DH], float* sSum) {
   constexpr int PER = DH / 32, LOADS = 4;
-  const int valid = d.z >> 16, kvh = d.z & 0xffff, n = d.w - (int)blockIdx.x + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SPLIT;
-  auto slot = [&](int i, int row) { return (long long)((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row; };
-  for (int r0 = blockIdx.y * (8 / SPLIT); r0 < valid; r0 += 4 * (8 / SPLIT)) {
-    const int row = r0 + warp / SPLIT;
-    float sum = 0.f, x[PER] = {};
-    if (row < valid) {
-      float top = -INFINITY;
-      for (int i = lane; i < n; i += 32) top = fmaxf(top, a.ml[slot(i, row)].x);
+  const int valid = d.z >> 16, kvh = d.z & 0xffff, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int row = blockIdx.y; row < valid; row += 4) {
+    auto slot = [&](int i) { return (long long)((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row; };
+    float sum = 0.f, x[PER] = {}, top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, a.ml[slot(i)].x);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      for (int i0 = sub; i0 < n; i0 += SPLIT * LOADS) {
-        float2 ml[LOADS];
-        float p[LOADS][PER];
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int i0 = warp; i0 < n; i0 += 8 * LOADS) {
+      float2 ml[LOADS], p[LOADS][PER / 2];
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-          const int i = i0 + u * SPLIT;
-          ml[u] = make_float2(-INFINITY, 0.f);
+      for (int u = 0; u < LOADS; ++u) {
+        const int i = i0 + 8 * u;
+        ml[u] = i < n ? a.ml[slot(i)] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-          for (int c = 0; c < PER; ++c) p[u][c] = 0.f;
-          if (i < n) {
-            ml[u] = a.ml[slot(i, row)];
-            const float* src = a.part + slot(i, row) * DH + lane * PER;
+        for (int c = 0; c < PER / 2; ++c)
+          p[u][c] = i < n ? reinterpret_cast<const float2*>(a.part + slot(i) * DH + lane * PER)[c] : make_float2(0.f, 0.f);
+      }
 #pragma unroll
-            for (int c = 0; c < PER; c += 2) {
-              const float2 y = *reinterpret_cast<const float2*>(src + c);
-              p[u][c] = y.x;
-              p[u][c + 1] = y.y;
-            }
-          }
-        }
+      for (int u = 0; u < LOADS; ++u) {
+        const float w = ml[u].x == -INFINITY ? 0.f : fast_exp2(ml[u].x - top);
+        sum += ml[u].x == -INFINITY ? ml[u].y : w * ml[u].y;
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-          const float w = ml[u].x == -INFINITY ? 0.f : fast_exp2(ml[u].x - top);
-          sum += w * ml[u].y;
-#pragma unroll
-          for (int c = 0; c < PER; ++c) x[c] += w * p[u][c];
+        for (int c = 0; c < PER / 2; ++c) {
+          x[2 * c] += w * p[u][c].x;
+          x[2 * c + 1] += w * p[u][c].y;
         }
       }
     }
-    if (SPLIT > 1) {
 #pragma unroll
-      for (int c = 0; c < PER; ++c) sO[warp][lane * PER + c] = x[c];
-      if (lane == 0) sSum[warp] = sum;
-      __syncthreads();
-      if (sub == 0) {
+    for (int c = 0; c < PER; ++c) sO[warp][lane * PER + c] = x[c];
+    if (lane == 0) sSum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x < DH) {
+      float y = 0.f, l = 0.f;
 #pragma unroll
-        for (int w = 1; w < SPLIT; ++w) {
-          sum += sSum[warp + w];
-#pragma unroll
-          for (int c = 0; c < PER; ++c) x[c] += sO[warp + w][lane * PER + c];
-        }
+      for (int w = 0; w < 8; ++w) {
+        y += sO[w][threadIdx.x];
+        l += sSum[w];
       }
-    }
-    if (row < valid && sub == 0) {
       const int e = d.y + row;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      bf16* o = a.o + (long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + lane * PER;
-#pragma unroll
-      for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(x[c] * inv, x[c + 1] * inv);
+      a.o[(long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + threadIdx.x] =
+          __float2bfloat16_rn(l == 0.f ? 0.f : y / l);
     }
-    if (SPLIT > 1) __syncthreads();
+    __syncthreads();
   }
 }
 template <int DH, int ROWS>
@@ -1039,13 +1064,15 @@ __global__ void __launch_bounds__(256) attention_paged_join_kernel(const PagedAt
   griddep_wait();
   griddep_launch();
   const int4 d = a.desc[blockIdx.x];
-  if (d.w - (int)blockIdx.x < 16) join_rows<DH, ROWS, 1>(a, d, sO, sSum);
-  else join_rows<DH, ROWS, 8>(a, d, sO, sSum);
+  const int n = d.w - (int)blockIdx.x + 1;
+  if (d.z >> 16 == 0) return;
+  if (n <= 16) join_few<DH, ROWS>(a, d, n);
+  else join_many<DH, ROWS>(a, d, n, sO, sSum);
 }
 
 namespace {
 
-constexpr int AP_SLOT_ROWS = 128;   // most of (CTAs per SM) x (rows of a tile): 4 x 16, 3 x 32, 2 x 64
+constexpr int AP_SLOT_ROWS = 96;   // most of (CTAs per SM) x (rows of a tile): 4 x 8, 4 x 16, 3 x 32
 
 // pool [n_pages][Hkv][page_size][head_dim] (or its scales, without the last dimension) in boxes of at most 64 places
 int page_map(CUtensorMap* out, const surelock_paged_kv& c, void* base, bool scales) {
@@ -1137,16 +1164,17 @@ int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long 
   a.max_tokens = c.max_pages * c.page_size;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c.head_dim);
   a.status = status;
-  // rows of a tile: as many as a sequence has on average share the conversions of the codes; more would be padding
+  // Rows of a tile: what a sequence has on average, padded as little as possible, up to 32.  Tiles of 64 share the conversions
+  // of the codes among more rows, but leave fewer CTAs per SM: 4 x 8192 tokens, 64 rows each: 198 against 178 us; 1536 tokens,
+  // 128 rows: 37 against 31 us; tiles of 16 there: 222 and 33 us.
   const long long rows = ((long long)max_rows * a.G + B - 1) / B;
-  const int mt = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4, tile_rows = mt ? 16 * mt : 8;
+  const int mt = rows <= 8 ? 0 : rows <= 16 ? 1 : 2, tile_rows = mt ? 16 * mt : 8;
   const long long tiles = ((long long)max_rows * a.G + tile_rows - 1) / tile_rows + B;
   const long long max_units = tiles * a.Hkv * ((a.max_tokens + AP_KEYS - 1) / AP_KEYS);
 #define SL_AP(DH, KIND)                                                                                        \
   (mt == 0   ? launch_ap<DH, KIND, 0>(maps, a, max_units, workspace, st)                                       \
    : mt == 1 ? launch_ap<DH, KIND, 1>(maps, a, max_units, workspace, st)                                       \
-   : mt == 2 ? launch_ap<DH, KIND, 2>(maps, a, max_units, workspace, st)                                       \
-             : launch_ap<DH, KIND, 4>(maps, a, max_units, workspace, st))
+             : launch_ap<DH, KIND, 2>(maps, a, max_units, workspace, st))
   if (c.head_dim == 128) return c.dtype == SL_BF16 ? SL_AP(128, SL_BF16) : c.dtype == SL_E4M3 ? SL_AP(128, SL_E4M3) : SL_AP(128, SL_INT8);
   return c.dtype == SL_BF16 ? SL_AP(64, SL_BF16) : c.dtype == SL_E4M3 ? SL_AP(64, SL_E4M3) : SL_AP(64, SL_INT8);
 #undef SL_AP
