@@ -236,6 +236,61 @@ def test_codes_next_to_borders(kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", KINDS[1:])
+def test_every_quotient_of_two_bf16_significands(kind):
+    """bf16 rows: every significand of the largest magnitude times every significand of an element, 12 binades down."""
+    dh = 128
+    m = torch.arange(128, 256, dtype=torch.float64)
+    rows = []
+    for e, top in ((0, m), (120, m[::9]), (-71, m[::9]), (-76, m[::9])):      # the last two on both sides of 2^-64
+        for amax in top:
+            x = (m[None] * 2.0 ** -torch.arange(13.0, dtype=torch.float64)[:, None]).reshape(-1)
+            x = x[x <= amax]
+            x = torch.cat([x, torch.zeros(-len(x) % (dh - 1), dtype=torch.float64)]).reshape(-1, dh - 1)
+            x *= 1 - 2 * (torch.arange(dh - 1) % 2)
+            rows.append(torch.cat([torch.full((len(x), 1), float(amax), dtype=torch.float64), x], 1) * 2.0 ** e)
+    x = torch.cat(rows)[:, None].to(torch.bfloat16)
+    n = len(x)
+    pool = Pool(kind, 1, n, 1, dh, 256)
+    SL.surelock_kv_scatter_paged(pool.cache, x.to(DEV), x.flip(0).to(DEV), torch.arange(n, dtype=torch.int32, device=DEV), _i32([n]), n)
+    for t, p, s in ((x, pool.k, pool.ks), (x.flip(0), pool.v, pool.vs)):
+        code, scale = quantise(t.double().numpy(), kind)
+        assert np.array_equal(pool.rows(s, 0, n).astype(np.float32), scale)
+        assert np.array_equal(pool.rows(p, 0, n), code)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dh,Hkv,M,dtype", [(128, 5, 3001, torch.bfloat16), (64, 7, 4201, torch.float32), (128, 33, 701, torch.float32)])
+def test_many_rows_of_odd_heads(kind, dh, Hkv, M, dtype):
+    """More (row, head) pairs than the SMs hold at once, heads that do not divide evenly, a count below the capacity."""
+    n = M - 1
+    g = torch.Generator().manual_seed(M)
+    k, v = (torch.randn(M, Hkv, dh, generator=g).to(dtype) for _ in range(2))
+    idx = torch.randperm(M + 40, generator=g)[:M].to(torch.int32)
+    pool = Pool(kind, 1, M + 40, Hkv, dh, 64)
+    SL.surelock_kv_scatter_paged(pool.cache, k.to(DEV), v.to(DEV), idx.to(DEV), _i32([n]), M + 40)
+    out = [torch.full((M, Hkv, dh), 7.0, device=DEV) for _ in range(2)]
+    SL.surelock_kv_gather_paged(pool.cache, idx.to(DEV), _i32([n]), M + 40, out[0], out[1])
+    at = idx[:n].long().numpy()
+    for t, which, p, s, o in ((k, "k", pool.k, pool.ks, out[0]), (v, "v", pool.v, pool.vs, out[1])):
+        got = pool.rows(p, 0, M + 40)
+        if kind == torch.bfloat16:
+            assert np.array_equal(got[at], t[:n].to(torch.bfloat16).double().numpy())
+        else:
+            code, scale = quantise(t[:n].double().numpy(), kind)
+            assert np.array_equal(got[at], code)
+            assert np.array_equal(pool.rows(s, 0, M + 40)[at].astype(np.float32), scale)
+        want = torch.from_numpy(pool.values(which, 0, M + 40)[at]).float()
+        assert torch.equal(o[:n].cpu(), want) and torch.all(o[n:] == 7.0)
+        untouched = np.setdiff1d(np.arange(M + 40), at)
+        if kind != torch.int8:
+            assert np.all(np.isnan(got[untouched]))
+        else:
+            assert np.all(got[untouched] == -128)
+
+
+@gpu
 def test_rows_of_a_wider_buffer_and_small_counts():
     """k and v as parts of packed [q | k | v] rows; no row, one row, fewer rows than the capacity."""
     Hkv, dh, M = 4, 64, 9
