@@ -224,7 +224,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
 
   float acc[NT][4];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+  for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 
   if (warp == GQ_WARPS) {
     if (lane == 0) {
@@ -267,24 +267,24 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     const int mat = DUAL ? warp / (GQ_WARPS / 2) : 0;
     const uint32_t row0 = (uint32_t)(warp * 16 + rev) * 128;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int f = (DUAL ? warp % (GQ_WARPS / 2) : warp) * 16 + h * 8 + rev;
-        const long long at = (long long)min(n0 + f, a.n_out - 1) * a.ng;   // features behind the last one: any scales, codes are 0
-        rd[h].s = (const uint8_t*)a.scales[mat] + at * (FP32 ? 4 : 2);
-        rd[h].z = a.zeros[mat] ? a.zeros[mat] + at : nullptr;
-      }
+    for (int h = 0; h < 2; ++h) {
+      const int f = (DUAL ? warp % (GQ_WARPS / 2) : warp) * 16 + h * 8 + rev;
+      const long long at = (long long)min(n0 + f, a.n_out - 1) * a.ng;   // features behind the last one: any scales, codes are 0
+      rd[h].s = (const uint8_t*)a.scales[mat] + at * (FP32 ? 4 : 2);
+      rd[h].z = a.zeros[mat] ? a.zeros[mat] + at : nullptr;
+    }
     constexpr int CH = GroupReader<FP32>::CHUNK;
     int grp = b0 * P::GPT;
     auto fetch = [&](int g0) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) rd[h].fetch(g0, t, a.ng, a.pairs != 0);
+      for (int h = 0; h < 2; ++h) rd[h].fetch(g0, t, a.ng, a.pairs != 0);
     };
     auto turn = [&](int g0) {                                 // the chunk that was requested becomes the present one
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          rd[h].c = rd[h].n;
-          rd[h].cz = rd[h].nz;
-        }
+      for (int h = 0; h < 2; ++h) {
+        rd[h].c = rd[h].n;
+        rd[h].cz = rd[h].nz;
+      }
       fetch(g0 + CH);
     };
     if (n > 0) fetch(grp & ~(CH - 1));
@@ -298,40 +298,40 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       for (int hf = 0; hf < 2; ++hf) {
         uint32_t cw[2][4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t* c = cw[h];
-            const uint32_t at = base + row0 + h * 8 * 128;
-            if (G == 128) {
-              const uint4 x = gq_lds128(at + (((hf * 4 + t) << 4) ^ sw));
-              c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
-            } else if (G == 64) {
+        for (int h = 0; h < 2; ++h) {
+          uint32_t* c = cw[h];
+          const uint32_t at = base + row0 + h * 8 * 128;
+          if (G == 128) {
+            const uint4 x = gq_lds128(at + (((hf * 4 + t) << 4) ^ sw));
+            c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
+          } else if (G == 64) {
 #pragma unroll
-              for (int q = 0; q < 2; ++q)
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[2 * q]), "=r"(c[2 * q + 1])
-                             : "r"(at + (((hf * 4 + 2 * q + (t >> 1)) << 4) ^ sw) + (t & 1) * 8) : "memory");
-            } else {
+            for (int q = 0; q < 2; ++q)
+              asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[2 * q]), "=r"(c[2 * q + 1])
+                           : "r"(at + (((hf * 4 + 2 * q + (t >> 1)) << 4) ^ sw) + (t & 1) * 8) : "memory");
+          } else {
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(c[q]) : "r"(at + (((hf * 4 + q) << 4) ^ sw) + t * 4) : "memory");
-            }
+            for (int q = 0; q < 4; ++q)
+              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(c[q]) : "r"(at + (((hf * 4 + q) << 4) ^ sw) + t * 4) : "memory");
           }
+        }
         float ga[NT][4];
         constexpr int WPG = G / 32;                           // words per group
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           if (w % WPG == 0) {
 #pragma unroll
-              for (int j = 0; j < NT; ++j) ga[j][0] = ga[j][1] = ga[j][2] = ga[j][3] = 0.f;
+            for (int j = 0; j < NT; ++j) ga[j][0] = ga[j][1] = ga[j][2] = ga[j][3] = 0.f;
           }
-          uint32_t x[2][4];                              // codes 0 4 1 5 | 2 6 3 7
+          uint32_t x[2][4];                                   // codes 0 4 1 5 | 2 6 3 7
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t lo = cw[h][w], hi = lo >> 8;
-              x[0][h] = lo & 0x000f000fu;
-              x[0][2 + h] = lo & 0x00f000f0u;
-              x[1][h] = hi & 0x000f000fu;
-              x[1][2 + h] = hi & 0x00f000f0u;
-            }
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t lo = cw[h][w], hi = lo >> 8;
+            x[0][h] = lo & 0x000f000fu;
+            x[0][2 + h] = lo & 0x00f000f0u;
+            x[1][h] = hi & 0x000f000fu;
+            x[1][2 + h] = hi & 0x00f000f0u;
+          }
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             const uint4 b = gq_lds128(tb + j * P::CHUNK + (hf * 4 + w) * 512);
@@ -344,10 +344,10 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             if (((grp & (CH - 1)) == 0) || (i == 0 && gi == 0)) turn(grp & ~(CH - 1));
             float sc[2], mz[2];
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                if (gi & 1) rd[h].template get<1>(grp, lane, sc[h], mz[h]);
-                else rd[h].template get<0>(grp, lane, sc[h], mz[h]);
-              }
+            for (int h = 0; h < 2; ++h) {
+              if (gi & 1) rd[h].template get<1>(grp, lane, sc[h], mz[h]);
+              else rd[h].template get<0>(grp, lane, sc[h], mz[h]);
+            }
             ++grp;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -355,8 +355,8 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
               asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(q[0]), "=f"(q[1])
                            : "r"(base + GQ_CODES + j * P::CHUNK + GQ_ROWS + gi * 32 + t * 8) : "memory");
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  acc[j][e] = fmaf(sc[e >> 1], fmaf(mz[e >> 1], q[e & 1], ga[j][e]), acc[j][e]);
+              for (int e = 0; e < 4; ++e)
+                acc[j][e] = fmaf(sc[e >> 1], fmaf(mz[e >> 1], q[e & 1], ga[j][e]), acc[j][e]);
             }
           }
         }
@@ -373,10 +373,10 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   if (warp < GQ_WARPS) {
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + warp * 16 + (e >> 1) * 8 + rev] = acc[j][e];
+      for (int e = 0; e < 4; ++e)
+        sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + warp * 16 + (e >> 1) * 8 + rev] = acc[j][e];
   }
   if (S > 1) cluster_sync_all(); else __syncthreads();
   if (M > 0 && good) {
