@@ -109,13 +109,13 @@ template <int G, int NT> struct GqPlan {
 // One CTA per row, 8 k per thread at a time.  A row with an infinity or a NaN is NaN throughout.  Out: per (256 k, 8 rows) one
 // chunk of GqPlan::CHUNK bytes, [word of a code fragment][lane] of 16 bytes: a' of the 8 k whose codes that word holds, in the
 // order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16), zeros behind K; then q of the groups, [group][row].  Or, not in FRAGMENTS, the
-// same 16 bytes row by row, and q apart, [group][ld].  And e + 24 per row.
+// same 16 bytes row by row, without q.  And e + 24 per row.
 constexpr int GS_THREADS = 512;
 
 template <int G, bool FRAGMENTS>
 __global__ void __launch_bounds__(GS_THREADS)
 gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n_active, int max_rows, int K, uint8_t* __restrict__ rows,
-                       float* __restrict__ sums, int ld, int32_t* __restrict__ row_exp) {
+                       int32_t* __restrict__ row_exp) {
   __shared__ uint32_t sTop[GS_THREADS / 32];
   griddep_wait();
   griddep_launch();
@@ -164,22 +164,22 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
       sum += (back.x + back.y) * (j & 1 ? 16.f : 1.f);
       out[j] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
     }
-    if (bad) sum = __uint_as_float(0x7fffffffu);
+    if (FRAGMENTS) {
+      if (bad) sum = __uint_as_float(0x7fffffffu);
 #pragma unroll
-    for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
     const int block = i / 32, k8 = i % 32, in = k8 % 16;
     if (block < blocks) {
       const uint4 y = make_uint4(out[0], out[1], out[2], out[3]);
-      const float q = sum * 5.9604644775390625e-8f;
       if (FRAGMENTS) {
         const int word = G == 128 ? in % 4 : G == 64 ? 2 * (in / 8) + in % 2 : in / 4;
         const int t = G == 128 ? in / 4 : G == 64 ? in % 8 / 2 : in % 4;
         uint8_t* chunk = rows + ((long long)block * ((max_rows + 7) / 8) + r / 8) * GqPlan<G, 1>::CHUNK;
         *reinterpret_cast<uint4*>(chunk + (((k8 / 16 * 4 + word) * 32 + (r % 8) * 4 + t) << 4)) = y;
-        if (k8 % (G / 8) == 0) *reinterpret_cast<float*>(chunk + GQ_ROWS + k8 / (G / 8) * 32 + (r % 8) * 4) = q;
+        if (k8 % (G / 8) == 0) *reinterpret_cast<float*>(chunk + GQ_ROWS + k8 / (G / 8) * 32 + (r % 8) * 4) = sum * 5.9604644775390625e-8f;
       } else {
         *reinterpret_cast<uint4*>(rows + ((long long)r * blocks * 32 + i) * 16) = y;
-        if (i % (G / 8) == 0) sums[(long long)(i / (G / 8)) * ld + r] = q;
       }
     }
   }
@@ -419,11 +419,11 @@ template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const G
   if (a.max_rows <= 24) return launch_gq<G, 3, DUAL, FP32>(w, a, epilogue, st);
   return launch_gq<G, 4, DUAL, FP32>(w, a, epilogue, st);
 }
-template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, float* q, int ld, int epilogue, bool fp32, cudaStream_t st) {
+template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
   const bool few = a.max_rows <= GQ_FEW;
   SL_CUDA_TRY(launch_pdl(few ? gq_rewrite_rows_kernel<G, true> : gq_rewrite_rows_kernel<G, false>, dim3(a.max_rows), dim3(GS_THREADS), 0, st,
-                         (const bf16*)A, a.n_active, a.max_rows, a.K, (uint8_t*)a.rows, q, ld, (int32_t*)a.row_exp));
-  if (!few) return launch_gemm_quantized_tc(w, a, q, ld, G, fp32, epilogue, st);
+                         (const bf16*)A, a.n_active, a.max_rows, a.K, (uint8_t*)a.rows, (int32_t*)a.row_exp));
+  if (!few) return launch_gemm_quantized_tc(w, a, G, fp32, epilogue, st);
   if (epilogue == EPI_SWIGLU) return fp32 ? by_rows<G, true, true>(w, a, epilogue, st) : by_rows<G, true, false>(w, a, epilogue, st);
   return fp32 ? by_rows<G, false, true>(w, a, epilogue, st) : by_rows<G, false, false>(w, a, epilogue, st);
 }
@@ -436,8 +436,7 @@ int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, 
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * elem};
   const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
   const CUresult r = fn(out, type, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        type == CU_TENSOR_MAP_DATA_TYPE_FLOAT32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SL_OK : SL_ECUDA;
 }
 
@@ -445,7 +444,7 @@ int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, 
 static size_t gq_rows_bytes(int max_rows, int K) {
   const size_t blocks = (K + GQ_BK - 1) / GQ_BK;
   if (max_rows <= GQ_FEW) return blocks * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
-  return blocks * GQ_BK * 2 * max_rows + blocks * (GQ_BK / 32) * ((max_rows + 3) / 4 * 4) * 4;
+  return blocks * GQ_BK * 2 * max_rows;
 }
 size_t gemm_quantized_workspace_bytes(int max_rows, int K) { return gq_rows_bytes(max_rows, K) + (size_t)max_rows * sizeof(int32_t); }
 
@@ -473,12 +472,10 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   a.n_out = n_out;
   a.K = K;
   a.status = status;
-  const int ld = (max_rows + 3) / 4 * 4;             // rows of 16 bytes
-  float* q = reinterpret_cast<float*>((uint8_t*)workspace + (size_t)((K + GQ_BK - 1) / GQ_BK) * GQ_BK * 2 * max_rows);   // of the row-by-row layout
   switch (W->group) {
-    case 32: return by_kind<32>(maps, A, a, q, ld, epilogue, fp32, st);
-    case 64: return by_kind<64>(maps, A, a, q, ld, epilogue, fp32, st);
-    default: return by_kind<128>(maps, A, a, q, ld, epilogue, fp32, st);
+    case 32: return by_kind<32>(maps, A, a, epilogue, fp32, st);
+    case 64: return by_kind<64>(maps, A, a, epilogue, fp32, st);
+    default: return by_kind<128>(maps, A, a, epilogue, fp32, st);
   }
 }
 

@@ -78,7 +78,7 @@ template <bool DUAL> __device__ __forceinline__ void gq_store(const GqArgs& a, i
   }
 }
 
-// 2-D row-major tensor map, zeros out of bounds; operands (not fp32) in boxes of 128-byte rows under the 128-byte swizzle
+// 2-D row-major tensor map, zeros out of bounds, in boxes of 128-byte rows under the 128-byte swizzle
 int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, long long rows, long long cols, int box_rows, int box_cols);
 // launch with a cluster of S CTAs along x and programmatic dependent launch
 template <typename... KArgs, typename... Args>
@@ -99,7 +99,7 @@ inline cudaError_t gq_launch(void (*kernel)(KArgs...), dim3 grid, int threads, s
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// the product for more rows (gemm_quantized_tc.cu); rows rewritten as [max_rows][K up to GQ_BK] fp16, q as [K / group][ld]
-int launch_gemm_quantized_tc(const CUtensorMap* w, const GqArgs& a, const float* q, int ld, int group, bool fp32, int epilogue, cudaStream_t st);
+// the product for more rows (gemm_quantized_tc.cu); rows rewritten as [max_rows][K up to GQ_BK] fp16
+int launch_gemm_quantized_tc(const CUtensorMap* w, const GqArgs& a, int group, bool fp32, int epilogue, cudaStream_t st);
 
 }  // namespace sl
