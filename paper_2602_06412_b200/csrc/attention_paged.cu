@@ -1166,11 +1166,12 @@ int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long 
   a.status = status;
   // Rows of a tile: what a sequence has on average, padded as little as possible, up to 32.  Tiles of 64 share the conversions
   // of the codes among more rows, but leave fewer CTAs per SM: 4 x 8192 tokens, 64 rows each: 198 against 178 us; 1536 tokens,
-  // 128 rows: 37 against 31 us; tiles of 16 there: 222 and 33 us.
-  const long long rows = ((long long)max_rows * a.G + B - 1) / B;
-  const int mt = rows <= 8 ? 0 : rows <= 16 ? 1 : 2, tile_rows = mt ? 16 * mt : 8;
-  const long long tiles = ((long long)max_rows * a.G + tile_rows - 1) / tile_rows + B;
-  const long long max_units = tiles * a.Hkv * ((a.max_tokens + AP_KEYS - 1) / AP_KEYS);
+  // 128 rows: 37 against 31 us; tiles of 16 there: 222 and 33 us.  But where tiles of 32 leave SMs without work, tiles of 16 give
+  // more of it a start at once (512 tokens, 23 rows, 32 heads: 11.7 against 10.4 us).
+  const long long rows = ((long long)max_rows * a.G + B - 1) / B, per_tile = (long long)a.Hkv * ((a.max_tokens + AP_KEYS - 1) / AP_KEYS);
+  const bool little = B * ((rows + 31) / 32) * per_tile < (long long)sm_count() * ap_occupancy<2>();
+  const int mt = rows <= 8 ? 0 : rows <= 16 || little ? 1 : 2, tile_rows = mt ? 16 * mt : 8;
+  const long long max_units = (((long long)max_rows * a.G + tile_rows - 1) / tile_rows + B) * per_tile;
 #define SL_AP(DH, KIND)                                                                                        \
   (mt == 0   ? launch_ap<DH, KIND, 0>(maps, a, max_units, workspace, st)                                       \
    : mt == 1 ? launch_ap<DH, KIND, 1>(maps, a, max_units, workspace, st)                                       \
