@@ -1,0 +1,145 @@
+"""The quantised operators together, as one attention block of a served model uses them: 4-bit products for q, k and v, the new
+rows written into a paged 8-bit cache, attention over it, and the 4-bit output product added to the residual stream; first a
+prompt, then single tokens, eagerly and as a replayed graph.  Every operator is checked in its own file; here each stage is
+held against a plain statement in 64 bits of what the stage before it left in memory, with the same bounds, so that a wrong
+hand-over (order, layout, count, stream) shows as more than a rounding."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_06412_b200 import binding as SL
+
+from .test_gemm_quantized import _tol, _weights
+from .test_paged_kv import DEV, Pool, _i32, _near, _want, quantise
+
+pytestmark = pytest.mark.gpu
+
+
+class Block:
+    """d_model 512, 4 query heads on 2 key heads of 128, three sequences on pages of 16."""
+    d, H, Hkv, dh, B, N, group = 512, 4, 2, 128, 3, 90, 64
+
+    def __init__(self, kind):
+        self.kind = kind
+        qkv = (self.H + 2 * self.Hkv) * self.dh
+        self.Wqkv, self.wqkv = _weights(qkv, self.d, self.group, True, torch.bfloat16, seed=1)
+        self.Wo, self.wo = _weights(self.d, self.H * self.dh, self.group, False, torch.float32, seed=2)
+        self.pool = Pool(kind, self.B, self.N, self.Hkv, self.dh, 16)
+        self.lens = [0] * self.B
+        self.status = _i32([0])
+
+    def buffers(self, M):
+        """Device buffers of a step with at most M rows."""
+        z = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t, device=DEV)
+        return dict(x=z(M, self.d), qkv=z(M, self.wqkv.shape[0]), o=z(M, self.H * self.dh), res=z(M, self.d, t=torch.float32),
+                    idx=_i32([0] * M), n=_i32([M]), offs=_i32([0] * (self.B + 1)), lens=_i32([0] * self.B),
+                    ws=z(SL.surelock_attention_paged_workspace_bytes(self.dh), t=torch.uint8))
+
+    def launch(self, t):
+        """The step's six calls on the current stream."""
+        SL.surelock_gemm_quantized(t["x"], self.Wqkv, t["qkv"], t["n"], dev_status=self.status)
+        heads = t["qkv"].view(-1, self.H + 2 * self.Hkv, self.dh)
+        k, v = heads[:, self.H:self.H + self.Hkv], heads[:, self.H + self.Hkv:]
+        SL.surelock_kv_scatter_paged(self.pool.cache, k, v, t["idx"], t["n"], self.N, self.status)
+        SL.surelock_attention_paged(self.pool.cache, heads[:, :self.H], t["offs"], t["lens"], t["o"].view(-1, self.H, self.dh), t["ws"], self.status)
+        SL.surelock_gemm_quantized(t["o"], self.Wo, t["res"], t["n"], epilogue=1, dev_status=self.status)
+
+    def fill(self, t, new, seed):
+        """`new` tokens more for every sequence: inputs and the step's indices; returns the row offsets."""
+        g = torch.Generator().manual_seed(seed)
+        M = sum(new)
+        t["x"][:M] = torch.randn(M, self.d, generator=g).to(torch.bfloat16).to(DEV)
+        t["res"].copy_(torch.randn(t["res"].shape, generator=g))
+        idx = [b * self.N + self.lens[b] + i for b in range(self.B) for i in range(new[b])]
+        self.lens = [have + m for have, m in zip(self.lens, new)]
+        offs = [0] + np.cumsum(new).tolist()
+        t["idx"][:M] = _i32(idx)
+        t["n"].fill_(M)
+        t["offs"].copy_(_i32(offs))
+        t["lens"].copy_(_i32(self.lens))
+        return idx, offs
+
+    def check(self, t, before, idx, offs):
+        """Every stage against what the one before it left."""
+        M = offs[-1]
+        np64 = lambda x: x.cpu().double().numpy()
+        x, qkv, o = np64(t["x"][:M]), np64(t["qkv"][:M]), np64(t["o"][:M])
+        tol = _tol(x, self.wqkv, self.d, self.group) + 2.0 ** -8 * np.abs(x @ self.wqkv.T)
+        assert np.all(np.abs(qkv - x @ self.wqkv.T) <= tol)
+        heads = qkv.reshape(M, self.H + 2 * self.Hkv, self.dh)
+        for part, p, s in ((heads[:, self.H:self.H + self.Hkv], self.pool.k, self.pool.ks), (heads[:, self.H + self.Hkv:], self.pool.v, self.pool.vs)):
+            for b in range(self.B):
+                rows = range(offs[b], offs[b + 1])
+                place = [idx[r] % self.N for r in rows]
+                got = self.pool.rows(p, b, self.N)[place]
+                if s is None:
+                    assert np.array_equal(got, part[rows])
+                else:
+                    code, scale = quantise(part[rows], self.kind)
+                    assert np.array_equal(got, code) and np.array_equal(self.pool.rows(s, b, self.N)[place].astype(np.float32), scale)
+        want, A = _want(self.pool, heads[:, :self.H], offs, self.lens, self.H // self.Hkv)
+        _near(t["o"][:M].view(M, self.H, self.dh), want, A, self.kind)
+        res = np64(before[:M]) + o @ self.wo.T
+        d = np.abs(np64(t["res"][:M]) - res)
+        assert np.all(d <= _tol(o, self.wo, self.H * self.dh, self.group) + 2.0 ** -24 * np.abs(res))
+        assert torch.equal(t["res"][M:], before[M:]) and self.status.item() == 0
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float8_e4m3fn, torch.int8])
+def test_prompt_and_single_tokens(kind):
+    block = Block(kind)
+    t = block.buffers(80)
+    for seed, new in enumerate([(41, 17, 5), (0, 20, 33)]):           # 63 rows, then a longer prompt for two of them
+        idx, offs = block.fill(t, new, seed)
+        before = t["res"].clone()
+        block.launch(t)
+        block.check(t, before, idx, offs)
+    # single tokens, captured once; a sequence that has ended contributes no row
+    t = block.buffers(block.B)
+    torch.cuda.synchronize()
+    keep = [block.pool.k.clone(), block.pool.v.clone()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        block.launch(t)
+    raw = lambda x: x.view(torch.uint8) if x.element_size() == 1 else x.view(torch.int16)
+    assert all(torch.equal(raw(a), raw(b)) for a, b in zip(keep, (block.pool.k, block.pool.v)))
+    for seed, new in enumerate([(1, 1, 1), (1, 0, 1), (1, 1, 1), (0, 0, 0), (0, 1, 1)]):
+        idx, offs = block.fill(t, new, 10 + seed)
+        before = t["res"].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        block.check(t, before, idx, offs)
+
+
+@pytest.mark.parametrize("kind", [torch.float8_e4m3fn, torch.int8])
+def test_read_back_into_a_contiguous_cache(kind):
+    """Pages read back into [B][N] rows serve the framework's own attention: the same answer from both, within the roundings of
+    K and V to bf16 (2^-8 of a score's sum |q||k| / sqrt(d), 2^-8 of the values) and of either result."""
+    B, N, H, dh, M = 2, 64, 2, 128, 6
+    pool = Pool(kind, B, N, H, dh, 32)
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(B * N, H, dh, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    every = torch.arange(B * N, dtype=torch.int32, device=DEV)
+    SL.surelock_kv_scatter_paged(pool.cache, k, v, every, _i32([B * N]), N)
+    kc, vc = (torch.zeros(B * N, H, dh, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    SL.surelock_kv_gather_paged(pool.cache, every, _i32([B * N]), N, kc, vc)
+    offs, idx = [0, 2, M], _i32([3, 9, N, N + 1, N + 20, N + 63])
+    q = torch.randn(M, H, dh, generator=g).to(torch.bfloat16).to(DEV)
+    contiguous, paged = torch.zeros_like(q), torch.zeros_like(q)
+    SL.surelock_attention(q, kc, vc, idx, _i32(offs), _i32([M]), B, N, contiguous)
+    ws = torch.empty(SL.surelock_attention_paged_workspace_bytes(dh), dtype=torch.uint8, device=DEV)
+    SL.surelock_attention_paged(pool.cache, q, _i32(offs), _i32([N, N]), paged, ws)
+    for b in range(B):
+        kb, vb = pool.values("k", b, N), pool.values("v", b, N)
+        for h in range(H):
+            rows = range(offs[b], offs[b + 1])
+            qh = q[rows, h].cpu().double().numpy()
+            s = qh @ kb[:, h].T / np.sqrt(dh)
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            o, spread = p @ vb[:, h], p @ np.abs(vb[:, h])
+            ds = 2.0 ** -8 * (np.abs(qh) @ np.abs(kb[:, h]).T / np.sqrt(dh)).max(1, keepdims=True)
+            # a score off by ds moves a weight by a factor exp(2 ds) at most; then the rounding of weights, values and result
+            tol = (np.exp(2 * ds) - 1 + 2 * 2.0 ** -8 + 2.0 ** -11) * spread + 2.0 ** -8 * np.abs(o)
+            for got in (contiguous, paged):
+                assert np.all(np.abs(got[rows, h].cpu().double().numpy() - o) <= tol)
