@@ -415,15 +415,17 @@ typedef struct {
 /* surelock_gemm_fused with 4-bit weights, for few rows: C[r][n] = sum_k A[r][k] W[n][k] for r < *n_active, A dev bf16 [M][K],
  * epilogue 0: C bf16 [M][n_out]; 1: C is the fp32 residual stream, C[r][n] += sum; 2: C bf16 = silu(A W^T) * (A W2^T), W2 of
  * the same group, scale type and kind of zero point as W (W2 is ignored otherwise).  The codes enter the products exactly,
- * the rows as fp16 numbers (exact down to 2^-25 of the row's largest magnitude, off by at most 2^-35 of it below); group sums are fp32 and are multiplied by their scale in fp32.  A row with an infinity or a NaN gives NaN,
- * and no other row is
- * affected.  Any n_out; K a multiple of the group.  A pass over the weights serves up to 64 rows; more take further passes,
- * at most 65535 rows in all.  Rows >= *n_active of C are not touched.
- * Deterministic.  workspace: dev, surelock_gemm_quantized_workspace_bytes(max_rows, K) bytes, any contents, 256-byte
- * aligned, used during the call only: calls (and captured graphs) that may run at the same time need one each.  SL_EINVAL on
- * NULL pointers, a group that does not divide K, an unknown epilogue, a missing or different W2; SL_EUNSUPPORTED for another
- * group, more rows, or codes or A that are not 16-byte aligned.  dev_status may be NULL; 2 = a bounded wait ran out.
- * Asynchronous on `stream`. */
+ * the rows as fp16 numbers (exact down to 2^-25 of the row's largest magnitude, off by at most 2^-35 of it below); group sums
+ * are fp32 and are multiplied by their scale in fp32.  With up to 32 rows the zero point's share leaves a group's sum behind
+ * the product, so roundings are relative to sum |a| (code + zero) scale, and a group of codes at their zero point need not
+ * give an exact 0.  A row with an infinity or a NaN gives NaN, and no other row is affected.
+ * Any n_out; K a multiple of the group.  Up to 32 rows take one pass over the weights; more take one per 128 rows (per 64 up
+ * to 64 rows, or with groups of 32), at most 65535 rows in all.  Rows >= *n_active of C are not touched.  Deterministic.
+ * workspace: dev, surelock_gemm_quantized_workspace_bytes(max_rows, K) bytes, any contents, 256-byte aligned, used during the
+ * call only: calls (and captured graphs) that may run at the same time need one each.  SL_EINVAL on NULL pointers, a group
+ * that does not divide K, an unknown epilogue, a missing or different W2; SL_EUNSUPPORTED for another group, more rows, codes
+ * or A that are not 16-byte aligned, or a bf16 C that is not 8-byte aligned.  dev_status may be NULL; 2 = a bounded wait ran
+ * out.  Asynchronous on `stream`. */
 int surelock_gemm_quantized(const void *A, const surelock_w4 *W, const surelock_w4 *W2, void *C, const int32_t *n_active,
                             int max_rows, int n_out, int K, int epilogue, void *workspace, int32_t *dev_status, void *stream);
 size_t surelock_gemm_quantized_workspace_bytes(int max_rows, int K);
@@ -477,7 +479,8 @@ typedef struct {
  * infinity or NaN gets scale NaN.  k, v: dev, row r at r * row_stride elements, heads packed [n_kv_heads][head_dim], of
  * `dtype` SL_BF16 or SL_FP32; row_stride * sizeof(elem) a multiple of 16, so they may be parts of wider rows.  The positions
  * are distinct, and two of them do not share a page place through equal table entries (the values left there would be a
- * mixture).  max_rows * n_kv_heads < 2^31.  A position outside the tables, or on a bad page, is skipped (device status 4).  Nothing else is touched.
+ * mixture).  max_rows * n_kv_heads < 2^31.  A position outside the tables, or on a bad page, is skipped (device status 4).
+ * Nothing else is touched.
  * dev_status may be NULL.  Asynchronous on `stream`; may be captured into a graph. */
 int surelock_kv_scatter_paged(const surelock_paged_kv *cache, const void *k, const void *v, int64_t row_stride,
                               const int32_t *active_idx, const int32_t *n_active, int max_rows, int B, int N, int dtype,

@@ -457,6 +457,17 @@ def _w4(W, K: int):
     return _W4(_p(codes), _p(scales), _p(zeros), K // ng, _dt(scales)), n
 
 
+def _here(first, *others) -> int:
+    """The current stream of the device that all the tensors (or None) are on, which has to be the current one."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise SurelockError(f"all tensors on one CUDA device are wanted, got some on {first.device} and {t.device}")
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise SurelockError(f"tensors on the current CUDA device are wanted, got them on {first.device}")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
 def surelock_gemm_quantized_workspace_bytes(max_rows: int, K: int) -> int:
     return lib().surelock_gemm_quantized_workspace_bytes(max_rows, K)
 
@@ -474,13 +485,16 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
             raise SurelockError("surelock_gemm_quantized: W and W2 must have the same features")
     if A.dtype != torch.bfloat16 or Cout.dtype != (torch.float32 if epilogue == 1 else torch.bfloat16) or Cout.shape != (M, n):
         raise SurelockError("surelock_gemm_quantized: A bf16 [M][K], Cout [M][n_out] (fp32 with epilogue 1, else bf16)")
+    stream = _here(A, Cout, n_active, *W, *(W2 or ()), workspace, dev_status)
+    if not M:
+        return
     need = surelock_gemm_quantized_workspace_bytes(M, K)
     if workspace is None:
         workspace = torch.empty(need or 1, dtype=torch.uint8, device=A.device)
     elif workspace.nbytes < need:
         raise SurelockError("surelock_gemm_quantized: workspace too small")
-    _check(lib().surelock_gemm_quantized(_p(A), C.byref(w), C.byref(w2) if w2 is not None else None, _p(Cout), _p(n_active), M, n, K,
-                                         epilogue, _p(workspace), _p(dev_status), _stream()), "surelock_gemm_quantized")
+    _check(lib().surelock_gemm_quantized(_p(A), C.byref(w), C.byref(w2) if w2 is not None else None, _p(Cout), _ints(n_active, 1), M, n, K,
+                                         epilogue, _p(workspace), _p(dev_status), stream), "surelock_gemm_quantized")
 
 
 # ---- paged K/V cache ---------------------------------------------------------------------------------------
@@ -520,7 +534,7 @@ class PagedKV:
             _want(s is None or (s.dtype == torch.float32 and s.shape == k.shape[:3]), "scales: fp32 [n_pages][n_kv_heads][page_size]")
         tensors = [t for t in (k, v, page_table, k_scale, v_scale) if t is not None]
         _want(all(t.is_cuda and t.device == k.device and t.is_contiguous() for t in tensors), "pools, scales and table: contiguous, on one CUDA device")
-        self._keep = tensors
+        self._keep, self.k = tensors, k
         self.n_seq, self.n_kv_heads, self.head_dim = page_table.shape[0], k.shape[1], k.shape[3]
         self.raw = _PagedKV(k.data_ptr(), v.data_ptr(), _p(k_scale), _p(v_scale), page_table.data_ptr(), k.shape[0], k.shape[2],
                             page_table.shape[1], k.shape[1], k.shape[3], _PAGED_DT[k.dtype])
@@ -530,19 +544,25 @@ class PagedKV:
 
 def surelock_kv_scatter_paged(cache: PagedKV, k, v, active_idx, n_active, N: int, dev_status=None):
     """Rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32; rows may lie apart) into the pages, quantised on the way."""
-    stride = _rows(k, cache.n_kv_heads, cache.head_dim)
-    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == stride, "k and v must be laid out alike")
-    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), stride, _ints(active_idx, k.shape[0]),
-                                           _p(n_active), k.shape[0], cache.n_seq, N, _dt(k), _p(dev_status), _stream()),
+    pitch = _rows(k, cache.n_kv_heads, cache.head_dim)
+    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == pitch, "k and v must be laid out alike")
+    stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
+    if not k.shape[0]:
+        return
+    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), pitch, _ints(active_idx, k.shape[0]),
+                                           _ints(n_active, 1), k.shape[0], cache.n_seq, N, _dt(k), _p(dev_status), stream),
            "surelock_kv_scatter_paged")
 
 
 def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v, dev_status=None):
     """Positions active_idx back into the rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32)."""
-    stride = _rows(k, cache.n_kv_heads, cache.head_dim)
-    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == stride, "k and v must be laid out alike")
-    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0]), _p(n_active), k.shape[0], cache.n_seq,
-                                          N, k.data_ptr(), v.data_ptr(), stride, _dt(k), _p(dev_status), _stream()),
+    pitch = _rows(k, cache.n_kv_heads, cache.head_dim)
+    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == pitch, "k and v must be laid out alike")
+    stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
+    if not k.shape[0]:
+        return
+    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0]), _ints(n_active, 1), k.shape[0], cache.n_seq,
+                                          N, k.data_ptr(), v.data_ptr(), pitch, _dt(k), _p(dev_status), stream),
            "surelock_kv_gather_paged")
 
 
@@ -559,6 +579,9 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
     if not cache._ws_bytes:
         cache._ws_bytes = surelock_attention_paged_workspace_bytes(dh)
     _want(workspace.is_cuda and workspace.is_contiguous() and workspace.nbytes >= cache._ws_bytes, "workspace too small, or not on the GPU")
+    stream = _here(cache.k, q, row_offsets, seq_lens, o, workspace, dev_status)
+    if not q.shape[0]:
+        return
     _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh), _ints(row_offsets, B + 1), _ints(seq_lens, B), q.shape[0],
-                                          B, H, o.data_ptr(), _rows(o, H, dh), workspace.data_ptr(), _p(dev_status), _stream()),
+                                          B, H, o.data_ptr(), _rows(o, H, dh), workspace.data_ptr(), _p(dev_status), stream),
            "surelock_attention_paged")

@@ -1047,6 +1047,7 @@ int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_
   }
   if (rc != SL_OK) return rc;
   if ((reinterpret_cast<uintptr_t>(A) & 15) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return SL_EUNSUPPORTED;
+  if (epilogue != EPI_RESIDUAL && (reinterpret_cast<uintptr_t>(C) & 7)) return SL_EUNSUPPORTED;   // written four features at a time
   if (max_rows == 0) return SL_OK;
   return launch_gemm_quantized(A, W, epilogue == EPI_SWIGLU ? W2 : nullptr, C, n_active, max_rows, n_out, K, epilogue, workspace,
                                dev_status, (cudaStream_t)stream);

@@ -26,8 +26,6 @@
 // fp16 under a power of two per row that follows the row's largest weight so far; both keep 11 bits, and weights below
 // 2^-33 of the largest vanish.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
 // weight outgrows its power of two.  With a bf16 cache q and p are bf16.
-#include <mutex>
-
 #include "paged_kv.cuh"
 #include "tc_common.cuh"
 
@@ -1106,12 +1104,8 @@ template <int DH, int KIND, int MT>
 int launch_ap(const CUtensorMap* maps, PagedAttnArgs a, long long max_units, void* workspace, cudaStream_t st) {
   using PL = Plan<DH, KIND, MT>;
   const int smem = PL::SMEM + (a.B + 1) * 8;
-  static std::once_flag once;
-  static cudaError_t attr;
-  std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(attention_paged_kernel<DH, KIND, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM + (AP_MAX_B + 1) * 8);
-  });
-  SL_CUDA_TRY(attr);
+  static std::atomic<uint64_t> allowed{0};
+  SL_CUDA_TRY(allow_smem(attention_paged_kernel<DH, KIND, MT>, PL::SMEM + (AP_MAX_B + 1) * 8, allowed));
   const int fit = 228 * 1024 / (smem + 1024);   // all CTAs of the grid are resident at once, so equal runs end together
   const int occ = fit < ap_occupancy<MT>() ? fit : ap_occupancy<MT>();
   const int cap = sm_count() * occ, grid = (int)(max_units < cap ? max_units : cap);

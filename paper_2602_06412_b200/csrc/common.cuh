@@ -7,6 +7,9 @@
 #include <stdio.h>
 #include <stdlib.h>
 
+#include <atomic>
+
+
 #include "surelock.h"
 
 // Device status codes stored (first writer wins) in the ctx status word.
@@ -98,6 +101,16 @@ inline int sm_count() {
     if (n <= 0) n = 148;
   }
   return n;
+}
+
+// The limit of a kernel's dynamic shared memory belongs to a device: set on the first call there.  `done`: one bit per device.
+template <typename Kernel> inline cudaError_t allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  const cudaError_t rc = cudaGetDevice(&dev);
+  if (rc != cudaSuccess || (done.load(std::memory_order_acquire) >> (dev & 63) & 1)) return rc;
+  const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (set == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+  return set;
 }
 
 // ---- launchers (one per kernel family); all asynchronous on `st`, rows beyond *n_active are not touched ----

@@ -97,7 +97,7 @@ template <int G, int NT> struct GqPlan {
   static constexpr int GPT = GQ_BK / G;                       // groups per stage
   static constexpr int CHUNK = GQ_ROWS + GPT * 32;           // 8 rewritten rows, then their q: [group][row]
   static constexpr int STAGE = GQ_CODES + (NT * CHUNK + 1023) / 1024 * 1024;
-  static constexpr int OCC = NT <= 4 ? 3 : 2;
+  static constexpr int OCC = 3;
   static constexpr int ROOM = 228 * 1024 / OCC - 1024 - 1024 - 256;
   static constexpr int STAGES = ROOM / STAGE > 4 ? 4 : ROOM / STAGE;
   static constexpr int PITCH = 132;                           // floats per packed row of the partial sums
@@ -187,6 +187,7 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
 
 }  // namespace
 
+// NT = number of eights of rows, max_rows / 8 rounded up
 template <int G, int NT, bool DUAL, bool FP32>
 __global__ void __launch_bounds__(GQ_THREADS, GqPlan<G, NT>::OCC)
 gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2, const GqArgs a, const int epilogue) {
@@ -215,9 +216,9 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   uint32_t S, rank = 0;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(S));
   if (S > 1) rank = cluster_ctarank();
-  const int n0 = (int)(blockIdx.x / S) * TO, r0 = blockIdx.y * 8 * NT;
+  const int n0 = (int)(blockIdx.x / S) * TO;
   // *n_active, the weights and C were written before the rewriting kernel began; its rows come after griddep_wait()
-  const int M = min(*a.n_active, a.max_rows) - r0;            // rows of this tile; none: the whole cluster leaves
+  const int M = min(*a.n_active, a.max_rows);                 // none: the whole cluster leaves
   const int nblk = (a.K + GQ_BK - 1) / GQ_BK;
   const int b0 = (int)((long long)nblk * rank / S), b1 = (int)((long long)nblk * (rank + 1) / S);
   const int n = M > 0 ? b1 - b0 : 0;
@@ -228,12 +229,12 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
 
   if (warp == GQ_WARPS) {
     if (lane == 0) {
-      const uint64_t once = gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();   // a code is read once per row tile
-      const int row_tiles = (a.max_rows + 7) / 8, mine = min(NT, row_tiles - r0 / 8), ahead = min(n, P::STAGES);
+      const uint64_t once = l2_policy_evict_first();
+      const int ahead = min(n, P::STAGES);
       auto codes = [&](int i) {
         const int st = i % P::STAGES;
         const uint32_t at = smem_u32(smem + st * P::STAGE);
-        mbar_expect_tx(full(st), GQ_CODES + mine * P::CHUNK);
+        mbar_expect_tx(full(st), GQ_CODES + NT * P::CHUNK);
         tma_load_2d_hint(at, &tmW, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
         if (DUAL) tma_load_2d_hint(at + GQ_CODES / 2, &tmW2, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
       };
@@ -248,8 +249,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
           if (!(ok = mbar_wait(empty(st), ((i / P::STAGES) & 1) ^ 1, s_abort))) break;
           codes(i);
         }
-        bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.rows + ((long long)(b0 + i) * row_tiles + r0 / 8) * P::CHUNK,
-                  (uint32_t)(mine * P::CHUNK), full(st));
+        bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.rows + (long long)(b0 + i) * NT * P::CHUNK, NT * P::CHUNK, full(st));
       }
       if (!ok) {
         // gave up: wait (bounded) for the copies in flight, which write to this CTA's shared memory
@@ -385,7 +385,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       const int r = i / cols, col = 4 * (c0 + i % cols);
       if (n0 + col >= a.n_out) continue;
       const float4 y = gq_total(sRed, S, r * P::PITCH + col);
-      gq_store<DUAL>(a, epilogue, r0 + r, n0 + col, y, DUAL ? gq_total(sRed, S, r * P::PITCH + 64 + col) : y);
+      gq_store<DUAL>(a, epilogue, r, n0 + col, y, DUAL ? gq_total(sRed, S, r * P::PITCH + 64 + col) : y);
     }
   }
   if (S > 1) cluster_sync_all();                              // the others may still be reading this CTA's partial sums
@@ -397,17 +397,15 @@ template <int G, int NT, bool DUAL, bool FP32>
 int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
   using P = GqPlan<G, NT>;
   constexpr int TO = DUAL ? 64 : 128;
-  const int tiles = (a.n_out + TO - 1) / TO, nblk = (a.K + GQ_BK - 1) / GQ_BK, row_tiles = (a.max_rows + 8 * NT - 1) / (8 * NT);
+  const int tiles = (a.n_out + TO - 1) / TO, nblk = (a.K + GQ_BK - 1) / GQ_BK;
   // K is split over S CTAs of a cluster while the CTAs still fit the GPU at once
-  const long long slots = (long long)sm_count() * P::OCC, work = (long long)tiles * row_tiles;
+  const long long slots = (long long)sm_count() * P::OCC;
   int S = 1;
-  while (S < 8 && S < nblk && work * (S + 1) <= slots) ++S;
+  while (S < 8 && S < nblk && (long long)tiles * (S + 1) <= slots) ++S;
   auto kernel = gemm_quantized_kernel<G, NT, DUAL, FP32>;
-  static std::once_flag once;
-  static cudaError_t attr;
-  std::call_once(once, [&] { attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P::SMEM); });
-  SL_CUDA_TRY(attr);
-  SL_CUDA_TRY(gq_launch(kernel, dim3(tiles * S, row_tiles), GQ_THREADS, P::SMEM, S, st, w[0], w[1], a, epilogue));
+  static std::atomic<uint64_t> allowed{0};
+  SL_CUDA_TRY(allow_smem(kernel, P::SMEM, allowed));
+  SL_CUDA_TRY(gq_launch(kernel, dim3(tiles * S), GQ_THREADS, P::SMEM, S, st, w[0], w[1], a, epilogue));
   return SL_OK;
 }
 

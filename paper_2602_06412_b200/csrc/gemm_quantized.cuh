@@ -3,8 +3,6 @@
 #pragma once
 #include <cuda_fp16.h>
 
-#include <mutex>
-
 #include "tc_common.cuh"
 
 namespace sl {

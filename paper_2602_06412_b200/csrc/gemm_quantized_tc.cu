@@ -387,10 +387,8 @@ int launch_gt(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
     }
   }
   auto kernel = gemm_quantized_tc_kernel<G, NP, DUAL, FP32>;
-  static std::once_flag once;
-  static cudaError_t attr;
-  std::call_once(once, [&] { attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P::SMEM); });
-  SL_CUDA_TRY(attr);
+  static std::atomic<uint64_t> allowed{0};
+  SL_CUDA_TRY(allow_smem(kernel, P::SMEM, allowed));
   const dim3 grid((a.n_out + TO - 1) / TO * S, (a.max_rows + NP - 1) / NP);
   SL_CUDA_TRY(gq_launch(kernel, grid, GT_THREADS, P::SMEM, S, st, w[0], w[1], rows, a, epilogue));
   return SL_OK;

@@ -182,3 +182,101 @@ def test_graph_streams_and_changing_counts():
                 SL.surelock_gemm_quantized(A, W, o, count)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+# ---- what the shapes above leave out --------------------------------------------------------------------------------
+def test_outputs_that_cannot_be_written_in_fours_are_refused():
+    build_mod.build()
+    L = SL.lib()
+    w = ctypes.byref(SL._W4(codes=0x1000, scales=0x2000, zeros=None, group=64, scale_dtype=SL.SL_BF16))
+    for epilogue, c, rc in [(0, 0x204, -5), (0, 0x202, -5), (2, 0x204, -5), (0, 0x208, 0), (1, 0x204, 0)]:
+        assert L.surelock_gemm_quantized(0x100, w, w, c, 0x300, 0, 10, 128, epilogue, 0x1000, None, None) == rc
+
+
+@gpu
+@pytest.mark.parametrize("scale_t", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,n,K,group", [(2, 70, 1344, 64), (19, 130, 640, 128), (32, 64, 416, 32), (34, 200, 1056, 32), (50, 70, 1344, 64), (127, 257, 1280, 64),
+                                         (128, 131, 1152, 128), (129, 40, 160, 32)])
+def test_large_zero_points_are_exact(M, n, K, group, scale_t):
+    """Zero points over their whole range, 0 ... 127; |sum| <= 1344 x 4 x 127 x 4 < 2^24, so the whole numbers stay exact."""
+    (codes, scales, _), _ = _weights(n, K, group, False, scale_t, seed=M, exact=True)
+    g = torch.Generator().manual_seed(M)
+    z = torch.randint(0, 128, (n, K // group), generator=g, dtype=torch.uint8)
+    z[:, 0], z[0] = 127, 0
+    c = codes.cpu()
+    u = torch.stack([c & 15, c >> 4], 2).reshape(n, -1, group).double().numpy()
+    w = ((u - z.double().numpy()[..., None]) * scales.cpu().double().numpy()[..., None]).reshape(n, K)
+    a = torch.randint(-4, 5, (M, K), generator=g)
+    D = torch.zeros(M, n, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    SL.surelock_gemm_quantized(a.to(torch.bfloat16).to(DEV), (codes, scales, z.to(DEV)), D, torch.tensor([M], dtype=torch.int32, device=DEV),
+                               epilogue=1, dev_status=status)
+    assert np.array_equal(D.cpu().double().numpy(), a.double().numpy() @ w.T) and status.item() == 0
+
+
+@gpu
+@pytest.mark.parametrize("scale_t", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,n,K,group", [(4, 66, 256, 32), (16, 190, 640, 64), (30, 129, 1152, 128), (33, 66, 800, 32), (64, 190, 640, 64), (65, 129, 1152, 128),
+                                         (100, 65, 2112, 64), (128, 640, 512, 128), (131, 100, 96, 32)])
+def test_swiglu(M, n, K, group, scale_t):
+    W, w = _weights(n, K, group, True, scale_t, seed=M)
+    W2, w2 = _weights(n, K, group, True, scale_t, seed=M + 1)
+    A = torch.randn(M + 1, K, generator=torch.Generator().manual_seed(M)).to(torch.bfloat16)
+    a = A[:M].double().numpy()
+    x, tx, y, ty = a @ w.T, _tol(a, w, K, group), a @ w2.T, _tol(a, w2, K, group)
+    s = x / (1 + np.exp(-x))
+    want = s * y
+    tol = 1.1 * tx * (np.abs(y) + ty) + np.abs(s) * (ty + 2.0 ** -20 * np.abs(y)) + 2.0 ** -8 * np.abs(want)
+    D = torch.full((M + 1, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    _run(A.to(DEV), W, D, M, 2, W2)
+    d = np.abs(D[:M].cpu().double().numpy() - want)
+    assert np.all(d <= tol), float((d / tol).max())
+    assert torch.all(D[M:] == 7.0)
+
+
+@gpu
+@pytest.mark.parametrize("M,counts", [(70, (70, 0, 1, 33, 64, 65)), (200, (200, 128, 129, 7))])
+def test_many_rows_under_a_graph_with_changing_counts(M, counts):
+    """A workspace that holds NaN, counts below the capacity, and a replay beside calls on another stream."""
+    n, K = 200, 1056
+    W, w = _weights(n, K, 32, True, torch.bfloat16, seed=9)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(10)).to(torch.bfloat16).to(DEV)
+    want = torch.zeros(M, n, dtype=torch.bfloat16, device=DEV)
+    _run(A, W, want, M, 0)
+    count, full = (torch.tensor([M], dtype=torch.int32, device=DEV) for _ in range(2))
+    out, beside = torch.zeros_like(want), torch.zeros_like(want)
+    ws = torch.full((SL.surelock_gemm_quantized_workspace_bytes(M, K),), 255, dtype=torch.uint8, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        SL.surelock_gemm_quantized(A, W, out, count, workspace=ws, dev_status=status)
+    other = torch.cuda.Stream()
+    for m in counts:
+        out.zero_()
+        beside.zero_()
+        ws.fill_(255)
+        count.fill_(m)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            SL.surelock_gemm_quantized(A, W, beside, full, dev_status=status)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:m], want[:m]) and torch.all(out[m:] == 0) and torch.equal(beside, want)
+    assert status.item() == 0
+
+
+@gpu
+def test_refusals_with_tensors(monkeypatch):
+    W, _ = _weights(40, 128, 64, False, torch.bfloat16, seed=11)
+    A, C, one = torch.zeros(2, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 40, dtype=torch.bfloat16, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    SL.surelock_gemm_quantized(A[:0], W, C[:0], one)                  # no rows: nothing to do
+    wide = torch.zeros(81, dtype=torch.bfloat16, device=DEV)
+    for bad in [(A, W, C, one.cpu()), (A, W, C, one.long()), (A, (W[0].cpu(), *W[1:]), C, one), (A, W, wide[1:].reshape(2, 40), one), (A.cpu(), W, C, one)]:
+        with pytest.raises(SL.SurelockError):
+            SL.surelock_gemm_quantized(*bad)
+    with pytest.raises(SL.SurelockError):
+        SL.surelock_gemm_quantized(A, W, C, one, workspace=torch.zeros(8, dtype=torch.uint8, device=DEV))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)       # as if another device were the current one
+    with pytest.raises(SL.SurelockError):
+        SL.surelock_gemm_quantized(A, W, C, one)

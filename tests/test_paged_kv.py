@@ -561,3 +561,37 @@ def test_offsets_beyond_32_bits():
     got = _attend(pool, q, [0, 2], [400])
     o, A = _want(pool, q.cpu().double().numpy(), [0, 2], [400], 1)
     _near(got, o, A, pool.kind)
+
+
+@gpu
+def test_refusals_with_tensors(monkeypatch):
+    Hkv, dh, N = 2, 64, 48
+    pool = Pool(torch.int8, 1, N, Hkv, dh, 16)
+    k, v = (torch.randn(3, Hkv, dh, device=DEV) for _ in range(2))
+    idx, n = _i32([0, 1, 2]), _i32([3])
+    q = torch.randn(3, 4, dh, device=DEV).to(torch.bfloat16)
+    offs, lens, ws = _i32([0, 3]), _i32([3]), torch.empty(SL.surelock_attention_paged_workspace_bytes(dh), dtype=torch.uint8, device=DEV)
+    write = lambda *a: SL.surelock_kv_scatter_paged(pool.cache, *a)
+    read = lambda *a: SL.surelock_kv_gather_paged(pool.cache, *a)
+    attend = lambda *a: SL.surelock_attention_paged(pool.cache, *a)
+    write(k[:0], v[:0], idx, n, N)                                    # no rows: nothing to do
+    read(idx, n, N, k[:0], v[:0])
+    attend(q[:0], offs, lens, q[:0], ws)
+    good = [(write, (k, v, idx, n, N)), (read, (idx, n, N, k, v)), (attend, (q, offs, lens, q.clone(), ws))]
+    for f, a in good:
+        f(*a)
+        for i, t in enumerate(a):
+            if isinstance(t, torch.Tensor):                           # one on the CPU, or of another type
+                for bad in (t.cpu(), t.long()) if t.dtype == torch.int32 else (t.cpu(),):
+                    with pytest.raises(SL.SurelockError):
+                        f(*a[:i], bad, *a[i + 1:])
+    for f, a in [(write, (k[:, :1], v[:, :1], idx, n, N)), (write, (k, v[:2], idx, n, N)), (write, (k, v, idx[:2], n, N)), (write, (k, v, idx, n, 0)),
+                 (read, (idx, n, N, k.half(), v.half())), (read, (idx, n, N, k[:1].expand(3, Hkv, dh), v[:1].expand(3, Hkv, dh))),
+                 (attend, (q[:, :3], offs, lens, q[:, :3], ws)), (attend, (q, offs, lens, q, ws[:100])), (attend, (q, offs, _i32([1, 1]), q, ws)),
+                 (attend, (q.float(), offs, lens, q.float(), ws))]:
+        with pytest.raises(SL.SurelockError):
+            f(*a)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)       # as if another device were the current one
+    for f, a in good:
+        with pytest.raises(SL.SurelockError):
+            f(*a)
