@@ -30,6 +30,12 @@ __device__ __forceinline__ void gt_mma(uint32_t d_tmem, uint32_t a_tmem, uint64_
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum)
       : "memory");
 }
+// true in one lane of the (whole) warp
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -146,7 +152,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + P::BARS);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < P::CODES; ++i) {
       mbar_init(c_full(i), 1);
@@ -223,31 +229,35 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
       }
     }
   } else if (warp == GT_WORKERS + 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // fp16 x fp16 -> fp32, M = 128, N = NP
-      bool ok = true;
-      int g = 0;
-      for (int i = 0; i < steps && ok; ++i) {
-        ok = mbar_wait(r_full(i), (i / P::ROWS) & 1, s_abort) && mbar_wait(unpacked(i), (i >> 1) & 1, s_abort);
-        const uint32_t rows = rows0 + i % P::ROWS * 2 * P::SLAB, op = tmem + (i & 1) * P::A_COLS;
+    // The warp stays together and elects a lane per group: in a branch of one lane every operand of an MMA would first have to
+    // be moved to the uniform registers that it is issued from (170 clocks per MMA).
+    constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // fp16 x fp16 -> fp32, M = 128, N = NP
+    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0), ring = __shfl_sync(0xffffffffu, rows0, 0);
+    bool ok = true;
+    int g = 0;
+    for (int i = 0; i < steps && ok; ++i) {
+      ok = __all_sync(0xffffffffu, mbar_wait(r_full(i), (i / P::ROWS) & 1, s_abort) && mbar_wait(unpacked(i), (i >> 1) & 1, s_abort));
+      const uint32_t rows = ring + i % P::ROWS * 2 * P::SLAB, op = base + (i & 1) * P::A_COLS;
 #pragma unroll
-        for (int q = 0; q < GPS; ++q) {
-          if (!ok || !(ok = mbar_wait(added(g), ((g / P::SETS) & 1) ^ 1, s_abort))) break;
-          tc_fence_after();
-          const uint32_t d = tmem + P::D_COL + g % P::SETS * NP;
+      for (int q = 0; q < GPS; ++q) {
+        if (!ok || !(ok = __all_sync(0xffffffffu, mbar_wait(added(g), ((g / P::SETS) & 1) ^ 1, s_abort)))) break;
+        tc_fence_after();
+        const uint32_t d = base + P::D_COL + g % P::SETS * NP;
+        if (elect_one()) {
 #pragma unroll
           for (int k = q * (G / 16); k < (q + 1) * (G / 16); ++k)   // 16 k: 8 columns of the operand, 32 bytes of a slab's rows
             gt_mma(d, op + k * 8, smem_desc_k_sw128(rows + (k >> 2) * P::SLAB + (k & 3) * 32), idesc, k % (G / 16) != 0);
           tc_commit(done(g));
-          ++g;
+          if (q == GPS - 1) tc_commit(r_empty(i));
         }
-        if (ok) tc_commit(r_empty(i));
+        __syncwarp();
+        ++g;
       }
-      if (!ok) {
-        set_status(a.status, SL_DEV_GEMM_TIMEOUT);
-        const unsigned long long t0 = clock64();              // the last group issued still uses the tensor memory
-        while (g > 0 && !mbar_try(done(g - 1), ((g - 1) / P::SETS) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-      }
+    }
+    if (!ok && lane == 0) {
+      set_status(a.status, SL_DEV_GEMM_TIMEOUT);
+      const unsigned long long t0 = clock64();                // the last group issued still uses the tensor memory
+      while (g > 0 && !mbar_try(done(g - 1), ((g - 1) / P::SETS) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
   } else {
     const int feature = (warp & 3) * 32 + lane, quarter = warp >> 2;
