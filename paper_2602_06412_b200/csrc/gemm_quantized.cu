@@ -453,12 +453,12 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   CUtensorMap maps[2];
   a.ng = K / W->group;
   const bool fp32 = W->scale_dtype == SL_FP32, few = max_rows <= GQ_FEW;
-  a.pairs = a.ng % (few || fp32 ? 2 : 4) == 0;
+  a.pairs = a.ng % (few ? 2 : GQ_BK / W->group) == 0;
   for (int i = 0; i < 2; ++i) {
     const surelock_w4* w = i && W2 ? W2 : W;
     a.zeros[i] = (const uint8_t*)w->zeros;
     a.scales[i] = w->scales;
-    if ((reinterpret_cast<uintptr_t>(w->scales) & 7) || (reinterpret_cast<uintptr_t>(w->zeros) & 3)) a.pairs = 0;
+    if ((reinterpret_cast<uintptr_t>(w->scales) & 15) || (reinterpret_cast<uintptr_t>(w->zeros) & 1)) a.pairs = 0;
     const int rc = gq_map(&maps[i], w->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128, GQ_BK / 2);
     if (rc != SL_OK) return rc;
   }

@@ -60,57 +60,46 @@ __device__ __forceinline__ void fma2(float* acc, float s, const uint32_t* d) {
       : "+f"(acc[0]), "+f"(acc[1]) : "f"(__uint_as_float(d[0])), "f"(__uint_as_float(d[1])), "f"(s));
 }
 
-// Scales of one feature, group after group: 8 bytes (4 bf16 or 2 fp32) at a time, the next ones requested one such chunk ahead.
-template <bool FP32> struct FeatureScales {
-  static constexpr int CHUNK = FP32 ? 2 : 4;
+// Scales of one feature, a stage's groups at a time; the next stage's are requested when one begins.
+template <int G, bool FP32> struct FeatureScales {
+  static constexpr int GPT = GQ_BK / G, WORDS = GPT * (FP32 ? 4 : 2) / 4;
   const uint8_t* s;            // of the feature
-  uint32_t c0, c1, n0, n1;     // present and next chunk
-  int grp;
+  uint32_t c[WORDS], n[WORDS];
 
-  __device__ __forceinline__ void fetch(int g0, int ng, bool aligned) {
-    n0 = n1 = 0;
+  __device__ __forceinline__ void fetch(int g0, int ng, bool aligned) {   // groups from g0 on -> n
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) n[i] = 0;
     if (aligned) {
       if (g0 < ng) {
-        const uint2 x = __ldg(reinterpret_cast<const uint2*>(s + (size_t)g0 * (FP32 ? 4 : 2)));
-        n0 = x.x;
-        n1 = x.y;
+        const uint8_t* p = s + (size_t)g0 * (FP32 ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) {
+          if (WORDS == 1) {
+            n[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+          } else if (WORDS == 2) {
+            const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+            n[0] = x.x; n[1 % WORDS] = x.y;
+          } else {
+            const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i / 4);
+            n[i] = x.x; n[(i + 1) % WORDS] = x.y; n[(i + 2) % WORDS] = x.z; n[(i + 3) % WORDS] = x.w;
+          }
+        }
       }
       return;
     }
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i)
+    for (int i = 0; i < GPT; ++i)
       if (g0 + i < ng) {
-        const uint32_t x = FP32 ? __ldg(reinterpret_cast<const uint32_t*>(s) + g0 + i) : __ldg(reinterpret_cast<const uint16_t*>(s) + g0 + i);
-        if (FP32) (i ? n1 : n0) = x;
-        else (i < 2 ? n0 : n1) |= x << (16 * (i & 1));
+        if (FP32) n[i % WORDS] = __ldg(reinterpret_cast<const uint32_t*>(s) + g0 + i);
+        else n[i / 2 % WORDS] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(s) + g0 + i) << (16 * (i & 1));
       }
   }
-  __device__ __forceinline__ void rotate() {          // drop the first group of the chunk
-    if (FP32) {
-      c0 = c1;
-    } else {
-      c0 = __funnelshift_r(c0, c1, 16);
-      c1 >>= 16;
-    }
+  __device__ __forceinline__ void turn() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) c[i] = n[i];
   }
-  __device__ __forceinline__ void prime(int ng, bool aligned) {   // before the first next(): the first chunk was requested
-    const int at = grp & ~(CHUNK - 1);
-    c0 = n0;
-    c1 = n1;
-    fetch(at + CHUNK, ng, aligned);
-    for (int i = at; i < grp; ++i) rotate();
-  }
-  // scale of the next group; behind the feature's last one 0
-  __device__ __forceinline__ float next(int ng, bool aligned) {
-    const float scale = __uint_as_float(FP32 ? c0 : c0 << 16);
-    if ((++grp & (CHUNK - 1)) == 0) {
-      c0 = n0;
-      c1 = n1;
-      fetch(grp + CHUNK, ng, aligned);
-    } else {
-      rotate();
-    }
-    return scale;
+  __device__ __forceinline__ float get(int i) const {   // behind the feature's last group 0
+    return __uint_as_float(FP32 ? c[i % WORDS] : i & 1 ? c[i / 2 % WORDS] & 0xffff0000u : c[i / 2 % WORDS] << 16);
   }
 };
 
@@ -141,14 +130,14 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   float* sRed = reinterpret_cast<float*>(smem);               // [NP][PITCH] after the last step
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + P::BUFFERS);
   const uint32_t codes0 = smem_u32(smem), rows0 = codes0 + P::CODES * GQ_CODES, bar0 = smem_u32(bars);
-  // barriers and their phases: of stage s of codes, step i, group g
+  // barriers: of stage s of codes, step i, set of accumulators
   auto c_full = [&](int s) { return bar0 + 8u * (s % P::CODES); };
   auto c_empty = [&](int s) { return bar0 + 8u * (P::CODES + s % P::CODES); };
   auto r_full = [&](int i) { return bar0 + 8u * (2 * P::CODES + i % P::ROWS); };
   auto r_empty = [&](int i) { return bar0 + 8u * (2 * P::CODES + P::ROWS + i % P::ROWS); };
   auto unpacked = [&](int i) { return bar0 + 8u * (2 * P::CODES + 2 * P::ROWS + (i & 1)); };            // operand tile written
-  auto done = [&](int g) { return bar0 + 8u * (2 * P::CODES + 2 * P::ROWS + 2 + g % P::SETS); };        // MMAs finished
-  auto added = [&](int g) { return bar0 + 8u * (2 * P::CODES + 2 * P::ROWS + 2 + P::SETS + g % P::SETS); };
+  auto done = [&](int set) { return bar0 + 8u * (2 * P::CODES + 2 * P::ROWS + 2 + set); };              // MMAs finished
+  auto added = [&](int set) { return bar0 + 8u * (2 * P::CODES + 2 * P::ROWS + 2 + P::SETS + set); };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + P::BARS);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
@@ -234,64 +223,73 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
     constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // fp16 x fp16 -> fp32, M = 128, N = NP
     const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0), ring = __shfl_sync(0xffffffffu, rows0, 0);
     bool ok = true;
-    int g = 0;
+    int set = 0, last = -1;                                   // set of the group at hand, of the last one issued
+    uint32_t phase = 0;
     for (int i = 0; i < steps && ok; ++i) {
       ok = __all_sync(0xffffffffu, mbar_wait(r_full(i), (i / P::ROWS) & 1, s_abort) && mbar_wait(unpacked(i), (i >> 1) & 1, s_abort));
       const uint32_t rows = ring + i % P::ROWS * 2 * P::SLAB, op = base + (i & 1) * P::A_COLS;
 #pragma unroll
       for (int q = 0; q < GPS; ++q) {
-        if (!ok || !(ok = __all_sync(0xffffffffu, mbar_wait(added(g), ((g / P::SETS) & 1) ^ 1, s_abort)))) break;
+        if (!ok || !(ok = __all_sync(0xffffffffu, mbar_wait(added(set), phase ^ 1, s_abort)))) break;
         tc_fence_after();
-        const uint32_t d = base + P::D_COL + g % P::SETS * NP;
+        const uint32_t d = base + P::D_COL + set * NP;
         if (elect_one()) {
 #pragma unroll
           for (int k = q * (G / 16); k < (q + 1) * (G / 16); ++k)   // 16 k: 8 columns of the operand, 32 bytes of a slab's rows
             gt_mma(d, op + k * 8, smem_desc_k_sw128(rows + (k >> 2) * P::SLAB + (k & 3) * 32), idesc, k % (G / 16) != 0);
-          tc_commit(done(g));
+          tc_commit(done(set));
           if (q == GPS - 1) tc_commit(r_empty(i));
         }
         __syncwarp();
-        ++g;
+        last = set;
+        if (++set == P::SETS) {
+          set = 0;
+          phase ^= 1;
+        }
       }
     }
     if (!ok && lane == 0) {
       set_status(a.status, SL_DEV_GEMM_TIMEOUT);
       const unsigned long long t0 = clock64();                // the last group issued still uses the tensor memory
-      while (g > 0 && !mbar_try(done(g - 1), ((g - 1) / P::SETS) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      while (last >= 0 && !mbar_try(done(last), set ? phase : phase ^ 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
   } else {
     const int feature = (warp & 3) * 32 + lane, quarter = warp >> 2;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's lanes of the tensor memory
     const bool aligned = a.pairs != 0;
-    FeatureScales<FP32> rd;
+    FeatureScales<G, FP32> rd;
     const uint8_t* zeros;                                     // of the feature, or null
     {
       const int m = DUAL ? feature >> 6 : 0;                  // with SwiGLU the first 64 are the gate's, the others the up matrix's
       const long long f = (long long)min(n0 + (DUAL ? feature & 63 : feature), a.n_out - 1) * a.ng;   // behind the last feature any will do
-      rd.s = (const uint8_t*)a.scales[m] + f * (FP32 ? 4 : 2);
-      zeros = a.zeros[m] ? a.zeros[m] + f : nullptr;
-      rd.grp = b0 * P::GPT;
-      if (stages > 0) rd.fetch(rd.grp & ~(FeatureScales<FP32>::CHUNK - 1), a.ng, aligned);
+      rd.s = (const uint8_t*)(m ? a.scales[1] : a.scales[0]) + f * (FP32 ? 4 : 2);
+      zeros = m ? a.zeros[1] : a.zeros[0];
+      if (zeros) zeros += f;
     }
-    // zero point of this thread's k of step i; behind K the rows are 0
-    auto zero_of = [&](int i) -> uint32_t {
-      const int g = b0 * P::GPT + (i * P::KS + quarter * 32) / G;
-      return zeros && g < a.ng ? __ldg(zeros + g) : 8u;
+    // zero points of this thread's k of the two steps of a stage; behind K the rows are 0
+    uint32_t z[2], zn[2];
+    auto fetch = [&](int sg) {
+      const int g0 = (b0 + sg) * P::GPT;
+      rd.fetch(g0, a.ng, aligned);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        const int g = g0 + (part * P::KS + quarter * 32) / G;
+        zn[part] = 8u;
+        if (zeros && g < a.ng) zn[part] = __ldg(zeros + g);
+      }
     };
-    uint32_t z0 = stages > 0 ? zero_of(0) : 0u, z1 = stages > 0 ? zero_of(1) : 0u;
     bool ok = true;
-    // the codes of step i, half `part` of its stage, minus their zero points (exact in fp16) -> operand tile i & 1.  That tile is
-    // free: this warp has seen the MMAs of step i - 2 finished.
-    auto unpack = [&](int i, const int part) {
-      const int s = i >> 1;
-      if (part == 0) ok = __all_sync(0xffffffffu, mbar_wait(c_full(s), (s / P::CODES) & 1, s_abort));
+    uint32_t cphase = 0, phase = 0;
+    int cstage = 0, set = 0;
+    // the codes of half `part` of a stage, minus their zero points (exact in fp16) -> operand tile `part`.  That tile is free: this
+    // warp has seen the MMAs of the step before the last finished.
+    auto unpack = [&](const int part) {
+      if (part == 0) ok = __all_sync(0xffffffffu, mbar_wait(c_full(cstage), cphase, s_abort));
       if (!ok) return;
       const uint32_t chunk = part * 4 + quarter;              // of the 128-byte row, swizzled
-      const uint4 v = gq_lds128(codes0 + s % P::CODES * GQ_CODES + feature * 128 + ((chunk ^ (lane & 7)) << 4));
+      const uint4 v = gq_lds128(codes0 + cstage * GQ_CODES + feature * 128 + ((chunk ^ (lane & 7)) << 4));
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t zl = z0 * 0x00010001u, zh = zl << 4;           // like the codes: z 2^-24 and z 2^-20
-      z0 = z1;
-      z1 = zero_of(i + 2);
+      uint32_t zl = z[part] * 0x00010001u, zh = zl << 4;      // like the codes: z 2^-24 and z 2^-20
       auto minus = [](uint32_t x, uint32_t z) {
         const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&x), *reinterpret_cast<__half2*>(&z));
         return *reinterpret_cast<const uint32_t*>(&d);
@@ -305,46 +303,54 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         x[4 * j + 2] = minus(hi & 0x000f000fu, zl);
         x[4 * j + 3] = minus(hi & 0x00f000f0u, zh);
       }
-      tc_st16(tmem + lanes + (i & 1) * P::A_COLS + quarter * 16, x);
+      tc_st16(tmem + lanes + part * P::A_COLS + quarter * 16, x);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(unpacked(i));
-        if (part == 1) mbar_arrive(c_empty(s));
+        mbar_arrive(unpacked(part));
+        if (part == 1) mbar_arrive(c_empty(cstage));
+      }
+      if (part == 1 && ++cstage == P::CODES) {
+        cstage = 0;
+        cphase ^= 1;
       }
     };
-    auto add = [&](int i) {                                   // add up step i
+    auto add = [&](const int part) {                          // add up a step
 #pragma unroll
       for (int q = 0; q < GPS; ++q) {
-        const int g = i * GPS + q;
-        ok = __all_sync(0xffffffffu, mbar_wait(done(g), (g / P::SETS) & 1, s_abort));
+        ok = __all_sync(0xffffffffu, mbar_wait(done(set), phase, s_abort));
         if (!ok) return;
         tc_fence_after();
         uint32_t d[HC];
 #pragma unroll
-        for (int c = 0; c < HC; c += 16) tc_ld16(tmem + lanes + P::D_COL + g % P::SETS * NP + quarter * HC + c, d + c);
-        const float sc = rd.next(a.ng, aligned);
+        for (int c = 0; c < HC; c += 16) tc_ld16(tmem + lanes + P::D_COL + set * NP + quarter * HC + c, d + c);
         tc_wait_ld();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(added(g));
+        if (lane == 0) mbar_arrive(added(set));
+        if (++set == P::SETS) {
+          set = 0;
+          phase ^= 1;
+        }
+        const float sc = rd.get(part * GPS + q);
 #pragma unroll
         for (int c = 0; c < HC; c += 2) fma2(acc + c, sc, d + c);
       }
     };
+    if (stages > 0) fetch(0);
     for (int sg = 0; sg < stages && ok; ++sg) {
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        const int i = sg * 2 + part;
-        unpack(i, part);
-        if (!ok) break;
-        if (i == 0) rd.prime(a.ng, aligned);
-        else add(i - 1);
-        if (!ok) break;
-      }
+      z[0] = zn[0];
+      z[1] = zn[1];
+      unpack(0);
+      if (ok && sg > 0) add(1);
+      if (!ok) break;
+      rd.turn();
+      if (sg + 1 < stages) fetch(sg + 1);
+      unpack(1);
+      if (ok) add(0);
     }
-    if (stages > 0 && ok) add(steps - 1);
+    if (stages > 0 && ok) add(1);
     if (!ok && lane == 0) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
   }
 
