@@ -458,7 +458,7 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
     const surelock_w4* w = i && W2 ? W2 : W;
     a.zeros[i] = (const uint8_t*)w->zeros;
     a.scales[i] = w->scales;
-    if ((reinterpret_cast<uintptr_t>(w->scales) & 15) || (reinterpret_cast<uintptr_t>(w->zeros) & 1)) a.pairs = 0;
+    if ((reinterpret_cast<uintptr_t>(w->scales) & 15) || (reinterpret_cast<uintptr_t>(w->zeros) & 7)) a.pairs = 0;
     const int rc = gq_map(&maps[i], w->codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, n_out, K / 2, epilogue == EPI_SWIGLU ? 64 : 128, GQ_BK / 2);
     if (rc != SL_OK) return rc;
   }

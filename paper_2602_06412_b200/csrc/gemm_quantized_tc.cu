@@ -4,13 +4,15 @@
 //
 // With this many rows the products themselves would bound mma.sync (970 multiply-adds per clock and SM: 22 us for 128 rows of
 // 4096 x 12288), so they go to tcgen05: the weights are the 128-row operand, read from TENSOR MEMORY, where one thread per
-// feature and quarter of the k puts its codes after unpacking, less their zero points (u - z is exact in fp16 as u is, so there
+// feature puts its codes after unpacking, less their zero points (u - z is exact in fp16 as u is, so there
 // is no q here: a multiply-add less per element and group); the rows are the N operand, by TMA.  What bounds it then is
 // adding up: every group's accumulator (128 features x rows) is read back and takes one multiply-add per element.
-//   warps 0-15  feature 32 (w % 4) + lane; w / 4 = quarter of the step's k for unpacking, of the rows for adding up
-//   warp 16     one thread issues the TMA copies: codes in stages of 256 k of 128 features (with SwiGLU 64 of the gate and the
-//               same 64 of the up matrix), rows in stages of a step
-//   warp 17     one thread issues the MMAs of a step (128 k), group by group
+//   warps 0-15   add up: feature 32 (w % 4) + lane, w / 4 = quarter of the rows
+//   warps 16-19  unpack: feature 32 (w % 4) + lane (the same warps doing both, 16 of them: 192 against 168 us, 128 rows of the
+//                4096 x 126464 head: a step's chain of waits was twice as long)
+//   warp 20      one thread issues the TMA copies: codes in stages of 256 k of 128 features (with SwiGLU 64 of the gate and the
+//                same 64 of the up matrix), rows in stages of a step
+//   warp 21      issues the MMAs of a step (128 k), group by group
 // A step is unpacked into one of two operand tiles while the MMAs of the step before run, and that one is added up while its
 // own run: tensor memory holds 3 (128 rows) or 6 (64 rows) groups' accumulators.  K is split over a cluster of up to 8 CTAs
 // (sums through distributed shared memory in a fixed order).  All waits are bounded.
@@ -20,7 +22,7 @@ namespace sl {
 
 namespace {
 
-constexpr int GT_WORKERS = 16, GT_THREADS = 32 * (GT_WORKERS + 2);
+constexpr int GT_ADDERS = 16, GT_UNPACKERS = 4, GT_COPY = GT_ADDERS + GT_UNPACKERS, GT_MMA = GT_COPY + 1, GT_THREADS = 32 * (GT_MMA + 1);   // warps
 
 __device__ __forceinline__ void gt_mma(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
   asm volatile(
@@ -103,6 +105,40 @@ template <int G, bool FP32> struct FeatureScales {
   }
 };
 
+// Zero points of one feature likewise, packed; behind the feature's last group anything (the rows are 0 there)
+template <int G> struct FeatureZeros {
+  static constexpr int GPT = GQ_BK / G;
+  const uint8_t* z;            // of the feature, or null
+  uint32_t c[2], n[2];
+
+  __device__ __forceinline__ void fetch(int g0, int ng, bool aligned) {
+    n[0] = n[1] = 0x08080808u;
+    if (!z) return;
+    if (aligned) {
+      if (g0 < ng) {
+        if (GPT == 2) {
+          n[0] = __ldg(reinterpret_cast<const uint16_t*>(z + g0));
+        } else if (GPT == 4) {
+          n[0] = __ldg(reinterpret_cast<const uint32_t*>(z + g0));
+        } else {
+          const uint2 x = __ldg(reinterpret_cast<const uint2*>(z + g0));
+          n[0] = x.x; n[1] = x.y;
+        }
+      }
+      return;
+    }
+    n[0] = n[1] = 0;
+#pragma unroll
+    for (int i = 0; i < GPT; ++i)
+      if (g0 + i < ng) n[i / 4] |= (uint32_t)__ldg(z + g0 + i) << (8 * (i & 3));
+  }
+  __device__ __forceinline__ void turn() {
+    c[0] = n[0];
+    c[1] = n[1];
+  }
+  __device__ __forceinline__ uint32_t get(int i) const { return c[i / 4] >> (8 * (i & 3)) & 0xffu; }
+};
+
 template <int G, int NP> struct GtPlan {
   static constexpr int KS = 128, GPS = KS / G, GPT = GQ_BK / G;   // k and groups of a step, groups of a stage
   static constexpr int SLAB = NP * 128;                       // bytes of 64 k of the rows
@@ -145,21 +181,21 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   if (threadIdx.x == 0) {
     for (int i = 0; i < P::CODES; ++i) {
       mbar_init(c_full(i), 1);
-      mbar_init(c_empty(i), GT_WORKERS);
+      mbar_init(c_empty(i), GT_UNPACKERS);
     }
     for (int i = 0; i < P::ROWS; ++i) {
       mbar_init(r_full(i), 1);
       mbar_init(r_empty(i), 1);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(unpacked(i), GT_WORKERS);
+    for (int i = 0; i < 2; ++i) mbar_init(unpacked(i), GT_UNPACKERS);
     for (int i = 0; i < P::SETS; ++i) {
       mbar_init(done(i), 1);
-      mbar_init(added(i), GT_WORKERS);
+      mbar_init(added(i), GT_ADDERS);
     }
     *s_abort = 0;
     fence_mbar_init();
   }
-  if (warp == GT_WORKERS + 1) tc_alloc(smem_u32(s_tmem), 512);
+  if (warp == GT_MMA) tc_alloc(smem_u32(s_tmem), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -179,7 +215,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
 #pragma unroll
   for (int c = 0; c < HC; ++c) acc[c] = 0.f;
 
-  if (warp == GT_WORKERS) {
+  if (warp == GT_COPY) {
     if (lane == 0) {
       const uint64_t once = gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();   // a code is read once per row tile
       const int ahead = min(stages, P::CODES);
@@ -217,28 +253,32 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         set_status(a.status, SL_DEV_GEMM_TIMEOUT);
       }
     }
-  } else if (warp == GT_WORKERS + 1) {
+  } else if (warp == GT_MMA) {
     // The warp stays together and elects a lane per group: in a branch of one lane every operand of an MMA would first have to
     // be moved to the uniform registers that it is issued from (170 clocks per MMA).
     constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // fp16 x fp16 -> fp32, M = 128, N = NP
-    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0), ring = __shfl_sync(0xffffffffu, rows0, 0);
+    const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0), ring = __shfl_sync(0xffffffffu, rows0, 0), bars0 = __shfl_sync(0xffffffffu, bar0, 0);
+    const int n_steps = __shfl_sync(0xffffffffu, steps, 0);
+    auto bar = [&](int i) { return bars0 + 8u * i; };
+    constexpr int R_FULL = 2 * P::CODES, R_EMPTY = R_FULL + P::ROWS, UNPACKED = R_EMPTY + P::ROWS, DONE = UNPACKED + 2, ADDED = DONE + P::SETS;
     bool ok = true;
-    int set = 0, last = -1;                                   // set of the group at hand, of the last one issued
-    uint32_t phase = 0;
-    for (int i = 0; i < steps && ok; ++i) {
-      ok = __all_sync(0xffffffffu, mbar_wait(r_full(i), (i / P::ROWS) & 1, s_abort) && mbar_wait(unpacked(i), (i >> 1) & 1, s_abort));
-      const uint32_t rows = ring + i % P::ROWS * 2 * P::SLAB, op = base + (i & 1) * P::A_COLS;
+    int set = 0, last = -1, slot = 0;                         // set of the group at hand, of the last one issued; stage of rows
+    uint32_t phase = 0, rphase = 0;
+    for (int i = 0; i < n_steps && ok; ++i) {
+      const uint32_t rows = ring + slot * 2 * P::SLAB, op = base + (i & 1) * P::A_COLS;
+      ok = mbar_wait(bar(R_FULL + slot), rphase, s_abort) && mbar_wait(bar(UNPACKED + (i & 1)), (i >> 1) & 1, s_abort);
 #pragma unroll
       for (int q = 0; q < GPS; ++q) {
-        if (!ok || !(ok = __all_sync(0xffffffffu, mbar_wait(added(set), phase ^ 1, s_abort)))) break;
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(bar(ADDED + set), phase ^ 1, s_abort));
+        if (!ok) break;
         tc_fence_after();
         const uint32_t d = base + P::D_COL + set * NP;
         if (elect_one()) {
 #pragma unroll
           for (int k = q * (G / 16); k < (q + 1) * (G / 16); ++k)   // 16 k: 8 columns of the operand, 32 bytes of a slab's rows
             gt_mma(d, op + k * 8, smem_desc_k_sw128(rows + (k >> 2) * P::SLAB + (k & 3) * 32), idesc, k % (G / 16) != 0);
-          tc_commit(done(set));
-          if (q == GPS - 1) tc_commit(r_empty(i));
+          tc_commit(bar(DONE + set));
+          if (q == GPS - 1) tc_commit(bar(R_EMPTY + slot));
         }
         __syncwarp();
         last = set;
@@ -247,6 +287,10 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
           phase ^= 1;
         }
       }
+      if (++slot == P::ROWS) {
+        slot = 0;
+        rphase ^= 1;
+      }
     }
     if (!ok && lane == 0) {
       set_status(a.status, SL_DEV_GEMM_TIMEOUT);
@@ -254,103 +298,90 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
       while (last >= 0 && !mbar_try(done(last), set ? phase : phase ^ 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
   } else {
-    const int feature = (warp & 3) * 32 + lane, quarter = warp >> 2;
+    const int feature = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's lanes of the tensor memory
     const bool aligned = a.pairs != 0;
-    FeatureScales<G, FP32> rd;
-    const uint8_t* zeros;                                     // of the feature, or null
-    {
-      const int m = DUAL ? feature >> 6 : 0;                  // with SwiGLU the first 64 are the gate's, the others the up matrix's
-      const long long f = (long long)min(n0 + (DUAL ? feature & 63 : feature), a.n_out - 1) * a.ng;   // behind the last feature any will do
-      rd.s = (const uint8_t*)(m ? a.scales[1] : a.scales[0]) + f * (FP32 ? 4 : 2);
-      zeros = m ? a.zeros[1] : a.zeros[0];
-      if (zeros) zeros += f;
-    }
-    // zero points of this thread's k of the two steps of a stage; behind K the rows are 0
-    uint32_t z[2], zn[2];
-    auto fetch = [&](int sg) {
-      const int g0 = (b0 + sg) * P::GPT;
-      rd.fetch(g0, a.ng, aligned);
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        const int g = g0 + (part * P::KS + quarter * 32) / G;
-        zn[part] = 8u;
-        if (zeros && g < a.ng) zn[part] = __ldg(zeros + g);
-      }
-    };
+    const int m = DUAL ? feature >> 6 : 0;                    // with SwiGLU the first 64 are the gate's, the others the up matrix's
+    const long long f = (long long)min(n0 + (DUAL ? feature & 63 : feature), a.n_out - 1) * a.ng;   // behind the last feature any will do
     bool ok = true;
-    uint32_t cphase = 0, phase = 0;
-    int cstage = 0, set = 0;
-    // the codes of half `part` of a stage, minus their zero points (exact in fp16) -> operand tile `part`.  That tile is free: this
-    // warp has seen the MMAs of the step before the last finished.
-    auto unpack = [&](const int part) {
-      if (part == 0) ok = __all_sync(0xffffffffu, mbar_wait(c_full(cstage), cphase, s_abort));
-      if (!ok) return;
-      const uint32_t chunk = part * 4 + quarter;              // of the 128-byte row, swizzled
-      const uint4 v = gq_lds128(codes0 + cstage * GQ_CODES + feature * 128 + ((chunk ^ (lane & 7)) << 4));
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t zl = z[part] * 0x00010001u, zh = zl << 4;      // like the codes: z 2^-24 and z 2^-20
-      auto minus = [](uint32_t x, uint32_t z) {
-        const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&x), *reinterpret_cast<__half2*>(&z));
-        return *reinterpret_cast<const uint32_t*>(&d);
-      };
-      uint32_t x[16];
+    if (warp >= GT_ADDERS) {
+      FeatureZeros<G> rd;
+      rd.z = m ? a.zeros[1] : a.zeros[0];
+      if (rd.z) rd.z += f;
+      if (stages > 0) rd.fetch(b0 * P::GPT, a.ng, aligned);
+      for (int i = 0; i < steps; ++i) {
+        const int sg = i >> 1, part = i & 1;
+        if (part == 0) {
+          rd.turn();
+          if (sg + 1 < stages) rd.fetch((b0 + sg + 1) * P::GPT, a.ng, aligned);
+          ok = __all_sync(0xffffffffu, mbar_wait(c_full(sg), (sg / P::CODES) & 1, s_abort));
+        } else {
+          rd.c[0] = P::GPS == 4 ? rd.c[1] : rd.c[0] >> (8 * P::GPS % 32);
+        }
+        // the operand tile is free when the MMAs of step i - 2 are finished
+        if (ok && i >= 2) ok = __all_sync(0xffffffffu, mbar_wait(r_empty(i - 2), ((i - 2) / P::ROWS) & 1, s_abort));
+        if (!ok) break;
+        const uint32_t from = codes0 + sg % P::CODES * GQ_CODES + feature * 128, to = tmem + lanes + part * P::A_COLS;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t hi = w[j] >> 8;
-        x[4 * j] = minus(w[j] & 0x000f000fu, zl);
-        x[4 * j + 1] = minus(w[j] & 0x00f000f0u, zh);
-        x[4 * j + 2] = minus(hi & 0x000f000fu, zl);
-        x[4 * j + 3] = minus(hi & 0x00f000f0u, zh);
-      }
-      tc_st16(tmem + lanes + part * P::A_COLS + quarter * 16, x);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(unpacked(part));
-        if (part == 1) mbar_arrive(c_empty(cstage));
-      }
-      if (part == 1 && ++cstage == P::CODES) {
-        cstage = 0;
-        cphase ^= 1;
-      }
-    };
-    auto add = [&](const int part) {                          // add up a step
+        for (int q = 0; q < 4; ++q) {                         // 32 k: the codes minus their zero points, exact in fp16
+          const uint4 v = gq_lds128(from + (((part * 4 + q) ^ (lane & 7)) << 4));   // of the 128-byte row, swizzled
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          const uint32_t zl = rd.get(q * P::GPS / 4) * 0x00010001u, zh = zl << 4;   // like the codes: z 2^-24 and z 2^-20
+          auto minus = [](uint32_t x, uint32_t z) {
+            const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&x), *reinterpret_cast<__half2*>(&z));
+            return *reinterpret_cast<const uint32_t*>(&d);
+          };
+          uint32_t x[16];
 #pragma unroll
-      for (int q = 0; q < GPS; ++q) {
-        ok = __all_sync(0xffffffffu, mbar_wait(done(set), phase, s_abort));
-        if (!ok) return;
-        tc_fence_after();
-        uint32_t d[HC];
-#pragma unroll
-        for (int c = 0; c < HC; c += 16) tc_ld16(tmem + lanes + P::D_COL + set * NP + quarter * HC + c, d + c);
-        tc_wait_ld();
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t hi = w[j] >> 8;
+            x[4 * j] = minus(w[j] & 0x000f000fu, zl);
+            x[4 * j + 1] = minus(w[j] & 0x00f000f0u, zh);
+            x[4 * j + 2] = minus(hi & 0x000f000fu, zl);
+            x[4 * j + 3] = minus(hi & 0x00f000f0u, zh);
+          }
+          tc_st16(to + q * 16, x);
+        }
+        tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(added(set));
-        if (++set == P::SETS) {
-          set = 0;
-          phase ^= 1;
+        if (lane == 0) {
+          mbar_arrive(unpacked(i));
+          if (part == 1) mbar_arrive(c_empty(sg));
         }
-        const float sc = rd.get(part * GPS + q);
-#pragma unroll
-        for (int c = 0; c < HC; c += 2) fma2(acc + c, sc, d + c);
       }
-    };
-    if (stages > 0) fetch(0);
-    for (int sg = 0; sg < stages && ok; ++sg) {
-      z[0] = zn[0];
-      z[1] = zn[1];
-      unpack(0);
-      if (ok && sg > 0) add(1);
-      if (!ok) break;
-      rd.turn();
-      if (sg + 1 < stages) fetch(sg + 1);
-      unpack(1);
-      if (ok) add(0);
+    } else {
+      const int quarter = warp >> 2;                          // of the rows
+      FeatureScales<G, FP32> rd;
+      rd.s = (const uint8_t*)(m ? a.scales[1] : a.scales[0]) + f * (FP32 ? 4 : 2);
+      if (stages > 0) rd.fetch(b0 * P::GPT, a.ng, aligned);
+      int set = 0;
+      uint32_t phase = 0;
+      for (int sg = 0; sg < stages && ok; ++sg) {
+        rd.turn();
+        if (sg + 1 < stages) rd.fetch((b0 + sg + 1) * P::GPT, a.ng, aligned);
+#pragma unroll
+        for (int q = 0; q < P::GPT; ++q) {
+          ok = __all_sync(0xffffffffu, mbar_wait(done(set), phase, s_abort));
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t d[HC];
+#pragma unroll
+          for (int c = 0; c < HC; c += 16) tc_ld16(tmem + lanes + P::D_COL + set * NP + quarter * HC + c, d + c);
+          tc_wait_ld();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(added(set));
+          if (++set == P::SETS) {
+            set = 0;
+            phase ^= 1;
+          }
+          const float sc = rd.get(q);
+#pragma unroll
+          for (int c = 0; c < HC; c += 2) fma2(acc + c, sc, d + c);
+        }
+      }
     }
-    if (stages > 0 && ok) add(1);
     if (!ok && lane == 0) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
   }
 
@@ -358,12 +389,12 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   tc_fence_before();
   __syncthreads();
   const bool good = *s_abort == 0;
-  if (warp == GT_WORKERS + 1) {
+  if (warp == GT_MMA) {
     __syncwarp();
     tc_fence_after();
     tc_dealloc(tmem, 512);
   }
-  if (warp < GT_WORKERS) {
+  if (warp < GT_ADDERS) {
     const int feature = (warp & 3) * 32 + lane, quarter = warp >> 2;
 #pragma unroll
     for (int c = 0; c < HC; ++c) sRed[(quarter * HC + c) * P::PITCH + feature] = acc[c];
