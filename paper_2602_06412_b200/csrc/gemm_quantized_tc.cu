@@ -7,12 +7,12 @@
 // feature puts its codes after unpacking, less their zero points (u - z is exact in fp16 as u is, so there
 // is no q here: a multiply-add less per element and group); the rows are the N operand, by TMA.  What bounds it then is
 // adding up: every group's accumulator (128 features x rows) is read back and takes one multiply-add per element.
-//   warps 0-15   add up: feature 32 (w % 4) + lane, w / 4 = quarter of the rows
-//   warps 16-19  unpack: feature 32 (w % 4) + lane (the same warps doing both, 16 of them: 192 against 168 us, 128 rows of the
-//                4096 x 126464 head: a step's chain of waits was twice as long)
-//   warp 20      one thread issues the TMA copies: codes in stages of 256 k of 128 features (with SwiGLU 64 of the gate and the
-//                same 64 of the up matrix), rows in stages of a step
-//   warp 21      issues the MMAs of a step (128 k), group by group
+//   warps 0-15  add up: feature 32 (w % 4) + lane, w / 4 = quarter of the rows
+//   4 or 8      unpack: feature 32 (w % 4) + lane (16 warps that did both: 192 against 166 us, 128 rows of the 4096 x 126464
+//               head: a step's chain of waits was twice as long)
+//   1           one thread issues the TMA copies: codes in stages of 256 k of 128 features (with SwiGLU 64 of the gate and the
+//               same 64 of the up matrix), rows in stages of a step
+//   2           issue the MMAs of a step (128 k), group by group, each of every other step
 // A step is unpacked into one of two operand tiles while the MMAs of the step before run, and that one is added up while its
 // own run: tensor memory holds 3 (128 rows) or 6 (64 rows) groups' accumulators.  K is split over a cluster of up to 8 CTAs
 // (sums through distributed shared memory in a fixed order).  All waits are bounded.
@@ -22,7 +22,7 @@ namespace sl {
 
 namespace {
 
-constexpr int GT_ADDERS = 16, GT_UNPACKERS = 4, GT_COPY = GT_ADDERS + GT_UNPACKERS, GT_MMA = GT_COPY + 1, GT_THREADS = 32 * (GT_MMA + 1);   // warps
+constexpr int GT_ADDERS = 16;          // warps
 
 __device__ __forceinline__ void gt_mma(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
   asm volatile(
@@ -140,6 +140,9 @@ template <int G> struct FeatureZeros {
 };
 
 template <int G, int NP> struct GtPlan {
+  // warps: unpacking in teams of four, that take steps in turn (a second team at 128 rows would leave 72 registers to a thread,
+  // which then spills: 203 against 166 us)
+  static constexpr int TEAMS = NP == 128 ? 1 : 2, COPY = GT_ADDERS + 4 * TEAMS, MMA = COPY + 1, THREADS = 32 * (MMA + 2);
   static constexpr int KS = 128, GPS = KS / G, GPT = GQ_BK / G;   // k and groups of a step, groups of a stage
   static constexpr int SLAB = NP * 128;                       // bytes of 64 k of the rows
   static constexpr int CODES = NP == 128 ? 3 : 4, ROWS = NP == 128 ? 5 : 8;   // stages of codes (two steps each) and of rows (a step)
@@ -155,7 +158,7 @@ template <int G, int NP> struct GtPlan {
 }  // namespace
 
 template <int G, int NP, bool DUAL, bool FP32>
-__global__ void __launch_bounds__(GT_THREADS, 1)
+__global__ void __launch_bounds__(GtPlan<G, NP>::THREADS, 1)
 gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2, const __grid_constant__ CUtensorMap tmR,
                          const GqArgs a, const int epilogue) {
   using P = GtPlan<G, NP>;
@@ -181,13 +184,13 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   if (threadIdx.x == 0) {
     for (int i = 0; i < P::CODES; ++i) {
       mbar_init(c_full(i), 1);
-      mbar_init(c_empty(i), GT_UNPACKERS);
+      mbar_init(c_empty(i), 4 * P::TEAMS);
     }
     for (int i = 0; i < P::ROWS; ++i) {
       mbar_init(r_full(i), 1);
       mbar_init(r_empty(i), 1);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(unpacked(i), GT_UNPACKERS);
+    for (int i = 0; i < 2; ++i) mbar_init(unpacked(i), 4);
     for (int i = 0; i < P::SETS; ++i) {
       mbar_init(done(i), 1);
       mbar_init(added(i), GT_ADDERS);
@@ -195,7 +198,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
     *s_abort = 0;
     fence_mbar_init();
   }
-  if (warp == GT_MMA) tc_alloc(smem_u32(s_tmem), 512);
+  if (warp == P::MMA) tc_alloc(smem_u32(s_tmem), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -215,7 +218,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
 #pragma unroll
   for (int c = 0; c < HC; ++c) acc[c] = 0.f;
 
-  if (warp == GT_COPY) {
+  if (warp == P::COPY) {
     if (lane == 0) {
       const uint64_t once = gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();   // a code is read once per row tile
       const int ahead = min(stages, P::CODES);
@@ -253,20 +256,22 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         set_status(a.status, SL_DEV_GEMM_TIMEOUT);
       }
     }
-  } else if (warp == GT_MMA) {
-    // The warp stays together and elects a lane per group: in a branch of one lane every operand of an MMA would first have to
-    // be moved to the uniform registers that it is issued from (170 clocks per MMA).
+  } else if (warp >= P::MMA) {
+    // Two warps take turns, as the waits before a step's first MMA take as long as issuing its MMAs.  A warp stays together and
+    // elects a lane per group: in a branch of one lane every operand of an MMA would first have to be moved to the uniform
+    // registers that it is issued from (170 clocks per MMA).
     constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NP >> 3) << 17) | (8u << 24);   // fp16 x fp16 -> fp32, M = 128, N = NP
     const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0), ring = __shfl_sync(0xffffffffu, rows0, 0), bars0 = __shfl_sync(0xffffffffu, bar0, 0);
     const int n_steps = __shfl_sync(0xffffffffu, steps, 0);
     auto bar = [&](int i) { return bars0 + 8u * i; };
     constexpr int R_FULL = 2 * P::CODES, R_EMPTY = R_FULL + P::ROWS, UNPACKED = R_EMPTY + P::ROWS, DONE = UNPACKED + 2, ADDED = DONE + P::SETS;
     bool ok = true;
-    int set = 0, last = -1, slot = 0;                         // set of the group at hand, of the last one issued; stage of rows
-    uint32_t phase = 0, rphase = 0;
-    for (int i = 0; i < n_steps && ok; ++i) {
-      const uint32_t rows = ring + slot * 2 * P::SLAB, op = base + (i & 1) * P::A_COLS;
-      ok = mbar_wait(bar(R_FULL + slot), rphase, s_abort) && mbar_wait(bar(UNPACKED + (i & 1)), (i >> 1) & 1, s_abort);
+    const int first = warp - P::MMA;                          // of this warp's steps, every other one
+    int set = first * GPS, last = -1, slot = first;           // set of the group at hand, of the last one issued; stage of rows
+    uint32_t phase = 0, last_phase = 0, rphase = 0;
+    for (int i = first; i < n_steps && ok; i += 2) {
+      const uint32_t rows = ring + slot * 2 * P::SLAB, op = base + first * P::A_COLS;
+      ok = mbar_wait(bar(R_FULL + slot), rphase, s_abort) && mbar_wait(bar(UNPACKED + first), (i >> 1) & 1, s_abort);
 #pragma unroll
       for (int q = 0; q < GPS; ++q) {
         ok = __all_sync(0xffffffffu, ok && mbar_wait(bar(ADDED + set), phase ^ 1, s_abort));
@@ -282,20 +287,23 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         }
         __syncwarp();
         last = set;
-        if (++set == P::SETS) {
-          set = 0;
+        last_phase = phase;
+        set += q == GPS - 1 ? GPS + 1 : 1;                    // past the other warp's step
+        if (set >= P::SETS) {
+          set -= P::SETS;
           phase ^= 1;
         }
       }
-      if (++slot == P::ROWS) {
-        slot = 0;
+      slot += 2;
+      if (slot >= P::ROWS) {
+        slot -= P::ROWS;
         rphase ^= 1;
       }
     }
     if (!ok && lane == 0) {
       set_status(a.status, SL_DEV_GEMM_TIMEOUT);
       const unsigned long long t0 = clock64();                // the last group issued still uses the tensor memory
-      while (last >= 0 && !mbar_try(done(last), set ? phase : phase ^ 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      while (last >= 0 && !mbar_try(done(last), last_phase) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
   } else {
     const int feature = (warp & 3) * 32 + lane;
@@ -309,15 +317,14 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
       rd.z = m ? a.zeros[1] : a.zeros[0];
       if (rd.z) rd.z += f;
       if (stages > 0) rd.fetch(b0 * P::GPT, a.ng, aligned);
-      for (int i = 0; i < steps; ++i) {
+      for (int i = (warp - GT_ADDERS) / 4; i < steps; i += P::TEAMS) {
         const int sg = i >> 1, part = i & 1;
-        if (part == 0) {
+        if (P::TEAMS == 2 || part == 0) {
           rd.turn();
           if (sg + 1 < stages) rd.fetch((b0 + sg + 1) * P::GPT, a.ng, aligned);
           ok = __all_sync(0xffffffffu, mbar_wait(c_full(sg), (sg / P::CODES) & 1, s_abort));
-        } else {
-          rd.c[0] = P::GPS == 4 ? rd.c[1] : rd.c[0] >> (8 * P::GPS % 32);
         }
+        if (part) rd.c[0] = P::GPS == 4 ? rd.c[1] : rd.c[0] >> (8 * P::GPS % 32);
         // the operand tile is free when the MMAs of step i - 2 are finished
         if (ok && i >= 2) ok = __all_sync(0xffffffffu, mbar_wait(r_empty(i - 2), ((i - 2) / P::ROWS) & 1, s_abort));
         if (!ok) break;
@@ -347,7 +354,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(unpacked(i));
-          if (part == 1) mbar_arrive(c_empty(sg));
+          if (P::TEAMS == 2 || part == 1) mbar_arrive(c_empty(sg));
         }
       }
     } else {
@@ -389,7 +396,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   tc_fence_before();
   __syncthreads();
   const bool good = *s_abort == 0;
-  if (warp == GT_MMA) {
+  if (warp == P::MMA) {
     __syncwarp();
     tc_fence_after();
     tc_dealloc(tmem, 512);
@@ -402,7 +409,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   if (S > 1) cluster_sync_all(); else __syncthreads();
   if (M > 0 && good) {
     const int c0 = (int)(TO / 4 * rank / S), cols = (int)(TO / 4 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
-    for (int i = threadIdx.x; i < min(M, NP) * cols; i += GT_THREADS) {
+    for (int i = threadIdx.x; i < min(M, NP) * cols; i += P::THREADS) {
       const int r = i / cols, col = 4 * (c0 + i % cols);
       if (n0 + col >= a.n_out) continue;
       const float4 y = gq_total(sRed, S, r * P::PITCH + col);
@@ -437,7 +444,7 @@ int launch_gt(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
   static std::atomic<uint64_t> allowed{0};
   SL_CUDA_TRY(allow_smem(kernel, P::SMEM, allowed));
   const dim3 grid((a.n_out + TO - 1) / TO * S, (a.max_rows + NP - 1) / NP);
-  SL_CUDA_TRY(gq_launch(kernel, grid, GT_THREADS, P::SMEM, S, st, w[0], w[1], rows, a, epilogue));
+  SL_CUDA_TRY(gq_launch(kernel, grid, P::THREADS, P::SMEM, S, st, w[0], w[1], rows, a, epilogue));
   return SL_OK;
 }
 
