@@ -416,8 +416,8 @@ typedef struct {
  * epilogue 0: C bf16 [M][n_out]; 1: C is the fp32 residual stream, C[r][n] += sum; 2: C bf16 = silu(A W^T) * (A W2^T), W2 of
  * the same group, scale type and kind of zero point as W (W2 is ignored otherwise).  The codes enter the products exactly,
  * the rows as fp16 numbers (exact down to 2^-25 of the row's largest magnitude, off by at most 2^-35 of it below); group sums
- * are fp32 and are multiplied by their scale in fp32.  With up to 32 rows the zero point's share leaves a group's sum behind
- * the product, so roundings are relative to sum |a| (code + zero) scale, and a group of codes at their zero point need not
+ * are fp32 and are multiplied by their scale in fp32.  With up to 32 rows the zero point's share may leave a group's sum behind
+ * the product: roundings are relative to sum |a| (code + zero) scale then, and a group of codes at their zero point need not
  * give an exact 0.  A row with an infinity or a NaN gives NaN, and no other row is affected.
  * Any n_out; K a multiple of the group.  Up to 32 rows take one pass over the weights; more take one per 128 rows (per 64 up
  * to 64 rows, or with groups of 32), at most 65535 rows in all.  Rows >= *n_active of C are not touched.  Deterministic.

@@ -409,7 +409,15 @@ int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
   return SL_OK;
 }
 
+// Whether the kernel for few rows takes the call.  From 17 rows on its products bound it, where the weights are so few that the
+// other kernel works on all of them at once, with a quarter of the k or less to a CTA (K = 12288, 4096 features: 24.7 against
+// 20.5 us for 23 rows, 17.1 against 20.5 for 16); with more of them its fixed cost counts per round of CTAs (K = 4096, gate
+// and up matrices of 12288 features: 27.9 against 42 us).
 constexpr int GQ_FEW = 32;             // most rows of the kernel for few rows
+bool gq_few(int max_rows, int n_out, int epilogue) {
+  const int tiles = (n_out - 1) / (epilogue == EPI_SWIGLU ? 64 : 128) + 1;
+  return max_rows <= 16 || (max_rows <= GQ_FEW && 4ll * tiles > sm_count());
+}
 
 template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
   if (a.max_rows <= 8) return launch_gq<G, 1, DUAL, FP32>(w, a, epilogue, st);
@@ -418,7 +426,7 @@ template <int G, bool DUAL, bool FP32> int by_rows(const CUtensorMap* w, const G
   return launch_gq<G, 4, DUAL, FP32>(w, a, epilogue, st);
 }
 template <int G> int by_kind(const CUtensorMap* w, const void* A, const GqArgs& a, int epilogue, bool fp32, cudaStream_t st) {
-  const bool few = a.max_rows <= GQ_FEW;
+  const bool few = gq_few(a.max_rows, a.n_out, epilogue);
   SL_CUDA_TRY(launch_pdl(few ? gq_rewrite_rows_kernel<G, true> : gq_rewrite_rows_kernel<G, false>, dim3(a.max_rows), dim3(GS_THREADS), 0, st,
                          (const bf16*)A, a.n_active, a.max_rows, a.K, (uint8_t*)a.rows, (int32_t*)a.row_exp));
   if (!few) return launch_gemm_quantized_tc(w, a, G, fp32, epilogue, st);
@@ -438,7 +446,8 @@ int gq_map(CUtensorMap* out, const void* p, CUtensorMapDataType type, int elem, 
   return r == CUDA_SUCCESS ? SL_OK : SL_ECUDA;
 }
 
-// the workspace: the rewritten rows in either layout with room for the smallest groups, then their exponents
+// the workspace: the rewritten rows in either layout with room for the smallest groups (up to GQ_FEW rows the fragments take
+// more), then their exponents
 static size_t gq_rows_bytes(int max_rows, int K) {
   const size_t blocks = (K + GQ_BK - 1) / GQ_BK;
   if (max_rows <= GQ_FEW) return blocks * ((max_rows + 7) / 8) * GqPlan<32, 1>::CHUNK;
@@ -452,7 +461,7 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   GqArgs a{};
   CUtensorMap maps[2];
   a.ng = K / W->group;
-  const bool fp32 = W->scale_dtype == SL_FP32, few = max_rows <= GQ_FEW;
+  const bool fp32 = W->scale_dtype == SL_FP32, few = gq_few(max_rows, n_out, epilogue);
   a.pairs = a.ng % (few ? 2 : GQ_BK / W->group) == 0;
   for (int i = 0; i < 2; ++i) {
     const surelock_w4* w = i && W2 ? W2 : W;
