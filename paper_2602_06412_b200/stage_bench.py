@@ -5,6 +5,10 @@
     python -m paper_2602_06412_b200.stage_bench --stage softmax_kl --rows 820
     python -m paper_2602_06412_b200.stage_bench --stage kv_scatter --rows 6144
     python -m paper_2602_06412_b200.stage_bench --stage compact --flags 67108864
+    python -m paper_2602_06412_b200.stage_bench --stage gemm_quantized --M 1 --n_out 4096 --K 4096 --group 128
+    python -m paper_2602_06412_b200.stage_bench --stage kv_scatter_paged --rows 12288 --B 8 --N 1536 --cache e4m3
+    python -m paper_2602_06412_b200.stage_bench --stage kv_gather_paged --rows 6144 --B 8 --N 1536 --cache int8
+    python -m paper_2602_06412_b200.stage_bench --stage attention_paged --B 4 --N 16384 --rows 4 --cache e4m3
 
 Prints one JSON line: median and minimum device time (CUDA events on the launching stream, after warm-up), the
 algorithmic bytes / FLOPs of the launch, and the achieved fraction of the measured HBM or bf16 peak.  A buffer
@@ -55,7 +59,8 @@ def _time(fn, iters, warmup, flush):
 
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    ap.add_argument("--stage", required=True, choices=["gemm", "attention", "softmax_kl", "kv_scatter", "compact"])
+    ap.add_argument("--stage", required=True, choices=["gemm", "attention", "softmax_kl", "kv_scatter", "compact",
+                                                          "gemm_quantized", "kv_scatter_paged", "kv_gather_paged", "attention_paged"])
     ap.add_argument("--M", type=int, default=4096)
     ap.add_argument("--n_out", type=int, default=12288)
     ap.add_argument("--K", type=int, default=4096)
@@ -70,6 +75,10 @@ def main(argv=None):
     ap.add_argument("--V", type=int, default=126464)
     ap.add_argument("--d", type=int, default=4096)
     ap.add_argument("--flags", type=int, default=1 << 26)
+    ap.add_argument("--group", type=int, default=128, help="gemm_quantized: weights to a scale")
+    ap.add_argument("--cache", choices=["bf16", "e4m3", "int8"], default="e4m3", help="paged cache: element type")
+    ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--Hkv", type=int, default=32, help="paged cache: key heads")
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--warm-l2", action="store_true")
@@ -143,6 +152,47 @@ def main(argv=None):
         fn = lambda: SL.surelock_kv_scatter(k, v, idx, n, kc, vc)
         byts = 2.0 * 2 * rows * d * 2          # K and V, read + write
         res.update(shape=dict(rows=rows, d=d), bytes=byts, flops=0.0)
+    elif a.stage == "gemm_quantized":
+        K, ng = a.K, a.K // a.group
+        w4 = lambda: (torch.randint(0, 256, (a.n_out, K // 2), device=dev, generator=g, dtype=torch.uint8),
+                      (rnd(a.n_out, ng) * 0.02).to(torch.bfloat16), None)
+        A = rnd(a.M, K).to(torch.bfloat16)
+        W, W2 = w4(), w4() if a.epilogue == 2 else None
+        Cout = torch.zeros((a.M, a.n_out), dtype=torch.float32 if a.epilogue == 1 else torch.bfloat16, device=dev)
+        n = torch.tensor([a.M], dtype=torch.int32, device=dev)
+        wsp = torch.empty(SL.surelock_gemm_quantized_workspace_bytes(a.M, K), dtype=torch.uint8, device=dev)
+        fn = lambda: SL.surelock_gemm_quantized(A, W, Cout, n, a.epilogue, W2, wsp, status)
+        mats = 2 if W2 else 1
+        byts = mats * a.n_out * (K / 2 + 2.0 * ng) + 2.0 * a.M * K + (8.0 if a.epilogue == 1 else 2.0) * a.M * a.n_out
+        res.update(shape=[a.M, a.n_out, K], group=a.group, epilogue=a.epilogue, flops=2.0 * mats * a.M * a.n_out * K, bytes=byts)
+    elif a.stage in ("kv_scatter_paged", "kv_gather_paged", "attention_paged"):
+        B, N, Hkv, dh, M = a.B, a.N, a.Hkv, a.dh, a.rows
+        kind = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[a.cache]
+        per = -(-N // a.page)
+        mk = lambda: rnd(B * per, Hkv, a.page, dh).mul_(0.5 if a.cache == "bf16" else 40).to(kind)
+        sc = lambda: torch.full((B * per, Hkv, a.page), 0.0125, device=dev) if a.cache != "bf16" else None
+        table = torch.randperm(B * per, device=dev, generator=g).to(torch.int32).reshape(B, per)
+        cache = SL.PagedKV(mk(), mk(), table, sc(), sc())
+        token = Hkv * (dh * cache.k.element_size() + (0 if a.cache == "bf16" else 4))   # of K or of V
+        n = torch.tensor([M], dtype=torch.int32, device=dev)
+        flops = 0.0
+        if a.stage == "attention_paged":                          # M rows spread over the sequences, all of N tokens
+            offs = torch.tensor([M * b // B for b in range(B + 1)], dtype=torch.int32, device=dev)
+            lens = torch.full((B,), N, dtype=torch.int32, device=dev)
+            q = rnd(M, a.H, dh).to(torch.bfloat16)
+            o = torch.empty_like(q)
+            wsp = torch.empty(SL.surelock_attention_paged_workspace_bytes(dh), dtype=torch.uint8, device=dev)
+            fn = lambda: SL.surelock_attention_paged(cache, q, offs, lens, o, wsp, status)
+            byts, flops = 2.0 * B * N * token + 4.0 * M * a.H * dh, 4.0 * M * N * a.H * dh
+        else:
+            idx = torch.randperm(B * N, device=dev, generator=g)[:M].sort().values.to(torch.int32)
+            k, v = (rnd(M, Hkv, dh).to(torch.bfloat16) for _ in range(2))
+            if a.stage == "kv_scatter_paged":
+                fn = lambda: SL.surelock_kv_scatter_paged(cache, k, v, idx, n, N, status)
+            else:
+                fn = lambda: SL.surelock_kv_gather_paged(cache, idx, n, N, k, v, status)
+            byts = 2.0 * M * (token + 2 * Hkv * dh)
+        res.update(shape=dict(B=B, N=N, H=a.H, Hkv=Hkv, dh=dh, M=M, page=a.page), cache=a.cache, flops=flops, bytes=byts)
     else:
         total = a.flags
         lock = (torch.rand(total, device=dev, generator=g) < 0.5).to(torch.uint8)
