@@ -506,12 +506,18 @@ def _want(ok: bool, what: str):
         raise SurelockError(what)
 
 
-def _rows(t: torch.Tensor, heads: int, dh: int) -> int:
-    """Row stride, in elements, of a CUDA tensor [rows][heads][dh] whose rows are packed (they may lie apart)."""
+def _rows(t: torch.Tensor, heads: int, dh: int, like=None):
+    """(rows, row stride in elements) of a CUDA tensor [rows][heads][dh] whose rows are packed (they may lie apart); `like`:
+    a second one laid out the same way."""
     shape, st = t.shape, t.stride()
     if not (t.is_cuda and len(shape) == 3 and shape[1] == heads and shape[2] == dh and st[2] == 1 and (st[1] == dh or heads == 1)):
         raise SurelockError(f"a CUDA tensor [rows][{heads}][{dh}] with packed rows is wanted, got {tuple(shape)}, strides {st}, on {t.device}")
-    return st[0] if shape[0] > 1 else max(st[0], heads * dh)
+    n, pitch = shape[0], st[0]
+    if n <= 1:
+        pitch = max(pitch, heads * dh)
+    if like is not None and not (like.shape == shape and like.dtype == t.dtype and (like.stride() == st or _rows(like, heads, dh) == (n, pitch))):
+        raise SurelockError(f"two tensors laid out alike are wanted, got {tuple(shape)} {t.dtype}, strides {st}, and {tuple(like.shape)} {like.dtype}, strides {like.stride()}")
+    return n, pitch
 
 
 def _ints(t: torch.Tensor, least: int) -> int:
@@ -544,26 +550,20 @@ class PagedKV:
 
 def surelock_kv_scatter_paged(cache: PagedKV, k, v, active_idx, n_active, N: int, dev_status=None):
     """Rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32; rows may lie apart) into the pages, quantised on the way."""
-    pitch = _rows(k, cache.n_kv_heads, cache.head_dim)
-    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == pitch, "k and v must be laid out alike")
+    M, pitch = _rows(k, cache.n_kv_heads, cache.head_dim, v)
     stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
-    if not k.shape[0]:
-        return
-    _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), pitch, _ints(active_idx, k.shape[0]),
-                                           _ints(n_active, 1), k.shape[0], cache.n_seq, N, _dt(k), _p(dev_status), stream),
-           "surelock_kv_scatter_paged")
+    if M:
+        _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), pitch, _ints(active_idx, M), _ints(n_active, 1), M,
+                                               cache.n_seq, N, _dt(k), _p(dev_status), stream), "surelock_kv_scatter_paged")
 
 
 def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v, dev_status=None):
     """Positions active_idx back into the rows of k, v [M][n_kv_heads][head_dim] (bf16 or fp32)."""
-    pitch = _rows(k, cache.n_kv_heads, cache.head_dim)
-    _want(v.shape == k.shape and v.dtype == k.dtype and _rows(v, cache.n_kv_heads, cache.head_dim) == pitch, "k and v must be laid out alike")
+    M, pitch = _rows(k, cache.n_kv_heads, cache.head_dim, v)
     stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
-    if not k.shape[0]:
-        return
-    _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, k.shape[0]), _ints(n_active, 1), k.shape[0], cache.n_seq,
-                                          N, k.data_ptr(), v.data_ptr(), pitch, _dt(k), _p(dev_status), stream),
-           "surelock_kv_gather_paged")
+    if M:
+        _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, M), _ints(n_active, 1), M, cache.n_seq, N, k.data_ptr(),
+                                              v.data_ptr(), pitch, _dt(k), _p(dev_status), stream), "surelock_kv_gather_paged")
 
 
 def surelock_attention_paged_workspace_bytes(head_dim: int) -> int:
@@ -574,14 +574,13 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
     """q, o: bf16 [M][H][head_dim] (rows may lie apart); row_offsets int32 [B+1], seq_lens int32 [B]; workspace: uint8 tensor of
     surelock_attention_paged_workspace_bytes(head_dim) bytes, one per call that may run at the same time."""
     _want(q.dim() == 3 and o.shape == q.shape and q.dtype == torch.bfloat16 and o.dtype == torch.bfloat16, "q, o: bf16 [M][H][head_dim], alike")
-    H, B, dh = q.shape[1], seq_lens.numel(), cache.head_dim
-    _want(B <= cache.n_seq, "more sequences than the page table has")
+    (M, H, dh), B = q.shape, seq_lens.numel()
+    _want(B <= cache.n_seq and dh == cache.head_dim, "more sequences than the page table has, or another head_dim")
     if not cache._ws_bytes:
         cache._ws_bytes = surelock_attention_paged_workspace_bytes(dh)
-    _want(workspace.is_cuda and workspace.is_contiguous() and workspace.nbytes >= cache._ws_bytes, "workspace too small, or not on the GPU")
+    _want(workspace.is_contiguous() and workspace.nbytes >= cache._ws_bytes, "workspace too small")
     stream = _here(cache.k, q, row_offsets, seq_lens, o, workspace, dev_status)
-    if not q.shape[0]:
-        return
-    _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh), _ints(row_offsets, B + 1), _ints(seq_lens, B), q.shape[0],
-                                          B, H, o.data_ptr(), _rows(o, H, dh), workspace.data_ptr(), _p(dev_status), stream),
-           "surelock_attention_paged")
+    if M:
+        _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh)[1], _ints(row_offsets, B + 1), _ints(seq_lens, B), M, B, H,
+                                              o.data_ptr(), _rows(o, H, dh)[1], workspace.data_ptr(), _p(dev_status), stream),
+               "surelock_attention_paged")
