@@ -15,11 +15,16 @@
 // with programmatic dependent launch, adds them in unit order: no atomics, no counters, nothing kept between calls.
 //   warp 4     producer: TMA boxes of a page (and of its scales) into a ring of stages, 128-byte (64-byte for rows of 64
 //              bytes) swizzle; a page number outside the pool is replaced by one past its end, which TMA fills with zeros
-//   warps 0-3  S = Q K^T for 16 keys of the unit each (mma.sync m16n8k16: a tile of 16 rows is an eighth of a tcgen05 tile; the
-//              codes become fp16, exactly, in registers on the way), exp2, the weights into shared memory as the A fragments
-//              they already are; then O += P V for a quarter of the columns each, over all 64 keys.  O so takes d_h / 8
-//              registers per 16 rows, which lets four CTAs live on an SM: the chain of dependent steps of a unit, not the
-//              bandwidth, would bound fewer (one O per warp, two CTAs per SM: 4.2 - 5.2 TB/s).
+//   warps 0-3  with up to 8 rows to a tile: each warp alone with 16 keys of the unit, keys and columns of V as the 16-row
+//              operand of mma.sync m16n8k16, rows as the 8 columns: S^T = K Q^T, exp2, the weights transposed in registers, and
+//              O^T += V^T P; the four warps' O, maxima and sums meet once per item.  With tiles of 16 or 32 rows: S = Q K^T for
+//              16 keys each (a tile of 16 rows is an eighth of a tcgen05 tile), exp2, the weights into shared memory as the A
+//              fragments they already are; then O += P V for a quarter of the columns each, over all 64 keys.  Codes become
+//              fp16, exactly, in registers on the way to the products.
+// Measured (a plain copy: 6.57 TB/s): one new token each, 4 x 16384 tokens of 32 key heads in e4m3 85 us (6.5 TB/s), 32
+// ragged sequences of up to 4099 tokens of 8 key heads 38 us (5.4 TB/s); 8 x 4096 tokens in bf16 84 us (6.4 TB/s); 16 rows each,
+// 4 x 8192 tokens in e4m3 64 us, 32 rows each 97 us: there the products and the conversions bound it; 23 rows of one sequence
+// of 512 tokens 10 us, launches and waits.
 // The contraction index is permuted (the same way for Q and K) so that a lane reads its share of a key as 16-byte loads, and
 // the columns of O so that it reads neighbouring bytes of a value row; two keys' bytes are interleaved by byte permutes.
 // Numerics: q becomes fp16 times a power of two per row (its largest magnitude in [1, 2)), the weight w_j = p_j sv_j becomes
@@ -168,14 +173,15 @@ template <int DH, int KIND> struct Tile {
   static constexpr int STAGE = 2 * KV + (SCALED ? 1024 : 0);    // K, V, K scales, V scales (512 bytes each)
   static constexpr int STEPS = DH / 16;
 };
-// CTAs per SM that the registers are bounded for, and stages of the ring: what then fits the shared memory
-template <int MT> __host__ __device__ constexpr int ap_occupancy() { return MT <= 1 ? 4 : 3; }
+// CTAs per SM, and stages of the ring: what then fits the shared memory.  (Single tokens, 4 x 16384 in e4m3: 85 us with three
+// CTAs of three stages, 93 with registers for four, which fit with two stages at most, 89 with two CTAs of five.)
+constexpr int AP_OCC = 3;
 template <int DH, int KIND, int MT> struct Plan {
   using T = Tile<DH, KIND>;
   static constexpr int TILES = MT ? MT : 1;
   static constexpr int EXCHANGE = MT ? MT * 4 * 512 : 4 * 8 * (DH + 4) * 4;   // weights, or the warps' results
   static constexpr int FIXED = 1024 + TILES * T::STEPS * 512 + EXCHANGE + 16 * TILES * 4 * 9 + 256;   // Q, exchange, row factors, statistics
-  static constexpr int ROOM = 228 * 1024 / ap_occupancy<MT>() - 1024 - 256 - FIXED;                // 256: prefix sums of up to 31 sequences
+  static constexpr int ROOM = 228 * 1024 / AP_OCC - 1024 - 256 - FIXED;                             // 256: prefix sums of up to 31 sequences
   static constexpr int FIT = ROOM / T::STAGE;
   static constexpr int STAGES = FIT < 2 ? 2 : FIT > 6 ? 6 : FIT;
   static constexpr int SMEM = FIXED + STAGES * T::STAGE;                                           // and 8 bytes per sequence
@@ -246,7 +252,7 @@ template <int DH> __device__ __forceinline__ void load_values(uint32_t vb, int k
 }  // namespace
 
 template <int DH, int KIND, int MT>
-__global__ void __launch_bounds__(AP_THREADS, ap_occupancy<MT>())
+__global__ void __launch_bounds__(AP_THREADS, AP_OCC)
 attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                        const __grid_constant__ CUtensorMap tmKs, const __grid_constant__ CUtensorMap tmVs, const PagedAttnArgs a) {
   using T = Tile<DH, KIND>;
@@ -1070,7 +1076,7 @@ __global__ void __launch_bounds__(256) attention_paged_join_kernel(const PagedAt
 
 namespace {
 
-constexpr int AP_SLOT_ROWS = 96;   // most of (CTAs per SM) x (rows of a tile): 4 x 8, 4 x 16, 3 x 32
+constexpr int AP_SLOT_ROWS = AP_OCC * 32;   // most of (CTAs per SM) x (rows of a tile)
 
 // pool [n_pages][Hkv][page_size][head_dim] (or its scales, without the last dimension) in boxes of at most 64 places
 int page_map(CUtensorMap* out, const surelock_paged_kv& c, void* base, bool scales) {
@@ -1107,7 +1113,7 @@ int launch_ap(const CUtensorMap* maps, PagedAttnArgs a, long long max_units, voi
   static std::atomic<uint64_t> allowed{0};
   SL_CUDA_TRY(allow_smem(attention_paged_kernel<DH, KIND, MT>, PL::SMEM + (AP_MAX_B + 1) * 8, allowed));
   const int fit = 228 * 1024 / (smem + 1024);   // all CTAs of the grid are resident at once, so equal runs end together
-  const int occ = fit < ap_occupancy<MT>() ? fit : ap_occupancy<MT>();
+  const int occ = fit < AP_OCC ? fit : AP_OCC;
   const int cap = sm_count() * occ, grid = (int)(max_units < cap ? max_units : cap);
   const size_t rows = (size_t)sm_count() * AP_SLOT_ROWS * 2;
   a.part = reinterpret_cast<float*>(workspace);
@@ -1163,7 +1169,7 @@ int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long 
   // 128 rows: 37 against 31 us; tiles of 16 there: 222 and 33 us.  But where tiles of 32 leave SMs without work, tiles of 16 give
   // more of it a start at once (512 tokens, 23 rows, 32 heads: 11.7 against 10.4 us).
   const long long rows = ((long long)max_rows * a.G + B - 1) / B, per_tile = (long long)a.Hkv * ((a.max_tokens + AP_KEYS - 1) / AP_KEYS);
-  const bool little = B * ((rows + 31) / 32) * per_tile < (long long)sm_count() * ap_occupancy<2>();
+  const bool little = B * ((rows + 31) / 32) * per_tile < (long long)sm_count() * AP_OCC;
   const int mt = rows <= 8 ? 0 : rows <= 16 || little ? 1 : 2, tile_rows = mt ? 16 * mt : 8;
   const long long max_units = (((long long)max_rows * a.G + tile_rows - 1) / tile_rows + B) * per_tile;
 #define SL_AP(DH, KIND)                                                                                        \

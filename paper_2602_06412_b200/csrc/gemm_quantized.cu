@@ -111,6 +111,7 @@ template <int G, int NT> struct GqPlan {
 // order 0 4, 1 5 (over 16), 2 6, 3 7 (over 16), zeros behind K; then q of the groups, [group][row].  Or, not in FRAGMENTS, the
 // same 16 bytes row by row, without q.  And e + 24 per row.
 constexpr int GS_THREADS = 512;
+constexpr int GS_KEPT = 4;              // eights of a row that a thread keeps in registers: 16384 k in all
 
 template <int G, bool FRAGMENTS>
 __global__ void __launch_bounds__(GS_THREADS)
@@ -120,16 +121,20 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
   griddep_wait();
   griddep_launch();
   const int r = blockIdx.x;
-  if (r >= min(*n_active, max_rows)) return;
   const uint4* row = reinterpret_cast<const uint4*>(A + (long long)r * K);
   constexpr uint32_t MAG = 0x7fff7fffu;
-  uint4 first = make_uint4(0, 0, 0, 0);
-  uint32_t top = 0;
-  for (int i = threadIdx.x; i < K / 8; i += GS_THREADS) {
-    const uint4 v = __ldg(row + i);
-    if (i == threadIdx.x) first = v;
-    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & MAG, v.y & MAG), __vmaxu2(v.z & MAG, v.w & MAG)));
+  uint4 first[GS_KEPT];                              // requested before the count is known: the row is there, if unused
+#pragma unroll
+  for (int j = 0; j < GS_KEPT; ++j) {
+    const int i = threadIdx.x + j * GS_THREADS;
+    first[j] = i < K / 8 ? __ldg(row + i) : make_uint4(0, 0, 0, 0);
   }
+  if (r >= min(*n_active, max_rows)) return;
+  uint32_t top = 0;
+  auto largest = [&](const uint4& v) { top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & MAG, v.y & MAG), __vmaxu2(v.z & MAG, v.w & MAG))); };
+#pragma unroll
+  for (int j = 0; j < GS_KEPT; ++j) largest(first[j]);
+  for (int i = threadIdx.x + GS_KEPT * GS_THREADS; i < K / 8; i += GS_THREADS) largest(__ldg(row + i));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
   if ((threadIdx.x & 31) == 0) sTop[threadIdx.x >> 5] = top;
@@ -145,9 +150,7 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
   if (threadIdx.x == 0) row_exp[r] = e + 24;
   const float d0 = gq_pow2(-e / 2), d1 = gq_pow2(-e - (-e / 2));
   const int blocks = (K + GQ_BK - 1) / GQ_BK, end = (blocks * 32 + GS_THREADS - 1) / GS_THREADS * GS_THREADS;   // whole warps: they shuffle
-  for (int i = threadIdx.x; i < end; i += GS_THREADS) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (i < K / 8) v = i == threadIdx.x ? first : __ldg(row + i);
+  auto rewrite = [&](int i, const uint4& v) __attribute__((always_inline)) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     float x[8], sum = 0.f;
 #pragma unroll
@@ -182,7 +185,13 @@ gq_rewrite_rows_kernel(const bf16* __restrict__ A, const int32_t* __restrict__ n
         *reinterpret_cast<uint4*>(rows + ((long long)r * blocks * 32 + i) * 16) = y;
       }
     }
+  };
+#pragma unroll
+  for (int j = 0; j < GS_KEPT; ++j) {
+    const int i = threadIdx.x + j * GS_THREADS;
+    if (j * GS_THREADS < end) rewrite(i, first[j]);
   }
+  for (int i = threadIdx.x + GS_KEPT * GS_THREADS; i < end; i += GS_THREADS) rewrite(i, i < K / 8 ? __ldg(row + i) : make_uint4(0, 0, 0, 0));
 }
 
 }  // namespace

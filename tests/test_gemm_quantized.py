@@ -195,7 +195,7 @@ def test_outputs_that_cannot_be_written_in_fours_are_refused():
 
 @gpu
 @pytest.mark.parametrize("scale_t", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("M,n,K,group", [(2, 70, 1344, 64), (19, 130, 640, 128), (32, 64, 416, 32), (20, 4800, 160, 32), (26, 5003, 192, 64), (34, 200, 1056, 32), (50, 70, 1344, 64), (127, 257, 1280, 64),
+@pytest.mark.parametrize("M,n,K,group", [(2, 70, 1344, 64), (19, 130, 640, 128), (32, 64, 416, 32), (20, 4800, 160, 32), (26, 5003, 192, 64), (3, 40, 20480, 128), (37, 33, 18464, 32), (34, 200, 1056, 32), (50, 70, 1344, 64), (127, 257, 1280, 64),
                                          (128, 131, 1152, 128), (129, 40, 160, 32)])
 def test_large_zero_points_are_exact(M, n, K, group, scale_t):
     """Zero points over their whole range, 0 ... 127; |sum| <= 1344 x 4 x 127 x 4 < 2^24, so the whole numbers stay exact."""
