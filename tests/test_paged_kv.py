@@ -595,3 +595,36 @@ def test_refusals_with_tensors(monkeypatch):
     for f, a in good:
         with pytest.raises(SL.SurelockError):
             f(*a)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,dh", [([1, 3], 128), ([8, 2], 64), ([12, 9], 128), ([21, 1], 64)])
+def test_attention_paged_nan_stays_where_it_is(kind, rows, dh):
+    """A NaN in a query spoils that (row, head); one in a token spoils its key head's rows of that sequence; infinities in q too."""
+    lens, Hkv, G = [300, 130], 2, 2
+    pool = Pool(kind, 2, 300, Hkv, dh, 32)
+    _fill(pool, lens, Hkv, dh, seed=3)
+    offs = [0] + np.cumsum(rows).tolist()
+    q = torch.randn(offs[-1], Hkv * G, dh, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    o, A = _want(pool, q.double().numpy(), offs, lens, G)
+
+    def check(got, spoilt):
+        assert torch.all(torch.isnan(got[spoilt])), "spoilt rows are NaN"
+        keep = ~spoilt.numpy()
+        _near(got.cpu()[~spoilt], o[keep], A[keep], kind)
+
+    for value in (float("nan"), float("inf")):
+        bad = q.clone()
+        bad[0, 1, 7] = value
+        spoilt = torch.zeros(offs[-1], Hkv * G, dtype=torch.bool)
+        spoilt[0, 1] = True
+        check(_attend(pool, bad.to(DEV), offs, lens).cpu(), spoilt)
+    page, place = int(pool.table[0, 200 // 32]), 200 % 32
+    spoilt = torch.zeros(offs[-1], Hkv * G, dtype=torch.bool)
+    spoilt[:offs[1], G:] = True                                       # sequence 0, key head 1
+    for t in ((pool.k, pool.v) if pool.ks is None else (pool.ks, pool.vs)):
+        was = t[page, 1, place].clone()
+        t[page, 1, place] = float("nan")
+        check(_attend(pool, q.to(DEV), offs, lens).cpu(), spoilt)
+        t[page, 1, place] = was
