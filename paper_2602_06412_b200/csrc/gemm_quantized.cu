@@ -30,8 +30,8 @@
 // The first codes are requested before the rewriting kernel has finished: it does not write them.  K is split over the CTAs
 // of a cluster when the features alone do not fill the GPU; the sums meet through distributed shared memory in a fixed
 // order: deterministic.  All waits are bounded.
-// Measured, 1 / 8 / 16 rows: 4096 x 4096 6.8 / 7.2 / 8.8 us, 4096 x 12288 13.4 / 14.0 / 16.6, gate and up 12288 x 4096 with SwiGLU
-// 18.7 / 19.1 / 22.2 (23 rows 27.8), 126464 x 4096 55 / 55.5 / 71 (4.9 TB/s).  About 5 us of each are start, rewriting and join.
+// Measured, 1 / 8 / 16 rows: 4096 x 4096 6.6 / 7.0 / 8.1 us, 4096 x 12288 12.5 / 12.9 / 15.9, gate and up 12288 x 4096 with SwiGLU
+// 17.6 / 18.1 / 20.7 (23 rows 26.6), 126464 x 4096 55 / 55.5 / 70 (4.9 TB/s).  About 5 us of each are start, rewriting and join.
 #include "gemm_quantized.cuh"
 
 namespace sl {
@@ -50,48 +50,57 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// Scales and zero points of one feature, shared out over the four lanes that work on it: a chunk of 8 groups (bf16 scales,
-// two groups per lane) or 4 (fp32, one per lane); the next chunk is requested when one begins.  Zero points are kept like
-// the scales, negated.
-template <bool FP32> struct GroupReader {
-  static constexpr int CHUNK = FP32 ? 4 : 8;
+// Scales and zero points of one feature for the groups of a stage, requested a stage ahead.  The four lanes that work on the
+// feature have them all, or, with 8 groups to a stage, two each.
+template <int G, bool FP32> struct GroupReader {
+  static constexpr int GPT = GQ_BK / G, COUNT = GPT > 4 ? 2 : GPT, WORDS = COUNT * (FP32 ? 4 : 2) / 4;
   const uint8_t *s, *z;        // of the feature; z may be null
-  uint32_t c, cz, n, nz;       // present and next chunk
+  uint32_t c[WORDS], n[WORDS], cz, nz;   // present and next stage
 
-  __device__ __forceinline__ void fetch(int g0, int t, int ng, bool pairs) {   // chunk of groups from g0 -> n, nz
-    if (FP32) {
-      const int g = g0 + t;
-      n = g < ng ? __ldg(reinterpret_cast<const uint32_t*>(s) + g) : 0u;
-      nz = __float_as_uint(z && g < ng ? -(float)__ldg(z + g) : -8.f);
-    } else {
-      const int g = g0 + 2 * t;
-      uint32_t a = 8, b = 8;
-      n = 0;
-      if (pairs) {
-        if (g < ng) {
-          n = __ldg(reinterpret_cast<const uint32_t*>(s + 2 * (size_t)g));
-          if (z) {
-            const uint32_t y = __ldg(reinterpret_cast<const uint16_t*>(z + g));
-            a = y & 0xffu;
-            b = y >> 8;
-          }
+  __device__ __forceinline__ void fetch(int g0, int t, int ng, bool aligned) {   // of the stage whose first group is g0 -> n, nz
+    const int g = g0 + (GPT > COUNT ? COUNT * t : 0);
+    nz = 0x08080808u;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) n[i] = 0;
+    if (aligned) {
+      if (g < ng) {
+        const uint8_t* p = s + (size_t)g * (FP32 ? 4 : 2);
+        if (WORDS == 1) {
+          n[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+        } else if (WORDS == 2) {
+          const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+          n[0] = x.x; n[1 % WORDS] = x.y;
+        } else {
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+          n[0] = x.x; n[1 % WORDS] = x.y; n[2 % WORDS] = x.z; n[3 % WORDS] = x.w;
         }
-      } else {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(s);
-        if (g < ng) n = __ldg(p + g);
-        if (g + 1 < ng) n |= (uint32_t)__ldg(p + g + 1) << 16;
-        if (z && g < ng) a = __ldg(z + g);
-        if (z && g + 1 < ng) b = __ldg(z + g + 1);
+        if (z) nz = COUNT == 2 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(z + g)) : __ldg(reinterpret_cast<const uint32_t*>(z + g));
       }
-      nz = pack_bf16(-(float)a, -(float)b);
+    } else {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+        if (g + i < ng) {
+          if (FP32) n[i % WORDS] = __ldg(reinterpret_cast<const uint32_t*>(s) + g + i);
+          else n[i / 2 % WORDS] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(s) + g + i) << (16 * (i & 1));
+          if (z) nz = (nz & ~(0xffu << (8 * i))) | (uint32_t)__ldg(z + g + i) << (8 * i);
+        }
     }
   }
-  // group g: scale and minus the zero point (behind the feature's last group anything finite: its D and q are 0)
-  template <int ODD> __device__ __forceinline__ void get(int g, int lane, float& scale, float& minus_z) const {
-    const int src = (lane & 28) | (FP32 ? g & 3 : (g >> 1) & 3);
-    const uint32_t x = __shfl_sync(0xffffffffu, c, src), y = __shfl_sync(0xffffffffu, cz, src);
-    scale = __uint_as_float(FP32 ? x : ODD ? x & 0xffff0000u : x << 16);
-    minus_z = __uint_as_float(FP32 ? y : ODD ? y & 0xffff0000u : y << 16);
+  __device__ __forceinline__ void turn() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) c[i] = n[i];
+    cz = nz;
+  }
+  // group i of the stage: scale and minus the zero point (behind the feature's last group anything finite: its D and q are 0)
+  __device__ __forceinline__ void get(int i, int lane, float& scale, float& minus_z) const {
+    const int at = i % COUNT;
+    uint32_t x = c[FP32 ? at % WORDS : at / 2 % WORDS], y = cz;
+    if (GPT > COUNT) {
+      x = __shfl_sync(0xffffffffu, x, (lane & 28) | (i / COUNT));
+      y = __shfl_sync(0xffffffffu, y, (lane & 28) | (i / COUNT));
+    }
+    scale = __uint_as_float(FP32 ? x : at & 1 ? x & 0xffff0000u : x << 16);
+    minus_z = 8388608.f - __uint_as_float(__byte_perm(y, 0x4b000000u, 0x7440 + at));   // 2^23 - (2^23 + z)
   }
 };
 
@@ -275,35 +284,29 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
     // feature rows of this lane in a stage: rows rev and 8 + rev of the warp's 16; with SwiGLU the first 64 of a
     // stage are the gate's, the others the up matrix's
-    GroupReader<FP32> rd[2];
+    GroupReader<G, FP32> rd[2];
     const int mat = DUAL ? warp / (GQ_WARPS / 2) : 0;
     const uint32_t row0 = (uint32_t)(warp * 16 + rev) * 128;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int f = (DUAL ? warp % (GQ_WARPS / 2) : warp) * 16 + h * 8 + rev;
       const long long at = (long long)min(n0 + f, a.n_out - 1) * a.ng;   // features behind the last one: any scales, codes are 0
-      rd[h].s = (const uint8_t*)a.scales[mat] + at * (FP32 ? 4 : 2);
-      rd[h].z = a.zeros[mat] ? a.zeros[mat] + at : nullptr;
+      rd[h].s = (const uint8_t*)(mat ? a.scales[1] : a.scales[0]) + at * (FP32 ? 4 : 2);
+      const uint8_t* zeros = mat ? a.zeros[1] : a.zeros[0];
+      rd[h].z = zeros ? zeros + at : nullptr;
     }
-    constexpr int CH = GroupReader<FP32>::CHUNK;
-    int grp = b0 * P::GPT;
-    auto fetch = [&](int g0) {
+    auto fetch = [&](int i) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) rd[h].fetch(g0, t, a.ng, a.pairs != 0);
+      for (int h = 0; h < 2; ++h) rd[h].fetch((b0 + i) * P::GPT, t, a.ng, a.pairs != 0);
     };
-    auto turn = [&](int g0) {                                 // the chunk that was requested becomes the present one
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        rd[h].c = rd[h].n;
-        rd[h].cz = rd[h].nz;
-      }
-      fetch(g0 + CH);
-    };
-    if (n > 0) fetch(grp & ~(CH - 1));
+    if (n > 0) fetch(0);
     bool ok = true;
     for (int i = 0; i < n; ++i) {
       const int st = i % P::STAGES;
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(st), (i / P::STAGES) & 1, s_abort)))) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) rd[h].turn();
+      if (i + 1 < n) fetch(i + 1);
       const uint32_t base = smem_u32(smem + st * P::STAGE), tb = base + GQ_CODES + lane * 16;
       const uint32_t sw = (uint32_t)rev << 4;                 // swizzle: rows rev and 8 + rev of a tile have the same low bits
 #pragma unroll
@@ -353,14 +356,9 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
           if (w % WPG == WPG - 1) {
             constexpr int HG = 4 / WPG;                       // groups per 128 k
             const int gi = hf * HG + w / WPG;
-            if (((grp & (CH - 1)) == 0) || (i == 0 && gi == 0)) turn(grp & ~(CH - 1));
             float sc[2], mz[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (gi & 1) rd[h].template get<1>(grp, lane, sc[h], mz[h]);
-              else rd[h].template get<0>(grp, lane, sc[h], mz[h]);
-            }
-            ++grp;
+            for (int h = 0; h < 2; ++h) rd[h].get(gi, lane, sc[h], mz[h]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               float q[2];                                     // of rows 2 t, 2 t + 1
@@ -423,8 +421,8 @@ int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
 
 // Whether the kernel for few rows takes the call.  From 17 rows on its products bound it, where the weights are so few that the
 // other kernel works on all of them at once, with a quarter of the k or less to a CTA (K = 12288, 4096 features: 24.7 against
-// 20.5 us for 23 rows, 17.1 against 20.5 for 16); with more of them its fixed cost counts per round of CTAs (K = 4096, gate
-// and up matrices of 12288 features: 27.9 against 42 us).
+// 20.1 us for 23 rows, 15.9 against 20.1 for 16); with more of them its fixed cost counts per round of CTAs (K = 4096, gate
+// and up matrices of 12288 features: 26.7 against 42 us).
 constexpr int GQ_FEW = 32;             // most rows of the kernel for few rows
 bool gq_few(int max_rows, int n_out, int epilogue) {
   const int tiles = (n_out - 1) / (epilogue == EPI_SWIGLU ? 64 : 128) + 1;
@@ -474,7 +472,7 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   CUtensorMap maps[2];
   a.ng = K / W->group;
   const bool fp32 = W->scale_dtype == SL_FP32, few = gq_few(max_rows, n_out, epilogue);
-  a.pairs = a.ng % (few ? 2 : GQ_BK / W->group) == 0;
+  a.pairs = a.ng % (few && W->group == 32 ? 2 : GQ_BK / W->group) == 0;
   for (int i = 0; i < 2; ++i) {
     const surelock_w4* w = i && W2 ? W2 : W;
     a.zeros[i] = (const uint8_t*)w->zeros;
