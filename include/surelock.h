@@ -495,7 +495,8 @@ int surelock_kv_gather_paged(const surelock_paged_kv *cache, const int32_t *acti
 /* Attention of the packed queries against a paged cache (Algorithm 1 line 12; with one row per sequence, the attention of a
  * new token): for packed row r of sequence b, row_offsets[b] <= r < row_offsets[b + 1], and every head h of H,
  *   o[r][h] = softmax_j(q[r][h] . K_j[h'] / sqrt(d_h)) V_j[h'],  0 <= j < seq_lens[b],  h' = h / (H / n_kv_heads)
- * over the sequence's cached tokens; no mask besides the length.  seq_lens[b] = 0 gives rows of zeros.
+ * over the sequence's cached tokens; no mask besides the length.  seq_lens[b] = 0 gives rows of zeros; scores that are all -inf
+ * give NaN, as 0 / 0 does.
  *   q, o         dev bf16, row r at r * q_stride / o_stride elements (multiples of 8), heads packed [H][head_dim]
  *   row_offsets  dev int32 [B + 1], seq_lens dev int32 [B] (0 ... max_pages * page_size); a value out of range is clamped to
  *                it and stores device status 4; rows behind row_offsets[B] are left as they are

@@ -630,7 +630,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
             sum += sL[w * ROWS + row] * (mw == -INFINITY ? 1.f : fast_exp2(mw - top));   // without keys 0, or NaN from a score that is none
           }
           const int e = tile * ROWS + row;
-          const float inv = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+          const float inv = !whole ? 1.f : s.len == 0 ? 0.f : 1.f / sum;   // a sum of 0 over keys (all scores -inf): 0 / 0
           if (!whole && part == 0) a.ml[slot + row] = make_float2(top, sum);
           bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH;
           float* pt = a.part + (slot + row) * DH;
@@ -937,7 +937,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
           const float* p = sL + row;
           const float sum = (p[0] + p[ROWS]) + (p[2 * ROWS] + p[3 * ROWS]);
           const int e = tile * ROWS + row;
-          const float f = (T::SCALED ? pow2i(E[mt][h] - AP_W_EXP) : 1.f) * (whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f);
+          const float f = (T::SCALED ? pow2i(E[mt][h] - AP_W_EXP) : 1.f) * (whole ? (s.len == 0 ? 0.f : 1.f / sum) : 1.f);
           bf16* o = a.o + (long long)(s.r0 + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + warp * (DH / 4);
           float* part = a.part + (slot + row) * DH + warp * (DH / 4);
           if (!whole && warp == 0 && t == 0) a.ml[slot + row] = make_float2(m[mt][h], sum);
@@ -971,7 +971,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
 // (c, y) has the item that starts in run c.
 //
 // Few pieces (at most 16): a warp per row, 32 rows at once over the grid's 4 y; lane i has the statistics of piece i, and the
-// pieces' values are requested together with them.
+// pieces' values are requested together with them.  (An item that was cut has keys: a sum of 0 means that all scores are -inf, and
+// gives NaN.)
 template <int DH, int ROWS> __device__ __forceinline__ void join_few(const PagedAttnArgs& a, const int4& d, int n) {
   constexpr int PER = DH / 32, LOADS = 8;
   const int valid = d.z >> 16, kvh = d.z & 0xffff, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1006,7 +1007,7 @@ template <int DH, int ROWS> __device__ __forceinline__ void join_few(const Paged
       }
     }
     const int e = d.y + row;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;
     bf16* o = a.o + (long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + lane * PER;
 #pragma unroll
     for (int c = 0; c < PER; c += 2) *reinterpret_cast<uint32_t*>(o + c) = pack_bf16(x[c] * inv, x[c + 1] * inv);
@@ -1056,7 +1057,7 @@ template <int DH, int ROWS> __device__ __forceinline__ void join_many(const Page
       }
       const int e = d.y + row;
       a.o[(long long)(d.x + e / a.G) * a.o_stride + (long long)(kvh * a.G + e % a.G) * DH + threadIdx.x] =
-          __float2bfloat16_rn(l == 0.f ? 0.f : y / l);
+          __float2bfloat16_rn(y / l);
     }
     __syncthreads();
   }

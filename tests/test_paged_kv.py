@@ -628,3 +628,45 @@ def test_attention_paged_nan_stays_where_it_is(kind, rows, dh):
         t[page, 1, place] = float("nan")
         check(_attend(pool, q.to(DEV), offs, lens).cpu(), spoilt)
         t[page, 1, place] = was
+
+
+# ---- rows whose scores are all minus infinity -------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lens,rows,Hkv,G,tokens", [
+    ([1, 2, 0], [1, 2, 1], 2, 2, 64),                                 # tiles of 8 rows, whole items
+    ([300, 0, 64], [1, 2, 1], 2, 2, 300),                             # cut into a few pieces
+    ([2500, 1], [1, 1], 1, 4, 2500),                                  # and into many
+    ([1, 2, 0], [9, 13, 5], 2, 1, 64),                                # tiles of 16
+    ([300, 0, 2000], [9, 13, 5], 1, 1, 2000),
+    ([1, 0], [20, 21], 8, 1, 2048),                                   # tiles of 32
+    ([600, 2], [20, 21], 8, 1, 2048),
+])
+def test_scores_of_minus_infinity_give_nan_and_no_key_gives_zeros(kind, lens, rows, Hkv, G, tokens):
+    """softmax over scores that are all -inf is 0 / 0; only a sequence without keys has rows of zeros."""
+    dh = 128
+    pool = Pool(kind, len(lens), tokens, Hkv, dh, 32)
+    _fill(pool, lens, Hkv, dh, seed=sum(lens))
+    if kind == torch.bfloat16:
+        pool.k[..., 7] = -1.0
+    else:
+        pool.k.view(torch.uint8)[..., 7] = 0xb8 if kind != torch.int8 else 251      # -1, -5
+    offs = [0] + np.cumsum(rows).tolist()
+    q = torch.randn(offs[-1], Hkv * G, dh, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    o, A = _want(pool, q.double().numpy(), offs, lens, G)
+    spoilt = torch.zeros(offs[-1], Hkv * G, dtype=torch.bool)
+    for b in range(len(lens)):
+        spoilt[offs[b], 0] = spoilt[offs[b + 1] - 1, -1] = True
+    bad = q.clone()
+    bad[..., 7] = torch.where(spoilt, float("inf"), bad[..., 7])
+    status = _i32([0])
+    got = _attend(pool, bad.to(DEV), offs, lens, status).cpu()
+    assert status.item() == 0
+    for b, n in enumerate(lens):
+        at = slice(offs[b], offs[b + 1])
+        if n == 0:
+            assert torch.all(got[at] == 0)
+            continue
+        assert torch.all(torch.isnan(got[at][spoilt[at]]))
+        keep = ~spoilt[at]
+        _near(got[at][keep], o[at][keep.numpy()], A[at][keep.numpy()], kind)
