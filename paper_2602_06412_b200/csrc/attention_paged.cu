@@ -154,8 +154,8 @@ struct Seq {
 };
 template <int MT> __device__ __forceinline__ Seq seq_of(const PagedAttnArgs& a, int b) {
   Seq s;
-  s.r0 = max(0, a.row_offsets[b]);
-  s.rows = min(a.row_offsets[b + 1], a.max_rows) - s.r0;
+  s.r0 = min(max(a.row_offsets[b], 0), a.max_rows);   // both clamped before the difference, which then cannot overflow
+  s.rows = min(max(a.row_offsets[b + 1], 0), a.max_rows) - s.r0;
   const int len = a.seq_lens[b];
   s.len = min(max(len, 0), a.max_tokens);
   s.tiles = s.rows > 0 ? (int)(((long long)s.rows * a.G + ap_rows<MT>() - 1) / ap_rows<MT>()) : 0;
@@ -295,7 +295,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   for (int b = threadIdx.x; b < a.B; b += AP_THREADS) {
     const Seq s = seq_of<MT>(a, b);
     sCum[b + 1] = (long long)a.Hkv * s.tiles * s.nb;
-    if (blockIdx.x == 0 && (a.seq_lens[b] != s.len || a.row_offsets[b] != s.r0 || s.rows < 0 || a.row_offsets[b + 1] > a.max_rows))
+    if (blockIdx.x == 0 && (a.seq_lens[b] != s.len || a.row_offsets[b] != s.r0 || a.row_offsets[b + 1] != s.r0 + s.rows || s.rows < 0))
       set_status(a.status, SL_DEV_BAD_INDEX);
   }
   if (threadIdx.x == 0) sCum[0] = 0;

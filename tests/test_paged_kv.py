@@ -670,3 +670,16 @@ def test_scores_of_minus_infinity_give_nan_and_no_key_gives_zeros(kind, lens, ro
         assert torch.all(torch.isnan(got[at][spoilt[at]]))
         keep = ~spoilt[at]
         _near(got[at][keep], o[at][keep.numpy()], A[at][keep.numpy()], kind)
+
+
+@gpu
+@pytest.mark.parametrize("offs,same", [([0, 2, -2 ** 31], [0, 2, 2]), ([0, 2, 2 ** 31 - 1], [0, 2, 4]), ([-2 ** 31, 2, 4], [0, 2, 4]),
+                                       ([2 ** 31 - 1, -2 ** 31, 3], [0, 0, 3]), ([0, 0, -1], [0, 0, 0]), ([2 ** 31 - 1, 2 ** 31 - 1, -2 ** 31], [4, 4, 4])])
+def test_row_offsets_of_any_value_are_clamped(offs, same):
+    """A difference of two offsets may pass 32 bits; rows that no sequence has left keep their bytes."""
+    pool = Pool(torch.int8, 2, 64, 1, 64, 16)
+    _fill(pool, [64, 50], 1, 64)
+    q = torch.randn(4, 2, 64, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    status = _i32([0])
+    got = _attend(pool, q, offs, [64, 50], status)
+    assert status.item() == 4 and torch.equal(got, _attend(pool, q, same, [64, 50]))
