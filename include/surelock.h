@@ -424,7 +424,8 @@ typedef struct {
  * workspace: dev, surelock_gemm_quantized_workspace_bytes(max_rows, K) bytes, any contents, 256-byte aligned, used during the
  * call only: calls (and captured graphs) that may run at the same time need one each.  SL_EINVAL on NULL pointers, a group
  * that does not divide K, an unknown epilogue, a missing or different W2; SL_EUNSUPPORTED for another group, more rows, codes
- * or A that are not 16-byte aligned, or a bf16 C that is not 8-byte aligned.  dev_status may be NULL; 2 = a bounded wait ran
+ * or A that are not 16-byte aligned, a bf16 C that is not 8-byte aligned, or scales or an fp32 C that are not aligned to their
+ * elements.  dev_status may be NULL; 2 = a bounded wait ran
  * out.  Asynchronous on `stream`. */
 int surelock_gemm_quantized(const void *A, const surelock_w4 *W, const surelock_w4 *W2, void *C, const int32_t *n_active,
                             int max_rows, int n_out, int K, int epilogue, void *workspace, int32_t *dev_status, void *stream);

@@ -1033,7 +1033,8 @@ static int w4_check(const surelock_w4* W, int K) {
   if (!W || !W->codes || !W->scales || W->group <= 0 || K % W->group) return SL_EINVAL;
   if (W->scale_dtype != SL_BF16 && W->scale_dtype != SL_FP32) return SL_EINVAL;
   if (W->group != 32 && W->group != 64 && W->group != 128) return SL_EUNSUPPORTED;
-  return (reinterpret_cast<uintptr_t>(W->codes) & 15) ? SL_EUNSUPPORTED : SL_OK;
+  const uintptr_t elem = W->scale_dtype == SL_FP32 ? 4 : 2;   // scales are read one at a time where nothing more is known of them
+  return (reinterpret_cast<uintptr_t>(W->codes) & 15) || (reinterpret_cast<uintptr_t>(W->scales) & (elem - 1)) ? SL_EUNSUPPORTED : SL_OK;
 }
 
 int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4* W2, void* C, const int32_t* n_active,
@@ -1047,7 +1048,7 @@ int surelock_gemm_quantized(const void* A, const surelock_w4* W, const surelock_
   }
   if (rc != SL_OK) return rc;
   if ((reinterpret_cast<uintptr_t>(A) & 15) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return SL_EUNSUPPORTED;
-  if (epilogue != EPI_RESIDUAL && (reinterpret_cast<uintptr_t>(C) & 7)) return SL_EUNSUPPORTED;   // written four features at a time
+  if (reinterpret_cast<uintptr_t>(C) & (epilogue == EPI_RESIDUAL ? 3 : 7)) return SL_EUNSUPPORTED;   // bf16 is written four features at a time
   if (max_rows == 0) return SL_OK;
   return launch_gemm_quantized(A, W, epilogue == EPI_SWIGLU ? W2 : nullptr, C, n_active, max_rows, n_out, K, epilogue, workspace,
                                dev_status, (cudaStream_t)stream);

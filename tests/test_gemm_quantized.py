@@ -280,3 +280,17 @@ def test_refusals_with_tensors(monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)       # as if another device were the current one
     with pytest.raises(SL.SurelockError):
         SL.surelock_gemm_quantized(A, W, C, one)
+
+
+# ---- alignment of scales and of an fp32 output ------------------------------------------------------------------------
+def test_elements_off_their_alignment_are_refused():
+    """Read or written one at a time, which the device cannot do off an element's alignment.  Without rows: nothing is launched."""
+    build_mod.build()
+    L = SL.lib()
+    w = lambda at, t: ctypes.byref(SL._W4(codes=0x1000, scales=at, zeros=None, group=64, scale_dtype=t))
+    call = lambda a, b, c, epilogue: L.surelock_gemm_quantized(0x100, a, b, c, 0x300, 0, 10, 128, epilogue, 0x1000, None, None)
+    for t, at, rc in [(SL.SL_BF16, 0x2001, -5), (SL.SL_BF16, 0x2002, 0), (SL.SL_FP32, 0x2002, -5), (SL.SL_FP32, 0x2001, -5), (SL.SL_FP32, 0x2004, 0)]:
+        assert call(w(at, t), None, 0x200, 0) == rc
+        assert call(w(0x2000, t), w(at, t), 0x200, 2) == rc           # and of the second matrix
+    for c, rc in [(0x202, -5), (0x201, -5), (0x204, 0)]:
+        assert call(w(0x2000, SL.SL_BF16), None, c, 1) == rc
