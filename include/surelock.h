@@ -513,6 +513,13 @@ int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int6
                              const int32_t *seq_lens, int max_rows, int B, int H, void *o, int64_t o_stride, void *workspace,
                              int32_t *dev_status, void *stream);
 
+/* Failure-detection diagnostic for the two calls with few bits that wait on copies: in the next surelock_gemm_quantized or
+ * surelock_attention_paged that this thread launches, the first CTA waits for 16 bytes that are never copied.  Its bounded waits
+ * run out (about 2 s each), it stores device status 2 or 3 in the call's dev_status, and the kernel returns with the outputs of
+ * that CTA undefined; nothing hangs or traps, and the workspace may be used again.  The call must be given at least one
+ * active row. */
+int surelock_lose_next_copy(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -113,6 +113,7 @@ def lib() -> C.CDLL:
         "surelock_kv_gather_paged": (i32, [C.POINTER(_PagedKV), vp, vp, i32, i32, i32, vp, vp, C.c_int64, i32, vp, vp]),
         "surelock_attention_paged_workspace_bytes": (sz, [i32]),
         "surelock_attention_paged": (i32, [C.POINTER(_PagedKV), vp, C.c_int64, vp, vp, i32, i32, i32, vp, C.c_int64, vp, vp, vp]),
+        "surelock_lose_next_copy": (i32, []),
         "surelock_attention": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i32, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -495,6 +496,11 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
         raise SurelockError("surelock_gemm_quantized: workspace too small")
     _check(lib().surelock_gemm_quantized(_p(A), C.byref(w), C.byref(w2) if w2 is not None else None, _p(Cout), _ints(n_active, 1), M, n, K,
                                          epilogue, _p(workspace), _p(dev_status), stream), "surelock_gemm_quantized")
+
+
+def surelock_lose_next_copy():
+    """Diagnostic: a copy that the next quantised product or paged attention of this thread waits for is never made."""
+    _check(lib().surelock_lose_next_copy(), "surelock_lose_next_copy")
 
 
 # ---- paged K/V cache ---------------------------------------------------------------------------------------

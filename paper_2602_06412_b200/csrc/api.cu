@@ -343,6 +343,14 @@ static int run_layer(surelock_ctx* c, int l, float* x) {
   return layer_back(c, l, x);
 }
 
+// bytes that the first copy of this thread's next launch waits for in vain (see surelock_lose_next_copy)
+static thread_local int g_lost_copy = 0;
+int sl::take_lost_copy() {
+  const int lost = g_lost_copy;
+  g_lost_copy = 0;
+  return lost;
+}
+
 extern "C" {
 
 int surelock_init(surelock_ctx** out, const surelock_model_cfg* cfg, const surelock_weights* w, int N, int batch,
@@ -1027,6 +1035,11 @@ int surelock_gemm_fused(const void* A, const void* W, const void* W2, void* C, c
     if (rc != SL_EUNSUPPORTED) return rc;
   }
   return launch_gemm_simt(A, W, W2, C, n_active, max_rows, n_out, K, dtype, epilogue, (cudaStream_t)stream);
+}
+
+int surelock_lose_next_copy(void) {
+  g_lost_copy = 16;
+  return SL_OK;
 }
 
 static int w4_check(const surelock_w4* W, int K) {

@@ -58,6 +58,7 @@ struct PagedAttnArgs {
   float2* ml;      // [grid][2][rows]
   float* part;     // [grid][2][rows][DH]
   int32_t* status;
+  int lost;        // bytes that CTA 0's first stage waits for in vain: 0, but for the diagnostic
 };
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar, uint64_t policy) {
@@ -362,7 +363,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         }
         if (!(ok = warp_wait(empty(st), ph ^ 1, s_abort))) break;
         const int n = __popc(__ballot_sync(0xffffffffu, have));
-        if (lane == 0) mbar_expect_tx(full(st), (uint32_t)(n * box * 2 * (T::ROW + (T::SCALED ? 4 : 0))));
+        if (lane == 0) mbar_expect_tx(full(st), (uint32_t)(n * box * 2 * (T::ROW + (T::SCALED ? 4 : 0)) + (cnt == 0 && blockIdx.x == 0 ? a.lost : 0)));
         __syncwarp();
         if (have) {
           const int x = t % a.page_size;
@@ -382,13 +383,12 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
       }
       u += nblk;
     }
-    if (!ok) {
-      // gave up: the copies in flight still write to this CTA's shared memory, wait for them (bounded)
-      const unsigned long long t0 = clock64();
-      for (unsigned i = cnt > (unsigned)STAGES ? cnt - STAGES : 0; i < cnt; ++i)
-        while (!mbar_try(full((int)(i % STAGES)), (i / STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-      if (lane == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
-    }
+    // The copies in flight still write to this CTA's shared memory: they have landed (a bounded wait) before this warp leaves,
+    // whichever warp's wait may have run out.
+    const unsigned long long t0 = clock64();
+    for (unsigned i = cnt > (unsigned)STAGES ? cnt - STAGES : 0; i < cnt; ++i)
+      while (!mbar_try(full((int)(i % STAGES)), (i / STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+    if (!ok && lane == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
     return;
   }
 
@@ -1165,6 +1165,7 @@ int launch_attention_paged(const surelock_paged_kv& c, const void* q, long long 
   a.max_tokens = c.max_pages * c.page_size;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c.head_dim);
   a.status = status;
+  a.lost = take_lost_copy();
   // Rows of a tile: what a sequence has on average, padded as little as possible, up to 32.  Tiles of 64 share the conversions
   // of the codes among more rows, but leave fewer CTAs per SM: 4 x 8192 tokens, 64 rows each: 198 against 178 us; 1536 tokens,
   // 128 rows: 37 against 31 us; tiles of 16 there: 222 and 33 us.  But where tiles of 32 leave SMs without work, tiles of 16 give

@@ -190,6 +190,9 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
                           int n_out, int K, int epilogue, void* workspace, int32_t* status, cudaStream_t st);
 size_t gemm_quantized_workspace_bytes(int max_rows, int K);
 
+// 16 once after surelock_lose_next_copy() on this thread, otherwise 0
+int take_lost_copy();
+
 // optional un-locking (unlock.cu)
 int launch_invert_mask(const uint8_t* lock, uint8_t* inv, int total, cudaStream_t st);
 int launch_lock_commit(const float* kl, const float* conf, const float* lse, const int32_t* idx, const int32_t* n_active,

@@ -255,7 +255,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       auto codes = [&](int i) {
         const int st = i % P::STAGES;
         const uint32_t at = smem_u32(smem + st * P::STAGE);
-        mbar_expect_tx(full(st), GQ_CODES + NT * P::CHUNK);
+        mbar_expect_tx(full(st), GQ_CODES + NT * P::CHUNK + (i == 0 && blockIdx.x == 0 ? a.lost : 0));
         tma_load_2d_hint(at, &tmW, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
         if (DUAL) tma_load_2d_hint(at + GQ_CODES / 2, &tmW2, (b0 + i) * (GQ_BK / 2), n0, full(st), once);
       };
@@ -272,13 +272,12 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         }
         bulk_load(smem_u32(smem + st * P::STAGE) + GQ_CODES, a.rows + (long long)(b0 + i) * NT * P::CHUNK, NT * P::CHUNK, full(st));
       }
-      if (!ok) {
-        // gave up: wait (bounded) for the copies in flight, which write to this CTA's shared memory
-        const unsigned long long t0 = clock64();
-        for (int k = max(0, i - P::STAGES); k < i; ++k)
-          while (!mbar_try(full(k % P::STAGES), (k / P::STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-        set_status(a.status, SL_DEV_GEMM_TIMEOUT);
-      }
+      // The copies in flight still write to this CTA's shared memory: they have landed (a bounded wait) before this thread goes
+      // on, whichever warp's wait may have run out.
+      const unsigned long long t0 = clock64();
+      for (int k = max(0, i - P::STAGES); k < i; ++k)
+        while (!mbar_try(full(k % P::STAGES), (k / P::STAGES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      if (!ok) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
     }
   } else {
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
@@ -489,6 +488,7 @@ int launch_gemm_quantized(const void* A, const surelock_w4* W, const surelock_w4
   a.n_out = n_out;
   a.K = K;
   a.status = status;
+  a.lost = take_lost_copy();
   switch (W->group) {
     case 32: return by_kind<32>(maps, A, a, epilogue, fp32, st);
     case 64: return by_kind<64>(maps, A, a, epilogue, fp32, st);

@@ -19,6 +19,7 @@ struct GqArgs {
   int max_rows, n_out, K, ng;
   int pairs;                           // scales and zero points of a few neighbouring groups lie on aligned addresses
   int32_t* status;
+  int lost;                            // bytes that CTA 0's first stage waits for in vain: 0, but for the diagnostic
 };
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {

@@ -227,7 +227,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
       const int ahead = min(stages, P::CODES);
       auto codes = [&](int s) {
         const uint32_t at = codes0 + s % P::CODES * GQ_CODES;
-        mbar_expect_tx(c_full(s), GQ_CODES);
+        mbar_expect_tx(c_full(s), GQ_CODES + (s == 0 && blockIdx.x + blockIdx.y == 0 ? a.lost : 0));
         tma_load_2d_hint(at, &tmW, (b0 + s) * (GQ_BK / 2), n0, c_full(s), once);
         if (DUAL) tma_load_2d_hint(at + GQ_CODES / 2, &tmW2, (b0 + s) * (GQ_BK / 2), n0, c_full(s), once);
       };
@@ -249,15 +249,14 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
 #pragma unroll
         for (int k = 0; k < 2; ++k) tma_load_2d(at + k * P::SLAB, &tmR, b0 * GQ_BK + i * P::KS + k * 64, r0, r_full(i));
       }
-      if (!ok) {
-        // gave up: wait (bounded) for the copies in flight, which write to this CTA's shared memory
-        const unsigned long long t0 = clock64();
-        for (int k = max(0, asked - P::CODES); k < asked; ++k)
-          while (!mbar_try(c_full(k), (k / P::CODES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-        for (int k = max(0, i - P::ROWS); k < i; ++k)
-          while (!mbar_try(r_full(k), (k / P::ROWS) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
-        set_status(a.status, SL_DEV_GEMM_TIMEOUT);
-      }
+      // The copies in flight still write to this CTA's shared memory: they have landed (a bounded wait) before this thread goes
+      // on, whichever warp's wait may have run out.
+      const unsigned long long t0 = clock64();
+      for (int k = max(0, asked - P::CODES); k < asked; ++k)
+        while (!mbar_try(c_full(k), (k / P::CODES) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      for (int k = max(0, i - P::ROWS); k < i; ++k)
+        while (!mbar_try(r_full(k), (k / P::ROWS) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
+      if (!ok) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
     }
   } else if (warp >= P::MMA) {
     // Two warps take turns, as the waits before a step's first MMA take as long as issuing its MMAs.  A warp stays together and

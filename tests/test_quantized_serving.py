@@ -10,7 +10,7 @@ import torch
 from paper_2602_06412_b200 import binding as SL
 
 from .test_gemm_quantized import _tol, _weights
-from .test_paged_kv import DEV, Pool, _i32, _near, _want, quantise
+from .test_paged_kv import DEV, Pool, _attend, _fill, _i32, _near, _want, quantise
 
 pytestmark = pytest.mark.gpu
 
@@ -143,3 +143,45 @@ def test_read_back_into_a_contiguous_cache(kind):
             tol = (np.exp(2 * ds) - 1 + 2 * 2.0 ** -8 + 2.0 ** -11) * spread + 2.0 ** -8 * np.abs(o)
             for got in (contiguous, paged):
                 assert np.all(np.abs(got[rows, h].cpu().double().numpy() - o) <= tol)
+
+
+# ---- failure detection: a copy that never arrives --------------------------------------------------------------------
+@pytest.mark.parametrize("M,n,K,group", [(5, 600, 1024, 64), (13, 5003, 4096, 128), (70, 200, 1056, 32), (128, 300, 4096, 128)])
+def test_a_lost_copy_ends_a_product_with_a_status(M, n, K, group):
+    """Calls of both kernels, with stages that all fit the ring and with more: the bounded waits run out, status 2 is stored, and
+    the next call on the same workspace is right, bit for bit."""
+    W, _ = _weights(n, K, group, True, torch.bfloat16, seed=1)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    want, got = (torch.zeros(M, n, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = torch.full((SL.surelock_gemm_quantized_workspace_bytes(M, K),), 255, dtype=torch.uint8, device=DEV)
+    status, count = _i32([0]), _i32([M])
+    call = lambda out: SL.surelock_gemm_quantized(A, W, out, count, workspace=ws, dev_status=status)
+    call(want)
+    assert status.item() == 0
+    SL.surelock_lose_next_copy()
+    call(got)
+    assert status.item() == 2
+    assert torch.equal(got[:, -8:], want[:, -8:])                     # features of another CTA than the first
+    status.zero_()
+    call(got)
+    assert status.item() == 0 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("kind,lens,rows", [(torch.int8, [64, 200], [1, 2]), (torch.bfloat16, [5000, 100], [1, 1]), (torch.float8_e4m3fn, [3000, 900], [20, 9])])
+def test_a_lost_copy_ends_an_attention_with_a_status(kind, lens, rows):
+    Hkv, dh = 2, 128
+    pool = Pool(kind, 2, max(lens), Hkv, dh, 64)
+    _fill(pool, lens, Hkv, dh)
+    offs = [0] + np.cumsum(rows).tolist()
+    q = torch.randn(offs[-1], Hkv, dh, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+    ws = torch.full((SL.surelock_attention_paged_workspace_bytes(dh),), 255, dtype=torch.uint8, device=DEV)
+    status = _i32([0])
+    want = _attend(pool, q, offs, lens, status, ws)
+    assert status.item() == 0
+    SL.surelock_lose_next_copy()
+    got = _attend(pool, q, offs, lens, status, ws)
+    assert status.item() == 3
+    assert torch.equal(got[-1, -1], want[-1, -1])                     # of the last sequence and head, far from the first CTA
+    status.zero_()
+    got = _attend(pool, q, offs, lens, status, ws)
+    assert status.item() == 0 and torch.equal(got, want)
