@@ -302,9 +302,13 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
         rphase ^= 1;
       }
     }
-    if (!ok && lane == 0) {
-      set_status(a.status, SL_DEV_GEMM_TIMEOUT);
-      const unsigned long long t0 = clock64();                // the last group issued still uses the tensor memory
+    // The tensor memory is freed behind the barrier below: this warp's MMAs, which end in order, are through with it (a bounded
+    // wait), whichever warp's wait may have run out.  When both warps finish, at most GPS groups, of the other warp, were issued
+    // after its last one, on other accumulators (SETS > GPS), so that group's barrier has not gone on a phase; after a wait that ran
+    // out it may have, and then this one runs to its limit.
+    if (lane == 0) {
+      if (!ok) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
+      const unsigned long long t0 = clock64();
       while (last >= 0 && !mbar_try(done(last), last_phase) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
   } else {

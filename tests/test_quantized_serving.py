@@ -185,3 +185,33 @@ def test_a_lost_copy_ends_an_attention_with_a_status(kind, lens, rows):
     status.zero_()
     got = _attend(pool, q, offs, lens, status, ws)
     assert status.item() == 0 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("K", [32 * i for i in (1, 8, 9, 16, 24, 40, 57, 130)])
+def test_no_wait_runs_to_its_limit_when_a_kernel_leaves(K):
+    """Before a CTA leaves it waits for its copies and matrix instructions, at most 2 s and without a status: a wait for the wrong
+    phase would show as time only.  Numbers of stages below, at and above the rings' sizes, both kernels, odd and even steps."""
+    lens = [K, 3 * K]
+    pool = Pool(torch.int8, 2, 3 * K, 1, 64, 16)
+    _fill(pool, lens, 1, 64)
+    ws = torch.empty(SL.surelock_attention_paged_workspace_bytes(64), dtype=torch.uint8, device=DEV)
+    calls = []
+    for M, n in ((3, 70), (20, 4800), (40, 130), (128, 300)):
+        for group in (32, 64, 128):
+            if K % group:
+                continue
+            W, _ = _weights(n, K, group, True, torch.bfloat16, seed=1)
+            A, out = torch.ones(M, K, dtype=torch.bfloat16, device=DEV), torch.zeros(M, n, dtype=torch.bfloat16, device=DEV)
+            calls.append(lambda A=A, W=W, out=out, n=_i32([M]): SL.surelock_gemm_quantized(A, W, out, n))
+    for rows in ([1, 1], [9, 8], [40, 2]):
+        q, offs = torch.ones(sum(rows), 2, 64, dtype=torch.bfloat16, device=DEV), _i32([0, rows[0], sum(rows)])
+        calls.append(lambda q=q, offs=offs, o=torch.zeros_like(q), n=_i32(lens): SL.surelock_attention_paged(pool.cache, q, offs, n, o, ws))
+    for call in calls:
+        call()                                                        # loads the kernel
+        t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        torch.cuda.synchronize()
+        t[0].record()
+        call()
+        t[1].record()
+        torch.cuda.synchronize()
+        assert t[0].elapsed_time(t[1]) < 100
