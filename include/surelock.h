@@ -426,7 +426,7 @@ typedef struct {
  * that does not divide K, an unknown epilogue, a missing or different W2; SL_EUNSUPPORTED for another group, more rows, codes
  * or A that are not 16-byte aligned, a bf16 C that is not 8-byte aligned, or scales or an fp32 C that are not aligned to their
  * elements.  dev_status may be NULL; 2 = a bounded wait ran
- * out.  Asynchronous on `stream`. */
+ * out, and the features that this concerns are NaN.  Asynchronous on `stream`. */
 int surelock_gemm_quantized(const void *A, const surelock_w4 *W, const surelock_w4 *W2, void *C, const int32_t *n_active,
                             int max_rows, int n_out, int K, int epilogue, void *workspace, int32_t *dev_status, void *stream);
 size_t surelock_gemm_quantized_workspace_bytes(int max_rows, int K);
@@ -507,17 +507,18 @@ int surelock_kv_gather_paged(const surelock_paged_kv *cache, const int32_t *acti
  * parts are joined in a fixed order: results do not change from run to run.  Made for few rows per sequence (1 ... 128 /
  * (H / n_kv_heads)); more rows are correct but re-read the cache per 16 or 32 (row, head) pairs.  A bad page reads as
  * zeros (K = V = 0).  Scores, maxima, sums and outputs are accumulated in fp32; the weights enter the last product with 11
- * (SL_BF16 cache: 8) bits.  dev_status may be NULL; 3 = a bounded wait ran out.  Asynchronous on `stream`. */
+ * (SL_BF16 cache: 8) bits.  dev_status may be NULL; 3 = a bounded wait ran out, and the rows that this concerns are NaN or
+ * not written.  Asynchronous on `stream`. */
 size_t surelock_attention_paged_workspace_bytes(int head_dim);
 int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int64_t q_stride, const int32_t *row_offsets,
                              const int32_t *seq_lens, int max_rows, int B, int H, void *o, int64_t o_stride, void *workspace,
                              int32_t *dev_status, void *stream);
 
 /* Failure-detection diagnostic for the two calls with few bits that wait on copies: in the next surelock_gemm_quantized or
- * surelock_attention_paged that this thread launches, the first CTA waits for 16 bytes that are never copied.  Its bounded waits
- * run out (about 2 s each), it stores device status 2 or 3 in the call's dev_status, and the kernel returns with the outputs of
- * that CTA undefined; nothing hangs or traps, and the workspace may be used again.  The call must be given at least one
- * active row. */
+ * surelock_attention_paged that this thread launches, one CTA (the product's first, the attention's second if there is one)
+ * waits for 16 bytes that are never copied.  Its bounded waits run out (about 2 s each), it stores device status 2 or 3 in the
+ * call's dev_status, and the kernel returns with outputs as described there; nothing hangs or traps, and the workspace may be used
+ * again.  The call must be given at least one active row. */
 int surelock_lose_next_copy(void);
 
 #ifdef __cplusplus

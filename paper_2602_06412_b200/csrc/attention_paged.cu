@@ -58,7 +58,7 @@ struct PagedAttnArgs {
   float2* ml;      // [grid][2][rows]
   float* part;     // [grid][2][rows][DH]
   int32_t* status;
-  int lost;        // bytes that CTA 0's first stage waits for in vain: 0, but for the diagnostic
+  int lost;        // bytes that the second CTA's first stage waits for in vain: 0, but for the diagnostic
 };
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar, uint64_t policy) {
@@ -363,7 +363,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         }
         if (!(ok = warp_wait(empty(st), ph ^ 1, s_abort))) break;
         const int n = __popc(__ballot_sync(0xffffffffu, have));
-        if (lane == 0) mbar_expect_tx(full(st), (uint32_t)(n * box * 2 * (T::ROW + (T::SCALED ? 4 : 0)) + (cnt == 0 && blockIdx.x == 0 ? a.lost : 0)));
+        if (lane == 0) mbar_expect_tx(full(st), (uint32_t)(n * box * 2 * (T::ROW + (T::SCALED ? 4 : 0)) + (cnt == 0 && blockIdx.x == (gridDim.x > 1) ? a.lost : 0)));
         __syncwarp();
         if (have) {
           const int x = t % a.page_size;
@@ -393,6 +393,13 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   }
 
   // ---- consumers ----
+  // A wait ran out.  Of an item that started in an earlier CTA, this one's piece becomes NaN, so that the rows do; the rows of the
+  // items that start here are not written.
+  auto give_up = [&](bool piece) {
+    if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
+    const float nan = __uint_as_float(0x7fffffffu);
+    if (piece && threadIdx.x < ROWS) a.ml[(long long)blockIdx.x * 2 * ROWS + threadIdx.x] = make_float2(nan, nan);
+  };
   const int g = lane >> 2, t = lane & 3;
   const uint32_t jkey = warp * 16;                 // this warp's keys in a unit
   unsigned cnt = 0;
@@ -589,7 +596,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         }
       }
       if (!epilogue_warps_agree(ok)) {
-        if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
+        give_up(blk0 > 0);
         return;
       }
       const bool starts = blk0 == 0, whole = starts && nblk == s.nb;
@@ -919,7 +926,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
           if (t == 0) sL[warp * ROWS + mt * 16 + g + 8 * h] = x;
         }
       if (!epilogue_warps_agree(ok)) {
-        if (threadIdx.x == 0) set_status(a.status, SL_DEV_ATTN_TIMEOUT);
+        give_up(blk0 > 0);
         return;
       }
       const bool starts = blk0 == 0, whole = starts && nblk == s.nb;

@@ -381,6 +381,10 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   const bool good = *s_abort == 0;
   if (warp < GQ_WARPS) {
     const int t = lane & 3, g = lane >> 2, rev = ((g & 1) << 2) | (g & 2) | (g >> 2);
+    if (!good) {                                              // an incomplete sum is NaN, for whichever CTA adds it
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = __uint_as_float(0x7fffffffu);
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -388,7 +392,7 @@ gemm_quantized_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         sRed[(j * 8 + 2 * t + (e & 1)) * P::PITCH + warp * 16 + (e >> 1) * 8 + rev] = acc[j][e];
   }
   if (S > 1) cluster_sync_all(); else __syncthreads();
-  if (M > 0 && good) {
+  if (M > 0) {
     const int c0 = (int)(TO / 4 * rank / S), cols = (int)(TO / 4 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
     for (int i = threadIdx.x; i < min(M, 8 * NT) * cols; i += GQ_THREADS) {
       const int r = i / cols, col = 4 * (c0 + i % cols);

@@ -409,11 +409,15 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_c
   }
   if (warp < GT_ADDERS) {
     const int feature = (warp & 3) * 32 + lane, quarter = warp >> 2;
+    if (!good) {                                              // an incomplete sum is NaN, for whichever CTA adds it
+#pragma unroll
+      for (int c = 0; c < HC; ++c) acc[c] = __uint_as_float(0x7fffffffu);
+    }
 #pragma unroll
     for (int c = 0; c < HC; ++c) sRed[(quarter * HC + c) * P::PITCH + feature] = acc[c];
   }
   if (S > 1) cluster_sync_all(); else __syncthreads();
-  if (M > 0 && good) {
+  if (M > 0) {
     const int c0 = (int)(TO / 4 * rank / S), cols = (int)(TO / 4 * (rank + 1) / S) - c0;   // features in fours that this CTA finishes
     for (int i = threadIdx.x; i < min(M, NP) * cols; i += P::THREADS) {
       const int r = i / cols, col = 4 * (c0 + i % cols);

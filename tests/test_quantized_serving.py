@@ -215,3 +215,35 @@ def test_no_wait_runs_to_its_limit_when_a_kernel_leaves(K):
         t[1].record()
         torch.cuda.synchronize()
         assert t[0].elapsed_time(t[1]) < 100
+
+
+@pytest.mark.parametrize("M,n,K,group,epilogue", [(5, 600, 4096, 64, 0), (13, 200, 1024, 32, 1), (29, 5003, 1024, 128, 2), (70, 200, 2048, 32, 1),
+                                                  (128, 300, 4096, 128, 0), (128, 300, 4096, 64, 2)])
+def test_no_feature_keeps_an_incomplete_sum(M, n, K, group, epilogue):
+    """K is split over CTAs whose sums meet: what the one that gave up was to contribute to is NaN, without a status too."""
+    W, _ = _weights(n, K, group, True, torch.float32, seed=1)
+    W2, _ = _weights(n, K, group, True, torch.float32, seed=2)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    out = lambda: torch.ones(M, n, dtype=torch.float32 if epilogue == 1 else torch.bfloat16, device=DEV)
+    call = lambda c: SL.surelock_gemm_quantized(A, W, c, _i32([M]), epilogue, W2 if epilogue == 2 else None)
+    want, got = out(), out()
+    call(want)
+    SL.surelock_lose_next_copy()
+    call(got)
+    rows, first = min(M, 64 if group == 32 else 128), 64 if epilogue == 2 else 128   # of a CTA
+    assert torch.all(torch.isnan(got[:rows, :first])) and torch.equal(got[:, first:], want[:, first:]) and torch.equal(got[rows:], want[rows:])
+
+
+@pytest.mark.parametrize("kind,rows", [(torch.int8, [1]), (torch.bfloat16, [1]), (torch.float8_e4m3fn, [12]), (torch.bfloat16, [13])])
+def test_no_row_keeps_an_incomplete_softmax(kind, rows):
+    """A long sequence whose pieces are joined: without one piece its rows are NaN, those of the other key head as they were."""
+    Hkv, dh, lens = 2, 128, [40000]
+    pool = Pool(kind, 1, lens[0], Hkv, dh, 256)
+    _fill(pool, lens, Hkv, dh)
+    offs = [0, rows[0]]
+    q = torch.randn(rows[0], Hkv, dh, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+    ws = torch.zeros(SL.surelock_attention_paged_workspace_bytes(dh), dtype=torch.uint8, device=DEV)
+    want = _attend(pool, q, offs, lens, ws=ws)
+    SL.surelock_lose_next_copy()
+    got = _attend(pool, q, offs, lens, ws=ws)                         # the workspace holds the pieces of the call before
+    assert torch.all(torch.isnan(got[:, 0])) and torch.equal(got[:, 1], want[:, 1])
