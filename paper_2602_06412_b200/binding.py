@@ -450,6 +450,8 @@ def surelock_attention(q, k_cache, v_cache, active_idx, row_offsets, n_active, B
 # ---- 4-bit weights ------------------------------------------------------------------------------------------
 def _w4(W, K: int):
     """The C struct of (codes uint8 [n_out][K/2], scales bf16 or fp32 [n_out][K/group], zeros uint8 [n_out][K/group] or None)."""
+    if len(W) != 3 or W[1].dim() != 2:
+        raise SurelockError("4-bit weights: (codes, scales, zeros or None) with scales [n_out][K/group] are wanted")
     codes, scales, zeros = W
     n, ng = shape = scales.shape
     if codes.dtype != torch.uint8 or codes.shape != (n, K // 2) or not ng or K % ng or \
@@ -477,6 +479,8 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
     """4-bit weights W = (codes, scales, zeros or None); epilogue 0: Cout (bf16) = A W^T; 1: Cout (fp32) += A W^T;
     2: Cout (bf16) = silu(A W^T) * (A W2^T).  workspace: uint8 CUDA tensor of surelock_gemm_quantized_workspace_bytes(M, K)
     bytes that no call running at the same time uses; None takes one from torch's allocator for this call."""
+    if A.dim() != 2:
+        raise SurelockError(f"surelock_gemm_quantized: A [M][K] is wanted, got {tuple(A.shape)}")
     M, K = A.shape
     w, n = _w4(W, K)
     w2 = None

@@ -294,3 +294,12 @@ def test_elements_off_their_alignment_are_refused():
         assert call(w(0x2000, t), w(at, t), 0x200, 2) == rc           # and of the second matrix
     for c, rc in [(0x202, -5), (0x201, -5), (0x204, 0)]:
         assert call(w(0x2000, SL.SL_BF16), None, c, 1) == rc
+
+
+def test_binding_refuses_other_numbers_of_dimensions():
+    A, C = torch.zeros(2, 128, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.bfloat16)
+    codes, scales, n = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, 2), torch.zeros(1, dtype=torch.int32)
+    for a, w, w2 in [(A, (codes, scales[:, 0], None), None), (A, (codes, scales[None], None), None), (A[0], (codes, scales, None), None),
+                     (A[None], (codes, scales, None), None), (A, (codes, scales), None), (A, (codes, scales, None), (codes, scales[0], None))]:
+        with pytest.raises(SL.SurelockError):
+            SL.surelock_gemm_quantized(a, w, C, n, epilogue=2 if w2 else 0, W2=w2)
