@@ -471,6 +471,13 @@ def _here(first, *others) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _word(t: Optional[torch.Tensor]):
+    """Address of the int32 status word, or None."""
+    if t is not None and (t.dtype != torch.int32 or not t.numel()):
+        raise SurelockError(f"dev_status: an int32 CUDA tensor is wanted, got {t.dtype} {tuple(t.shape)}")
+    return None if t is None else t.data_ptr()
+
+
 def surelock_gemm_quantized_workspace_bytes(max_rows: int, K: int) -> int:
     return lib().surelock_gemm_quantized_workspace_bytes(max_rows, K)
 
@@ -499,7 +506,7 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
     elif workspace.nbytes < need:
         raise SurelockError("surelock_gemm_quantized: workspace too small")
     _check(lib().surelock_gemm_quantized(_p(A), C.byref(w), C.byref(w2) if w2 is not None else None, _p(Cout), _ints(n_active, 1), M, n, K,
-                                         epilogue, _p(workspace), _p(dev_status), stream), "surelock_gemm_quantized")
+                                         epilogue, _p(workspace), _word(dev_status), stream), "surelock_gemm_quantized")
 
 
 def surelock_lose_next_copy():
@@ -564,7 +571,7 @@ def surelock_kv_scatter_paged(cache: PagedKV, k, v, active_idx, n_active, N: int
     stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
     if M:
         _check(lib().surelock_kv_scatter_paged(cache.ref, k.data_ptr(), v.data_ptr(), pitch, _ints(active_idx, M), _ints(n_active, 1), M,
-                                               cache.n_seq, N, _dt(k), _p(dev_status), stream), "surelock_kv_scatter_paged")
+                                               cache.n_seq, N, _dt(k), _word(dev_status), stream), "surelock_kv_scatter_paged")
 
 
 def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v, dev_status=None):
@@ -573,7 +580,7 @@ def surelock_kv_gather_paged(cache: PagedKV, active_idx, n_active, N: int, k, v,
     stream = _here(cache.k, k, v, active_idx, n_active, dev_status)
     if M:
         _check(lib().surelock_kv_gather_paged(cache.ref, _ints(active_idx, M), _ints(n_active, 1), M, cache.n_seq, N, k.data_ptr(),
-                                              v.data_ptr(), pitch, _dt(k), _p(dev_status), stream), "surelock_kv_gather_paged")
+                                              v.data_ptr(), pitch, _dt(k), _word(dev_status), stream), "surelock_kv_gather_paged")
 
 
 def surelock_attention_paged_workspace_bytes(head_dim: int) -> int:
@@ -592,5 +599,5 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
     stream = _here(cache.k, q, row_offsets, seq_lens, o, workspace, dev_status)
     if M:
         _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh)[1], _ints(row_offsets, B + 1), _ints(seq_lens, B), M, B, H,
-                                              o.data_ptr(), _rows(o, H, dh)[1], workspace.data_ptr(), _p(dev_status), stream),
+                                              o.data_ptr(), _rows(o, H, dh)[1], workspace.data_ptr(), _word(dev_status), stream),
                "surelock_attention_paged")

@@ -247,3 +247,20 @@ def test_no_row_keeps_an_incomplete_softmax(kind, rows):
     SL.surelock_lose_next_copy()
     got = _attend(pool, q, offs, lens, ws=ws)                         # the workspace holds the pieces of the call before
     assert torch.all(torch.isnan(got[:, 0])) and torch.equal(got[:, 1], want[:, 1])
+
+
+@pytest.mark.parametrize("status", [torch.zeros(1, dtype=torch.uint8), torch.zeros(1), torch.zeros(2, dtype=torch.int64), torch.zeros(0, dtype=torch.int32)])
+def test_a_status_that_is_not_an_int32_word_is_refused(status):
+    status = status.to(DEV)
+    pool = Pool(torch.int8, 1, 32, 1, 64, 16)
+    k = torch.randn(2, 1, 64, device=DEV)
+    q, ws = k.to(torch.bfloat16), torch.empty(SL.surelock_attention_paged_workspace_bytes(64), dtype=torch.uint8, device=DEV)
+    W, _ = _weights(40, 128, 64, False, torch.bfloat16, seed=1)
+    A, C = torch.zeros(2, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 40, dtype=torch.bfloat16, device=DEV)
+    for call in (lambda s: SL.surelock_kv_scatter_paged(pool.cache, k, k, _i32([0, 1]), _i32([2]), 32, s),
+                 lambda s: SL.surelock_kv_gather_paged(pool.cache, _i32([0, 1]), _i32([2]), 32, k, k.clone(), s),
+                 lambda s: SL.surelock_attention_paged(pool.cache, q, _i32([0, 2]), _i32([2]), q.clone(), ws, s),
+                 lambda s: SL.surelock_gemm_quantized(A, W, C, _i32([2]), dev_status=s)):
+        call(_i32([0]))
+        with pytest.raises(SL.SurelockError):
+            call(status)
