@@ -303,3 +303,86 @@ def test_binding_refuses_other_numbers_of_dimensions():
                      (A[None], (codes, scales, None), None), (A, (codes, scales), None), (A, (codes, scales, None), (codes, scales[0], None))]:
         with pytest.raises(SL.SurelockError):
             SL.surelock_gemm_quantized(a, w, C, n, epilogue=2 if w2 else 0, W2=w2)
+
+
+# ---- the same on both kernels: up to 16 rows, up to 32 of many features, and more ------------------------------------------
+KERNELS = [(13, 600), (20, 4800), (20, 600), (33, 200), (70, 200), (128, 130)]
+
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,n", KERNELS)
+def test_counts_replays_and_streams(M, n, group):
+    """Workspaces full of NaN (rows behind the count are not rewritten), counts that change between replays of one graph, and calls
+    on three streams at once, each with a workspace of its own."""
+    K = 1152
+    W, _ = _weights(n, K, group, True, torch.bfloat16, seed=9)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(10)).to(torch.bfloat16).to(DEV)
+    want = torch.zeros(M, n, dtype=torch.bfloat16, device=DEV)
+    _run(A, W, want, M, 0)
+    space = lambda: torch.full((SL.surelock_gemm_quantized_workspace_bytes(M, K),), 255, dtype=torch.uint8, device=DEV)
+    count, out, ws, status = torch.tensor([M], dtype=torch.int32, device=DEV), torch.zeros_like(want), space(), torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        SL.surelock_gemm_quantized(A, W, out, count, workspace=ws, dev_status=status)
+    for m in (M, 0, 1, M - 1, 9, M):
+        out.fill_(7.0)
+        ws.fill_(255)
+        count.fill_(m)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:m], want[:m]) and torch.all(out[m:] == 7.0)
+    streams, outs, spaces = [torch.cuda.Stream() for _ in range(3)], [torch.zeros_like(want) for _ in range(3)], [space() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, o, w in zip(streams, outs, spaces):
+            with torch.cuda.stream(s):
+                SL.surelock_gemm_quantized(A, W, o, count, workspace=w, dev_status=status)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs) and status.item() == 0
+
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,n", KERNELS)
+def test_rows_do_not_meet_in_either_kernel(M, n, group):
+    K = 640
+    W, _ = _weights(n, K, group, True, torch.bfloat16, seed=5)
+    A = torch.randn(M, K, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    D, E = (torch.empty(M, n, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    _run(A.to(DEV), W, D, M, 0)
+    B = A.clone()
+    B[3], B[M - 1, 7], B[5] = float("inf"), float("nan"), A[5] * 2.0 ** 100
+    _run(B.to(DEV), W, E, M, 0)
+    rest = [r for r in range(M) if r not in (3, 5, M - 1)]
+    assert torch.equal(D[rest], E[rest]) and torch.all(torch.isnan(E[M - 1])) and torch.all(torch.isnan(E[3]))
+    assert torch.equal(E[5].float(), D[5].float() * 2.0 ** 100)
+
+
+@gpu
+@pytest.mark.parametrize("most", [16, 128])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,n", KERNELS)
+def test_rows_with_a_common_mean(M, n, group, most):
+    """Where sum (u - z) a is small beside its two shares.  The kernel for few rows subtracts them: its roundings are relative to
+    sum |a| (u + z) s (the shares' chains are as long as those of the bound above).  The other takes z off the codes, exactly: to
+    sum |a| |u - z| s, and groups of codes at their zero point give an exact 0."""
+    K = 1152
+    (codes, scales, _), _ = _weights(n, K, group, False, torch.float32, seed=4)
+    g = torch.Generator().manual_seed(M)
+    z = torch.randint(0, most, (n, K // group), generator=g, dtype=torch.uint8)
+    codes, scales = codes.cpu(), scales.cpu()
+    z[0] = torch.randint(0, 16, z[0].shape, generator=g, dtype=torch.uint8)
+    codes[0] = (z[0] * 17).repeat_interleave(group // 2)              # feature 0: every code its zero point
+    u = torch.stack([codes & 15, codes >> 4], 2).reshape(n, -1, group).double().numpy()
+    s = scales.double().numpy()[..., None]
+    w, both = (((u - z.double().numpy()[..., None]) * s).reshape(n, K), ((u + z.double().numpy()[..., None]) * np.abs(s)).reshape(n, K))
+    A = (5 + 0.1 * torch.randn(M, K, generator=g)).to(torch.bfloat16)
+    a = A.double().numpy()
+    D = torch.zeros(M, n, device=DEV)
+    _run(A.to(DEV), (codes.to(DEV), scales.to(DEV), z.to(DEV)), D, M, 1)
+    want, few = a @ w.T, M <= 16 or (M <= 32 and n > 128 * 37)
+    d, tol = np.abs(D.cpu().double().numpy() - want), _tol(a, both if few else w, K, group) + 2.0 ** -24 * np.abs(want)
+    assert np.all(d <= tol), float((d / np.maximum(tol, 1e-30)).max())
+    assert few or torch.all(D[:, 0] == 0)

@@ -683,3 +683,38 @@ def test_row_offsets_of_any_value_are_clamped(offs, same):
     status = _i32([0])
     got = _attend(pool, q, offs, [64, 50], status)
     assert status.item() == 4 and torch.equal(got, _attend(pool, q, same, [64, 50]))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS[1:])
+def test_fp32_codes_next_to_borders_at_every_size(kind):
+    """Values up to two steps on both sides of every border between two codes, for largest magnitudes whose quotient by the
+    largest code is exact, rounded up and rounded down, on both sides of 2^-64, next to the largest fp32 number, and with subnormal scales."""
+    dh, Q = 128, QMAX[kind]
+    up, down = lambda x: np.nextafter(x, np.float32(np.inf)), lambda x: np.nextafter(x, np.float32(0))
+    f = np.float32
+    tops = [f(Q), f(Q * 1.5), f(Q * 2.0 ** -40), f(3.7), f(1.0), f(0.3), f(7.1), f(1e-5), f(12345.678), f(2.0 ** -64), up(f(2.0 ** -64)), down(f(2.0 ** -64)),
+            f(3e-20), f(6e-20), f(1e-30), f(1e-36), f(1e-37), f(3e-38), f(2.0 ** -130), f(1e38), down(f(np.inf)), f(2.0 ** 127)]
+    exact = [float(t) - Q * float(f(float(t) / Q)) for t in tops]
+    assert any(r == 0 for r in exact) and any(r > 0 for r in exact) and any(r < 0 for r in exact)
+    grid = np.arange(0, 128.0) if kind == torch.int8 else E4M3
+    rows = []
+    for amax in tops:
+        s = f(float(amax) / Q)
+        mid = ((grid[1:] + grid[:-1]) / 2 * np.float64(s)).astype(f)
+        vals = np.concatenate([mid, up(mid), down(mid), up(up(mid)), down(down(mid))])
+        vals = np.minimum(np.concatenate([vals, -vals]), amax)
+        x = np.zeros((-(-len(vals) // (dh - 1)), dh), f)
+        flat = np.zeros(len(x) * (dh - 1), f)
+        flat[: len(vals)] = vals
+        x[:, 0], x[:, 1:] = amax, flat.reshape(len(x), dh - 1)
+        rows.append(np.maximum(x, -amax))
+    x = np.concatenate(rows)[:, None]
+    n = len(x)
+    pool = Pool(kind, 1, n, 1, dh, 16)
+    k, v = torch.from_numpy(x).to(DEV), torch.from_numpy(x[::-1].copy()).to(DEV)
+    _write(pool, k, v, list(range(n)), n)
+    for t, p, sc in ((x, pool.k, pool.ks), (x[::-1], pool.v, pool.vs)):
+        code, scale = quantise(t.astype(np.float64), kind)
+        assert np.array_equal(pool.rows(sc, 0, n).astype(np.float32), scale)
+        assert np.array_equal(pool.rows(p, 0, n), code)
