@@ -461,8 +461,9 @@ int launch_gt(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
 // rows to a pass: with groups of 32 the accumulators of a step (four sets) leave room for 64
 template <int G, bool DUAL, bool FP32>
 int tc_rows(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
-  if (G == 32 || a.max_rows <= 64) return launch_gt<G, 64, DUAL, FP32>(w, a, epilogue, st);
-  return launch_gt<G, G == 32 ? 64 : 128, DUAL, FP32>(w, a, epilogue, st);
+  if constexpr (G != 32)
+    if (a.max_rows > 64) return launch_gt<G, 128, DUAL, FP32>(w, a, epilogue, st);
+  return launch_gt<G, 64, DUAL, FP32>(w, a, epilogue, st);
 }
 template <int G> int tc_kind(const CUtensorMap* w, const GqArgs& a, bool fp32, int epilogue, cudaStream_t st) {
   if (epilogue == EPI_SWIGLU) return fp32 ? tc_rows<G, true, true>(w, a, epilogue, st) : tc_rows<G, true, false>(w, a, epilogue, st);
