@@ -507,7 +507,7 @@ int surelock_kv_gather_paged(const surelock_paged_kv *cache, const int32_t *acti
  * parts are joined in a fixed order: results do not change from run to run.  Made for few rows per sequence (1 ... 128 /
  * (H / n_kv_heads)); more rows are correct but re-read the cache per 16 or 32 (row, head) pairs.  A bad page reads as
  * zeros (K = V = 0).  Scores, maxima, sums and outputs are accumulated in fp32; the weights enter the last product with 11
- * (SL_BF16 cache: 8) bits.  dev_status may be NULL; 3 = a bounded wait ran out, and the rows that this concerns are NaN or
+ * (SL_BF16 cache: 16) bits.  dev_status may be NULL; 3 = a bounded wait ran out, and the rows that this concerns are NaN or
  * not written.  Asynchronous on `stream`. */
 size_t surelock_attention_paged_workspace_bytes(int head_dim);
 int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int64_t q_stride, const int32_t *row_offsets,

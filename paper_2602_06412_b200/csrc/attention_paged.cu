@@ -30,7 +30,9 @@
 // Numerics: q becomes fp16 times a power of two per row (its largest magnitude in [1, 2)), the weight w_j = p_j sv_j becomes
 // fp16 under a power of two per row that follows the row's largest weight so far; both keep 11 bits, and weights below
 // 2^-33 of the largest vanish.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
-// weight outgrows its power of two.  With a bf16 cache q and p are bf16.
+// weight outgrows its power of two.  With a bf16 cache V cannot become fp16, so q is bf16 as it is and p two bf16 terms, p
+// rounded and what that left, of 16 bits together: with the first term alone (8 bits) the error of the result was a third above
+// that of its rounding to bf16.
 #include "paged_kv.cuh"
 #include "tc_common.cuh"
 
@@ -144,6 +146,13 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+// two values as bf16; what the rounding left of them takes their place
+__device__ __forceinline__ uint32_t take_bf16(float& a, float& b) {
+  const uint32_t w = pack_bf16(a, b);
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+  return w;
+}
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 // rows of a query tile: MT tiles of 16 as the 16-row operand of the products, or (MT = 0) 8 as their columns
@@ -180,7 +189,8 @@ constexpr int AP_OCC = 3;
 template <int DH, int KIND, int MT> struct Plan {
   using T = Tile<DH, KIND>;
   static constexpr int TILES = MT ? MT : 1;
-  static constexpr int EXCHANGE = MT ? MT * 4 * 512 : 4 * 8 * (DH + 4) * 4;   // weights, or the warps' results
+  static constexpr int TERMS = KIND == SL_BF16 ? 2 : 1;         // of a weight
+  static constexpr int EXCHANGE = MT ? TERMS * MT * 4 * 512 : 4 * 8 * (DH + 4) * 4;   // weights, or the warps' results
   static constexpr int FIXED = 1024 + TILES * T::STEPS * 512 + EXCHANGE + 16 * TILES * 4 * 9 + 256;   // Q, exchange, row factors, statistics
   static constexpr int ROOM = 228 * 1024 / AP_OCC - 1024 - 256 - FIXED;                             // 256: prefix sums of up to 31 sequences
   static constexpr int FIT = ROOM / T::STAGE;
@@ -268,7 +278,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* sStage = smem;
   uint4* sQ = reinterpret_cast<uint4*>(sStage + STAGES * T::STAGE);                         // [TILES][STEPS][32]
-  uint4* sP = sQ + TILES * T::STEPS * 32;                                                   // [TILES][4][32]
+  uint4* sP = sQ + TILES * T::STEPS * 32;                                                   // [terms][TILES][4][32]
   float* sJoin = reinterpret_cast<float*>(sP);                                              // [4][8][DH + 4]: MT = 0
   float* sRow = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(sP) + Plan<DH, KIND, MT>::EXCHANGE);   // [ROWS] factor of S
   float* sM = sRow + ROWS;                                                                  // [4][ROWS]
@@ -548,15 +558,17 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
           }
           // the weights to 16 bits, [key][row] -> [row][key]: the B operand of O^T += V^T P^T
           const float u0 = T::SCALED ? pow2i(AP_W_EXP - E[0]) : 1.f, u1 = T::SCALED ? pow2i(AP_W_EXP - E[1]) : 1.f;
-          const uint32_t p0 = transposed(BF ? pack_bf16(x[0], x[1]) : pack_f16(x[0] * u0, x[1] * u1));
-          const uint32_t p1 = transposed(BF ? pack_bf16(x[2], x[3]) : pack_f16(x[2] * u0, x[3] * u1));
+          const uint32_t p0 = transposed(BF ? take_bf16(x[0], x[1]) : pack_f16(x[0] * u0, x[1] * u1));
+          const uint32_t p1 = transposed(BF ? take_bf16(x[2], x[3]) : pack_f16(x[2] * u0, x[3] * u1));
           if (BF) {
+            const uint32_t r0 = transposed(pack_bf16(x[0], x[1])), r1 = transposed(pack_bf16(x[2], x[3]));
 #pragma unroll
             for (int c = 0; c < VT; ++c) {
               uint4 v;
               const uint32_t key = jkey + (lane >> 4) * 8 + (lane & 7), chunk = 2 * c + ((lane >> 3) & 1);
               ldsm_x4_t(vb + (chunk >> 3) * T::SLAB + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), reinterpret_cast<uint32_t*>(&v));
               mma16<BF>(acc[c], v, p0, p1);
+              mma16<BF>(acc[c], v, r0, r1);
             }
           } else {
             uint32_t v[4][VT / 2];                             // four keys, DH / 8 consecutive columns
@@ -851,15 +863,19 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         auto put_weights = [&]() {
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
-            uint32_t pr[4];
+            uint32_t pr[4], rest[4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float up = T::SCALED ? pow2i(AP_W_EXP - E[mt][h]) : 1.f;
 #pragma unroll
-              for (int n = 0; n < 2; ++n)
-                pr[2 * n + h] = BF ? pack_bf16(sc[mt][n][2 * h], sc[mt][n][2 * h + 1]) : pack_f16(sc[mt][n][2 * h] * up, sc[mt][n][2 * h + 1] * up);
+              for (int n = 0; n < 2; ++n) {
+                float &x = sc[mt][n][2 * h], &y = sc[mt][n][2 * h + 1];
+                pr[2 * n + h] = BF ? take_bf16(x, y) : pack_f16(x * up, y * up);
+                if (BF) rest[2 * n + h] = pack_bf16(x, y);
+              }
             }
             sP[(mt * 4 + warp) * 32 + lane] = make_uint4(pr[0], pr[1], pr[2], pr[3]);
+            if (BF) sP[((MT + mt) * 4 + warp) * 32 + lane] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
           }
         };
         put_weights();
@@ -882,6 +898,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) pa[mt] = sP[(mt * 4 + k) * 32 + lane];
           if (BF) {
+            uint4 pb[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) pb[mt] = sP[((MT + mt) * 4 + k) * 32 + lane];
 #pragma unroll
             for (int c = 0; c < NT; c += 2) {
               uint32_t v[4];
@@ -891,6 +910,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
               for (int mt = 0; mt < MT; ++mt) {
                 mma16<BF>(acc[mt][c], pa[mt], v[0], v[1]);
                 mma16<BF>(acc[mt][c + 1], pa[mt], v[2], v[3]);
+                mma16<BF>(acc[mt][c], pb[mt], v[0], v[1]);
+                mma16<BF>(acc[mt][c + 1], pb[mt], v[2], v[3]);
               }
             }
           } else {

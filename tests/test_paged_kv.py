@@ -718,3 +718,23 @@ def test_fp32_codes_next_to_borders_at_every_size(kind):
         code, scale = quantise(t.astype(np.float64), kind)
         assert np.array_equal(pool.rows(sc, 0, n).astype(np.float32), scale)
         assert np.array_equal(pool.rows(p, 0, n), code)
+
+
+# ---- weights of the last product ----------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("lens,rows,Hkv,G,tokens", [
+    ([2, 3, 4, 5, 6, 7, 8, 70], [2] * 8, 4, 4, 70),                   # tiles of 8 rows
+    ([2, 3, 5, 40], [16] * 4, 2, 1, 40),                              # of 16
+    ([2, 3, 5, 7, 300], [32] * 5, 8, 1, 2048),                        # of 32
+])
+def test_attention_over_bf16_pages_keeps_sixteen_bits_of_a_weight(dh, lens, rows, Hkv, G, tokens):
+    """Few keys of either sign, so that results are small beside sum p |v|: the weights enter the product as two bf16 terms, the
+    second off by half a step (2^-8) of a residual of at most half a step (2^-8) of the weight."""
+    pool = Pool(torch.bfloat16, len(lens), tokens, Hkv, dh, 64)
+    _fill(pool, lens, Hkv, dh, seed=dh)
+    offs = [0] + np.cumsum(rows).tolist()
+    q = torch.randn(offs[-1], Hkv * G, dh, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    got = _attend(pool, q, offs, lens)
+    o, A = _want(pool, q.cpu().double().numpy(), offs, lens, G)
+    _near(got, o, A * (2.0 ** -16 + 2.0 ** -12) / (2.0 ** -8 + 2.0 ** -12), pool.kind)
