@@ -29,10 +29,12 @@
 // the columns of O so that it reads neighbouring bytes of a value row; two keys' bytes are interleaved by byte permutes.
 // Numerics: q becomes fp16 times a power of two per row (its largest magnitude in [1, 2)), the weight w_j = p_j sv_j becomes
 // fp16 under a power of two per row that follows the row's largest weight so far; both keep 11 bits, and weights below
-// 2^-33 of the largest vanish.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
+// 2^-33 of the largest vanish.  For w that is a choice: the results' error against the definition is 1 % above that of their own
+// rounding to bf16 (0.00168 against 0.00166, relative to the values), and a second fp16 term for what the first leaves cost 3 to 11 %
+// for single tokens, 12 % for 16 rows, 19 % for 32.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
 // weight outgrows its power of two.  With a bf16 cache V cannot become fp16, so q is bf16 as it is and p two bf16 terms, p
-// rounded and what that left, of 16 bits together: with the first term alone (8 bits) the error of the result was a third above
-// that of its rounding to bf16.
+// rounded and what that left, of 16 bits together: with the first term alone (8 bits) the error was a third above that of the
+// results' rounding (0.0022 against 0.0017; 5 sequences of 33 rows and 64 columns 17.8 us with one term, 19.0 with two).
 #include "paged_kv.cuh"
 #include "tc_common.cuh"
 
