@@ -410,7 +410,7 @@ template <int G, int NT, bool DUAL, bool FP32>
 int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
   using P = GqPlan<G, NT>;
   constexpr int TO = DUAL ? 64 : 128;
-  const int tiles = (a.n_out + TO - 1) / TO, nblk = (a.K + GQ_BK - 1) / GQ_BK;
+  const int tiles = (a.n_out - 1) / TO + 1, nblk = (a.K - 1) / GQ_BK + 1;
   // K is split over S CTAs of a cluster while the CTAs still fit the GPU at once
   const long long slots = (long long)sm_count() * P::OCC;
   int S = 1;

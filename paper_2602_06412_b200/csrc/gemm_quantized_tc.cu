@@ -435,12 +435,12 @@ template <int G, int NP, bool DUAL, bool FP32>
 int launch_gt(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t st) {
   using P = GtPlan<G, NP>;
   constexpr int TO = DUAL ? 64 : 128;
-  const int nblk = (a.K + GQ_BK - 1) / GQ_BK;
+  const int tiles = (a.n_out - 1) / TO + 1, nblk = (a.K - 1) / GQ_BK + 1;
   CUtensorMap rows;
   const int rc = gq_map(&rows, a.rows, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, a.max_rows, (long long)nblk * GQ_BK, NP, 64);
   if (rc != SL_OK) return rc;
   // the split of K with the least estimated time: rounds of CTAs (one per SM) times (stages of one + two stages' time to start and join)
-  const long long work = (long long)((a.n_out + TO - 1) / TO) * ((a.max_rows + NP - 1) / NP);
+  const long long work = (long long)tiles * ((a.max_rows + NP - 1) / NP);
   int S = 1;
   long long best = 0;
   for (int s = 1; s <= 8 && s <= nblk; ++s) {
@@ -453,7 +453,7 @@ int launch_gt(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
   auto kernel = gemm_quantized_tc_kernel<G, NP, DUAL, FP32>;
   static std::atomic<uint64_t> allowed{0};
   SL_CUDA_TRY(allow_smem(kernel, P::SMEM, allowed));
-  const dim3 grid((a.n_out + TO - 1) / TO * S, (a.max_rows + NP - 1) / NP);
+  const dim3 grid(tiles * S, (a.max_rows + NP - 1) / NP);
   SL_CUDA_TRY(gq_launch(kernel, grid, P::THREADS, P::SMEM, S, st, w[0], w[1], rows, a, epilogue));
   return SL_OK;
 }

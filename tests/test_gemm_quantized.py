@@ -386,3 +386,39 @@ def test_rows_with_a_common_mean(M, n, group, most):
     d, tol = np.abs(D.cpu().double().numpy() - want), _tol(a, both if few else w, K, group) + 2.0 ** -24 * np.abs(want)
     assert np.all(d <= tol), float((d / np.maximum(tol, 1e-30)).max())
     assert few or torch.all(D[:, 0] == 0)
+
+
+# ---- far ends -----------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("M,n,K,group", [(9, 70, 640, 64), (40, 70, 640, 128), (100, 33, 320, 32)])
+@pytest.mark.parametrize("power", [-133, -126, -100, 100, 112])
+def test_rows_of_any_magnitude_are_exact(M, n, K, group, power):
+    """Whole numbers up to 4 times a power of two, down to subnormal bf16 rows and fp32 results: |sum| < 2^15 quarters, so every
+    result is a number of fp32 and the powers only move its exponent."""
+    W, w = _weights(n, K, group, True, torch.float32, seed=M, exact=True)
+    a = torch.randint(-4, 5, (M, K), generator=torch.Generator().manual_seed(M)).double()
+    a[1] = 0
+    D = torch.zeros(M, n, device=DEV)
+    _run((a * 2.0 ** power).to(torch.bfloat16).to(DEV), W, D, M, 1)
+    assert np.array_equal(D.cpu().double().numpy(), (a.numpy() @ w.T) * 2.0 ** power)
+
+
+@gpu
+@pytest.mark.parametrize("M,n,K,group", [(1, 2 ** 31 - 1, 32, 32), (2, 150001, 40960, 128), (33, 150001, 40960, 64)])
+def test_codes_beyond_32_bits(M, n, K, group):
+    """More than 2^31 bytes of codes, and the most features there can be: the first, the last and some features between."""
+    at = [0, 1, 127, 128, n // 2, n // 2 + 5, n - 130, n - 2, n - 1]
+    W, w = _weights(len(at), K, group, True, torch.bfloat16, seed=3, exact=True)
+    codes = torch.zeros(n, K // 2, dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(n, K // group, dtype=torch.bfloat16, device=DEV)
+    zeros = torch.zeros(n, K // group, dtype=torch.uint8, device=DEV)
+    for i, f in enumerate(at):
+        codes[f], scales[f], zeros[f] = W[0][i], W[1][i], W[2][i]
+    a = torch.randint(-4, 5, (M, K), generator=torch.Generator().manual_seed(4))
+    a[:, 4096:] = 0                                                   # so that the whole numbers stay exact
+    D = torch.full((M, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    _run(a.to(torch.bfloat16).to(DEV), (codes, scales, zeros), D, M, 0)
+    want = torch.from_numpy(a.double().numpy() @ w.T).float().to(torch.bfloat16)
+    assert torch.equal(torch.stack([D[:, f] for f in at], 1).cpu(), want)
+    D[:, torch.tensor(at, device=DEV)] = 0
+    assert not D.any()
