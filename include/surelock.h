@@ -499,7 +499,7 @@ int surelock_kv_gather_paged(const surelock_paged_kv *cache, const int32_t *acti
  * over the sequence's cached tokens; no mask besides the length.  seq_lens[b] = 0 gives rows of zeros; scores that are all -inf
  * give NaN, as 0 / 0 does.
  *   q, o         dev bf16, row r at r * q_stride / o_stride elements (multiples of 8), heads packed [H][head_dim]
- *   row_offsets  dev int32 [B + 1], seq_lens dev int32 [B] (0 ... max_pages * page_size); a value out of range is clamped to
+ *   row_offsets  dev int32 [B + 1], ascending, seq_lens dev int32 [B] (0 ... max_pages * page_size); a value out of range is clamped to
  *                it and stores device status 4; rows behind row_offsets[B] are left as they are
  *   workspace    dev, surelock_attention_paged_workspace_bytes(head_dim) bytes, any contents, 16-byte aligned; holds partial
  *                results during the call only, so calls (and captured graphs) that may run at the same time need one each

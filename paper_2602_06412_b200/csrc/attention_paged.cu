@@ -21,20 +21,21 @@
 //              16 keys each (a tile of 16 rows is an eighth of a tcgen05 tile), exp2, the weights into shared memory as the A
 //              fragments they already are; then O += P V for a quarter of the columns each, over all 64 keys.  Codes become
 //              fp16, exactly, in registers on the way to the products.
-// Measured (a plain copy: 6.57 TB/s): one new token each, 4 x 16384 tokens of 32 key heads in e4m3 85 us (6.5 TB/s), 32
-// ragged sequences of up to 4099 tokens of 8 key heads 38 us (5.4 TB/s); 8 x 4096 tokens in bf16 84 us (6.4 TB/s); 16 rows each,
-// 4 x 8192 tokens in e4m3 64 us, 32 rows each 97 us: there the products and the conversions bound it; 23 rows of one sequence
-// of 512 tokens 10 us, launches and waits.
+// Measured in replayed graphs (a plain copy: 6.57 TB/s): one new token each, 4 x 16384 tokens of 32 key heads in e4m3 85 us (6.5 TB/s), 32
+// ragged sequences of up to 4099 tokens of 8 key heads 38 us (5.4 TB/s); 8 x 4096 tokens in bf16 87 us (6.2 TB/s); 16 rows each,
+// 4 x 8192 tokens in e4m3 64 us, 32 rows each 92 us: there the products and the conversions bound it; 23 rows of one sequence
+// of 512 tokens 11 us, launches and waits.
 // The contraction index is permuted (the same way for Q and K) so that a lane reads its share of a key as 16-byte loads, and
 // the columns of O so that it reads neighbouring bytes of a value row; two keys' bytes are interleaved by byte permutes.
 // Numerics: q becomes fp16 times a power of two per row (its largest magnitude in [1, 2)), the weight w_j = p_j sv_j becomes
 // fp16 under a power of two per row that follows the row's largest weight so far; both keep 11 bits, and weights below
-// 2^-33 of the largest vanish.  For w that is a choice: the results' error against the definition is 1 % above that of their own
-// rounding to bf16 (0.00168 against 0.00166, relative to the values), and a second fp16 term for what the first leaves cost 3 to 11 %
-// for single tokens, 12 % for 16 rows, 19 % for 32.  S, the statistics and O are fp32.  O is rescaled when a maximum grows by more than 2^6 or a
-// weight outgrows its power of two.  With a bf16 cache V cannot become fp16, so q is bf16 as it is and p two bf16 terms, p
-// rounded and what that left, of 16 bits together: with the first term alone (8 bits) the error was a third above that of the
-// results' rounding (0.0022 against 0.0017; 5 sequences of 33 rows and 64 columns 17.8 us with one term, 19.0 with two).
+// 2^-33 of the largest vanish.  For w that is a choice: the results' error against the definition is 1 % above that of their
+// own rounding to bf16 (0.00168 against 0.00166, relative to the values), and a second fp16 term for what the first leaves cost
+// 1 to 11 % for single tokens, 12 % for 16 rows, 19 % for 32.  S, the statistics and O are fp32.  O is rescaled when a maximum
+// grows by more than 2^6 or a weight outgrows its power of two.  With a bf16 cache V cannot become fp16, so q is bf16 as it is and
+// p two bf16 terms, p rounded and what that left, of 16 bits together: with the first term alone (8 bits) the error was a third
+// above that of the results' rounding (0.0022 against 0.0017; 5 sequences of 33 rows and 64 columns 17.8 us with one term, 19.0
+// with two).
 #include "paged_kv.cuh"
 #include "tc_common.cuh"
 
@@ -1000,9 +1001,11 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
 // The pieces of an item that run borders cut: o = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m), in unit order.  CTA
 // (c, y) has the item that starts in run c.
 //
-// Few pieces (at most 16): a warp per row, 32 rows at once over the grid's 4 y; lane i has the statistics of piece i, and the
+// Few pieces (at most 16; at most 32 would fit the lanes): a warp per row, 32 rows at once over the grid's 4 y; lane i has the statistics of piece i, and the
 // pieces' values are requested together with them.  (An item that was cut has keys: a sum of 0 means that all scores are -inf, and
 // gives NaN.)
+// (int8, 16 rows, 8 heads, a warp per row against the way below: 8 pieces 8.2 and 12.5 us in all, 16 pieces 9.2 and 13.1; 32 pieces
+// 11.5 and 15.0 with 16 rows, but 9.6 and 9.2 with one.)
 template <int DH, int ROWS> __device__ __forceinline__ void join_few(const PagedAttnArgs& a, const int4& d, int n) {
   constexpr int PER = DH / 32, LOADS = 8;
   const int valid = d.z >> 16, kvh = d.z & 0xffff, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;

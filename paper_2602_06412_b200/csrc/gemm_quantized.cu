@@ -30,8 +30,12 @@
 // The first codes are requested before the rewriting kernel has finished: it does not write them.  K is split over the CTAs
 // of a cluster when the features alone do not fill the GPU; the sums meet through distributed shared memory in a fixed
 // order: deterministic.  All waits are bounded.
-// Measured, 1 / 8 / 16 rows: 4096 x 4096 6.6 / 7.0 / 8.1 us, 4096 x 12288 12.5 / 12.9 / 15.9, gate and up 12288 x 4096 with SwiGLU
-// 17.6 / 18.1 / 20.7 (23 rows 26.6), 126464 x 4096 55 / 55.5 / 70 (4.9 TB/s).  About 5 us of each are start, rewriting and join.
+// Measured in replayed graphs (calls made one by one take 6 - 7 us more, the host's part), 1 / 8 / 16 rows: 4096 x 4096
+// 6.6 / 7.0 / 8.1 us, 4096 x 12288 12.5 / 12.9 / 15.9, gate and up 12288 x 4096 with SwiGLU 17.6 / 18.1 / 20.7 (23 rows 26.6),
+// 126464 x 4096 55 / 55.5 / 70 (4.9 TB/s).  About 5 us of each are start, rewriting and join.
+// 288 threads and three CTAs per SM leave 72 registers to a thread: every instance but those for 8 rows in groups of 32 without
+// SwiGLU spills, 4 to 96 bytes (about 150 for 32 rows in groups of 32 with SwiGLU, 64 for the 23 rows above).  With four warps of 32
+// features, which read every row fragment half as often, the 23 rows took 25.7 us, but one row of the same matrices 23.5.
 #include "gemm_quantized.cuh"
 
 namespace sl {
@@ -411,7 +415,9 @@ int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
   using P = GqPlan<G, NT>;
   constexpr int TO = DUAL ? 64 : 128;
   const int tiles = (a.n_out - 1) / TO + 1, nblk = (a.K - 1) / GQ_BK + 1;
-  // K is split over S CTAs of a cluster while the CTAs still fit the GPU at once
+  // K is split over S CTAs of a cluster while the CTAs still fit the GPU at once.  Unsplit / at most 4 / at most 8 / up to two rounds
+  // of CTAs, 8 rows: 4096 x 4096 14.3 / 8.0 / 7.6 / 7.6 us, 4096 x 12288 35.8 / 14.1 / 13.0 / 12.9, gate and up 12288 x 4096 20.9 /
+  // 19.3 / 19.3 / 24.2; 24 rows of these 34.2 / 28.5 / 28.3 / 34.0.
   const long long slots = (long long)sm_count() * P::OCC;
   int S = 1;
   while (S < 8 && S < nblk && (long long)tiles * (S + 1) <= slots) ++S;
@@ -423,9 +429,15 @@ int launch_gq(const CUtensorMap* w, const GqArgs& a, int epilogue, cudaStream_t 
 }
 
 // Whether the kernel for few rows takes the call.  From 17 rows on its products bound it, where the weights are so few that the
-// other kernel works on all of them at once, with a quarter of the k or less to a CTA (K = 12288, 4096 features: 24.7 against
-// 20.1 us for 23 rows, 15.9 against 20.1 for 16); with more of them its fixed cost counts per round of CTAs (K = 4096, gate
-// and up matrices of 12288 features: 26.7 against 42 us).
+// other kernel works on all of them at once, with a quarter of the k or less to a CTA (K = 12288, 4096 features: 25.0 against
+// 21.5 us for 24 rows, 15.9 against 20.1 for 16); with more of them its fixed cost counts per round of CTAs (K = 4096, gate
+// and up matrices of 12288 features: 28.5 against 42.4 us).  K = 4096, 17 / 24 / 32 rows, this kernel against the other:
+//   1000 features 7.8 / 7.8 / 8.9 against 8.0 / 8.6 / 8.6     5120  11.7 / 12.1 / 15.8 against 12.9 / 13.0 / 13.1
+//   2048          9.2 / 9.4 / 11.7 against 14.3 / 14.8 / 15.0  6144  12.1 / 12.5 / 21.9 against 22.1 / 22.3 / 22.5
+//   4096          9.6 / 11.9 / 15.6 against 10.9 / 10.9 / 11.1 8192  13.9 / 15.4 / 19.7 against 15.4 / 15.2 / 15.4
+//   4736          11.7 / 11.9 / 15.8 against 18.8 / 18.6 / 19.3 12288 16.6 / 17.0 / 20.9 against 33.4 / 33.8 / 33.4
+// So the border is right on average; it loses where the other kernel's split of K comes out badly (2048 and 4736 features) and
+// for 32 rows of 5120 or 8192.
 constexpr int GQ_FEW = 32;             // most rows of the kernel for few rows
 bool gq_few(int max_rows, int n_out, int epilogue) {
   const int tiles = (n_out - 1) / (epilogue == EPI_SWIGLU ? 64 : 128) + 1;

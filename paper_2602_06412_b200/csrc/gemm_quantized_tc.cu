@@ -8,7 +8,7 @@
 // multiply-add less per element and group); the rows are the N operand, by TMA.  Every group's accumulator (128 features x
 // rows) is read back and takes one multiply-add per element.  What bounds it: the chain unpack -> product -> add, some 1200
 // clocks per 128 k, each satisfied wait of it 100 - 150; at 128 rows also the rows that every CTA reads from L2 (9 TB/s).
-// Measured: 4096 x 12288 in groups of 64, 128 rows 29 us, 64 rows 22 us; 4096 x 4096 13 and 11 us; gate and up 12288 x 4096 with
+// Measured in replayed graphs: 4096 x 12288 in groups of 64, 128 rows 29 us, 64 rows 22 us; 4096 x 4096 13 and 11 us; gate and up 12288 x 4096 with
 // SwiGLU 50 and 43 us; 126464 x 4096 163 and 136 us.
 //   warps 0-15  add up: feature 32 (w % 4) + lane, w / 4 = quarter of the rows
 //   4 or 8      unpack: feature 32 (w % 4) + lane (16 warps that did both: 192 against 166 us, 128 rows of the 4096 x 126464

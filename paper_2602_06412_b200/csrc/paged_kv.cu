@@ -20,7 +20,9 @@
 // Memory-bound: DH / 8 lanes take one (row, head) of K and of V, 8 elements a lane in 16-byte loads, all loads issued before
 // the first use; the 8-byte stores of a half-warp (DH = 128) fill one 128-byte line, as one head's places in a page are
 // contiguous.  Index chain (position -> page table -> slot) runs under the data loads.
-// Measured: 12288 rows of 32 heads from bf16 to e4m3 51 us (6.0 TB/s), 6144 rows from int8 to bf16 29 us (5.2 TB/s).
+// Measured in replayed graphs, 32 heads of 128: 12288 rows written from bf16 to e4m3 / int8 / bf16 pages 52 / 53 / 62 us (5.9 / 5.7 / 6.5
+// TB/s), from fp32 82 / 84 / 89 us (6.2 / 6.0 / 6.8 TB/s); 6144 rows read back to bf16 27 / 29 / 33 us (5.6 / 5.2 / 6.0 TB/s), to fp32 56 / 58 /
+// 59 us (4.5 / 4.3 / 5.2 TB/s).  Calls made one by one take 5 - 6 us more.
 #include "paged_kv.cuh"
 
 namespace sl {
