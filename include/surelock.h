@@ -518,7 +518,7 @@ int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int6
  * surelock_attention_paged that this thread launches, one CTA (the product's first, the attention's second if there is one)
  * waits for 16 bytes that are never copied.  Its bounded waits run out (about 2 s each), it stores device status 2 or 3 in the
  * call's dev_status, and the kernel returns with outputs as described there; nothing hangs or traps, and the workspace may be used
- * again.  The call must be given at least one active row. */
+ * again.  The call must be given at least one active row; captured into a graph, every replay waits so. */
 int surelock_lose_next_copy(void);
 
 #ifdef __cplusplus

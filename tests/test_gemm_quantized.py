@@ -422,3 +422,5 @@ def test_codes_beyond_32_bits(M, n, K, group):
     assert torch.equal(torch.stack([D[:, f] for f in at], 1).cpu(), want)
     D[:, torch.tensor(at, device=DEV)] = 0
     assert not D.any()
+    del codes, scales, zeros, D
+    torch.cuda.empty_cache()                                          # some 40 GB, which later tests need not find taken
