@@ -311,11 +311,9 @@ def run(state):
         SL.surelock_rope(s["rope"], s["q"], s["k"], s["pos"], s["n"], q_out=s["q_out"], k_out=s["k_out"])
         return dict(q=s["q_out"], k=s["k_out"])
     if c["op"] == "adapters":
-        if "adapters" not in s:    # the handle of the pool, and the workspace, that a program keeps
+        if "adapters" not in s:    # the handle of the pool that a program keeps
             s["adapters"] = SL.Adapters(s["a"], s["b"], s["scale"], s["ranks"])
-            need = SL.surelock_gemm_adapters_workspace_bytes(s["x"].shape[0], c["rank"])
-            s["workspace"] = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
-        SL.surelock_gemm_adapters(s["x"], s["adapters"], s["which"], s["offsets"], s["y"], workspace=s["workspace"])
+        SL.surelock_gemm_adapters(s["x"], s["adapters"], s["which"], s["offsets"], s["y"])
         return s["y"]
     if "sampling" not in s:    # the settings of the requests that a program keeps
         s["sampling"] = SL.Sampling(s["temperature"], s["top_k"], s["top_p"], s["min_p"])
