@@ -514,6 +514,127 @@ int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int6
                              const int32_t *seq_lens, int max_rows, int B, int H, void *o, int64_t o_stride, void *workspace,
                              int32_t *dev_status, void *stream);
 
+/* ---- a served batch on the paged cache: from request lengths to tokens -------------------------------------------------
+ * The work between the products and the attention of a step that serves many requests. */
+
+/* Pages, rows and positions for new tokens.  Sequence b of seq_lens[b] cached tokens gets new_tokens[b] more and, for them,
+ *   ceil((seq_lens + new_tokens) / page_size) - ceil(seq_lens / page_size)
+ * pages off the end of the free list: the j-th page handed out by the call is free_pages[*n_free - 1 - j], in the order of
+ * sequences and, within one, of tokens.  First come, first served: a sequence gets all its tokens, or none where they pass its
+ * table's width, or its rows and those of all sequences before it that fit their tables pass max_rows, or it needs pages and those
+ * wanted up to and with it are more than *n_free.
+ *   page_table    dev int32 [B][max_pages], in place: only the new pages are written
+ *   seq_lens      dev int32 [B], seq_lens_out dev int32 [B]: lengths before and with the new tokens; may be the same array
+ *   free_pages    dev int32 [n_pages], read only; n_free, n_free_out dev int32 [1]: pages on the list before and after; may be the same
+ *   row_offsets   dev int32 [B + 1], n_active dev int32 [1]: the packing of the tokens that were granted
+ *   active_idx    dev int32 [max_rows]: flat positions b*N + i of the rows, N = max_pages * page_size, as surelock_kv_scatter_paged
+ *                 takes them; entries behind *n_active are left as they are
+ * page_size as in surelock_paged_kv; B <= 1024 and B*N < 2^31 (SL_EUNSUPPORTED otherwise).  A negative count, a length or a free
+ * count out of range is clamped, a page outside 0 ... n_pages - 1 is handed out as it is: both store device status 4.  One launch;
+ * asynchronous on `stream`; may be captured. */
+int surelock_paged_extend(int32_t *page_table, int B, int page_size, int max_pages, int n_pages, const int32_t *seq_lens,
+                          const int32_t *new_tokens, const int32_t *free_pages, const int32_t *n_free, int32_t *row_offsets,
+                          int32_t *active_idx, int32_t *n_active, int max_rows, int32_t *seq_lens_out, int32_t *n_free_out,
+                          int32_t *dev_status, void *stream);
+
+/* The way back: sequence b is cut to min(seq_lens[b], keep[b]) tokens (0: it has ended), and the pages that hold none of the
+ * rest go to the end of the free list, in the order of sequences and, within one, of tokens.  page_table is read only (entries behind
+ * a sequence's last token mean nothing).  A page that is on the tables of several sequences must be given back by one of
+ * them only.  Pages beyond the list's n_pages places are dropped (device status 4).  Otherwise as above. */
+int surelock_paged_truncate(const int32_t *page_table, int B, int page_size, int max_pages, int n_pages, const int32_t *seq_lens,
+                            const int32_t *keep, int32_t *free_pages, const int32_t *n_free, int32_t *seq_lens_out,
+                            int32_t *n_free_out, int32_t *dev_status, void *stream);
+
+/* Rotary positions.  Pair i < rotary_dim / 2 of a head, elements (i, i + rotary_dim / 2) or, interleaved, (2i, 2i + 1), turns by the
+ * angle position * freq[i] and is multiplied by scale; elements from rotary_dim on are copied.
+ *   freq   dev fp64 [rotary_dim / 2], e.g. from surelock_rope_frequencies */
+typedef struct {
+  const double *freq;
+  int32_t rotary_dim, interleaved;
+  float scale;
+} surelock_rope_cfg;
+
+/* Frequencies for contexts longer than a model was trained on.  With f = factor, L = original_len, D = rotary_dim:
+ *   SL_ROPE_PLAIN   theta^(-2i/D)
+ *   SL_ROPE_LINEAR  divided by f (positions are interpolated)
+ *   SL_ROPE_NTK     theta replaced by theta f^(D/(D-2))
+ *   SL_ROPE_YARN    divided by f for pairs from `high` on, kept up to `low`, a line in between, where low (high) is the floor (ceiling) of
+ *                   the pair that makes `fast` (`slow`) turns over L tokens; scale = attn_scale, or 0.1 ln f + 1 where that is 0
+ *   SL_ROPE_BANDS   kept where L tokens make at least `fast` turns, divided by f at most `slow`, a line in the number of turns in between
+ */
+enum { SL_ROPE_PLAIN = 0, SL_ROPE_LINEAR = 1, SL_ROPE_NTK = 2, SL_ROPE_YARN = 3, SL_ROPE_BANDS = 4 };
+typedef struct {
+  int32_t kind;
+  double factor, original_len, fast, slow, attn_scale;
+} surelock_rope_scaling;
+
+/* Host function: freq_out HOST fp64 [rotary_dim / 2] and *scale_out for a surelock_rope_cfg; scaling NULL = plain.  rotary_dim even, > 2 with
+ * SL_ROPE_NTK; theta > 1; factor > 0; with SL_ROPE_YARN and SL_ROPE_BANDS original_len > 0 and fast > slow > 0. */
+int surelock_rope_frequencies(int rotary_dim, double theta, const surelock_rope_scaling *scaling, double *freq_out, float *scale_out);
+
+/* Rotates packed rows r < *n_active of q [M][H][head_dim] and, where k is not NULL, k [M][n_kv_heads][head_dim], of `dtype` SL_BF16 or
+ * SL_FP32, row r at r * stride elements with its heads packed, into q_out and k_out (which may be q and k with their strides, for a
+ * call in place; otherwise they do not overlap them).  The position of row r is positions[r], or positions[r] % N with N > 0 (flat
+ * positions b*N + i).  A negative one leaves the row as it is (device status 4).  transposed: the rotation by -angle, with the same scale: the
+ * gradient, and for scale 1 the inverse.  Angles are exact to 2^-53 of themselves at any position; products are fp32, rounded once.
+ * Any head_dim, an even rotary_dim <= head_dim; 16-byte accesses where pointers, strides, head_dim and rotary_dim / 2 allow them, element by
+ * element otherwise.  dev_status may be NULL.  Asynchronous on `stream`. */
+int surelock_rope(const surelock_rope_cfg *cfg, const void *q, int64_t q_stride, int H, const void *k, int64_t k_stride, int n_kv_heads,
+                  int head_dim, const int32_t *positions, int N, const int32_t *n_active, int max_rows, void *q_out,
+                  int64_t q_out_stride, void *k_out, int64_t k_out_stride, int dtype, int transposed, int32_t *dev_status,
+                  void *stream);
+
+/* Low-rank adapters of many requests beside a shared projection of surelock_gemm, surelock_gemm_fused or surelock_gemm_quantized: for the packed rows
+ * row_offsets[b] <= r < row_offsets[b + 1] of sequence b, with a = adapter_of_seq[b] (negative: none),
+ *   C[r] += scale[a] B_a (A_a x_r)
+ *   a      dev bf16 [n_adapters][max_rank][K]        b     dev bf16 [n_adapters][n_out][max_rank]
+ *   scale  dev fp32 [n_adapters]                     ranks dev int32 [n_adapters] or NULL: rows of a, columns of b from there on
+ *                                                    are not used, whatever they hold */
+typedef struct {
+  const void *a, *b;
+  const float *scale;
+  const int32_t *ranks;
+  int32_t n_adapters, max_rank;
+} surelock_adapters;
+
+/* x: dev bf16 [M][K] packed; C: dev [M][n_out] of `dtype` SL_BF16 or SL_FP32 (the residual stream), row r at r * c_stride elements, so it
+ * may be a part of a wider row.  row_offsets dev int32 [B + 1], ascending, clamped to 0 ... max_rows (device status 4, as for an adapter or a
+ * rank out of range; such an adapter is none).  Rows of no sequence are left as they are.  K and max_rank multiples of 8, max_rank <= 128,
+ * x, a, b 16-byte aligned (SL_EUNSUPPORTED otherwise); any n_out, c_stride and alignment of C to its elements.  A_a x is summed in fp32 and
+ * enters the second product as an fp32 number (as one of 17 bits for a bf16 C); C is rounded once.  Deterministic; no workspace; one launch;
+ * asynchronous on `stream`. */
+int surelock_gemm_adapters(const void *x, const surelock_adapters *adapters, const int32_t *adapter_of_seq, const int32_t *row_offsets, int B,
+                           void *C, int64_t c_stride, int max_rows, int n_out, int K, int dtype, int32_t *dev_status, void *stream);
+
+/* Settings of sampled requests, n_sets of them: dev arrays [n_sets], each of which may be NULL (temperature 1, no filter).
+ *   temperature  >= 0; 0 takes the largest logit (lowest index on ties).  Negative or NaN: the row is undefined, see below
+ *   top_k        keeps the k largest; <= 0: all
+ *   top_p        keeps, of those, the fewest largest whose weights sum to at least top_p of theirs; not below 1 (or NaN): all
+ *   min_p        keeps those of at least min_p times the largest one's weight; not above 0 (or NaN): all; above 1 counts as 1 */
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  int32_t n_sets;
+} surelock_sampling;
+
+/* A token per row of logits from one uniform number per row, for rows r < *n_active: the stochastic counterpart of the argmax that
+ * surelock_softmax_kl_sure leaves for surelock_update_mask.  Tokens are ordered by falling logit, the lowest index first among
+ * equal ones; their weights are exp((x - max) / temperature).  Every filter keeps a prefix of that order, the shortest one counts (at
+ * least one token, none of -inf), and the token drawn is the first whose running sum of weights exceeds u[r] times the prefix's.
+ *   logits     dev [M][vocab] of `dtype` SL_BF16 or SL_FP32, row r at r * row_stride elements
+ *   set_of_row dev int32 [M] or NULL: row r uses set r, or the only one (n_sets 1 or >= max_rows then)
+ *   u          dev fp32 [M], in [0, 1); clamped to it, NaN counts as 0
+ *   token      dev int32 [M];  conf dev fp32 [M] or NULL: softmax(logits[r])[token], temperature 1 and unfiltered, the
+ *              confidence that surelock_update_mask orders by;  n_kept dev int32 [M] or NULL: the length of the prefix
+ * A row with a NaN or +inf, with nothing but -inf, or with an undefined setting gives token -1, conf NaN, n_kept 0; so does a set out
+ * of range (device status 4).  Sums are held in 64 bits: the result does not depend on how rows are split, up to 2^-50 of the sum.
+ * vocab < 2^20 - 128 (SL_EUNSUPPORTED otherwise), any row_stride >= vocab.  Deterministic; no workspace; one launch;
+ * asynchronous on `stream`. */
+int surelock_sample(const void *logits, int64_t row_stride, const surelock_sampling *sampling, const int32_t *set_of_row, const float *u,
+                    const int32_t *n_active, int max_rows, int vocab, int dtype, int32_t *token, float *conf, int32_t *n_kept,
+                    int32_t *dev_status, void *stream);
+
 /* Failure-detection diagnostic for the two calls with few bits that wait on copies: in the next surelock_gemm_quantized or
  * surelock_attention_paged that this thread launches, one CTA (the product's first, the attention's second if there is one)
  * waits for 16 bytes that are never copied.  Its bounded waits run out (about 2 s each), it stores device status 2 or 3 in the

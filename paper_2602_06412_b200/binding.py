@@ -60,6 +60,22 @@ class _PagedKV(C.Structure):
                [(n, C.c_int32) for n in ("n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim", "dtype")]
 
 
+class _RopeCfg(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float)]
+
+
+class _RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in ("factor", "original_len", "fast", "slow", "attn_scale")]
+
+
+class _Adapters(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("a", "b", "scale", "ranks")] + [("n_adapters", C.c_int32), ("max_rank", C.c_int32)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")] + [("n_sets", C.c_int32)]
+
+
 def lib() -> C.CDLL:
     """Load libsurelock.so (built in-tree by `paper_2602_06412_b200.build`); raises if it is not there."""
     global _lib
@@ -113,6 +129,13 @@ def lib() -> C.CDLL:
         "surelock_kv_gather_paged": (i32, [C.POINTER(_PagedKV), vp, vp, i32, i32, i32, vp, vp, C.c_int64, i32, vp, vp]),
         "surelock_attention_paged_workspace_bytes": (sz, [i32]),
         "surelock_attention_paged": (i32, [C.POINTER(_PagedKV), vp, C.c_int64, vp, vp, i32, i32, i32, vp, C.c_int64, vp, vp, vp]),
+        "surelock_paged_extend": (i32, [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]),
+        "surelock_paged_truncate": (i32, [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "surelock_rope_frequencies": (i32, [i32, C.c_double, C.POINTER(_RopeScaling), vp, C.POINTER(f32)]),
+        "surelock_rope": (i32, [C.POINTER(_RopeCfg), vp, C.c_int64, i32, vp, C.c_int64, i32, i32, vp, i32, vp, i32, vp, C.c_int64, vp, C.c_int64,
+                                i32, i32, vp, vp]),
+        "surelock_gemm_adapters": (i32, [vp, C.POINTER(_Adapters), vp, vp, i32, vp, C.c_int64, i32, i32, i32, i32, vp, vp]),
+        "surelock_sample": (i32, [vp, C.c_int64, C.POINTER(_Sampling), vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]),
         "surelock_lose_next_copy": (i32, []),
         "surelock_attention": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i32, i32, vp, vp]),
     }
@@ -601,3 +624,144 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
         _check(lib().surelock_attention_paged(cache.ref, q.data_ptr(), _rows(q, H, dh)[1], _ints(row_offsets, B + 1), _ints(seq_lens, B), M, B, H,
                                               o.data_ptr(), _rows(o, H, dh)[1], workspace.data_ptr(), _word(dev_status), stream),
                "surelock_attention_paged")
+
+
+# ---- a served batch on the paged cache: from request lengths to tokens ------------------------------------------------------
+def _plan_sizes(page_table, free_pages):
+    _want(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.is_cuda,
+          "page_table: a contiguous int32 CUDA tensor [B][max_pages] is wanted")
+    return page_table.shape[0], page_table.shape[1], free_pages.numel()
+
+
+def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active,
+                          seq_lens_out=None, n_free_out=None, dev_status=None):
+    """Pages off the free list, row offsets and flat positions (N = max_pages * page_size) for new_tokens[b] more tokens of every
+    sequence; seq_lens and n_free are updated in place unless seq_lens_out, n_free_out are given.  All int32 CUDA tensors:
+    page_table [B][max_pages], seq_lens, new_tokens [B], free_pages [n_pages], n_free, n_active [1], row_offsets [B+1], active_idx [rows]."""
+    B, width, n_pages = _plan_sizes(page_table, free_pages)
+    lens_out, free_out = seq_lens if seq_lens_out is None else seq_lens_out, n_free if n_free_out is None else n_free_out
+    stream = _here(page_table, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active, lens_out, free_out, dev_status)
+    _check(lib().surelock_paged_extend(page_table.data_ptr(), B, page_size, width, n_pages, _ints(seq_lens, B), _ints(new_tokens, B),
+                                       _ints(free_pages, 1), _ints(n_free, 1), _ints(row_offsets, B + 1), _ints(active_idx, 0),
+                                       _ints(n_active, 1), active_idx.numel(), _ints(lens_out, B), _ints(free_out, 1), _word(dev_status),
+                                       stream), "surelock_paged_extend")
+
+
+def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pages, n_free, seq_lens_out=None, n_free_out=None,
+                            dev_status=None):
+    """Sequence b cut to min(seq_lens[b], keep[b]) tokens, its pages back onto the free list (free_pages, n_free: in place)."""
+    B, width, n_pages = _plan_sizes(page_table, free_pages)
+    lens_out, free_out = seq_lens if seq_lens_out is None else seq_lens_out, n_free if n_free_out is None else n_free_out
+    stream = _here(page_table, seq_lens, keep, free_pages, n_free, lens_out, free_out, dev_status)
+    _check(lib().surelock_paged_truncate(page_table.data_ptr(), B, page_size, width, n_pages, _ints(seq_lens, B), _ints(keep, B),
+                                         _ints(free_pages, 1), _ints(n_free, 1), _ints(lens_out, B), _ints(free_out, 1), _word(dev_status),
+                                         stream), "surelock_paged_truncate")
+
+
+ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+def surelock_rope_frequencies(rotary_dim: int, theta: float, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,
+                              fast: float = 32.0, slow: float = 1.0, attn_scale: float = 0.0):
+    """(fp64 CPU tensor [rotary_dim / 2] of radians per position, scale): see the header for the kinds of scaling."""
+    if scaling not in ROPE_SCALING:
+        raise SurelockError(f"scaling: one of {sorted(ROPE_SCALING)} is wanted, got {scaling!r}")
+    freq = torch.empty(max(rotary_dim, 0) // 2, dtype=torch.float64)
+    m = C.c_float(0.0)
+    s = _RopeScaling(ROPE_SCALING[scaling], factor, original_len, fast, slow, attn_scale)
+    _check(lib().surelock_rope_frequencies(rotary_dim, theta, C.byref(s), freq.data_ptr(), C.byref(m)), "surelock_rope_frequencies")
+    return freq, m.value
+
+
+class Rope:
+    """Rotary positions: freq, a fp64 CUDA tensor [rotary_dim / 2] (e.g. of surelock_rope_frequencies), and the layout of pairs."""
+
+    def __init__(self, freq, interleaved: bool = False, scale: float = 1.0):
+        _want(freq.is_cuda and freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: fp64 CUDA tensor [rotary_dim / 2]")
+        self.freq = freq
+        self.raw = _RopeCfg(freq.data_ptr(), 2 * freq.numel(), int(interleaved), scale)
+        self.ref = C.byref(self.raw)
+
+
+def surelock_rope(rope: Rope, q, k, positions, n_active, N: int = 0, q_out=None, k_out=None, transposed: bool = False, dev_status=None):
+    """Rotates rows of q [M][H][head_dim] and k [M][n_kv_heads][head_dim] (or None), bf16 or fp32, rows may lie apart; in place
+    unless q_out, k_out are given.  positions int32 [M], taken modulo N when N > 0 (flat positions of a step)."""
+    _want(q.dim() == 3, f"q: [M][H][head_dim] is wanted, got {tuple(q.shape)}")
+    M, H, dh = q.shape
+    qo, ko = q if q_out is None else q_out, k if k_out is None else k_out
+    _want(qo.dtype == q.dtype and qo.shape == q.shape, "q_out must be like q")
+    qs, qos = _rows(q, H, dh)[1], _rows(qo, H, dh)[1]
+    Hkv = ks = kos = 0
+    if k is not None:
+        _want(k.dim() == 3 and k.shape[0] == M and k.dtype == q.dtype and ko.dtype == q.dtype and ko.shape == k.shape, "k, k_out: rows and type of q")
+        Hkv = k.shape[1]
+        ks, kos = _rows(k, Hkv, dh)[1], _rows(ko, Hkv, dh)[1]
+    stream = _here(q, k, positions, n_active, qo, ko, rope.freq, dev_status)
+    if M:
+        _check(lib().surelock_rope(rope.ref, q.data_ptr(), qs, H, None if k is None else k.data_ptr(), ks, Hkv, dh, _ints(positions, M), N,
+                                   _ints(n_active, 1), M, qo.data_ptr(), qos, None if k is None else ko.data_ptr(), kos, _dt(q),
+                                   int(transposed), _word(dev_status), stream), "surelock_rope")
+
+
+class Adapters:
+    """A pool of low-rank adapters of one projection: a bf16 [n][max_rank][K], b bf16 [n][n_out][max_rank], scale fp32 [n], ranks
+    int32 [n] or None.  Keeps the tensors alive."""
+
+    def __init__(self, a, b, scale, ranks=None):
+        _want(a.dim() == 3 and b.dim() == 3 and a.dtype == torch.bfloat16 and b.dtype == torch.bfloat16, "a [n][max_rank][K], b [n][n_out][max_rank]: bf16")
+        n, r, self.K = a.shape
+        _want(b.shape[0] == n and b.shape[2] == r, "a and b: adapters of the same number and rank")
+        _want(scale.dtype == torch.float32 and scale.shape == (n,) and (ranks is None or (ranks.dtype == torch.int32 and ranks.shape == (n,))),
+              "scale: fp32 [n], ranks: int32 [n] or None")
+        tensors = [t for t in (a, b, scale, ranks) if t is not None]
+        _want(all(t.is_cuda and t.device == a.device and t.is_contiguous() for t in tensors), "adapters: contiguous, on one CUDA device")
+        self._keep, self.a, self.n_out = tensors, a, b.shape[1]
+        self.raw = _Adapters(a.data_ptr(), b.data_ptr(), scale.data_ptr(), None if ranks is None else ranks.data_ptr(), n, r)
+        self.ref = C.byref(self.raw)
+
+
+def surelock_gemm_adapters(x, adapters: Adapters, adapter_of_seq, row_offsets, Cout, dev_status=None):
+    """Cout[r] += scale B (A x[r]) with the adapter of the row's sequence.  x bf16 [M][K]; Cout bf16 or fp32 [M][n_out], rows may
+    lie apart; adapter_of_seq int32 [B] (negative: none), row_offsets int32 [B+1]."""
+    _want(x.dim() == 2 and x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape[1] == adapters.K, "x: contiguous bf16 [M][K] of the adapters' K")
+    M, n = x.shape[0], adapters.n_out
+    st = Cout.stride()
+    _want(Cout.shape == (M, n) and (st[1] == 1 or n == 1) and (st[0] >= n or M <= 1), "Cout: [M][n_out] with packed rows")
+    B = adapter_of_seq.numel()
+    stream = _here(x, adapters.a, adapter_of_seq, row_offsets, Cout, dev_status)
+    if M and B:
+        _check(lib().surelock_gemm_adapters(x.data_ptr(), adapters.ref, _ints(adapter_of_seq, B), _ints(row_offsets, B + 1), B, Cout.data_ptr(),
+                                            max(st[0], n), M, n, adapters.K, _dt(Cout), _word(dev_status), stream), "surelock_gemm_adapters")
+
+
+class Sampling:
+    """Settings of sampled requests: CUDA tensors [n_sets], each of which may be None (temperature 1, no filter).  Keeps them alive."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        tensors = [t for t in (temperature, top_k, top_p, min_p) if t is not None]
+        for t in tensors:
+            _want(t.is_cuda and t.dim() == 1 and t.is_contiguous() and t.shape == tensors[0].shape and t.device == tensors[0].device and t.numel() > 0 and
+                  t.dtype == (torch.int32 if t is top_k else torch.float32), "settings: fp32 (top_k: int32) CUDA tensors [n_sets] of one length")
+        self._keep, self.first, self.n_sets = tensors, tensors[0] if tensors else None, tensors[0].numel() if tensors else 1
+        self.raw = _Sampling(*[None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)], self.n_sets)
+        self.ref = C.byref(self.raw)
+
+
+def _floats(t: torch.Tensor, least: int) -> int:
+    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= least):
+        raise SurelockError(f"a contiguous fp32 CUDA tensor of at least {least} entries is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def surelock_sample(logits, sampling: Sampling, u, n_active, token, conf=None, n_kept=None, set_of_row=None, dev_status=None):
+    """A token per row of logits [M][vocab] (bf16 or fp32, rows may lie apart) from one uniform number per row, u fp32 [M].  token,
+    n_kept int32 [M], conf fp32 [M]; row r uses set set_of_row[r], or set r, or the only one."""
+    _want(logits.dim() == 2, f"logits: [M][vocab] is wanted, got {tuple(logits.shape)}")
+    M, V = logits.shape
+    st = logits.stride()
+    _want((st[1] == 1 or V == 1) and (st[0] >= V or M <= 1), "logits: packed rows are wanted")
+    stream = _here(logits, sampling.first, u, n_active, token, conf, n_kept, set_of_row, dev_status)
+    if M:
+        _check(lib().surelock_sample(logits.data_ptr(), max(st[0], V), sampling.ref, None if set_of_row is None else _ints(set_of_row, M), _floats(u, M),
+                                     _ints(n_active, 1), M, V, _dt(logits), _ints(token, M), None if conf is None else _floats(conf, M),
+                                     None if n_kept is None else _ints(n_kept, M), _word(dev_status), stream), "surelock_sample")

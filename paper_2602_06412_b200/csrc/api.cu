@@ -1146,6 +1146,90 @@ int surelock_kv_gather_paged(const surelock_paged_kv* cache, const int32_t* acti
                                 (cudaStream_t)stream);
 }
 
+static bool bad_page_size(int p) { return p != 16 && p != 32 && p != 64 && p != 128 && p != 256; }
+
+int surelock_paged_extend(int32_t* page_table, int B, int page_size, int max_pages, int n_pages, const int32_t* seq_lens,
+                          const int32_t* new_tokens, const int32_t* free_pages, const int32_t* n_free, int32_t* row_offsets,
+                          int32_t* active_idx, int32_t* n_active, int max_rows, int32_t* seq_lens_out, int32_t* n_free_out,
+                          int32_t* dev_status, void* stream) {
+  if (!page_table || !seq_lens || !new_tokens || !free_pages || !n_free || !row_offsets || (!active_idx && max_rows > 0) || !n_active || !seq_lens_out ||
+      !n_free_out || B <= 0 || max_pages <= 0 || n_pages <= 0 || max_rows < 0)
+    return SL_EINVAL;
+  if (bad_page_size(page_size) || B > 1024 || (long long)B * max_pages * page_size > 0x7fffffffll) return SL_EUNSUPPORTED;
+  return launch_paged_extend(page_table, B, page_size, max_pages, n_pages, seq_lens, new_tokens, free_pages, n_free, row_offsets,
+                             active_idx, n_active, max_rows, seq_lens_out, n_free_out, dev_status, (cudaStream_t)stream);
+}
+
+int surelock_paged_truncate(const int32_t* page_table, int B, int page_size, int max_pages, int n_pages, const int32_t* seq_lens,
+                            const int32_t* keep, int32_t* free_pages, const int32_t* n_free, int32_t* seq_lens_out,
+                            int32_t* n_free_out, int32_t* dev_status, void* stream) {
+  if (!page_table || !seq_lens || !keep || !free_pages || !n_free || !seq_lens_out || !n_free_out || B <= 0 || max_pages <= 0 || n_pages <= 0)
+    return SL_EINVAL;
+  if (bad_page_size(page_size) || B > 1024 || (long long)B * max_pages * page_size > 0x7fffffffll) return SL_EUNSUPPORTED;
+  return launch_paged_truncate(page_table, B, page_size, max_pages, n_pages, seq_lens, keep, free_pages, n_free, seq_lens_out, n_free_out,
+                               dev_status, (cudaStream_t)stream);
+}
+
+int surelock_rope_frequencies(int rotary_dim, double theta, const surelock_rope_scaling* scaling, double* freq_out, float* scale_out) {
+  if (!freq_out || !scale_out || rotary_dim <= 0 || rotary_dim % 2 || !(theta > 1.0) || isinf(theta)) return SL_EINVAL;
+  if (scaling) {
+    const surelock_rope_scaling& s = *scaling;
+    if (s.kind < SL_ROPE_PLAIN || s.kind > SL_ROPE_BANDS) return SL_EINVAL;
+    if (s.kind != SL_ROPE_PLAIN && (!(s.factor > 0.0) || isinf(s.factor))) return SL_EINVAL;
+    if (s.kind == SL_ROPE_NTK && rotary_dim == 2) return SL_EINVAL;
+    if ((s.kind == SL_ROPE_YARN || s.kind == SL_ROPE_BANDS) &&
+        (!(s.original_len > 0.0) || isinf(s.original_len) || !(s.slow > 0.0) || !(s.fast > s.slow) || isinf(s.fast)))
+      return SL_EINVAL;
+    if (s.kind == SL_ROPE_YARN && (!(s.attn_scale >= 0.0) || isinf(s.attn_scale))) return SL_EINVAL;
+  }
+  rope_frequencies(freq_out, scale_out, rotary_dim, theta, scaling);
+  return SL_OK;
+}
+
+int surelock_rope(const surelock_rope_cfg* cfg, const void* q, int64_t q_stride, int H, const void* k, int64_t k_stride, int n_kv_heads,
+                  int head_dim, const int32_t* positions, int N, const int32_t* n_active, int max_rows, void* q_out,
+                  int64_t q_out_stride, void* k_out, int64_t k_out_stride, int dtype, int transposed, int32_t* dev_status,
+                  void* stream) {
+  if (!cfg || !cfg->freq || !q || !q_out || !positions || !n_active || max_rows < 0 || H <= 0 || head_dim <= 0 || N < 0) return SL_EINVAL;
+  if (dtype != SL_BF16 && dtype != SL_FP32) return SL_EINVAL;
+  if (cfg->rotary_dim <= 0 || cfg->rotary_dim % 2 || cfg->rotary_dim > head_dim) return SL_EINVAL;
+  if (q_stride < (int64_t)H * head_dim || q_out_stride < (int64_t)H * head_dim || (q == q_out && q_stride != q_out_stride)) return SL_EINVAL;
+  if (k && (!k_out || n_kv_heads <= 0 || k_stride < (int64_t)n_kv_heads * head_dim || k_out_stride < (int64_t)n_kv_heads * head_dim ||
+            (k == k_out && k_stride != k_out_stride)))
+    return SL_EINVAL;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) |
+                       (k ? reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(k_out) : 0);
+  if ((at & (dtype == SL_BF16 ? 1 : 3)) || (reinterpret_cast<uintptr_t>(cfg->freq) & 7)) return SL_EUNSUPPORTED;
+  if (head_dim > 4096 || H > 65536 || n_kv_heads > 65536) return SL_EUNSUPPORTED;
+  if (max_rows == 0) return SL_OK;
+  return launch_rope_rows(*cfg, q, q_stride, H, k, k_stride, n_kv_heads, head_dim, positions, N, n_active, max_rows, q_out, q_out_stride,
+                          k_out, k_out_stride, dtype, transposed, dev_status, (cudaStream_t)stream);
+}
+
+int surelock_gemm_adapters(const void* x, const surelock_adapters* w, const int32_t* adapter_of_seq, const int32_t* row_offsets, int B,
+                           void* C, int64_t c_stride, int max_rows, int n_out, int K, int dtype, int32_t* dev_status, void* stream) {
+  if (!x || !w || !w->a || !w->b || !w->scale || !adapter_of_seq || !row_offsets || !C || B <= 0 || max_rows < 0 || n_out <= 0 || K <= 0)
+    return SL_EINVAL;
+  if (w->n_adapters <= 0 || w->max_rank <= 0 || c_stride < n_out || (dtype != SL_BF16 && dtype != SL_FP32)) return SL_EINVAL;
+  if (K % 8 || w->max_rank % 8 || w->max_rank > 128) return SL_EUNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(w->a) | reinterpret_cast<uintptr_t>(w->b)) & 15) return SL_EUNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(C) & (dtype == SL_BF16 ? 1 : 3)) return SL_EUNSUPPORTED;
+  if (max_rows == 0) return SL_OK;
+  return launch_gemm_adapters(x, *w, adapter_of_seq, row_offsets, B, C, c_stride, max_rows, n_out, K, dtype, dev_status, (cudaStream_t)stream);
+}
+
+int surelock_sample(const void* logits, int64_t row_stride, const surelock_sampling* sampling, const int32_t* set_of_row, const float* u,
+                    const int32_t* n_active, int max_rows, int vocab, int dtype, int32_t* token, float* conf, int32_t* n_kept,
+                    int32_t* dev_status, void* stream) {
+  if (!logits || !sampling || !u || !n_active || !token || max_rows < 0 || vocab <= 0 || row_stride < vocab) return SL_EINVAL;
+  if (dtype != SL_BF16 && dtype != SL_FP32) return SL_EINVAL;
+  if (sampling->n_sets <= 0 || (!set_of_row && sampling->n_sets != 1 && sampling->n_sets < max_rows)) return SL_EINVAL;
+  if (reinterpret_cast<uintptr_t>(logits) & (dtype == SL_BF16 ? 1 : 3)) return SL_EUNSUPPORTED;
+  if (max_rows == 0) return SL_OK;
+  return launch_sample(logits, row_stride, *sampling, set_of_row, u, n_active, max_rows, vocab, dtype, token, conf, n_kept, dev_status,
+                       (cudaStream_t)stream);
+}
+
 size_t surelock_attention_paged_workspace_bytes(int head_dim) { return attention_paged_workspace_bytes(head_dim); }
 
 int surelock_attention_paged(const surelock_paged_kv* cache, const void* q, int64_t q_stride, const int32_t* row_offsets,

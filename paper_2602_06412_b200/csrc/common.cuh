@@ -92,6 +92,15 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
+// x / d by the reciprocal m = fast_div_by(d), x below 2^31: the product is the quotient or one more
+__device__ __forceinline__ unsigned fast_div(unsigned x, unsigned d, unsigned m) {
+  if (m == 0) return x;
+  const unsigned q = __umulhi(x, m);
+  return q * d > x ? q - 1 : q;
+}
+// ceil(2^32 / d), 0 for d = 1
+inline uint32_t fast_div_by(int d) { return d == 1 ? 0u : (uint32_t)(0x100000000ull / d + (0x100000000ull % d != 0)); }
+
 inline int sm_count() {
   static int n = 0;
   if (!n) {
@@ -206,6 +215,27 @@ int launch_unlock(const float* drift, const float* conf, const int32_t* idx, con
 
 // step precondition check (cache_check.cu): locked positions need kv_valid, active ones become valid
 int launch_cache_check(const uint8_t* lock, uint8_t* kv_valid, int total, int32_t* status, cudaStream_t st);
+
+// pages and rows of new tokens, and of those given up (paged_plan.cu)
+int launch_paged_extend(int32_t* table, int B, int page_size, int max_pages, int n_pages, const int32_t* seq_lens, const int32_t* want,
+                        const int32_t* free_pages, const int32_t* n_free, int32_t* row_offsets, int32_t* active_idx, int32_t* n_active,
+                        int max_rows, int32_t* seq_lens_out, int32_t* n_free_out, int32_t* status, cudaStream_t st);
+int launch_paged_truncate(const int32_t* table, int B, int page_size, int max_pages, int n_pages, const int32_t* seq_lens,
+                          const int32_t* keep, int32_t* free_pages, const int32_t* n_free, int32_t* seq_lens_out, int32_t* n_free_out,
+                          int32_t* status, cudaStream_t st);
+// rotary positions of packed rows (rope.cu)
+int launch_rope_rows(const surelock_rope_cfg& c, const void* q, long long q_stride, int H, const void* k, long long k_stride, int Hkv,
+                     int head_dim, const int32_t* positions, int N, const int32_t* n_active, int max_rows, void* q_out,
+                     long long q_out_stride, void* k_out, long long k_out_stride, int dtype, int transposed, int32_t* status,
+                     cudaStream_t st);
+void rope_frequencies(double* freq, float* scale, int D, double theta, const surelock_rope_scaling* s);
+// C[r] += scale B_a (A_a x_r), adapters by sequence (gemm_adapters.cu)
+int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_t* adapter_of_seq, const int32_t* row_offsets, int B,
+                         void* C, long long c_stride, int max_rows, int n_out, int K, int dtype, int32_t* status, cudaStream_t st);
+// a token per row (sample.cu)
+int launch_sample(const void* logits, long long row_stride, const surelock_sampling& sets, const int32_t* set_of_row, const float* u,
+                  const int32_t* n_active, int max_rows, int vocab, int dtype, int32_t* token, float* conf, int32_t* n_kept,
+                  int32_t* status, cudaStream_t st);
 
 int launch_update_mask(const float* conf, const int32_t* argmax, const int32_t* idx, const int32_t* row_offsets, int B,
                        int N, int lo, int hi, int k, int32_t mask_token, int32_t* tokens, uint8_t* mask_state,

@@ -1,0 +1,310 @@
+// Low-rank adapters of many requests beside a shared projection: for the rows r of a sequence that uses adapter a,
+//   C[r] += scale_a B_a (A_a x_r),   A_a [rank][K], B_a [n_out][rank].
+//
+// One launch, no workspace: a cluster of CL CTAs takes 16 WR rows of one sequence (its adapter's weights are read once for
+// them).  Each CTA multiplies its 1 / CL of K, the partial t = A_a x of all CTAs meet through distributed shared memory in a
+// fixed order, and each CTA then adds its 1 / CL of the features to C.  Both products are mma.sync m16n8k16 with the rows on the
+// 16 side: they are far from the tensor cores' rate (rank operations per byte), and their operands come straight from global
+// memory in 16- and 8-byte loads, since any order of k serves as long as both operands keep it.
+//
+// x and the weights are bf16, so the first product's terms are exact and summed in fp32.  t scale stays an fp32 number: it enters
+// the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
+#include "tc_common.cuh"
+
+namespace sl {
+namespace {
+
+constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS;
+
+struct AdapterArgs {
+  const bf16 *x, *a, *b;
+  const float* scale;
+  const int32_t *ranks, *adapter_of_seq, *row_offsets;
+  void* c;
+  int32_t* status;
+  long long c_stride;
+  int n_adapters, max_rank, B, max_rows, n_out, K;
+};
+
+__device__ __forceinline__ void mma_16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+
+// The group-th tile of `tile` rows of one sequence: its sequence, first row and rows; every lane of a warp gets the same.
+__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& seq, int& row0, int& rows) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;                                    // tiles of the sequences before this round's 32
+  bool bad = false;
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int b = b0 + lane;
+    // offsets are clamped, so that no row is outside C
+    int from = b < a.B ? a.row_offsets[b] : 0, to = b < a.B ? a.row_offsets[b + 1] : 0;
+    if (b < a.B) bad |= from < 0 || to < from || to > a.max_rows;
+    from = min(max(from, 0), a.max_rows);
+    to = min(max(to, from), a.max_rows);
+    const int mine = (int)(((long long)to - from + tile - 1) / tile);
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, group - before < sum);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      const int first = group - before - __shfl_sync(0xffffffffu, sum - mine, l);
+      seq = b0 + l;
+      row0 = __shfl_sync(0xffffffffu, from, l) + first * tile;
+      rows = min(tile, __shfl_sync(0xffffffffu, to, l) - row0);
+      if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
+  return false;
+}
+
+// the k-th term of v as a sum of bf16 numbers
+template <int TERMS> __device__ __forceinline__ void bf16_terms(float v, bf16* to, int pitch) {
+#pragma unroll
+  for (int i = 0; i < TERMS; ++i) {
+    const bf16 h = __float2bfloat16_rn(v);
+    to[i * pitch] = h;
+    const float left = v - __bfloat162float(h);
+    v = isfinite(left) ? left : 0.f;                 // an infinity is its own only term
+  }
+}
+
+template <int WR, int NT, typename CT> struct AdapterTile {
+  static constexpr int ROWS = 16 * WR, KS = AD_WARPS / WR, TERMS = sizeof(CT) == 2 ? 2 : 3;
+  static constexpr int TP = 8 * NT + 4;                               // pitch of t in floats: rows 4 banks apart
+  static constexpr int SP = (8 * NT < 16 ? 16 : 8 * NT) + 8;          // pitch of its bf16 terms
+  static constexpr int T_BYTES = KS * ROWS * TP * 4, BYTES = T_BYTES + TERMS * ROWS * SP * 2;
+};
+
+template <int WR, int NT, typename CT>
+__global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a) {
+  using L = AdapterTile<WR, NT, CT>;
+  constexpr int ROWS = L::ROWS, KS = L::KS, TERMS = L::TERMS, TP = L::TP, SP = L::SP, KSTEPS = (8 * NT + 15) / 16;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* part = reinterpret_cast<float*>(smem);
+  bf16* terms = reinterpret_cast<bf16*>(smem + L::T_BYTES);
+  griddep_wait();
+  griddep_launch();
+  uint32_t ctas;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+  const int CL = (int)ctas, rank_cta = (int)cluster_ctarank();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int wr = warp % WR, kw = warp / WR;
+  int seq, row0, rows;
+  if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, seq, row0, rows)) return;
+  const int ad = a.adapter_of_seq[seq];
+  if (ad < 0 || ad >= a.n_adapters) {
+    if (ad >= a.n_adapters) set_status(a.status, SL_DEV_BAD_INDEX);
+    return;
+  }
+  int rank = a.max_rank;
+  if (a.ranks) {
+    const int given = a.ranks[ad];
+    if (given < 0 || given > a.max_rank) set_status(a.status, SL_DEV_BAD_INDEX);
+    rank = min(max(given, 0), a.max_rank);
+  }
+  if (rank == 0) return;
+  const bf16* wa = a.a + (long long)ad * a.max_rank * a.K;
+  const bf16* wb = a.b + (long long)ad * a.n_out * a.max_rank;
+  const int fgs = (a.n_out + 31) >> 5, fg0 = (int)((long long)fgs * rank_cta / CL), fg1 = (int)((long long)fgs * (rank_cta + 1) / CL);
+  if (WR == 1) {                                     // few rows wait for these weights: have them in the L2 by then
+    const long long lines = ((long long)(min(fg1 * 32, a.n_out) - fg0 * 32) * a.max_rank * 2 + 127) >> 7;
+    for (long long i = threadIdx.x; i < lines; i += AD_THREADS)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(wb + (long long)fg0 * 32 * a.max_rank) + (i << 7)));
+  }
+
+  // ---- t = A_a x over this warp's k
+  float acc[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+  {
+    const int chunks = (a.K + 31) >> 5, splits = CL * KS, s = rank_cta * KS + kw;
+    const int c0 = (int)((long long)chunks * s / splits), c1 = (int)((long long)chunks * (s + 1) / splits);
+    const int ra = wr * 16 + g, rb = ra + 8;
+    const bf16 *xa = a.x + (long long)(row0 + ra) * a.K, *xb = a.x + (long long)(row0 + rb) * a.K;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 2
+    for (int ch = c0; ch < c1; ++ch) {
+      const int k = ch * 32 + t * 8;
+      const bool in = k < a.K;
+      const uint4 u = in && ra < rows ? *reinterpret_cast<const uint4*>(xa + k) : zero;
+      const uint4 v = in && rb < rows ? *reinterpret_cast<const uint4*>(xb + k) : zero;
+      uint4 w[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j] = in && 8 * j + g < rank ? __ldg(reinterpret_cast<const uint4*>(wa + (long long)(8 * j + g) * a.K + k)) : zero;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (8 * j >= rank) break;
+        mma_16816(acc[j], u.x, v.x, u.y, v.y, w[j].x, w[j].y);
+        mma_16816(acc[j], u.z, v.z, u.w, v.w, w[j].z, w[j].w);
+      }
+    }
+    float* to = part + (kw * ROWS + wr * 16 + g) * TP + 2 * t;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      *reinterpret_cast<float2*>(to + 8 * j) = make_float2(acc[j][0], acc[j][1]);
+      *reinterpret_cast<float2*>(to + 8 * TP + 8 * j) = make_float2(acc[j][2], acc[j][3]);
+    }
+  }
+  __syncthreads();
+  if (KS > 1) {
+    for (int i = threadIdx.x; i < ROWS * 8 * NT; i += AD_THREADS) {
+      const int at = (i / (8 * NT)) * TP + i % (8 * NT);
+      float v = part[at];
+#pragma unroll
+      for (int w = 1; w < KS; ++w) v += part[w * ROWS * TP + at];
+      part[at] = v;
+    }
+  }
+  cluster_sync_all();
+  {
+    const float scale = a.scale[ad];
+    const uint32_t base = smem_u32(part);
+    for (int i = threadIdx.x; i < ROWS * 16 * KSTEPS; i += AD_THREADS) {
+      const int r = i / (16 * KSTEPS), j = i % (16 * KSTEPS);
+      float v = 0.f;
+      if (j < rank) {
+        const uint32_t at = base + 4 * (r * TP + j);
+        for (int c = 0; c < CL; ++c) v += ld_cluster(mapa_u32(at, c));
+        v *= scale;
+      }
+      bf16_terms<TERMS>(v, terms + r * SP + j, ROWS * SP);
+    }
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the others' t
+  __syncthreads();
+
+  // ---- C += B_a t over this CTA's features, 32 at a time to a warp: lane t of a quad ends up with 8 neighbours
+  CT* c = reinterpret_cast<CT*>(a.c);
+  const bool wide = (reinterpret_cast<uintptr_t>(c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;
+  const int ra = wr * 16 + g, rb = ra + 8;
+  const bf16* mine = terms + (wr * 16 + g) * SP + 4 * t;
+  for (int fg = fg0 + kw; fg < fg1; fg += KS) {
+    const int f0 = fg * 32 + 8 * t;
+    float d[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+    CT* p[2] = {c + (row0 + ra) * a.c_stride + f0, c + (row0 + rb) * a.c_stride + f0};
+    const bool whole = wide && f0 + 8 <= a.n_out;
+    __align__(16) CT old[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if ((h ? rb : ra) < rows) {
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(CT) / 2; ++i)
+            reinterpret_cast<uint4*>(old[h])[i] = reinterpret_cast<const uint4*>(p[h])[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (f0 + i < a.n_out) old[h][i] = p[h][i];
+        }
+      }
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+      if (16 * s >= rank) break;
+      const int k = 16 * s + 4 * t;
+      uint2 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int f = fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
+        w[j] = make_uint2(0u, 0u);
+        if (f < a.n_out && k < rank) w[j] = __ldg(reinterpret_cast<const uint2*>(wb + (long long)f * a.max_rank + k));
+        if (k + 4 > rank) {                          // what lies behind the adapter's own rank is not read into the sum
+          if (k + 3 >= rank) w[j].y &= 0xffffu;
+          if (k + 2 >= rank) w[j].y = 0u;
+          if (k + 1 >= rank) w[j].x &= 0xffffu;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < TERMS; ++m) {
+        const uint2 u = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 16 * s);
+        const uint2 v = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 8 * SP + 16 * s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, w[j].x, w[j].y);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if ((h ? rb : ra) < rows) {
+        __align__(16) CT out[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = from_f<CT>(to_f(old[h][i]) + d[i >> 1][2 * h + (i & 1)]);
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(CT) / 2; ++i) reinterpret_cast<uint4*>(p[h])[i] = reinterpret_cast<const uint4*>(out)[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (f0 + i < a.n_out) p[h][i] = out[i];
+        }
+      }
+  }
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody reads this CTA's t any more
+}
+
+template <int WR, int NT, typename CT>
+int launch_tile(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
+  using L = AdapterTile<WR, NT, CT>;
+  static std::atomic<uint64_t> done{0};
+  SL_CUDA_TRY(allow_smem(gemm_adapters_kernel<WR, NT, CT>, L::BYTES, done));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)groups * CL);
+  cfg.blockDim = dim3(AD_THREADS);
+  cfg.dynamicSmemBytes = L::BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = CL;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_adapters_kernel<WR, NT, CT>, a));
+  return SL_OK;
+}
+
+template <int WR, typename CT>
+int launch_rank(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
+  if (a.max_rank <= 16) return launch_tile<WR, 2, CT>(a, groups, CL, st);
+  if (a.max_rank <= 32) return launch_tile<WR, 4, CT>(a, groups, CL, st);
+  if (a.max_rank <= 64) return launch_tile<WR, 8, CT>(a, groups, CL, st);
+  return launch_tile<WR, 16, CT>(a, groups, CL, st);
+}
+
+template <typename CT> int launch_rows(const AdapterArgs& a, cudaStream_t st) {
+  // tiles of 64 rows where sequences are that long on average
+  const bool many = a.max_rows >= 32 * (long long)a.B;
+  const int tile = many ? 64 : 16;
+  // every sequence may end in a tile that is not full
+  const long long groups = a.max_rows / tile + (a.max_rows < a.B ? a.max_rows : a.B);
+  if (groups > (1 << 27)) return SL_EUNSUPPORTED;
+  int CL = 8;
+  while (CL > 1 && groups * CL > 4ll * sm_count()) CL >>= 1;
+  return many ? launch_rank<4, CT>(a, (int)groups, CL, st) : launch_rank<1, CT>(a, (int)groups, CL, st);
+}
+
+}  // namespace
+
+int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_t* adapter_of_seq, const int32_t* row_offsets, int B,
+                         void* C, long long c_stride, int max_rows, int n_out, int K, int dtype, int32_t* status, cudaStream_t st) {
+  const AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
+                         c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K};
+  return dtype == SL_BF16 ? launch_rows<bf16>(a, st) : launch_rows<float>(a, st);
+}
+
+}  // namespace sl

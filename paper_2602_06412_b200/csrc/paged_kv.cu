@@ -56,12 +56,6 @@ struct PagedArgs {
   int32_t* status;
 };
 
-// x / d by the reciprocal m = ceil(2^32 / d) (0 for d = 1): the product is the quotient or one more
-__device__ __forceinline__ unsigned fast_div(unsigned x, unsigned d, unsigned m) {
-  if (m == 0) return x;
-  const unsigned q = __umulhi(x, m);
-  return q * d > x ? q - 1 : q;
-}
 // slot index ((page * Hkv + h) * page_size + place) of flat position f, or -1
 __device__ __forceinline__ long long paged_slot(const PagedArgs& a, int f, int h) {
   if (f < 0) return -1;
@@ -376,9 +370,6 @@ __global__ void __launch_bounds__(PK_THREADS, PK_GATHER_BLOCKS) kv_gather_paged_
     }
   }
 }
-
-// ceil(2^32 / d), 0 for d = 1
-uint32_t fast_div_by(int d) { return d == 1 ? 0u : (uint32_t)(0x100000000ull / d + (0x100000000ull % d != 0)); }
 
 PagedArgs paged_args(const surelock_paged_kv& c, const int32_t* idx, const int32_t* n_active, int max_rows, int B, int N,
                      long long row_stride, int32_t* status, int heads) {

@@ -1,0 +1,877 @@
+// A token per row of logits from one given uniform number, with temperature, top-k, top-p and min-p.
+//
+// With m the row's largest logit and w_v = exp((x_v - m) / T), put the tokens in order of falling x (ties: the lowest index first;
+// tokens of -inf do not count).  Each filter keeps a prefix of that order:
+//   top-k   the first k;   top-p  of those, the shortest prefix whose weights sum to at least top_p of theirs;
+//   min-p   the tokens with w_v >= min_p;
+// the token drawn is the first one of the shortest prefix whose running sum of weights exceeds u times the prefix's.  So nothing
+// needs sorting: all that is asked of the row is "which token has rank n" and "at which token does the running sum reach s", and
+// both are answered by sums over values.  Sums are held in 64 bits: with 100000 tokens in the prefix, 32 would draw a neighbour of
+// the right token in one row of a hundred.
+//
+// bf16 rows (WindowSums): a bf16 number is its own histogram bin.  One pass counts the row's values in shared memory, 6144 bins
+// to a sign for magnitudes in [2^-32, 2^16), which leaves the sums to the few thousand distinct values: one exponential each instead of
+// one per token, and a sum is exact but for 2^-53 roundings.  The occupied range of bins is then walked in order, a few bins to
+// a thread.  The token's index is found by a second pass that counts the tokens of the value that was drawn, out of the L2.  A row with a
+// finite value outside the window (not zero) is done by the other method.
+//
+// fp32 rows (RadixSums): a radix search with 11 + 11 + 10 bits of the ordered key.  A pass adds every token's weight, as four
+// 14-bit limbs of a fixed-point number (exact sums in any order), to its bin; the bin in question is then opened by another pass
+// over the row's tokens in it.
+//
+// A row is one CTA's work, or with few rows that of a cluster of CTAs, whose shares meet through distributed shared memory.
+#include "tc_common.cuh"
+
+namespace sl {
+namespace {
+
+constexpr int SM_THREADS = 512, SM_WARPS = SM_THREADS / 32;
+
+struct SampleArgs {
+  const void* logits;
+  long long row_stride;
+  surelock_sampling sets;
+  const int32_t *set_of_row, *n_active;
+  const float* u;
+  int32_t *token, *n_kept, *status;
+  float* conf;
+  int max_rows, vocab;
+};
+
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_shared(uint32_t addr, uint32_t v) {
+  asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// all threads of the row: one CTA's, or a cluster's
+template <bool CLUSTER> __device__ __forceinline__ void row_sync() {
+  if (CLUSTER) cluster_sync_all(); else __syncthreads();
+}
+
+// Ordered keys: a larger number has a larger key; both zeros have the same.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// This CTA's share of a row: whole 16-byte words, the first CTA also what lies before the first of them, the last what is left.
+template <typename T> struct Share {
+  static constexpr int V = 16 / sizeof(T);
+  const T* row;
+  int head, tail0, vocab;           // tokens before the first word, first token behind the last
+  int v0, v1;                       // this CTA's words
+  bool first, last;
+  __device__ Share(const T* p, int n, int cta, int ctas) : row(p), vocab(n) {
+    head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(T)));
+    const int words = (n - head) / V;
+    tail0 = head + words * V;
+    v0 = (int)((long long)words * cta / ctas);
+    v1 = (int)((long long)words * (cta + 1) / ctas);
+    first = cta == 0;
+    last = cta == ctas - 1;
+  }
+  __device__ const uint4* words() const { return reinterpret_cast<const uint4*>(row + head); }
+  // f(x) for every token of this CTA's share, in no particular order
+  template <typename F> __device__ void each(F f) const {
+    const uint4* w = words();
+    for (int v = v0 + (int)threadIdx.x; v < v1; v += SM_THREADS) {
+      const uint4 u = w[v];
+      const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int i = 0; i < V; ++i) f(to_f(e[i]));
+    }
+    if (first && (int)threadIdx.x < head) f(to_f(row[threadIdx.x]));
+    if (last && tail0 + (int)threadIdx.x < vocab) f(to_f(row[tail0 + threadIdx.x]));
+  }
+};
+
+// a token by its place in the order: its rank (0 = the largest), the sum of weights up to and with it, its value and which of the
+// tokens of that value it is
+struct Found {
+  double mass;
+  uint32_t rank, key, nth;
+};
+
+struct Shared {                     // beside the bins
+  double part_w[SM_WARPS], part_m[SM_WARPS], part_raw[SM_WARPS];
+  uint32_t part_n[SM_WARPS], part_nm[SM_WARPS], matches[SM_WARPS];
+  double cta_w, cta_m, cta_raw;     // this CTA's sums, read by the cluster
+  uint32_t cta_n, cta_nm, cta_matches;
+  uint32_t top, lo, hi, flags, zeros;
+  uint32_t owner, before_n;
+  double before_w;
+};
+
+enum { ROW_UNDEFINED = 1, ROW_OUTSIDE = 2 };
+
+// the settings of a row
+struct Settings {
+  double T, top_p, min_p;
+  float u;
+  int top_k;
+  bool greedy, ok;
+};
+
+// What both methods leave in registers: every thread has a run of values in falling order, the runs in order of threads (and
+// CTAs).  n, w: tokens of the run and their weights, incl_*: running sums up to and with it.
+struct Runs {
+  uint32_t n, incl_n, excl_n;
+  double w, incl_w, excl_w;
+  uint32_t total_n, total_nm;
+  double total_w, total_m, total_raw;
+};
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xffffffffu, v); }
+
+// Running sums of the runs over the row.  nm, m: tokens and weights that min-p keeps; raw: weights at T = 1.
+template <bool CLUSTER>
+__device__ void sum_runs(Shared& s, Runs& q, uint32_t nm, double m, double raw, int ctas, int cta) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t n = q.n;
+  double w = q.w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, n, o);
+    const double b = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) {
+      n += a;
+      w += b;
+    }
+  }
+  nm = warp_sum(nm);
+  m = warp_sum(m);
+  raw = warp_sum(raw);
+  if (lane == 31) {
+    s.part_n[warp] = n;
+    s.part_w[warp] = w;
+    s.part_nm[warp] = nm;
+    s.part_m[warp] = m;
+    s.part_raw[warp] = raw;
+  }
+  __syncthreads();
+  uint32_t n0 = 0, nn = 0, nnm = 0;
+  double w0 = 0, ww = 0, mm = 0, rr = 0;
+#pragma unroll
+  for (int i = 0; i < SM_WARPS; ++i) {
+    if (i == warp) {
+      n0 = nn;
+      w0 = ww;
+    }
+    nn += s.part_n[i];
+    ww += s.part_w[i];
+    nnm += s.part_nm[i];
+    mm += s.part_m[i];
+    rr += s.part_raw[i];
+  }
+  double before_w = 0;
+  uint32_t before_n = 0;
+  if (CLUSTER) {
+    if (threadIdx.x == 0) {
+      s.cta_n = nn;
+      s.cta_w = ww;
+      s.cta_nm = nnm;
+      s.cta_m = mm;
+      s.cta_raw = rr;
+    }
+    cluster_sync_all();
+    nn = nnm = 0;
+    ww = mm = rr = 0;
+    for (int c = 0; c < ctas; ++c) {
+      if (c == cta) {
+        before_n = nn;
+        before_w = ww;
+      }
+      nn += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_n), c));
+      nnm += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_nm), c));
+      ww += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_w), c));
+      mm += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_m), c));
+      rr += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_raw), c));
+    }
+  }
+  q.total_n = nn; q.total_nm = nnm; q.total_w = ww; q.total_m = mm; q.total_raw = rr;
+  q.incl_n = before_n + n0 + n;
+  q.incl_w = before_w + (w0 + w);
+  q.excl_n = q.incl_n - q.n;
+  const double up = __shfl_up_sync(0xffffffffu, q.incl_w, 1);
+  q.excl_w = lane ? up : before_w + w0;
+}
+
+// The number of tokens of weight w, 1 ... c, after which cum reaches the target (strict: exceeds it); c if none does.
+__device__ __forceinline__ bool reaches(double cum, double target, bool strict) { return strict ? cum > target : cum >= target; }
+__device__ __forceinline__ uint32_t tokens_until(double cum, double w, uint32_t c, double target, bool strict) {
+  const double about = ceil((target - cum) / w);
+  uint32_t j = about >= 1.0 ? (about <= (double)c ? (uint32_t)about : c) : 1u;   // also where w = 0
+  while (j > 1 && reaches(cum + (j - 1) * w, target, strict)) --j;
+  while (j < c && !reaches(cum + j * w, target, strict)) ++j;
+  return j;
+}
+
+// What a find asks for: the token of a rank, or the first token at which the running sum of weights reaches a target.
+struct Ask {
+  bool by_rank, strict;
+  uint32_t rank;
+  double target;
+  __device__ bool in(const Runs& q) const {
+    return q.n && (by_rank ? rank < q.incl_n : reaches(q.incl_w, target, strict));
+  }
+};
+__device__ __forceinline__ Ask ask_rank(uint32_t rank) { return {true, false, rank, 0.0}; }
+__device__ __forceinline__ Ask ask_mass(double target, bool strict) { return {false, strict, 0u, target}; }
+
+// A walk down a run, value by value; true once the token is found.  `last`: the place to take should roundings leave none.
+struct Walk {
+  double cum;
+  uint32_t n;
+  Found f;
+  __device__ bool step(const Ask& a, uint32_t c, double w, uint32_t key) {
+    if (!c) return false;
+    const bool here = a.by_rank ? a.rank < n + c : reaches(cum + c * w, a.target, a.strict);
+    const uint32_t j = !here ? c : a.by_rank ? a.rank - n + 1 : tokens_until(cum, w, c, a.target, a.strict);
+    f.mass = cum + j * w;
+    f.rank = n + j - 1;
+    f.key = key;
+    f.nth = j - 1;
+    cum += c * w;
+    n += c;
+    return here;
+  }
+};
+
+// The first thread of this CTA whose run holds what is asked for, SM_THREADS if none does.
+__device__ __forceinline__ uint32_t first_thread(Shared& s, bool in) {
+  if (threadIdx.x == 0) s.owner = SM_THREADS;
+  __syncthreads();
+  const unsigned b = __ballot_sync(0xffffffffu, in);
+  if (b && (threadIdx.x & 31) == 0) atomicMin(&s.owner, threadIdx.x + __ffs(b) - 1);
+  __syncthreads();
+  const uint32_t o = s.owner;
+  __syncthreads();
+  return o;
+}
+
+// ---- bf16: counts of values -----------------------------------------------------------------------------------------------
+constexpr uint32_t WIN_LO = (127 - 32) << 7, WIN_HI = (127 + 16) << 7, WIN_BINS = WIN_HI - WIN_LO;   // magnitudes' bits
+constexpr int FINDS = 6;
+
+template <bool CLUSTER> struct WindowSums {
+  typedef bf16 T;
+  static constexpr int SMEM = 2 * WIN_BINS * 4 + (CLUSTER ? (WIN_BINS + 8) * 4 : 0);
+  uint32_t* bins;                   // [magnitude][sign]
+  uint32_t* merged;                 // this CTA's run of places, summed over the cluster
+  Shared& s;
+  Found* found;                     // [FINDS], one per find of a row, so that none is overwritten while the cluster reads it
+  uint32_t* valid;
+  int cta, ctas, finds = 0;
+  uint32_t hi, R, zeros, lo, p0, p1;    // places: positive values from magnitude hi down, zero at R, negative ones from lo up
+  uint32_t base;                    // first place of this CTA
+  double T1, top;
+  Runs q;
+
+  __device__ WindowSums(Shared& sh, Found* f, uint32_t* v, void* smem, int c, int n) : s(sh), found(f), valid(v), cta(c), ctas(n) {
+    bins = reinterpret_cast<uint32_t*>(smem);
+    merged = bins + 2 * WIN_BINS;
+  }
+  // Counts the row.  0, ROW_UNDEFINED (a NaN, +inf, or nothing finite) or ROW_OUTSIDE (values outside the window).
+  __device__ uint32_t count(const Share<bf16>& row) {
+    uint4* b4 = reinterpret_cast<uint4*>(bins);
+    for (int i = threadIdx.x; i < (int)(2 * WIN_BINS / 4); i += SM_THREADS) b4[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x == 0) {
+      s.top = s.hi = s.flags = s.zeros = 0u;
+      s.lo = 0xffffu;
+    }
+    __syncthreads();
+    const uint32_t at = smem_u32(bins) - 8 * WIN_LO;
+    uint32_t most = 0u, least = 0xffffffffu, zero = 0u, flags = 0u;   // magnitudes, two at a time
+    __nv_bfloat162 top2 = __float2bfloat162_rn(-INFINITY);
+    auto one = [&](uint32_t h) {
+      const uint32_t m = h & 0x7fffu;
+      if (m == 0u) ++zero;
+      else if (m >= 0x7f80u) {
+        if (h != 0xff80u) flags |= ROW_UNDEFINED;
+        return;
+      } else if (m < WIN_LO || m >= WIN_HI) flags |= ROW_OUTSIDE;
+      else {
+        add_shared(at + 8 * m + 4 * (h >> 15), 1u);
+        most = __vmaxu2(most, m);
+        least = __vminu2(least, m | 0xffff0000u);
+      }
+      const __nv_bfloat162 v = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)h));
+      top2 = __hmax2(top2, v);
+    };
+    auto eight = [&](const uint4& u) {
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      uint32_t mx = 0u, mn = 0xffffffffu;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        mx = __vmaxu2(mx, w[i] & 0x7fff7fffu);
+        mn = __vminu2(mn, w[i] & 0x7fff7fffu);
+      }
+      constexpr uint32_t C1 = (0x8000u - WIN_HI) * 0x10001u, C2 = (0x8000u - WIN_LO) * 0x10001u;
+      if ((((mx + C1) | ~(mn + C2)) & 0x80008000u) == 0u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // each half turned left by one bit: magnitude and then sign, the number of its bin
+          const uint32_t r = ((w[i] << 1) & 0xfffefffeu) | ((w[i] >> 15) & 0x00010001u);
+          add_shared(at + ((r << 2) & 0x3fffcu), 1u);
+          add_shared(at + ((r >> 14) & 0x3fffcu), 1u);
+          top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+        }
+        most = __vmaxu2(most, mx);
+        least = __vminu2(least, mn);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          one(w[i] & 0xffffu);
+          one(w[i] >> 16);
+        }
+      }
+    };
+    const uint4* w = row.words();
+    int v = row.v0 + (int)threadIdx.x;
+    for (; v + 3 * SM_THREADS < row.v1; v += 4 * SM_THREADS) {
+      uint4 u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = w[v + i * SM_THREADS];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) eight(u[i]);
+    }
+    for (; v < row.v1; v += SM_THREADS) eight(w[v]);
+    const uint16_t* raw = reinterpret_cast<const uint16_t*>(row.row);
+    if (row.first && (int)threadIdx.x < row.head) one(raw[threadIdx.x]);
+    if (row.last && row.tail0 + (int)threadIdx.x < row.vocab) one(raw[row.tail0 + threadIdx.x]);
+
+    const uint32_t hi1 = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
+    const uint32_t lo1 = __reduce_min_sync(0xffffffffu, min(least & 0xffffu, least >> 16));
+    const uint32_t top1 = __reduce_max_sync(0xffffffffu, key_of(fmaxf(__low2float(top2), __high2float(top2))));
+    const uint32_t zero1 = warp_sum(zero);
+    flags = __reduce_or_sync(0xffffffffu, flags);
+    if ((threadIdx.x & 31) == 0) {
+      atomicMax(&s.hi, hi1);
+      atomicMin(&s.lo, lo1);
+      atomicMax(&s.top, top1);
+      atomicAdd(&s.zeros, zero1);
+      atomicOr(&s.flags, flags);
+    }
+    row_sync<CLUSTER>();
+    uint32_t t = s.top, f = s.flags;
+    hi = s.hi; lo = s.lo; zeros = s.zeros;
+    if (CLUSTER) {
+      hi = t = f = zeros = 0u;
+      lo = 0xffffu;
+      for (int c = 0; c < ctas; ++c) {
+        hi = max(hi, ld_cluster_u32(mapa_u32(smem_u32(&s.hi), c)));
+        lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
+        t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
+        f |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
+        zeros += ld_cluster_u32(mapa_u32(smem_u32(&s.zeros), c));
+      }
+    }
+    top = (double)value_of(t);
+    if ((f & ROW_UNDEFINED) || t == key_of(-INFINITY)) return ROW_UNDEFINED;
+    return f & ROW_OUTSIDE;
+  }
+  // bin and value of a place
+  __device__ uint32_t bin_of(uint32_t p) const { return p < R ? 2 * (hi - p - WIN_LO) : 2 * (lo + (p - R - 1) - WIN_LO) + 1; }
+  __device__ float value(uint32_t p) const {
+    return p == R ? 0.f : __uint_as_float(p < R ? (hi - p) << 16 : 0x80000000u | (lo + (p - R - 1)) << 16);
+  }
+  __device__ uint32_t tokens(uint32_t p) const { return CLUSTER ? merged[p - base] : p == R ? zeros : bins[bin_of(p)]; }
+  __device__ double largest_value() const { return top; }
+  __device__ double weight(uint32_t p) const { return exp(((double)value(p) - top) / T1); }
+
+  __device__ void sum(const Share<bf16>&, const Settings& set) {
+    T1 = set.greedy ? 1.0 : set.T;
+    R = hi >= lo ? hi - lo + 1 : 0u;
+    const uint32_t places = 2 * R + 1;
+    base = (uint32_t)((unsigned long long)places * cta / ctas);
+    const uint32_t end = (uint32_t)((unsigned long long)places * (cta + 1) / ctas);
+    if (CLUSTER) {
+      for (uint32_t p = base + threadIdx.x; p < end; p += SM_THREADS) {
+        uint32_t c = zeros;
+        if (p != R) {
+          const uint32_t a = smem_u32(bins + bin_of(p));
+          c = 0u;
+          for (int i = 0; i < ctas; ++i) c += ld_cluster_u32(mapa_u32(a, i));
+        }
+        merged[p - base] = c;
+      }
+      __syncthreads();
+    }
+    const uint32_t each = (end - base + SM_THREADS - 1) / SM_THREADS;
+    p0 = min(end, base + each * threadIdx.x);
+    p1 = min(end, p0 + each);
+    q.n = 0u;
+    q.w = 0.0;
+    uint32_t nm = 0u;
+    double m = 0.0, raw = 0.0;
+    for (uint32_t p = p0; p < p1; ++p) {
+      const uint32_t c = tokens(p);
+      if (!c) continue;
+      const double w = weight(p), cw = c * w;
+      q.n += c;
+      q.w += cw;
+      raw += T1 == 1.0 ? cw : c * exp((double)value(p) - top);
+      if (w >= set.min_p) {
+        nm += c;
+        m += cw;
+      }
+    }
+    sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
+  }
+  __device__ Found find(const Share<bf16>&, const Ask& ask) {
+    const uint32_t o = first_thread(s, ask.in(q));
+    const int slot = finds++;
+    if (threadIdx.x == 0 && o == SM_THREADS) valid[slot] = 0u;
+    if (threadIdx.x == o) {
+      Walk k;
+      k.cum = q.excl_w;
+      k.n = q.excl_n;
+      for (uint32_t p = p0; p < p1; ++p) {
+        const uint32_t c = tokens(p);
+        if (c && k.step(ask, c, weight(p), key_of(value(p)))) break;
+      }
+      found[slot] = k.f;
+      valid[slot] = 1u;
+    }
+    row_sync<CLUSTER>();
+    for (int c = 0; CLUSTER && c < ctas; ++c)
+      if (ld_cluster_u32(mapa_u32(smem_u32(valid + slot), c))) {
+        const uint32_t a = mapa_u32(smem_u32(found + slot), c);
+        Found f;
+        f.mass = ld_cluster_f64(a + offsetof(Found, mass));
+        f.rank = ld_cluster_u32(a + offsetof(Found, rank));
+        f.key = ld_cluster_u32(a + offsetof(Found, key));
+        f.nth = ld_cluster_u32(a + offsetof(Found, nth));
+        return f;
+      }
+    return !CLUSTER && valid[slot] ? found[slot] : find_last();
+  }
+  // no run reached the target, by roundings: a rank behind the last
+  __device__ Found find_last() const { return {q.total_w, 0xffffffffu, 0u, 0u}; }
+};
+
+// ---- any type: a radix search with exact sums ---------------------------------------------------------------------------------
+// Levels of the ordered key, highest bits first.  The last level's bins are single values.
+template <typename T> struct RadixLevels {
+  static constexpr int N = sizeof(T) == 2 ? 2 : 3;
+  __host__ __device__ static constexpr int bits(int l) { return l == 0 ? 11 : sizeof(T) == 2 ? 5 : l == 1 ? 11 : 10; }
+  __host__ __device__ static constexpr int shift(int l) { return l == 0 ? 21 : sizeof(T) == 2 ? 16 : l == 1 ? 10 : 0; }
+};
+
+constexpr int LIMBS = 4, LIMB_BITS = 14;   // of a weight in units of 2^-56; 2^17 tokens to a CTA fit a 32-bit sum of limbs
+
+template <typename T, bool CLUSTER> struct RadixSums {
+  typedef RadixLevels<T> L;
+  static constexpr int BINS0 = 1 << 11, BINS1 = 1 << L::bits(1);
+  static constexpr int SMEM = (BINS0 + BINS1) * (1 + LIMBS) * 4;
+  uint32_t *bins0, *bins1;          // [1 + LIMBS][bins]: tokens, limbs
+  Shared& s;
+  Found* found;
+  int cta, ctas;
+  double T1;
+  float topf;
+  Runs q;
+  static constexpr int EACH = BINS0 / SM_THREADS;
+  uint32_t c0[EACH];                // this thread's bins of the first level, from the top
+  double w0[EACH];
+
+  __device__ RadixSums(Shared& sh, Found* f, void* smem, int c, int n) : s(sh), found(f), cta(c), ctas(n) {
+    bins0 = reinterpret_cast<uint32_t*>(smem);
+    bins1 = bins0 + BINS0 * (1 + LIMBS);
+  }
+  // the row's largest logit; 0 or ROW_UNDEFINED
+  __device__ uint32_t largest(const Share<T>& row) {
+    if (threadIdx.x == 0) s.top = s.flags = 0u;
+    __syncthreads();
+    uint32_t t = 0u, flags = 0u;
+    row.each([&](float x) {
+      if (!(x < INFINITY)) flags |= ROW_UNDEFINED;   // NaN or +inf
+      t = max(t, key_of(x));
+    });
+    t = __reduce_max_sync(0xffffffffu, t);
+    flags = __reduce_or_sync(0xffffffffu, flags);
+    if ((threadIdx.x & 31) == 0) {
+      atomicMax(&s.top, t);
+      atomicOr(&s.flags, flags);
+    }
+    row_sync<CLUSTER>();
+    t = s.top;
+    flags = s.flags;
+    if (CLUSTER)
+      for (int c = 0; c < ctas; ++c) {
+        t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
+        flags |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
+      }
+    topf = value_of(t);
+    return flags || t == key_of(-INFINITY) ? ROW_UNDEFINED : 0u;
+  }
+  __device__ double largest_value() const { return (double)topf; }
+  __device__ double weight(float x) const { return exp(((double)x - (double)topf) / T1); }
+  __device__ static void add(uint32_t* bins, int n, uint32_t bin, double w) {
+    const uint32_t a = smem_u32(bins + bin);
+    unsigned long long v = __double2ull_rn(w * 72057594037927936.0);   // 2^56
+    add_shared(a, 1u);
+#pragma unroll
+    for (int i = 0; i < LIMBS; ++i) {
+      const uint32_t limb = i + 1 < LIMBS ? (uint32_t)v & ((1u << LIMB_BITS) - 1) : (uint32_t)v;
+      if (limb) add_shared(a + 4 * n * (i + 1), limb);
+      v >>= LIMB_BITS;
+    }
+  }
+  // a bin summed over the row
+  __device__ void bin_sum(uint32_t* bins, int n, uint32_t bin, uint32_t& c, double& w) const {
+    const uint32_t a = smem_u32(bins + bin);
+    uint32_t total = 0u;
+    unsigned long long limb[LIMBS] = {};
+    for (int i = 0; i < (CLUSTER ? ctas : 1); ++i) {
+      const uint32_t b = CLUSTER ? mapa_u32(a, i) : 0u;
+      total += CLUSTER ? ld_cluster_u32(b) : bins[bin];
+#pragma unroll
+      for (int l = 0; l < LIMBS; ++l) limb[l] += CLUSTER ? ld_cluster_u32(b + 4 * n * (l + 1)) : bins[bin + n * (l + 1)];
+    }
+    c = total;
+    double v = 0.0;
+#pragma unroll
+    for (int l = LIMBS - 1; l >= 0; --l) v = v * (double)(1 << LIMB_BITS) + (double)limb[l];
+    w = v * 1.3877787807814457e-17;                 // 2^-56
+  }
+  __device__ void clear(uint32_t* bins, int n) {
+    for (int i = threadIdx.x; i < n * (1 + LIMBS); i += SM_THREADS) bins[i] = 0u;
+    __syncthreads();
+  }
+  __device__ void sum(const Share<T>& row, const Settings& set) {
+    T1 = set.greedy ? 1.0 : set.T;
+    row_sync<CLUSTER>();                            // nobody reads what this memory held before
+    clear(bins0, BINS0);
+    uint32_t nm = 0u;
+    double m = 0.0, raw = 0.0;
+    row.each([&](float x) {
+      if (x == -INFINITY) return;
+      const double w = weight(x);
+      add(bins0, BINS0, key_of(x) >> L::shift(0), w);
+      raw += T1 == 1.0 ? w : (double)expf(x - topf);
+      if (w >= set.min_p) {
+        ++nm;
+        m += w;
+      }
+    });
+    q.n = 0u;
+    q.w = 0.0;
+    sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
+    const Runs all = q;
+    if (!CLUSTER) __syncthreads();
+    q.n = 0u;
+    q.w = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      bin_sum(bins0, BINS0, BINS0 - 1 - (threadIdx.x * EACH + i), c0[i], w0[i]);
+      q.n += c0[i];
+      q.w += w0[i];
+    }
+    sum_runs<false>(s, q, 0u, 0.0, 0.0, 1, 0);
+    q.total_nm = all.total_nm;
+    q.total_m = all.total_m;
+    q.total_raw = all.total_raw;
+  }
+  // one level: whose run holds it, and there the bin; every CTA finds the same
+  template <int E> __device__ Found walk_bins(Ask ask, bool whole_row, const Runs& r, const uint32_t* c, const double* w, uint32_t first_bin, double* before_w, uint32_t* before_n) {
+    uint32_t o = first_thread(s, ask.in(r));
+    if (o == SM_THREADS) {                           // by roundings: the last token of the row, or of the opened bin
+      if (whole_row) return find_last();
+      ask = ask_rank(*before_n + r.total_n - 1);
+      o = first_thread(s, ask.in(r));
+    }
+    if (threadIdx.x == o) {
+      Walk k;
+      k.cum = r.excl_w;
+      k.n = r.excl_n;
+      double bw = k.cum;
+      uint32_t bn = k.n;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        if (!c[i]) continue;
+        bw = k.cum;
+        bn = k.n;
+        if (k.step(ask, c[i], w[i] / c[i], first_bin - i)) break;
+      }
+      found[0] = k.f;
+      s.before_w = bw;
+      s.before_n = bn;
+    }
+    __syncthreads();
+    *before_w = s.before_w;
+    *before_n = s.before_n;
+    const Found f = found[0];
+    __syncthreads();
+    return f;
+  }
+  __device__ Found find_last() const { return {q.total_w, 0xffffffffu, 0u, 0u}; }
+  __device__ Found find(const Share<T>& row, const Ask& ask) {
+    double before_w;
+    uint32_t before_n;
+    Found f = walk_bins<EACH>(ask, true, q, c0, w0, BINS0 - 1 - threadIdx.x * EACH, &before_w, &before_n);
+    uint32_t prefix = f.key;
+#pragma unroll
+    for (int l = 1; l < L::N; ++l) {
+      if (f.rank == 0xffffffffu) return f;
+      row_sync<CLUSTER>();                          // nobody reads these bins any more
+      const int n = 1 << L::bits(l);
+      clear(bins1, BINS1);
+      row.each([&](float x) {
+        const uint32_t k = key_of(x);
+        if (k >> L::shift(l - 1) == prefix && x != -INFINITY) add(bins1, BINS1, (k >> L::shift(l)) & (n - 1), weight(x));
+      });
+      row_sync<CLUSTER>();
+      constexpr int E = BINS1 < SM_THREADS ? 1 : BINS1 / SM_THREADS;
+      uint32_t c[E];
+      double w[E];
+      Runs r;
+      r.n = 0u;
+      r.w = 0.0;
+      const int first = n - 1 - (int)threadIdx.x * E;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        c[i] = 0u;
+        w[i] = 0.0;
+        if (first - i >= 0) bin_sum(bins1, BINS1, first - i, c[i], w[i]);
+        r.n += c[i];
+        r.w += w[i];
+      }
+      sum_runs<false>(s, r, 0u, 0.0, 0.0, 1, 0);
+      r.excl_n += before_n; r.incl_n += before_n;
+      r.excl_w += before_w; r.incl_w += before_w;
+      f = walk_bins<E>(ask, false, r, c, w, (uint32_t)first, &before_w, &before_n);
+      prefix = prefix << L::bits(l) | f.key;
+    }
+    f.key = prefix << L::shift(L::N - 1);
+    if (!(f.key >> 31)) f.key |= (1u << L::shift(L::N - 1)) - 1;   // a negative number's key is its complement
+    return f;
+  }
+};
+
+// The settings' prefix and the token drawn from it.
+template <typename S, typename T> __device__ Found draw(S& sums, const Share<T>& row, const Settings& set, uint32_t& kept) {
+  const Runs& q = sums.q;
+  uint32_t n = q.total_n;
+  double mass = q.total_w;
+  if (set.greedy) {
+    kept = 1u;
+    return sums.find(row, ask_rank(0u));
+  }
+  if (set.top_k > 0 && (uint32_t)set.top_k < n) {
+    n = (uint32_t)set.top_k;
+    mass = sums.find(row, ask_rank(n - 1)).mass;
+  }
+  if (set.top_p < 1.0) {
+    const Found f = sums.find(row, ask_mass(set.top_p * mass, false));
+    if (f.rank < n - 1) {
+      n = f.rank + 1;
+      mass = f.mass;
+    }
+  }
+  if (q.total_nm < n) {                              // min-p keeps the largest at least: its weight is 1
+    n = q.total_nm;
+    mass = q.total_m;
+  }
+  kept = n;
+  const Found f = sums.find(row, ask_mass((double)set.u * mass, true));
+  return f.rank < n ? f : sums.find(row, ask_rank(n - 1));
+}
+
+// The nth token whose value has this key: a count over the row, then the one warp's words that hold it once more.
+template <typename T> __device__ __forceinline__ uint32_t matches_of(const uint4& u, float x) {   // a bit for each
+  const T* e = reinterpret_cast<const T*>(&u);
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) m |= (to_f(e[i]) == x ? 1u : 0u) << i;
+  return m;
+}
+template <typename T, bool CLUSTER>
+__device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int cta, int ctas, int32_t* token) {
+  constexpr int V = Share<T>::V;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float x = value_of(f.key);
+  const uint4* words = row.words();
+  const int a = row.v0 + (int)((long long)(row.v1 - row.v0) * warp / SM_WARPS), b = row.v0 + (int)((long long)(row.v1 - row.v0) * (warp + 1) / SM_WARPS);
+  const int heads = row.first && warp == 0 ? row.head : 0, tails = row.last && warp == SM_WARPS - 1 ? row.vocab - row.tail0 : 0;
+  uint32_t n = 0u;
+  for (int v = a + lane; v < b; v += 32) n += __popc(matches_of<T>(words[v], x));
+  const bool in_head = lane < heads && to_f(row.row[lane]) == x, in_tail = lane < tails && to_f(row.row[row.tail0 + lane]) == x;
+  n = warp_sum(n + in_head + in_tail);
+  if (lane == 0) s.matches[warp] = n;
+  __syncthreads();
+  uint32_t before = 0u, all = 0u;
+  for (int i = 0; i < SM_WARPS; ++i) {
+    if (i == warp) before = all;
+    all += s.matches[i];
+  }
+  if (CLUSTER) {
+    if (threadIdx.x == 0) s.cta_matches = all;
+    cluster_sync_all();
+    for (int c = 0; c < cta; ++c) before += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_matches), c));
+  }
+  if (f.nth < before || f.nth >= before + n) return;
+  uint32_t left = f.nth - before;                    // of this warp's tokens of that value
+  const uint32_t head_at = __ballot_sync(0xffffffffu, in_head);
+  if (left < (uint32_t)__popc(head_at)) {
+    if (in_head && (uint32_t)__popc(head_at & ((1u << lane) - 1)) == left) *token = lane;
+    return;
+  }
+  left -= __popc(head_at);
+  for (int v0 = a; v0 < b; v0 += 32) {
+    const int v = v0 + lane;
+    uint32_t m = v < b ? matches_of<T>(words[v], x) : 0u, sum = __popc(m);
+    const uint32_t mine = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const uint32_t here = __shfl_sync(0xffffffffu, sum, 31);
+    if (left < here) {
+      if (sum > left && sum - mine <= left) {
+        for (uint32_t skip = left - (sum - mine); skip > 0; --skip) m &= m - 1;
+        *token = row.head + v * V + __ffs(m) - 1;
+      }
+      return;
+    }
+    left -= here;
+  }
+  const uint32_t tail_at = __ballot_sync(0xffffffffu, in_tail);
+  if (in_tail && (uint32_t)__popc(tail_at & ((1u << lane) - 1)) == left) *token = row.tail0 + lane;
+}
+
+template <typename T, bool CLUSTER> struct SampleSmem {
+  static constexpr int BYTES = RadixSums<T, CLUSTER>::SMEM;
+};
+template <bool CLUSTER> struct SampleSmem<bf16, CLUSTER> {
+  static constexpr int W = WindowSums<CLUSTER>::SMEM, R = RadixSums<bf16, CLUSTER>::SMEM, BYTES = W > R ? W : R;
+};
+
+template <typename S, typename T, bool CLUSTER>
+__device__ void finish(Shared& s, S& sums, const Share<T>& row, const Settings& set, const SampleArgs& a, int r, int cta, int ctas) {
+  sums.sum(row, set);
+  uint32_t kept;
+  const Found f = draw(sums, row, set, kept);
+  write_token<T, CLUSTER>(s, row, f, cta, ctas, a.token + r);
+  if (cta == 0 && threadIdx.x == 0) {
+    if (a.conf) a.conf[r] = (float)(exp((double)value_of(f.key) - sums.largest_value()) / sums.q.total_raw);
+    if (a.n_kept) a.n_kept[r] = (int32_t)kept;
+  }
+}
+
+template <typename T, bool CLUSTER>
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(SampleArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Shared s;
+  __shared__ Found found[FINDS];
+  __shared__ uint32_t valid[FINDS];
+  griddep_wait();
+  griddep_launch();
+  int cta = 0, ctas = 1;
+  if (CLUSTER) {
+    uint32_t n;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+    ctas = (int)n;
+    cta = (int)cluster_ctarank();
+  }
+  const int r = blockIdx.x / ctas;
+  if (r >= min(*a.n_active, a.max_rows)) return;
+  Settings set;
+  {
+    const int i = a.set_of_row ? a.set_of_row[r] : a.sets.n_sets == 1 ? 0 : r;
+    set.ok = (unsigned)i < (unsigned)a.sets.n_sets;
+    if (!set.ok && threadIdx.x == 0) set_status(a.status, SL_DEV_BAD_INDEX);
+    const int j = set.ok ? i : 0;
+    const float t = a.sets.temperature ? a.sets.temperature[j] : 1.f;
+    set.ok = set.ok && t >= 0.f;                     // not where it is NaN
+    set.greedy = t == 0.f;
+    set.T = t;
+    set.top_k = a.sets.top_k ? a.sets.top_k[j] : 0;
+    const float p = a.sets.top_p ? a.sets.top_p[j] : 1.f, m = a.sets.min_p ? a.sets.min_p[j] : 0.f;
+    set.top_p = p < 1.f ? (double)p : 1.0;
+    set.min_p = m > 0.f ? (double)fminf(m, 1.f) : 0.0;
+    set.u = fminf(fmaxf(a.u[r], 0.f), 0.99999994f);
+  }
+  const Share<T> row((const T*)a.logits + r * a.row_stride, a.vocab, cta, ctas);
+  uint32_t state = ROW_UNDEFINED;
+  if (set.ok) {
+    if constexpr (sizeof(T) == 2) {
+      WindowSums<CLUSTER> sums(s, found, valid, smem, cta, ctas);
+      state = sums.count(row);
+      if (state == 0u) finish<WindowSums<CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+      if (state == ROW_OUTSIDE) {
+        RadixSums<T, CLUSTER> other(s, found, smem, cta, ctas);
+        other.topf = (float)sums.top;
+        finish<RadixSums<T, CLUSTER>, T, CLUSTER>(s, other, row, set, a, r, cta, ctas);
+      }
+    } else {
+      RadixSums<T, CLUSTER> sums(s, found, smem, cta, ctas);
+      state = sums.largest(row);
+      if (state == 0u) finish<RadixSums<T, CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+    }
+  }
+  if (state == ROW_UNDEFINED && cta == 0 && threadIdx.x == 0) {
+    a.token[r] = -1;
+    if (a.conf) a.conf[r] = __int_as_float(0x7fffffff);
+    if (a.n_kept) a.n_kept[r] = 0;
+  }
+  if (CLUSTER) cluster_sync_all();                   // nobody reads this CTA's shared memory any more
+}
+
+template <typename T, bool CLUSTER>
+int launch_sample_ctas(const SampleArgs& a, int ctas, cudaStream_t st) {
+  constexpr int bytes = SampleSmem<T, CLUSTER>::BYTES;
+  static std::atomic<uint64_t> done{0};
+  SL_CUDA_TRY(allow_smem(sample_kernel<T, CLUSTER>, bytes, done));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)a.max_rows * ctas);
+  cfg.blockDim = dim3(SM_THREADS);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ctas;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = pdl_enabled() ? at : at + 1;
+  cfg.numAttrs = (pdl_enabled() ? 1 : 0) + (CLUSTER ? 1 : 0);
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<T, CLUSTER>, a));
+  return SL_OK;
+}
+
+template <typename T> int launch_sample_typed(const SampleArgs& a, cudaStream_t st) {
+  int ctas = 8;
+  while (ctas > 1 && ((long long)a.max_rows * ctas > 2ll * sm_count() || a.vocab < ctas * 4096)) ctas >>= 1;
+  while (a.vocab / ctas > (1 << 17) - 16) ctas <<= 1;   // limbs' sums are 32 bits wide
+  if ((long long)a.max_rows * ctas > 0x7fffffffll) return SL_EUNSUPPORTED;
+  return ctas > 1 ? launch_sample_ctas<T, true>(a, ctas, st) : launch_sample_ctas<T, false>(a, ctas, st);
+}
+
+}  // namespace
+
+int launch_sample(const void* logits, long long row_stride, const surelock_sampling& sets, const int32_t* set_of_row, const float* u,
+                  const int32_t* n_active, int max_rows, int vocab, int dtype, int32_t* token, float* conf, int32_t* n_kept,
+                  int32_t* status, cudaStream_t st) {
+  SampleArgs a = {logits, row_stride, sets, set_of_row, n_active, u, token, n_kept, status, conf, max_rows, vocab};
+  if (vocab > (1 << 20) - 128) return SL_EUNSUPPORTED;
+  return dtype == SL_BF16 ? launch_sample_typed<bf16>(a, st) : launch_sample_typed<float>(a, st);
+}
+
+}  // namespace sl
