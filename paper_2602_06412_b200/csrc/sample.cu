@@ -15,9 +15,9 @@
 // a thread.  The token's index is found by a second pass that counts the tokens of the value that was drawn, out of the L2.  A row with a
 // finite value outside the window (not zero) is done by the other method.
 //
-// fp32 rows (RadixSums): a radix search with 11 + 11 + 10 bits of the ordered key.  A pass adds every token's weight, as four
-// 14-bit limbs of a fixed-point number (exact sums in any order), to its bin; the bin in question is then opened by another pass
-// over the row's tokens in it.
+// fp32 rows (BinnedSums): 2048 bins of equal width over the values that weigh anything.  One pass adds every token's weight, as four limbs of
+// a fixed-point number (exact sums in any order), to its bin; a bin that is asked for is opened by another pass over the row's tokens
+// in it: a few are ranked against one another, more of them are binned once more by their keys.
 //
 // A row is one CTA's work, or with few rows that of a cluster of CTAs, whose shares meet through distributed shared memory.
 #include "tc_common.cuh"
@@ -95,11 +95,11 @@ template <typename T> struct Share {
   }
 };
 
-// a token by its place in the order: its rank (0 = the largest), the sum of weights up to and with it, its value and which of the
-// tokens of that value it is
+// a token by its place in the order: its rank (0 = the largest), the sum of weights up to and with it, its value (or bin) and which of
+// the tokens of that value it is; for a bin also its tokens and what lies before it
 struct Found {
-  double mass;
-  uint32_t rank, key, nth;
+  double mass, before_w;
+  uint32_t rank, key, nth, before_n, tokens, valid;
 };
 
 struct Shared {                     // beside the bins
@@ -107,9 +107,8 @@ struct Shared {                     // beside the bins
   uint32_t part_n[SM_WARPS], part_nm[SM_WARPS], matches[SM_WARPS];
   double cta_w, cta_m, cta_raw;     // this CTA's sums, read by the cluster
   uint32_t cta_n, cta_nm, cta_matches;
-  uint32_t top, lo, hi, flags, zeros;
-  uint32_t owner, before_n;
-  double before_w;
+  uint32_t top, lo, hi, flags, zeros, list_n, owner;
+  Found found[2], here;             // found: by turns, so that none is overwritten while the cluster reads it
 };
 
 enum { ROW_UNDEFINED = 1, ROW_OUTSIDE = 2 };
@@ -246,6 +245,9 @@ struct Walk {
     f.rank = n + j - 1;
     f.key = key;
     f.nth = j - 1;
+    f.before_w = cum;
+    f.before_n = n;
+    f.tokens = c;
     cum += c * w;
     n += c;
     return here;
@@ -264,25 +266,67 @@ __device__ __forceinline__ uint32_t first_thread(Shared& s, bool in) {
   return o;
 }
 
+// What both methods share: whose run holds what is asked for, its walk there, and the answer for all threads of the row.
+template <bool CLUSTER> struct Finder {
+  Shared& s;
+  int cta, ctas, turn = 0;
+  Runs q;
+  double T1;
+  __device__ Finder(Shared& sh, int c, int n) : s(sh), cta(c), ctas(n) {}
+  template <typename F> __device__ Found search(const Ask& ask, const Runs& r, F walk) {
+    const uint32_t o = first_thread(s, ask.in(r));
+    Found& mine = s.found[turn];
+    turn ^= 1;
+    if (threadIdx.x == 0 && o == SM_THREADS) mine.valid = 0u;
+    if (threadIdx.x == o) {
+      Walk k;
+      k.cum = r.excl_w;
+      k.n = r.excl_n;
+      walk(k);
+      k.f.valid = 1u;
+      mine = k.f;
+    }
+    row_sync<CLUSTER>();
+    if (!CLUSTER) return mine;
+    Found f;
+    f.valid = 0u;
+    for (int c = 0; c < ctas && !f.valid; ++c) {
+      const uint32_t a = mapa_u32(smem_u32(&mine), c);
+      f.valid = ld_cluster_u32(a + offsetof(Found, valid));
+      if (!f.valid) continue;
+      f.mass = ld_cluster_f64(a + offsetof(Found, mass));
+      f.before_w = ld_cluster_f64(a + offsetof(Found, before_w));
+      f.rank = ld_cluster_u32(a + offsetof(Found, rank));
+      f.key = ld_cluster_u32(a + offsetof(Found, key));
+      f.nth = ld_cluster_u32(a + offsetof(Found, nth));
+      f.before_n = ld_cluster_u32(a + offsetof(Found, before_n));
+      f.tokens = ld_cluster_u32(a + offsetof(Found, tokens));
+    }
+    return f;
+  }
+  // no run reached the target, by roundings: it is behind the last token
+  __device__ static Found behind_all(double mass) {
+    Found f = {};
+    f.mass = mass;
+    f.rank = 0xffffffffu;
+    return f;
+  }
+};
+
 // ---- bf16: counts of values -----------------------------------------------------------------------------------------------
 constexpr uint32_t WIN_LO = (127 - 32) << 7, WIN_HI = (127 + 16) << 7, WIN_BINS = WIN_HI - WIN_LO;   // magnitudes' bits
-constexpr int FINDS = 6;
 
-template <bool CLUSTER> struct WindowSums {
-  typedef bf16 T;
+template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
+  typedef Finder<CLUSTER> F;
+  using F::s; using F::cta; using F::ctas; using F::q; using F::T1;
   static constexpr int SMEM = 2 * WIN_BINS * 4 + (CLUSTER ? (WIN_BINS + 8) * 4 : 0);
   uint32_t* bins;                   // [magnitude][sign]
   uint32_t* merged;                 // this CTA's run of places, summed over the cluster
-  Shared& s;
-  Found* found;                     // [FINDS], one per find of a row, so that none is overwritten while the cluster reads it
-  uint32_t* valid;
-  int cta, ctas, finds = 0;
   uint32_t hi, R, zeros, lo, p0, p1;    // places: positive values from magnitude hi down, zero at R, negative ones from lo up
   uint32_t base;                    // first place of this CTA
-  double T1, top;
-  Runs q;
+  double top;
 
-  __device__ WindowSums(Shared& sh, Found* f, uint32_t* v, void* smem, int c, int n) : s(sh), found(f), valid(v), cta(c), ctas(n) {
+  __device__ WindowSums(Shared& sh, void* smem, int c, int n) : F(sh, c, n) {
     bins = reinterpret_cast<uint32_t*>(smem);
     merged = bins + 2 * WIN_BINS;
   }
@@ -394,7 +438,7 @@ template <bool CLUSTER> struct WindowSums {
   __device__ double largest_value() const { return top; }
   __device__ double weight(uint32_t p) const { return exp(((double)value(p) - top) / T1); }
 
-  __device__ void sum(const Share<bf16>&, const Settings& set) {
+  __device__ void sum(const Settings& set) {
     T1 = set.greedy ? 1.0 : set.T;
     R = hi >= lo ? hi - lo + 1 : 0u;
     const uint32_t places = 2 * R + 1;
@@ -434,233 +478,277 @@ template <bool CLUSTER> struct WindowSums {
     sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
   }
   __device__ Found find(const Share<bf16>&, const Ask& ask) {
-    const uint32_t o = first_thread(s, ask.in(q));
-    const int slot = finds++;
-    if (threadIdx.x == 0 && o == SM_THREADS) valid[slot] = 0u;
-    if (threadIdx.x == o) {
-      Walk k;
-      k.cum = q.excl_w;
-      k.n = q.excl_n;
+    const Found f = F::search(ask, q, [&](Walk& k) {
       for (uint32_t p = p0; p < p1; ++p) {
         const uint32_t c = tokens(p);
         if (c && k.step(ask, c, weight(p), key_of(value(p)))) break;
       }
-      found[slot] = k.f;
-      valid[slot] = 1u;
-    }
-    row_sync<CLUSTER>();
-    for (int c = 0; CLUSTER && c < ctas; ++c)
-      if (ld_cluster_u32(mapa_u32(smem_u32(valid + slot), c))) {
-        const uint32_t a = mapa_u32(smem_u32(found + slot), c);
-        Found f;
-        f.mass = ld_cluster_f64(a + offsetof(Found, mass));
-        f.rank = ld_cluster_u32(a + offsetof(Found, rank));
-        f.key = ld_cluster_u32(a + offsetof(Found, key));
-        f.nth = ld_cluster_u32(a + offsetof(Found, nth));
-        return f;
-      }
-    return !CLUSTER && valid[slot] ? found[slot] : find_last();
+    });
+    return f.valid ? f : F::behind_all(q.total_w);
   }
-  // no run reached the target, by roundings: a rank behind the last
-  __device__ Found find_last() const { return {q.total_w, 0xffffffffu, 0u, 0u}; }
 };
 
-// ---- any type: a radix search with exact sums ---------------------------------------------------------------------------------
-// Levels of the ordered key, highest bits first.  The last level's bins are single values.
-template <typename T> struct RadixLevels {
-  static constexpr int N = sizeof(T) == 2 ? 2 : 3;
-  __host__ __device__ static constexpr int bits(int l) { return l == 0 ? 11 : sizeof(T) == 2 ? 5 : l == 1 ? 11 : 10; }
-  __host__ __device__ static constexpr int shift(int l) { return l == 0 ? 21 : sizeof(T) == 2 ? 16 : l == 1 ? 10 : 0; }
-};
+// ---- any type: bins with exact sums of weights ---------------------------------------------------------------------------------
+constexpr int BINS = 2048, LIMBS = 4, LIMB_BITS = 14;   // of a weight in units of 2^-54; 2^17 tokens to a CTA fit a 32-bit sum of limbs
+constexpr double WEIGHT_UNIT = 18014398509481984.0;     // 2^54
+constexpr int LIST = 256;                               // tokens that are ranked against one another
 
-constexpr int LIMBS = 4, LIMB_BITS = 14;   // of a weight in units of 2^-56; 2^17 tokens to a CTA fit a 32-bit sum of limbs
-
-template <typename T, bool CLUSTER> struct RadixSums {
-  typedef RadixLevels<T> L;
-  static constexpr int BINS0 = 1 << 11, BINS1 = 1 << L::bits(1);
-  static constexpr int SMEM = (BINS0 + BINS1) * (1 + LIMBS) * 4;
-  uint32_t *bins0, *bins1;          // [1 + LIMBS][bins]: tokens, limbs
-  Shared& s;
-  Found* found;
-  int cta, ctas;
-  double T1;
-  float topf;
-  Runs q;
-  static constexpr int EACH = BINS0 / SM_THREADS;
-  uint32_t c0[EACH];                // this thread's bins of the first level, from the top
+template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
+  typedef Finder<CLUSTER> F;
+  using F::s; using F::cta; using F::ctas; using F::q; using F::T1;
+  static constexpr int SMEM = BINS * (1 + LIMBS) * 4 + LIST * 16;
+  static constexpr int EACH = BINS / SM_THREADS;        // bins to a thread; in a cluster the CTAs share them out
+  uint32_t* bins;                   // [1 + LIMBS][BINS]: tokens, limbs
+  unsigned long long* weights;      // [LIST]
+  uint32_t *list, *keys;            // [LIST]: this CTA's tokens of a bin, and those of the whole row
+  float topf, step;                 // bins to a unit of the logits
+  uint32_t c0[EACH];                // this thread's bins, from the top
   double w0[EACH];
 
-  __device__ RadixSums(Shared& sh, Found* f, void* smem, int c, int n) : s(sh), found(f), cta(c), ctas(n) {
-    bins0 = reinterpret_cast<uint32_t*>(smem);
-    bins1 = bins0 + BINS0 * (1 + LIMBS);
+  __device__ BinnedSums(Shared& sh, void* smem, int c, int n) : F(sh, c, n) {
+    bins = reinterpret_cast<uint32_t*>(smem);
+    weights = reinterpret_cast<unsigned long long*>(bins + BINS * (1 + LIMBS));
+    list = reinterpret_cast<uint32_t*>(weights + LIST);
+    keys = list + LIST;
   }
-  // the row's largest logit; 0 or ROW_UNDEFINED
-  __device__ uint32_t largest(const Share<T>& row) {
-    if (threadIdx.x == 0) s.top = s.flags = 0u;
+  // the row's largest and smallest finite logits; 0 or ROW_UNDEFINED
+  __device__ uint32_t range(const Share<T>& row, float& least) {
+    row_sync<CLUSTER>();                            // nobody reads what these words held before
+    if (threadIdx.x == 0) {
+      s.top = s.flags = 0u;
+      s.lo = 0xffffffffu;
+    }
     __syncthreads();
-    uint32_t t = 0u, flags = 0u;
+    uint32_t t = 0u, lo = 0xffffffffu, flags = 0u;
     row.each([&](float x) {
       if (!(x < INFINITY)) flags |= ROW_UNDEFINED;   // NaN or +inf
-      t = max(t, key_of(x));
+      const uint32_t k = key_of(x);
+      t = max(t, k);
+      if (x != -INFINITY) lo = min(lo, k);
     });
     t = __reduce_max_sync(0xffffffffu, t);
+    lo = __reduce_min_sync(0xffffffffu, lo);
     flags = __reduce_or_sync(0xffffffffu, flags);
     if ((threadIdx.x & 31) == 0) {
       atomicMax(&s.top, t);
+      atomicMin(&s.lo, lo);
       atomicOr(&s.flags, flags);
     }
     row_sync<CLUSTER>();
     t = s.top;
+    lo = s.lo;
     flags = s.flags;
-    if (CLUSTER)
-      for (int c = 0; c < ctas; ++c) {
-        t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
-        flags |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
-      }
+    for (int c = 0; CLUSTER && c < ctas; ++c) {
+      t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
+      lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
+      flags |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
+    }
+    if (flags || lo == 0xffffffffu) return ROW_UNDEFINED;
     topf = value_of(t);
-    return flags || t == key_of(-INFINITY) ? ROW_UNDEFINED : 0u;
+    least = value_of(lo);
+    return 0u;
   }
   __device__ double largest_value() const { return (double)topf; }
-  __device__ double weight(float x) const { return exp(((double)x - (double)topf) / T1); }
-  __device__ static void add(uint32_t* bins, int n, uint32_t bin, double w) {
+  __device__ unsigned long long weight(float x) const { return __double2ull_rn(exp(((double)x - (double)topf) / T1) * WEIGHT_UNIT); }
+  // Falls with x; what is too far below the largest shares the last bin.
+  __device__ uint32_t bin_of(float x) const { return min((uint32_t)BINS - 1, __float2uint_rz((topf - x) * step)); }
+
+  __device__ void clear() {
+    for (int i = threadIdx.x; i < BINS * (1 + LIMBS) / 4; i += SM_THREADS) reinterpret_cast<uint4*>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+  }
+  __device__ void add(uint32_t bin, unsigned long long w) {
     const uint32_t a = smem_u32(bins + bin);
-    unsigned long long v = __double2ull_rn(w * 72057594037927936.0);   // 2^56
     add_shared(a, 1u);
 #pragma unroll
     for (int i = 0; i < LIMBS; ++i) {
-      const uint32_t limb = i + 1 < LIMBS ? (uint32_t)v & ((1u << LIMB_BITS) - 1) : (uint32_t)v;
-      if (limb) add_shared(a + 4 * n * (i + 1), limb);
-      v >>= LIMB_BITS;
+      const uint32_t limb = i + 1 < LIMBS ? (uint32_t)w & ((1u << LIMB_BITS) - 1) : (uint32_t)w;
+      if (limb) add_shared(a + 4 * BINS * (i + 1), limb);
+      w >>= LIMB_BITS;
     }
   }
-  // a bin summed over the row
-  __device__ void bin_sum(uint32_t* bins, int n, uint32_t bin, uint32_t& c, double& w) const {
-    const uint32_t a = smem_u32(bins + bin);
-    uint32_t total = 0u;
-    unsigned long long limb[LIMBS] = {};
-    for (int i = 0; i < (CLUSTER ? ctas : 1); ++i) {
-      const uint32_t b = CLUSTER ? mapa_u32(a, i) : 0u;
-      total += CLUSTER ? ld_cluster_u32(b) : bins[bin];
+  // this thread's bins summed over the row, and the runs they make
+  __device__ void collect(Runs& r, uint32_t* c, double* w, uint32_t& first, uint32_t nm, double m, double raw) {
+    const uint32_t per = CLUSTER ? BINS / ctas : BINS, each = (per + SM_THREADS - 1) / SM_THREADS;
+    first = cta * per + threadIdx.x * each;
+    r.n = 0u;
+    r.w = 0.0;
 #pragma unroll
-      for (int l = 0; l < LIMBS; ++l) limb[l] += CLUSTER ? ld_cluster_u32(b + 4 * n * (l + 1)) : bins[bin + n * (l + 1)];
+    for (int i = 0; i < EACH; ++i) {
+      c[i] = 0u;
+      w[i] = 0.0;
+      if (i >= (int)each || threadIdx.x * each + i >= per) continue;
+      const uint32_t a = smem_u32(bins + first + i);
+      unsigned long long limb[LIMBS] = {};
+      for (int p = 0; p < (CLUSTER ? ctas : 1); ++p) {
+        const uint32_t b = CLUSTER ? mapa_u32(a, p) : 0u;
+        c[i] += CLUSTER ? ld_cluster_u32(b) : bins[first + i];
+#pragma unroll
+        for (int l = 0; l < LIMBS; ++l) limb[l] += CLUSTER ? ld_cluster_u32(b + 4 * BINS * (l + 1)) : bins[first + i + BINS * (l + 1)];
+      }
+      double v = 0.0;
+#pragma unroll
+      for (int l = LIMBS - 1; l >= 0; --l) v = v * (double)(1 << LIMB_BITS) + (double)limb[l];
+      w[i] = v / WEIGHT_UNIT;
+      r.n += c[i];
+      r.w += w[i];
     }
-    c = total;
-    double v = 0.0;
+    sum_runs<CLUSTER>(s, r, nm, m, raw, ctas, cta);
+  }
+  // the bin that holds what is asked for
+  __device__ Found open(const Ask& ask, const Runs& r, const uint32_t* c, const double* w, uint32_t first) {
+    return F::search(ask, r, [&](Walk& k) {
 #pragma unroll
-    for (int l = LIMBS - 1; l >= 0; --l) v = v * (double)(1 << LIMB_BITS) + (double)limb[l];
-    w = v * 1.3877787807814457e-17;                 // 2^-56
+      for (int i = 0; i < EACH; ++i)
+        if (c[i] && k.step(ask, c[i], w[i] / c[i], first + i)) break;
+    });
   }
-  __device__ void clear(uint32_t* bins, int n) {
-    for (int i = threadIdx.x; i < n * (1 + LIMBS); i += SM_THREADS) bins[i] = 0u;
-    __syncthreads();
-  }
-  __device__ void sum(const Share<T>& row, const Settings& set) {
+  uint32_t first0;
+  __device__ void sum(const Share<T>& row, const Settings& set, float least) {
     T1 = set.greedy ? 1.0 : set.T;
-    row_sync<CLUSTER>();                            // nobody reads what this memory held before
-    clear(bins0, BINS0);
+    // beyond 50 T the weights are below 2^-72 of the largest
+    const float span = (float)fmin((double)topf - (double)least, 50.0 * T1);
+    step = span > 0.f ? fminf((float)BINS / span, 3.4e38f) : 0.f;
+    clear();
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
     row.each([&](float x) {
       if (x == -INFINITY) return;
-      const double w = weight(x);
-      add(bins0, BINS0, key_of(x) >> L::shift(0), w);
-      raw += T1 == 1.0 ? w : (double)expf(x - topf);
-      if (w >= set.min_p) {
+      const unsigned long long w = weight(x);
+      add(bin_of(x), w);
+      const double v = (double)w / WEIGHT_UNIT;
+      raw += T1 == 1.0 ? v : (double)expf(x - topf);
+      if (v >= set.min_p) {
         ++nm;
-        m += w;
+        m += v;
       }
     });
-    q.n = 0u;
-    q.w = 0.0;
-    sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
-    const Runs all = q;
-    if (!CLUSTER) __syncthreads();
-    q.n = 0u;
-    q.w = 0.0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      bin_sum(bins0, BINS0, BINS0 - 1 - (threadIdx.x * EACH + i), c0[i], w0[i]);
-      q.n += c0[i];
-      q.w += w0[i];
-    }
-    sum_runs<false>(s, q, 0u, 0.0, 0.0, 1, 0);
-    q.total_nm = all.total_nm;
-    q.total_m = all.total_m;
-    q.total_raw = all.total_raw;
+    row_sync<CLUSTER>();
+    collect(q, c0, w0, first0, nm, m, raw);
   }
-  // one level: whose run holds it, and there the bin; every CTA finds the same
-  template <int E> __device__ Found walk_bins(Ask ask, bool whole_row, const Runs& r, const uint32_t* c, const double* w, uint32_t first_bin, double* before_w, uint32_t* before_n) {
-    uint32_t o = first_thread(s, ask.in(r));
-    if (o == SM_THREADS) {                           // by roundings: the last token of the row, or of the opened bin
-      if (whole_row) return find_last();
-      ask = ask_rank(*before_n + r.total_n - 1);
-      o = first_thread(s, ask.in(r));
-    }
-    if (threadIdx.x == o) {
-      Walk k;
-      k.cum = r.excl_w;
-      k.n = r.excl_n;
-      double bw = k.cum;
-      uint32_t bn = k.n;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        if (!c[i]) continue;
-        bw = k.cum;
-        bn = k.n;
-        if (k.step(ask, c[i], w[i] / c[i], first_bin - i)) break;
+  // Members of a bin: of the first binning, and where that was not enough keys from ka to kb.
+  struct Members {
+    uint32_t bin, ka, kb;
+  };
+  __device__ bool in(const Members& b, float x, uint32_t k) const { return x != -INFINITY && bin_of(x) == b.bin && k >= b.ka && k <= b.kb; }
+
+  __device__ Found find(const Share<T>& row, const Ask& asked) {
+    Ask ask = asked;
+    Found f = open(ask, q, c0, w0, first0);
+    if (!f.valid) return F::behind_all(q.total_w);
+    Members b = {f.key, 0u, 0xffffffffu};
+    while (f.tokens > LIST) {
+      // the keys that occur, and bins for them
+      if (threadIdx.x == 0) {
+        s.hi = 0u;
+        s.lo = 0xffffffffu;
       }
-      found[0] = k.f;
-      s.before_w = bw;
-      s.before_n = bn;
-    }
-    __syncthreads();
-    *before_w = s.before_w;
-    *before_n = s.before_n;
-    const Found f = found[0];
-    __syncthreads();
-    return f;
-  }
-  __device__ Found find_last() const { return {q.total_w, 0xffffffffu, 0u, 0u}; }
-  __device__ Found find(const Share<T>& row, const Ask& ask) {
-    double before_w;
-    uint32_t before_n;
-    Found f = walk_bins<EACH>(ask, true, q, c0, w0, BINS0 - 1 - threadIdx.x * EACH, &before_w, &before_n);
-    uint32_t prefix = f.key;
-#pragma unroll
-    for (int l = 1; l < L::N; ++l) {
-      if (f.rank == 0xffffffffu) return f;
-      row_sync<CLUSTER>();                          // nobody reads these bins any more
-      const int n = 1 << L::bits(l);
-      clear(bins1, BINS1);
+      clear();
+      uint32_t lo = 0xffffffffu, hi = 0u;
       row.each([&](float x) {
         const uint32_t k = key_of(x);
-        if (k >> L::shift(l - 1) == prefix && x != -INFINITY) add(bins1, BINS1, (k >> L::shift(l)) & (n - 1), weight(x));
+        if (in(b, x, k)) {
+          lo = min(lo, k);
+          hi = max(hi, k);
+        }
+      });
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      hi = __reduce_max_sync(0xffffffffu, hi);
+      if ((threadIdx.x & 31) == 0) {
+        atomicMin(&s.lo, lo);
+        atomicMax(&s.hi, hi);
+      }
+      row_sync<CLUSTER>();
+      lo = s.lo;
+      hi = s.hi;
+      for (int c = 0; CLUSTER && c < ctas; ++c) {
+        lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
+        hi = max(hi, ld_cluster_u32(mapa_u32(smem_u32(&s.hi), c)));
+      }
+      if (lo == hi) {                               // one value: no need to look at its tokens
+        Walk k;
+        k.cum = f.before_w;
+        k.n = f.before_n;
+        k.step(ask, f.tokens, (double)weight(value_of(lo)) / WEIGHT_UNIT, lo);
+        row_sync<CLUSTER>();
+        return k.f;
+      }
+      const int shift = max(0, 21 - __clz(hi - lo));  // 32 - clz bits, of which the bins tell 11
+      row.each([&](float x) {
+        const uint32_t k = key_of(x);
+        if (in(b, x, k)) add((hi - k) >> shift, weight(x));
       });
       row_sync<CLUSTER>();
-      constexpr int E = BINS1 < SM_THREADS ? 1 : BINS1 / SM_THREADS;
-      uint32_t c[E];
-      double w[E];
+      uint32_t c[EACH], first;
+      double w[EACH];
       Runs r;
-      r.n = 0u;
-      r.w = 0.0;
-      const int first = n - 1 - (int)threadIdx.x * E;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        c[i] = 0u;
-        w[i] = 0.0;
-        if (first - i >= 0) bin_sum(bins1, BINS1, first - i, c[i], w[i]);
-        r.n += c[i];
-        r.w += w[i];
+      collect(r, c, w, first, 0u, 0.0, 0.0);
+      r.excl_n += f.before_n; r.incl_n += f.before_n;
+      r.excl_w += f.before_w; r.incl_w += f.before_w;
+      const uint32_t last = f.before_n + f.tokens - 1;
+      Found g = open(ask, r, c, w, first);
+      if (!g.valid) {                               // by roundings: the last token of the bin
+        ask = ask_rank(last);
+        g = open(ask, r, c, w, first);
       }
-      sum_runs<false>(s, r, 0u, 0.0, 0.0, 1, 0);
-      r.excl_n += before_n; r.incl_n += before_n;
-      r.excl_w += before_w; r.incl_w += before_w;
-      f = walk_bins<E>(ask, false, r, c, w, (uint32_t)first, &before_w, &before_n);
-      prefix = prefix << L::bits(l) | f.key;
+      f = g;
+      b.kb = hi - (g.key << shift);
+      b.ka = shift ? max(lo, b.kb - ((1u << shift) - 1)) : b.kb;
     }
-    f.key = prefix << L::shift(L::N - 1);
-    if (!(f.key >> 31)) f.key |= (1u << L::shift(L::N - 1)) - 1;   // a negative number's key is its complement
-    return f;
+    // few tokens: each is ranked against all
+    if (threadIdx.x == 0) s.list_n = 0u;
+    __syncthreads();
+    row.each([&](float x) {
+      const uint32_t k = key_of(x);
+      if (in(b, x, k)) {
+        const uint32_t at = atomicAdd(&s.list_n, 1u);
+        if (at < LIST) list[at] = k;
+      }
+    });
+    row_sync<CLUSTER>();
+    const uint32_t n = f.tokens, i = threadIdx.x;
+    if (i < n) {
+      uint32_t at = i, k = 0u;
+      for (int c = 0; c < (CLUSTER ? ctas : 1); ++c) {
+        const uint32_t has = CLUSTER ? ld_cluster_u32(mapa_u32(smem_u32(&s.list_n), c)) : s.list_n;
+        if (at < has) {
+          k = CLUSTER ? ld_cluster_u32(mapa_u32(smem_u32(list + at), c)) : list[at];
+          break;
+        }
+        at -= has;
+      }
+      keys[i] = k;
+      weights[i] = weight(value_of(k));
+    }
+    if (i == 0) s.owner = 0xffffffffu;
+    __syncthreads();
+    uint32_t before = 0u, same = 0u;
+    unsigned long long sum = 0ull;
+    if (i < n) {
+      const uint32_t k = keys[i];
+      for (uint32_t j = 0; j < n; ++j) {
+        const uint32_t o = keys[j];
+        same += o == k;
+        if (o > k) {
+          ++before;
+          sum += weights[j];
+        }
+      }
+      const double w = (double)weights[i] / WEIGHT_UNIT, cum = f.before_w + (double)sum / WEIGHT_UNIT;
+      if (ask.by_rank ? ask.rank < f.before_n + before + same : reaches(cum + same * w, ask.target, ask.strict)) atomicMin(&s.owner, before);
+    }
+    __syncthreads();
+    const bool none = s.owner == 0xffffffffu;        // by roundings: the last token
+    if (i < n && (none ? before + same == n : before == s.owner)) {
+      if (none) ask = ask_rank(f.before_n + n - 1);
+      Walk k;
+      k.cum = f.before_w + (double)sum / WEIGHT_UNIT;
+      k.n = f.before_n + before;
+      k.step(ask, same, (double)weights[i] / WEIGHT_UNIT, keys[i]);
+      s.here = k.f;                                  // equal tokens write the same
+    }
+    __syncthreads();
+    return s.here;
   }
 };
 
@@ -757,15 +845,14 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
 }
 
 template <typename T, bool CLUSTER> struct SampleSmem {
-  static constexpr int BYTES = RadixSums<T, CLUSTER>::SMEM;
+  static constexpr int BYTES = BinnedSums<T, CLUSTER>::SMEM;
 };
 template <bool CLUSTER> struct SampleSmem<bf16, CLUSTER> {
-  static constexpr int W = WindowSums<CLUSTER>::SMEM, R = RadixSums<bf16, CLUSTER>::SMEM, BYTES = W > R ? W : R;
+  static constexpr int W = WindowSums<CLUSTER>::SMEM, R = BinnedSums<bf16, CLUSTER>::SMEM, BYTES = W > R ? W : R;
 };
 
 template <typename S, typename T, bool CLUSTER>
 __device__ void finish(Shared& s, S& sums, const Share<T>& row, const Settings& set, const SampleArgs& a, int r, int cta, int ctas) {
-  sums.sum(row, set);
   uint32_t kept;
   const Found f = draw(sums, row, set, kept);
   write_token<T, CLUSTER>(s, row, f, cta, ctas, a.token + r);
@@ -775,12 +862,24 @@ __device__ void finish(Shared& s, S& sums, const Share<T>& row, const Settings& 
   }
 }
 
+// apart, so that the bf16 rows' method keeps its registers
+template <typename T, bool CLUSTER>
+__device__ __noinline__ uint32_t sample_binned(Shared& s, void* smem, const Share<T>& row, const Settings& set, const SampleArgs& a, int r,
+                                               int cta, int ctas) {
+  BinnedSums<T, CLUSTER> sums(s, smem, cta, ctas);
+  float least;
+  const uint32_t state = sums.range(row, least);
+  if (state == 0u) {
+    sums.sum(row, set, least);
+    finish<BinnedSums<T, CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+  }
+  return state;
+}
+
 template <typename T, bool CLUSTER>
 __global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ Shared s;
-  __shared__ Found found[FINDS];
-  __shared__ uint32_t valid[FINDS];
   griddep_wait();
   griddep_launch();
   int cta = 0, ctas = 1;
@@ -811,19 +910,20 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(SampleArgs a) {
   const Share<T> row((const T*)a.logits + r * a.row_stride, a.vocab, cta, ctas);
   uint32_t state = ROW_UNDEFINED;
   if (set.ok) {
+    bool binned = true;
     if constexpr (sizeof(T) == 2) {
-      WindowSums<CLUSTER> sums(s, found, valid, smem, cta, ctas);
+      WindowSums<CLUSTER> sums(s, smem, cta, ctas);
       state = sums.count(row);
-      if (state == 0u) finish<WindowSums<CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
-      if (state == ROW_OUTSIDE) {
-        RadixSums<T, CLUSTER> other(s, found, smem, cta, ctas);
-        other.topf = (float)sums.top;
-        finish<RadixSums<T, CLUSTER>, T, CLUSTER>(s, other, row, set, a, r, cta, ctas);
+      binned = state == ROW_OUTSIDE;
+      if (state == 0u) {
+        sums.sum(set);
+        finish<WindowSums<CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
       }
-    } else {
-      RadixSums<T, CLUSTER> sums(s, found, smem, cta, ctas);
-      state = sums.largest(row);
-      if (state == 0u) finish<RadixSums<T, CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+    }
+    if (binned) {
+      const Share<T> row1 = row;                     // copies: the function wants their addresses
+      const Settings set1 = set;
+      state = sample_binned<T, CLUSTER>(s, smem, row1, set1, a, r, cta, ctas);
     }
   }
   if (state == ROW_UNDEFINED && cta == 0 && threadIdx.x == 0) {
