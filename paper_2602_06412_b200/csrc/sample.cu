@@ -52,6 +52,23 @@ __device__ __forceinline__ void add_shared(uint32_t addr, uint32_t v) {
   asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
+// of two 16-bit numbers at a time
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t add_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // all threads of the row: one CTA's, or a cluster's
 template <bool CLUSTER> __device__ __forceinline__ void row_sync() {
   if (CLUSTER) cluster_sync_all(); else __syncthreads();
@@ -105,6 +122,7 @@ struct Found {
 struct Shared {                     // beside the bins
   double part_w[SM_WARPS], part_m[SM_WARPS], part_raw[SM_WARPS];
   uint32_t part_n[SM_WARPS], part_nm[SM_WARPS], matches[SM_WARPS];
+  double powers[32];                // 2^(i / 32)
   double cta_w, cta_m, cta_raw;     // this CTA's sums, read by the cluster
   uint32_t cta_n, cta_nm, cta_matches;
   uint32_t top, lo, hi, flags, zeros, list_n, owner;
@@ -120,6 +138,22 @@ struct Settings {
   int top_k;
   bool greedy, ok;
 };
+
+// e^z for z <= 0, by a table of 2^(i/32) and the Taylor polynomial of what is left (Tang's table-driven method): |r| <= ln 2 / 64, so that
+// r^6 / 720 is 2^-48 of the result at most.  Below e^-700 it stays e^-700, which no sum notices.
+__device__ __forceinline__ double exp_falling(double z, const double* table) {
+  z = fmax(z, -700.0);
+  const double n = rint(z * 46.16624130844683);                     // 32 / ln 2
+  const double r = fma(-n, 5.9631716539705866e-12, fma(-n, 0.02166084938653512, z));   // ln 2 / 32 in two terms, the first of 32 bits
+  const int k = (int)n;
+  double p = fma(r, 1.0 / 120, 1.0 / 24);
+  p = fma(p, r, 1.0 / 6);
+  p = fma(p, r, 0.5);
+  p = fma(p * r, r, r);
+  const double t = table[k & 31];
+  const double v = fma(t, p, t);
+  return __hiloint2double(__double2hiint(v) + ((k >> 5) << 20), __double2loint(v));
+}
 
 // What both methods leave in registers: every thread has a run of values in falling order, the runs in order of threads (and
 // CTAs).  n, w: tokens of the run and their weights, incl_*: running sums up to and with it.
@@ -271,7 +305,7 @@ template <bool CLUSTER> struct Finder {
   Shared& s;
   int cta, ctas, turn = 0;
   Runs q;
-  double T1;
+  double inv_T;                     // (x - max) / T as a product: off by 2^-52 of itself
   __device__ Finder(Shared& sh, int c, int n) : s(sh), cta(c), ctas(n) {}
   template <typename F> __device__ Found search(const Ask& ask, const Runs& r, F walk) {
     const uint32_t o = first_thread(s, ask.in(r));
@@ -318,17 +352,17 @@ constexpr uint32_t WIN_LO = (127 - 32) << 7, WIN_HI = (127 + 16) << 7, WIN_BINS 
 
 template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
   typedef Finder<CLUSTER> F;
-  using F::s; using F::cta; using F::ctas; using F::q; using F::T1;
-  static constexpr int SMEM = 2 * WIN_BINS * 4 + (CLUSTER ? (WIN_BINS + 8) * 4 : 0);
-  uint32_t* bins;                   // [magnitude][sign]
+  using F::s; using F::cta; using F::ctas; using F::q; using F::inv_T;
+  static constexpr int SMEM = (2 * WIN_BINS + 32) * 4 + (CLUSTER ? (WIN_BINS + 8) * 4 : 0);
+  uint32_t* bins;                   // [magnitude][sign], and 32 that nobody reads
   uint32_t* merged;                 // this CTA's run of places, summed over the cluster
-  uint32_t hi, R, zeros, lo, p0, p1;    // places: positive values from magnitude hi down, zero at R, negative ones from lo up
+  uint32_t hi, R, zeros, lo, p0, p1;    // places: positive values from magnitude hi of the window down, zero at R, negative ones from lo up
   uint32_t base;                    // first place of this CTA
   double top;
 
   __device__ WindowSums(Shared& sh, void* smem, int c, int n) : F(sh, c, n) {
     bins = reinterpret_cast<uint32_t*>(smem);
-    merged = bins + 2 * WIN_BINS;
+    merged = bins + 2 * WIN_BINS + 32;
   }
   // Counts the row.  0, ROW_UNDEFINED (a NaN, +inf, or nothing finite) or ROW_OUTSIDE (values outside the window).
   __device__ uint32_t count(const Share<bf16>& row) {
@@ -339,51 +373,47 @@ template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
       s.lo = 0xffffu;
     }
     __syncthreads();
-    const uint32_t at = smem_u32(bins) - 8 * WIN_LO;
-    uint32_t most = 0u, least = 0xffffffffu, zero = 0u, flags = 0u;   // magnitudes, two at a time
+    // a bf16 number turned left by a bit is its magnitude and then its sign; less the window's start, the number of its bin
+    constexpr uint32_t SHIFT = (0x10000u - 2 * WIN_LO) * 0x10001u, LIMIT = (0x8000u - 2 * WIN_BINS) * 0x10001u;
+    uint32_t most = 0u, least = 0xffffffffu, zero = 0u, flags = 0u;   // bins, two at a time
     __nv_bfloat162 top2 = __float2bfloat162_rn(-INFINITY);
-    auto one = [&](uint32_t h) {
-      const uint32_t m = h & 0x7fffu;
-      if (m == 0u) ++zero;
-      else if (m >= 0x7f80u) {
-        if (h != 0xff80u) flags |= ROW_UNDEFINED;
-        return;
-      } else if (m < WIN_LO || m >= WIN_HI) flags |= ROW_OUTSIDE;
-      else {
-        add_shared(at + 8 * m + 4 * (h >> 15), 1u);
-        most = __vmaxu2(most, m);
-        least = __vminu2(least, m | 0xffff0000u);
+    const uint32_t aside = (2 * WIN_BINS + (threadIdx.x & 31)) * 0x10001u;   // a bin per lane for what is outside
+    // what makes a word have bins outside: zeros are counted apart, -inf is left out, and the rest is for the row to know
+    auto explain = [&](uint32_t w, uint32_t b) {
+      const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w);
+      const uint32_t zeros2 = __heq2_mask(x, __float2bfloat162_rn(0.f)), none2 = __heq2_mask(x, __float2bfloat162_rn(-INFINITY));
+      zero += __popc(zeros2 & 0x10001u);
+#pragma unroll
+      for (int h = 0; h < 32; h += 16) {
+        const uint32_t bin = (b >> h) & 0xffffu;
+        if (bin < 2 * WIN_BINS) most = max_u16x2(most, bin);
+        else if (!(((zeros2 | none2) >> h) & 1u)) flags |= ((w >> h) & 0x7fffu) >= 0x7f80u ? ROW_UNDEFINED : ROW_OUTSIDE;
       }
-      const __nv_bfloat162 v = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)h));
-      top2 = __hmax2(top2, v);
     };
     auto eight = [&](const uint4& u) {
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-      uint32_t mx = 0u, mn = 0xffffffffu;
+      uint32_t b[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        mx = __vmaxu2(mx, w[i] & 0x7fff7fffu);
-        mn = __vminu2(mn, w[i] & 0x7fff7fffu);
+        b[i] = min_u16x2(add_u16x2(((w[i] << 1) & 0xfffefffeu) | ((w[i] >> 15) & 0x00010001u), SHIFT), aside);
+        atomicAdd(bins + (b[i] & 0xffffu), 1u);
+        atomicAdd(bins + (b[i] >> 16), 1u);
+        top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
       }
-      constexpr uint32_t C1 = (0x8000u - WIN_HI) * 0x10001u, C2 = (0x8000u - WIN_LO) * 0x10001u;
-      if ((((mx + C1) | ~(mn + C2)) & 0x80008000u) == 0u) {
+      const uint32_t mx = max_u16x2(max_u16x2(b[0], b[1]), max_u16x2(b[2], b[3]));
+      least = min_u16x2(least, min_u16x2(min_u16x2(b[0], b[1]), min_u16x2(b[2], b[3])));
+      if (((mx + LIMIT) & 0x80008000u) == 0u) most = max_u16x2(most, mx);   // all inside
+      else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // each half turned left by one bit: magnitude and then sign, the number of its bin
-          const uint32_t r = ((w[i] << 1) & 0xfffefffeu) | ((w[i] >> 15) & 0x00010001u);
-          add_shared(at + ((r << 2) & 0x3fffcu), 1u);
-          add_shared(at + ((r >> 14) & 0x3fffcu), 1u);
-          top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-        }
-        most = __vmaxu2(most, mx);
-        least = __vminu2(least, mn);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          one(w[i] & 0xffffu);
-          one(w[i] >> 16);
-        }
-      }
+        for (int i = 0; i < 4; ++i) explain(w[i], b[i]);
+    };
+    auto one = [&](uint32_t h) {                     // with a -inf beside it
+      const uint32_t w = h | 0xff800000u;
+      const uint32_t b = min_u16x2(add_u16x2(((w << 1) & 0xfffefffeu) | ((w >> 15) & 0x00010001u), SHIFT), aside);
+      atomicAdd(bins + (b & 0xffffu), 1u);
+      least = min_u16x2(least, b);
+      explain(w, b);
+      top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w));
     };
     const uint4* w = row.words();
     int v = row.v0 + (int)threadIdx.x;
@@ -400,7 +430,7 @@ template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
     if (row.last && row.tail0 + (int)threadIdx.x < row.vocab) one(raw[row.tail0 + threadIdx.x]);
 
     const uint32_t hi1 = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
-    const uint32_t lo1 = __reduce_min_sync(0xffffffffu, min(least & 0xffffu, least >> 16));
+    const uint32_t lo1 = __reduce_min_sync(0xffffffffu, min(least & 0xffffu, least >> 16));   // behind the window where there are none
     const uint32_t top1 = __reduce_max_sync(0xffffffffu, key_of(fmaxf(__low2float(top2), __high2float(top2))));
     const uint32_t zero1 = warp_sum(zero);
     flags = __reduce_or_sync(0xffffffffu, flags);
@@ -425,25 +455,29 @@ template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
         zeros += ld_cluster_u32(mapa_u32(smem_u32(&s.zeros), c));
       }
     }
+    hi >>= 1;
+    lo >>= 1;
     top = (double)value_of(t);
     if ((f & ROW_UNDEFINED) || t == key_of(-INFINITY)) return ROW_UNDEFINED;
     return f & ROW_OUTSIDE;
   }
   // bin and value of a place
-  __device__ uint32_t bin_of(uint32_t p) const { return p < R ? 2 * (hi - p - WIN_LO) : 2 * (lo + (p - R - 1) - WIN_LO) + 1; }
+  __device__ uint32_t bin_of(uint32_t p) const { return p < R ? 2 * (hi - p) : 2 * (lo + (p - R - 1)) + 1; }
   __device__ float value(uint32_t p) const {
-    return p == R ? 0.f : __uint_as_float(p < R ? (hi - p) << 16 : 0x80000000u | (lo + (p - R - 1)) << 16);
+    return p == R ? 0.f : __uint_as_float(p < R ? (WIN_LO + hi - p) << 16 : 0x80000000u | (WIN_LO + lo + (p - R - 1)) << 16);
   }
   __device__ uint32_t tokens(uint32_t p) const { return CLUSTER ? merged[p - base] : p == R ? zeros : bins[bin_of(p)]; }
   __device__ double largest_value() const { return top; }
-  __device__ double weight(uint32_t p) const { return exp(((double)value(p) - top) / T1); }
+  __device__ double weight(uint32_t p) const { return exp_falling(((double)value(p) - top) * inv_T, s.powers); }
 
   __device__ void sum(const Settings& set) {
-    T1 = set.greedy ? 1.0 : set.T;
+    inv_T = set.greedy ? 1.0 : 1.0 / set.T;
     R = hi >= lo ? hi - lo + 1 : 0u;
-    const uint32_t places = 2 * R + 1;
-    base = (uint32_t)((unsigned long long)places * cta / ctas);
-    const uint32_t end = (uint32_t)((unsigned long long)places * (cta + 1) / ctas);
+    // the place of the largest logit: those before it are empty
+    const uint32_t mag = (__float_as_uint((float)top) & 0x7fffffffu) >> 16;
+    const uint32_t p_top = top > 0.0 ? hi - (mag - WIN_LO) : top == 0.0 ? R : R + 1 + (mag - WIN_LO - lo), places = 2 * R + 1 - p_top;
+    base = p_top + places * cta / ctas;
+    const uint32_t end = p_top + places * (cta + 1) / ctas;
     if (CLUSTER) {
       for (uint32_t p = base + threadIdx.x; p < end; p += SM_THREADS) {
         uint32_t c = zeros;
@@ -463,17 +497,17 @@ template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
     q.w = 0.0;
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
-    for (uint32_t p = p0; p < p1; ++p) {
+    const bool plain = inv_T == 1.0;
+#pragma unroll 2
+    for (uint32_t p = p0; p < p1; ++p) {              // no branch on empty bins: a warp has hardly a step without a full one
       const uint32_t c = tokens(p);
-      if (!c) continue;
       const double w = weight(p), cw = c * w;
       q.n += c;
       q.w += cw;
-      raw += T1 == 1.0 ? cw : c * exp((double)value(p) - top);
-      if (w >= set.min_p) {
-        nm += c;
-        m += cw;
-      }
+      raw += plain ? cw : (double)((float)c * expf((float)((double)value(p) - top)));
+      const bool keeps = w >= set.min_p;
+      nm += keeps ? c : 0u;
+      m += keeps ? cw : 0.0;
     }
     sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
   }
@@ -495,7 +529,7 @@ constexpr int LIST = 256;                               // tokens that are ranke
 
 template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
   typedef Finder<CLUSTER> F;
-  using F::s; using F::cta; using F::ctas; using F::q; using F::T1;
+  using F::s; using F::cta; using F::ctas; using F::q; using F::inv_T;
   static constexpr int SMEM = BINS * (1 + LIMBS) * 4 + LIST * 16;
   static constexpr int EACH = BINS / SM_THREADS;        // bins to a thread; in a cluster the CTAs share them out
   uint32_t* bins;                   // [1 + LIMBS][BINS]: tokens, limbs
@@ -549,7 +583,7 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
     return 0u;
   }
   __device__ double largest_value() const { return (double)topf; }
-  __device__ unsigned long long weight(float x) const { return __double2ull_rn(exp(((double)x - (double)topf) / T1) * WEIGHT_UNIT); }
+  __device__ unsigned long long weight(float x) const { return __double2ull_rn(exp_falling(((double)x - (double)topf) * inv_T, s.powers) * WEIGHT_UNIT); }
   // Falls with x; what is too far below the largest shares the last bin.
   __device__ uint32_t bin_of(float x) const { return min((uint32_t)BINS - 1, __float2uint_rz((topf - x) * step)); }
 
@@ -605,9 +639,9 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
   }
   uint32_t first0;
   __device__ void sum(const Share<T>& row, const Settings& set, float least) {
-    T1 = set.greedy ? 1.0 : set.T;
+    inv_T = set.greedy ? 1.0 : 1.0 / set.T;
     // beyond 50 T the weights are below 2^-72 of the largest
-    const float span = (float)fmin((double)topf - (double)least, 50.0 * T1);
+    const float span = (float)fmin((double)topf - (double)least, 50.0 / inv_T);
     step = span > 0.f ? fminf((float)BINS / span, 3.4e38f) : 0.f;
     clear();
     uint32_t nm = 0u;
@@ -617,7 +651,7 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
       const unsigned long long w = weight(x);
       add(bin_of(x), w);
       const double v = (double)w / WEIGHT_UNIT;
-      raw += T1 == 1.0 ? v : (double)expf(x - topf);
+      raw += inv_T == 1.0 ? v : (double)expf(x - topf);
       if (v >= set.min_p) {
         ++nm;
         m += v;
@@ -781,14 +815,32 @@ template <typename S, typename T> __device__ Found draw(S& sums, const Share<T>&
   return f.rank < n ? f : sums.find(row, ask_rank(n - 1));
 }
 
-// The nth token whose value has this key: a count over the row, then the one warp's words that hold it once more.
-template <typename T> __device__ __forceinline__ uint32_t matches_of(const uint4& u, float x) {   // a bit for each
-  const T* e = reinterpret_cast<const T*>(&u);
-  uint32_t m = 0u;
-#pragma unroll
-  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) m |= (to_f(e[i]) == x ? 1u : 0u) << i;
-  return m;
-}
+// The tokens of a 16-byte word that equal x, a bit for each, and their number.
+template <typename T> struct Matcher;
+template <> struct Matcher<float> {
+  float x;
+  __device__ Matcher(float v) : x(v) {}
+  __device__ uint32_t bits(const uint4& u) const {
+    return (__uint_as_float(u.x) == x) | (__uint_as_float(u.y) == x) << 1 | (__uint_as_float(u.z) == x) << 2 | (__uint_as_float(u.w) == x) << 3;
+  }
+  __device__ uint32_t number(const uint4& u) const {
+    return (__uint_as_float(u.x) == x) + (__uint_as_float(u.y) == x) + (__uint_as_float(u.z) == x) + (__uint_as_float(u.w) == x);
+  }
+};
+template <> struct Matcher<bf16> {
+  __nv_bfloat162 x;
+  __device__ Matcher(float v) : x(__float2bfloat162_rn(v)) {}
+  __device__ uint32_t mask(uint32_t w) const { return __heq2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w), x); }   // 0xffff for each
+  __device__ uint32_t bits(const uint4& u) const {
+    const uint32_t a = (mask(u.x) & 0x20001u) | (mask(u.y) & 0x80004u) | (mask(u.z) & 0x200010u) | (mask(u.w) & 0x800040u);
+    return (a | a >> 16) & 0xffu;
+  }
+  __device__ uint32_t number(const uint4& u) const {
+    return __popc((mask(u.x) & 0x10001u) | (mask(u.y) & 0x20002u) | (mask(u.z) & 0x40004u) | (mask(u.w) & 0x80008u));
+  }
+};
+
+// The nth token of the value that has this key: a count over the row, then the one warp's words that hold it once more.
 template <typename T, bool CLUSTER>
 __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int cta, int ctas, int32_t* token) {
   constexpr int V = Share<T>::V;
@@ -798,7 +850,14 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
   const int a = row.v0 + (int)((long long)(row.v1 - row.v0) * warp / SM_WARPS), b = row.v0 + (int)((long long)(row.v1 - row.v0) * (warp + 1) / SM_WARPS);
   const int heads = row.first && warp == 0 ? row.head : 0, tails = row.last && warp == SM_WARPS - 1 ? row.vocab - row.tail0 : 0;
   uint32_t n = 0u;
-  for (int v = a + lane; v < b; v += 32) n += __popc(matches_of<T>(words[v], x));
+  const Matcher<T> equal(x);
+  int v = a + lane;
+  for (; v + 96 < b; v += 128) {
+    const uint4 u[4] = {words[v], words[v + 32], words[v + 64], words[v + 96]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += equal.number(u[i]);
+  }
+  for (; v < b; v += 32) n += equal.number(words[v]);
   const bool in_head = lane < heads && to_f(row.row[lane]) == x, in_tail = lane < tails && to_f(row.row[row.tail0 + lane]) == x;
   n = warp_sum(n + in_head + in_tail);
   if (lane == 0) s.matches[warp] = n;
@@ -822,8 +881,8 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
   }
   left -= __popc(head_at);
   for (int v0 = a; v0 < b; v0 += 32) {
-    const int v = v0 + lane;
-    uint32_t m = v < b ? matches_of<T>(words[v], x) : 0u, sum = __popc(m);
+    v = v0 + lane;
+    uint32_t m = v < b ? equal.bits(words[v]) : 0u, sum = __popc(m);
     const uint32_t mine = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -877,11 +936,12 @@ __device__ __noinline__ uint32_t sample_binned(Shared& s, void* smem, const Shar
 }
 
 template <typename T, bool CLUSTER>
-__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ Shared s;
   griddep_wait();
   griddep_launch();
+  if (threadIdx.x < 32) s.powers[threadIdx.x] = exp2(threadIdx.x / 32.0);   // seen after the first barrier
   int cta = 0, ctas = 1;
   if (CLUSTER) {
     uint32_t n;
