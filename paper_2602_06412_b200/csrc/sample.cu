@@ -40,12 +40,7 @@ struct SampleArgs {
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
-  double v;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
   return v;
 }
 __device__ __forceinline__ void add_shared(uint32_t addr, uint32_t v) {
@@ -53,11 +48,6 @@ __device__ __forceinline__ void add_shared(uint32_t addr, uint32_t v) {
 }
 
 // of two 16-bit numbers at a time
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 __device__ __forceinline__ uint32_t add_u16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("add.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -70,8 +60,8 @@ __device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
 }
 
 // all threads of the row: one CTA's, or a cluster's
-template <bool CLUSTER> __device__ __forceinline__ void row_sync() {
-  if (CLUSTER) cluster_sync_all(); else __syncthreads();
+template <int CTAS> __device__ __forceinline__ void row_sync() {
+  if (CTAS > 1) cluster_sync_all(); else __syncthreads();
 }
 
 // Ordered keys: a larger number has a larger key; both zeros have the same.
@@ -112,21 +102,30 @@ template <typename T> struct Share {
   }
 };
 
-// a token by its place in the order: its rank (0 = the largest), the sum of weights up to and with it, its value (or bin) and which of
-// the tokens of that value it is; for a bin also its tokens and what lies before it
+// a token by its place in the order: its rank (0 = the largest), the sum of weights up to and with it, its value's key and which of the
+// tokens of that value it is; `entry` is the value's or bin's number, `tokens` how many it has, before_* what lies before it
 struct Found {
   double mass, before_w;
-  uint32_t rank, key, nth, before_n, tokens, valid;
+  uint32_t rank, key, nth, before_n, tokens, entry;
 };
 
+// sums over the whole row: tokens, their weights, those that min-p keeps, and weights at T = 1
+struct Totals {
+  double w, m, raw;
+  uint32_t n, nm;
+};
+
+constexpr int MOST_CTAS = 8, MOST_GROUPS = 400;
+
 struct Shared {                     // beside the bins
-  double part_w[SM_WARPS], part_m[SM_WARPS], part_raw[SM_WARPS];
-  uint32_t part_n[SM_WARPS], part_nm[SM_WARPS], matches[SM_WARPS];
   double powers[32];                // 2^(i / 32)
-  double cta_w, cta_m, cta_raw;     // this CTA's sums, read by the cluster
-  uint32_t cta_n, cta_nm, cta_matches;
+  // in the first CTA, written by all of the row's: sums of groups of 32 entries, and every warp's share of the other sums
+  double group_w[MOST_GROUPS], warp_m[MOST_CTAS * SM_WARPS], warp_raw[MOST_CTAS * SM_WARPS];
+  uint32_t group_n[MOST_GROUPS], warp_nm[MOST_CTAS * SM_WARPS];
+  Found found[2];                   // by turns, so that none is overwritten while somebody reads it
+  Totals totals;
+  uint32_t matches[SM_WARPS], cta_matches;
   uint32_t top, lo, hi, flags, zeros, list_n, owner;
-  Found found[2], here;             // found: by turns, so that none is overwritten while the cluster reads it
 };
 
 enum { ROW_UNDEFINED = 1, ROW_OUTSIDE = 2 };
@@ -155,94 +154,12 @@ __device__ __forceinline__ double exp_falling(double z, const double* table) {
   return __hiloint2double(__double2hiint(v) + ((k >> 5) << 20), __double2loint(v));
 }
 
-// What both methods leave in registers: every thread has a run of values in falling order, the runs in order of threads (and
-// CTAs).  n, w: tokens of the run and their weights, incl_*: running sums up to and with it.
-struct Runs {
-  uint32_t n, incl_n, excl_n;
-  double w, incl_w, excl_w;
-  uint32_t total_n, total_nm;
-  double total_w, total_m, total_raw;
-};
-
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 __device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xffffffffu, v); }
-
-// Running sums of the runs over the row.  nm, m: tokens and weights that min-p keeps; raw: weights at T = 1.
-template <bool CLUSTER>
-__device__ void sum_runs(Shared& s, Runs& q, uint32_t nm, double m, double raw, int ctas, int cta) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t n = q.n;
-  double w = q.w;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, n, o);
-    const double b = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) {
-      n += a;
-      w += b;
-    }
-  }
-  nm = warp_sum(nm);
-  m = warp_sum(m);
-  raw = warp_sum(raw);
-  if (lane == 31) {
-    s.part_n[warp] = n;
-    s.part_w[warp] = w;
-    s.part_nm[warp] = nm;
-    s.part_m[warp] = m;
-    s.part_raw[warp] = raw;
-  }
-  __syncthreads();
-  uint32_t n0 = 0, nn = 0, nnm = 0;
-  double w0 = 0, ww = 0, mm = 0, rr = 0;
-#pragma unroll
-  for (int i = 0; i < SM_WARPS; ++i) {
-    if (i == warp) {
-      n0 = nn;
-      w0 = ww;
-    }
-    nn += s.part_n[i];
-    ww += s.part_w[i];
-    nnm += s.part_nm[i];
-    mm += s.part_m[i];
-    rr += s.part_raw[i];
-  }
-  double before_w = 0;
-  uint32_t before_n = 0;
-  if (CLUSTER) {
-    if (threadIdx.x == 0) {
-      s.cta_n = nn;
-      s.cta_w = ww;
-      s.cta_nm = nnm;
-      s.cta_m = mm;
-      s.cta_raw = rr;
-    }
-    cluster_sync_all();
-    nn = nnm = 0;
-    ww = mm = rr = 0;
-    for (int c = 0; c < ctas; ++c) {
-      if (c == cta) {
-        before_n = nn;
-        before_w = ww;
-      }
-      nn += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_n), c));
-      nnm += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_nm), c));
-      ww += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_w), c));
-      mm += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_m), c));
-      rr += ld_cluster_f64(mapa_u32(smem_u32(&s.cta_raw), c));
-    }
-  }
-  q.total_n = nn; q.total_nm = nnm; q.total_w = ww; q.total_m = mm; q.total_raw = rr;
-  q.incl_n = before_n + n0 + n;
-  q.incl_w = before_w + (w0 + w);
-  q.excl_n = q.incl_n - q.n;
-  const double up = __shfl_up_sync(0xffffffffu, q.incl_w, 1);
-  q.excl_w = lane ? up : before_w + w0;
-}
 
 // The number of tokens of weight w, 1 ... c, after which cum reaches the target (strict: exceeds it); c if none does.
 __device__ __forceinline__ bool reaches(double cum, double target, bool strict) { return strict ? cum > target : cum >= target; }
@@ -259,266 +176,359 @@ struct Ask {
   bool by_rank, strict;
   uint32_t rank;
   double target;
-  __device__ bool in(const Runs& q) const {
-    return q.n && (by_rank ? rank < q.incl_n : reaches(q.incl_w, target, strict));
+  // whether a run with these running sums up to and with it holds it, if none before did
+  __device__ bool in(uint32_t incl_n, double incl_w) const { return by_rank ? rank < incl_n : reaches(incl_w, target, strict); }
+  // the token among c of weight w, before which there are before_n of sum before_w
+  __device__ void among(uint32_t c, double w, Found& f) const {
+    const uint32_t j = by_rank ? rank - f.before_n + 1 : tokens_until(f.before_w, w, c, target, strict);
+    f.tokens = c;
+    f.nth = j - 1;
+    f.rank = f.before_n + f.nth;
+    f.mass = f.before_w + j * w;
   }
 };
 __device__ __forceinline__ Ask ask_rank(uint32_t rank) { return {true, false, rank, 0.0}; }
 __device__ __forceinline__ Ask ask_mass(double target, bool strict) { return {false, strict, 0u, target}; }
 
-// A walk down a run, value by value; true once the token is found.  `last`: the place to take should roundings leave none.
-struct Walk {
-  double cum;
-  uint32_t n;
-  Found f;
-  __device__ bool step(const Ask& a, uint32_t c, double w, uint32_t key) {
-    if (!c) return false;
-    const bool here = a.by_rank ? a.rank < n + c : reaches(cum + c * w, a.target, a.strict);
-    const uint32_t j = !here ? c : a.by_rank ? a.rank - n + 1 : tokens_until(cum, w, c, a.target, a.strict);
-    f.mass = cum + j * w;
-    f.rank = n + j - 1;
-    f.key = key;
-    f.nth = j - 1;
-    f.before_w = cum;
-    f.before_n = n;
-    f.tokens = c;
-    cum += c * w;
-    n += c;
-    return here;
+// The first lane of a warp whose n tokens of weight w in all hold what is asked for; f.before_*, the sums before the warp's, become those
+// before the lane's.  Where roundings leave none: the last lane that has tokens, and its last token is asked for from there on.
+__device__ __forceinline__ int pick_lane(Ask& ask, uint32_t n, double w, Found& f) {
+  const int lane = threadIdx.x & 31;
+  uint32_t in = n;
+  double iw = w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, in, o);
+    const double b = __shfl_up_sync(0xffffffffu, iw, o);
+    if (lane >= o) {
+      in += a;
+      iw += b;
+    }
   }
-};
-
-// The first thread of this CTA whose run holds what is asked for, SM_THREADS if none does.
-__device__ __forceinline__ uint32_t first_thread(Shared& s, bool in) {
-  if (threadIdx.x == 0) s.owner = SM_THREADS;
-  __syncthreads();
-  const unsigned b = __ballot_sync(0xffffffffu, in);
-  if (b && (threadIdx.x & 31) == 0) atomicMin(&s.owner, threadIdx.x + __ffs(b) - 1);
-  __syncthreads();
-  const uint32_t o = s.owner;
-  __syncthreads();
-  return o;
+  const unsigned some = __ballot_sync(0xffffffffu, n != 0u), hit = __ballot_sync(0xffffffffu, n && ask.in(f.before_n + in, f.before_w + iw));
+  const int l = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+  const uint32_t upto = __shfl_sync(0xffffffffu, in, l), mine = __shfl_sync(0xffffffffu, n, l);
+  if (!hit) ask = ask_rank(f.before_n + upto - 1);
+  const double before = __shfl_sync(0xffffffffu, iw, max(l - 1, 0));
+  f.before_n += upto - mine;
+  f.before_w += l ? before : 0.0;
+  return l;
 }
 
-// What both methods share: whose run holds what is asked for, its walk there, and the answer for all threads of the row.
-template <bool CLUSTER> struct Finder {
-  Shared& s;
-  int cta, ctas, turn = 0;
-  Runs q;
-  double inv_T;                     // (x - max) / T as a product: off by 2^-52 of itself
-  __device__ Finder(Shared& sh, int c, int n) : s(sh), cta(c), ctas(n) {}
-  template <typename F> __device__ Found search(const Ask& ask, const Runs& r, F walk) {
-    const uint32_t o = first_thread(s, ask.in(r));
-    Found& mine = s.found[turn];
-    turn ^= 1;
-    if (threadIdx.x == 0 && o == SM_THREADS) mine.valid = 0u;
-    if (threadIdx.x == o) {
-      Walk k;
-      k.cum = r.excl_w;
-      k.n = r.excl_n;
-      walk(k);
-      k.f.valid = 1u;
-      mine = k.f;
-    }
-    row_sync<CLUSTER>();
-    if (!CLUSTER) return mine;
-    Found f;
-    f.valid = 0u;
-    for (int c = 0; c < ctas && !f.valid; ++c) {
-      const uint32_t a = mapa_u32(smem_u32(&mine), c);
-      f.valid = ld_cluster_u32(a + offsetof(Found, valid));
-      if (!f.valid) continue;
-      f.mass = ld_cluster_f64(a + offsetof(Found, mass));
-      f.before_w = ld_cluster_f64(a + offsetof(Found, before_w));
-      f.rank = ld_cluster_u32(a + offsetof(Found, rank));
-      f.key = ld_cluster_u32(a + offsetof(Found, key));
-      f.nth = ld_cluster_u32(a + offsetof(Found, nth));
-      f.before_n = ld_cluster_u32(a + offsetof(Found, before_n));
-      f.tokens = ld_cluster_u32(a + offsetof(Found, tokens));
-    }
-    return f;
+// The entry that holds what is asked for, by one warp: first among 32 runs of groups, then among a run's groups, then among a
+// group's 32 entries; entry(i, tokens, weight of a token).
+template <typename F> __device__ Found search(const Shared& s, int groups, Ask& ask, F entry, uint32_t before_n = 0u, double before_w = 0.0) {
+  const int lane = threadIdx.x & 31, per = (groups + 31) >> 5;
+  Found f;
+  f.before_n = before_n;
+  f.before_w = before_w;
+  uint32_t n = 0u;
+  double w = 0.0;
+  for (int g = lane * per; g < min(groups, (lane + 1) * per); ++g) {
+    n += s.group_n[g];
+    w += s.group_w[g];
   }
-  // no run reached the target, by roundings: it is behind the last token
-  __device__ static Found behind_all(double mass) {
-    Found f = {};
-    f.mass = mass;
-    f.rank = 0xffffffffu;
-    return f;
+  int g = pick_lane(ask, n, w, f) * per;
+  const bool one = lane < per && g + lane < groups;
+  g += pick_lane(ask, one ? s.group_n[g + lane] : 0u, one ? s.group_w[g + lane] : 0.0, f);
+  uint32_t c;
+  double each;
+  entry(32 * g + lane, c, each);
+  const int l = pick_lane(ask, c, c * each, f);
+  f.entry = 32 * g + l;
+  c = __shfl_sync(0xffffffffu, c, l);
+  each = __shfl_sync(0xffffffffu, each, l);
+  ask.among(c, each, f);
+  return f;
+}
+
+template <int CTAS> __device__ __forceinline__ uint32_t in_first_cta(const void* p) { return CTAS > 1 ? mapa_u32(smem_u32(p), 0) : smem_u32(p); }
+template <int CTAS> __device__ __forceinline__ void put(uint32_t addr, double v) {
+  if (CTAS > 1) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+  else asm volatile("st.shared.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+template <int CTAS> __device__ __forceinline__ void put(uint32_t addr, uint32_t v) {
+  if (CTAS > 1) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+  else asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+// a struct of whole words to its place in every CTA of the row, lane by lane
+template <int CTAS, typename S> __device__ __forceinline__ void publish(S& to, const S& v) {
+  static_assert(sizeof(S) % 4 == 0, "whole words");
+  uint32_t words[sizeof(S) / 4];
+  memcpy(words, &v, sizeof(S));
+  const int lane = threadIdx.x & 31;
+  if (lane < CTAS) {
+    const uint32_t a = CTAS > 1 ? mapa_u32(smem_u32(&to), lane) : smem_u32(&to);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(S) / 4); ++i) put<CTAS>(a + 4 * i, words[i]);
+  }
+}
+
+// What both methods share.
+template <int CTAS> struct Sums {
+  Shared& s;
+  int cta, groups = 0;
+  double inv_T;                     // (x - max) / T as a product: off by 2^-52 of itself
+  __device__ Sums(Shared& sh, int c) : s(sh), cta(c) {}
+  __device__ bool leads() const { return cta == 0 && threadIdx.x < 32; }   // the warp that searches
+  // a group of 32 entries, c tokens of weight cw in all to a lane
+  __device__ void put_group(int g, uint32_t c, double cw) {
+    c = warp_sum(c);
+    cw = warp_sum(cw);
+    if ((threadIdx.x & 31) == 0) {
+      put<CTAS>(in_first_cta<CTAS>(&s.group_n[g]), c);
+      put<CTAS>(in_first_cta<CTAS>(&s.group_w[g]), cw);
+    }
+  }
+  // four groups at once, of which lanes exchange what the others sum: lane's bits 4 and 3 say whose sums it ends with
+  __device__ void put_groups4(int g, const uint32_t* c, const double* cw) {
+    const int lane = threadIdx.x & 31;
+    const bool a = lane & 16, b = lane & 8;
+    uint32_t n0 = (a ? c[2] : c[0]) + __shfl_xor_sync(0xffffffffu, a ? c[0] : c[2], 16), n1 = (a ? c[3] : c[1]) + __shfl_xor_sync(0xffffffffu, a ? c[1] : c[3], 16);
+    double w0 = (a ? cw[2] : cw[0]) + __shfl_xor_sync(0xffffffffu, a ? cw[0] : cw[2], 16), w1 = (a ? cw[3] : cw[1]) + __shfl_xor_sync(0xffffffffu, a ? cw[1] : cw[3], 16);
+    uint32_t n = (b ? n1 : n0) + __shfl_xor_sync(0xffffffffu, b ? n0 : n1, 8);
+    double w = (b ? w1 : w0) + __shfl_xor_sync(0xffffffffu, b ? w0 : w1, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      n += __shfl_xor_sync(0xffffffffu, n, o);
+      w += __shfl_xor_sync(0xffffffffu, w, o);
+    }
+    if ((lane & 7) == 0) {
+      const int at = g + (a ? 2 : 0) + (b ? 1 : 0);
+      put<CTAS>(in_first_cta<CTAS>(&s.group_n[at]), n);
+      put<CTAS>(in_first_cta<CTAS>(&s.group_w[at]), w);
+    }
+  }
+  __device__ void put_rest(const Settings& set, uint32_t nm, double m, double raw) {
+    const int at = cta * SM_WARPS + (threadIdx.x >> 5);
+    if (set.min_p > 0.0) {
+      nm = warp_sum(nm);
+      m = warp_sum(m);
+    }
+    if (inv_T != 1.0) raw = warp_sum(raw);
+    if ((threadIdx.x & 31) == 0) {
+      put<CTAS>(in_first_cta<CTAS>(&s.warp_nm[at]), nm);
+      put<CTAS>(in_first_cta<CTAS>(&s.warp_m[at]), m);
+      put<CTAS>(in_first_cta<CTAS>(&s.warp_raw[at]), raw);
+    }
+  }
+  // by the leading warp, after a barrier
+  __device__ Totals total(const Settings& set) const {
+    const int lane = threadIdx.x & 31;
+    Totals t = {};
+    for (int g = lane; g < groups; g += 32) {
+      t.n += s.group_n[g];
+      t.w += s.group_w[g];
+    }
+    for (int i = lane; i < CTAS * SM_WARPS; i += 32) {
+      t.nm += s.warp_nm[i];
+      t.m += s.warp_m[i];
+      t.raw += s.warp_raw[i];
+    }
+    t.n = warp_sum(t.n);
+    t.w = warp_sum(t.w);
+    t.nm = warp_sum(t.nm);
+    t.m = warp_sum(t.m);
+    t.raw = warp_sum(t.raw);
+    if (!(set.min_p > 0.0)) t.nm = t.n;
+    if (inv_T == 1.0) t.raw = t.w;
+    return t;
   }
 };
 
 // ---- bf16: counts of values -----------------------------------------------------------------------------------------------
 constexpr uint32_t WIN_LO = (127 - 32) << 7, WIN_HI = (127 + 16) << 7, WIN_BINS = WIN_HI - WIN_LO;   // magnitudes' bits
+constexpr int EXPS = WIN_BINS / 128;
+static_assert(8 * EXPS + 1 <= MOST_GROUPS, "groups of the window");
 
-template <bool CLUSTER> struct WindowSums : Finder<CLUSTER> {
-  typedef Finder<CLUSTER> F;
-  using F::s; using F::cta; using F::ctas; using F::q; using F::inv_T;
-  static constexpr int SMEM = (2 * WIN_BINS + 32) * 4 + (CLUSTER ? (WIN_BINS + 8) * 4 : 0);
-  uint32_t* bins;                   // [magnitude][sign], and 32 that nobody reads
-  uint32_t* merged;                 // this CTA's run of places, summed over the cluster
-  uint32_t hi, R, zeros, lo, p0, p1;    // places: positive values from magnitude hi of the window down, zero at R, negative ones from lo up
-  uint32_t base;                    // first place of this CTA
+// Entries, in falling order: the positive values from the window's top binary exponent down, 128 to an exponent; zero, with 31 empty
+// ones behind it; the negative values.  So 32 neighbours have one exponent, and their weights are a geometric sequence.
+template <int CTAS> struct WindowSums : Sums<CTAS> {
+  typedef Sums<CTAS> F;
+  using F::s; using F::cta; using F::groups; using F::inv_T;
+  static constexpr int SMEM = (2 * WIN_BINS + 32) * 4;
+  static constexpr uint32_t ZERO = WIN_BINS;          // entry of zero
+  uint32_t* bins;                   // [magnitude][sign], and 32 for what is outside
+  uint32_t zeros;
   double top;
+  Totals totals;                    // of the leading warp
 
-  __device__ WindowSums(Shared& sh, void* smem, int c, int n) : F(sh, c, n) {
-    bins = reinterpret_cast<uint32_t*>(smem);
-    merged = bins + 2 * WIN_BINS + 32;
-  }
+  __device__ WindowSums(Shared& sh, void* smem, int c) : F(sh, c), bins(reinterpret_cast<uint32_t*>(smem)) { groups = 8 * EXPS + 1; }
+
   // Counts the row.  0, ROW_UNDEFINED (a NaN, +inf, or nothing finite) or ROW_OUTSIDE (values outside the window).
   __device__ uint32_t count(const Share<bf16>& row) {
     uint4* b4 = reinterpret_cast<uint4*>(bins);
-    for (int i = threadIdx.x; i < (int)(2 * WIN_BINS / 4); i += SM_THREADS) b4[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < SMEM / 16; i += SM_THREADS) b4[i] = make_uint4(0u, 0u, 0u, 0u);
     if (threadIdx.x == 0) {
-      s.top = s.hi = s.flags = s.zeros = 0u;
-      s.lo = 0xffffu;
+      s.lo = 0xffffffffu;
+      s.flags = s.zeros = 0u;
     }
     __syncthreads();
-    // a bf16 number turned left by a bit is its magnitude and then its sign; less the window's start, the number of its bin
-    constexpr uint32_t SHIFT = (0x10000u - 2 * WIN_LO) * 0x10001u, LIMIT = (0x8000u - 2 * WIN_BINS) * 0x10001u;
-    uint32_t most = 0u, least = 0xffffffffu, zero = 0u, flags = 0u;   // bins, two at a time
-    __nv_bfloat162 top2 = __float2bfloat162_rn(-INFINITY);
-    const uint32_t aside = (2 * WIN_BINS + (threadIdx.x & 31)) * 0x10001u;   // a bin per lane for what is outside
-    // what makes a word have bins outside: zeros are counted apart, -inf is left out, and the rest is for the row to know
-    auto explain = [&](uint32_t w, uint32_t b) {
-      const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w);
-      const uint32_t zeros2 = __heq2_mask(x, __float2bfloat162_rn(0.f)), none2 = __heq2_mask(x, __float2bfloat162_rn(-INFINITY));
-      zero += __popc(zeros2 & 0x10001u);
-#pragma unroll
-      for (int h = 0; h < 32; h += 16) {
-        const uint32_t bin = (b >> h) & 0xffffu;
-        if (bin < 2 * WIN_BINS) most = max_u16x2(most, bin);
-        else if (!(((zeros2 | none2) >> h) & 1u)) flags |= ((w >> h) & 0x7fffu) >= 0x7f80u ? ROW_UNDEFINED : ROW_OUTSIDE;
-      }
-    };
+    // A bf16 number turned left by a bit is its magnitude and then its sign; less the window's start, the number of its bin.  What
+    // is outside goes to a bin of its lane.
+    constexpr uint32_t SHIFT = (0x10000u - 2 * WIN_LO) * 0x10001u;
+    const uint32_t aside = (2 * WIN_BINS + (threadIdx.x & 31)) * 0x10001u;
+    auto two = [&](uint32_t w) { return min_u16x2(add_u16x2(((w << 1) & 0xfffefffeu) | ((w >> 15) & 0x00010001u), SHIFT), aside); };
+    const uint4* words = row.words();
+    int v = row.v0 + (int)threadIdx.x;
     auto eight = [&](const uint4& u) {
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-      uint32_t b[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        b[i] = min_u16x2(add_u16x2(((w[i] << 1) & 0xfffefffeu) | ((w[i] >> 15) & 0x00010001u), SHIFT), aside);
-        atomicAdd(bins + (b[i] & 0xffffu), 1u);
-        atomicAdd(bins + (b[i] >> 16), 1u);
-        top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+        const uint32_t b = two(w[i]);
+        atomicAdd(bins + (b & 0xffffu), 1u);
+        atomicAdd(bins + (b >> 16), 1u);
       }
-      const uint32_t mx = max_u16x2(max_u16x2(b[0], b[1]), max_u16x2(b[2], b[3]));
-      least = min_u16x2(least, min_u16x2(min_u16x2(b[0], b[1]), min_u16x2(b[2], b[3])));
-      if (((mx + LIMIT) & 0x80008000u) == 0u) most = max_u16x2(most, mx);   // all inside
-      else
-#pragma unroll
-        for (int i = 0; i < 4; ++i) explain(w[i], b[i]);
     };
-    auto one = [&](uint32_t h) {                     // with a -inf beside it
-      const uint32_t w = h | 0xff800000u;
-      const uint32_t b = min_u16x2(add_u16x2(((w << 1) & 0xfffefffeu) | ((w >> 15) & 0x00010001u), SHIFT), aside);
-      atomicAdd(bins + (b & 0xffffu), 1u);
-      least = min_u16x2(least, b);
-      explain(w, b);
-      top2 = __hmax2(top2, *reinterpret_cast<const __nv_bfloat162*>(&w));
-    };
-    const uint4* w = row.words();
-    int v = row.v0 + (int)threadIdx.x;
     for (; v + 3 * SM_THREADS < row.v1; v += 4 * SM_THREADS) {
       uint4 u[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = w[v + i * SM_THREADS];
+      for (int i = 0; i < 4; ++i) u[i] = words[v + i * SM_THREADS];
 #pragma unroll
       for (int i = 0; i < 4; ++i) eight(u[i]);
     }
-    for (; v < row.v1; v += SM_THREADS) eight(w[v]);
+    for (; v < row.v1; v += SM_THREADS) eight(words[v]);
     const uint16_t* raw = reinterpret_cast<const uint16_t*>(row.row);
-    if (row.first && (int)threadIdx.x < row.head) one(raw[threadIdx.x]);
-    if (row.last && row.tail0 + (int)threadIdx.x < row.vocab) one(raw[row.tail0 + threadIdx.x]);
-
-    const uint32_t hi1 = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
-    const uint32_t lo1 = __reduce_min_sync(0xffffffffu, min(least & 0xffffu, least >> 16));   // behind the window where there are none
-    const uint32_t top1 = __reduce_max_sync(0xffffffffu, key_of(fmaxf(__low2float(top2), __high2float(top2))));
-    const uint32_t zero1 = warp_sum(zero);
-    flags = __reduce_or_sync(0xffffffffu, flags);
-    if ((threadIdx.x & 31) == 0) {
-      atomicMax(&s.hi, hi1);
-      atomicMin(&s.lo, lo1);
-      atomicMax(&s.top, top1);
-      atomicAdd(&s.zeros, zero1);
-      atomicOr(&s.flags, flags);
+    const int at_head = row.first && (int)threadIdx.x < row.head ? (int)threadIdx.x : -1;
+    const int at_tail = row.last && row.tail0 + (int)threadIdx.x < row.vocab ? row.tail0 + (int)threadIdx.x : -1;
+    if (at_head >= 0) atomicAdd(bins + (two(raw[at_head]) & 0xffffu), 1u);
+    if (at_tail >= 0) atomicAdd(bins + (two(raw[at_tail]) & 0xffffu), 1u);
+    __syncthreads();
+    // the first entry that has tokens: that of the largest logit, if nothing above the window comes to light
+    uint32_t first = 0xffffffffu;
+    for (uint32_t e = threadIdx.x; e < 2 * WIN_BINS; e += SM_THREADS)
+      if (bins[bin_of(e < ZERO ? e : e + 32)]) {
+        first = e < ZERO ? e : e + 32;
+        break;
+      }
+    // were there any outside?  zeros are counted apart, -inf is left out, and the rest is for the row to know
+    if (__syncthreads_or(threadIdx.x < 32 && bins[2 * WIN_BINS + threadIdx.x])) {
+      uint32_t zero = 0u, flags = 0u;
+      auto explain = [&](uint32_t w) {
+        const uint32_t m = w & 0x7fff7fffu;
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+          const uint32_t x = (m >> h) & 0xffffu;
+          if (x - WIN_LO < WIN_BINS) continue;
+          if (x == 0u) ++zero;
+          else if (x < 0x7f80u) flags |= ROW_OUTSIDE;
+          else if (((w >> h) & 0xffffu) != 0xff80u) flags |= ROW_UNDEFINED;
+        }
+      };
+      for (v = row.v0 + (int)threadIdx.x; v < row.v1; v += SM_THREADS) {
+        const uint4 u = words[v];
+        explain(u.x);
+        explain(u.y);
+        explain(u.z);
+        explain(u.w);
+      }
+      if (at_head >= 0) explain(raw[at_head] | 0xff800000u);
+      if (at_tail >= 0) explain(raw[at_tail] | 0xff800000u);
+      zero = warp_sum(zero);
+      flags = __reduce_or_sync(0xffffffffu, flags);
+      if ((threadIdx.x & 31) == 0) {
+        atomicAdd(&s.zeros, zero);
+        atomicOr(&s.flags, flags);
+      }
     }
-    row_sync<CLUSTER>();
-    uint32_t t = s.top, f = s.flags;
-    hi = s.hi; lo = s.lo; zeros = s.zeros;
-    if (CLUSTER) {
-      hi = t = f = zeros = 0u;
-      lo = 0xffffu;
-      for (int c = 0; c < ctas; ++c) {
-        hi = max(hi, ld_cluster_u32(mapa_u32(smem_u32(&s.hi), c)));
-        lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
-        t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
+    first = __reduce_min_sync(0xffffffffu, first);
+    if ((threadIdx.x & 31) == 0) atomicMin(&s.lo, first);
+    row_sync<CTAS>();
+    uint32_t f = s.flags;
+    first = s.lo;
+    zeros = s.zeros;
+    if (CTAS > 1) {
+      f = zeros = 0u;
+      for (int c = 0; c < CTAS; ++c) {
+        first = min(first, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
         f |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
         zeros += ld_cluster_u32(mapa_u32(smem_u32(&s.zeros), c));
       }
     }
-    hi >>= 1;
-    lo >>= 1;
-    top = (double)value_of(t);
-    if ((f & ROW_UNDEFINED) || t == key_of(-INFINITY)) return ROW_UNDEFINED;
-    return f & ROW_OUTSIDE;
+    if (f) return f & ROW_UNDEFINED ? ROW_UNDEFINED : ROW_OUTSIDE;
+    if (zeros) first = min(first, ZERO);
+    if (first == 0xffffffffu) return ROW_UNDEFINED;
+    top = (double)value(first);
+    return 0u;
   }
-  // bin and value of a place
-  __device__ uint32_t bin_of(uint32_t p) const { return p < R ? 2 * (hi - p) : 2 * (lo + (p - R - 1)) + 1; }
-  __device__ float value(uint32_t p) const {
-    return p == R ? 0.f : __uint_as_float(p < R ? (WIN_LO + hi - p) << 16 : 0x80000000u | (WIN_LO + lo + (p - R - 1)) << 16);
+  // bin and value of an entry other than zero's group
+  __device__ static uint32_t bin_of(uint32_t e) { return e < ZERO ? 2 * (WIN_BINS - 1 - e) : 2 * (e - ZERO - 32) + 1; }
+  __device__ static float value(uint32_t e) {
+    if (e < ZERO) return __uint_as_float((WIN_HI - 1 - e) << 16);
+    return e < ZERO + 32 ? 0.f : __uint_as_float(0x80000000u | (WIN_LO + e - ZERO - 32) << 16);
   }
-  __device__ uint32_t tokens(uint32_t p) const { return CLUSTER ? merged[p - base] : p == R ? zeros : bins[bin_of(p)]; }
   __device__ double largest_value() const { return top; }
-  __device__ double weight(uint32_t p) const { return exp_falling(((double)value(p) - top) * inv_T, s.powers); }
+  __device__ uint32_t tokens(uint32_t e) const {
+    if (e - ZERO < 32u) return e == ZERO ? zeros : 0u;
+    const uint32_t b = bin_of(e);
+    if (CTAS == 1) return bins[b];
+    uint32_t c[CTAS], sum = 0u;
+#pragma unroll
+    for (int i = 0; i < CTAS; ++i) c[i] = ld_cluster_u32(mapa_u32(smem_u32(bins + b), i));
+#pragma unroll
+    for (int i = 0; i < CTAS; ++i) sum += c[i];
+    return sum;
+  }
+  // of an entry that has tokens
+  __device__ double weight(uint32_t e) const { return exp_falling(fmin((double)value(e) - top, 0.0) * inv_T, s.powers); }
 
+  // Four groups at a time, those of an exponent: 128 neighbours, lane + 32 k.  The k-th weight is the first times that of 32 steps to the k, but in
+  // the exponent of the largest logit, where there are values above it.
   __device__ void sum(const Settings& set) {
     inv_T = set.greedy ? 1.0 : 1.0 / set.T;
-    R = hi >= lo ? hi - lo + 1 : 0u;
-    // the place of the largest logit: those before it are empty
-    const uint32_t mag = (__float_as_uint((float)top) & 0x7fffffffu) >> 16;
-    const uint32_t p_top = top > 0.0 ? hi - (mag - WIN_LO) : top == 0.0 ? R : R + 1 + (mag - WIN_LO - lo), places = 2 * R + 1 - p_top;
-    base = p_top + places * cta / ctas;
-    const uint32_t end = p_top + places * (cta + 1) / ctas;
-    if (CLUSTER) {
-      for (uint32_t p = base + threadIdx.x; p < end; p += SM_THREADS) {
-        uint32_t c = zeros;
-        if (p != R) {
-          const uint32_t a = smem_u32(bins + bin_of(p));
-          c = 0u;
-          for (int i = 0; i < ctas; ++i) c += ld_cluster_u32(mapa_u32(a, i));
-        }
-        merged[p - base] = c;
-      }
-      __syncthreads();
-    }
-    const uint32_t each = (end - base + SM_THREADS - 1) / SM_THREADS;
-    p0 = min(end, base + each * threadIdx.x);
-    p1 = min(end, p0 + each);
-    q.n = 0u;
-    q.w = 0.0;
+    const int lane = threadIdx.x & 31;
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
-    const bool plain = inv_T == 1.0;
-#pragma unroll 2
-    for (uint32_t p = p0; p < p1; ++p) {              // no branch on empty bins: a warp has hardly a step without a full one
-      const uint32_t c = tokens(p);
-      const double w = weight(p), cw = c * w;
-      q.n += c;
-      q.w += cw;
-      raw += plain ? cw : (double)((float)c * expf((float)((double)value(p) - top)));
-      const bool keeps = w >= set.min_p;
-      nm += keeps ? c : 0u;
-      m += keeps ? cw : 0.0;
-    }
-    sum_runs<CLUSTER>(s, q, nm, m, raw, ctas, cta);
-  }
-  __device__ Found find(const Share<bf16>&, const Ask& ask) {
-    const Found f = F::search(ask, q, [&](Walk& k) {
-      for (uint32_t p = p0; p < p1; ++p) {
-        const uint32_t c = tokens(p);
-        if (c && k.step(ask, c, weight(p), key_of(value(p)))) break;
+    auto account = [&](uint32_t c, double w, double cw, uint32_t e) {
+      if (inv_T != 1.0 && c) raw += (float)c * expf((float)((double)value(e) - top));
+      if (set.min_p > 0.0 && w >= set.min_p) {
+        nm += c;
+        m += cw;
       }
+    };
+    for (int x = cta * SM_WARPS + (threadIdx.x >> 5); x < 2 * EXPS + 1; x += CTAS * SM_WARPS) {
+      if (x == 2 * EXPS) {
+        const uint32_t c = lane ? 0u : zeros;
+        const double w = c ? weight(ZERO) : 0.0, cw = c * w;
+        account(c, w, cw, ZERO);
+        this->put_group(ZERO / 32, c, cw);
+        continue;
+      }
+      const uint32_t e = (x < EXPS ? 0u : 32u) + 128u * x + lane;
+      uint32_t c[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] = tokens(e + 32 * k);
+      double cw[4];
+      if (!__any_sync(0xffffffffu, c[0] | c[1] | c[2] | c[3])) {
+        if (lane < 4) {
+          put<CTAS>(in_first_cta<CTAS>(&s.group_n[(e >> 5) + lane]), 0u);
+          put<CTAS>(in_first_cta<CTAS>(&s.group_w[(e >> 5) + lane]), 0.0);
+        }
+      } else {
+        double w = weight(e);
+        const bool with_top = (double)value(e - lane) > top;
+        const double ratio = exp_falling(((double)value(e - lane + 32) - (double)value(e - lane)) * inv_T, s.powers);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (k) w = with_top ? weight(e + 32 * k) : w * ratio;
+          cw[k] = c[k] ? c[k] * w : 0.0;
+          account(c[k], w, cw[k], e + 32 * k);
+        }
+        this->put_groups4((int)(e >> 5), c, cw);
+      }
+    }
+    this->put_rest(set, nm, m, raw);
+    row_sync<CTAS>();
+    if (this->leads()) totals = this->total(set);
+  }
+  // by the leading warp alone
+  __device__ Found find(const Share<bf16>&, Ask ask) const {
+    Found f = search(s, groups, ask, [&](int e, uint32_t& c, double& w) {
+      c = tokens(e);
+      w = c ? weight(e) : 0.0;
     });
-    return f.valid ? f : F::behind_all(q.total_w);
+    f.key = key_of(value(f.entry));
+    return f;
   }
 };
 
@@ -527,27 +537,28 @@ constexpr int BINS = 2048, LIMBS = 4, LIMB_BITS = 14;   // of a weight in units 
 constexpr double WEIGHT_UNIT = 18014398509481984.0;     // 2^54
 constexpr int LIST = 256;                               // tokens that are ranked against one another
 
-template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
-  typedef Finder<CLUSTER> F;
-  using F::s; using F::cta; using F::ctas; using F::q; using F::inv_T;
+template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
+  typedef Sums<CTAS> F;
+  using F::s; using F::cta; using F::groups; using F::inv_T;
   static constexpr int SMEM = BINS * (1 + LIMBS) * 4 + LIST * 16;
-  static constexpr int EACH = BINS / SM_THREADS;        // bins to a thread; in a cluster the CTAs share them out
   uint32_t* bins;                   // [1 + LIMBS][BINS]: tokens, limbs
   unsigned long long* weights;      // [LIST]
   uint32_t *list, *keys;            // [LIST]: this CTA's tokens of a bin, and those of the whole row
-  float topf, step;                 // bins to a unit of the logits
-  uint32_t c0[EACH];                // this thread's bins, from the top
-  double w0[EACH];
+  float topf, step;                 // the largest, and bins to a unit of the logits
+  int turn = 0;
+  bool whole = false;               // the bins are those of the whole row
+  Totals totals;
 
-  __device__ BinnedSums(Shared& sh, void* smem, int c, int n) : F(sh, c, n) {
+  __device__ BinnedSums(Shared& sh, void* smem, int c) : F(sh, c) {
     bins = reinterpret_cast<uint32_t*>(smem);
     weights = reinterpret_cast<unsigned long long*>(bins + BINS * (1 + LIMBS));
     list = reinterpret_cast<uint32_t*>(weights + LIST);
     keys = list + LIST;
+    groups = BINS / 32;
   }
   // the row's largest and smallest finite logits; 0 or ROW_UNDEFINED
   __device__ uint32_t range(const Share<T>& row, float& least) {
-    row_sync<CLUSTER>();                            // nobody reads what these words held before
+    row_sync<CTAS>();                            // nobody reads what these words held before
     if (threadIdx.x == 0) {
       s.top = s.flags = 0u;
       s.lo = 0xffffffffu;
@@ -568,11 +579,11 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
       atomicMin(&s.lo, lo);
       atomicOr(&s.flags, flags);
     }
-    row_sync<CLUSTER>();
+    row_sync<CTAS>();
     t = s.top;
     lo = s.lo;
     flags = s.flags;
-    for (int c = 0; CLUSTER && c < ctas; ++c) {
+    for (int c = 0; CTAS > 1 && c < CTAS; ++c) {
       t = max(t, ld_cluster_u32(mapa_u32(smem_u32(&s.top), c)));
       lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
       flags |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
@@ -601,64 +612,82 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
       w >>= LIMB_BITS;
     }
   }
-  // this thread's bins summed over the row, and the runs they make
-  __device__ void collect(Runs& r, uint32_t* c, double* w, uint32_t& first, uint32_t nm, double m, double raw) {
-    const uint32_t per = CLUSTER ? BINS / ctas : BINS, each = (per + SM_THREADS - 1) / SM_THREADS;
-    first = cta * per + threadIdx.x * each;
-    r.n = 0u;
-    r.w = 0.0;
+  // a bin summed over the row: tokens and their mean weight
+  __device__ void entry(uint32_t e, uint32_t& c, double& w) const {
+    const uint32_t a = smem_u32(bins + e);
+    unsigned long long limb[LIMBS] = {};
+    c = 0u;
+    uint32_t part[CTAS][1 + LIMBS];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      c[i] = 0u;
-      w[i] = 0.0;
-      if (i >= (int)each || threadIdx.x * each + i >= per) continue;
-      const uint32_t a = smem_u32(bins + first + i);
-      unsigned long long limb[LIMBS] = {};
-      for (int p = 0; p < (CLUSTER ? ctas : 1); ++p) {
-        const uint32_t b = CLUSTER ? mapa_u32(a, p) : 0u;
-        c[i] += CLUSTER ? ld_cluster_u32(b) : bins[first + i];
+    for (int p = 0; p < CTAS; ++p)
 #pragma unroll
-        for (int l = 0; l < LIMBS; ++l) limb[l] += CLUSTER ? ld_cluster_u32(b + 4 * BINS * (l + 1)) : bins[first + i + BINS * (l + 1)];
-      }
-      double v = 0.0;
+      for (int l = 0; l <= LIMBS; ++l) part[p][l] = CTAS > 1 ? ld_cluster_u32(mapa_u32(a, p) + 4 * BINS * l) : bins[e + BINS * l];
 #pragma unroll
-      for (int l = LIMBS - 1; l >= 0; --l) v = v * (double)(1 << LIMB_BITS) + (double)limb[l];
-      w[i] = v / WEIGHT_UNIT;
-      r.n += c[i];
-      r.w += w[i];
+    for (int p = 0; p < CTAS; ++p) {
+      c += part[p][0];
+#pragma unroll
+      for (int l = 0; l < LIMBS; ++l) limb[l] += part[p][l + 1];
     }
-    sum_runs<CLUSTER>(s, r, nm, m, raw, ctas, cta);
-  }
-  // the bin that holds what is asked for
-  __device__ Found open(const Ask& ask, const Runs& r, const uint32_t* c, const double* w, uint32_t first) {
-    return F::search(ask, r, [&](Walk& k) {
+    double v = 0.0;
 #pragma unroll
-      for (int i = 0; i < EACH; ++i)
-        if (c[i] && k.step(ask, c[i], w[i] / c[i], first + i)) break;
-    });
+    for (int l = LIMBS - 1; l >= 0; --l) v = v * (double)(1 << LIMB_BITS) + (double)limb[l];
+    w = v / (WEIGHT_UNIT * max(c, 1u));
   }
-  uint32_t first0;
+  __device__ void collect() {
+    for (int g = cta * SM_WARPS + (threadIdx.x >> 5); g < groups; g += CTAS * SM_WARPS) {
+      uint32_t c;
+      double w;
+      entry(32 * g + (threadIdx.x & 31), c, w);
+      this->put_group(g, c, c * w);
+    }
+  }
+  template <typename G> __device__ void bin_all(const Share<T>& row, G also) {
+    clear();
+    row.each([&](float x) {
+      if (x == -INFINITY) return;
+      const unsigned long long w = weight(x);
+      add(bin_of(x), w);
+      also(x, w);
+    });
+    row_sync<CTAS>();
+    collect();
+    whole = true;
+  }
   __device__ void sum(const Share<T>& row, const Settings& set, float least) {
     inv_T = set.greedy ? 1.0 : 1.0 / set.T;
     // beyond 50 T the weights are below 2^-72 of the largest
     const float span = (float)fmin((double)topf - (double)least, 50.0 / inv_T);
     step = span > 0.f ? fminf((float)BINS / span, 3.4e38f) : 0.f;
-    clear();
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
-    row.each([&](float x) {
-      if (x == -INFINITY) return;
-      const unsigned long long w = weight(x);
-      add(bin_of(x), w);
+    bin_all(row, [&](float x, unsigned long long w) {
+      if (inv_T != 1.0) raw += (double)expf(x - topf);
       const double v = (double)w / WEIGHT_UNIT;
-      raw += inv_T == 1.0 ? v : (double)expf(x - topf);
-      if (v >= set.min_p) {
+      if (set.min_p > 0.0 && v >= set.min_p) {
         ++nm;
         m += v;
       }
     });
-    row_sync<CLUSTER>();
-    collect(q, c0, w0, first0, nm, m, raw);
+    this->put_rest(set, nm, m, raw);
+    row_sync<CTAS>();
+    if (this->leads()) publish<CTAS>(s.totals, this->total(set));
+    row_sync<CTAS>();
+    totals = s.totals;
+  }
+  // the bin that holds what is asked for, for all threads; also whether roundings had it changed
+  __device__ Found open(Ask& ask, uint32_t before_n, double before_w) {
+    Found& slot = s.found[turn];
+    turn ^= 1;
+    if (this->leads()) {
+      Ask mine = ask;
+      const Found f = search(s, groups, mine, [&](int e, uint32_t& c, double& w) { entry(e, c, w); }, before_n, before_w);
+      publish<CTAS>(slot, f);
+    }
+    row_sync<CTAS>();
+    const Found f = slot;
+    // the target lies behind the whole of what was searched: its last token
+    if (!ask.by_rank && !reaches(f.mass, ask.target, ask.strict) && f.nth == f.tokens - 1) ask = ask_rank(f.rank);
+    return f;
   }
   // Members of a bin: of the first binning, and where that was not enough keys from ka to kb.
   struct Members {
@@ -666,13 +695,16 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
   };
   __device__ bool in(const Members& b, float x, uint32_t k) const { return x != -INFINITY && bin_of(x) == b.bin && k >= b.ka && k <= b.kb; }
 
-  __device__ Found find(const Share<T>& row, const Ask& asked) {
-    Ask ask = asked;
-    Found f = open(ask, q, c0, w0, first0);
-    if (!f.valid) return F::behind_all(q.total_w);
-    Members b = {f.key, 0u, 0xffffffffu};
+  __device__ Found find(const Share<T>& row, Ask ask) {
+    if (!whole) {                                   // an earlier find has opened a bin
+      bin_all(row, [](float, unsigned long long) {});
+      row_sync<CTAS>();
+    }
+    Found f = open(ask, 0u, 0.0);
+    Members b = {f.entry, 0u, 0xffffffffu};
     while (f.tokens > LIST) {
       // the keys that occur, and bins for them
+      whole = false;
       if (threadIdx.x == 0) {
         s.hi = 0u;
         s.lo = 0xffffffffu;
@@ -692,41 +724,29 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
         atomicMin(&s.lo, lo);
         atomicMax(&s.hi, hi);
       }
-      row_sync<CLUSTER>();
+      row_sync<CTAS>();
       lo = s.lo;
       hi = s.hi;
-      for (int c = 0; CLUSTER && c < ctas; ++c) {
+      for (int c = 0; CTAS > 1 && c < CTAS; ++c) {
         lo = min(lo, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
         hi = max(hi, ld_cluster_u32(mapa_u32(smem_u32(&s.hi), c)));
       }
       if (lo == hi) {                               // one value: no need to look at its tokens
-        Walk k;
-        k.cum = f.before_w;
-        k.n = f.before_n;
-        k.step(ask, f.tokens, (double)weight(value_of(lo)) / WEIGHT_UNIT, lo);
-        row_sync<CLUSTER>();
-        return k.f;
+        ask.among(f.tokens, (double)weight(value_of(lo)) / WEIGHT_UNIT, f);
+        f.key = lo;
+        row_sync<CTAS>();
+        return f;
       }
       const int shift = max(0, 21 - __clz(hi - lo));  // 32 - clz bits, of which the bins tell 11
       row.each([&](float x) {
         const uint32_t k = key_of(x);
         if (in(b, x, k)) add((hi - k) >> shift, weight(x));
       });
-      row_sync<CLUSTER>();
-      uint32_t c[EACH], first;
-      double w[EACH];
-      Runs r;
-      collect(r, c, w, first, 0u, 0.0, 0.0);
-      r.excl_n += f.before_n; r.incl_n += f.before_n;
-      r.excl_w += f.before_w; r.incl_w += f.before_w;
-      const uint32_t last = f.before_n + f.tokens - 1;
-      Found g = open(ask, r, c, w, first);
-      if (!g.valid) {                               // by roundings: the last token of the bin
-        ask = ask_rank(last);
-        g = open(ask, r, c, w, first);
-      }
-      f = g;
-      b.kb = hi - (g.key << shift);
+      row_sync<CTAS>();
+      collect();
+      row_sync<CTAS>();
+      f = open(ask, f.before_n, f.before_w);
+      b.kb = hi - (f.entry << shift);
       b.ka = shift ? max(lo, b.kb - ((1u << shift) - 1)) : b.kb;
     }
     // few tokens: each is ranked against all
@@ -739,14 +759,14 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
         if (at < LIST) list[at] = k;
       }
     });
-    row_sync<CLUSTER>();
+    row_sync<CTAS>();
     const uint32_t n = f.tokens, i = threadIdx.x;
     if (i < n) {
       uint32_t at = i, k = 0u;
-      for (int c = 0; c < (CLUSTER ? ctas : 1); ++c) {
-        const uint32_t has = CLUSTER ? ld_cluster_u32(mapa_u32(smem_u32(&s.list_n), c)) : s.list_n;
+      for (int c = 0; c < CTAS; ++c) {
+        const uint32_t has = CTAS > 1 ? ld_cluster_u32(mapa_u32(smem_u32(&s.list_n), c)) : s.list_n;
         if (at < has) {
-          k = CLUSTER ? ld_cluster_u32(mapa_u32(smem_u32(list + at), c)) : list[at];
+          k = CTAS > 1 ? ld_cluster_u32(mapa_u32(smem_u32(list + at), c)) : list[at];
           break;
         }
         at -= has;
@@ -769,50 +789,61 @@ template <typename T, bool CLUSTER> struct BinnedSums : Finder<CLUSTER> {
         }
       }
       const double w = (double)weights[i] / WEIGHT_UNIT, cum = f.before_w + (double)sum / WEIGHT_UNIT;
-      if (ask.by_rank ? ask.rank < f.before_n + before + same : reaches(cum + same * w, ask.target, ask.strict)) atomicMin(&s.owner, before);
+      if (ask.in(f.before_n + before + same, cum + same * w)) atomicMin(&s.owner, before);
     }
     __syncthreads();
     const bool none = s.owner == 0xffffffffu;        // by roundings: the last token
+    Found& here = s.found[turn];
+    turn ^= 1;
     if (i < n && (none ? before + same == n : before == s.owner)) {
       if (none) ask = ask_rank(f.before_n + n - 1);
-      Walk k;
-      k.cum = f.before_w + (double)sum / WEIGHT_UNIT;
-      k.n = f.before_n + before;
-      k.step(ask, same, (double)weights[i] / WEIGHT_UNIT, keys[i]);
-      s.here = k.f;                                  // equal tokens write the same
+      Found g = f;
+      g.before_w = f.before_w + (double)sum / WEIGHT_UNIT;
+      g.before_n = f.before_n + before;
+      g.key = keys[i];
+      ask.among(same, (double)weights[i] / WEIGHT_UNIT, g);
+      here = g;                                      // equal tokens write the same
     }
-    __syncthreads();
-    return s.here;
+    row_sync<CTAS>();
+    return here;
   }
 };
 
-// The settings' prefix and the token drawn from it.
+// The settings' prefix and the token drawn from it: up to four finds, one after another.
 template <typename S, typename T> __device__ Found draw(S& sums, const Share<T>& row, const Settings& set, uint32_t& kept) {
-  const Runs& q = sums.q;
-  uint32_t n = q.total_n;
-  double mass = q.total_w;
-  if (set.greedy) {
-    kept = 1u;
-    return sums.find(row, ask_rank(0u));
-  }
-  if (set.top_k > 0 && (uint32_t)set.top_k < n) {
-    n = (uint32_t)set.top_k;
-    mass = sums.find(row, ask_rank(n - 1)).mass;
-  }
-  if (set.top_p < 1.0) {
-    const Found f = sums.find(row, ask_mass(set.top_p * mass, false));
-    if (f.rank < n - 1) {
-      n = f.rank + 1;
-      mass = f.mass;
-    }
-  }
-  if (q.total_nm < n) {                              // min-p keeps the largest at least: its weight is 1
-    n = q.total_nm;
-    mass = q.total_m;
+  const Totals& q = sums.totals;
+  uint32_t n = q.n;
+  double mass = q.w;
+  enum { TOP_K, TOP_P, MIN_P, DRAW, LAST };
+  Found f;
+#pragma unroll 1
+  for (int step = TOP_K;; ++step) {
+    Ask ask;
+    if (step == TOP_K) {
+      if (set.top_k <= 0 || (uint32_t)set.top_k >= n || set.greedy) continue;
+      ask = ask_rank((uint32_t)set.top_k - 1);
+    } else if (step == TOP_P) {
+      if (!(set.top_p < 1.0) || set.greedy) continue;
+      ask = ask_mass(set.top_p * mass, false);
+    } else if (step == MIN_P) {                      // keeps the largest at least: its weight is 1
+      if (set.greedy) n = 1u;
+      else if (q.nm < n) {
+        n = q.nm;
+        mass = q.m;
+      }
+      continue;
+    } else if (step == DRAW && !set.greedy) ask = ask_mass((double)set.u * mass, true);
+    else ask = ask_rank(n - 1);                      // the largest, or by roundings the prefix's last
+    f = sums.find(row, ask);
+    if (step <= TOP_P) {
+      if (f.rank < n - 1) {
+        n = f.rank + 1;
+        mass = f.mass;
+      }
+    } else if (f.rank < n) break;
   }
   kept = n;
-  const Found f = sums.find(row, ask_mass((double)set.u * mass, true));
-  return f.rank < n ? f : sums.find(row, ask_rank(n - 1));
+  return f;
 }
 
 // The tokens of a 16-byte word that equal x, a bit for each, and their number.
@@ -841,8 +872,8 @@ template <> struct Matcher<bf16> {
 };
 
 // The nth token of the value that has this key: a count over the row, then the one warp's words that hold it once more.
-template <typename T, bool CLUSTER>
-__device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int cta, int ctas, int32_t* token) {
+template <typename T, int CTAS>
+__device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int cta, int32_t* token) {
   constexpr int V = Share<T>::V;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float x = value_of(f.key);
@@ -867,7 +898,7 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
     if (i == warp) before = all;
     all += s.matches[i];
   }
-  if (CLUSTER) {
+  if (CTAS > 1) {
     if (threadIdx.x == 0) s.cta_matches = all;
     cluster_sync_all();
     for (int c = 0; c < cta; ++c) before += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_matches), c));
@@ -903,54 +934,38 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
   if (in_tail && (uint32_t)__popc(tail_at & ((1u << lane) - 1)) == left) *token = row.tail0 + lane;
 }
 
-template <typename T, bool CLUSTER> struct SampleSmem {
-  static constexpr int BYTES = BinnedSums<T, CLUSTER>::SMEM;
+template <typename T, int CTAS> struct SampleSmem {
+  static constexpr int BYTES = BinnedSums<T, CTAS>::SMEM;
 };
-template <bool CLUSTER> struct SampleSmem<bf16, CLUSTER> {
-  static constexpr int W = WindowSums<CLUSTER>::SMEM, R = BinnedSums<bf16, CLUSTER>::SMEM, BYTES = W > R ? W : R;
+template <int CTAS> struct SampleSmem<bf16, CTAS> {
+  static constexpr int W = WindowSums<CTAS>::SMEM, R = BinnedSums<bf16, CTAS>::SMEM, BYTES = W > R ? W : R;
 };
 
-template <typename S, typename T, bool CLUSTER>
-__device__ void finish(Shared& s, S& sums, const Share<T>& row, const Settings& set, const SampleArgs& a, int r, int cta, int ctas) {
-  uint32_t kept;
-  const Found f = draw(sums, row, set, kept);
-  write_token<T, CLUSTER>(s, row, f, cta, ctas, a.token + r);
-  if (cta == 0 && threadIdx.x == 0) {
-    if (a.conf) a.conf[r] = (float)(exp((double)value_of(f.key) - sums.largest_value()) / sums.q.total_raw);
-    if (a.n_kept) a.n_kept[r] = (int32_t)kept;
-  }
+// by one thread of the row, which has the sums
+template <typename S> __device__ void write_rest(const S& sums, const Found& f, uint32_t kept, const SampleArgs& a, int r) {
+  if (a.conf) a.conf[r] = (float)(exp_falling((double)value_of(f.key) - sums.largest_value(), sums.s.powers) / sums.totals.raw);
+  if (a.n_kept) a.n_kept[r] = (int32_t)kept;
 }
 
 // apart, so that the bf16 rows' method keeps its registers
-template <typename T, bool CLUSTER>
+template <typename T, int CTAS>
 __device__ __noinline__ uint32_t sample_binned(Shared& s, void* smem, const Share<T>& row, const Settings& set, const SampleArgs& a, int r,
-                                               int cta, int ctas) {
-  BinnedSums<T, CLUSTER> sums(s, smem, cta, ctas);
+                                               int cta) {
+  BinnedSums<T, CTAS> sums(s, smem, cta);
   float least;
   const uint32_t state = sums.range(row, least);
   if (state == 0u) {
     sums.sum(row, set, least);
-    finish<BinnedSums<T, CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+    uint32_t kept;
+    const Found f = draw(sums, row, set, kept);
+    if (cta == 0 && threadIdx.x == 0) write_rest(sums, f, kept, a, r);
+    write_token<T, CTAS>(s, row, f, cta, a.token + r);
   }
   return state;
 }
 
-template <typename T, bool CLUSTER>
-__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ Shared s;
-  griddep_wait();
-  griddep_launch();
-  if (threadIdx.x < 32) s.powers[threadIdx.x] = exp2(threadIdx.x / 32.0);   // seen after the first barrier
-  int cta = 0, ctas = 1;
-  if (CLUSTER) {
-    uint32_t n;
-    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
-    ctas = (int)n;
-    cta = (int)cluster_ctarank();
-  }
-  const int r = blockIdx.x / ctas;
-  if (r >= min(*a.n_active, a.max_rows)) return;
+template <typename T, int CTAS>
+__device__ __forceinline__ void sample_row(const SampleArgs& a, Shared& s, unsigned char* smem, int r, int cta) {
   Settings set;
   {
     const int i = a.set_of_row ? a.set_of_row[r] : a.sets.n_sets == 1 ? 0 : r;
@@ -967,23 +982,30 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_cons
     set.min_p = m > 0.f ? (double)fminf(m, 1.f) : 0.0;
     set.u = fminf(fmaxf(a.u[r], 0.f), 0.99999994f);
   }
-  const Share<T> row((const T*)a.logits + r * a.row_stride, a.vocab, cta, ctas);
+  const Share<T> row((const T*)a.logits + r * a.row_stride, a.vocab, cta, CTAS);
   uint32_t state = ROW_UNDEFINED;
   if (set.ok) {
     bool binned = true;
     if constexpr (sizeof(T) == 2) {
-      WindowSums<CLUSTER> sums(s, smem, cta, ctas);
+      WindowSums<CTAS> sums(s, smem, cta);
       state = sums.count(row);
       binned = state == ROW_OUTSIDE;
       if (state == 0u) {
         sums.sum(set);
-        finish<WindowSums<CLUSTER>, T, CLUSTER>(s, sums, row, set, a, r, cta, ctas);
+        if (sums.leads()) {
+          uint32_t kept;
+          const Found f = draw(sums, row, set, kept);
+          publish<CTAS>(s.found[0], f);
+          if (threadIdx.x == 0) write_rest(sums, f, kept, a, r);
+        }
+        row_sync<CTAS>();
+        write_token<T, CTAS>(s, row, s.found[0], cta, a.token + r);
       }
     }
     if (binned) {
       const Share<T> row1 = row;                     // copies: the function wants their addresses
       const Settings set1 = set;
-      state = sample_binned<T, CLUSTER>(s, smem, row1, set1, a, r, cta, ctas);
+      state = sample_binned<T, CTAS>(s, smem, row1, set1, a, r, cta);
     }
   }
   if (state == ROW_UNDEFINED && cta == 0 && threadIdx.x == 0) {
@@ -991,16 +1013,28 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_cons
     if (a.conf) a.conf[r] = __int_as_float(0x7fffffff);
     if (a.n_kept) a.n_kept[r] = 0;
   }
-  if (CLUSTER) cluster_sync_all();                   // nobody reads this CTA's shared memory any more
 }
 
-template <typename T, bool CLUSTER>
-int launch_sample_ctas(const SampleArgs& a, int ctas, cudaStream_t st) {
-  constexpr int bytes = SampleSmem<T, CLUSTER>::BYTES;
+template <typename T, int CTAS>
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Shared s;
+  griddep_wait();
+  griddep_launch();
+  if (threadIdx.x < 32) s.powers[threadIdx.x] = exp2(threadIdx.x / 32.0);   // seen after the first barrier
+  const int r = blockIdx.x / CTAS, cta = CTAS > 1 ? (int)cluster_ctarank() : 0;
+  if (r >= min(*a.n_active, a.max_rows)) return;
+  sample_row<T, CTAS>(a, s, smem, r, cta);
+  if (CTAS > 1) cluster_sync_all();                   // nobody reads this CTA's shared memory any more
+}
+
+template <typename T, int CTAS>
+int launch_sample_ctas(const SampleArgs& a, cudaStream_t st) {
+  constexpr int bytes = SampleSmem<T, CTAS>::BYTES;
   static std::atomic<uint64_t> done{0};
-  SL_CUDA_TRY(allow_smem(sample_kernel<T, CLUSTER>, bytes, done));
+  SL_CUDA_TRY(allow_smem(sample_kernel<T, CTAS>, bytes, done));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.max_rows * ctas);
+  cfg.gridDim = dim3((unsigned)a.max_rows * CTAS);
   cfg.blockDim = dim3(SM_THREADS);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
@@ -1008,11 +1042,11 @@ int launch_sample_ctas(const SampleArgs& a, int ctas, cudaStream_t st) {
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = ctas;
+  at[1].val.clusterDim.x = CTAS;
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = pdl_enabled() ? at : at + 1;
-  cfg.numAttrs = (pdl_enabled() ? 1 : 0) + (CLUSTER ? 1 : 0);
-  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<T, CLUSTER>, a));
+  cfg.numAttrs = (pdl_enabled() ? 1 : 0) + (CTAS > 1 ? 1 : 0);
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<T, CTAS>, a));
   return SL_OK;
 }
 
@@ -1021,7 +1055,10 @@ template <typename T> int launch_sample_typed(const SampleArgs& a, cudaStream_t 
   while (ctas > 1 && ((long long)a.max_rows * ctas > 2ll * sm_count() || a.vocab < ctas * 4096)) ctas >>= 1;
   while (a.vocab / ctas > (1 << 17) - 16) ctas <<= 1;   // limbs' sums are 32 bits wide
   if ((long long)a.max_rows * ctas > 0x7fffffffll) return SL_EUNSUPPORTED;
-  return ctas > 1 ? launch_sample_ctas<T, true>(a, ctas, st) : launch_sample_ctas<T, false>(a, ctas, st);
+  return ctas == 8   ? launch_sample_ctas<T, 8>(a, st)
+         : ctas == 4 ? launch_sample_ctas<T, 4>(a, st)
+         : ctas == 2 ? launch_sample_ctas<T, 2>(a, st)
+                     : launch_sample_ctas<T, 1>(a, st);
 }
 
 }  // namespace
