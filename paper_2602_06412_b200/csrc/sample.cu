@@ -9,8 +9,8 @@
 // both are answered by sums over values.  Sums are held in 64 bits: with 100000 tokens in the prefix, 32 would draw a neighbour of
 // the right token in one row of a hundred.
 //
-// bf16 rows (WindowSums): a bf16 number is its own histogram bin.  One pass counts the row's values in shared memory, 6144 bins
-// to a sign for magnitudes in [2^-32, 2^16), which leaves the sums to the few thousand distinct values: one exponential each instead of
+// bf16 rows (WindowSums): a bf16 number is its own histogram bin.  One pass counts the row's values in shared memory, 5120 bins
+// to a sign for magnitudes in [2^-28, 2^12), which leaves the sums to the few thousand distinct values: one exponential each instead of
 // one per token, and a sum is exact but for 2^-53 roundings.  The occupied range of bins is then walked in order, a few bins to
 // a thread.  The token's index is found by a second pass that counts the tokens of the value that was drawn, out of the L2.  A row with a
 // finite value outside the window (not zero) is done by the other method.
@@ -51,6 +51,11 @@ __device__ __forceinline__ void add_shared(uint32_t addr, uint32_t v) {
 __device__ __forceinline__ uint32_t add_u16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("add.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 __device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
@@ -125,7 +130,7 @@ struct Shared {                     // beside the bins
   Found found[2];                   // by turns, so that none is overwritten while somebody reads it
   Totals totals;
   uint32_t matches[SM_WARPS], cta_matches;
-  uint32_t top, lo, hi, flags, zeros, list_n, owner;
+  uint32_t top, lo, hi, flags, zeros, list_n, owner, exps[2];
 };
 
 enum { ROW_UNDEFINED = 1, ROW_OUTSIDE = 2 };
@@ -337,19 +342,20 @@ template <int CTAS> struct Sums {
 };
 
 // ---- bf16: counts of values -----------------------------------------------------------------------------------------------
-constexpr uint32_t WIN_LO = (127 - 32) << 7, WIN_HI = (127 + 16) << 7, WIN_BINS = WIN_HI - WIN_LO;   // magnitudes' bits
+constexpr uint32_t WIN_LO = (127 - 28) << 7, WIN_HI = (127 + 12) << 7, WIN_BINS = WIN_HI - WIN_LO;   // magnitudes' bits
 constexpr int EXPS = WIN_BINS / 128;
-static_assert(8 * EXPS + 1 <= MOST_GROUPS, "groups of the window");
+static_assert(8 * EXPS + 1 <= MOST_GROUPS && EXPS <= 64, "groups and exponents of the window");
 
 // Entries, in falling order: the positive values from the window's top binary exponent down, 128 to an exponent; zero, with 31 empty
 // ones behind it; the negative values.  So 32 neighbours have one exponent, and their weights are a geometric sequence.
 template <int CTAS> struct WindowSums : Sums<CTAS> {
   typedef Sums<CTAS> F;
   using F::s; using F::cta; using F::groups; using F::inv_T;
-  static constexpr int SMEM = (2 * WIN_BINS + 32) * 4;
+  static constexpr int SMEM = 2 * (WIN_BINS + 32) * 4;
   static constexpr uint32_t ZERO = WIN_BINS;          // entry of zero
-  uint32_t* bins;                   // [magnitude][sign], and 32 for what is outside
+  uint32_t* bins;                   // [magnitude][sign], and 32 magnitudes for what is outside
   uint32_t zeros;
+  unsigned long long exps;          // the binary exponents that occur, the window's lowest first
   double top;
   Totals totals;                    // of the leading warp
 
@@ -357,126 +363,164 @@ template <int CTAS> struct WindowSums : Sums<CTAS> {
 
   // Counts the row.  0, ROW_UNDEFINED (a NaN, +inf, or nothing finite) or ROW_OUTSIDE (values outside the window).
   __device__ uint32_t count(const Share<bf16>& row) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint4* b4 = reinterpret_cast<uint4*>(bins);
     for (int i = threadIdx.x; i < SMEM / 16; i += SM_THREADS) b4[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < groups; i += SM_THREADS) {
+      s.group_n[i] = 0u;
+      s.group_w[i] = 0.0;
+    }
     if (threadIdx.x == 0) {
-      s.lo = 0xffffffffu;
-      s.flags = s.zeros = 0u;
+      s.hi = s.flags = s.zeros = s.exps[0] = s.exps[1] = 0u;
+      s.lo = WIN_BINS;
     }
     __syncthreads();
-    // A bf16 number turned left by a bit is its magnitude and then its sign; less the window's start, the number of its bin.  What
-    // is outside goes to a bin of its lane.
-    constexpr uint32_t SHIFT = (0x10000u - 2 * WIN_LO) * 0x10001u;
-    const uint32_t aside = (2 * WIN_BINS + (threadIdx.x & 31)) * 0x10001u;
-    auto two = [&](uint32_t w) { return min_u16x2(add_u16x2(((w << 1) & 0xfffefffeu) | ((w >> 15) & 0x00010001u), SHIFT), aside); };
+    // Two numbers at a time: the place of a magnitude in the window, that of this lane's bin aside where it is outside, and from it and
+    // the sign the bin's address.
+    constexpr uint32_t START = (0x10000u - WIN_LO) * 0x10001u;
+    const uint32_t aside = (WIN_BINS + lane) * 0x10001u;
+    auto two = [&](uint32_t w) { return (min_u16x2(add_u16x2(w & 0x7fff7fffu, START), aside) << 3) + ((w >> 13) & 0x00040004u); };
+    auto count_one = [&](uint32_t at) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(bins) + at), 1u); };
     const uint4* words = row.words();
     int v = row.v0 + (int)threadIdx.x;
     auto eight = [&](const uint4& u) {
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t b = two(w[i]);
-        atomicAdd(bins + (b & 0xffffu), 1u);
-        atomicAdd(bins + (b >> 16), 1u);
+        const uint32_t at = two(w[i]);
+        count_one(at & 0xffffu);
+        count_one(at >> 16);
       }
     };
-    for (; v + 3 * SM_THREADS < row.v1; v += 4 * SM_THREADS) {
-      uint4 u[4];
+    uint4 u[4];                                      // the next words, always on their way
 #pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = words[v + i * SM_THREADS];
+    for (int i = 0; i < 4; ++i)
+      if (v + i * SM_THREADS < row.v1) u[i] = words[v + i * SM_THREADS];
+    for (; v < row.v1; v += 4 * SM_THREADS) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) eight(u[i]);
+      for (int i = 0; i < 4; ++i) {
+        const uint4 now = u[i];
+        if (v + (i + 4) * SM_THREADS < row.v1) u[i] = words[v + (i + 4) * SM_THREADS];
+        if (v + i * SM_THREADS < row.v1) eight(now);
+      }
     }
-    for (; v < row.v1; v += SM_THREADS) eight(words[v]);
     const uint16_t* raw = reinterpret_cast<const uint16_t*>(row.row);
     const int at_head = row.first && (int)threadIdx.x < row.head ? (int)threadIdx.x : -1;
     const int at_tail = row.last && row.tail0 + (int)threadIdx.x < row.vocab ? row.tail0 + (int)threadIdx.x : -1;
-    if (at_head >= 0) atomicAdd(bins + (two(raw[at_head]) & 0xffffu), 1u);
-    if (at_tail >= 0) atomicAdd(bins + (two(raw[at_tail]) & 0xffffu), 1u);
+    if (at_head >= 0) count_one(two(raw[at_head]) & 0xffffu);
+    if (at_tail >= 0) count_one(two(raw[at_tail]) & 0xffffu);
     __syncthreads();
-    // the first entry that has tokens: that of the largest logit, if nothing above the window comes to light
-    uint32_t first = 0xffffffffu;
-    for (uint32_t e = threadIdx.x; e < 2 * WIN_BINS; e += SM_THREADS)
-      if (bins[bin_of(e < ZERO ? e : e + 32)]) {
-        first = e < ZERO ? e : e + 32;
-        break;
-      }
-    // were there any outside?  zeros are counted apart, -inf is left out, and the rest is for the row to know
-    if (__syncthreads_or(threadIdx.x < 32 && bins[2 * WIN_BINS + threadIdx.x])) {
-      uint32_t zero = 0u, flags = 0u;
-      auto explain = [&](uint32_t w) {
-        const uint32_t m = w & 0x7fff7fffu;
+    // which binary exponents occur, and the largest positive and the smallest negative magnitude
+    for (int x = warp; x < EXPS; x += SM_WARPS) {
+      uint32_t hi = 0u, lo = WIN_BINS;
 #pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-          const uint32_t x = (m >> h) & 0xffffu;
-          if (x - WIN_LO < WIN_BINS) continue;
-          if (x == 0u) ++zero;
-          else if (x < 0x7f80u) flags |= ROW_OUTSIDE;
-          else if (((w >> h) & 0xffffu) != 0xff80u) flags |= ROW_UNDEFINED;
-        }
+      for (int k = 3; k >= 0; --k) {
+        const uint32_t m = 128 * x + 32 * k + lane;
+        const uint2 c = reinterpret_cast<const uint2*>(bins)[m];
+        if (c.x && !hi) hi = m + 1;
+        if (c.y) lo = m;
+      }
+      if (!__any_sync(0xffffffffu, hi || lo < WIN_BINS)) continue;
+      hi = __reduce_max_sync(0xffffffffu, hi);
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      if (lane == 0) {
+        atomicOr(&s.exps[x >> 5], 1u << (x & 31));
+        atomicMax(&s.hi, hi);
+        atomicMin(&s.lo, lo);
+      }
+    }
+    // were there any outside?  zeros are counted apart, -inf is left out, and the rest is for the row to know
+    const uint2 out = reinterpret_cast<const uint2*>(bins)[WIN_BINS + lane];
+    if (__any_sync(0xffffffffu, out.x | out.y)) {    // the same for all warps
+      uint32_t zero = 0u, worst = 0u;                // two at a time
+      auto explain = [&](uint32_t w) {
+        const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w);
+        const uint32_t z = __heq2_mask(x, __float2bfloat162_rn(0.f)), none = __heq2_mask(x, __float2bfloat162_rn(-INFINITY));
+        zero += z & 0x10001u;
+        worst = max_u16x2(worst, add_u16x2(w & 0x7fff7fffu, START) & ~(z | none));
       };
       for (v = row.v0 + (int)threadIdx.x; v < row.v1; v += SM_THREADS) {
-        const uint4 u = words[v];
-        explain(u.x);
-        explain(u.y);
-        explain(u.z);
-        explain(u.w);
+        const uint4 w = words[v];
+        explain(w.x);
+        explain(w.y);
+        explain(w.z);
+        explain(w.w);
       }
       if (at_head >= 0) explain(raw[at_head] | 0xff800000u);
       if (at_tail >= 0) explain(raw[at_tail] | 0xff800000u);
-      zero = warp_sum(zero);
-      flags = __reduce_or_sync(0xffffffffu, flags);
-      if ((threadIdx.x & 31) == 0) {
+      zero = warp_sum((zero & 0xffffu) + (zero >> 16));
+      uint32_t flags = max(worst & 0xffffu, worst >> 16) < WIN_BINS ? 0u : ROW_OUTSIDE;
+      if (__any_sync(0xffffffffu, flags)) {
+        row.each([&](float x) {
+          if (!(x < INFINITY)) flags |= ROW_UNDEFINED;
+        });
+        flags = __reduce_or_sync(0xffffffffu, flags);
+      }
+      if (lane == 0) {
         atomicAdd(&s.zeros, zero);
         atomicOr(&s.flags, flags);
       }
     }
-    first = __reduce_min_sync(0xffffffffu, first);
-    if ((threadIdx.x & 31) == 0) atomicMin(&s.lo, first);
     row_sync<CTAS>();
-    uint32_t f = s.flags;
-    first = s.lo;
+    uint32_t f = s.flags, hi = s.hi, lo = s.lo, e0 = s.exps[0], e1 = s.exps[1];
     zeros = s.zeros;
     if (CTAS > 1) {
-      f = zeros = 0u;
+      uint32_t got[CTAS][6];
+      const uint32_t from[6] = {smem_u32(&s.flags), smem_u32(&s.hi), smem_u32(&s.lo), smem_u32(&s.exps[0]), smem_u32(&s.exps[1]), smem_u32(&s.zeros)};
+#pragma unroll
+      for (int c = 0; c < CTAS; ++c)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) got[c][i] = ld_cluster_u32(mapa_u32(from[i], c));
+      zeros = 0u;
+#pragma unroll
       for (int c = 0; c < CTAS; ++c) {
-        first = min(first, ld_cluster_u32(mapa_u32(smem_u32(&s.lo), c)));
-        f |= ld_cluster_u32(mapa_u32(smem_u32(&s.flags), c));
-        zeros += ld_cluster_u32(mapa_u32(smem_u32(&s.zeros), c));
+        f |= got[c][0];
+        hi = max(hi, got[c][1]);
+        lo = min(lo, got[c][2]);
+        e0 |= got[c][3];
+        e1 |= got[c][4];
+        zeros += got[c][5];
       }
     }
+    exps = (unsigned long long)e1 << 32 | e0;
     if (f) return f & ROW_UNDEFINED ? ROW_UNDEFINED : ROW_OUTSIDE;
-    if (zeros) first = min(first, ZERO);
-    if (first == 0xffffffffu) return ROW_UNDEFINED;
-    top = (double)value(first);
+    if (!hi && !zeros && lo == WIN_BINS) return ROW_UNDEFINED;
+    top = hi ? (double)value(WIN_BINS - hi) : zeros ? 0.0 : (double)value(ZERO + 32 + lo);
     return 0u;
   }
-  // bin and value of an entry other than zero's group
-  __device__ static uint32_t bin_of(uint32_t e) { return e < ZERO ? 2 * (WIN_BINS - 1 - e) : 2 * (e - ZERO - 32) + 1; }
+  // value of an entry
   __device__ static float value(uint32_t e) {
     if (e < ZERO) return __uint_as_float((WIN_HI - 1 - e) << 16);
     return e < ZERO + 32 ? 0.f : __uint_as_float(0x80000000u | (WIN_LO + e - ZERO - 32) << 16);
   }
   __device__ double largest_value() const { return top; }
+  // tokens of a magnitude, positive and negative
+  __device__ uint2 both(uint32_t m) const {
+    if (CTAS == 1) return reinterpret_cast<const uint2*>(bins)[m];
+    uint2 c[CTAS], sum = make_uint2(0u, 0u);
+#pragma unroll
+    for (int i = 0; i < CTAS; ++i)
+      asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(c[i].x), "=r"(c[i].y) : "r"(mapa_u32(smem_u32(bins + 2 * m), i)));
+#pragma unroll
+    for (int i = 0; i < CTAS; ++i) {
+      sum.x += c[i].x;
+      sum.y += c[i].y;
+    }
+    return sum;
+  }
   __device__ uint32_t tokens(uint32_t e) const {
     if (e - ZERO < 32u) return e == ZERO ? zeros : 0u;
-    const uint32_t b = bin_of(e);
-    if (CTAS == 1) return bins[b];
-    uint32_t c[CTAS], sum = 0u;
-#pragma unroll
-    for (int i = 0; i < CTAS; ++i) c[i] = ld_cluster_u32(mapa_u32(smem_u32(bins + b), i));
-#pragma unroll
-    for (int i = 0; i < CTAS; ++i) sum += c[i];
-    return sum;
+    const uint2 c = both(e < ZERO ? WIN_BINS - 1 - e : e - ZERO - 32);
+    return e < ZERO ? c.x : c.y;
   }
   // of an entry that has tokens
   __device__ double weight(uint32_t e) const { return exp_falling(fmin((double)value(e) - top, 0.0) * inv_T, s.powers); }
 
-  // Four groups at a time, those of an exponent: 128 neighbours, lane + 32 k.  The k-th weight is the first times that of 32 steps to the k, but in
-  // the exponent of the largest logit, where there are values above it.
+  // An exponent at a time, its 4 groups of either sign: 128 neighbours, lane + 32 k from the largest magnitude down.  Weights 32 apart have a fixed
+  // ratio, so there is an exponential for it and one for either sign; but in the exponent of the largest logit, where there are values above it.
   __device__ void sum(const Settings& set) {
     inv_T = set.greedy ? 1.0 : 1.0 / set.T;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, mine = cta * SM_WARPS + (threadIdx.x >> 5);
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
     auto account = [&](uint32_t c, double w, double cw, uint32_t e) {
@@ -486,36 +530,38 @@ template <int CTAS> struct WindowSums : Sums<CTAS> {
         m += cw;
       }
     };
-    for (int x = cta * SM_WARPS + (threadIdx.x >> 5); x < 2 * EXPS + 1; x += CTAS * SM_WARPS) {
-      if (x == 2 * EXPS) {
-        const uint32_t c = lane ? 0u : zeros;
-        const double w = c ? weight(ZERO) : 0.0, cw = c * w;
-        account(c, w, cw, ZERO);
-        this->put_group(ZERO / 32, c, cw);
-        continue;
-      }
-      const uint32_t e = (x < EXPS ? 0u : 32u) + 128u * x + lane;
-      uint32_t c[4];
+    auto four = [&](const uint32_t* c, uint32_t e, double ratio) {
+      if (!__any_sync(0xffffffffu, c[0] | c[1] | c[2] | c[3])) return;
+      const bool with_top = (double)value(e & ~127u | (e < ZERO ? 0u : 32u)) > top;
+      double w = 0.0, cw[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) c[k] = tokens(e + 32 * k);
-      double cw[4];
-      if (!__any_sync(0xffffffffu, c[0] | c[1] | c[2] | c[3])) {
-        if (lane < 4) {
-          put<CTAS>(in_first_cta<CTAS>(&s.group_n[(e >> 5) + lane]), 0u);
-          put<CTAS>(in_first_cta<CTAS>(&s.group_w[(e >> 5) + lane]), 0.0);
-        }
-      } else {
-        double w = weight(e);
-        const bool with_top = (double)value(e - lane) > top;
-        const double ratio = exp_falling(((double)value(e - lane + 32) - (double)value(e - lane)) * inv_T, s.powers);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (k) w = with_top ? weight(e + 32 * k) : w * ratio;
-          cw[k] = c[k] ? c[k] * w : 0.0;
-          account(c[k], w, cw[k], e + 32 * k);
-        }
-        this->put_groups4((int)(e >> 5), c, cw);
+      for (int k = 0; k < 4; ++k) {
+        w = k == 0 || with_top ? weight(e + 32 * k) : w * ratio;
+        cw[k] = c[k] ? c[k] * w : 0.0;
+        account(c[k], w, cw[k], e + 32 * k);
       }
+      this->put_groups4((int)(e >> 5), c, cw);
+    };
+    int turn = 0;
+    for (unsigned long long left = exps; left; left &= left - 1, ++turn) {
+      if (turn % (CTAS * SM_WARPS) != mine) continue;
+      const uint32_t x = __ffsll((long long)left) - 1, big = 128 * x + 127 - lane;   // the lane's largest magnitude
+      uint32_t pos[4], neg[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint2 c = both(big - 32 * k);
+        pos[k] = c.x;
+        neg[3 - k] = c.y;
+      }
+      const double ratio = exp_falling(((double)value(WIN_BINS - 1 - big + 32) - (double)value(WIN_BINS - 1 - big)) * inv_T, s.powers);
+      four(pos, WIN_BINS - 1 - big, ratio);
+      four(neg, ZERO + 32 + big - 96, ratio);
+    }
+    if (turn % (CTAS * SM_WARPS) == mine && zeros) {
+      const uint32_t c = lane ? 0u : zeros;
+      const double w = weight(ZERO), cw = c * w;
+      account(c, w, cw, ZERO);
+      this->put_group(ZERO / 32, c, cw);
     }
     this->put_rest(set, nm, m, raw);
     row_sync<CTAS>();
@@ -883,12 +929,18 @@ __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int 
   uint32_t n = 0u;
   const Matcher<T> equal(x);
   int v = a + lane;
-  for (; v + 96 < b; v += 128) {
-    const uint4 u[4] = {words[v], words[v + 32], words[v + 64], words[v + 96]};
+  uint4 u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n += equal.number(u[i]);
+  for (int i = 0; i < 4; ++i)
+    if (v + 32 * i < b) u[i] = words[v + 32 * i];
+  for (; v < b; v += 128) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 now = u[i];
+      if (v + 32 * (i + 4) < b) u[i] = words[v + 32 * (i + 4)];
+      if (v + 32 * i < b) n += equal.number(now);
+    }
   }
-  for (; v < b; v += 32) n += equal.number(words[v]);
   const bool in_head = lane < heads && to_f(row.row[lane]) == x, in_tail = lane < tails && to_f(row.row[row.tail0 + lane]) == x;
   n = warp_sum(n + in_head + in_tail);
   if (lane == 0) s.matches[warp] = n;
