@@ -129,7 +129,7 @@ struct Shared {                     // beside the bins
   uint32_t group_n[MOST_GROUPS], warp_nm[MOST_CTAS * SM_WARPS];
   Found found[2];                   // by turns, so that none is overwritten while somebody reads it
   Totals totals;
-  uint32_t matches[SM_WARPS], cta_matches;
+  uint32_t matches[2][SM_WARPS], cta_matches;
   uint32_t top, lo, hi, flags, zeros, list_n, owner, exps[2];
 };
 
@@ -921,69 +921,81 @@ template <> struct Matcher<bf16> {
 template <typename T, int CTAS>
 __device__ void write_token(Shared& s, const Share<T>& row, const Found& f, int cta, int32_t* token) {
   constexpr int V = Share<T>::V;
+  // one CTA looks at a quarter of the row after the other until it has met the token: 5 / 8 of it on average (all of it at once: 51 us
+  // more for 1536 rows of 126464); a cluster's shares are short and looked at as a whole
+  constexpr int ROUNDS = CTAS == 1 ? 4 : 1;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float x = value_of(f.key);
-  const uint4* words = row.words();
-  const int a = row.v0 + (int)((long long)(row.v1 - row.v0) * warp / SM_WARPS), b = row.v0 + (int)((long long)(row.v1 - row.v0) * (warp + 1) / SM_WARPS);
-  const int heads = row.first && warp == 0 ? row.head : 0, tails = row.last && warp == SM_WARPS - 1 ? row.vocab - row.tail0 : 0;
-  uint32_t n = 0u;
   const Matcher<T> equal(x);
-  int v = a + lane;
-  uint4 u[4];
+  const uint4* words = row.words();
+  const long long all_words = row.v1 - row.v0;
+  uint32_t met = 0u;                                 // in the rounds so far
+  for (int round = 0; round < ROUNDS; ++round) {
+    const int part = round * SM_WARPS + warp;
+    const int a = row.v0 + (int)(all_words * part / (ROUNDS * SM_WARPS)), b = row.v0 + (int)(all_words * (part + 1) / (ROUNDS * SM_WARPS));
+    const int heads = row.first && part == 0 ? row.head : 0, tails = row.last && part == ROUNDS * SM_WARPS - 1 ? row.vocab - row.tail0 : 0;
+    uint32_t n = 0u;
+    int v = a + lane;
+    uint4 u[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (v + 32 * i < b) u[i] = words[v + 32 * i];
-  for (; v < b; v += 128) {
+    for (int i = 0; i < 4; ++i)
+      if (v + 32 * i < b) u[i] = words[v + 32 * i];
+    for (; v < b; v += 128) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 now = u[i];
-      if (v + 32 * (i + 4) < b) u[i] = words[v + 32 * (i + 4)];
-      if (v + 32 * i < b) n += equal.number(now);
+      for (int i = 0; i < 4; ++i) {
+        const uint4 now = u[i];
+        if (v + 32 * (i + 4) < b) u[i] = words[v + 32 * (i + 4)];
+        if (v + 32 * i < b) n += equal.number(now);
+      }
     }
-  }
-  const bool in_head = lane < heads && to_f(row.row[lane]) == x, in_tail = lane < tails && to_f(row.row[row.tail0 + lane]) == x;
-  n = warp_sum(n + in_head + in_tail);
-  if (lane == 0) s.matches[warp] = n;
-  __syncthreads();
-  uint32_t before = 0u, all = 0u;
-  for (int i = 0; i < SM_WARPS; ++i) {
-    if (i == warp) before = all;
-    all += s.matches[i];
-  }
-  if (CTAS > 1) {
-    if (threadIdx.x == 0) s.cta_matches = all;
-    cluster_sync_all();
-    for (int c = 0; c < cta; ++c) before += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_matches), c));
-  }
-  if (f.nth < before || f.nth >= before + n) return;
-  uint32_t left = f.nth - before;                    // of this warp's tokens of that value
-  const uint32_t head_at = __ballot_sync(0xffffffffu, in_head);
-  if (left < (uint32_t)__popc(head_at)) {
-    if (in_head && (uint32_t)__popc(head_at & ((1u << lane) - 1)) == left) *token = lane;
-    return;
-  }
-  left -= __popc(head_at);
-  for (int v0 = a; v0 < b; v0 += 32) {
-    v = v0 + lane;
-    uint32_t m = v < b ? equal.bits(words[v]) : 0u, sum = __popc(m);
-    const uint32_t mine = sum;
+    const bool in_head = lane < heads && to_f(row.row[lane]) == x, in_tail = lane < tails && to_f(row.row[row.tail0 + lane]) == x;
+    n = warp_sum(n + in_head + in_tail);
+    uint32_t* matches = s.matches[round & 1];
+    if (lane == 0) matches[warp] = n;
+    __syncthreads();
+    uint32_t before = 0u;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
+    for (int i = 0; i < SM_WARPS; ++i) {
+      if (i == warp) before = met;
+      met += matches[i];
     }
-    const uint32_t here = __shfl_sync(0xffffffffu, sum, 31);
-    if (left < here) {
+    if (CTAS > 1) {
+      if (threadIdx.x == 0) s.cta_matches = met;
+      cluster_sync_all();
+      for (int c = 0; c < cta; ++c) before += ld_cluster_u32(mapa_u32(smem_u32(&s.cta_matches), c));
+    } else if (f.nth >= met) continue;               // all warps go on to the next round
+    if (f.nth < before || f.nth >= before + n) return;
+    uint32_t left = f.nth - before;                  // of this warp's tokens of that value
+    const uint32_t head_at = __ballot_sync(0xffffffffu, in_head);
+    if (left < (uint32_t)__popc(head_at)) {
+      if (in_head && (uint32_t)__popc(head_at & ((1u << lane) - 1)) == left) *token = lane;
+      return;
+    }
+    left -= __popc(head_at);
+    for (int v0 = a; v0 < b; v0 += 32) {
+      v = v0 + lane;
+      uint32_t m = v < b ? equal.bits(words[v]) : 0u, sum = __popc(m);
+      const uint32_t here = warp_sum(sum);
+      if (left >= here) {
+        left -= here;
+        continue;
+      }
+      const uint32_t mine = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+      }
       if (sum > left && sum - mine <= left) {
         for (uint32_t skip = left - (sum - mine); skip > 0; --skip) m &= m - 1;
         *token = row.head + v * V + __ffs(m) - 1;
       }
       return;
     }
-    left -= here;
+    const uint32_t tail_at = __ballot_sync(0xffffffffu, in_tail);
+    if (in_tail && (uint32_t)__popc(tail_at & ((1u << lane) - 1)) == left) *token = row.tail0 + lane;
+    return;
   }
-  const uint32_t tail_at = __ballot_sync(0xffffffffu, in_tail);
-  if (in_tail && (uint32_t)__popc(tail_at & ((1u << lane) - 1)) == left) *token = row.tail0 + lane;
 }
 
 template <typename T, int CTAS> struct SampleSmem {
