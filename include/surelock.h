@@ -577,7 +577,7 @@ int surelock_rope_frequencies(int rotary_dim, double theta, const surelock_rope_
  * call in place; otherwise they do not overlap them).  The position of row r is positions[r], or positions[r] % N with N > 0 (flat
  * positions b*N + i).  A negative one leaves the row as it is (device status 4).  transposed: the rotation by -angle, with the same scale: the
  * gradient, and for scale 1 the inverse.  Angles are exact to 2^-53 of themselves at any position; products are fp32, rounded once.
- * Any head_dim, an even rotary_dim <= head_dim; 16-byte accesses where pointers, strides, head_dim and rotary_dim / 2 allow them, element by
+ * Any head_dim <= 4096 (heads of a row: 2^24 elements at most, SL_EUNSUPPORTED otherwise), an even rotary_dim <= head_dim; 16-byte accesses where pointers, strides, head_dim and rotary_dim / 2 allow them, element by
  * element otherwise.  dev_status may be NULL.  Asynchronous on `stream`. */
 int surelock_rope(const surelock_rope_cfg *cfg, const void *q, int64_t q_stride, int H, const void *k, int64_t k_stride, int n_kv_heads,
                   int head_dim, const int32_t *positions, int N, const int32_t *n_active, int max_rows, void *q_out,

@@ -1200,7 +1200,7 @@ int surelock_rope(const surelock_rope_cfg* cfg, const void* q, int64_t q_stride,
   const uintptr_t at = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) |
                        (k ? reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(k_out) : 0);
   if ((at & (dtype == SL_BF16 ? 1 : 3)) || (reinterpret_cast<uintptr_t>(cfg->freq) & 7)) return SL_EUNSUPPORTED;
-  if (head_dim > 4096 || H > 65536 || n_kv_heads > 65536) return SL_EUNSUPPORTED;
+  if (head_dim > 4096 || ((int64_t)H + (k ? n_kv_heads : 0)) * head_dim > (1 << 24)) return SL_EUNSUPPORTED;
   if (max_rows == 0) return SL_OK;
   return launch_rope_rows(*cfg, q, q_stride, H, k, k_stride, n_kv_heads, head_dim, positions, N, n_active, max_rows, q_out, q_out_stride,
                           k_out, k_out_stride, dtype, transposed, dev_status, (cudaStream_t)stream);

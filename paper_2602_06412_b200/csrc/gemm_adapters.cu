@@ -14,7 +14,7 @@
 namespace sl {
 namespace {
 
-constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS;
+constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS, AD_CLUSTER = 8, AD_CHAIN = 8;
 
 struct AdapterArgs {
   const bf16 *x, *a, *b;
@@ -124,6 +124,9 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
     const long long lines = ((long long)(min(fg1 * 32, a.n_out) - fg0 * 32) * a.max_rank * 2 + 127) >> 7;
     for (long long i = threadIdx.x; i < lines; i += AD_THREADS)
       asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(wb + (long long)fg0 * 32 * a.max_rank) + (i << 7)));
+    const int of_row = ((min(fg1 * 32, a.n_out) - fg0 * 32) * (int)sizeof(CT) + 127) >> 7;
+    for (int i = threadIdx.x; i < rows * of_row; i += AD_THREADS)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(reinterpret_cast<const CT*>(a.c) + (row0 + i / of_row) * a.c_stride + fg0 * 32) + ((i % of_row) << 7)));
   }
 
   // ---- t = A_a x over this warp's k
@@ -136,8 +139,28 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
     const int ra = wr * 16 + g, rb = ra + 8;
     const bf16 *xa = a.x + (long long)(row0 + ra) * a.K, *xb = a.x + (long long)(row0 + rb) * a.K;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    // A matrix instruction may cut off where an addition would round, so long chains are joined outside: the sums so far go to shared memory
+    float* to = part + (kw * ROWS + wr * 16 + g) * TP + 2 * t;
+    auto flush = [&](bool first) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float2* p = reinterpret_cast<float2*>(to + 8 * h * TP + 8 * j);
+          float2 v = make_float2(acc[j][2 * h], acc[j][2 * h + 1]);
+          if (!first) {
+            const float2 o = *p;
+            v.x += o.x;
+            v.y += o.y;
+          }
+          *p = v;
+        }
+        acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+      }
+    };
 #pragma unroll 2
     for (int ch = c0; ch < c1; ++ch) {
+      if (ch > c0 && (ch - c0) % AD_CHAIN == 0) flush(ch - c0 == AD_CHAIN);
       const int k = ch * 32 + t * 8;
       const bool in = k < a.K;
       const uint4 u = in && ra < rows ? *reinterpret_cast<const uint4*>(xa + k) : zero;
@@ -152,12 +175,7 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
         mma_16816(acc[j], u.z, v.z, u.w, v.w, w[j].z, w[j].w);
       }
     }
-    float* to = part + (kw * ROWS + wr * 16 + g) * TP + 2 * t;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      *reinterpret_cast<float2*>(to + 8 * j) = make_float2(acc[j][0], acc[j][1]);
-      *reinterpret_cast<float2*>(to + 8 * TP + 8 * j) = make_float2(acc[j][2], acc[j][3]);
-    }
+    flush(c1 - c0 <= AD_CHAIN);
   }
   __syncthreads();
   if (KS > 1) {
@@ -176,9 +194,13 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
     for (int i = threadIdx.x; i < ROWS * 16 * KSTEPS; i += AD_THREADS) {
       const int r = i / (16 * KSTEPS), j = i % (16 * KSTEPS);
       float v = 0.f;
-      if (j < rank) {
+      if (j < rank && r < rows) {
         const uint32_t at = base + 4 * (r * TP + j);
-        for (int c = 0; c < CL; ++c) v += ld_cluster(mapa_u32(at, c));
+        float w[AD_CLUSTER];
+#pragma unroll
+        for (int c = 0; c < AD_CLUSTER; ++c) w[c] = c < CL ? ld_cluster(mapa_u32(at, c)) : 0.f;
+#pragma unroll
+        for (int c = 0; c < AD_CLUSTER; ++c) v += w[c];
         v *= scale;
       }
       bf16_terms<TERMS>(v, terms + r * SP + j, ROWS * SP);
@@ -187,71 +209,94 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the others' t
   __syncthreads();
 
-  // ---- C += B_a t over this CTA's features, 32 at a time to a warp: lane t of a quad ends up with 8 neighbours
+  // ---- C += B_a t over this CTA's features, 32 at a time to a warp: lane t of a quad ends up with 8 neighbours.  The next 32 features'
+  // weights and C are on their way while these are multiplied.
   CT* c = reinterpret_cast<CT*>(a.c);
   const bool wide = (reinterpret_cast<uintptr_t>(c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;
   const int ra = wr * 16 + g, rb = ra + 8;
   const bf16* mine = terms + (wr * 16 + g) * SP + 4 * t;
-  for (int fg = fg0 + kw; fg < fg1; fg += KS) {
+  CT* const row_a = c + (row0 + ra) * a.c_stride + 8 * t;
+  CT* const row_b = c + (row0 + rb) * a.c_stride + 8 * t;
+  constexpr int WORDS = sizeof(CT) / 2;
+  struct alignas(16) Eight { CT e[8]; };
+  Eight old[2];
+  uint2 w[KSTEPS][4];
+  auto load_w = [&](int fg, int s) {
+    const int k = 16 * s + 4 * t;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int f = fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
+      w[s][j] = f < a.n_out && k < rank ? __ldg(reinterpret_cast<const uint2*>(wb + (long long)f * a.max_rank + k)) : make_uint2(0u, 0u);
+    }
+  };
+  auto load_c = [&](int fg, Eight* to) {
     const int f0 = fg * 32 + 8 * t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const CT* p = (h ? row_b : row_a) + fg * 32;
+      if ((h ? rb : ra) >= rows) continue;
+      if (wide && f0 + 8 <= a.n_out) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint4*>(&to[h])[i] = reinterpret_cast<const uint4*>(p)[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (f0 + i < a.n_out) to[h].e[i] = p[i];
+      }
+    }
+  };
+  int fg = fg0 + kw;
+  if (fg < fg1) {
+    load_c(fg, old);
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) load_w(fg, s);
+  }
+  for (; fg < fg1; fg += KS) {
+    const int next = fg + KS, f0 = fg * 32 + 8 * t;
+    Eight after[2];
+    if (next < fg1) load_c(next, after);
     float d[4][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
-    CT* p[2] = {c + (row0 + ra) * a.c_stride + f0, c + (row0 + rb) * a.c_stride + f0};
-    const bool whole = wide && f0 + 8 <= a.n_out;
-    __align__(16) CT old[2][8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if ((h ? rb : ra) < rows) {
-        if (whole) {
-#pragma unroll
-          for (int i = 0; i < (int)sizeof(CT) / 2; ++i)
-            reinterpret_cast<uint4*>(old[h])[i] = reinterpret_cast<const uint4*>(p[h])[i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (f0 + i < a.n_out) old[h][i] = p[h][i];
-        }
-      }
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
       if (16 * s >= rank) break;
       const int k = 16 * s + 4 * t;
-      uint2 w[4];
+      if (k + 4 > rank) {                            // what lies behind the adapter's own rank is not read into the sum
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int f = fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
-        w[j] = make_uint2(0u, 0u);
-        if (f < a.n_out && k < rank) w[j] = __ldg(reinterpret_cast<const uint2*>(wb + (long long)f * a.max_rank + k));
-        if (k + 4 > rank) {                          // what lies behind the adapter's own rank is not read into the sum
-          if (k + 3 >= rank) w[j].y &= 0xffffu;
-          if (k + 2 >= rank) w[j].y = 0u;
-          if (k + 1 >= rank) w[j].x &= 0xffffu;
+        for (int j = 0; j < 4; ++j) {
+          if (k + 3 >= rank) w[s][j].y &= 0xffffu;
+          if (k + 2 >= rank) w[s][j].y = 0u;
+          if (k + 1 >= rank) w[s][j].x &= 0xffffu;
         }
       }
 #pragma unroll
-      for (int m = 0; m < TERMS; ++m) {
+      for (int m = TERMS - 1; m >= 0; --m) {         // the small terms first
         const uint2 u = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 16 * s);
         const uint2 v = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 8 * SP + 16 * s);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, w[j].x, w[j].y);
+        for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, w[s][j].x, w[s][j].y);
       }
+      if (next < fg1) load_w(next, s);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       if ((h ? rb : ra) < rows) {
-        __align__(16) CT out[8];
+        CT* p = (h ? row_b : row_a) + fg * 32;
+        Eight out;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = from_f<CT>(to_f(old[h][i]) + d[i >> 1][2 * h + (i & 1)]);
-        if (whole) {
+        for (int i = 0; i < 8; ++i) out.e[i] = from_f<CT>(to_f(old[h].e[i]) + d[i >> 1][2 * h + (i & 1)]);
+        if (wide && f0 + 8 <= a.n_out) {
 #pragma unroll
-          for (int i = 0; i < (int)sizeof(CT) / 2; ++i) reinterpret_cast<uint4*>(p[h])[i] = reinterpret_cast<const uint4*>(out)[i];
+          for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(&out)[i];
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (f0 + i < a.n_out) p[h][i] = out[i];
+            if (f0 + i < a.n_out) p[i] = out.e[i];
         }
       }
+    old[0] = after[0];
+    old[1] = after[1];
   }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody reads this CTA's t any more
 }
@@ -293,7 +338,7 @@ template <typename CT> int launch_rows(const AdapterArgs& a, cudaStream_t st) {
   // every sequence may end in a tile that is not full
   const long long groups = a.max_rows / tile + (a.max_rows < a.B ? a.max_rows : a.B);
   if (groups > (1 << 27)) return SL_EUNSUPPORTED;
-  int CL = 8;
+  int CL = AD_CLUSTER;
   while (CL > 1 && groups * CL > 4ll * sm_count()) CL >>= 1;
   return many ? launch_rank<4, CT>(a, (int)groups, CL, st) : launch_rank<1, CT>(a, (int)groups, CL, st);
 }

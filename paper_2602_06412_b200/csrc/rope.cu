@@ -5,16 +5,18 @@
 //
 // Far positions: position * freq is taken in 64 bits and reduced there to an eighth of a turn either side of a quarter turn (2 pi
 // in two terms), sine and cosine of what is left in 32 bits, so that the angle's error is 2^-53 of it and not 2^-24.  Sines are shared by
-// all heads of a row: a block computes those of its rows once, in shared memory, while its first loads are on their way.
+// all heads of a row: a block computes those of its rows once, in shared memory, while its first loads are on their way, and a thread
+// keeps those of its V pairs in registers while it goes through the heads.
 //
-// Memory-bound: a thread moves V pairs (16 bytes of either half of the pairs) at a time, U of them in flight before the sines
-// are waited for.  In a graph: ROPE_FIGURES
+// Memory-bound: 16-byte accesses of either half of V pairs, 4 heads in flight to a thread.  In a graph, 64 heads of 128 in bf16: 12288 rows
+// 63.5 us (6.3 TB/s, 97 % of the copy rate; sines read from shared memory for every head instead: 120 us, two thirds of it bank conflicts and
+// registers), 4 rows to a block (2: 69, 8: 66 us), 4 heads in flight (2: 66, 8: 65.5); 32 rows at positions up to 10^6 4.2 us.
 #include "common.cuh"
 
 namespace sl {
 namespace {
 
-constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_THREADS = 256, ROPE_ROWS = 4, ROPE_U = 4, ROPE_BLOCKS = 3;
 
 struct RopeArgs {
   const void* in[2];
@@ -26,11 +28,8 @@ struct RopeArgs {
   int32_t* status;
   float scale, scale_sin;          // the sine's is negative for the transposed rotation
   int max_rows, N, half, dh;       // half = pairs to a head
-  int pair_items, items;           // per head: groups of V pairs, and with the groups of V elements that are copied
-  int row_items;                   // per row: items * (heads[0] + heads[1])
-  int rows;                        // rows to a block
-  int parts;                       // blocks that share these rows
-  uint32_t div_items, div_row;     // ceil(2^32 / items), ceil(2^32 / row_items): see fast_div
+  int chunks, rest;                // groups of V pairs to a head, and of V elements to be copied
+  int rows, slots, parts;          // a block: rows, and heads of each at once; blocks that share these rows
 };
 
 // cosine and sine of pos * freq
@@ -47,7 +46,7 @@ __device__ __forceinline__ float2 turn(int pos, double freq) {
 }
 
 // V consecutive elements, as stored
-template <typename T, int V> struct Vec { T e[V]; };
+template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T e[V]; };
 template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T* p) {
   Vec<T, V> v;
   if (sizeof(T) * V == 16) *reinterpret_cast<uint4*>(&v) = *reinterpret_cast<const uint4*>(p);
@@ -63,34 +62,34 @@ template <typename T, int V> __device__ __forceinline__ void store(T* p, const V
     for (int i = 0; i < V; ++i) p[i] = v.e[i];
 }
 
+// A thread keeps the sines of V pairs and goes through heads with them, U at a time.
 template <typename T, int V, bool INTERLEAVED, int U>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeArgs a) {
+__global__ void __launch_bounds__(ROPE_THREADS, ROPE_BLOCKS) rope_rows_kernel(RopeArgs a) {
   extern __shared__ float2 turns[];                  // [rows][half]
   griddep_wait();
   griddep_launch();
   const int M = min(*a.n_active, a.max_rows), group = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const int r0 = group * a.rows, nr = min(a.rows, M - r0);
+  const int r0 = group * a.rows, nr = min(a.rows, M - r0), all = a.heads[0] + a.heads[1];
   if (nr <= 0) return;
-  const int total = nr * a.row_items, step = a.parts * ROPE_THREADS;
-  struct Item { T* to; int turn; bool rotate; };
   const int second = INTERLEAVED ? V : a.half;       // how far behind a thread's first V elements its other V are
+  const int wide = min(a.chunks, ROPE_THREADS), slot = threadIdx.x / wide, row = slot % a.rows, step = a.slots * a.parts;
+  const int h0 = slot / a.rows + part * a.slots;
+  const bool works = slot < a.rows * a.slots && row < nr && a.positions[r0 + min(row, nr - 1)] >= 0;
+  const T *from_q = (const T*)a.in[0] + (r0 + row) * a.in_stride[0], *from_k = (const T*)a.in[1] + (r0 + row) * a.in_stride[1] - (long long)a.heads[0] * a.dh;
+  T *to_q = (T*)a.out[0] + (r0 + row) * a.out_stride[0], *to_k = (T*)a.out[1] + (r0 + row) * a.out_stride[1] - (long long)a.heads[0] * a.dh;
   Vec<T, V> x[U], y[U];
-  Item it[U];
-  auto fetch = [&](int i, int u) {
-    const int r = fast_div(i, a.row_items, a.div_row), w = i - r * a.row_items, head = fast_div(w, a.items, a.div_items), c = w - head * a.items;
-    const int which = head >= a.heads[0], h = which ? head - a.heads[0] : head;
-    it[u].rotate = c < a.pair_items;
-    const int first = it[u].rotate ? (INTERLEAVED ? 2 * V * c : V * c) : 2 * a.half + V * (c - a.pair_items);
-    it[u].turn = r * a.half + V * c;
-    const T* from = (const T*)a.in[which] + (r0 + r) * a.in_stride[which] + h * a.dh + first;
-    it[u].to = a.positions[r0 + r] < 0 ? nullptr : (T*)a.out[which] + (r0 + r) * a.out_stride[which] + h * a.dh + first;
-    x[u] = load<T, V>(from);
-    if (it[u].rotate) y[u] = load<T, V>(from + second);
-  };
-  int i = part * ROPE_THREADS + threadIdx.x;
+  auto at = [&](int h, int c) { return h * a.dh + (INTERLEAVED ? 2 : 1) * V * c; };   // k's heads come after q's
+  auto fetch = [&](int h, int c) {
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (i + u * step < total) fetch(i + u * step, u);
+    for (int u = 0; u < U; ++u)
+      if (h + u * step < all) {
+        const T* p = (h + u * step < a.heads[0] ? from_q : from_k) + at(h + u * step, c);
+        x[u] = load<T, V>(p);
+        y[u] = load<T, V>(p + second);
+      }
+  };
+  int c = threadIdx.x % wide;
+  if (works) fetch(h0, c);
   for (int j = threadIdx.x; j < nr * a.half; j += ROPE_THREADS) {
     const int r = j / a.half;
     int pos = a.positions[r0 + r];
@@ -103,53 +102,56 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeArgs a) {
     turns[j] = make_float2(t.x * a.scale, t.y * a.scale_sin);
   }
   __syncthreads();
-  while (i < total) {
+  for (; works && c < a.chunks; c += wide) {
+    float2 t[V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u * step >= total) break;
-      if (!it[u].to) continue;
-      if (it[u].rotate) {
+    for (int k = 0; k < V; ++k) t[k] = turns[row * a.half + V * c + k];
+    if (c >= wide) fetch(h0, c);
+    for (int h = h0; h < all; h += U * step) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (h + u * step >= all) break;
+        T* p = (h + u * step < a.heads[0] ? to_q : to_k) + at(h + u * step, c);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float2 t = turns[it[u].turn + k];
-          T& p = INTERLEAVED ? (2 * k < V ? x[u].e[(2 * k) % V] : y[u].e[(2 * k) % V]) : x[u].e[k];
-          T& q = INTERLEAVED ? (2 * k + 1 < V ? x[u].e[(2 * k + 1) % V] : y[u].e[(2 * k + 1) % V]) : y[u].e[k];
-          const float e = to_f(p), f = to_f(q);
-          p = from_f<T>(e * t.x - f * t.y);
-          q = from_f<T>(f * t.x + e * t.y);
+          T& e = INTERLEAVED ? (2 * k < V ? x[u].e[(2 * k) % V] : y[u].e[(2 * k) % V]) : x[u].e[k];
+          T& f = INTERLEAVED ? (2 * k + 1 < V ? x[u].e[(2 * k + 1) % V] : y[u].e[(2 * k + 1) % V]) : y[u].e[k];
+          const float g = to_f(e), i = to_f(f);
+          e = from_f<T>(g * t[k].x - i * t[k].y);
+          f = from_f<T>(i * t[k].x + g * t[k].y);
         }
-        store<T, V>(it[u].to + second, y[u]);
+        store<T, V>(p, x[u]);
+        store<T, V>(p + second, y[u]);
       }
-      store<T, V>(it[u].to, x[u]);
+      fetch(h + U * step, c);
     }
-    i += U * step;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * step < total) fetch(i + u * step, u);
+  }
+  // what is not rotated, in a call that is not in place
+  for (int i = part * ROPE_THREADS + threadIdx.x; i < nr * all * a.rest; i += a.parts * ROPE_THREADS) {
+    const int w = i / a.rest, r = w / all, h = w - r * all, which = h >= a.heads[0];
+    if (a.positions[r0 + r] < 0) continue;
+    const long long e = (long long)(which ? h - a.heads[0] : h) * a.dh + 2 * a.half + V * (i - w * a.rest);
+    store<T, V>((T*)a.out[which] + (r0 + r) * a.out_stride[which] + e, load<T, V>((const T*)a.in[which] + (r0 + r) * a.in_stride[which] + e));
   }
 }
 
 template <typename T, int V, bool INTERLEAVED>
 int launch_rows(RopeArgs& a, bool copy, cudaStream_t st) {
-  a.pair_items = a.half / V;
-  a.items = a.pair_items + (copy ? (a.dh - 2 * a.half) / V : 0);
-  const long long row_items = (long long)a.items * (a.heads[0] + a.heads[1]);
-  if (row_items > (1 << 24)) return SL_EUNSUPPORTED;
-  a.row_items = (int)row_items;
-  a.div_items = fast_div_by(a.items);
-  a.div_row = fast_div_by(a.row_items);
-  // Few rows: a block for each 256 items of a row, so that every load of the call is on its way at once.  Many: as many rows to
-  // a block as give each thread one sine, and four items in flight.
-  const bool few = a.max_rows * row_items <= (long long)sm_count() * 8 * ROPE_THREADS;
-  a.rows = few || a.half >= ROPE_THREADS ? 1 : ROPE_THREADS / a.half;
-  const int per = ROPE_THREADS * (few ? 1 : 4);
-  a.parts = few ? (a.row_items + per - 1) / per : 1;
+  a.chunks = a.half / V;
+  a.rest = copy ? (a.dh - 2 * a.half) / V : 0;
+  const int wide = a.chunks < ROPE_THREADS ? a.chunks : ROPE_THREADS, all = a.heads[0] + a.heads[1], slots = ROPE_THREADS / wide;
+  // Few rows: blocks of one row that share its heads, one head to a thread, so that every load of the call is on its way at once.
+  // Many: as many rows to a block as leave each thread some heads.
+  const bool few = (long long)a.max_rows * all * wide <= (long long)sm_count() * 8 * ROPE_THREADS;
+  a.rows = few ? 1 : ROPE_ROWS < slots ? ROPE_ROWS : slots;
+  a.slots = slots / a.rows;
+  a.parts = few ? (all + a.slots - 1) / a.slots : 1;
   const long long groups = ((long long)a.max_rows + a.rows - 1) / a.rows;
   if (groups * a.parts > 0x7fffffffll) return SL_EUNSUPPORTED;
   const dim3 grid((unsigned)(groups * a.parts));
   const size_t smem = (size_t)a.rows * a.half * sizeof(float2);
   if (few) SL_CUDA_TRY(launch_pdl(rope_rows_kernel<T, V, INTERLEAVED, 1>, grid, dim3(ROPE_THREADS), smem, st, a));
-  else SL_CUDA_TRY(launch_pdl(rope_rows_kernel<T, V, INTERLEAVED, 4>, grid, dim3(ROPE_THREADS), smem, st, a));
+  else SL_CUDA_TRY(launch_pdl(rope_rows_kernel<T, V, INTERLEAVED, ROPE_U>, grid, dim3(ROPE_THREADS), smem, st, a));
   return SL_OK;
 }
 
