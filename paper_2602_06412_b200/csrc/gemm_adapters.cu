@@ -9,22 +9,12 @@
 //
 // x and the weights are bf16, so the first product's terms are exact and summed in fp32.  t scale stays an fp32 number: it enters
 // the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
-#include "tc_common.cuh"
+#include "gemm_adapters.cuh"
 
 namespace sl {
 namespace {
 
-constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS, AD_CLUSTER = 8, AD_CHAIN = 8;
-
-struct AdapterArgs {
-  const bf16 *x, *a, *b;
-  const float* scale;
-  const int32_t *ranks, *adapter_of_seq, *row_offsets;
-  void* c;
-  int32_t* status;
-  long long c_stride;
-  int n_adapters, max_rank, B, max_rows, n_out, K;
-};
+constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS, AD_CLUSTER = 8, AD_CHAIN = 8, AD_MANY = 32;
 
 __device__ __forceinline__ void mma_16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -34,41 +24,6 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
   return v;
-}
-
-// The group-th tile of `tile` rows of one sequence: its sequence, first row and rows; every lane of a warp gets the same.
-__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& seq, int& row0, int& rows) {
-  const int lane = threadIdx.x & 31;
-  int before = 0;                                    // tiles of the sequences before this round's 32
-  bool bad = false;
-  for (int b0 = 0; b0 < a.B; b0 += 32) {
-    const int b = b0 + lane;
-    // offsets are clamped, so that no row is outside C
-    int from = b < a.B ? a.row_offsets[b] : 0, to = b < a.B ? a.row_offsets[b + 1] : 0;
-    if (b < a.B) bad |= from < 0 || to < from || to > a.max_rows;
-    from = min(max(from, 0), a.max_rows);
-    to = min(max(to, from), a.max_rows);
-    const int mine = (int)(((long long)to - from + tile - 1) / tile);
-    int sum = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, group - before < sum);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      const int first = group - before - __shfl_sync(0xffffffffu, sum - mine, l);
-      seq = b0 + l;
-      row0 = __shfl_sync(0xffffffffu, from, l) + first * tile;
-      rows = min(tile, __shfl_sync(0xffffffffu, to, l) - row0);
-      if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
-      return true;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-  if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
-  return false;
 }
 
 // the k-th term of v as a sum of bf16 numbers
@@ -105,18 +60,8 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   const int wr = warp % WR, kw = warp / WR;
   int seq, row0, rows;
   if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, seq, row0, rows)) return;
-  const int ad = a.adapter_of_seq[seq];
-  if (ad < 0 || ad >= a.n_adapters) {
-    if (ad >= a.n_adapters) set_status(a.status, SL_DEV_BAD_INDEX);
-    return;
-  }
-  int rank = a.max_rank;
-  if (a.ranks) {
-    const int given = a.ranks[ad];
-    if (given < 0 || given > a.max_rank) set_status(a.status, SL_DEV_BAD_INDEX);
-    rank = min(max(given, 0), a.max_rank);
-  }
-  if (rank == 0) return;
+  int ad, rank;
+  if (!find_adapter(a, seq, ad, rank)) return;
   const bf16* wa = a.a + (long long)ad * a.max_rank * a.K;
   const bf16* wb = a.b + (long long)ad * a.n_out * a.max_rank;
   const int fgs = (a.n_out + 31) >> 5, fg0 = (int)((long long)fgs * rank_cta / CL), fg1 = (int)((long long)fgs * (rank_cta + 1) / CL);
@@ -323,24 +268,17 @@ int launch_tile(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
   return SL_OK;
 }
 
-template <int WR, typename CT>
-int launch_rank(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
-  if (a.max_rank <= 16) return launch_tile<WR, 2, CT>(a, groups, CL, st);
-  if (a.max_rank <= 32) return launch_tile<WR, 4, CT>(a, groups, CL, st);
-  if (a.max_rank <= 64) return launch_tile<WR, 8, CT>(a, groups, CL, st);
-  return launch_tile<WR, 16, CT>(a, groups, CL, st);
-}
-
-template <typename CT> int launch_rows(const AdapterArgs& a, cudaStream_t st) {
-  // tiles of 64 rows where sequences are that long on average
-  const bool many = a.max_rows >= 32 * (long long)a.B;
-  const int tile = many ? 64 : 16;
+template <typename CT>
+int launch_few(const AdapterArgs& a, cudaStream_t st) {
   // every sequence may end in a tile that is not full
-  const long long groups = a.max_rows / tile + (a.max_rows < a.B ? a.max_rows : a.B);
+  const long long groups = a.max_rows / 16 + (a.max_rows < a.B ? a.max_rows : a.B);
   if (groups > (1 << 27)) return SL_EUNSUPPORTED;
   int CL = AD_CLUSTER;
   while (CL > 1 && groups * CL > 4ll * sm_count()) CL >>= 1;
-  return many ? launch_rank<4, CT>(a, (int)groups, CL, st) : launch_rank<1, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 16) return launch_tile<1, 2, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 32) return launch_tile<1, 4, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 64) return launch_tile<1, 8, CT>(a, (int)groups, CL, st);
+  return launch_tile<1, 16, CT>(a, (int)groups, CL, st);
 }
 
 }  // namespace
@@ -349,7 +287,8 @@ int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_
                          void* C, long long c_stride, int max_rows, int n_out, int K, int dtype, int32_t* status, cudaStream_t st) {
   const AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
                          c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K};
-  return dtype == SL_BF16 ? launch_rows<bf16>(a, st) : launch_rows<float>(a, st);
+  if (a.max_rows >= AD_MANY * (long long)B) return launch_gemm_adapters_tc(a, dtype, st);
+  return dtype == SL_BF16 ? launch_few<bf16>(a, st) : launch_few<float>(a, st);
 }
 
 }  // namespace sl

@@ -1,0 +1,71 @@
+// Low-rank adapters of many requests: what the two kernels share (the few rows' in gemm_adapters.cu, the many rows' in
+// gemm_adapters_tc.cu).
+#pragma once
+#include "tc_common.cuh"
+
+namespace sl {
+
+struct AdapterArgs {
+  const bf16 *x, *a, *b;
+  const float* scale;
+  const int32_t *ranks, *adapter_of_seq, *row_offsets;
+  void* c;
+  int32_t* status;
+  long long c_stride;
+  int n_adapters, max_rank, B, max_rows, n_out, K;
+};
+
+// The group-th tile of `tile` rows of one sequence: its sequence, first row and rows; every lane of a warp gets the same.
+__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& seq, int& row0, int& rows) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;                                    // tiles of the sequences before this round's 32
+  bool bad = false;
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int b = b0 + lane;
+    // offsets are clamped, so that no row is outside C
+    int from = b < a.B ? a.row_offsets[b] : 0, to = b < a.B ? a.row_offsets[b + 1] : 0;
+    if (b < a.B) bad |= from < 0 || to < from || to > a.max_rows;
+    from = min(max(from, 0), a.max_rows);
+    to = min(max(to, from), a.max_rows);
+    const int mine = (int)(((long long)to - from + tile - 1) / tile);
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, group - before < sum);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      const int first = group - before - __shfl_sync(0xffffffffu, sum - mine, l);
+      seq = b0 + l;
+      row0 = __shfl_sync(0xffffffffu, from, l) + first * tile;
+      rows = min(tile, __shfl_sync(0xffffffffu, to, l) - row0);
+      if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
+  return false;
+}
+
+// The adapter of a tile's sequence and its rank; false where there is nothing to add.
+__device__ __forceinline__ bool find_adapter(const AdapterArgs& a, int seq, int& ad, int& rank) {
+  ad = a.adapter_of_seq[seq];
+  if (ad < 0 || ad >= a.n_adapters) {
+    if (ad >= a.n_adapters) set_status(a.status, SL_DEV_BAD_INDEX);
+    return false;
+  }
+  rank = a.max_rank;
+  if (a.ranks) {
+    const int given = a.ranks[ad];
+    if (given < 0 || given > a.max_rank) set_status(a.status, SL_DEV_BAD_INDEX);
+    rank = min(max(given, 0), a.max_rank);
+  }
+  return rank > 0;
+}
+
+int launch_gemm_adapters_tc(const AdapterArgs& a, int dtype, cudaStream_t st);
+
+}  // namespace sl
