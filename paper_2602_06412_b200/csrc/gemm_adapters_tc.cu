@@ -20,7 +20,7 @@ template <typename CT, int NH> struct AtPlan {
   static constexpr int SLOT = AT_X + NH * AT_W;
   static constexpr int PITCH = 68;                                        // floats of a staged row: 16-byte accesses of 8 rows miss one another's banks
   static constexpr int STAGE = 128 * PITCH * 4;
-  static constexpr int BARS = 2 * AT_STAGES + 6 + 8;
+  static constexpr int BARS = 3 * AT_STAGES + 6;
   static constexpr int SMEM = 1024 + AT_STAGES * SLOT + STAGE + BARS * 8 + 16;
   // tensor memory: terms of t (16 bits a number), then two accumulators of 64 features, in whose place t itself is accumulated
   static constexpr uint32_t T_COLS = 32 * NH, D_COL = TERMS * T_COLS, COLS = D_COL + 128 <= 256 ? 256 : 512;
@@ -50,19 +50,10 @@ __device__ __forceinline__ void st_cluster_f4(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
-// some 16-byte words of a row to shared memory, counted on a barrier, and back
-__device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
-               : "memory");
-}
-__device__ __forceinline__ void bulk_store(void* to, uint32_t from, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
-}
-
 template <typename CT, int NH>
 __global__ void __launch_bounds__(AT_THREADS, AtPlan<CT, NH>::CTAS)
 gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                        const __grid_constant__ AdapterArgs a) {
+                        const __grid_constant__ CUtensorMap tmC, const __grid_constant__ AdapterArgs a) {
   using P = AtPlan<CT, NH>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -74,6 +65,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   const uint32_t t_done = bar0 + 8u * (2 * AT_STAGES), t_ready = t_done + 8u;
   auto d_full = [&](int j) { return t_ready + 8u + 8u * (j & 1); };
   auto d_empty = [&](int j) { return t_ready + 24u + 8u * (j & 1); };
+  auto c_empty = [&](int j) { return t_ready + 40u + 8u * (j % AT_STAGES); };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + P::BARS);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
@@ -86,6 +78,9 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   int seq, row0, rows, ad, rank;                     // the same in the whole cluster
   if (!find_tile(a, (int)(blockIdx.x / CL), 128, seq, row0, rows) || !find_adapter(a, seq, ad, rank)) return;
   const int ranks = (a.max_rank + 15) & ~15;         // rows of A_a in a copy: a whole number of 16
+  const bool wide = (reinterpret_cast<uintptr_t>(a.c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;   // C may be copied in tiles
+  constexpr int VEC = 16 / sizeof(CT);
+  struct alignas(16) Vec { CT e[VEC]; };
   const int blocks = (a.K + 63) >> 6, b0 = (int)((long long)blocks * cta / CL), n1 = (int)((long long)blocks * (cta + 1) / CL) - b0;
   const int tiles = (a.n_out + 63) >> 6, f0 = (int)((long long)tiles * cta / CL), n2 = (int)((long long)tiles * (cta + 1) / CL) - f0;
 
@@ -100,7 +95,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
       mbar_init(d_full(j), 1);
       mbar_init(d_empty(j), 4);
     }
-    for (int k = 0; k < 8; ++k) mbar_init(d_empty(1) + 8u + 8u * k, 1);
+    for (int i = 0; i < AT_STAGES; ++i) mbar_init(c_empty(i), 1);
     *s_abort = 0;
     fence_mbar_init();
   }
@@ -112,37 +107,31 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   bool ok = true;
 
   if (warp == AT_COPY) {
-    int i = 0;                                       // copies that were started
-    if (lane == 0) {
-      auto load = [&](int n) {                       // the n-th: first the blocks of k, then the tiles of features
-        for (; i < n; ++i) {
-          if (!(ok = mbar_wait(empty(i), ((i / AT_STAGES) & 1) ^ 1, s_abort))) break;
-          const uint32_t at = ring + i % AT_STAGES * P::SLOT;
-          if (i < n1) {
-            mbar_expect_tx(full(i), AT_X + ranks * 128);
-            tma_load_2d(at, &tmX, (b0 + i) * 64, row0, full(i));
-            tma_load_2d(at + AT_X, &tmA, (b0 + i) * 64, ad * a.max_rank, full(i));
-          } else {
-            const int halves = rank > 64 ? 2 : 1, f = (f0 + i - n1) * 64;
-            mbar_expect_tx(full(i), halves * AT_W);
-            for (int h = 0; h < halves; ++h) tma_load_2d(at + h * AT_W, &tmB, 64 * h, (int)((long long)ad * a.n_out + f), full(i));
-          }
+    int i = 0;                                       // copies that were started: first the blocks of k, then the tiles of features
+    auto load = [&](int n) {
+      for (; i < n; ++i) {
+        if (!(ok = mbar_wait(empty(i), ((i / AT_STAGES) & 1) ^ 1, s_abort))) break;
+        const uint32_t at = ring + i % AT_STAGES * P::SLOT;
+        if (i < n1) {
+          mbar_expect_tx(full(i), AT_X + ranks * 128);
+          tma_load_2d(at, &tmX, (b0 + i) * 64, row0, full(i));
+          tma_load_2d(at + AT_X, &tmA, (b0 + i) * 64, ad * a.max_rank, full(i));
+        } else {
+          const int halves = rank > 64 ? 2 : 1, f = (f0 + i - n1) * 64;
+          const bool with_c = sizeof(CT) == 2 && wide && rows == 128;
+          if (with_c && i - n1 >= AT_STAGES && !(ok = mbar_wait(c_empty(i - n1 - AT_STAGES), ((i - n1) / AT_STAGES - 1) & 1, s_abort))) break;
+          mbar_expect_tx(full(i), halves * AT_W + (with_c ? AT_X : 0));
+          for (int h = 0; h < halves; ++h) tma_load_2d(at + h * AT_W, &tmB, 64 * h, (int)((long long)ad * a.n_out + f), full(i));
+          if (with_c) tma_load_2d(at + NH * AT_W, &tmC, f, row0, full(i));
         }
-      };
-      load(n1 + min(n2, AT_STAGES));
-    }
+      }
+    };
+    if (lane == 0) load(n1 + min(n2, AT_STAGES));
     __syncwarp();
     if (CL > 1)
       for (int h = 0; h < 3 * NH; ++h) cluster_sync_all();
     if (lane == 0) {
-      for (; ok && i < n1 + n2;) {
-        if (!(ok = mbar_wait(empty(i), ((i / AT_STAGES) & 1) ^ 1, s_abort))) break;
-        const uint32_t at = ring + i % AT_STAGES * P::SLOT;
-        const int halves = rank > 64 ? 2 : 1, f = (f0 + i - n1) * 64;
-        mbar_expect_tx(full(i), halves * AT_W);
-        for (int h = 0; h < halves; ++h) tma_load_2d(at + h * AT_W, &tmB, 64 * h, (int)((long long)ad * a.n_out + f), full(i));
-        ++i;
-      }
+      if (ok) load(n1 + n2);
       // the copies in flight have landed (a bounded wait) before this thread goes on, whichever warp's wait may have run out
       const unsigned long long t0 = clock64();
       for (int k = max(0, i - AT_STAGES); k < i; ++k)
@@ -292,107 +281,118 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
     __syncwarp();
     if (lane == 0) mbar_arrive(t_ready);
 
-    CT* c = reinterpret_cast<CT*>(a.c);
-    const bool wide = (reinterpret_cast<uintptr_t>(c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;
-    if constexpr (sizeof(CT) == 4) {
-      // fp32: a thread stages its row, 32 features at a time, and the L2 adds them to C as one bulk reduction: C is not read by the SM
-      const bool bulk = wide && a.n_out % 4 == 0;
-      float* out = c + (long long)(row0 + row) * a.c_stride;
-      for (int j = 0; j < n2 && ok; ++j) {
-        const int f = (f0 + j) * 64;
-        ok = __all_sync(0xffffffffu, mbar_wait(d_full(j), (j >> 1) & 1, s_abort));
-        if (!ok) break;
-        tc_fence_after();
+    const bool whole = wide && rows == 128, issues = threadIdx.x == 0, bulk = sizeof(CT) == 4 && wide && a.n_out % 4 == 0;
+    auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    int j = 0;
+    for (; j < n2 && ok; ++j) {
+      const int f = (f0 + j) * 64, slot = (n1 + j) % AT_STAGES;
+      ok = mbar_wait(d_full(j), (j >> 1) & 1, s_abort);
+      if (sizeof(CT) == 2 && whole) ok = ok && mbar_wait(full(n1 + j), ((n1 + j) / AT_STAGES) & 1, s_abort);   // C's tile is here too
+      ok = epilogue_warps_agree(ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t v[64];
+      tc_ld32(mine + P::D_COL + (j & 1) * 64, v);
+      tc_ld32(mine + P::D_COL + (j & 1) * 64 + 32, v + 32);
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(d_empty(j));
+      if (!whole) {
+        // the last rows of a sequence, or a C that is not aligned: by ordinary accesses, a row's numbers side by side in the lanes
+        if (bulk) bulk_wait_read0();
+#pragma unroll
+        for (int k = 0; k < 64; k += 4) *reinterpret_cast<uint4*>(own + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        if constexpr (sizeof(CT) == 4)
+          if (bulk) {                                // each row by a reduction of its own
+            fence_async_smem();
+            if (row < rows) bulk_reduce_add_f32(reinterpret_cast<float*>(a.c) + (long long)(row0 + row) * a.c_stride + f, smem_u32(own), 4 * min(64, a.n_out - f));
+            bulk_commit();
+            continue;
+          }
+        __syncwarp();
+        constexpr int PER_ROW = 64 / VEC, LR = 32 / PER_ROW, STEPS = 32 / LR;
+        const int lr = lane / PER_ROW, col = lane % PER_ROW * VEC, last = rows - warp * 32;
+        const float* from = stage + (warp * 32 + lr) * P::PITCH + col;
+        CT* to = reinterpret_cast<CT*>(a.c) + (long long)(row0 + warp * 32 + lr) * a.c_stride + f + col;
+        if (wide && f + 64 <= a.n_out) {
+          Vec o[STEPS];
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+            if (s * LR + lr < last) o[s] = *reinterpret_cast<const Vec*>(to + (long long)s * LR * a.c_stride);
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+            if (s * LR + lr < last) {
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) o[s].e[e] = from_f<CT>(to_f(o[s].e[e]) + from[s * LR * P::PITCH + e]);
+              *reinterpret_cast<Vec*>(to + (long long)s * LR * a.c_stride) = o[s];
+            }
+        } else {
+          CT* c = reinterpret_cast<CT*>(a.c) + (long long)(row0 + warp * 32) * a.c_stride + f + lane;
+          const bool in[2] = {f + lane < a.n_out, f + lane + 32 < a.n_out};
+          for (int r0 = 0; r0 < min(last, 32); r0 += 4) {
+            CT o[4][2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (in[h] && r0 + r < last) o[r][h] = c[(r0 + r) * a.c_stride + 32 * h];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (in[h] && r0 + r < last) c[(r0 + r) * a.c_stride + 32 * h] = from_f<CT>(to_f(o[r][h]) + stage[(warp * 32 + r0 + r) * P::PITCH + lane + 32 * h]);
+          }
+        }
+        __syncwarp();                                // the staged rows are written again
+        continue;
+      }
+      if constexpr (sizeof(CT) == 4) {
+        // fp32: 32 features at a time are staged and added to C by the L2, which the SM does not read
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t v[32];
-          tc_ld32(mine + P::D_COL + (j & 1) * 64 + 32 * h, v);
-          tc_wait_ld();
-          if (h == 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(d_empty(j));
-          }
-          const int n = min(32, a.n_out - f - 32 * h);
-          if (row >= rows || n <= 0) continue;
-          if (bulk) {
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // this half's last reduction has read its numbers
+          if (issues) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // this half's last reduction has read its numbers
+          together();
+          uint8_t* to = reinterpret_cast<uint8_t*>(stage) + h * AT_X + row * 128;
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4*>(own + 32 * h + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-            fence_async_smem();
-            bulk_reduce_add_f32(out + f + 32 * h, smem_u32(own + 32 * h), 4 * n);
-            bulk_commit();
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (k < n) out[f + 32 * h + k] += __uint_as_float(v[k]);
-          }
-        }
-      }
-      bulk_wait0();
-    } else {
-      // bf16: a thread has its row's 64 numbers copied into shared memory a tile ahead, adds to them there and has them copied back
-      const bool bulk = wide && a.n_out % 8 == 0;
-      CT* out = c + (long long)(row0 + row) * a.c_stride;
-      const int in_warp = min(max(rows - warp * 32, 0), 32);
-      auto loaded = [&](int j) { return bar0 + 8u * (2 * AT_STAGES + 6 + 2 * warp + (j & 1)); };
-      auto width = [&](int j) { return min(64, a.n_out - (f0 + j) * 64); };
-      auto fetch = [&](int j) {
-        if (!bulk || j >= n2) return;
-        if (lane == 0) mbar_expect_tx(loaded(j), in_warp * 2 * width(j));
-        __syncwarp();
-        if (lane < in_warp) bulk_load(smem_u32(own + 32 * (j & 1)), out + (f0 + j) * 64, 2 * width(j), loaded(j));
-      };
-      fetch(0);
-      int j = 0;
-      for (; j < n2 && ok; ++j) {
-        const int f = (f0 + j) * 64;
-        ok = __all_sync(0xffffffffu, mbar_wait(d_full(j), (j >> 1) & 1, s_abort));
-        if (!ok) break;
-        tc_fence_after();
-        uint32_t v[64];
-        tc_ld32(mine + P::D_COL + (j & 1) * 64, v);
-        tc_ld32(mine + P::D_COL + (j & 1) * 64 + 32, v + 32);
-        tc_wait_ld();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(d_empty(j));
-        if (bulk) {
-          bulk_wait_read0();                         // the other half of the row has been copied back: the next tile's may come
-          __syncwarp();
-          fetch(j + 1);
-          ok = __all_sync(0xffffffffu, mbar_wait(loaded(j), (j >> 1) & 1, s_abort));
-          if (!ok) {
-            ++j;
-            break;
-          }
-          uint4* p = reinterpret_cast<uint4*>(own + 32 * (j & 1));
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const uint4 o = p[k];
-            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-            uint32_t y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              y[e] = pack_bf16(__uint_as_float(w[e] << 16) + __uint_as_float(v[8 * k + 2 * e]), __uint_as_float(w[e] & 0xffff0000u) + __uint_as_float(v[8 * k + 2 * e + 1]));
-            p[k] = make_uint4(y[0], y[1], y[2], y[3]);
-          }
+          for (int k = 0; k < 8; ++k)
+            *reinterpret_cast<uint4*>(to + ((k ^ (row & 7)) << 4)) = make_uint4(v[32 * h + 4 * k], v[32 * h + 4 * k + 1], v[32 * h + 4 * k + 2], v[32 * h + 4 * k + 3]);
           fence_async_smem();
-          if (lane < in_warp) bulk_store(out + f, smem_u32(p), 2 * width(j));
-          bulk_commit();
-        } else if (row < rows) {
+          together();
+          if (issues && f + 32 * h < a.n_out) {
+            asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+                         ::"l"(&tmC), "r"(f + 32 * h), "r"(row0), "r"(smem_u32(stage) + h * AT_X) : "memory");
+          }
+          if (issues) bulk_commit();
+        }
+      } else {
+        // bf16: C's tile came with the weights'; it is added to in place and copied back
+        uint8_t* at = smem + slot * P::SLOT + NH * AT_W + row * 128;
 #pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (k < width(j)) out[f + k] = from_f<CT>(to_f(out[f + k]) + __uint_as_float(v[k]));
+        for (int k = 0; k < 8; ++k) {
+          uint4* p = reinterpret_cast<uint4*>(at + ((k ^ (row & 7)) << 4));
+          const uint4 o = *p;
+          const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+          uint32_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            y[e] = pack_bf16(__uint_as_float(w[e] << 16) + __uint_as_float(v[8 * k + 2 * e]), __uint_as_float(w[e] & 0xffff0000u) + __uint_as_float(v[8 * k + 2 * e + 1]));
+          *p = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        fence_async_smem();
+        together();
+        if (issues) {
+          asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                       ::"l"(&tmC), "r"(f), "r"(row0), "r"(smem_u32(smem) + slot * P::SLOT + NH * AT_W) : "memory");
+          bulk_commit();
+          if (j > 0) {
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            mbar_arrive(c_empty(j - 1));             // the last tile has been read
+          }
         }
       }
-      bulk_wait0();
-      // copies in flight after a wait that ran out have landed (a bounded wait)
-      const unsigned long long t0 = clock64();
-      if (bulk && !ok)
-        for (int k = max(0, j - 1); k <= j && k < n2; ++k)
-          while (!mbar_try(loaded(k), (k >> 1) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {}
     }
+    bulk_wait0();
   }
   if (!ok && lane == 0) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
   tc_fence_before();
@@ -405,12 +405,23 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
 
 template <typename CT, int NH> int launch_at(const AdapterArgs& a, cudaStream_t st) {
   using P = AtPlan<CT, NH>;
-  CUtensorMap x, wa, wb;
+  CUtensorMap x, wa, wb, c;
   const int ranks = (a.max_rank + 15) & ~15;
   int rc = get_tensor_map_2d(a.x, a.max_rows, a.K, 128, &x);
   if (rc == SL_OK) rc = get_tensor_map_2d(a.a, (long long)a.n_adapters * a.max_rank, a.K, ranks, &wa);
   if (rc == SL_OK) rc = get_tensor_map_2d(a.b, (long long)a.n_adapters * a.n_out, a.max_rank, 64, &wb);
   if (rc != SL_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(a.c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0) {
+    TensorMapEncodeFn fn = tensor_map_encode_fn();
+    const cuuint64_t dims[2] = {(cuuint64_t)a.n_out, (cuuint64_t)a.max_rows}, strides[1] = {(cuuint64_t)a.c_stride * sizeof(CT)};
+    const cuuint32_t box[2] = {128 / sizeof(CT), 128}, each[2] = {1, 1};
+    if (!fn || fn(&c, sizeof(CT) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, a.c, dims, strides, box, each,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return SL_ECUDA;
+  } else {
+    c = x;                                           // not used
+  }
   auto kernel = gemm_adapters_tc_kernel<CT, NH>;
   static std::atomic<uint64_t> done{0};
   SL_CUDA_TRY(allow_smem(kernel, P::SMEM, done));
@@ -441,7 +452,7 @@ template <typename CT, int NH> int launch_at(const AdapterArgs& a, cudaStream_t 
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, x, wa, wb, a));
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, x, wa, wb, c, a));
   return SL_OK;
 }
 
