@@ -627,10 +627,27 @@ def surelock_attention_paged(cache: PagedKV, q, row_offsets, seq_lens, o, worksp
 
 
 # ---- a served batch on the paged cache: from request lengths to tokens ------------------------------------------------------
-def _plan_sizes(page_table, free_pages):
-    _want(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.is_cuda,
-          "page_table: a contiguous int32 CUDA tensor [B][max_pages] is wanted")
-    return page_table.shape[0], page_table.shape[1], free_pages.numel()
+def _stream_of(dev: int) -> int:
+    """The current stream of a device, which has to be the current one."""
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise SurelockError(f"tensors on the current CUDA device are wanted, got them on {'cuda:%d' % dev if dev >= 0 else 'the CPU'}")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _ptrs(dev: int, dtype: torch.dtype, least: int, *tensors):
+    """Addresses of contiguous tensors of a type on a device, of at least so many entries."""
+    at = []
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != dev or t.numel() < least or not t.is_contiguous():
+            raise SurelockError(f"a contiguous {dtype} tensor of at least {least} entries on cuda:{dev} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        at.append(t.data_ptr())
+    return at
+
+
+def _status(t: Optional[torch.Tensor], dev: int):
+    if t is None:
+        return None
+    return _ptrs(dev, torch.int32, 1, t)[0]
 
 
 def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active,
@@ -638,24 +655,30 @@ def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free
     """Pages off the free list, row offsets and flat positions (N = max_pages * page_size) for new_tokens[b] more tokens of every
     sequence; seq_lens and n_free are updated in place unless seq_lens_out, n_free_out are given.  All int32 CUDA tensors:
     page_table [B][max_pages], seq_lens, new_tokens [B], free_pages [n_pages], n_free, n_active [1], row_offsets [B+1], active_idx [rows]."""
-    B, width, n_pages = _plan_sizes(page_table, free_pages)
-    lens_out, free_out = seq_lens if seq_lens_out is None else seq_lens_out, n_free if n_free_out is None else n_free_out
-    stream = _here(page_table, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active, lens_out, free_out, dev_status)
-    _check(lib().surelock_paged_extend(page_table.data_ptr(), B, page_size, width, n_pages, _ints(seq_lens, B), _ints(new_tokens, B),
-                                       _ints(free_pages, 1), _ints(n_free, 1), _ints(row_offsets, B + 1), _ints(active_idx, 0),
-                                       _ints(n_active, 1), active_idx.numel(), _ints(lens_out, B), _ints(free_out, 1), _word(dev_status),
-                                       stream), "surelock_paged_extend")
+    dev = page_table.get_device()
+    stream = _stream_of(dev)
+    _want(page_table.dim() == 2, "page_table: [B][max_pages] is wanted")
+    B, width = page_table.shape
+    i32 = torch.int32
+    table, lens, new, lens_out = _ptrs(dev, i32, B, page_table, seq_lens, new_tokens, seq_lens if seq_lens_out is None else seq_lens_out)
+    free, n, M, n_out = _ptrs(dev, i32, 1, free_pages, n_free, n_active, n_free if n_free_out is None else n_free_out)
+    offsets, = _ptrs(dev, i32, B + 1, row_offsets)
+    idx, = _ptrs(dev, i32, 0, active_idx)
+    _check(lib().surelock_paged_extend(table, B, page_size, width, free_pages.numel(), lens, new, free, n, offsets, idx, M, active_idx.numel(),
+                                       lens_out, n_out, _status(dev_status, dev), stream), "surelock_paged_extend")
 
 
 def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pages, n_free, seq_lens_out=None, n_free_out=None,
                             dev_status=None):
     """Sequence b cut to min(seq_lens[b], keep[b]) tokens, its pages back onto the free list (free_pages, n_free: in place)."""
-    B, width, n_pages = _plan_sizes(page_table, free_pages)
-    lens_out, free_out = seq_lens if seq_lens_out is None else seq_lens_out, n_free if n_free_out is None else n_free_out
-    stream = _here(page_table, seq_lens, keep, free_pages, n_free, lens_out, free_out, dev_status)
-    _check(lib().surelock_paged_truncate(page_table.data_ptr(), B, page_size, width, n_pages, _ints(seq_lens, B), _ints(keep, B),
-                                         _ints(free_pages, 1), _ints(n_free, 1), _ints(lens_out, B), _ints(free_out, 1), _word(dev_status),
-                                         stream), "surelock_paged_truncate")
+    dev = page_table.get_device()
+    stream = _stream_of(dev)
+    _want(page_table.dim() == 2, "page_table: [B][max_pages] is wanted")
+    B, width = page_table.shape
+    table, lens, kept, lens_out = _ptrs(dev, torch.int32, B, page_table, seq_lens, keep, seq_lens if seq_lens_out is None else seq_lens_out)
+    free, n, n_out = _ptrs(dev, torch.int32, 1, free_pages, n_free, n_free if n_free_out is None else n_free_out)
+    _check(lib().surelock_paged_truncate(table, B, page_size, width, free_pages.numel(), lens, kept, free, n, lens_out, n_out,
+                                         _status(dev_status, dev), stream), "surelock_paged_truncate")
 
 
 ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
@@ -683,24 +706,34 @@ class Rope:
         self.ref = C.byref(self.raw)
 
 
+def _heads(t, dev: int, dtype, like=None):
+    """(address, row stride in elements, shape) of a tensor [rows][heads][head_dim] whose rows are packed (they may lie apart)."""
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or st[2] != 1 or (st[1] != shape[2] and shape[1] != 1) or t.dtype is not dtype or t.get_device() != dev or \
+            (like is not None and shape != like):
+        raise SurelockError(f"a {dtype} tensor [rows][heads][head_dim] with packed rows on cuda:{dev} is wanted, got {t.dtype} {tuple(shape)}, strides {st}, on {t.device}")
+    return t.data_ptr(), st[0] if shape[0] > 1 else max(st[0], shape[1] * shape[2]), shape
+
+
 def surelock_rope(rope: Rope, q, k, positions, n_active, N: int = 0, q_out=None, k_out=None, transposed: bool = False, dev_status=None):
     """Rotates rows of q [M][H][head_dim] and k [M][n_kv_heads][head_dim] (or None), bf16 or fp32, rows may lie apart; in place
     unless q_out, k_out are given.  positions int32 [M], taken modulo N when N > 0 (flat positions of a step)."""
-    _want(q.dim() == 3, f"q: [M][H][head_dim] is wanted, got {tuple(q.shape)}")
-    M, H, dh = q.shape
-    qo, ko = q if q_out is None else q_out, k if k_out is None else k_out
-    _want(qo.dtype == q.dtype and qo.shape == q.shape, "q_out must be like q")
-    qs, qos = _rows(q, H, dh)[1], _rows(qo, H, dh)[1]
+    dev, dtype = q.get_device(), q.dtype
+    stream = _stream_of(dev)
+    qp, qs, (M, H, dh) = _heads(q, dev, dtype)
+    qo, qos = (qp, qs) if q_out is None else _heads(q_out, dev, dtype, q.shape)[:2]
+    kp = ko = None
     Hkv = ks = kos = 0
     if k is not None:
-        _want(k.dim() == 3 and k.shape[0] == M and k.dtype == q.dtype and ko.dtype == q.dtype and ko.shape == k.shape, "k, k_out: rows and type of q")
-        Hkv = k.shape[1]
-        ks, kos = _rows(k, Hkv, dh)[1], _rows(ko, Hkv, dh)[1]
-    stream = _here(q, k, positions, n_active, qo, ko, rope.freq, dev_status)
+        kp, ks, (Mk, Hkv, dk) = _heads(k, dev, dtype)
+        ko, kos = (kp, ks) if k_out is None else _heads(k_out, dev, dtype, k.shape)[:2]
+        _want(Mk == M and dk == dh, "k: rows and head_dim of q")
+    _want(rope.freq.get_device() == dev, "the frequencies are on another device")
     if M:
-        _check(lib().surelock_rope(rope.ref, q.data_ptr(), qs, H, None if k is None else k.data_ptr(), ks, Hkv, dh, _ints(positions, M), N,
-                                   _ints(n_active, 1), M, qo.data_ptr(), qos, None if k is None else ko.data_ptr(), kos, _dt(q),
-                                   int(transposed), _word(dev_status), stream), "surelock_rope")
+        pos, = _ptrs(dev, torch.int32, M, positions)
+        n, = _ptrs(dev, torch.int32, 1, n_active)
+        _check(lib().surelock_rope(rope.ref, qp, qs, H, kp, ks, Hkv, dh, pos, N, n, M, qo, qos, ko, kos, _dt(q), int(transposed),
+                                   _status(dev_status, dev), stream), "surelock_rope")
 
 
 class Adapters:
@@ -723,15 +756,20 @@ class Adapters:
 def surelock_gemm_adapters(x, adapters: Adapters, adapter_of_seq, row_offsets, Cout, dev_status=None):
     """Cout[r] += scale B (A x[r]) with the adapter of the row's sequence.  x bf16 [M][K]; Cout bf16 or fp32 [M][n_out], rows may
     lie apart; adapter_of_seq int32 [B] (negative: none), row_offsets int32 [B+1]."""
-    _want(x.dim() == 2 and x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape[1] == adapters.K, "x: contiguous bf16 [M][K] of the adapters' K")
+    dev = x.get_device()
+    stream = _stream_of(dev)
+    _want(x.dim() == 2 and x.shape[1] == adapters.K, "x: bf16 [M][K] of the adapters' K")
     M, n = x.shape[0], adapters.n_out
-    st = Cout.stride()
-    _want(Cout.shape == (M, n) and (st[1] == 1 or n == 1) and (st[0] >= n or M <= 1), "Cout: [M][n_out] with packed rows")
+    shape, st = Cout.shape, Cout.stride()
+    _want(shape == (M, n) and (st[1] == 1 or n == 1) and (st[0] >= n or M <= 1), "Cout: [M][n_out] with packed rows")
+    _want(Cout.get_device() == dev and adapters.a.get_device() == dev, "all tensors on one CUDA device are wanted")
     B = adapter_of_seq.numel()
-    stream = _here(x, adapters.a, adapter_of_seq, row_offsets, Cout, dev_status)
     if M and B:
-        _check(lib().surelock_gemm_adapters(x.data_ptr(), adapters.ref, _ints(adapter_of_seq, B), _ints(row_offsets, B + 1), B, Cout.data_ptr(),
-                                            max(st[0], n), M, n, adapters.K, _dt(Cout), _word(dev_status), stream), "surelock_gemm_adapters")
+        xp, = _ptrs(dev, torch.bfloat16, 1, x)
+        which, = _ptrs(dev, torch.int32, B, adapter_of_seq)
+        offsets, = _ptrs(dev, torch.int32, B + 1, row_offsets)
+        _check(lib().surelock_gemm_adapters(xp, adapters.ref, which, offsets, B, Cout.data_ptr(), max(st[0], n), M, n, adapters.K, _dt(Cout),
+                                            _status(dev_status, dev), stream), "surelock_gemm_adapters")
 
 
 class Sampling:
@@ -747,21 +785,20 @@ class Sampling:
         self.ref = C.byref(self.raw)
 
 
-def _floats(t: torch.Tensor, least: int) -> int:
-    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= least):
-        raise SurelockError(f"a contiguous fp32 CUDA tensor of at least {least} entries is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
 def surelock_sample(logits, sampling: Sampling, u, n_active, token, conf=None, n_kept=None, set_of_row=None, dev_status=None):
     """A token per row of logits [M][vocab] (bf16 or fp32, rows may lie apart) from one uniform number per row, u fp32 [M].  token,
     n_kept int32 [M], conf fp32 [M]; row r uses set set_of_row[r], or set r, or the only one."""
+    dev = logits.get_device()
+    stream = _stream_of(dev)
     _want(logits.dim() == 2, f"logits: [M][vocab] is wanted, got {tuple(logits.shape)}")
     M, V = logits.shape
     st = logits.stride()
     _want((st[1] == 1 or V == 1) and (st[0] >= V or M <= 1), "logits: packed rows are wanted")
-    stream = _here(logits, sampling.first, u, n_active, token, conf, n_kept, set_of_row, dev_status)
+    _want(sampling.first is None or sampling.first.get_device() == dev, "the settings are on another device")
     if M:
-        _check(lib().surelock_sample(logits.data_ptr(), max(st[0], V), sampling.ref, None if set_of_row is None else _ints(set_of_row, M), _floats(u, M),
-                                     _ints(n_active, 1), M, V, _dt(logits), _ints(token, M), None if conf is None else _floats(conf, M),
-                                     None if n_kept is None else _ints(n_kept, M), _word(dev_status), stream), "surelock_sample")
+        up, = _ptrs(dev, torch.float32, M, u)
+        n, = _ptrs(dev, torch.int32, 1, n_active)
+        tok, = _ptrs(dev, torch.int32, M, token)
+        _check(lib().surelock_sample(logits.data_ptr(), max(st[0], V), sampling.ref, None if set_of_row is None else _ptrs(dev, torch.int32, M, set_of_row)[0],
+                                     up, n, M, V, _dt(logits), tok, None if conf is None else _ptrs(dev, torch.float32, M, conf)[0],
+                                     None if n_kept is None else _ptrs(dev, torch.int32, M, n_kept)[0], _status(dev_status, dev), stream), "surelock_sample")

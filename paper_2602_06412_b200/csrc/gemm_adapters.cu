@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection: for the rows r of a sequence that uses adapter a,
 //   C[r] += scale_a B_a (A_a x_r),   A_a [rank][K], B_a [n_out][rank].
 //
-// One launch, no workspace: a cluster of CL CTAs takes 16 WR rows of one sequence (its adapter's weights are read once for
+// One launch, no workspace: a cluster of CL CTAs takes 16 rows of one sequence (its adapter's weights are read once for
 // them).  Each CTA multiplies its 1 / CL of K, the partial t = A_a x of all CTAs meet through distributed shared memory in a
 // fixed order, and each CTA then adds its 1 / CL of the features to C.  Both products are mma.sync m16n8k16 with the rows on the
 // 16 side: they are far from the tensor cores' rate (rank operations per byte), and their operands come straight from global
@@ -37,16 +37,17 @@ template <int TERMS> __device__ __forceinline__ void bf16_terms(float v, bf16* t
   }
 }
 
-template <int WR, int NT, typename CT> struct AdapterTile {
-  static constexpr int ROWS = 16 * WR, KS = AD_WARPS / WR, TERMS = sizeof(CT) == 2 ? 2 : 3;
+template <int NT, typename CT> struct AdapterTile {
+  static constexpr int AHEAD = NT <= 4 ? 3 : 1;         // times 32 features in registers (64 ranks and two: one CTA to an SM, 55 against 41 us)
+  static constexpr int ROWS = 16, KS = AD_WARPS, TERMS = sizeof(CT) == 2 ? 2 : 3;
   static constexpr int TP = 8 * NT + 4;                               // pitch of t in floats: rows 4 banks apart
   static constexpr int SP = (8 * NT < 16 ? 16 : 8 * NT) + 8;          // pitch of its bf16 terms
   static constexpr int T_BYTES = KS * ROWS * TP * 4, BYTES = T_BYTES + TERMS * ROWS * SP * 2;
 };
 
-template <int WR, int NT, typename CT>
+template <int NT, typename CT>
 __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a) {
-  using L = AdapterTile<WR, NT, CT>;
+  using L = AdapterTile<NT, CT>;
   constexpr int ROWS = L::ROWS, KS = L::KS, TERMS = L::TERMS, TP = L::TP, SP = L::SP, KSTEPS = (8 * NT + 15) / 16;
   extern __shared__ __align__(16) unsigned char smem[];
   float* part = reinterpret_cast<float*>(smem);
@@ -57,35 +58,24 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
   const int CL = (int)ctas, rank_cta = (int)cluster_ctarank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int wr = warp % WR, kw = warp / WR;
-  int seq, row0, rows;
-  if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, seq, row0, rows)) return;
-  int ad, rank;
-  if (!find_adapter(a, seq, ad, rank)) return;
+  int ad, row0, rows, rank;
+  if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const bf16* wa = a.a + (long long)ad * a.max_rank * a.K;
   const bf16* wb = a.b + (long long)ad * a.n_out * a.max_rank;
   const int fgs = (a.n_out + 31) >> 5, fg0 = (int)((long long)fgs * rank_cta / CL), fg1 = (int)((long long)fgs * (rank_cta + 1) / CL);
-  if (WR == 1) {                                     // few rows wait for these weights: have them in the L2 by then
-    const long long lines = ((long long)(min(fg1 * 32, a.n_out) - fg0 * 32) * a.max_rank * 2 + 127) >> 7;
-    for (long long i = threadIdx.x; i < lines; i += AD_THREADS)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(wb + (long long)fg0 * 32 * a.max_rank) + (i << 7)));
-    const int of_row = ((min(fg1 * 32, a.n_out) - fg0 * 32) * (int)sizeof(CT) + 127) >> 7;
-    for (int i = threadIdx.x; i < rows * of_row; i += AD_THREADS)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(reinterpret_cast<const CT*>(a.c) + (row0 + i / of_row) * a.c_stride + fg0 * 32) + ((i % of_row) << 7)));
-  }
 
   // ---- t = A_a x over this warp's k
   float acc[NT][4];
 #pragma unroll
   for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
   {
-    const int chunks = (a.K + 31) >> 5, splits = CL * KS, s = rank_cta * KS + kw;
+    const int chunks = (a.K + 31) >> 5, splits = CL * KS, s = rank_cta * KS + warp;
     const int c0 = (int)((long long)chunks * s / splits), c1 = (int)((long long)chunks * (s + 1) / splits);
-    const int ra = wr * 16 + g, rb = ra + 8;
+    const int ra = g, rb = g + 8;
     const bf16 *xa = a.x + (long long)(row0 + ra) * a.K, *xb = a.x + (long long)(row0 + rb) * a.K;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     // A matrix instruction may cut off where an addition would round, so long chains are joined outside: the sums so far go to shared memory
-    float* to = part + (kw * ROWS + wr * 16 + g) * TP + 2 * t;
+    float* to = part + (warp * ROWS + g) * TP + 2 * t;
     auto flush = [&](bool first) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
@@ -123,14 +113,12 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
     flush(c1 - c0 <= AD_CHAIN);
   }
   __syncthreads();
-  if (KS > 1) {
-    for (int i = threadIdx.x; i < ROWS * 8 * NT; i += AD_THREADS) {
-      const int at = (i / (8 * NT)) * TP + i % (8 * NT);
-      float v = part[at];
+  for (int i = threadIdx.x; i < ROWS * 8 * NT; i += AD_THREADS) {
+    const int at = (i / (8 * NT)) * TP + i % (8 * NT);
+    float v = part[at];
 #pragma unroll
-      for (int w = 1; w < KS; ++w) v += part[w * ROWS * TP + at];
-      part[at] = v;
-    }
+    for (int w = 1; w < KS; ++w) v += part[w * ROWS * TP + at];
+    part[at] = v;
   }
   cluster_sync_all();
   {
@@ -154,24 +142,30 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the others' t
   __syncthreads();
 
-  // ---- C += B_a t over this CTA's features, 32 at a time to a warp: lane t of a quad ends up with 8 neighbours.  The next 32 features'
-  // weights and C are on their way while these are multiplied.
+  // ---- C += B_a t over this CTA's features, 32 at a time to a warp: lane t of a quad ends up with 8 neighbours.  The weights and C of the
+  // next times are on their way while these are multiplied.
   CT* c = reinterpret_cast<CT*>(a.c);
   const bool wide = (reinterpret_cast<uintptr_t>(c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;
-  const int ra = wr * 16 + g, rb = ra + 8;
-  const bf16* mine = terms + (wr * 16 + g) * SP + 4 * t;
+  const int ra = g, rb = g + 8;
+  const bf16* mine = terms + g * SP + 4 * t;
   CT* const row_a = c + (row0 + ra) * a.c_stride + 8 * t;
   CT* const row_b = c + (row0 + rb) * a.c_stride + 8 * t;
   constexpr int WORDS = sizeof(CT) / 2;
   struct alignas(16) Eight { CT e[8]; };
-  Eight old[2];
-  uint2 w[KSTEPS][4];
-  auto load_w = [&](int fg, int s) {
-    const int k = 16 * s + 4 * t;
+  constexpr int AHEAD = L::AHEAD;
+  Eight old[AHEAD][2];
+  uint2 w[AHEAD][KSTEPS][4];
+  const bf16* const my_w = wb + (long long)(8 * (g >> 1) + (g & 1)) * a.max_rank + 4 * t;
+  auto load_w = [&](int fg, uint2* to, int s) {
+    const bf16* p = my_w + (long long)fg * 32 * a.max_rank + 16 * s;
+    const bool in = 16 * s + 4 * t < rank;
+    if (fg * 32 + 32 <= a.n_out) {                   // the same for the whole warp
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int f = fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
-      w[s][j] = f < a.n_out && k < rank ? __ldg(reinterpret_cast<const uint2*>(wb + (long long)f * a.max_rank + k)) : make_uint2(0u, 0u);
+      for (int j = 0; j < 4; ++j) to[j] = in ? __ldg(reinterpret_cast<const uint2*>(p + 2 * j * a.max_rank)) : make_uint2(0u, 0u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        to[j] = in && fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1) < a.n_out ? __ldg(reinterpret_cast<const uint2*>(p + 2 * j * a.max_rank)) : make_uint2(0u, 0u);
     }
   };
   auto load_c = [&](int fg, Eight* to) {
@@ -190,67 +184,69 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
       }
     }
   };
-  int fg = fg0 + kw;
-  if (fg < fg1) {
-    load_c(fg, old);
 #pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) load_w(fg, s);
-  }
-  for (; fg < fg1; fg += KS) {
-    const int next = fg + KS, f0 = fg * 32 + 8 * t;
-    Eight after[2];
-    if (next < fg1) load_c(next, after);
-    float d[4][4];
+  for (int u = 0; u < AHEAD; ++u)
+    if (fg0 + warp + u * KS < fg1) {
+      load_c(fg0 + warp + u * KS, old[u]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
-#pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) {
-      if (16 * s >= rank) break;
-      const int k = 16 * s + 4 * t;
-      if (k + 4 > rank) {                            // what lies behind the adapter's own rank is not read into the sum
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (k + 3 >= rank) w[s][j].y &= 0xffffu;
-          if (k + 2 >= rank) w[s][j].y = 0u;
-          if (k + 1 >= rank) w[s][j].x &= 0xffffu;
-        }
-      }
-#pragma unroll
-      for (int m = TERMS - 1; m >= 0; --m) {         // the small terms first
-        const uint2 u = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 16 * s);
-        const uint2 v = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 8 * SP + 16 * s);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, w[s][j].x, w[s][j].y);
-      }
-      if (next < fg1) load_w(next, s);
+      for (int s = 0; s < KSTEPS; ++s) load_w(fg0 + warp + u * KS, w[u][s], s);
     }
+  for (int fg_u = fg0 + warp; fg_u < fg1; fg_u += AHEAD * KS)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if ((h ? rb : ra) < rows) {
-        CT* p = (h ? row_b : row_a) + fg * 32;
-        Eight out;
+    for (int q = 0; q < AHEAD; ++q) {
+      const int fg = fg_u + q * KS, next = fg + AHEAD * KS, f0 = fg * 32 + 8 * t;
+      if (fg >= fg1) break;
+      float d[4][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out.e[i] = from_f<CT>(to_f(old[h].e[i]) + d[i >> 1][2 * h + (i & 1)]);
-        if (wide && f0 + 8 <= a.n_out) {
+      for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
 #pragma unroll
-          for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(&out)[i];
-        } else {
+      for (int s = 0; s < KSTEPS; ++s) {
+        if (16 * s >= rank) break;
+        const int k = 16 * s + 4 * t;
+        uint2* x = w[q][s];
+        if (16 * s + 16 > rank && k + 4 > rank) {    // what lies behind the adapter's own rank is not read into the sum
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (f0 + i < a.n_out) p[i] = out.e[i];
+          for (int j = 0; j < 4; ++j) {
+            if (k + 3 >= rank) x[j].y &= 0xffffu;
+            if (k + 2 >= rank) x[j].y = 0u;
+            if (k + 1 >= rank) x[j].x &= 0xffffu;
+          }
         }
+#pragma unroll
+        for (int m = TERMS - 1; m >= 0; --m) {       // the small terms first
+          const uint2 u = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 16 * s);
+          const uint2 v = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 8 * SP + 16 * s);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, x[j].x, x[j].y);
+        }
+        if (next < fg1) load_w(next, x, s);
       }
-    old[0] = after[0];
-    old[1] = after[1];
-  }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if ((h ? rb : ra) < rows) {
+          CT* p = (h ? row_b : row_a) + fg * 32;
+          Eight out;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) out.e[i] = from_f<CT>(to_f(old[q][h].e[i]) + d[i >> 1][2 * h + (i & 1)]);
+          if (wide && f0 + 8 <= a.n_out) {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(&out)[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (f0 + i < a.n_out) p[i] = out.e[i];
+          }
+        }
+      if (next < fg1) load_c(next, old[q]);
+    }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody reads this CTA's t any more
 }
 
-template <int WR, int NT, typename CT>
+template <int NT, typename CT>
 int launch_tile(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
-  using L = AdapterTile<WR, NT, CT>;
+  using L = AdapterTile<NT, CT>;
   static std::atomic<uint64_t> done{0};
-  SL_CUDA_TRY(allow_smem(gemm_adapters_kernel<WR, NT, CT>, L::BYTES, done));
+  SL_CUDA_TRY(allow_smem(gemm_adapters_kernel<NT, CT>, L::BYTES, done));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)groups * CL);
   cfg.blockDim = dim3(AD_THREADS);
@@ -264,7 +260,7 @@ int launch_tile(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_adapters_kernel<WR, NT, CT>, a));
+  SL_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_adapters_kernel<NT, CT>, a));
   return SL_OK;
 }
 
@@ -274,11 +270,11 @@ int launch_few(const AdapterArgs& a, cudaStream_t st) {
   const long long groups = a.max_rows / 16 + (a.max_rows < a.B ? a.max_rows : a.B);
   if (groups > (1 << 27)) return SL_EUNSUPPORTED;
   int CL = AD_CLUSTER;
-  while (CL > 1 && groups * CL > 4ll * sm_count()) CL >>= 1;
-  if (a.max_rank <= 16) return launch_tile<1, 2, CT>(a, (int)groups, CL, st);
-  if (a.max_rank <= 32) return launch_tile<1, 4, CT>(a, (int)groups, CL, st);
-  if (a.max_rank <= 64) return launch_tile<1, 8, CT>(a, (int)groups, CL, st);
-  return launch_tile<1, 16, CT>(a, (int)groups, CL, st);
+  while (CL > 1 && groups * CL > 2ll * sm_count()) CL >>= 1;
+  if (a.max_rank <= 16) return launch_tile<2, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 32) return launch_tile<4, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 64) return launch_tile<8, CT>(a, (int)groups, CL, st);
+  return launch_tile<16, CT>(a, (int)groups, CL, st);
 }
 
 }  // namespace

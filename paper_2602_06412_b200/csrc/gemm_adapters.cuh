@@ -15,8 +15,8 @@ struct AdapterArgs {
   int n_adapters, max_rank, B, max_rows, n_out, K;
 };
 
-// The group-th tile of `tile` rows of one sequence: its sequence, first row and rows; every lane of a warp gets the same.
-__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& seq, int& row0, int& rows) {
+// The group-th tile of `tile` rows of one sequence: its adapter's number, first row and rows; every lane of a warp gets the same.
+__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& ad, int& row0, int& rows) {
   const int lane = threadIdx.x & 31;
   int before = 0;                                    // tiles of the sequences before this round's 32
   bool bad = false;
@@ -24,6 +24,7 @@ __device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int t
     const int b = b0 + lane;
     // offsets are clamped, so that no row is outside C
     int from = b < a.B ? a.row_offsets[b] : 0, to = b < a.B ? a.row_offsets[b + 1] : 0;
+    const int its = b < a.B ? a.adapter_of_seq[b] : -1;    // for every sequence, so that its load does not wait for the search
     if (b < a.B) bad |= from < 0 || to < from || to > a.max_rows;
     from = min(max(from, 0), a.max_rows);
     to = min(max(to, from), a.max_rows);
@@ -38,7 +39,7 @@ __device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int t
     if (hit) {
       const int l = __ffs(hit) - 1;
       const int first = group - before - __shfl_sync(0xffffffffu, sum - mine, l);
-      seq = b0 + l;
+      ad = __shfl_sync(0xffffffffu, its, l);
       row0 = __shfl_sync(0xffffffffu, from, l) + first * tile;
       rows = min(tile, __shfl_sync(0xffffffffu, to, l) - row0);
       if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
@@ -50,9 +51,8 @@ __device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int t
   return false;
 }
 
-// The adapter of a tile's sequence and its rank; false where there is nothing to add.
-__device__ __forceinline__ bool find_adapter(const AdapterArgs& a, int seq, int& ad, int& rank) {
-  ad = a.adapter_of_seq[seq];
+// The rank of an adapter; false where there is nothing to add.
+__device__ __forceinline__ bool find_rank(const AdapterArgs& a, int ad, int& rank) {
   if (ad < 0 || ad >= a.n_adapters) {
     if (ad >= a.n_adapters) set_status(a.status, SL_DEV_BAD_INDEX);
     return false;

@@ -75,8 +75,8 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
   const int CL = (int)ctas, cta = (int)cluster_ctarank();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  int seq, row0, rows, ad, rank;                     // the same in the whole cluster
-  if (!find_tile(a, (int)(blockIdx.x / CL), 128, seq, row0, rows) || !find_adapter(a, seq, ad, rank)) return;
+  int row0, rows, ad, rank;                          // the same in the whole cluster
+  if (!find_tile(a, (int)(blockIdx.x / CL), 128, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const int ranks = (a.max_rank + 15) & ~15;         // rows of A_a in a copy: a whole number of 16
   const bool wide = (reinterpret_cast<uintptr_t>(a.c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;   // C may be copied in tiles
   constexpr int VEC = 16 / sizeof(CT);
