@@ -3,7 +3,8 @@
 The library call `surelock_step` is Algorithm 1 lines 6-15 and 18-24, `surelock_update_mask` is line 16
 (`UpdateMASK`); this module plays line 5 (the loop over diffusion steps): semi-autoregressive blocks, and in every step
 each sequence reveals the `k` masked positions of its current block whose posterior is most confident, with their
-argmax tokens (temperature 0, "low-confidence remasking": the rest stay masked).  Both calls are kernels of the
+argmax tokens (temperature 0, "low-confidence remasking": the rest stay masked) or, with `sampling`, with tokens drawn from
+it by `surelock_sample`.  These calls are kernels of the
 library working on device buffers, so the loop never waits for the GPU; per-step times are CUDA events read at the end.
 
 It also computes what the paper reports from such a run: the per-step active-row trace M_t, the micro-averaged active
@@ -46,7 +47,7 @@ def selection_skip_mask(lock: torch.Tensor, mask_state: torch.Tensor, fraction: 
 
 def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: int, block_len: int, steps: int,
         kl_eps: float, surelock: bool = True, unmask_per_step: int = 1, select_fraction: float = None,
-        select_seed: int = 0, observer=None, unlock: Dict = None) -> Dict:
+        select_seed: int = 0, observer=None, unlock: Dict = None, sampling: Dict = None) -> Dict:
     """Run `steps` diffusion steps on device tensors tokens int32 [B][N], mask_state uint8 [B][N] (both updated in
     place).  Generation positions n_prompt.. are decoded block by block (`block_len` positions, `steps_per_block` =
     ceil(block_len / unmask_per_step) steps each).  `select_fraction` (Experiment 5, e.g. 0.8) adds the selection
@@ -57,6 +58,9 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
     d_interval, d_cool, rho, m_percent) switches un-locking on for this run: after every step's unmasking the probe is
     called (it works every `period`-th step) and may return locked positions to the active set; the number of un-locked
     positions per step is in the result.
+    `sampling`: a dict of temperature, top_k, top_p, min_p (those that are wanted) and seed makes the revealed tokens samples of
+    the posterior instead of its argmax: `surelock_sample` draws a token for every row of a step from one uniform number, and
+    the positions whose drawn tokens are most probable (their softmax confidence, as before) are revealed.
     `observer`, when given, is called after every step, before the unmasking of line 16, as
     observer(t, out, lock_in, lock_out, tokens, mask_state) with lock_in a copy of the lock mask the step was given
     (skip mask included) and lock_out the mask after the step; it is for tests that look at a step from outside and
@@ -75,6 +79,13 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
     if unlock is not None:
         SL.surelock_set_unlocking(ctx, **unlock)                            # (resets the ctx)
         unlocked_trace = torch.zeros(steps, dtype=torch.int32, device=dev)
+    if sampling is not None:
+        value = lambda name, dtype: torch.tensor([sampling[name]], dtype=dtype, device=dev) if name in sampling else None
+        settings = SL.Sampling(value("temperature", torch.float32), value("top_k", torch.int32), value("top_p", torch.float32),
+                               value("min_p", torch.float32))
+        gen = torch.Generator(device=dev).manual_seed(int(sampling.get("seed", 0)))
+        u, drawn_conf = torch.empty(R, device=dev), torch.empty(R, device=dev)
+        drawn = torch.empty(R, dtype=torch.int32, device=dev)
     SL.surelock_reset(ctx)
     ev[0].record()
     for t in range(steps):
@@ -95,7 +106,12 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
         blk = min(t // steps_per_block, max((N - n_prompt + block_len - 1) // block_len - 1, 0))
         lo = n_prompt + blk * block_len
         hi = min(lo + block_len, N)
-        SL.surelock_update_mask(out.conf, out.argmax, out.active_idx, out.row_offsets, B, N, lo, hi, unmask_per_step,
+        conf, token = out.conf, out.argmax
+        if sampling is not None:
+            u.uniform_(generator=gen)
+            SL.surelock_sample(out.logits, settings, u, out.n_active, drawn, drawn_conf)
+            conf, token = drawn_conf, drawn
+        SL.surelock_update_mask(conf, token, out.active_idx, out.row_offsets, B, N, lo, hi, unmask_per_step,
                                 mask_token, tokens, mask_state, n_rev)
         unmasked_trace[t:t + 1] = n_rev.sum(dtype=torch.int32)
         if unlock is not None and surelock:

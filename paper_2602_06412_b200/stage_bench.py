@@ -9,6 +9,9 @@
     python -m paper_2602_06412_b200.stage_bench --stage kv_scatter_paged --rows 12288 --B 8 --N 1536 --cache e4m3
     python -m paper_2602_06412_b200.stage_bench --stage kv_gather_paged --rows 6144 --B 8 --N 1536 --cache int8
     python -m paper_2602_06412_b200.stage_bench --stage attention_paged --B 4 --N 16384 --rows 4 --cache e4m3
+    python -m paper_2602_06412_b200.stage_bench --stage rope --rows 12288 --N 1536
+    python -m paper_2602_06412_b200.stage_bench --stage gemm_adapters --M 64 --B 64 --n_out 12288 --rank 64
+    python -m paper_2602_06412_b200.stage_bench --stage sample --rows 820 --top_p 0.95
 
 Prints one JSON line: median and minimum device time (CUDA events on the launching stream, after warm-up), the
 algorithmic bytes / FLOPs of the launch, and the achieved fraction of the measured HBM or bf16 peak.  A buffer
@@ -60,7 +63,13 @@ def _time(fn, iters, warmup, flush):
 def main(argv=None):
     ap = argparse.ArgumentParser()
     ap.add_argument("--stage", required=True, choices=["gemm", "attention", "softmax_kl", "kv_scatter", "compact",
-                                                          "gemm_quantized", "kv_scatter_paged", "kv_gather_paged", "attention_paged"])
+                                                          "gemm_quantized", "kv_scatter_paged", "kv_gather_paged", "attention_paged",
+                                                          "rope", "gemm_adapters", "sample"])
+    ap.add_argument("--rank", type=int, default=16, help="gemm_adapters")
+    ap.add_argument("--temperature", type=float, default=1.0, help="sample, as the next three")
+    ap.add_argument("--top_k", type=int, default=0)
+    ap.add_argument("--top_p", type=float, default=1.0)
+    ap.add_argument("--min_p", type=float, default=0.0)
     ap.add_argument("--M", type=int, default=4096)
     ap.add_argument("--n_out", type=int, default=12288)
     ap.add_argument("--K", type=int, default=4096)
@@ -193,6 +202,34 @@ def main(argv=None):
                 fn = lambda: SL.surelock_kv_gather_paged(cache, idx, n, N, k, v, status)
             byts = 2.0 * M * (token + 2 * Hkv * dh)
         res.update(shape=dict(B=B, N=N, H=a.H, Hkv=Hkv, dh=dh, M=M, page=a.page), cache=a.cache, flops=flops, bytes=byts)
+    elif a.stage == "rope":
+        M, H, Hkv, dh = a.rows, a.H, a.Hkv, a.dh
+        q, k = (rnd(M, h, dh).to(torch.bfloat16) for h in (H, Hkv))
+        freq, scale = SL.surelock_rope_frequencies(dh, 500000.0)
+        rope = SL.Rope(freq.to(dev), scale=scale)
+        pos = torch.randint(0, a.N, (M,), device=dev, generator=g).to(torch.int32)
+        n = torch.tensor([M], dtype=torch.int32, device=dev)
+        fn = lambda: SL.surelock_rope(rope, q, k, pos, n, dev_status=status)
+        res.update(shape=dict(M=M, H=H, Hkv=Hkv, dh=dh), bytes=4.0 * M * (H + Hkv) * dh, flops=0.0)
+    elif a.stage == "gemm_adapters":
+        M, B, K = a.M, a.B, a.K                                    # M rows spread over B sequences, an adapter each
+        pool = SL.Adapters(rnd(B, a.rank, K).to(torch.bfloat16), rnd(B, a.n_out, a.rank).to(torch.bfloat16), torch.ones(B, device=dev))
+        which = torch.arange(B, dtype=torch.int32, device=dev)
+        offs = torch.tensor([M * b // B for b in range(B + 1)], dtype=torch.int32, device=dev)
+        x, Cout = rnd(M, K).to(torch.bfloat16), torch.zeros((M, a.n_out), dtype=torch.float32 if a.epilogue == 1 else torch.bfloat16, device=dev)
+        fn = lambda: SL.surelock_gemm_adapters(x, pool, which, offs, Cout, status)
+        res.update(shape=[M, a.n_out, K], sequences=B, rank=a.rank, flops=2.0 * M * a.rank * (K + a.n_out),
+                   bytes=2.0 * M * K + (8.0 if a.epilogue == 1 else 4.0) * M * a.n_out + 2.0 * B * a.rank * (K + a.n_out))
+    elif a.stage == "sample":
+        M, V = a.rows, a.V
+        logits = (rnd(M, V) * 3).to(torch.bfloat16)
+        f32 = lambda v: torch.tensor([v], device=dev)
+        sampling = SL.Sampling(f32(a.temperature), torch.tensor([a.top_k], dtype=torch.int32, device=dev), f32(a.top_p), f32(a.min_p))
+        u, conf = torch.rand(M, device=dev, generator=g), torch.empty(M, device=dev)
+        token = torch.empty(M, dtype=torch.int32, device=dev)
+        n = torch.tensor([M], dtype=torch.int32, device=dev)
+        fn = lambda: SL.surelock_sample(logits, sampling, u, n, token, conf, dev_status=status)
+        res.update(shape=dict(M=M, vocab=V), bytes=2.0 * M * V, flops=0.0)
     else:
         total = a.flags
         lock = (torch.rand(total, device=dev, generator=g) < 0.5).to(torch.uint8)
