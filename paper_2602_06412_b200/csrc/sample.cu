@@ -195,8 +195,19 @@ struct Ask {
 __device__ __forceinline__ Ask ask_rank(uint32_t rank) { return {true, false, rank, 0.0}; }
 __device__ __forceinline__ Ask ask_mass(double target, bool strict) { return {false, strict, 0u, target}; }
 
-// The first lane of a warp whose n tokens of weight w in all hold what is asked for; f.before_*, the sums before the warp's, become those
-// before the lane's.  Where roundings leave none: the last lane that has tokens, and its last token is asked for from there on.
+// The first lane of a warp whose n tokens, in and iw being the warp's running sums, hold what is asked for; f.before_*, the sums before the
+// warp's, become those before the lane's.  Where roundings leave none: the last lane that has tokens, and its last token is asked for from
+// there on.
+__device__ __forceinline__ int pick_lane(Ask& ask, uint32_t n, uint32_t in, double iw, Found& f) {
+  const unsigned some = __ballot_sync(0xffffffffu, n != 0u), hit = __ballot_sync(0xffffffffu, n && ask.in(f.before_n + in, f.before_w + iw));
+  const int l = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+  const uint32_t upto = __shfl_sync(0xffffffffu, in, l), mine = __shfl_sync(0xffffffffu, n, l);
+  if (!hit) ask = ask_rank(f.before_n + upto - 1);
+  const double before = __shfl_sync(0xffffffffu, iw, max(l - 1, 0));
+  f.before_n += upto - mine;
+  f.before_w += l ? before : 0.0;
+  return l;
+}
 __device__ __forceinline__ int pick_lane(Ask& ask, uint32_t n, double w, Found& f) {
   const int lane = threadIdx.x & 31;
   uint32_t in = n;
@@ -210,30 +221,43 @@ __device__ __forceinline__ int pick_lane(Ask& ask, uint32_t n, double w, Found& 
       iw += b;
     }
   }
-  const unsigned some = __ballot_sync(0xffffffffu, n != 0u), hit = __ballot_sync(0xffffffffu, n && ask.in(f.before_n + in, f.before_w + iw));
-  const int l = hit ? __ffs(hit) - 1 : 31 - __clz(some);
-  const uint32_t upto = __shfl_sync(0xffffffffu, in, l), mine = __shfl_sync(0xffffffffu, n, l);
-  if (!hit) ask = ask_rank(f.before_n + upto - 1);
-  const double before = __shfl_sync(0xffffffffu, iw, max(l - 1, 0));
-  f.before_n += upto - mine;
-  f.before_w += l ? before : 0.0;
-  return l;
+  return pick_lane(ask, n, in, iw, f);
 }
+
+// The leading warp's view of the groups: every lane has a run of them, with the sums of the run and up to and with it.
+struct Ladder {
+  uint32_t n, in;
+  double w, iw;
+  __device__ void climb(const Shared& s, int groups) {
+    const int lane = threadIdx.x & 31, per = (groups + 31) >> 5;
+    n = 0u;
+    w = 0.0;
+    for (int g = lane * per; g < min(groups, (lane + 1) * per); ++g) {
+      n += s.group_n[g];
+      w += s.group_w[g];
+    }
+    in = n;
+    iw = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t a = __shfl_up_sync(0xffffffffu, in, o);
+      const double b = __shfl_up_sync(0xffffffffu, iw, o);
+      if (lane >= o) {
+        in += a;
+        iw += b;
+      }
+    }
+  }
+};
 
 // The entry that holds what is asked for, by one warp: first among 32 runs of groups, then among a run's groups, then among a
 // group's 32 entries; entry(i, tokens, weight of a token).
-template <typename F> __device__ Found search(const Shared& s, int groups, Ask& ask, F entry, uint32_t before_n = 0u, double before_w = 0.0) {
+template <typename F> __device__ Found search(const Shared& s, const Ladder& ladder, int groups, Ask& ask, F entry, uint32_t before_n = 0u, double before_w = 0.0) {
   const int lane = threadIdx.x & 31, per = (groups + 31) >> 5;
   Found f;
   f.before_n = before_n;
   f.before_w = before_w;
-  uint32_t n = 0u;
-  double w = 0.0;
-  for (int g = lane * per; g < min(groups, (lane + 1) * per); ++g) {
-    n += s.group_n[g];
-    w += s.group_w[g];
-  }
-  int g = pick_lane(ask, n, w, f) * per;
+  int g = pick_lane(ask, ladder.n, ladder.in, ladder.iw, f) * per;
   const bool one = lane < per && g + lane < groups;
   g += pick_lane(ask, one ? s.group_n[g + lane] : 0u, one ? s.group_w[g + lane] : 0.0, f);
   uint32_t c;
@@ -318,23 +342,23 @@ template <int CTAS> struct Sums {
     }
   }
   // by the leading warp, after a barrier
-  __device__ Totals total(const Settings& set) const {
+  Ladder ladder;
+  __device__ Totals total(const Settings& set) {
     const int lane = threadIdx.x & 31;
     Totals t = {};
-    for (int g = lane; g < groups; g += 32) {
-      t.n += s.group_n[g];
-      t.w += s.group_w[g];
+    ladder.climb(s, groups);
+    t.n = __shfl_sync(0xffffffffu, ladder.in, 31);
+    t.w = __shfl_sync(0xffffffffu, ladder.iw, 31);
+    if (set.min_p > 0.0 || inv_T != 1.0) {
+      for (int i = lane; i < CTAS * SM_WARPS; i += 32) {
+        t.nm += s.warp_nm[i];
+        t.m += s.warp_m[i];
+        t.raw += s.warp_raw[i];
+      }
+      t.nm = warp_sum(t.nm);
+      t.m = warp_sum(t.m);
+      t.raw = warp_sum(t.raw);
     }
-    for (int i = lane; i < CTAS * SM_WARPS; i += 32) {
-      t.nm += s.warp_nm[i];
-      t.m += s.warp_m[i];
-      t.raw += s.warp_raw[i];
-    }
-    t.n = warp_sum(t.n);
-    t.w = warp_sum(t.w);
-    t.nm = warp_sum(t.nm);
-    t.m = warp_sum(t.m);
-    t.raw = warp_sum(t.raw);
     if (!(set.min_p > 0.0)) t.nm = t.n;
     if (inv_T == 1.0) t.raw = t.w;
     return t;
@@ -569,7 +593,7 @@ template <int CTAS> struct WindowSums : Sums<CTAS> {
   }
   // by the leading warp alone
   __device__ Found find(const Share<bf16>&, Ask ask) const {
-    Found f = search(s, groups, ask, [&](int e, uint32_t& c, double& w) {
+    Found f = search(s, this->ladder, groups, ask, [&](int e, uint32_t& c, double& w) {
       c = tokens(e);
       w = c ? weight(e) : 0.0;
     });
@@ -726,7 +750,8 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
     turn ^= 1;
     if (this->leads()) {
       Ask mine = ask;
-      const Found f = search(s, groups, mine, [&](int e, uint32_t& c, double& w) { entry(e, c, w); }, before_n, before_w);
+      this->ladder.climb(s, groups);
+      const Found f = search(s, this->ladder, groups, mine, [&](int e, uint32_t& c, double& w) { entry(e, c, w); }, before_n, before_w);
       publish<CTAS>(slot, f);
     }
     row_sync<CTAS>();
