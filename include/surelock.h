@@ -601,7 +601,8 @@ typedef struct {
  * may be a part of a wider row.  row_offsets dev int32 [B + 1], ascending, clamped to 0 ... max_rows (device status 4, as for an adapter or a
  * rank out of range; such an adapter is none).  Rows of no sequence are left as they are.  K and max_rank multiples of 8, max_rank <= 128,
  * x, a, b 16-byte aligned (SL_EUNSUPPORTED otherwise); any n_out, c_stride and alignment of C to its elements.  A_a x is summed in fp32 and
- * enters the second product as an fp32 number (as one of 17 bits for a bf16 C); C is rounded once.  Deterministic; no workspace; one launch;
+ * enters the second product as an fp32 number (as one of 17 bits for a bf16 C); C is rounded once (fp32 sums below 2^-126 may become 0).
+ * dev_status may be NULL; 2 = a bounded wait ran out, and the rows that this concerns are NaN.  Deterministic; no workspace; one launch;
  * asynchronous on `stream`. */
 int surelock_gemm_adapters(const void *x, const surelock_adapters *adapters, const int32_t *adapter_of_seq, const int32_t *row_offsets, int B,
                            void *C, int64_t c_stride, int max_rows, int n_out, int K, int dtype, int32_t *dev_status, void *stream);
@@ -635,8 +636,8 @@ int surelock_sample(const void *logits, int64_t row_stride, const surelock_sampl
                     const int32_t *n_active, int max_rows, int vocab, int dtype, int32_t *token, float *conf, int32_t *n_kept,
                     int32_t *dev_status, void *stream);
 
-/* Failure-detection diagnostic for the two calls with few bits that wait on copies: in the next surelock_gemm_quantized or
- * surelock_attention_paged that this thread launches, one CTA (the product's first, the attention's second if there is one)
+/* Failure-detection diagnostic for the calls that wait on copies: in the next surelock_gemm_quantized, surelock_attention_paged or (with
+ * 32 and more rows to a sequence) surelock_gemm_adapters that this thread launches, one CTA (the products' first, the attention's second if there is one)
  * waits for 16 bytes that are never copied.  Its bounded waits run out (about 2 s each), it stores device status 2 or 3 in the
  * call's dev_status, and the kernel returns with outputs as described there; nothing hangs or traps, and the workspace may be used
  * again.  The call must be given at least one active row; captured into a graph, every replay waits so. */

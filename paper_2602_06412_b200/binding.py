@@ -533,7 +533,7 @@ def surelock_gemm_quantized(A, W, Cout, n_active, epilogue: int = 0, W2=None, wo
 
 
 def surelock_lose_next_copy():
-    """Diagnostic: a copy that the next quantised product or paged attention of this thread waits for is never made."""
+    """Diagnostic: a copy that the next call of this thread that waits on copies waits for is never made (see the header)."""
     _check(lib().surelock_lose_next_copy(), "surelock_lose_next_copy")
 
 

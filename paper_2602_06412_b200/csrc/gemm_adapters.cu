@@ -281,9 +281,13 @@ int launch_few(const AdapterArgs& a, cudaStream_t st) {
 
 int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_t* adapter_of_seq, const int32_t* row_offsets, int B,
                          void* C, long long c_stride, int max_rows, int n_out, int K, int dtype, int32_t* status, cudaStream_t st) {
-  const AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
-                         c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K};
-  if (a.max_rows >= AD_MANY * (long long)B) return launch_gemm_adapters_tc(a, dtype, st);
+  AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
+                         c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K, 0};
+  // copies of the many rows' kernel count rows of a pool in 32 bits
+  if (a.max_rows >= AD_MANY * (long long)B && (long long)w.n_adapters * (n_out > w.max_rank ? n_out : w.max_rank) < 0x7fffff00ll) {
+    a.lost = take_lost_copy();
+    return launch_gemm_adapters_tc(a, dtype, st);
+  }
   return dtype == SL_BF16 ? launch_few<bf16>(a, st) : launch_few<float>(a, st);
 }
 

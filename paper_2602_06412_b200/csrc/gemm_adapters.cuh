@@ -13,6 +13,7 @@ struct AdapterArgs {
   int32_t* status;
   long long c_stride;
   int n_adapters, max_rank, B, max_rows, n_out, K;
+  int lost;                         // bytes of a copy that is waited for and never made (a diagnostic), or 0
 };
 
 // The group-th tile of `tile` rows of one sequence: its adapter's number, first row and rows; every lane of a warp gets the same.

@@ -117,7 +117,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
         if (!(ok = mbar_wait(empty(i), ((i / AT_STAGES) & 1) ^ 1, s_abort))) break;
         const uint32_t at = ring + i % AT_STAGES * P::SLOT;
         if (i < n1) {
-          mbar_expect_tx(full(i), AT_X + ranks * 128);
+          mbar_expect_tx(full(i), AT_X + ranks * 128 + (i == 0 && blockIdx.x == 0 ? a.lost : 0));
           tma_load_2d(at, &tmX, (b0 + i) * 64, row0, full(i));
           tma_load_2d(at + AT_X, &tmA, (b0 + i) * 64, ad * a.max_rank, full(i));
         } else {
@@ -224,6 +224,10 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[k + e] = __float_as_uint(__uint_as_float(v[k + e]) + __uint_as_float(u[e]));
         }
+      if (!ok) {                                     // an incomplete sum is NaN, for whichever CTA uses it
+#pragma unroll
+        for (int k = 0; k < 64; ++k) v[k] = 0x7fffffffu;
+      }
       if (CL > 1) {
         // each CTA sums its 1 / CL of the rows over the cluster, in the order of the CTAs, and gives every CTA the sums (all CTAs reading all
         // shares: CL times the traffic)
@@ -407,6 +411,9 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
       }
     }
     bulk_wait0();
+    if (!ok && row < rows)                           // what this CTA did not get to is NaN
+      for (int f = (f0 + j) * 64; f < min((f0 + n2) * 64, a.n_out); ++f)
+        reinterpret_cast<CT*>(a.c)[(long long)(row0 + row) * a.c_stride + f] = from_f<CT>(__uint_as_float(0x7fffffffu));
   }
   if (!ok && lane == 0) set_status(a.status, SL_DEV_GEMM_TIMEOUT);
   tc_fence_before();

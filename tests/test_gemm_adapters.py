@@ -184,3 +184,61 @@ def test_replayed_with_other_requests_and_deterministic(B, rows, cap):
             out.append(c.clone())
         want, tol = _want(x, c0, a, b, scale, [32] * 6, w, o)
         assert np.all(np.abs(out[0].cpu().double().numpy() - want) <= tol + 2.0 ** -23 * np.abs(want)) and torch.equal(*out)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rank,K", [(16, 1024), (128, 320)])
+def test_a_lost_copy_ends_the_call_with_a_status(dtype, rank, K):
+    """The bounded waits run out: status 2, the tile's rows are NaN, the others right, and so is the next call."""
+    a, b, scale = _make(2, rank, K, 300, 11)
+    ad = SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV))
+    x = torch.randn(700, K, generator=torch.Generator().manual_seed(11)).to(torch.bfloat16).to(DEV)
+    c0 = torch.randn(700, 300, generator=torch.Generator().manual_seed(12)).to(dtype).to(DEV)
+    which, offs, status = _i32([0, 1]), _i32([0, 400, 700]), _i32([0])
+    run = lambda: (lambda c: (SL.surelock_gemm_adapters(x, ad, which, offs, c, status), c)[1])(c0.clone())
+    want = run()
+    assert status.item() == 0
+    SL.surelock_lose_next_copy()
+    got = run()
+    assert status.item() == 2 and bool(torch.isnan(got[:128]).all()) and torch.equal(got[128:], want[128:])
+    status.zero_()
+    assert torch.equal(run(), want) and status.item() == 0
+
+
+@gpu
+def test_no_wait_runs_to_its_limit_when_a_kernel_leaves():
+    """Before a CTA leaves it waits for its copies and products, at most 2 s and without a status: a wait for the wrong phase would
+    show as time only.  Numbers of blocks of k and of features below, at and above the rings' sizes."""
+    import time
+    for K in (8, 64, 72, 192, 256, 520, 1104):
+        for n_out in (5, 64, 130, 260, 700):
+            for rank in (16, 128):
+                a, b, scale = _make(1, rank, K, n_out, 13)
+                ad = SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV))
+                x = torch.zeros(200, K, dtype=torch.bfloat16, device=DEV)
+                for dtype in (torch.bfloat16, torch.float32):
+                    c = torch.zeros(200, n_out, dtype=dtype, device=DEV)
+                    torch.cuda.synchronize()
+                    t = time.perf_counter()
+                    SL.surelock_gemm_adapters(x, ad, _i32([0]), _i32([0, 200]), c)
+                    torch.cuda.synchronize()
+                    assert time.perf_counter() - t < 1.0
+
+
+@gpu
+@pytest.mark.parametrize("rows,n_out,pitch,offset", [(500, 96, 96, 0), (500, 96, 104, 8), (500, 96, 97, 1), (500, 95, 96, 0), (40, 33, 40, 3), (300, 64, 1000, 936)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_outputs_anywhere(dtype, rows, n_out, pitch, offset):
+    """C in wider rows, off 16 bytes, with a last tile that is not whole: the neighbours of every row stay as they are."""
+    a, b, scale = _make(2, 24, 256, n_out, 14, exact=True)
+    x = torch.randint(-2, 3, (rows, 256), generator=torch.Generator().manual_seed(14)).to(torch.bfloat16)
+    flat = torch.randint(-9, 10, (rows * pitch + 64,), generator=torch.Generator().manual_seed(15)).to(dtype)
+    dev = flat.to(DEV)
+    view = lambda t: torch.as_strided(t, (rows, n_out), (pitch, 1), offset)
+    which, offs = [1, 0], [0, rows - rows // 3, rows]
+    SL.surelock_gemm_adapters(x.to(DEV), SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV)), _i32(which), _i32(offs), view(dev))
+    want, _ = _want(x, view(flat), a, b, scale, [24] * 2, which, offs)
+    assert np.array_equal(view(dev).cpu().double().numpy(), torch.from_numpy(want).to(dtype).double().numpy())
+    view(dev).copy_(view(flat))
+    assert torch.equal(dev.cpu(), flat)
