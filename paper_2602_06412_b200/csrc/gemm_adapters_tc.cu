@@ -82,8 +82,9 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   int row0, rows, ad, rank;                          // the same in the whole cluster
   if (!find_tile(a, (int)(blockIdx.x / CL), 128, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const int ranks = (a.max_rank + 15) & ~15;         // rows of A_a in a copy: a whole number of 16
-  const bool wide = (reinterpret_cast<uintptr_t>(a.c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;   // C may be copied in tiles
   constexpr int VEC = 16 / sizeof(CT);
+  // C may be copied in tiles: a copy writes whole 16 bytes, also where the row ends inside them
+  const bool wide = (reinterpret_cast<uintptr_t>(a.c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0 && a.n_out % VEC == 0;
   struct alignas(16) Vec { CT e[VEC]; };
   const int blocks = (a.K + 63) >> 6, b0 = (int)((long long)blocks * cta / CL), n1 = (int)((long long)blocks * (cta + 1) / CL) - b0;
   const int tiles = (a.n_out + 63) >> 6, f0 = (int)((long long)tiles * cta / CL), n2 = (int)((long long)tiles * (cta + 1) / CL) - f0;
@@ -299,7 +300,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
     __syncwarp();
     if (lane == 0) mbar_arrive(t_ready);
 
-    const bool whole = wide && rows == 128, issues = threadIdx.x == 0, bulk = sizeof(CT) == 4 && wide && a.n_out % 4 == 0;
+    const bool whole = wide && rows == 128, issues = threadIdx.x == 0, bulk = sizeof(CT) == 4 && wide;
     auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
     int j = 0;
     for (; j < n2 && ok; ++j) {
