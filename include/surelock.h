@@ -637,7 +637,7 @@ int surelock_sample(const void *logits, int64_t row_stride, const surelock_sampl
                     int32_t *dev_status, void *stream);
 
 /* Failure-detection diagnostic for the calls that wait on copies: in the next surelock_gemm_quantized, surelock_attention_paged or (with
- * 32 and more rows to a sequence) surelock_gemm_adapters that this thread launches, one CTA (the products' first, the attention's second if there is one)
+ * 64 and more rows to a sequence and max_rows * max_rank >= 49152) surelock_gemm_adapters that this thread launches, one CTA (the products' first, the attention's second if there is one)
  * waits for 16 bytes that are never copied.  Its bounded waits run out (about 2 s each), it stores device status 2 or 3 in the
  * call's dev_status, and the kernel returns with outputs as described there; nothing hangs or traps, and the workspace may be used
  * again.  The call must be given at least one active row; captured into a graph, every replay waits so. */

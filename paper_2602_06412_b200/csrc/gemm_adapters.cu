@@ -9,12 +9,16 @@
 //
 // x and the weights are bf16, so the first product's terms are exact and summed in fp32.  t scale stays an fp32 number: it enters
 // the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
+//
+// Bounded by latency for one row (6.4 us in a graph, K = n_out = 4096, rank 16: finding the sequence 1.2, each product about 1, joining t 1.2 us) and by
+// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 33 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
+// registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of two CTAs per SM allows (two rounds: 41 and 22.5 us).
 #include "gemm_adapters.cuh"
 
 namespace sl {
 namespace {
 
-constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS, AD_CLUSTER = 8, AD_CHAIN = 8, AD_MANY = 32;
+constexpr int AD_WARPS = 8, AD_THREADS = 32 * AD_WARPS, AD_CLUSTER = 8, AD_CHAIN = 8;
 
 __device__ __forceinline__ void mma_16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -283,8 +287,12 @@ int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_
                          void* C, long long c_stride, int max_rows, int n_out, int K, int dtype, int32_t* status, cudaStream_t st) {
   AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
                          c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K, 0};
-  // copies of the many rows' kernel count rows of a pool in 32 bits
-  if (a.max_rows >= AD_MANY * (long long)B && (long long)w.n_adapters * (n_out > w.max_rank ? n_out : w.max_rank) < 0x7fffff00ll) {
+  // The kernel for many rows takes 128 of a sequence at a time and 19 us at least; this one's time grows with rows x rank.  K = n_out = 4096, bf16, few
+  // / many, us: 1 x 512 rows of rank 64 16.5 / 20.6, of rank 128 49 / 26; 8 x 64 rows of rank 64 17 / 25, of rank 128 25 / 29; 8 x 128 rows of rank 16
+  // 12 / 19, 64 23 / 21, 128 41 / 27; 8 x 512 of rank 16 25 / 23; 32 x 32 of rank 128 41 / 72, 32 x 64 76 / 50.  fp32: the same within a sixth, but
+  // 32 x 128 of rank 16 54 / 35.  (Its copies count the pool's rows in 32 bits.)
+  const bool many = max_rows >= 64ll * B && (long long)max_rows * w.max_rank >= 49152;
+  if (many && (long long)w.n_adapters * (n_out > w.max_rank ? n_out : w.max_rank) < 0x7fffff00ll) {
     a.lost = take_lost_copy();
     return launch_gemm_adapters_tc(a, dtype, st);
   }

@@ -20,6 +20,11 @@
 // in it: a few are ranked against one another, more of them are binned once more by their keys.
 //
 // A row is one CTA's work, or with few rows that of a cluster of CTAs, whose shares meet through distributed shared memory.
+//
+// Bounds, and what it measured in a graph: one bf16 row of 126464 tokens with top-k and top-p 21 us (latency: counting 8.5 k cycles, sums over the
+// cluster 5 k, three finds of 3 to 4 k, meeting the token 4.5 k), 33 fp32 rows of 32003 with all filters 41 us (each find has three cluster barriers and
+// a pass over the row), 1536 bf16 rows with top-p 185 us for 388 MB: the counts' atomics meet in a bank 3.4 at a time, 80 us, and what follows
+// the counting overlaps another CTA's only in part.  (A search for the k largest and a sort of 126464 numbers per row take 20 ms.)
 #include "tc_common.cuh"
 
 namespace sl {
@@ -1140,8 +1145,13 @@ int launch_sample_ctas(const SampleArgs& a, cudaStream_t st) {
 }
 
 template <typename T> int launch_sample_typed(const SampleArgs& a, cudaStream_t st) {
+  // A cluster shortens a row's passes and pays for its barriers and for the histograms' way through distributed shared memory.  Rows of 126464, us
+  // with 1 / 2 / 4 / 8 CTAs, bf16: 1 row 25 / 26 / 21 / 21, 18 rows 33 / 27 / 23 / 27, 37: 32 / 27 / 27 / 45, 74: 33 / 29 / 43 / 70, 148: 33 / 37 / 65 /
+  // 119; fp32: 1 row 193 / 120 / 76 / 55, 18 rows 212 / 123 / 79 / 70, 37: 213 / 127 / 97 / 121, 148: 213 / 166 / 250 / 329, 296: 347 / 331 / 436 / 617.
+  // So many CTAs while each has an SM and more to itself, two up to about one CTA (fp32: two) per SM.
+  const long long room = (long long)sm_count() * (sizeof(T) == 2 ? 1 : 2);
   int ctas = 8;
-  while (ctas > 1 && ((long long)a.max_rows * ctas > 2ll * sm_count() || a.vocab < ctas * 4096)) ctas >>= 1;
+  while (ctas > 1 && ((long long)a.max_rows * ctas > (ctas == 2 ? room : room / 2) || a.vocab < ctas * 4096)) ctas >>= 1;
   while (a.vocab / ctas > (1 << 17) - 16) ctas <<= 1;   // limbs' sums are 32 bits wide
   if ((long long)a.max_rows * ctas > 0x7fffffffll) return SL_EUNSUPPORTED;
   return ctas == 8   ? launch_sample_ctas<T, 8>(a, st)

@@ -73,7 +73,9 @@ def test_refusals_on_the_host():
 
 # ---- on the GPU -------------------------------------------------------------------------------------------------------
 SHAPES = [(1, "one", 1, 16, 4096, 4096), (5, "some", 3, 8, 64, 40), (64, "one", 9, 64, 1024, 520), (70, "some", 7, 24, 200, 33), (3, "200", 4, 32, 520, 96),
-          (9, "90", 5, 128, 1032, 257), (2, "700", 2, 16, 96, 1000), (4, "130", 3, 56, 8, 5), (300, "one", 20, 16, 512, 64), (1, "4000", 1, 40, 256, 128)]
+          (9, "90", 5, 128, 1032, 257), (2, "700", 2, 16, 96, 1000), (4, "130", 3, 56, 8, 5), (300, "one", 20, 16, 512, 64), (1, "4000", 1, 40, 256, 128),
+          # many rows to a sequence and rank enough for the kernel that takes 128 at a time
+          (3, "2500", 4, 32, 520, 96), (9, "400", 5, 128, 1032, 257), (2, "6000", 2, 16, 96, 1000), (4, "900", 3, 56, 8, 5), (5, "300", 2, 72, 200, 64)]
 
 
 @gpu
@@ -159,7 +161,7 @@ def test_bad_numbers_are_reported():
 
 
 @gpu
-@pytest.mark.parametrize("B,rows,cap", [(8, 1, 8), (3, 70, 400)])
+@pytest.mark.parametrize("B,rows,cap", [(8, 1, 8), (3, 70, 400), (3, 500, 1600)])
 def test_replayed_with_other_requests_and_deterministic(B, rows, cap):
     a, b, scale = _make(6, 32, 256, 160, 9)
     ad = SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV))
@@ -188,14 +190,14 @@ def test_replayed_with_other_requests_and_deterministic(B, rows, cap):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("rank,K", [(16, 1024), (128, 320)])
-def test_a_lost_copy_ends_the_call_with_a_status(dtype, rank, K):
+@pytest.mark.parametrize("rank,K,rows", [(16, 1024, 3200), (128, 320, 700)])
+def test_a_lost_copy_ends_the_call_with_a_status(dtype, rank, K, rows):
     """The bounded waits run out: status 2, the tile's rows are NaN, the others right, and so is the next call."""
     a, b, scale = _make(2, rank, K, 300, 11)
     ad = SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV))
-    x = torch.randn(700, K, generator=torch.Generator().manual_seed(11)).to(torch.bfloat16).to(DEV)
-    c0 = torch.randn(700, 300, generator=torch.Generator().manual_seed(12)).to(dtype).to(DEV)
-    which, offs, status = _i32([0, 1]), _i32([0, 400, 700]), _i32([0])
+    x = torch.randn(rows, K, generator=torch.Generator().manual_seed(11)).to(torch.bfloat16).to(DEV)
+    c0 = torch.randn(rows, 300, generator=torch.Generator().manual_seed(12)).to(dtype).to(DEV)
+    which, offs, status = _i32([0, 1]), _i32([0, 400, rows]), _i32([0])
     run = lambda: (lambda c: (SL.surelock_gemm_adapters(x, ad, which, offs, c, status), c)[1])(c0.clone())
     want = run()
     assert status.item() == 0
@@ -216,18 +218,20 @@ def test_no_wait_runs_to_its_limit_when_a_kernel_leaves():
             for rank in (16, 128):
                 a, b, scale = _make(1, rank, K, n_out, 13)
                 ad = SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV))
-                x = torch.zeros(200, K, dtype=torch.bfloat16, device=DEV)
+                rows = 3200 if rank == 16 else 400
+                x = torch.zeros(rows, K, dtype=torch.bfloat16, device=DEV)
                 for dtype in (torch.bfloat16, torch.float32):
-                    c = torch.zeros(200, n_out, dtype=dtype, device=DEV)
+                    c = torch.zeros(rows, n_out, dtype=dtype, device=DEV)
                     torch.cuda.synchronize()
                     t = time.perf_counter()
-                    SL.surelock_gemm_adapters(x, ad, _i32([0]), _i32([0, 200]), c)
+                    SL.surelock_gemm_adapters(x, ad, _i32([0]), _i32([0, rows]), c)
                     torch.cuda.synchronize()
                     assert time.perf_counter() - t < 1.0
 
 
 @gpu
-@pytest.mark.parametrize("rows,n_out,pitch,offset", [(500, 96, 96, 0), (500, 96, 104, 8), (500, 96, 97, 1), (500, 95, 96, 0), (40, 33, 40, 3), (300, 64, 1000, 936)])
+@pytest.mark.parametrize("rows,n_out,pitch,offset", [(2200, 96, 96, 0), (2200, 96, 104, 8), (2200, 96, 97, 1), (2200, 95, 96, 0), (40, 33, 40, 3), (300, 64, 1000, 936),
+                                                       (2100, 64, 1000, 936), (2100, 100, 104, 0)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_outputs_anywhere(dtype, rows, n_out, pitch, offset):
     """C in wider rows, off 16 bytes, with a last tile that is not whole: the neighbours of every row stay as they are."""
