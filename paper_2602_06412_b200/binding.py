@@ -634,20 +634,24 @@ def _stream_of(dev: int) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _ptrs(dev: int, dtype: torch.dtype, least: int, *tensors):
-    """Addresses of contiguous tensors of a type on a device, of at least so many entries."""
+def _ptrs(dev: int, dtype: torch.dtype, *wanted):
+    """Addresses of contiguous tensors of a type on a device: a tensor (or None), the entries it has at least, the next tensor ..."""
     at = []
-    for t in tensors:
+    for t, least in zip(wanted[::2], wanted[1::2]):
+        if t is None:
+            at.append(None)
+            continue
         if t.dtype is not dtype or t.get_device() != dev or t.numel() < least or not t.is_contiguous():
             raise SurelockError(f"a contiguous {dtype} tensor of at least {least} entries on cuda:{dev} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
         at.append(t.data_ptr())
     return at
 
 
-def _status(t: Optional[torch.Tensor], dev: int):
-    if t is None:
-        return None
-    return _ptrs(dev, torch.int32, 1, t)[0]
+def _table(t: torch.Tensor):
+    shape = t.shape
+    if len(shape) != 2:
+        raise SurelockError(f"page_table: [B][max_pages] is wanted, got {tuple(shape)}")
+    return shape
 
 
 def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active,
@@ -657,15 +661,13 @@ def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free
     page_table [B][max_pages], seq_lens, new_tokens [B], free_pages [n_pages], n_free, n_active [1], row_offsets [B+1], active_idx [rows]."""
     dev = page_table.get_device()
     stream = _stream_of(dev)
-    _want(page_table.dim() == 2, "page_table: [B][max_pages] is wanted")
-    B, width = page_table.shape
-    i32 = torch.int32
-    table, lens, new, lens_out = _ptrs(dev, i32, B, page_table, seq_lens, new_tokens, seq_lens if seq_lens_out is None else seq_lens_out)
-    free, n, M, n_out = _ptrs(dev, i32, 1, free_pages, n_free, n_active, n_free if n_free_out is None else n_free_out)
-    offsets, = _ptrs(dev, i32, B + 1, row_offsets)
-    idx, = _ptrs(dev, i32, 0, active_idx)
-    _check(lib().surelock_paged_extend(table, B, page_size, width, free_pages.numel(), lens, new, free, n, offsets, idx, M, active_idx.numel(),
-                                       lens_out, n_out, _status(dev_status, dev), stream), "surelock_paged_extend")
+    B, width = _table(page_table)
+    rows, n_pages = active_idx.numel(), free_pages.numel()
+    table, lens, new, lens_out, free, n, M, n_out, offsets, idx, status = _ptrs(
+        dev, torch.int32, page_table, B * width, seq_lens, B, new_tokens, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1,
+        n_free, 1, n_active, 1, n_free if n_free_out is None else n_free_out, 1, row_offsets, B + 1, active_idx, 0, dev_status, 1)
+    _check(lib().surelock_paged_extend(table, B, page_size, width, n_pages, lens, new, free, n, offsets, idx, M, rows, lens_out, n_out, status,
+                                       stream), "surelock_paged_extend")
 
 
 def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pages, n_free, seq_lens_out=None, n_free_out=None,
@@ -673,12 +675,13 @@ def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pag
     """Sequence b cut to min(seq_lens[b], keep[b]) tokens, its pages back onto the free list (free_pages, n_free: in place)."""
     dev = page_table.get_device()
     stream = _stream_of(dev)
-    _want(page_table.dim() == 2, "page_table: [B][max_pages] is wanted")
-    B, width = page_table.shape
-    table, lens, kept, lens_out = _ptrs(dev, torch.int32, B, page_table, seq_lens, keep, seq_lens if seq_lens_out is None else seq_lens_out)
-    free, n, n_out = _ptrs(dev, torch.int32, 1, free_pages, n_free, n_free if n_free_out is None else n_free_out)
-    _check(lib().surelock_paged_truncate(table, B, page_size, width, free_pages.numel(), lens, kept, free, n, lens_out, n_out,
-                                         _status(dev_status, dev), stream), "surelock_paged_truncate")
+    B, width = _table(page_table)
+    n_pages = free_pages.numel()
+    table, lens, kept, lens_out, free, n, n_out, status = _ptrs(
+        dev, torch.int32, page_table, B * width, seq_lens, B, keep, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1, n_free, 1,
+        n_free if n_free_out is None else n_free_out, 1, dev_status, 1)
+    _check(lib().surelock_paged_truncate(table, B, page_size, width, n_pages, lens, kept, free, n, lens_out, n_out, status, stream),
+           "surelock_paged_truncate")
 
 
 ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
@@ -730,10 +733,9 @@ def surelock_rope(rope: Rope, q, k, positions, n_active, N: int = 0, q_out=None,
         _want(Mk == M and dk == dh, "k: rows and head_dim of q")
     _want(rope.freq.get_device() == dev, "the frequencies are on another device")
     if M:
-        pos, = _ptrs(dev, torch.int32, M, positions)
-        n, = _ptrs(dev, torch.int32, 1, n_active)
+        pos, n, status = _ptrs(dev, torch.int32, positions, M, n_active, 1, dev_status, 1)
         _check(lib().surelock_rope(rope.ref, qp, qs, H, kp, ks, Hkv, dh, pos, N, n, M, qo, qos, ko, kos, _dt(q), int(transposed),
-                                   _status(dev_status, dev), stream), "surelock_rope")
+                                   status, stream), "surelock_rope")
 
 
 class Adapters:
@@ -765,11 +767,10 @@ def surelock_gemm_adapters(x, adapters: Adapters, adapter_of_seq, row_offsets, C
     _want(Cout.get_device() == dev and adapters.a.get_device() == dev, "all tensors on one CUDA device are wanted")
     B = adapter_of_seq.numel()
     if M and B:
-        xp, = _ptrs(dev, torch.bfloat16, 1, x)
-        which, = _ptrs(dev, torch.int32, B, adapter_of_seq)
-        offsets, = _ptrs(dev, torch.int32, B + 1, row_offsets)
+        xp, = _ptrs(dev, torch.bfloat16, x, 1)
+        which, offsets, status = _ptrs(dev, torch.int32, adapter_of_seq, B, row_offsets, B + 1, dev_status, 1)
         _check(lib().surelock_gemm_adapters(xp, adapters.ref, which, offsets, B, Cout.data_ptr(), max(st[0], n), M, n, adapters.K, _dt(Cout),
-                                            _status(dev_status, dev), stream), "surelock_gemm_adapters")
+                                            status, stream), "surelock_gemm_adapters")
 
 
 class Sampling:
@@ -796,9 +797,7 @@ def surelock_sample(logits, sampling: Sampling, u, n_active, token, conf=None, n
     _want((st[1] == 1 or V == 1) and (st[0] >= V or M <= 1), "logits: packed rows are wanted")
     _want(sampling.first is None or sampling.first.get_device() == dev, "the settings are on another device")
     if M:
-        up, = _ptrs(dev, torch.float32, M, u)
-        n, = _ptrs(dev, torch.int32, 1, n_active)
-        tok, = _ptrs(dev, torch.int32, M, token)
-        _check(lib().surelock_sample(logits.data_ptr(), max(st[0], V), sampling.ref, None if set_of_row is None else _ptrs(dev, torch.int32, M, set_of_row)[0],
-                                     up, n, M, V, _dt(logits), tok, None if conf is None else _ptrs(dev, torch.float32, M, conf)[0],
-                                     None if n_kept is None else _ptrs(dev, torch.int32, M, n_kept)[0], _status(dev_status, dev), stream), "surelock_sample")
+        up, c = _ptrs(dev, torch.float32, u, M, conf, M)
+        n, tok, kept, sets, status = _ptrs(dev, torch.int32, n_active, 1, token, M, n_kept, M, set_of_row, M, dev_status, 1)
+        _check(lib().surelock_sample(logits.data_ptr(), max(st[0], V), sampling.ref, sets, up, n, M, V, _dt(logits), tok, c, kept, status, stream),
+               "surelock_sample")
