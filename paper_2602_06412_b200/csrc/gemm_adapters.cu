@@ -11,7 +11,7 @@
 // the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
 //
 // Bounded by latency for one row (6.4 us in a graph, K = n_out = 4096, rank 16: finding the sequence 1.2, each product about 1, joining t 1.2 us) and by
-// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 33 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
+// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 33 to 35 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
 // registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of two CTAs per SM allows (two rounds: 41 and 22.5 us).
 #include "gemm_adapters.cuh"
 
