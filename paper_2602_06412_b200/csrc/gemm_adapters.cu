@@ -11,8 +11,9 @@
 // the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
 //
 // Bounded by latency for one row (6.4 us in a graph, K = n_out = 4096, rank 16: finding the sequence 1.2, each product about 1, joining t 1.2 us) and by
-// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 33 to 35 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
-// registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of two CTAs per SM allows (two rounds: 41 and 22.5 us).
+// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 29 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
+// registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of the SMs' CTAs allows (two rounds, of two
+// CTAs to an SM: 41 and 22.5 us; of one, 64 rows of rank 128 with n_out = 4096: 39 instead of 34 us).
 #include "gemm_adapters.cuh"
 
 namespace sl {
@@ -30,6 +31,11 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
+// two numbers of ranks k and k + 1: those from `rank` on become zeros
+__device__ __forceinline__ uint32_t only(uint32_t two, int k, int rank) {
+  return k >= rank ? 0u : k + 1 >= rank ? two & 0xffffu : two;
+}
+
 // the k-th term of v as a sum of bf16 numbers
 template <int TERMS> __device__ __forceinline__ void bf16_terms(float v, bf16* to, int pitch) {
 #pragma unroll
@@ -42,17 +48,23 @@ template <int TERMS> __device__ __forceinline__ void bf16_terms(float v, bf16* t
 }
 
 template <int NT, typename CT> struct AdapterTile {
-  static constexpr int AHEAD = NT <= 4 ? 3 : 1;         // times 32 features in registers (64 ranks and two: one CTA to an SM, 55 against 41 us)
+  // times 32 features of weights and C in registers: as many as leave 128 registers to a thread and so two CTAs to an SM.  64 rows, n_out = 12288, with
+  // one CTA: rank 32 33 instead of 20.5 us, fp32 C 37 instead of 22.5, rank 16 with fp32 C 25 instead of 16.5.  More than 64 ranks take 252 registers.
+  static constexpr bool FP32 = sizeof(CT) == 4;
+  static constexpr int AHEAD = NT > 4 ? 1 : NT == 4 ? (FP32 ? 1 : 2) : (FP32 ? 2 : 3);
+  static constexpr int CTAS = NT <= 8 ? 2 : 1;
   static constexpr int ROWS = 16, KS = AD_WARPS, TERMS = sizeof(CT) == 2 ? 2 : 3;
   static constexpr int TP = 8 * NT + 4;                               // pitch of t in floats: rows 4 banks apart
-  static constexpr int SP = (8 * NT < 16 ? 16 : 8 * NT) + 8;          // pitch of its bf16 terms
+  // ranks to a load of weights: a quad's four lanes take 32 or 64 bytes of a feature, which costs the L1 half as many lines (64 ranks 35 -> 29 us)
+  static constexpr int WK = NT <= 2 ? 16 : 32;
+  static constexpr int SP = NT <= 2 ? 24 : NT == 4 ? 32 : 8 * NT + 32;  // pitch of its bf16 terms: neighbouring rows' WK miss one another's banks
   static constexpr int T_BYTES = KS * ROWS * TP * 4, BYTES = T_BYTES + TERMS * ROWS * SP * 2;
 };
 
 template <int NT, typename CT>
-__global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a) {
+__global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_adapters_kernel(AdapterArgs a) {
   using L = AdapterTile<NT, CT>;
-  constexpr int ROWS = L::ROWS, KS = L::KS, TERMS = L::TERMS, TP = L::TP, SP = L::SP, KSTEPS = (8 * NT + 15) / 16;
+  constexpr int ROWS = L::ROWS, KS = L::KS, TERMS = L::TERMS, TP = L::TP, SP = L::SP, WK = L::WK, KS2 = (8 * NT + WK - 1) / WK;
   extern __shared__ __align__(16) unsigned char smem[];
   float* part = reinterpret_cast<float*>(smem);
   bf16* terms = reinterpret_cast<bf16*>(smem + L::T_BYTES);
@@ -128,8 +140,8 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   {
     const float scale = a.scale[ad];
     const uint32_t base = smem_u32(part);
-    for (int i = threadIdx.x; i < ROWS * 16 * KSTEPS; i += AD_THREADS) {
-      const int r = i / (16 * KSTEPS), j = i % (16 * KSTEPS);
+    for (int i = threadIdx.x; i < ROWS * WK * KS2; i += AD_THREADS) {
+      const int r = i / (WK * KS2), j = i % (WK * KS2);
       float v = 0.f;
       if (j < rank && r < rows) {
         const uint32_t at = base + 4 * (r * TP + j);
@@ -151,25 +163,27 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
   CT* c = reinterpret_cast<CT*>(a.c);
   const bool wide = (reinterpret_cast<uintptr_t>(c) & 15) == 0 && (a.c_stride * sizeof(CT)) % 16 == 0;
   const int ra = g, rb = g + 8;
-  const bf16* mine = terms + g * SP + 4 * t;
+  constexpr int LK = WK / 4;                          // ranks to a lane
+  using Word = std::conditional_t<LK == 8, uint4, uint2>;
+  const bf16* mine = terms + g * SP + LK * t;
   CT* const row_a = c + (row0 + ra) * a.c_stride + 8 * t;
   CT* const row_b = c + (row0 + rb) * a.c_stride + 8 * t;
   constexpr int WORDS = sizeof(CT) / 2;
   struct alignas(16) Eight { CT e[8]; };
   constexpr int AHEAD = L::AHEAD;
   Eight old[AHEAD][2];
-  uint2 w[AHEAD][KSTEPS][4];
-  const bf16* const my_w = wb + (long long)(8 * (g >> 1) + (g & 1)) * a.max_rank + 4 * t;
-  auto load_w = [&](int fg, uint2* to, int s) {
-    const bf16* p = my_w + (long long)fg * 32 * a.max_rank + 16 * s;
-    const bool in = 16 * s + 4 * t < rank;
+  Word w[AHEAD][KS2][4];
+  const bf16* const my_w = wb + (long long)(8 * (g >> 1) + (g & 1)) * a.max_rank + LK * t;
+  auto load_w = [&](int fg, Word* to, int s) {
+    const bf16* p = my_w + (long long)fg * 32 * a.max_rank + WK * s;
+    const bool in = WK * s + LK * t < rank;
     if (fg * 32 + 32 <= a.n_out) {                   // the same for the whole warp
 #pragma unroll
-      for (int j = 0; j < 4; ++j) to[j] = in ? __ldg(reinterpret_cast<const uint2*>(p + 2 * j * a.max_rank)) : make_uint2(0u, 0u);
+      for (int j = 0; j < 4; ++j) to[j] = in ? __ldg(reinterpret_cast<const Word*>(p + 2 * j * a.max_rank)) : Word{};
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        to[j] = in && fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1) < a.n_out ? __ldg(reinterpret_cast<const uint2*>(p + 2 * j * a.max_rank)) : make_uint2(0u, 0u);
+        to[j] = in && fg * 32 + 8 * (g >> 1) + 2 * j + (g & 1) < a.n_out ? __ldg(reinterpret_cast<const Word*>(p + 2 * j * a.max_rank)) : Word{};
     }
   };
   auto load_c = [&](int fg, Eight* to) {
@@ -193,7 +207,7 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
     if (fg0 + warp + u * KS < fg1) {
       load_c(fg0 + warp + u * KS, old[u]);
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) load_w(fg0 + warp + u * KS, w[u][s], s);
+      for (int s = 0; s < KS2; ++s) load_w(fg0 + warp + u * KS, w[u][s], s);
     }
   for (int fg_u = fg0 + warp; fg_u < fg1; fg_u += AHEAD * KS)
 #pragma unroll
@@ -204,13 +218,17 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
 #pragma unroll
       for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        if (16 * s >= rank) break;
-        const int k = 16 * s + 4 * t;
-        uint2* x = w[q][s];
-        if (16 * s + 16 > rank && k + 4 > rank) {    // what lies behind the adapter's own rank is not read into the sum
+      for (int s = 0; s < KS2; ++s) {
+        if (WK * s >= rank) break;
+        const int k = WK * s + LK * t;
+        Word* x = w[q][s];
+        if (WK * s + WK > rank && k + LK > rank) {   // what lies behind the adapter's own rank is not read into the sum
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            if constexpr (LK == 8) {
+              x[j].w = only(x[j].w, k + 6, rank);
+              x[j].z = only(x[j].z, k + 4, rank);
+            }
             if (k + 3 >= rank) x[j].y &= 0xffffu;
             if (k + 2 >= rank) x[j].y = 0u;
             if (k + 1 >= rank) x[j].x &= 0xffffu;
@@ -218,10 +236,13 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
         }
 #pragma unroll
         for (int m = TERMS - 1; m >= 0; --m) {       // the small terms first
-          const uint2 u = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 16 * s);
-          const uint2 v = *reinterpret_cast<const uint2*>(mine + m * ROWS * SP + 8 * SP + 16 * s);
+          const Word u = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + WK * s);
+          const Word v = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + 8 * SP + WK * s);
 #pragma unroll
           for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, x[j].x, x[j].y);
+          if constexpr (LK == 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma_16816(d[j], u.z, v.z, u.w, v.w, x[j].z, x[j].w);
         }
         if (next < fg1) load_w(next, x, s);
       }
@@ -247,8 +268,13 @@ __global__ void __launch_bounds__(AD_THREADS) gemm_adapters_kernel(AdapterArgs a
 }
 
 template <int NT, typename CT>
-int launch_tile(const AdapterArgs& a, int groups, int CL, cudaStream_t st) {
+int launch_tile(const AdapterArgs& a, int groups, cudaStream_t st) {
   using L = AdapterTile<NT, CT>;
+  // As large as one round allows, where half of the sequences of 16 rows and more are taken to end in whole tiles (8 x 64 rows of rank 128: 23 us, by the
+  // bound alone 29)
+  const int likely = groups - (a.max_rows >= 16ll * a.B ? a.B / 2 : 0);
+  int CL = AD_CLUSTER;
+  while (CL > 1 && (long long)likely * CL > (long long)L::CTAS * sm_count()) CL >>= 1;
   static std::atomic<uint64_t> done{0};
   SL_CUDA_TRY(allow_smem(gemm_adapters_kernel<NT, CT>, L::BYTES, done));
   cudaLaunchConfig_t cfg = {};
@@ -273,12 +299,10 @@ int launch_few(const AdapterArgs& a, cudaStream_t st) {
   // every sequence may end in a tile that is not full
   const long long groups = a.max_rows / 16 + (a.max_rows < a.B ? a.max_rows : a.B);
   if (groups > (1 << 27)) return SL_EUNSUPPORTED;
-  int CL = AD_CLUSTER;
-  while (CL > 1 && groups * CL > 2ll * sm_count()) CL >>= 1;
-  if (a.max_rank <= 16) return launch_tile<2, CT>(a, (int)groups, CL, st);
-  if (a.max_rank <= 32) return launch_tile<4, CT>(a, (int)groups, CL, st);
-  if (a.max_rank <= 64) return launch_tile<8, CT>(a, (int)groups, CL, st);
-  return launch_tile<16, CT>(a, (int)groups, CL, st);
+  if (a.max_rank <= 16) return launch_tile<2, CT>(a, (int)groups, st);
+  if (a.max_rank <= 32) return launch_tile<4, CT>(a, (int)groups, st);
+  if (a.max_rank <= 64) return launch_tile<8, CT>(a, (int)groups, st);
+  return launch_tile<16, CT>(a, (int)groups, st);
 }
 
 }  // namespace
@@ -288,9 +312,10 @@ int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_
   AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
                          c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K, 0};
   // The kernel for many rows takes 128 of a sequence at a time and 19 us at least; this one's time grows with rows x rank.  K = n_out = 4096, bf16, few
-  // / many, us: 1 x 512 rows of rank 64 16.5 / 20.6, of rank 128 49 / 26; 8 x 64 rows of rank 64 17 / 25, of rank 128 25 / 29; 8 x 128 rows of rank 16
-  // 12 / 19, 64 23 / 21, 128 41 / 27; 8 x 512 of rank 16 25 / 23; 32 x 32 of rank 128 41 / 72, 32 x 64 76 / 50.  fp32: the same within a sixth, but
-  // 32 x 128 of rank 16 54 / 35.  (Its copies count the pool's rows in 32 bits.)
+  // / many, us: 1 x 512 rows of rank 64 16.5 / 20.6, of rank 128 23 / 26; 1 x 1536 of rank 64 29 / 21; 8 x 64 rows of rank 64 16.5 / 25, of rank 128 23 /
+  // 29; 8 x 128 rows of rank 16 12 / 19, 64 21 / 21, 128 33 / 27; 8 x 512 of rank 16 25 / 23, fp32 35 / 27; 32 x 64 of rank 64 30 / 31, fp32 35 / 29, of rank
+  // 128 62 / 51.  So the border costs up to 6 us at a few dozen rows of the highest ranks, and would cost 8 at many rows of low ones if it were
+  // twice as high.  (Its copies count the pool's rows in 32 bits.)
   const bool many = max_rows >= 64ll * B && (long long)max_rows * w.max_rank >= 49152;
   if (many && (long long)w.n_adapters * (n_out > w.max_rank ? n_out : w.max_rank) < 0x7fffff00ll) {
     a.lost = take_lost_copy();
