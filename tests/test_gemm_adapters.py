@@ -74,6 +74,7 @@ def test_refusals_on_the_host():
 # ---- on the GPU -------------------------------------------------------------------------------------------------------
 SHAPES = [(1, "one", 1, 16, 4096, 4096), (5, "some", 3, 8, 64, 40), (64, "one", 9, 64, 1024, 520), (70, "some", 7, 24, 200, 33), (3, "200", 4, 32, 520, 96),
           (9, "90", 5, 128, 1032, 257), (2, "700", 2, 16, 96, 1000), (4, "130", 3, 56, 8, 5), (300, "one", 20, 16, 512, 64), (1, "4000", 1, 40, 256, 128),
+          (7, "one", 4, 104, 264, 77), (20, "some", 6, 48, 1160, 161), (6, "20", 3, 120, 136, 1001),
           # many rows to a sequence and rank enough for the kernel that takes 128 at a time
           (3, "2500", 4, 32, 520, 96), (9, "400", 5, 128, 1032, 257), (2, "6000", 2, 16, 96, 1000), (4, "900", 3, 56, 8, 5), (5, "300", 2, 72, 200, 64)]
 
