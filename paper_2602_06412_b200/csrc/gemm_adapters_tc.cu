@@ -302,6 +302,9 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(t_ready);
+    // The loop below has barriers of these four warps, and each came here by a wait of its own, which may have run out for some of them only:
+    // all enter it, or none.  From here on `ok` is the same in all four at every turn.
+    ok = epilogue_warps_agree(ok);
 
     const bool whole = wide && rows == 128, issues = threadIdx.x == 0, bulk = sizeof(CT) == 4 && wide;
     auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
