@@ -77,7 +77,6 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
   griddep_wait();
-  griddep_launch();
   uint32_t ctas;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
   const int CL = (int)ctas, cta = (int)cluster_ctarank();
@@ -112,6 +111,9 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  // Only now may the next kernel start beside this one: one that took the tensor memory that this CTA is still to get, and then waited for this grid
+  // to end, would leave both waiting.
+  griddep_launch();
   bool ok = true;
 
   if (warp == AT_COPY) {

@@ -29,3 +29,10 @@ def test_epilogue_warps_of_the_adapters_enter_their_loop_together():
     assert not re.search(r"\bok =(?! epilogue_warps_agree)", between[between.index("epilogue_warps_agree"):]), "and its result stays agreed on"
     turn = body[loop:]
     assert turn.index("ok = epilogue_warps_agree(ok);") < turn.index("if (!ok) break;")
+
+
+def test_adapters_hold_their_tensor_memory_before_the_next_kernel_may_start():
+    """A kernel launched early may take tensor memory in its first instructions and then wait for this grid's end: if a CTA of this grid had
+    still to get its own, neither would go on."""
+    body = _kernel("gemm_adapters_tc.cu", "gemm_adapters_tc_kernel")
+    assert body.index("griddep_wait()") < body.index("tc_alloc(") < body.index("griddep_launch()") and body.count("griddep_launch()") == 1
