@@ -8,7 +8,7 @@
 // memory in 16- and 8-byte loads, since any order of k serves as long as both operands keep it.
 //
 // x and the weights are bf16, so the first product's terms are exact and summed in fp32.  t scale stays an fp32 number: it enters
-// the second product as two bf16 terms (17 bits) for a bf16 C, three (all 24) for an fp32 C.
+// the second product as three bf16 terms, all of its 24 bits.
 //
 // Bounded by latency for one row (6.4 us in a graph, K = n_out = 4096, rank 16: finding the sequence 1.2, each product about 1, joining t 1.2 us) and by
 // round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 29 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
@@ -53,7 +53,7 @@ template <int NT, typename CT> struct AdapterTile {
   static constexpr bool FP32 = sizeof(CT) == 4;
   static constexpr int AHEAD = NT > 4 ? 1 : NT == 4 ? (FP32 ? 1 : 2) : (FP32 ? 2 : 3);
   static constexpr int CTAS = NT <= 8 ? 2 : 1;
-  static constexpr int ROWS = 16, KS = AD_WARPS, TERMS = sizeof(CT) == 2 ? 2 : 3;
+  static constexpr int ROWS = 16, KS = AD_WARPS, TERMS = 3;
   static constexpr int TP = 8 * NT + 4;                               // pitch of t in floats: rows 4 banks apart
   // ranks to a load of weights: a quad's four lanes take 32 or 64 bytes of a feature, which costs the L1 half as many lines (64 ranks 35 -> 29 us)
   static constexpr int WK = NT <= 2 ? 16 : 32;
@@ -166,6 +166,11 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
   constexpr int LK = WK / 4;                          // ranks to a lane
   using Word = std::conditional_t<LK == 8, uint4, uint2>;
   const bf16* mine = terms + g * SP + LK * t;
+  // Up to 8 rows leave the lower half of the matrix instruction's 16 empty: it takes the rows' middle terms beside the first ones, which are added to those
+  // behind the products.  So the third term costs those tiles no instruction (64 x 1 rows of rank 64, bf16 C: 29 us, by
+  // three instructions for every tile 33; fp32 C: 29 and 33).
+  const bool half = rows <= 8;
+  const int lower = half ? ROWS * SP : 8 * SP;
   CT* const row_a = c + (row0 + ra) * a.c_stride + 8 * t;
   CT* const row_b = c + (row0 + rb) * a.c_stride + 8 * t;
   constexpr int WORDS = sizeof(CT) / 2;
@@ -236,8 +241,9 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
         }
 #pragma unroll
         for (int m = TERMS - 1; m >= 0; --m) {       // the small terms first
+          if (m == 1 && half) continue;
           const Word u = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + WK * s);
-          const Word v = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + 8 * SP + WK * s);
+          const Word v = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + (m == 0 ? lower : 8 * SP) + WK * s);
 #pragma unroll
           for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, x[j].x, x[j].y);
           if constexpr (LK == 8)
@@ -246,6 +252,12 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
         }
         if (next < fg1) load_w(next, x, s);
       }
+      if (half)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          d[j][0] += d[j][2];
+          d[j][1] += d[j][3];
+        }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         if ((h ? rb : ra) < rows) {

@@ -2,7 +2,7 @@
 //
 // A cluster of CL CTAs takes 128 rows of one sequence.  Each CTA multiplies its share of K,  t = x A_a^T  (128 x rank, accumulated in tensor
 // memory; x and A_a by TMA in 64 k at a time); the shares meet through distributed shared memory in a fixed order; t scale becomes the
-// tensor-memory operand of the second product as two (fp32 C: three) bf16 terms, 17 (24) bits of it; and each CTA adds  t B_a^T  to its share
+// tensor-memory operand of the second product as three bf16 terms, all 24 bits of it; and each CTA adds  t B_a^T  to its share
 // of the features, 64 at a time, C read ahead into registers while they are multiplied.
 //
 // Bound by x once and C twice (rank operations per byte are few for the tensor cores).  In a graph, K = n_out = 4096: 9216 rows of 8 ragged sequences, rank
@@ -19,7 +19,7 @@ constexpr int AT_X = 128 * 128, AT_W = 64 * 128;                          // byt
 
 // NH: halves of 64 ranks
 template <typename CT, int NH> struct AtPlan {
-  static constexpr int TERMS = sizeof(CT) == 2 ? 2 : 3;
+  static constexpr int TERMS = 3;
   static constexpr int SLOT = AT_X + NH * AT_W;
   static constexpr int PITCH = 68;                                        // floats of a staged row: 16-byte accesses of 8 rows miss one another's banks
   static constexpr int STAGE = 128 * PITCH * 4;

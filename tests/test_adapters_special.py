@@ -38,3 +38,20 @@ def test_followed_by_kernels_that_take_tensor_memory(rank, rows):
             f()
     torch.cuda.synchronize()
     assert all(torch.equal(t, w) for t, w in zip((c, few, plain), want)) and status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cap", [(1, 1), (8, 8), (9, 9), (40, 40), (300, 4000)])
+def test_t_keeps_24_bits(dtype, rows, cap):
+    """t of 21 bits in three places that two bf16 numbers do not hold; the second product cancels all but the last of them, exactly."""
+    a, b = torch.zeros(1, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 40, 16, dtype=torch.bfloat16)
+    a[0, 0, :3], a[0, 1, :2] = torch.tensor([1024.0, 32.0, 1.0]), torch.tensor([1024.0, 32.0])
+    b[0, :, 0], b[0, :, 1] = 1.0, -1.0
+    x = torch.zeros(cap, 64, dtype=torch.bfloat16)
+    x[:, :3] = torch.tensor([1024.0, 32.0, 1.0])               # t = 2^20 + 2^10 + 1 and 2^20 + 2^10
+    x[::2, 2] = -3.0
+    c = torch.zeros(cap, 40, dtype=dtype, device=DEV)
+    SL.surelock_gemm_adapters(x.to(DEV), SL.Adapters(a.to(DEV), b.to(DEV), torch.ones(1, device=DEV)), _i32([0]), _i32([0, rows]), c)
+    want = torch.zeros(cap, 40)
+    want[:rows] = x[:rows, 2:3].float()
+    assert torch.equal(c.cpu().float(), want)
