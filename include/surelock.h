@@ -601,7 +601,8 @@ typedef struct {
  * may be a part of a wider row.  row_offsets dev int32 [B + 1], ascending, clamped to 0 ... max_rows (device status 4, as for an adapter or a
  * rank out of range; such an adapter is none).  Rows of no sequence are left as they are.  K and max_rank multiples of 8, max_rank <= 128,
  * x, a, b 16-byte aligned (SL_EUNSUPPORTED otherwise); any n_out, c_stride and alignment of C to its elements.  A_a x is summed in fp32 and
- * enters the second product as an fp32 number; C is rounded once (fp32 sums below 2^-126 may become 0).
+ * enters the second product as an fp32 number; C is rounded once (fp32 sums below 2^-126 may become 0).  Infinities and NaN in x, a and b go through
+ * the sums as they do in fp32 (in b: where |scale A_a x| is 0 or at least 2^-108; below, an infinity may become NaN).
  * dev_status may be NULL; 2 = a bounded wait ran out, and the rows that this concerns are NaN.  Deterministic; no workspace; one launch;
  * asynchronous on `stream`. */
 int surelock_gemm_adapters(const void *x, const surelock_adapters *adapters, const int32_t *adapter_of_seq, const int32_t *row_offsets, int B,

@@ -36,24 +36,13 @@ __device__ __forceinline__ uint32_t only(uint32_t two, int k, int rank) {
   return k >= rank ? 0u : k + 1 >= rank ? two & 0xffffu : two;
 }
 
-// the k-th term of v as a sum of bf16 numbers
-template <int TERMS> __device__ __forceinline__ void bf16_terms(float v, bf16* to, int pitch) {
-#pragma unroll
-  for (int i = 0; i < TERMS; ++i) {
-    const bf16 h = __float2bfloat16_rn(v);
-    to[i * pitch] = h;
-    const float left = v - __bfloat162float(h);
-    v = isfinite(left) ? left : 0.f;                 // an infinity is its own only term
-  }
-}
-
 template <int NT, typename CT> struct AdapterTile {
   // times 32 features of weights and C in registers: as many as leave 128 registers to a thread and so two CTAs to an SM.  64 rows, n_out = 12288, with
   // one CTA: rank 32 33 instead of 20.5 us, fp32 C 37 instead of 22.5, rank 16 with fp32 C 25 instead of 16.5.  More than 64 ranks take 252 registers.
   static constexpr bool FP32 = sizeof(CT) == 4;
   static constexpr int AHEAD = NT > 4 ? 1 : NT == 4 ? (FP32 ? 1 : 2) : (FP32 ? 2 : 3);
   static constexpr int CTAS = NT <= 8 ? 2 : 1;
-  static constexpr int ROWS = 16, KS = AD_WARPS, TERMS = 3;
+  static constexpr int ROWS = 16, KS = AD_WARPS;
   static constexpr int TP = 8 * NT + 4;                               // pitch of t in floats: rows 4 banks apart
   // ranks to a load of weights: a quad's four lanes take 32 or 64 bytes of a feature, which costs the L1 half as many lines (64 ranks 35 -> 29 us)
   static constexpr int WK = NT <= 2 ? 16 : 32;
@@ -64,7 +53,7 @@ template <int NT, typename CT> struct AdapterTile {
 template <int NT, typename CT>
 __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_adapters_kernel(AdapterArgs a) {
   using L = AdapterTile<NT, CT>;
-  constexpr int ROWS = L::ROWS, KS = L::KS, TERMS = L::TERMS, TP = L::TP, SP = L::SP, WK = L::WK, KS2 = (8 * NT + WK - 1) / WK;
+  constexpr int ROWS = L::ROWS, KS = L::KS, TP = L::TP, SP = L::SP, WK = L::WK, KS2 = (8 * NT + WK - 1) / WK;
   extern __shared__ __align__(16) unsigned char smem[];
   float* part = reinterpret_cast<float*>(smem);
   bf16* terms = reinterpret_cast<bf16*>(smem + L::T_BYTES);
@@ -78,6 +67,10 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
   if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const bf16* wa = a.a + (long long)ad * a.max_rank * a.K;
   const bf16* wb = a.b + (long long)ad * a.n_out * a.max_rank;
+  // Up to 8 rows leave the lower half of the matrix instruction's 16 empty: it takes the rows' middle terms beside the first ones, and half of the last one
+  // beside the other half; what comes of it is added to the upper half's.  So the third term costs those tiles no instruction (64 x 1 rows of rank 64, bf16
+  // C: 29 us, by three instructions for every tile 33; fp32 C: 29 and 33).
+  const bool half = rows <= 8;
   const int fgs = (a.n_out + 31) >> 5, fg0 = (int)((long long)fgs * rank_cta / CL), fg1 = (int)((long long)fgs * (rank_cta + 1) / CL);
 
   // ---- t = A_a x over this warp's k
@@ -152,7 +145,9 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
         for (int c = 0; c < AD_CLUSTER; ++c) v += w[c];
         v *= scale;
       }
-      bf16_terms<TERMS>(v, terms + r * SP + j, ROWS * SP);
+#pragma unroll
+      for (int m = 0; m < TERMS; ++m)
+        terms[m * ROWS * SP + r * SP + j] = __ushort_as_bfloat16((unsigned short)((m + 1 < TERMS ? next_term(v) : last_term(half ? 0.5f * v : v)) >> 16));
     }
   }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the others' t
@@ -166,11 +161,6 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
   constexpr int LK = WK / 4;                          // ranks to a lane
   using Word = std::conditional_t<LK == 8, uint4, uint2>;
   const bf16* mine = terms + g * SP + LK * t;
-  // Up to 8 rows leave the lower half of the matrix instruction's 16 empty: it takes the rows' middle terms beside the first ones, which are added to those
-  // behind the products.  So the third term costs those tiles no instruction (64 x 1 rows of rank 64, bf16 C: 29 us, by
-  // three instructions for every tile 33; fp32 C: 29 and 33).
-  const bool half = rows <= 8;
-  const int lower = half ? ROWS * SP : 8 * SP;
   CT* const row_a = c + (row0 + ra) * a.c_stride + 8 * t;
   CT* const row_b = c + (row0 + rb) * a.c_stride + 8 * t;
   constexpr int WORDS = sizeof(CT) / 2;
@@ -243,7 +233,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
         for (int m = TERMS - 1; m >= 0; --m) {       // the small terms first
           if (m == 1 && half) continue;
           const Word u = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + WK * s);
-          const Word v = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + (m == 0 ? lower : 8 * SP) + WK * s);
+          const Word v = *reinterpret_cast<const Word*>(mine + m * ROWS * SP + (!half ? 8 * SP : m == 0 ? ROWS * SP : 0) + WK * s);
 #pragma unroll
           for (int j = 0; j < 4; ++j) mma_16816(d[j], u.x, v.x, u.y, v.y, x[j].x, x[j].y);
           if constexpr (LK == 8)

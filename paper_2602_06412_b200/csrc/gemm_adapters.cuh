@@ -67,6 +67,21 @@ __device__ __forceinline__ bool find_rank(const AdapterArgs& a, int ad, int& ran
   return rank > 0;
 }
 
+// t enters the second product as a sum of TERMS bf16 numbers.  next_term gives the first of what is left of v and takes it away: the upper 8 bits or, where
+// these are all of it, its half; last_term the rest.  So the terms of a number have its sign and none is zero: with an infinite weight their products have one
+// sign too, and sum up to the infinity that the number's product is (a term of zero, or of the other sign, would make it NaN); and no term of a
+// number next to the end of fp32 is rounded to an infinity.  Their last bit is a quarter of the number's own last bit at least (an
+// eighth, where the last term is halved once more), so sums that fp32 holds with three bits to spare stay exact.  The three are v itself where |v| >= 2^-108,
+// and off by 2^-132 below.  Zero gives zeros, an infinity or a NaN itself.
+constexpr int TERMS = 3;
+__device__ __forceinline__ uint32_t next_term(float& v) {        // in the word's upper half
+  float a = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  if (a == v) a = 0.5f * v;
+  v = isinf(v) ? v : v - a;
+  return __float_as_uint(a);
+}
+__device__ __forceinline__ uint32_t last_term(float v) { return __float_as_uint(v); }
+
 int launch_gemm_adapters_tc(const AdapterArgs& a, int dtype, cudaStream_t st);
 
 }  // namespace sl

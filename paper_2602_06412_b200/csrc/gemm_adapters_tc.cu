@@ -19,7 +19,6 @@ constexpr int AT_X = 128 * 128, AT_W = 64 * 128;                          // byt
 
 // NH: halves of 64 ranks
 template <typename CT, int NH> struct AtPlan {
-  static constexpr int TERMS = 3;
   static constexpr int SLOT = AT_X + NH * AT_W;
   static constexpr int PITCH = 68;                                        // floats of a staged row: 16-byte accesses of 8 rows miss one another's banks
   static constexpr int STAGE = 128 * PITCH * 4;
@@ -192,7 +191,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
       if (one_lane()) {
         bool more = false;
 #pragma unroll
-        for (int m = P::TERMS - 1; m >= 0; --m)      // the small terms first
+        for (int m = TERMS - 1; m >= 0; --m)      // the small terms first
           for (int s = 0; s < steps; ++s) {          // 16 ranks: 8 columns of the operand, 32 bytes of the weights' rows
             at_mma(d, base + m * P::T_COLS + 8 * s, smem_desc_k_sw128(at + (s >> 2) * AT_W + (s & 3) * 32), later, more);
             more = true;
@@ -287,15 +286,15 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
 #pragma unroll
       for (int k = 0; k < 64; ++k) v[k] = 64 * h + k < rank ? __float_as_uint(__uint_as_float(v[k]) * scale) : 0u;
 #pragma unroll
-      for (int m = 0; m < P::TERMS; ++m) {
+      for (int m = 0; m < TERMS; ++m) {
         uint32_t w[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          const float x = __uint_as_float(v[2 * k]), y = __uint_as_float(v[2 * k + 1]);
-          w[k] = pack_bf16(x, y);
-          const float dx = x - __uint_as_float(w[k] << 16), dy = y - __uint_as_float(w[k] & 0xffff0000u);
-          v[2 * k] = isfinite(dx) ? __float_as_uint(dx) : 0u;              // an infinity is its own only term
-          v[2 * k + 1] = isfinite(dy) ? __float_as_uint(dy) : 0u;
+          float x = __uint_as_float(v[2 * k]), y = __uint_as_float(v[2 * k + 1]);
+          const uint32_t a0 = m + 1 < TERMS ? next_term(x) : last_term(x), a1 = m + 1 < TERMS ? next_term(y) : last_term(y);
+          w[k] = __byte_perm(a0, a1, 0x7632);
+          v[2 * k] = __float_as_uint(x);
+          v[2 * k + 1] = __float_as_uint(y);
         }
         tc_st32(mine + m * P::T_COLS + 32 * h, w);
       }

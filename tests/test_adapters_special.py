@@ -55,3 +55,41 @@ def test_t_keeps_24_bits(dtype, rows, cap):
     want = torch.zeros(cap, 40)
     want[:rows] = x[:rows, 2:3].float()
     assert torch.equal(c.cpu().float(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rank,rows,cap", [(16, 1, 1), (64, 7, 7), (24, 13, 13), (128, 40, 40), (16, 300, 3100), (72, 300, 700), (128, 200, 400)])
+def test_infinite_weights(dtype, rank, rows, cap):
+    """Infinities in b, where t is a whole number that one bf16 number holds, one that takes two, and none (zero): infinity or NaN as the
+    definition has it, and finite results beside them exact."""
+    g = torch.Generator().manual_seed(rank)
+    a, b, scale = ad._make(1, rank, 128, 80, 24, exact=True)
+    scale[0] = -2.0
+    x = torch.randint(-2, 3, (cap, 128), generator=g).to(torch.bfloat16)
+    x[:, 0], a[0, :, 0] = 64.0, torch.tensor([256.0, 0.0, -256.0, 128.0] * rank)[:rank].to(torch.bfloat16)
+    a[0, 4] = 0.0                                              # this t is zero
+    for f, j, v in [(3, 0, "inf"), (5, 1, "-inf"), (9, 2, "inf"), (9, 3, "inf"), (20, 4, "inf"), (33, 7, "-inf"), (64, rank - 1, "inf"), (79, 0, "nan"), (78, 6, "-inf")]:
+        b[0, f, j] = float(v)
+    c0 = torch.randint(-9, 10, (cap, 80), generator=g).to(dtype)
+    c = c0.to(DEV)
+    SL.surelock_gemm_adapters(x.to(DEV), SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV)), _i32([0]), _i32([0, rows]), c)
+    with np.errstate(invalid="ignore"):
+        t = x[:rows].double().numpy() @ a[0].double().numpy().T
+        want = c0.double().numpy()
+        want[:rows] += (scale[0].item() * t[:, None, :] * b[0].double().numpy()[None]).sum(2)
+        size = np.abs(2 * t[:, None, :] * b[0].double().numpy()[None]).sum(2)
+    assert size[np.isfinite(size)].max() < 2 ** (21 if rows < 9 else 22) and np.isinf(want).any() and np.isnan(want).any()     # 3 and 2 bits to spare
+    assert np.array_equal(c.cpu().double().numpy(), torch.from_numpy(want).to(dtype).double().numpy(), equal_nan=True)
+
+
+@pytest.mark.parametrize("rows,cap", [(2, 2), (12, 12), (300, 3100)])
+def test_t_next_to_the_end_of_its_type(rows, cap):
+    """t = 2^128 - 2^116: an fp32 number that no bf16 number is near without being infinite."""
+    a, b = torch.zeros(1, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 24, 16, dtype=torch.bfloat16)
+    a[0, 0, :12] = 2.0 ** 100
+    b[0, :, 0] = 2.0 ** -100
+    x = torch.zeros(cap, 64, dtype=torch.bfloat16)
+    x[:, :12] = torch.exp2(torch.arange(27, 15, -1).float())
+    c = torch.zeros(cap, 24, device=DEV)
+    SL.surelock_gemm_adapters(x.to(DEV), SL.Adapters(a.to(DEV), b.to(DEV), torch.tensor([-1.0], device=DEV)), _i32([0]), _i32([0, rows]), c)
+    assert bool((c[:rows] == -(2.0 ** 28 - 2.0 ** 16)).all()) and not bool(c[rows:].any())
