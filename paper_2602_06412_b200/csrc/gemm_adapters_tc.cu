@@ -24,12 +24,13 @@ template <typename CT, int NH> struct AtPlan {
   static constexpr int STAGE = 128 * PITCH * 4;
   static constexpr int BARS = 3 * AT_STAGES + 6;
   static constexpr int SMEM = 1024 + AT_STAGES * SLOT + STAGE + BARS * 8 + 16;
-  // Tensor memory: terms of t (16 bits a number), then two accumulators of 64 features.  t itself is accumulated in ACC places, which take the
-  // blocks of k in turn and are added up in fp32 behind the products: a matrix instruction cuts off where an addition rounds, and one chain of
-  // 85 of them left 8.9e-7 in a result where four chains leave 1.9e-7.  With one half of ranks they may lie where the terms come to.
-  static constexpr uint32_t T_COLS = 32 * NH, D_COL = TERMS * T_COLS, COLS = NH == 1 ? 256 : 512, ACC_COL = NH == 1 ? 0 : D_COL;
-  static constexpr int ACC = (COLS - ACC_COL) / (64 * NH);
-  static_assert(D_COL + 128 <= COLS, "tensor memory");
+  // Tensor memory: terms of t (16 bits a number), then two accumulators of 64 features.  t itself is accumulated in ACC places from the first column on,
+  // which take the blocks of k in turn and are added up in fp32 behind the products: a matrix instruction cuts off where an addition rounds, and one chain
+  // of 85 of them left 8.9e-7 in a result where four chains leave 1.9e-7.  The terms come to lie where sums were that have been read: with two halves of
+  // ranks, the second's sums wait in the last place meanwhile.
+  static constexpr uint32_t T_COLS = 32 * NH, D_COL = TERMS * T_COLS, COLS = NH == 1 ? 256 : 512, KEPT_COL = COLS - 64;
+  static constexpr int ACC = COLS / (64 * NH);
+  static_assert(ACC == 4 && D_COL + 128 <= COLS && (NH == 1 || D_COL <= KEPT_COL), "tensor memory");
   static constexpr int CTAS = COLS == 256 && 2 * (SMEM + 1024) <= 227 * 1024 ? 2 : 1;
 };
 
@@ -158,7 +159,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
       if (one_lane()) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          tc_mma_bf16(base + P::ACC_COL + i % P::ACC * (64 * NH), smem_desc_k_sw128(at + 32 * k), smem_desc_k_sw128(at + AT_X + 32 * k), first,
+          tc_mma_bf16(base + i % P::ACC * (64 * NH), smem_desc_k_sw128(at + 32 * k), smem_desc_k_sw128(at + AT_X + 32 * k), first,
                       i >= P::ACC || k > 0);
         tc_commit(empty(i));
         if (i == n1 - 1) tc_commit(t_done);
@@ -214,21 +215,36 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
     const float scale = a.scale[ad];
     ok = __all_sync(0xffffffffu, mbar_wait(t_done, 0, s_abort));
     tc_fence_after();
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      uint32_t v[64];
-      tc_ld32(mine + P::ACC_COL + 64 * h, v);        // what is behind the ranks of the product is not used
-      tc_ld32(mine + P::ACC_COL + 64 * h + 32, v + 32);
+    auto sum = [&](int h, uint32_t* v) {               // a half of the ranks; what is behind the ranks of the product is not used
+      tc_ld32(mine + 64 * h, v);
+      tc_ld32(mine + 64 * h + 32, v + 32);
       tc_wait_ld();
       for (int c = 1; c < min(P::ACC, n1); ++c)
 #pragma unroll
         for (int k = 0; k < 64; k += 32) {
           uint32_t u[32];
-          tc_ld32(mine + P::ACC_COL + 64 * NH * c + 64 * h + k, u);
+          tc_ld32(mine + 64 * NH * c + 64 * h + k, u);
           tc_wait_ld();
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[k + e] = __float_as_uint(__uint_as_float(v[k + e]) + __uint_as_float(u[e]));
         }
+    };
+    if (NH == 2) {
+      uint32_t v[64];
+      sum(1, v);
+      tc_st32(mine + P::KEPT_COL, v);
+      tc_st32(mine + P::KEPT_COL + 32, v + 32);
+      tc_wait_st();
+    }
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      uint32_t v[64];
+      if (h == 0) sum(0, v);
+      else {
+        tc_ld32(mine + P::KEPT_COL, v);
+        tc_ld32(mine + P::KEPT_COL + 32, v + 32);
+        tc_wait_ld();
+      }
       if (!ok) {                                     // an incomplete sum is NaN, for whichever CTA uses it
 #pragma unroll
         for (int k = 0; k < 64; ++k) v[k] = 0x7fffffffu;

@@ -93,3 +93,19 @@ def test_t_next_to_the_end_of_its_type(rows, cap):
     c = torch.zeros(cap, 24, device=DEV)
     SL.surelock_gemm_adapters(x.to(DEV), SL.Adapters(a.to(DEV), b.to(DEV), torch.tensor([-1.0], device=DEV)), _i32([0]), _i32([0, rows]), c)
     assert bool((c[:rows] == -(2.0 ** 28 - 2.0 ** 16)).all()) and not bool(c[rows:].any())
+
+
+def test_ranks_above_64_are_summed_as_those_below():
+    """t = A x is accumulated in the same four places whatever the rank: b a unit matrix brings it out, and the first 64 ranks of 128 are, bit for
+    bit, those of an adapter that has only them.  Rows enough that one CTA takes a tile's whole K."""
+    rows, K = 3000 * 128, 512
+    g = torch.Generator(device=DEV).manual_seed(26)
+    x = torch.randn(rows, K, device=DEV, generator=g).to(torch.bfloat16)
+    a = torch.randn(1, 128, K, device=DEV, generator=g).to(torch.bfloat16)
+    out = []
+    for rank in (64, 128):
+        c = torch.zeros(rows, rank, device=DEV)
+        unit = torch.eye(rank, device=DEV).to(torch.bfloat16)[None].contiguous()
+        SL.surelock_gemm_adapters(x, SL.Adapters(a[:, :rank].contiguous(), unit, torch.ones(1, device=DEV)), _i32([0]), _i32([0, rows]), c)
+        out.append(c[:, :64])
+    assert torch.equal(*out) and out[0].any()
