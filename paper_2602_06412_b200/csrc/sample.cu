@@ -669,7 +669,9 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
     return 0u;
   }
   __device__ double largest_value() const { return (double)topf; }
-  __device__ unsigned long long weight(float x) const { return __double2ull_rn(exp_falling(((double)x - (double)topf) * inv_T, s.powers) * WEIGHT_UNIT); }
+  __device__ double weight_of(float x) const { return exp_falling(((double)x - (double)topf) * inv_T, s.powers); }
+  __device__ static unsigned long long units(double w) { return __double2ull_rn(w * WEIGHT_UNIT); }
+  __device__ unsigned long long weight(float x) const { return units(weight_of(x)); }
   // Falls with x; what is too far below the largest shares the last bin.
   __device__ uint32_t bin_of(float x) const { return min((uint32_t)BINS - 1, __float2uint_rz((topf - x) * step)); }
 
@@ -720,8 +722,8 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
     clear();
     row.each([&](float x) {
       if (x == -INFINITY) return;
-      const unsigned long long w = weight(x);
-      add(bin_of(x), w);
+      const double w = weight_of(x);
+      add(bin_of(x), units(w));
       also(x, w);
     });
     row_sync<CTAS>();
@@ -735,12 +737,11 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
     step = span > 0.f ? fminf((float)BINS / span, 3.4e38f) : 0.f;
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
-    bin_all(row, [&](float x, unsigned long long w) {
+    bin_all(row, [&](float x, double w) {
       if (inv_T != 1.0) raw += (double)expf(x - topf);
-      const double v = (double)w / WEIGHT_UNIT;
-      if (set.min_p > 0.0 && v >= set.min_p) {
+      if (set.min_p > 0.0 && w >= set.min_p) {           // the weight itself: in units of the sums a small one is no number to compare
         ++nm;
-        m += v;
+        m += (double)units(w) / WEIGHT_UNIT;
       }
     });
     this->put_rest(set, nm, m, raw);
@@ -773,7 +774,7 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
 
   __device__ Found find(const Share<T>& row, Ask ask) {
     if (!whole) {                                   // an earlier find has opened a bin
-      bin_all(row, [](float, unsigned long long) {});
+      bin_all(row, [](float, double) {});
       row_sync<CTAS>();
     }
     Found f = open(ask, 0u, 0.0);
