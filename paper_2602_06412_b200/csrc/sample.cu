@@ -553,7 +553,7 @@ template <int CTAS> struct WindowSums : Sums<CTAS> {
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
     auto account = [&](uint32_t c, double w, double cw, uint32_t e) {
-      if (inv_T != 1.0 && c) raw += (float)c * expf((float)((double)value(e) - top));
+      if (inv_T != 1.0 && c) raw += c * exp_falling(fmin((double)value(e) - top, 0.0), s.powers);
       if (set.min_p > 0.0 && w >= set.min_p) {
         nm += c;
         m += cw;
@@ -738,7 +738,7 @@ template <typename T, int CTAS> struct BinnedSums : Sums<CTAS> {
     uint32_t nm = 0u;
     double m = 0.0, raw = 0.0;
     bin_all(row, [&](float x, double w) {
-      if (inv_T != 1.0) raw += (double)expf(x - topf);
+      if (inv_T != 1.0) raw += exp_falling((double)x - (double)topf, s.powers);
       if (set.min_p > 0.0 && w >= set.min_p) {           // the weight itself: in units of the sums a small one is no number to compare
         ++nm;
         m += (double)units(w) / WEIGHT_UNIT;
