@@ -45,6 +45,14 @@ def selection_skip_mask(lock: torch.Tensor, mask_state: torch.Tensor, fraction: 
     return ((rank < n_skip) & eligible).to(torch.uint8)
 
 
+def _probability(out: SL.StepOut, drawn: torch.Tensor) -> torch.Tensor:
+    """softmax(logits[r])[drawn[r]] from the step's confidence, which is that of the argmax; NaN (never revealed) where nothing
+    was drawn.  Rows behind n_active give anything."""
+    last = out.logits.shape[1] - 1
+    at = lambda token: out.logits.gather(1, token.clamp(0, last).long()[:, None])[:, 0].float()
+    return torch.where(drawn < 0, float("nan"), out.conf * torch.exp(at(drawn) - at(out.argmax)))
+
+
 def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: int, block_len: int, steps: int,
         kl_eps: float, surelock: bool = True, unmask_per_step: int = 1, select_fraction: float = None,
         select_seed: int = 0, observer=None, unlock: Dict = None, sampling: Dict = None) -> Dict:
@@ -60,7 +68,8 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
     positions per step is in the result.
     `sampling`: a dict of temperature, top_k, top_p, min_p (those that are wanted) and seed makes the revealed tokens samples of
     the posterior instead of its argmax: `surelock_sample` draws a token for every row of a step from one uniform number, and
-    the positions whose drawn tokens are most probable (their softmax confidence, as before) are revealed.
+    the positions whose drawn tokens are most probable (their probability under the whole softmax, as before) are revealed.  The
+    mask token is no token to draw: the filters and the draw see the vocabulary without it.
     `observer`, when given, is called after every step, before the unmasking of line 16, as
     observer(t, out, lock_in, lock_out, tokens, mask_state) with lock_in a copy of the lock mask the step was given
     (skip mask included) and lock_out the mask after the step; it is for tests that look at a step from outside and
@@ -84,8 +93,7 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
         settings = SL.Sampling(value("temperature", torch.float32), value("top_k", torch.int32), value("top_p", torch.float32),
                                value("min_p", torch.float32))
         gen = torch.Generator(device=dev).manual_seed(int(sampling.get("seed", 0)))
-        u, drawn_conf = torch.empty(R, device=dev), torch.empty(R, device=dev)
-        drawn = torch.empty(R, dtype=torch.int32, device=dev)
+        u, drawn = torch.empty(R, device=dev), torch.zeros(R, dtype=torch.int32, device=dev)
     SL.surelock_reset(ctx)
     ev[0].record()
     for t in range(steps):
@@ -109,8 +117,8 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
         conf, token = out.conf, out.argmax
         if sampling is not None:
             u.uniform_(generator=gen)
-            SL.surelock_sample(out.logits, settings, u, out.n_active, drawn, drawn_conf)
-            conf, token = drawn_conf, drawn
+            SL.surelock_sample(out.logits[:, :mask_token], settings, u, out.n_active, drawn)   # the mask token is the last one
+            conf, token = _probability(out, drawn), drawn
         SL.surelock_update_mask(conf, token, out.active_idx, out.row_offsets, B, N, lo, hi, unmask_per_step,
                                 mask_token, tokens, mask_state, n_rev)
         unmasked_trace[t:t + 1] = n_rev.sum(dtype=torch.int32)
