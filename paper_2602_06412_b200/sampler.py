@@ -75,6 +75,9 @@ def run(ctx: SL.Ctx, tokens: torch.Tensor, mask_state: torch.Tensor, n_prompt: i
     (skip mask included) and lock_out the mask after the step; it is for tests that look at a step from outside and
     makes the loop wait for the GPU.
     Returns the trace and the paper's metrics."""
+    unknown = set(sampling or ()) - {"temperature", "top_k", "top_p", "min_p", "seed"}
+    if unknown:
+        raise SL.SurelockError(f"sampling: temperature, top_k, top_p, min_p and seed are known, got {sorted(unknown)}")
     B, N = tokens.shape
     dev = tokens.device
     R = B * N

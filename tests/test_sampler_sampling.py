@@ -50,6 +50,12 @@ def _replay(sampling, seed, mask_gain):
     return tokens[:, n_prompt:].cpu(), ran_into_mask
 
 
+@pytest.mark.parametrize("sampling", [dict(topk=4), dict(temperature=1.0, Seed=3)])
+def test_unknown_settings_are_refused(sampling):
+    with pytest.raises(SL.SurelockError, match="topk|Seed"):
+        sampler.run(None, torch.zeros(1, 8, dtype=torch.int32), torch.ones(1, 8, dtype=torch.uint8), 4, 4, 1, 1e-3, sampling=sampling)
+
+
 @gpu
 @pytest.mark.parametrize("sampling", [dict(temperature=0.0), dict(top_k=1), dict(temperature=1.0), dict(temperature=0.7, top_k=40, top_p=0.9)])
 @pytest.mark.parametrize("mask_gain", [1.0, 40.0])
