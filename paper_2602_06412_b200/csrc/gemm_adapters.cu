@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
   const int CL = (int)ctas, rank_cta = (int)cluster_ctarank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int ad, row0, rows, rank;
-  if (!find_tile(a, (int)(blockIdx.x / CL), ROWS, ad, row0, rows) || !find_rank(a, ad, rank)) return;
+  if (!find_tile(a, (int)(blockIdx.x / CL), (int)(gridDim.x / CL), ROWS, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const bf16* wa = a.a + (long long)ad * a.max_rank * a.K;
   const bf16* wb = a.b + (long long)ad * a.n_out * a.max_rank;
   // Up to 8 rows leave the lower half of the matrix instruction's 16 empty: it takes the rows' middle terms beside the first ones, and half of the last one

@@ -16,8 +16,8 @@ struct AdapterArgs {
   int lost;                         // bytes of a copy that is waited for and never made (a diagnostic), or 0
 };
 
-// The group-th tile of `tile` rows of one sequence: its adapter's number, first row and rows; every lane of a warp gets the same.
-__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int tile, int& ad, int& row0, int& rows) {
+// The group-th tile, of at most `groups`, of `tile` rows of one sequence: its adapter's number, first row and rows; every lane of a warp gets the same.
+__device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int groups, int tile, int& ad, int& row0, int& rows) {
   const int lane = threadIdx.x & 31;
   int before = 0;                                    // tiles of the sequences before this round's 32
   bool bad = false;
@@ -43,6 +43,8 @@ __device__ __forceinline__ bool find_tile(const AdapterArgs& a, int group, int t
       ad = __shfl_sync(0xffffffffu, its, l);
       row0 = __shfl_sync(0xffffffffu, from, l) + first * tile;
       rows = min(tile, __shfl_sync(0xffffffffu, to, l) - row0);
+      if (group + 1 == groups)                       // nobody else looks at the offsets behind these
+        for (int i = b0 + 32 + lane; i < a.B; i += 32) bad |= a.row_offsets[i] < 0 || a.row_offsets[i + 1] < a.row_offsets[i] || a.row_offsets[i + 1] > a.max_rows;
       if (bad) set_status(a.status, SL_DEV_BAD_INDEX);
       return true;
     }

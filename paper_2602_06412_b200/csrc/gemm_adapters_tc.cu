@@ -82,7 +82,7 @@ gemm_adapters_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_co
   const int CL = (int)ctas, cta = (int)cluster_ctarank();
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   int row0, rows, ad, rank;                          // the same in the whole cluster
-  if (!find_tile(a, (int)(blockIdx.x / CL), 128, ad, row0, rows) || !find_rank(a, ad, rank)) return;
+  if (!find_tile(a, (int)(blockIdx.x / CL), (int)(gridDim.x / CL), 128, ad, row0, rows) || !find_rank(a, ad, rank)) return;
   const int ranks = (a.max_rank + 15) & ~15;         // rows of A_a in a copy: a whole number of 16
   constexpr int VEC = 16 / sizeof(CT);
   // C may be copied in tiles: a copy writes whole 16 bytes, also where the row ends inside them

@@ -109,3 +109,16 @@ def test_ranks_above_64_are_summed_as_those_below():
         SL.surelock_gemm_adapters(x, SL.Adapters(a[:, :rank].contiguous(), unit, torch.ones(1, device=DEV)), _i32([0]), _i32([0, rows]), c)
         out.append(c[:, :64])
     assert torch.equal(*out) and out[0].any()
+
+
+@pytest.mark.parametrize("offs", [[0] + [1] * 39 + [7], [0] + [2] * 33 + [1] * 7, [0, 1] + [2] * 99 + [-4]])
+def test_bad_offsets_behind_the_last_row_are_reported(offs):
+    """Every row has its sequence already; the offsets of the many behind them are looked at all the same."""
+    a, b, scale = ad._make(2, 16, 64, 32, 27)
+    M = max(offs[:2] + offs[2:3])
+    x, c0, status = torch.randn(M, 64).to(torch.bfloat16).to(DEV), torch.randn(M, 32, device=DEV), _i32([0])
+    SL.surelock_gemm_adapters(x, SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV)), _i32([0] * (len(offs) - 1)), _i32(offs), c0, status)
+    assert status.item() == 4
+    good, status = [min(max(o, 0), M) for o in np.maximum.accumulate(offs).tolist()], _i32([0])
+    SL.surelock_gemm_adapters(x, SL.Adapters(a.to(DEV), b.to(DEV), scale.to(DEV)), _i32([0] * (len(offs) - 1)), _i32(good), c0, status)
+    assert status.item() == 0
