@@ -559,7 +559,8 @@ typedef struct {
  *   SL_ROPE_LINEAR  divided by f (positions are interpolated)
  *   SL_ROPE_NTK     theta replaced by theta f^(D/(D-2))
  *   SL_ROPE_YARN    divided by f for pairs from `high` on, kept up to `low`, a line in between, where low (high) is the floor (ceiling) of
- *                   the pair that makes `fast` (`slow`) turns over L tokens; scale = attn_scale, or 0.1 ln f + 1 where that is 0
+ *                   the pair that makes `fast` (`slow`) turns over L tokens, both within 0 ... D - 1; scale = attn_scale, or where that
+ *                   is 0 0.1 ln f + 1 (1 for f below 1)
  *   SL_ROPE_BANDS   kept where L tokens make at least `fast` turns, divided by f at most `slow`, a line in the number of turns in between
  */
 enum { SL_ROPE_PLAIN = 0, SL_ROPE_LINEAR = 1, SL_ROPE_NTK = 2, SL_ROPE_YARN = 3, SL_ROPE_BANDS = 4 };
