@@ -632,7 +632,7 @@ typedef struct {
  *              confidence that surelock_update_mask orders by;  n_kept dev int32 [M] or NULL: the length of the prefix
  * A row with a NaN or +inf, with nothing but -inf, or with an undefined setting gives token -1, conf NaN, n_kept 0; so does a set out
  * of range (device status 4).  Sums are held in 64 bits: the result does not depend on how rows are split, up to 2^-50 of the sum.
- * vocab < 2^20 - 128 (SL_EUNSUPPORTED otherwise), any row_stride >= vocab.  Deterministic; no workspace; one launch;
+ * vocab <= 2^20 - 128 (SL_EUNSUPPORTED otherwise), any row_stride >= vocab.  Deterministic; no workspace; one launch;
  * asynchronous on `stream`. */
 int surelock_sample(const void *logits, int64_t row_stride, const surelock_sampling *sampling, const int32_t *set_of_row, const float *u,
                     const int32_t *n_active, int max_rows, int vocab, int dtype, int32_t *token, float *conf, int32_t *n_kept,

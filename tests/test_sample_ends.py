@@ -1,10 +1,13 @@
 """Sampling at the ends of its settings, against the definition in 64 bits."""
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2602_06412_b200 import binding as SL
+from paper_2602_06412_b200 import build as build_mod
 
 from .test_sample import DEV, _check, _run
 
@@ -45,3 +48,21 @@ def test_conf_is_a_quotient_in_64_bits(dtype, M, V, far):
         z -= z.max(axis=1, keepdims=True)
         want = np.exp(z[np.arange(M), tokens]) / np.exp(z).sum(axis=1)
         assert np.all(np.abs(conf.astype(np.float64) - want) <= (2.0 ** -24 + 2.0 ** -35) * want)
+
+
+def test_a_vocabulary_too_large_is_refused_on_the_host():
+    build_mod.build()
+    sets = ctypes.byref(SL._Sampling(None, None, None, None, 1))
+    V = (1 << 20) - 127
+    assert SL.lib().surelock_sample(0x100, V, sets, None, 0x200, 0x300, 5, V, SL.SL_BF16, 0x400, 0x500, 0x600, None, None) == -5
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_largest_vocabulary(dtype):
+    V = (1 << 20) - 128
+    g = torch.Generator().manual_seed(28)
+    x = torch.randn(2, V, generator=g)
+    x[1] = 0.0                                                 # as many tokens as there are in one bin
+    for T, k, p in ((1.0, 0, 1.0), (3.0, V - 1, 0.999)):
+        _check(x.to(dtype).to(DEV), [0.999, 0.9999], T=T, k=k, p=p)
