@@ -666,6 +666,12 @@ def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free
     table, lens, new, lens_out, free, n, M, n_out, offsets, idx, status = _ptrs(
         dev, torch.int32, page_table, B * width, seq_lens, B, new_tokens, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1,
         n_free, 1, n_active, 1, n_free if n_free_out is None else n_free_out, 1, row_offsets, B + 1, active_idx, 0, dev_status, 1)
+    if B == 0:                                         # nobody to serve: no rows, and the list stays as it is
+        row_offsets[:1].zero_()
+        n_active[:1].zero_()
+        if n_free_out is not None:
+            n_free_out[:1].copy_(n_free[:1])
+        return
     _check(lib().surelock_paged_extend(table, B, page_size, width, n_pages, lens, new, free, n, offsets, idx, M, rows, lens_out, n_out, status,
                                        stream), "surelock_paged_extend")
 
@@ -680,6 +686,10 @@ def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pag
     table, lens, kept, lens_out, free, n, n_out, status = _ptrs(
         dev, torch.int32, page_table, B * width, seq_lens, B, keep, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1, n_free, 1,
         n_free if n_free_out is None else n_free_out, 1, dev_status, 1)
+    if B == 0:
+        if n_free_out is not None:
+            n_free_out[:1].copy_(n_free[:1])
+        return
     _check(lib().surelock_paged_truncate(table, B, page_size, width, n_pages, lens, kept, free, n, lens_out, n_out, status, stream),
            "surelock_paged_truncate")
 
