@@ -655,16 +655,17 @@ def _table(t: torch.Tensor):
 
 
 def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free_pages, n_free, row_offsets, active_idx, n_active,
-                          seq_lens_out=None, n_free_out=None, dev_status=None):
+                          seq_lens_out=None, n_free_out=None, dev_status=None, n_pages=None):
     """Pages off the free list, row offsets and flat positions (N = max_pages * page_size) for new_tokens[b] more tokens of every
     sequence; seq_lens and n_free are updated in place unless seq_lens_out, n_free_out are given.  All int32 CUDA tensors:
-    page_table [B][max_pages], seq_lens, new_tokens [B], free_pages [n_pages], n_free, n_active [1], row_offsets [B+1], active_idx [rows]."""
+    page_table [B][max_pages], seq_lens, new_tokens [B], free_pages [n_pages], n_free, n_active [1], row_offsets [B+1], active_idx [rows].
+    n_pages: the pages of the pool, for each of which the list has a place; all places of free_pages unless it is given."""
     dev = page_table.get_device()
     stream = _stream_of(dev)
     B, width = _table(page_table)
-    rows, n_pages = active_idx.numel(), free_pages.numel()
+    rows, n_pages = active_idx.numel(), free_pages.numel() if n_pages is None else n_pages
     table, lens, new, lens_out, free, n, M, n_out, offsets, idx, status = _ptrs(
-        dev, torch.int32, page_table, B * width, seq_lens, B, new_tokens, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1,
+        dev, torch.int32, page_table, B * width, seq_lens, B, new_tokens, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, max(n_pages, 1),
         n_free, 1, n_active, 1, n_free if n_free_out is None else n_free_out, 1, row_offsets, B + 1, active_idx, 0, dev_status, 1)
     if B == 0:                                         # nobody to serve: no rows, and the list stays as it is
         row_offsets[:1].zero_()
@@ -677,14 +678,15 @@ def surelock_paged_extend(page_table, page_size: int, seq_lens, new_tokens, free
 
 
 def surelock_paged_truncate(page_table, page_size: int, seq_lens, keep, free_pages, n_free, seq_lens_out=None, n_free_out=None,
-                            dev_status=None):
-    """Sequence b cut to min(seq_lens[b], keep[b]) tokens, its pages back onto the free list (free_pages, n_free: in place)."""
+                            dev_status=None, n_pages=None):
+    """Sequence b cut to min(seq_lens[b], keep[b]) tokens, its pages back onto the free list (free_pages, n_free: in place); n_pages as
+    in surelock_paged_extend."""
     dev = page_table.get_device()
     stream = _stream_of(dev)
     B, width = _table(page_table)
-    n_pages = free_pages.numel()
+    n_pages = free_pages.numel() if n_pages is None else n_pages
     table, lens, kept, lens_out, free, n, n_out, status = _ptrs(
-        dev, torch.int32, page_table, B * width, seq_lens, B, keep, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, 1, n_free, 1,
+        dev, torch.int32, page_table, B * width, seq_lens, B, keep, B, seq_lens if seq_lens_out is None else seq_lens_out, B, free_pages, max(n_pages, 1), n_free, 1,
         n_free if n_free_out is None else n_free_out, 1, dev_status, 1)
     if B == 0:
         if n_free_out is not None:
