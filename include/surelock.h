@@ -525,7 +525,7 @@ int surelock_attention_paged(const surelock_paged_kv *cache, const void *q, int6
  * wanted up to and with it are more than *n_free.
  *   page_table    dev int32 [B][max_pages], in place: only the new pages are written
  *   seq_lens      dev int32 [B], seq_lens_out dev int32 [B]: lengths before and with the new tokens; may be the same array
- *   free_pages    dev int32 [n_pages], read only; n_free, n_free_out dev int32 [1]: pages on the list before and after; may be the same
+ *   free_pages    dev int32 [n_pages], a place for every page of the pool, read only; n_free, n_free_out dev int32 [1]: pages on the list before and after; may be the same
  *   row_offsets   dev int32 [B + 1], n_active dev int32 [1]: the packing of the tokens that were granted
  *   active_idx    dev int32 [max_rows]: flat positions b*N + i of the rows, N = max_pages * page_size, as surelock_kv_scatter_paged
  *                 takes them; entries behind *n_active are left as they are
@@ -604,6 +604,7 @@ typedef struct {
  * x, a, b 16-byte aligned (SL_EUNSUPPORTED otherwise); any n_out, c_stride and alignment of C to its elements.  A_a x is summed in fp32 and
  * enters the second product as an fp32 number; C is rounded once (fp32 sums below 2^-126 may become 0).  Infinities and NaN in x, a and b go through
  * the sums as they do in fp32 (in b: where |scale A_a x| is 0 or at least 2^-108; below, an infinity may become NaN).
+ * C does not overlap x.  Offsets that are not ascending may give a row to several sequences, whose sum is undefined then.
  * dev_status may be NULL; 2 = a bounded wait ran out, and the rows that this concerns are NaN.  Deterministic; no workspace; one launch;
  * asynchronous on `stream`. */
 int surelock_gemm_adapters(const void *x, const surelock_adapters *adapters, const int32_t *adapter_of_seq, const int32_t *row_offsets, int B,
@@ -631,7 +632,8 @@ typedef struct {
  *   token      dev int32 [M];  conf dev fp32 [M] or NULL: softmax(logits[r])[token], temperature 1 and unfiltered, the
  *              confidence that surelock_update_mask orders by;  n_kept dev int32 [M] or NULL: the length of the prefix
  * A row with a NaN or +inf, with nothing but -inf, or with an undefined setting gives token -1, conf NaN, n_kept 0; so does a set out
- * of range (device status 4).  Sums are held in 64 bits: the result does not depend on how rows are split, up to 2^-50 of the sum.
+ * of range (device status 4).  Sums are held in 64 bits, up to 2^-50 of themselves; rows of SL_FP32, and of SL_BF16 with a finite value other than 0
+ * below 2^-28 or from 2^12 on, sum weights rounded to 2^-54 of the largest, exactly, and take longer: forbid tokens by -inf.
  * vocab <= 2^20 - 128 (SL_EUNSUPPORTED otherwise), any row_stride >= vocab.  Deterministic; no workspace; one launch;
  * asynchronous on `stream`. */
 int surelock_sample(const void *logits, int64_t row_stride, const surelock_sampling *sampling, const int32_t *set_of_row, const float *u,

@@ -11,9 +11,9 @@
 // the second product as three bf16 terms, all of its 24 bits.
 //
 // Bounded by latency for one row (6.4 us in a graph, K = n_out = 4096, rank 16: finding the sequence 1.2, each product about 1, joining t 1.2 us) and by
-// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 29 us for 74 MB; of rank 16: 16.5 us): 16 warps of 128
-// registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of the SMs' CTAs allows (two rounds, of two
-// CTAs to an SM: 41 and 22.5 us; of one, 64 rows of rank 128 with n_out = 4096: 39 instead of 34 us).
+// round trips to the L2 for many adapters (64 rows of 48 adapters of rank 64, 4096 x 12288: 29 us for 74 MB, of 64: 31; of rank 16: 16.5 us): 16 warps of
+// 128 registers to an SM, with the next 32 features' operands on their way.  Clusters as large as one round of the SMs' CTAs allows (two rounds, 64 adapters
+// of rank 64, 32, 16: 35, 24.5, 20.5 instead of 31, 20.5, 16.5 us; of rank 128 with n_out = 4096: 41 instead of 35 us).
 #include "gemm_adapters.cuh"
 
 namespace sl {
@@ -38,7 +38,8 @@ __device__ __forceinline__ uint32_t only(uint32_t two, int k, int rank) {
 
 template <int NT, typename CT> struct AdapterTile {
   // times 32 features of weights and C in registers: as many as leave 128 registers to a thread and so two CTAs to an SM.  64 rows, n_out = 12288, with
-  // one CTA: rank 32 33 instead of 20.5 us, fp32 C 37 instead of 22.5, rank 16 with fp32 C 25 instead of 16.5.  More than 64 ranks take 252 registers.
+  // twice as many and one CTA: rank 64 41 instead of 31 us, 32 26.5 instead of 20.5 with either C, 16 with fp32 C 22.5 instead of 16.5.  More than 64 ranks
+  // take 252 registers.
   static constexpr bool FP32 = sizeof(CT) == 4;
   static constexpr int AHEAD = NT > 4 ? 1 : NT == 4 ? (FP32 ? 1 : 2) : (FP32 ? 2 : 3);
   static constexpr int CTAS = NT <= 8 ? 2 : 1;
@@ -272,8 +273,8 @@ __global__ void __launch_bounds__(AD_THREADS, AdapterTile<NT, CT>::CTAS) gemm_ad
 template <int NT, typename CT>
 int launch_tile(const AdapterArgs& a, int groups, cudaStream_t st) {
   using L = AdapterTile<NT, CT>;
-  // As large as one round allows, where half of the sequences of 16 rows and more are taken to end in whole tiles (8 x 64 rows of rank 128: 23 us, by the
-  // bound alone 29)
+  // As large as one round allows, where half of the sequences of 16 rows and more are taken to end in whole tiles (16 x 24 rows of rank 128: 24.5 us, by
+  // the bound alone 37)
   const int likely = groups - (a.max_rows >= 16ll * a.B ? a.B / 2 : 0);
   int CL = AD_CLUSTER;
   while (CL > 1 && (long long)likely * CL > (long long)L::CTAS * sm_count()) CL >>= 1;
@@ -314,10 +315,11 @@ int launch_gemm_adapters(const void* A, const surelock_adapters& w, const int32_
   AdapterArgs a = {(const bf16*)A, (const bf16*)w.a, (const bf16*)w.b, w.scale, w.ranks, adapter_of_seq, row_offsets, C, status,
                          c_stride, w.n_adapters, w.max_rank, B, max_rows, n_out, K, 0};
   // The kernel for many rows takes 128 of a sequence at a time and 19 us at least; this one's time grows with rows x rank.  K = n_out = 4096, bf16, few
-  // / many, us: 1 x 512 rows of rank 64 16.5 / 20.6, of rank 128 23 / 26; 1 x 1536 of rank 64 29 / 21; 8 x 64 rows of rank 64 16.5 / 25, of rank 128 23 /
-  // 29; 8 x 128 rows of rank 16 12 / 19, 64 21 / 21, 128 33 / 27; 8 x 512 of rank 16 25 / 23, fp32 35 / 27; 32 x 64 of rank 64 30 / 31, fp32 35 / 29, of rank
-  // 128 62 / 51.  So the border costs up to 6 us at a few dozen rows of the highest ranks, and would cost 8 at many rows of low ones if it were
-  // twice as high.  (Its copies count the pool's rows in 32 bits.)
+  // / many, us: 1 x 512 rows of rank 64 16.5 / 20.5, of rank 128 25 / 29; 1 x 1536 of rank 64 32 / 22.5; 8 x 64 rows of rank 64 16.5 / 25, of rank 128 24.5 /
+  // 32.5; 8 x 128 rows of rank 16 12.5 / 20.5, 64 20.5 / 22.5, 128 37 / 29; 8 x 512 of rank 16 27 / 23.5, fp32 34.5 / 27; 32 x 64 of rank 64 33 / 31, fp32 35 /
+  // 30, of rank 128 70 / 53.  So the border costs up to 8 us at a few hundred rows of the highest ranks (they lie just above it: 1 x 512 and 8 x 64 rows of
+  // rank 128, where this kernel would be the faster one), and would cost as much at many rows of low ranks if it were twice as high.  (Its copies count the
+  // pool's rows in 32 bits.)
   const bool many = max_rows >= 64ll * B && (long long)max_rows * w.max_rank >= 49152;
   if (many && (long long)w.n_adapters * (n_out > w.max_rank ? n_out : w.max_rank) < 0x7fffff00ll) {
     a.lost = take_lost_copy();

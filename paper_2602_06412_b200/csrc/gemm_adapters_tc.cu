@@ -3,12 +3,14 @@
 // A cluster of CL CTAs takes 128 rows of one sequence.  Each CTA multiplies its share of K,  t = x A_a^T  (128 x rank, accumulated in tensor
 // memory; x and A_a by TMA in 64 k at a time); the shares meet through distributed shared memory in a fixed order; t scale becomes the
 // tensor-memory operand of the second product as three bf16 terms, all 24 bits of it; and each CTA adds  t B_a^T  to its share
-// of the features, 64 at a time, C read ahead into registers while they are multiplied.
+// of the features, 64 at a time.  Whole tiles of a bf16 C come with the weights, in the ring's slots, are added to there and copied back; those of an fp32 C
+// are added to by reductions of the L2, which the SM does not read.  A sequence's last rows, or a C off 16 bytes, are read when their product is there.
 //
 // Bound by x once and C twice (rank operations per byte are few for the tensor cores).  In a graph, K = n_out = 4096: 9216 rows of 8 ragged sequences, rank
-// 32, fp32 C 95 us (378 MB; phase by phase 5 TB/s for x, 6.2 for C, 7 us between them to find the tile and join t), 12288 rows of rank 64, bf16 C 76 us (4.0
-// TB/s), of rank 128, fp32 143 us.  C moves in whole tiles because a bulk copy takes some 16 clocks however short it is (a row of 128 bytes at
-// a time: 118 instead of 77 us; through registers, row by row of lanes: 240); only a sequence's last rows go by themselves.
+// 32, fp32 C 96 - 98 us for 378 MB.  Stamps of that run: 225 CTAs in clusters of 3 lie on 142 SMs, 166 of them two to an SM; the tile is found at 2 us, x read
+// by 18 (6 TB/s), t joined by 23, and the features take 28 us where a CTA has its SM alone and 54 where two share one, so that the former end at 51 -
+// 58 us and the latter at 78 - 92.  12288 rows of rank 64, bf16 C 80 us (3.9 TB/s), of rank 128, fp32 145 us.  C moves in whole tiles because a bulk copy
+// takes some 16 clocks however short it is (a row of 128 bytes at a time: 118 instead of 77 us; through registers, row by row of lanes: 240).
 #include "gemm_adapters.cuh"
 
 namespace sl {

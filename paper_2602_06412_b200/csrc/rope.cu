@@ -10,7 +10,8 @@
 //
 // Memory-bound: 16-byte accesses of either half of V pairs, 4 heads in flight to a thread.  In a graph, 64 heads of 128 in bf16: 12288 rows
 // 63.5 us (6.3 TB/s, 97 % of the copy rate; sines read from shared memory for every head instead: 120 us, two thirds of it bank conflicts and
-// registers), 4 rows to a block (2: 69, 8: 66 us), 4 heads in flight (2: 66, 8: 65.5); 32 rows at positions up to 10^6 4.2 us.
+// registers), 4 rows to a block (2: 69, 8: 66 us), 4 heads in flight (2: 66, 8: 65.5); 32 rows at positions up to 10^6 4.2 us.  Neighbours as pairs 75.5 us (a
+// thread's two loads lie side by side, so a warp's are apart); fp32 125 us for 805 MB, neighbours 136.5 (that variant spills 60 bytes).
 #include "common.cuh"
 
 namespace sl {

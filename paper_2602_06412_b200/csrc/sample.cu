@@ -7,13 +7,16 @@
 // the token drawn is the first one of the shortest prefix whose running sum of weights exceeds u times the prefix's.  So nothing
 // needs sorting: all that is asked of the row is "which token has rank n" and "at which token does the running sum reach s", and
 // both are answered by sums over values.  Sums are held in 64 bits: with 100000 tokens in the prefix, 32 would draw a neighbour of
-// the right token in one row of a hundred.
+// the right token in one row of a hundred.  (In the bins of the second method below a weight is a whole number of units of 2^-54 of the largest, so each
+// token is off by half a unit there; min-p looks at the weight itself.)
 //
 // bf16 rows (WindowSums): a bf16 number is its own histogram bin.  One pass counts the row's values in shared memory, 5120 bins
 // to a sign for magnitudes in [2^-28, 2^12), which leaves the sums to the few thousand distinct values: one exponential each instead of
 // one per token, and a sum is exact but for 2^-53 roundings.  The occupied range of bins is then walked in order, a few bins to
 // a thread.  The token's index is found by a second pass that counts the tokens of the value that was drawn, out of the L2.  A row with a
-// finite value outside the window (not zero) is done by the other method.
+// finite value outside the window (not zero) is done by the other method, after it has been counted in vain: tokens forbidden by a large finite number instead
+// of -inf cost that (a third of 126464 at -1e4 or the type's lowest value, top-p: 1 row 53 instead of 21 us, 33 rows 111 instead of 27, 1536 rows 1304 instead
+// of 207).
 //
 // fp32 rows (BinnedSums): 2048 bins of equal width over the values that weigh anything.  One pass adds every token's weight, as four limbs of
 // a fixed-point number (exact sums in any order), to its bin; a bin that is asked for is opened by another pass over the row's tokens
@@ -21,10 +24,10 @@
 //
 // A row is one CTA's work, or with few rows that of a cluster of CTAs, whose shares meet through distributed shared memory.
 //
-// Bounds, and what it measured in a graph: one bf16 row of 126464 tokens with top-k and top-p 21 us (latency: counting 8.5 k cycles, sums over the
-// cluster 5 k, three finds of 3 to 4 k, meeting the token 4.5 k), 33 fp32 rows of 32003 with all filters 41 us (each find has three cluster barriers and
+// Bounds, and what it measured in a graph: one bf16 row of 126464 tokens with top-k and top-p 21 - 22 us (latency: counting 8.5 k cycles, sums over the
+// cluster 5 k, three finds of 3 to 4 k, meeting the token 4.5 k), 33 fp32 rows of 32003 with all filters 41 - 42 us (each find has three cluster barriers and
 // a pass over the row), 1536 bf16 rows with top-p 185 us for 388 MB: the counts' atomics meet in a bank 3.4 at a time, 80 us, and what follows
-// the counting overlaps another CTA's only in part.  (A search for the k largest and a sort of 126464 numbers per row take 20 ms.)
+// the counting overlaps another CTA's only in part; a temperature other than 1 adds an exponential to each value that occurs, for conf, 15 us more.  (A search for the k largest and a sort of 126464 numbers per row take 20 ms.)
 #include "tc_common.cuh"
 
 namespace sl {
@@ -1146,10 +1149,12 @@ int launch_sample_ctas(const SampleArgs& a, cudaStream_t st) {
 }
 
 template <typename T> int launch_sample_typed(const SampleArgs& a, cudaStream_t st) {
-  // A cluster shortens a row's passes and pays for its barriers and for the histograms' way through distributed shared memory.  Rows of 126464, us
-  // with 1 / 2 / 4 / 8 CTAs, bf16: 1 row 25 / 26 / 21 / 21, 18 rows 33 / 27 / 23 / 27, 37: 32 / 27 / 27 / 45, 74: 33 / 29 / 43 / 70, 148: 33 / 37 / 65 /
-  // 119; fp32: 1 row 193 / 120 / 76 / 55, 18 rows 212 / 123 / 79 / 70, 37: 213 / 127 / 97 / 121, 148: 213 / 166 / 250 / 329, 296: 347 / 331 / 436 / 617.
-  // So many CTAs while each has an SM and more to itself, two up to about one CTA (fp32: two) per SM.
+  // A cluster shortens a row's passes and pays for its barriers and for the histograms' way through distributed shared memory.  Rows of 126464, T 0.8, top-k
+  // 50 and top-p 0.95, us with 1 / 2 / 4 / 8 CTAs, bf16: 1 row 27 / 27 / 23 / 23, 18 rows 33 / 27 / 23 / 29, 37: 33 / 29 / 29 / 45, 74: 33 / 29 / 45 / 72,
+  // 148: 33 / 39 / 68 / 123; fp32: 1 row 206 / 127 / 78 / 58, 18 rows 224 / 129 / 81 / 73, 37: 225 / 133 / 103 / 125, 148: 226 / 178 / 263 / 342, 296: 372 / 355 /
+  // 457 / 639.  Rows of 32000, bf16: 1 row 21 / 19 / 20 / 23, 37: 21 / 21 / 25 / 43, 148: 21 / 27 / 57 / 112; fp32: 1 row 70 / 49 / 39 / 40, 18: 73 / 51 / 41 /
+  // 47, 37: 72 / 52 / 48 / 82, 148: 74 / 68 / 127 / 219, 296: 98 / 128 / 216 / 403.  So many CTAs while each has an SM and more to itself, two up to about one
+  // CTA (fp32: two) per SM, and 4096 tokens to a CTA at least (8 of them for one row of 32000: 2 us more in bf16 than with 4, 1 in fp32).
   const long long room = (long long)sm_count() * (sizeof(T) == 2 ? 1 : 2);
   int ctas = 8;
   while (ctas > 1 && ((long long)a.max_rows * ctas > (ctas == 2 ? room : room / 2) || a.vocab < ctas * 4096)) ctas >>= 1;
